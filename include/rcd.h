@@ -68,7 +68,8 @@ typedef enum {
     RCD_ERR_BAD_SIMILARITY = 7 /* a similarity outside [0, 1] (or NaN) was found in a caller-supplied S */
 } rcd_status;
 
-typedef enum { RCD_F32 = 0, RCD_BF16 = 1 } rcd_dtype;
+/* RCD_MXFP8: 8-bit elements with scales, for the encoder's operators below alone (RCD_ERR_UNSUPPORTED elsewhere) */
+typedef enum { RCD_F32 = 0, RCD_BF16 = 1, RCD_MXFP8 = 2 } rcd_dtype;
 
 typedef enum {
     RCD_MODE_AUTO = 0,     /* RCD_MODE_INCREMENTAL if the workspace can hold at least one class's S, else
@@ -311,6 +312,120 @@ void rcd_last_stats(int64_t *out8_host);
  */
 void rcd_profile(int enable);
 void rcd_profile_read(double *out8_host);
+
+/* ------------------------------------------------------------------------------------------------------------------------
+ * Operators of the feature encoder: what turns a sample's hidden state into the feature row that rcd_similarity and the
+ * partition calls take (the paper's features are the bottleneck of a residual auto-encoder).  A layer of it is
+ *     y = rms_norm(x + r) -> gated block -> product with the residual in its epilogue.
+ *
+ * Common to all of them
+ *   - dt is RCD_F32 or RCD_BF16 for every matrix of a call that is not said to be something else.  Sums, statistics and
+ *     products are accumulated in fp32 (or more) whatever dt is, and every output is rounded once, when it is stored.
+ *     Products of RCD_F32 operands are exact to fp32: a factor goes to the matrix cores as three bf16 pieces that add up
+ *     to it.
+ *   - RCD_MXFP8 (where an entry point lists it): elements are e4m3 bytes, and each block of 32 consecutive elements of a
+ *     row (the last one may be shorter) shares a scale 2^(s - 127), s one byte; s = 255 means NaN.  Element i of a row
+ *     stands for e4m3(byte i) * 2^(s[i / 32] - 127).  Scales are a byte matrix of their own, rows x ceil(d / 32), with a
+ *     leading dimension in bytes.
+ *   - Asynchronous on `stream`; nothing is allocated, no host wait; calls can be captured into a graph.
+ *   - Outputs may not overlap inputs, workspace or each other, except where an entry point says so.  Elements of an
+ *     output's rows beyond its columns (a leading dimension larger than the columns) are left alone.
+ *   - Zero rows (rows = 0, M = 0) are legal: nothing is read, gradients of weights come out as zero.  Every other extent
+ *     is at least 1 and at most 2^31 - 256, products of extents may pass 2^31.
+ *   - NaN and infinities travel as the formulas say, also in RCD_F32 products.
+ */
+
+typedef enum { RCD_ACT_NONE = 0, RCD_ACT_RELU = 1, RCD_ACT_SILU = 2, RCD_ACT_GELU = 3 } rcd_act;
+/* relu max(z, 0) with slope 0 at 0; silu z / (1 + e^-z); gelu z * Phi(z), Phi the normal distribution (not its tanh form) */
+
+/*
+ * Root-mean-square norm with the residual's addition:
+ *     h = x + residual (h = x without one),  rstd = (mean_i h_i^2 + eps)^(-1/2),  y_i = h_i * rstd * weight_i
+ * per row of X (rows x d).  The norm is of the unrounded fp32 sum.
+ *   residual_dev, weight_dev (d elements of dt) may be null; eps >= 0
+ *   sum_dev (nullable)   h, rounded to dt: the residual stream from here on
+ *   Y_dev                out_dt is dt, or RCD_MXFP8 with scale_dev (rows x ceil(d / 32) bytes): the least power of two
+ *                        with every |y| of the block <= 448 * 2^e, e >= -127; elements rounded to nearest, ties to even.
+ *                        A block with an infinity or a NaN gets NaN codes there; the scale comes from its finite values.
+ *   rstd_dev (nullable)  float[rows], what the backward call takes
+ * sum_dev and Y_dev (in dt) may each be X_dev or residual_dev with the same leading dimension (not both the same).
+ */
+int rcd_rms_norm(const void *X_dev, int dt, int64_t rows, int64_t d, int64_t ld_x, const void *residual_dev, int64_t ld_r,
+                 const void *weight_dev, float eps, void *sum_dev, int64_t ld_s, void *Y_dev, int out_dt, int64_t ld_y,
+                 uint8_t *scale_dev, int64_t ld_scale, float *rstd_dev, void *stream);
+
+/*
+ * Its gradients.  With H = h as stored by the forward call (X itself without a residual), xh = h * rstd, g = dy * weight:
+ *     dx_i = rstd * (g_i - xh_i * mean_j(g_j xh_j)) + dsum_i,      dweight_i = sum over rows of dy_i * xh_i
+ * dx is the gradient of x and of the residual alike.  dsum_dev (nullable): the gradient that reaches h along the residual
+ * stream; dX_dev may be dY_dev or dsum_dev (same leading dimension).  dweight_dev (nullable): d elements of dt, summed in a fixed order.
+ * workspace: rcd_rms_norm_backward_workspace_bytes(rows, d) bytes (none needed without dweight_dev).
+ */
+int rcd_rms_norm_backward(const void *dY_dev, int dt, int64_t rows, int64_t d, int64_t ld_dy, const void *H_dev, int64_t ld_h,
+                          const float *rstd_dev, const void *weight_dev, const void *dsum_dev, int64_t ld_ds,
+                          void *dX_dev, int64_t ld_dx, void *dweight_dev,
+                          void *workspace_dev, size_t workspace_bytes, void *stream);
+size_t rcd_rms_norm_backward_workspace_bytes(int64_t rows, int64_t d);
+
+/* Rows in 8 bits with scales, by the rule of rcd_rms_norm's RCD_MXFP8 output (weights are laid out with it once). */
+int rcd_quantize_mxfp8(const void *X_dev, int dt, int64_t rows, int64_t d, int64_t ld_x, uint8_t *Q_dev, int64_t ld_q,
+                       uint8_t *scale_dev, int64_t ld_scale, void *stream);
+
+/*
+ * Matrix product with bias, activation and residual in its epilogue:
+ *     z = A W^T + bias,      y = act(z) + residual             A: M x K, W: N x K, y: M x N
+ *   dt RCD_F32 or RCD_BF16 with out_dt = dt, or bf16 operands with out_dt RCD_F32, or RCD_MXFP8 (A_scale_dev, W_scale_dev
+ *   given, else ignored) with out_dt RCD_BF16 or RCD_F32; bias_dev (N) and residual_dev (M x N) are of out_dt and may be null.
+ *   preact_dev (nullable): z in fp32, M x N, what the backward call takes.  Y_dev may be residual_dev (same leading dimension).
+ * workspace: rcd_linear_workspace_bytes(M, N, K, dt) bytes.
+ */
+int rcd_linear(const void *A_dev, const uint8_t *A_scale_dev, int64_t ld_a, int64_t ld_a_scale,
+               const void *W_dev, const uint8_t *W_scale_dev, int64_t ld_w, int64_t ld_w_scale, int dt, int out_dt,
+               int64_t M, int64_t N, int64_t K, const void *bias_dev, int act, const void *residual_dev, int64_t ld_r,
+               float *preact_dev, int64_t ld_p, void *Y_dev, int64_t ld_y,
+               void *workspace_dev, size_t workspace_bytes, void *stream);
+size_t rcd_linear_workspace_bytes(int64_t M, int64_t N, int64_t K, int dt);
+
+/*
+ * Its gradients (dt RCD_F32 or RCD_BF16; the residual's gradient is dY itself), dz = dy * act'(z):
+ *     dA = dz W,   dW = dz^T A,   dbias = sum over rows of dz
+ * Each of dA_dev, dW_dev, dbias_dev may be null.  preact_dev: z of the forward call (not read for RCD_ACT_NONE).
+ * dz is rounded to bf16 before its products for RCD_BF16 (they are matrix-core products; dbias sums the unrounded dz).
+ * workspace: rcd_linear_backward_workspace_bytes(M, N, K, dt) bytes.
+ */
+int rcd_linear_backward(const void *dY_dev, int64_t ld_dy, const void *A_dev, int64_t ld_a, const void *W_dev, int64_t ld_w,
+                        int dt, int64_t M, int64_t N, int64_t K, const float *preact_dev, int64_t ld_p, int act,
+                        void *dA_dev, int64_t ld_da, void *dW_dev, int64_t ld_dw, void *dbias_dev,
+                        void *workspace_dev, size_t workspace_bytes, void *stream);
+size_t rcd_linear_backward_workspace_bytes(int64_t M, int64_t N, int64_t K, int dt);
+
+/*
+ * Gated block: both projections, the activation and the product,
+ *     g = A Wg^T,  u = A Wu^T,  h = act(g) * u                 A: M x K, Wg and Wu: F x K, h: M x F
+ * Types as for rcd_linear.  saved_dev (nullable): float[2 M F], what the backward call takes: g and u of row m side by
+ * side at saved[2 (m F + f)].
+ * workspace: rcd_gated_linear_workspace_bytes(M, F, K, dt) bytes.
+ */
+int rcd_gated_linear(const void *A_dev, const uint8_t *A_scale_dev, int64_t ld_a, int64_t ld_a_scale,
+                     const void *Wg_dev, const uint8_t *Wg_scale_dev, int64_t ld_wg, int64_t ld_wg_scale,
+                     const void *Wu_dev, const uint8_t *Wu_scale_dev, int64_t ld_wu, int64_t ld_wu_scale,
+                     int dt, int out_dt, int64_t M, int64_t F, int64_t K, int act, float *saved_dev,
+                     void *H_dev, int64_t ld_h, void *workspace_dev, size_t workspace_bytes, void *stream);
+size_t rcd_gated_linear_workspace_bytes(int64_t M, int64_t F, int64_t K, int dt);
+
+/*
+ * Its gradients (dt RCD_F32 or RCD_BF16), dg = dh * u * act'(g), du = dh * act(g):
+ *     dA = dg Wg + du Wu,   dWg = dg^T A,   dWu = du^T A
+ * dA_dev may be null, and so may dWg_dev and dWu_dev, together.  dg and du are rounded to bf16 before their products for
+ * RCD_BF16.
+ * workspace: rcd_gated_linear_backward_workspace_bytes(M, F, K, dt) bytes.
+ */
+int rcd_gated_linear_backward(const void *dH_dev, int64_t ld_dh, const void *A_dev, int64_t ld_a,
+                              const void *Wg_dev, int64_t ld_wg, const void *Wu_dev, int64_t ld_wu,
+                              int dt, int64_t M, int64_t F, int64_t K, const float *saved_dev, int act,
+                              void *dA_dev, int64_t ld_da, void *dWg_dev, int64_t ld_dwg, void *dWu_dev, int64_t ld_dwu,
+                              void *workspace_dev, size_t workspace_bytes, void *stream);
+size_t rcd_gated_linear_backward_workspace_bytes(int64_t M, int64_t F, int64_t K, int dt);
 
 #ifdef __cplusplus
 }

@@ -1,5 +1,6 @@
 """MI355X (gfx950) implementation of the ratio-constrained submodular partitioner
-of RCD-SGD (arXiv 2211.00839, Algorithm 1): thin Python binding over librcd.so.
+of RCD-SGD (arXiv 2211.00839, Algorithm 1), and operators of the encoder its features come from: thin Python binding
+over librcd.so.
 
 Every function only marshals torch device tensors into the C ABI declared in
 ``include/rcd.h``; all arithmetic of the method runs in the library's HIP
@@ -30,9 +31,20 @@ from .binding import (  # noqa: F401
     worker_shards,
     workspace_bytes,
 )
+from .encoder import (  # noqa: F401
+    RmsNorm,
+    gated_linear,
+    gated_linear_backward,
+    linear,
+    linear_backward,
+    quantize_mxfp8,
+    rms_norm,
+    rms_norm_backward,
+)
 
 F32 = 0
 BF16 = 1
+MXFP8 = 2
 MODE_AUTO = 0
 MODE_STORED = 1
 MODE_RECOMPUTE = 2

@@ -20,6 +20,10 @@ EXPORTS = [
     "rcd_dataset_workspace_bytes", "rcd_strerror", "rcd_last_hip_error", "rcd_last_stats",
     "rcd_profile", "rcd_profile_read", "rcd_partition_class_mode", "rcd_workspace_bytes", "rcd_init", "rcd_release",
     "rcd_similarity_static",
+    "rcd_rms_norm", "rcd_rms_norm_backward", "rcd_rms_norm_backward_workspace_bytes", "rcd_quantize_mxfp8",
+    "rcd_linear", "rcd_linear_workspace_bytes", "rcd_linear_backward", "rcd_linear_backward_workspace_bytes",
+    "rcd_gated_linear", "rcd_gated_linear_workspace_bytes", "rcd_gated_linear_backward",
+    "rcd_gated_linear_backward_workspace_bytes",
 ]
 
 
@@ -96,6 +100,30 @@ def load_library():
     lib.rcd_release.argtypes = []
     lib.rcd_similarity_static.restype = i32
     lib.rcd_similarity_static.argtypes = [vp, i32, i64, i64, i64, vp, f32, vp, i64, vp]
+    lib.rcd_rms_norm.restype = i32
+    lib.rcd_rms_norm.argtypes = [vp, i32, i64, i64, i64, vp, i64, vp, f32, vp, i64, vp, i32, i64, vp, i64, vp, vp]
+    lib.rcd_rms_norm_backward.restype = i32
+    lib.rcd_rms_norm_backward.argtypes = [vp, i32, i64, i64, i64, vp, i64, vp, vp, vp, i64, vp, i64, vp, vp, sz, vp]
+    lib.rcd_rms_norm_backward_workspace_bytes.restype = sz
+    lib.rcd_rms_norm_backward_workspace_bytes.argtypes = [i64, i64]
+    lib.rcd_quantize_mxfp8.restype = i32
+    lib.rcd_quantize_mxfp8.argtypes = [vp, i32, i64, i64, i64, vp, i64, vp, i64, vp]
+    lib.rcd_linear.restype = i32
+    lib.rcd_linear.argtypes = [vp, vp, i64, i64, vp, vp, i64, i64, i32, i32, i64, i64, i64, vp, i32, vp, i64, vp, i64, vp, i64,
+                               vp, sz, vp]
+    lib.rcd_linear_backward.restype = i32
+    lib.rcd_linear_backward.argtypes = [vp, i64, vp, i64, vp, i64, i32, i64, i64, i64, vp, i64, i32, vp, i64, vp, i64, vp,
+                                        vp, sz, vp]
+    lib.rcd_gated_linear.restype = i32
+    lib.rcd_gated_linear.argtypes = [vp, vp, i64, i64, vp, vp, i64, i64, vp, vp, i64, i64, i32, i32, i64, i64, i64, i32, vp,
+                                     vp, i64, vp, sz, vp]
+    lib.rcd_gated_linear_backward.restype = i32
+    lib.rcd_gated_linear_backward.argtypes = [vp, i64, vp, i64, vp, i64, vp, i64, i32, i64, i64, i64, vp, i32, vp, i64, vp, i64,
+                                              vp, i64, vp, sz, vp]
+    for name in ("rcd_linear", "rcd_linear_backward", "rcd_gated_linear", "rcd_gated_linear_backward"):
+        query = getattr(lib, name + "_workspace_bytes")
+        query.restype = sz
+        query.argtypes = [i64, i64, i64, i32]
     _lib = lib
     return lib
 

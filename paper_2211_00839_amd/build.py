@@ -13,7 +13,7 @@ CSRC = os.path.join(HERE, "csrc")
 LIB = os.path.join(HERE, "librcd.so")
 
 HIPCC_FLAGS = [
-    "-O3", "-std=c++17", "--offload-arch=gfx950", "-shared", "-fPIC",
+    "-O3", "-std=c++17", "--offload-arch=gfx950", "-fPIC",
     # compiler-generated packed fp32 ops are kept out of every kernel
     "-Xclang", "-target-feature", "-Xclang", "-packed-fp32-ops",
     # no multiply and add is fused behind the source's back: every fused multiply-add in the kernels is
@@ -23,21 +23,41 @@ HIPCC_FLAGS = [
 ]
 
 
+# one object each, compiled side by side
+SOURCES = ["rcd_lib.hip", "encoder_lib.hip"]
+
+
 def build(verbose: bool = False) -> str:
     hipcc = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
-    tmp = LIB + ".tmp.%d" % os.getpid()
-    cmd = [hipcc] + HIPCC_FLAGS + [os.path.join(CSRC, "rcd_lib.hip"), "-o", tmp]
-    if verbose:
-        print(" ".join(cmd), flush=True)
-    res = subprocess.run(cmd, stdout=subprocess.PIPE, stderr=subprocess.STDOUT, text=True)
-    out = "\n".join(l for l in res.stdout.splitlines() if "packed-fp32-ops" not in l)
-    if res.returncode != 0:
-        if os.path.exists(tmp):
-            os.remove(tmp)
-        raise RuntimeError("hipcc failed:\n" + out)
-    if verbose and out.strip():
-        print(out)
-    os.replace(tmp, LIB)
+    suffix = ".tmp.%d" % os.getpid()
+    tmp = LIB + suffix
+    objects = [os.path.join(HERE, src.replace(".hip", ".o")) + suffix for src in SOURCES]
+    try:
+        jobs = []
+        for src, obj in zip(SOURCES, objects):
+            cmd = [hipcc] + HIPCC_FLAGS + ["-c", os.path.join(CSRC, src), "-o", obj]
+            if verbose:
+                print(" ".join(cmd), flush=True)
+            jobs.append(subprocess.Popen(cmd, stdout=subprocess.PIPE, stderr=subprocess.STDOUT, text=True))
+        said = [job.communicate()[0] for job in jobs]
+        failed = any(job.returncode != 0 for job in jobs)
+        if not failed:
+            cmd = [hipcc, "--offload-arch=gfx950", "-shared", "-fPIC"] + objects + ["-o", tmp]
+            if verbose:
+                print(" ".join(cmd), flush=True)
+            res = subprocess.run(cmd, stdout=subprocess.PIPE, stderr=subprocess.STDOUT, text=True)
+            said.append(res.stdout)
+            failed = res.returncode != 0
+        out = "\n".join(l for l in "".join(said).splitlines() if "packed-fp32-ops" not in l)
+        if failed:
+            raise RuntimeError("hipcc failed:\n" + out)
+        if verbose and out.strip():
+            print(out)
+        os.replace(tmp, LIB)
+    finally:
+        for path in objects + [tmp]:
+            if os.path.exists(path):
+                os.remove(path)
     return LIB
 
 

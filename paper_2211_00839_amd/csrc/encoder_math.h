@@ -1,0 +1,123 @@
+// Element types, activations and the 8-bit block format of the feature encoder's kernels.
+#pragma once
+#include <hip/hip_runtime.h>
+#include <stdint.h>
+
+namespace enc {
+
+typedef float f32x16 __attribute__((ext_vector_type(16)));
+typedef float f32x4 __attribute__((ext_vector_type(4)));
+typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
+typedef int i32x8 __attribute__((ext_vector_type(8)));
+
+constexpr int MX_BLOCK = 32;     // elements that share a scale
+
+__device__ __forceinline__ float to_f32(float v) { return v; }
+__device__ __forceinline__ float to_f32(__bf16 v) { return (float)v; }
+
+// 8 consecutive elements of a row as fp32; `count` of them exist, the others come out as 0.  vec: 16-byte loads are
+// allowed for a full group.
+template <typename T>
+__device__ __forceinline__ void load8(const T *__restrict__ p, int count, bool vec, float (&v)[8])
+{
+    if (vec && count >= 8) {
+        if constexpr (sizeof(T) == 4) {
+            const float4 a = reinterpret_cast<const float4 *>(p)[0], b = reinterpret_cast<const float4 *>(p)[1];
+            v[0] = a.x; v[1] = a.y; v[2] = a.z; v[3] = a.w;
+            v[4] = b.x; v[5] = b.y; v[6] = b.z; v[7] = b.w;
+        } else {
+            const bf16x8 a = *reinterpret_cast<const bf16x8 *>(p);
+#pragma unroll
+            for (int i = 0; i < 8; ++i) v[i] = (float)a[i];
+        }
+        return;
+    }
+#pragma unroll
+    for (int i = 0; i < 8; ++i) v[i] = i < count ? to_f32(p[i]) : 0.f;
+}
+
+template <typename T>
+__device__ __forceinline__ void store8(T *__restrict__ p, int count, bool vec, const float (&v)[8])
+{
+    if (vec && count >= 8) {
+        if constexpr (sizeof(T) == 4) {
+            reinterpret_cast<float4 *>(p)[0] = make_float4(v[0], v[1], v[2], v[3]);
+            reinterpret_cast<float4 *>(p)[1] = make_float4(v[4], v[5], v[6], v[7]);
+        } else {
+            bf16x8 a;
+#pragma unroll
+            for (int i = 0; i < 8; ++i) a[i] = (__bf16)v[i];
+            *reinterpret_cast<bf16x8 *>(p) = a;
+        }
+        return;
+    }
+#pragma unroll
+    for (int i = 0; i < 8; ++i)
+        if (i < count) p[i] = (T)v[i];
+}
+
+// e^x to about an ulp: 2^(x log2 e) with the product's rounding error given back.  x is held within -104 (0) .. 88.7
+// (3.3e38) first, so that no infinity meets its own negative below; a NaN comes out as a number, which no caller lets
+// through (each multiplies by the NaN itself).
+__device__ __forceinline__ float exp_f32(float x)
+{
+    const float c = __builtin_amdgcn_fmed3f(x, -104.f, 88.7f);
+    const float t = c * 1.44269504f;
+    const float lost = fmaf(c, 1.44269504f, -t) + c * 1.92596299e-8f;    // log2 e = 1.44269504 + 1.926e-8
+    return fmaf(__builtin_amdgcn_exp2f(t), lost * 0.693147181f, __builtin_amdgcn_exp2f(t));
+}
+
+__device__ __forceinline__ float logistic(float z) { return 1.f / (1.f + exp_f32(-z)); }
+__device__ __forceinline__ float normal_cdf(float z) { return fmaf(0.5f, erff(z * 0.707106781f), 0.5f); }
+
+// act(z): 0 none, 1 relu, 2 silu, 3 gelu (rcd_act)
+__device__ __forceinline__ float activate(float z, int act)
+{
+    if (act == 0) return z;
+    if (act == 1) return z < 0.f ? 0.f : z;        // (a NaN stays one)
+    if (act == 2) return z * logistic(z);
+    return z * normal_cdf(z);
+}
+
+// act(z) and act'(z)
+__device__ __forceinline__ void activate_both(float z, int act, float *value, float *slope)
+{
+    if (act == 0) {
+        *value = z;
+        *slope = 1.f;
+    } else if (act == 1) {
+        *value = z < 0.f ? 0.f : z;
+        *slope = z > 0.f ? 1.f : 0.f;
+    } else if (act == 2) {
+        const float s = logistic(z);
+        *value = z * s;
+        *slope = s * fmaf(z, 1.f - s, 1.f);
+    } else {
+        const float cdf = normal_cdf(z);
+        *value = z * cdf;
+        *slope = fmaf(z, 0.398942280f * exp_f32(-0.5f * z * z), cdf);
+    }
+}
+
+// The block exponent e: the least power of two with amax <= 448 * 2^e, not below 2^-127.  448 = 1.75 * 2^8.
+__device__ __forceinline__ int mx_exponent(float amax)
+{
+    const unsigned bits = __builtin_bit_cast(unsigned, amax);
+    const int e = (int)(bits >> 23) - 127 - 8 + ((bits & 0x7fffffu) > 0x600000u ? 1 : 0);
+    return max(e, -127);            // (zero and denormals: the exponent field is 0)
+}
+__device__ __forceinline__ float pow2(int e) { return __builtin_bit_cast(float, (unsigned)(e + 127) << 23); }   // -126 .. 127
+
+// Four values, already divided by their scale, as e4m3 bytes; what is not finite becomes NaN (0x7f).
+__device__ __forceinline__ unsigned to_e4m3x4(float a, float b, float c, float d)
+{
+    int w = __builtin_amdgcn_cvt_pk_fp8_f32(a, b, 0, false);
+    w = __builtin_amdgcn_cvt_pk_fp8_f32(c, d, w, true);
+    const float v[4] = {a, b, c, d};
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+        if (!(fabsf(v[i]) <= 448.f)) w = (w & ~(0xff << (8 * i))) | (0x7f << (8 * i));
+    return (unsigned)w;
+}
+
+} // namespace enc

@@ -1,6 +1,6 @@
 // Host side of librcd: argument checks, workspace layout, class grouping and the
-// round loop that drives the kernels.  One translation unit: the kernel files
-// are included so that their launch stubs are local to this library.
+// round loop that drives the kernels.  The partitioner is one translation unit: its kernel files
+// are included here.  (encoder_lib.hip, the feature encoder's operators, is the other one.)
 #include <hip/hip_runtime.h>
 #include <algorithm>
 #include <cmath>
@@ -12,6 +12,7 @@
 #include <thread>
 
 #include "../../include/rcd.h"
+#include "host_error.h"
 #include "rcd_state.h"
 #include "launch_rules.h"
 #include "shared_units.h"
@@ -1468,6 +1469,12 @@ int split_by_label(const int32_t *labels, int64_t N, int L, int allow_unassigned
 } // namespace
 
 // ===========================================================================
+int rcd_note_hip_error(const char *what, hipError_t e)
+{
+    snprintf(g_hip_err, sizeof g_hip_err, "%s -> %s", what, hipGetErrorString(e));
+    return RCD_ERR_HIP;
+}
+
 extern "C" {
 
 const char *rcd_strerror(int status)
