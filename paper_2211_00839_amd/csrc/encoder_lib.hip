@@ -2,10 +2,13 @@
 #include <algorithm>
 #include <cmath>
 #include <cstdint>
+#include <mutex>
+#include <type_traits>
 
 #include "host_error.h"
 #include "norm_kernels.hip"
 #include "product_kernels.hip"
+#include "few_rows_kernels.hip"
 
 namespace {
 
@@ -82,15 +85,337 @@ inline int64_t part_pitch(int64_t d) { return (d + 63) / 64 * 64; }
 
 // ---- products -------------------------------------------------------------------------------------------------------------
 
-int launch_product(bool gated, const Operand &a, const Operand &b, const Operand &a2, const Operand &b2, int pairs, int64_t M,
-                   int64_t N, int64_t K, const Epilogue &e, hipStream_t stream)
+// What is set up once per device: the tile kernels use more LDS than a kernel may by default.
+constexpr int MAX_DEVICES = 64;
+std::mutex g_setup_mutex;
+int g_units[MAX_DEVICES] = {};          // compute units; 0: not set up yet
+
+template <int WT, int KA, int KB, bool MX, int TO> hipError_t raise_lds_limit()
 {
-    const int64_t tiles = ((M + 63) / 64) * ((N + 63) / 64);
-    if (tiles > 0x7fffffff) return RCD_ERR_UNSUPPORTED;
-    if (gated)
-        hipLaunchKernelGGL(k_product<true>, dim3((unsigned)tiles), dim3(256), 0, stream, a, b, a2, b2, pairs, (int)M, (int)N, (int)K, e);
-    else
-        hipLaunchKernelGGL(k_product<false>, dim3((unsigned)tiles), dim3(256), 0, stream, a, b, a2, b2, pairs, (int)M, (int)N, (int)K, e);
+    return hipFuncSetAttribute(reinterpret_cast<const void *>(&tile::k_tile<WT, KA, KB, MX, TO>),
+                               hipFuncAttributeMaxDynamicSharedMemorySize, tile::Shape<WT, MX>::LDS_BYTES);
+}
+
+// Calls go(WT, KA, KB, MX, TO) as constants, for the variants that there are: both operands with k contiguous (bf16, pieces of
+// fp32, 8 bits; linear or gated), and for the gradients a K_RUNS by ROWS_RUN and a ROWS_RUN by ROWS_RUN product.
+template <typename Go> int with_tile_variant(int wt, int ka, int kb, bool mx, int to, Go go)
+{
+    using std::integral_constant;
+    auto by_target = [&](auto w, auto a, auto b, auto x) {
+        constexpr int A = decltype(a)::value;
+        constexpr int B = decltype(b)::value;
+        if (to == tile::TO_LINEAR) return go(w, a, b, x, integral_constant<int, tile::TO_LINEAR>{});
+        if (to == tile::TO_PARTS) return go(w, a, b, x, integral_constant<int, tile::TO_PARTS>{});
+        if constexpr (A == tile::K_RUNS && B == tile::K_RUNS) {
+            if (to == tile::TO_GATED) return go(w, a, b, x, integral_constant<int, tile::TO_GATED>{});
+            if (to == tile::TO_GATED_PARTS) return go(w, a, b, x, integral_constant<int, tile::TO_GATED_PARTS>{});
+        }
+        return (int)RCD_ERR_UNSUPPORTED;
+    };
+    using K = integral_constant<int, tile::K_RUNS>;
+    using R = integral_constant<int, tile::ROWS_RUN>;
+    auto by_order = [&](auto w) {
+        if (mx) return by_target(w, K{}, K{}, std::true_type{});
+        if (ka == tile::K_RUNS && kb == tile::K_RUNS) return by_target(w, K{}, K{}, std::false_type{});
+        if (ka == tile::K_RUNS) return by_target(w, K{}, R{}, std::false_type{});
+        return by_target(w, R{}, R{}, std::false_type{});
+    };
+    return wt == 128 ? by_order(integral_constant<int, 128>{}) : by_order(integral_constant<int, 64>{});
+}
+
+int set_up(int *units)
+{
+    int dev = 0;
+    ENC_HIP_TRY(hipGetDevice(&dev));
+    if (dev < 0 || dev >= MAX_DEVICES) return rcd_note_hip_error("device index beyond 63", hipErrorInvalidDevice);
+    std::lock_guard<std::mutex> lock(g_setup_mutex);
+    if (g_units[dev] == 0) {
+        for (int wt : {64, 128})
+            for (int order = 0; order < 4; ++order)
+                for (int to : {tile::TO_LINEAR, tile::TO_GATED, tile::TO_PARTS, tile::TO_GATED_PARTS}) {
+                    const bool mx = order == 3;
+                    const int ka = order == 2 ? tile::ROWS_RUN : tile::K_RUNS, kb = order == 1 || order == 2 ? tile::ROWS_RUN : tile::K_RUNS;
+                    if (kb == tile::ROWS_RUN && (to == tile::TO_GATED || to == tile::TO_GATED_PARTS)) continue;
+                    ENC_TRY(with_tile_variant(wt, ka, kb, mx, to, [](auto w, auto a, auto b, auto x, auto t) {
+                        ENC_HIP_TRY((raise_lds_limit<decltype(w)::value, decltype(a)::value, decltype(b)::value, decltype(x)::value,
+                                                     decltype(t)::value>()));
+                        return (int)RCD_OK;
+                    }));
+                }
+        int cus = 0;
+        ENC_HIP_TRY(hipDeviceGetAttribute(&cus, hipDeviceAttributeMultiprocessorCount, dev));
+        g_units[dev] = std::max(cus, 1);
+    }
+    *units = g_units[dev];
+    return RCD_OK;
+}
+
+// A matrix as the tile kernel reads it: where it lies if its rows can go into LDS 16 bytes at a time, else its packed copy.
+struct Laid {
+    const unsigned char *p = nullptr;
+    const uint8_t *scale = nullptr;
+    int64_t pitch = 0, scale_pitch = 0;     // bytes
+    int64_t plane = 0;                      // bytes between the pieces of fp32
+    int64_t cols = 0;                       // what may be read of a row, a multiple of 8
+};
+
+inline int64_t up64(int64_t n) { return (n + 63) / 64 * 64; }
+inline int64_t up128(int64_t n) { return (n + 127) / 128 * 128; }
+
+// 8-bit products of fewer k than this are computed in bf16, from widened copies.  The scaled matrix instruction lines
+// up the 64 products that it adds with the largest of them and cuts off what lies some 2^-11 below (measured: at most 2^-12.3 of the
+// sum of the products' sizes, over all bit patterns).  From about 1024 k on that is within what an fp32 sum of so many
+// terms may be off, (K + 8) 2^-23; a shorter sum would lose precision by it.
+constexpr int64_t MX_INSTRUCTION_FROM = 1024;
+inline int product_type(int dt, int64_t K) { return dt == RCD_MXFP8 && K < MX_INSTRUCTION_FROM ? RCD_BF16 : dt; }
+
+// Room for a matrix's packed copy, whatever its alignment (8 bits: its scales too).
+size_t packed_bytes(int64_t rows, int64_t cols, int dt)
+{
+    dt = product_type(dt, cols);
+    if (dt == RCD_MXFP8) return up256((size_t)rows * up128(cols)) + up256((size_t)rows * (up128(cols) / MX_BLOCK));
+    return up256((size_t)rows * up64(cols) * 2 * (dt == RCD_F32 ? 3 : 1));
+}
+
+inline unsigned copy_grid(int64_t items) { return (unsigned)std::min<int64_t>((items + 255) / 256, 8192); }
+
+// Packs what of up to three matrices cannot be read in place (fp32: all of them, in pieces), in one launch.
+struct Packer {
+    int dt;
+    PackJobs jobs{};
+    ByteJobs bytes{};
+    WidenJobs wide{};
+    int njobs = 0, nbytes = 0, nwide = 0;
+    int64_t most = 0;
+    bool always = false;
+
+    Laid lay(Pieces &room, const void *src, const uint8_t *scale, int64_t ld_scale, int64_t rows, int64_t cols, int64_t ld)
+    {
+        Laid l;
+        // offsets inside a tile are 32 bits: rows too far apart are brought together first
+        const int64_t far = (int64_t)1 << 23;
+        if (dt == RCD_MXFP8 && product_type(dt, cols) == RCD_BF16) {
+            __bf16 *q = room.take<__bf16>((size_t)rows * up64(cols));
+            l.p = (const unsigned char *)q;
+            l.pitch = up64(cols) * 2;
+            l.cols = up64(cols);
+            wide.job[nwide++] = WidenJob{(const uint8_t *)src, scale, q, (long long)ld, (long long)ld_scale, (long long)up64(cols),
+                                         (int)rows, (int)cols, rows_aligned(src, ld, 1, 8)};
+            most = std::max(most, rows * up64(cols) / 8);
+            return l;
+        }
+        if (dt == RCD_MXFP8) {
+            uint8_t *q = room.take<uint8_t>((size_t)rows * up128(cols));
+            uint8_t *s = room.take<uint8_t>((size_t)rows * (up128(cols) / MX_BLOCK));
+            l.p = (const unsigned char *)src;
+            l.pitch = ld;
+            if (always || !rows_aligned(src, ld, 1) || cols % 16 || ld > far) {
+                l.p = q;
+                l.pitch = up128(cols);
+                add(ByteJob{(const uint8_t *)src, q, (long long)ld, (long long)l.pitch, (int)rows, (int)cols});
+            }
+            l.scale = scale;
+            l.scale_pitch = ld_scale;
+            if (always || !rows_aligned(scale, ld_scale, 1, 4) || cols % 128 || ld_scale > far) {
+                l.scale = s;
+                l.scale_pitch = up128(cols) / MX_BLOCK;
+                add(ByteJob{scale, s, (long long)ld_scale, (long long)l.scale_pitch, (int)rows, (int)blocks_of(cols)});
+            }
+            return l;
+        }
+        const bool f32 = dt == RCD_F32;
+        __bf16 *q = room.take<__bf16>((size_t)rows * up64(cols) * (f32 ? 3 : 1));
+        l.p = (const unsigned char *)src;
+        l.pitch = ld * 2;
+        l.cols = cols;
+        if (always || f32 || !rows_aligned(src, ld, 2) || cols % 8 || l.pitch > far) {
+            l.p = (const unsigned char *)q;
+            l.pitch = up64(cols) * 2;
+            l.plane = rows * l.pitch;
+            l.cols = up64(cols);
+            jobs.job[njobs++] = PackJob{src, q, (long long)ld, (long long)up64(cols), (long long)(rows * up64(cols)), (int)rows,
+                                        (int)cols, rows_aligned(src, ld, size_of(dt))};
+            most = std::max(most, rows * up64(cols) / 8);
+        }
+        return l;
+    }
+    void add(const ByteJob &j)
+    {
+        bytes.job[nbytes++] = j;
+        most = std::max<int64_t>(most, (int64_t)j.rows * j.pitch / 4);
+    }
+    int launch(hipStream_t stream)
+    {
+        if (njobs) {
+            const dim3 grid(copy_grid(most), (unsigned)njobs);
+            if (dt == RCD_F32) hipLaunchKernelGGL((k_pack<float, 3>), grid, dim3(256), 0, stream, jobs);
+            else hipLaunchKernelGGL((k_pack<__bf16, 1>), grid, dim3(256), 0, stream, jobs);
+        }
+        if (nbytes) hipLaunchKernelGGL(k_pack_bytes, dim3(copy_grid(most), (unsigned)nbytes), dim3(256), 0, stream, bytes);
+        if (nwide) hipLaunchKernelGGL(k_widen, dim3(copy_grid(most), (unsigned)nwide), dim3(256), 0, stream, wide);
+        ENC_HIP_TRY(hipGetLastError());
+        return RCD_OK;
+    }
+};
+
+// The pairs of pieces whose products make up an fp32 product: the dropped ones are below 2^-24 of it.  Largest last.
+constexpr int PIECE_PAIRS[6][2] = {{2, 0}, {0, 2}, {1, 1}, {1, 0}, {0, 1}, {0, 0}};
+
+// C (M x N) = sum over pairs of a_i b_i, over k of K.
+struct Product {
+    int64_t M, N, K;
+    int dt;                             // RCD_F32: operands in pieces
+    int ka, kb;                         // tile::K_RUNS or ROWS_RUN
+    bool gated;
+    int pairs;                          // 1, or 2 products summed
+    Laid a[2], b[2];                    // gated: b[1] is the second weight
+    int64_t a_shift;                    // bytes from the first pair's a to the second's (same matrix)
+    Epilogue e;
+};
+
+// The cut of a product into workgroups.
+struct Cut {
+    int wt, splits;
+    int64_t tiles_m, tiles_n;
+};
+
+int64_t stages_of(int64_t K, int dt, int pairs)
+{
+    const int64_t per = dt == RCD_MXFP8 ? 128 : 64;
+    return (K + per - 1) / per * (dt == RCD_F32 ? 6 : 1) * pairs;
+}
+inline int64_t parts_pitch(int64_t N, bool gated) { return (N + 7) / 8 * 8 * (gated ? 2 : 1); }
+
+Cut cut_of(int64_t M, int64_t N, int64_t K, int dt, int pairs, bool gated)
+{
+    const int64_t stages = stages_of(K, dt, pairs);
+    auto tiles = [&](int wt, Cut &c) {
+        c.wt = wt;
+        c.tiles_m = (M + 2 * wt - 1) / (2 * wt);
+        c.tiles_n = gated ? (N + wt - 1) / wt : (N + 2 * wt - 1) / (2 * wt);
+        return c.tiles_m * c.tiles_n;
+    };
+    Cut c;
+    int64_t t = tiles(128, c);
+    if (t < 192) t = tiles(64, c);
+    c.splits = 1;
+    const int64_t room = 256;
+    if (t < room / 2) c.splits = (int)std::max<int64_t>(1, std::min<int64_t>({room / t, stages / 4, 64}));
+    return c;
+}
+size_t parts_bytes(const Cut &c, int64_t M, int64_t N, bool gated)
+{
+    return c.splits > 1 ? up256((size_t)c.splits * M * parts_pitch(N, gated) * 4) : 0;
+}
+
+int launch_product(const Product &p, Pieces &room, hipStream_t stream)
+{
+    int units = 0;
+    ENC_TRY(set_up(&units));
+    const Cut c = cut_of(p.M, p.N, p.K, p.dt, p.pairs, p.gated);
+    const int64_t workgroups = c.tiles_m * c.tiles_n * c.splits;
+    if (workgroups > 0x7ffffff0) return RCD_ERR_UNSUPPORTED;
+    const bool mx = p.dt == RCD_MXFP8;
+    tile::Args x{};
+    auto side = [](const Laid &l, const Laid &second, int64_t rows, int kind) {
+        Side s{};
+        s.p = l.p;
+        s.p2 = second.p;
+        s.scale = l.scale;
+        s.scale2 = second.scale;
+        s.pitch = l.pitch;
+        s.scale_pitch = l.scale_pitch;
+        s.extent = (int)(kind == tile::K_RUNS ? rows : l.cols);
+        return s;
+    };
+    x.a = side(p.a[0], p.a[0], p.M, p.ka);
+    x.b = side(p.b[0], p.gated ? p.b[1] : p.b[0], p.N, p.kb);
+    const int64_t per = mx ? 128 : 64;
+    x.seg.stages = (int)((p.K + per - 1) / per);
+    x.seg.rem = (int)(p.K % per);
+    const int pieces = p.dt == RCD_F32 ? 6 : 1;
+    for (int pair = 0; pair < p.pairs; ++pair)
+        for (int i = 0; i < pieces; ++i) {
+            const int s = x.seg.count++;
+            x.seg.a[s] = pair * p.a_shift + (pieces == 6 ? PIECE_PAIRS[i][0] * p.a[0].plane : 0);
+            x.seg.b[s] = (pair ? p.b[1].p - p.b[0].p : 0) + (pieces == 6 ? PIECE_PAIRS[i][1] * p.b[pair].plane : 0);
+        }
+    if (p.dt == RCD_F32) {
+        Pieces3 &q = x.pieces;
+        q.pairs = p.pairs;
+        q.K = (int)p.K;
+        for (int i = 0; i < 2; ++i) {
+            q.a[i] = (const __bf16 *)(p.a[0].p + (i < p.pairs ? i * p.a_shift : 0));
+            q.b[i] = (const __bf16 *)p.b[i < p.pairs || p.gated ? i : 0].p;
+        }
+        q.a_plane = p.a[0].plane / 2;
+        q.b_plane = p.b[0].plane / 2;
+        q.a_row = p.ka == tile::K_RUNS ? p.a[0].pitch / 2 : 1;
+        q.a_k = p.ka == tile::K_RUNS ? 1 : p.a[0].pitch / 2;
+        q.b_row = p.kb == tile::K_RUNS ? p.b[0].pitch / 2 : 1;
+        q.b_k = p.kb == tile::K_RUNS ? 1 : p.b[0].pitch / 2;
+    }
+    x.e = p.e;
+    x.M = (int)p.M;
+    x.N = (int)p.N;
+    x.tiles_m = (int)c.tiles_m;
+    x.tiles_n = (int)c.tiles_n;
+    x.splits = c.splits;
+    int to = p.gated ? tile::TO_GATED : tile::TO_LINEAR;
+    if (c.splits > 1) {
+        to = p.gated ? tile::TO_GATED_PARTS : tile::TO_PARTS;
+        x.parts_pitch = parts_pitch(p.N, p.gated);
+        x.parts_half = (int)(x.parts_pitch / 2);
+        x.parts = room.take<float>((size_t)c.splits * p.M * x.parts_pitch);
+    }
+    ENC_TRY(with_tile_variant(c.wt, p.ka, p.kb, mx, to, [&](auto w, auto a, auto b, auto m, auto t) {
+        constexpr int W = decltype(w)::value;
+        constexpr bool X = decltype(m)::value;
+        hipLaunchKernelGGL((tile::k_tile<W, decltype(a)::value, decltype(b)::value, X, decltype(t)::value>),
+                           dim3((unsigned)((workgroups + 7) / 8 * 8)), dim3(tile::THREADS), (tile::Shape<W, X>::LDS_BYTES), stream, x);
+        return (int)RCD_OK;
+    }));
+    if (c.splits > 1) {
+        const dim3 grid(copy_grid(p.M * ((p.N + 7) / 8)));
+        if (p.gated) hipLaunchKernelGGL(tile::k_join<true>, grid, dim3(256), 0, stream, x);
+        else hipLaunchKernelGGL(tile::k_join<false>, grid, dim3(256), 0, stream, x);
+    }
+    ENC_HIP_TRY(hipGetLastError());
+    return RCD_OK;
+}
+
+// Up to so many rows the weights are read once, straight into registers.
+inline int64_t few_rows(int dt) { return dt == RCD_F32 ? 32 : 64; }
+
+int launch_few(int dt, bool gated, const few::Args &x, hipStream_t stream)
+{
+    if (dt == RCD_F32) {
+        const int cols = gated ? 4 : 8;
+        auto go = [&](auto mr) {
+            constexpr int MR = decltype(mr)::value;
+            const dim3 grid((unsigned)((x.N + cols - 1) / cols), (unsigned)((x.M + MR - 1) / MR));
+            if (gated) hipLaunchKernelGGL((few::k_few_f32<MR, true>), grid, dim3(256), 0, stream, x);
+            else hipLaunchKernelGGL((few::k_few_f32<MR, false>), grid, dim3(256), 0, stream, x);
+        };
+        if (x.M == 1) go(std::integral_constant<int, 1>{});
+        else go(std::integral_constant<int, 4>{});
+    } else {
+        const dim3 grid((unsigned)((x.N + 15) / 16));
+        auto go = [&](auto mt, auto waves) {
+            constexpr int MT = decltype(mt)::value, W = decltype(waves)::value;
+            if (dt == RCD_MXFP8) {
+                if (gated) hipLaunchKernelGGL((few::k_few<MT, W, true, true>), grid, dim3(64 * W), 0, stream, x);
+                else hipLaunchKernelGGL((few::k_few<MT, W, true, false>), grid, dim3(64 * W), 0, stream, x);
+            } else {
+                if (gated) hipLaunchKernelGGL((few::k_few<MT, W, false, true>), grid, dim3(64 * W), 0, stream, x);
+                else hipLaunchKernelGGL((few::k_few<MT, W, false, false>), grid, dim3(64 * W), 0, stream, x);
+            }
+        };
+        using std::integral_constant;
+        if (x.M <= 16) go(integral_constant<int, 1>{}, integral_constant<int, 8>{});
+        else if (x.M <= 32) go(integral_constant<int, 2>{}, integral_constant<int, 4>{});
+        else go(integral_constant<int, 4>{}, integral_constant<int, 4>{});
+    }
     ENC_HIP_TRY(hipGetLastError());
     return RCD_OK;
 }
@@ -116,27 +441,34 @@ int sum_columns(const float *part, int64_t pitch, int64_t groups, int64_t d, voi
     return RCD_OK;
 }
 
-constexpr int64_t SLOPE_GROUPS = 256;
-
-struct LinearBack {
-    float *dz, *part;
+// The pass before a backward product: threads side by side over eight columns each, groups of rows.
+struct SlopeCut {
+    int across;
+    int64_t pieces, groups;
 };
-size_t linear_back_pieces(void *ws, int64_t M, int64_t N, LinearBack *p)
+SlopeCut slope_cut(int64_t M, int64_t cols)
 {
-    Pieces w(ws);
-    p->dz = w.take<float>((size_t)M * N);
-    p->part = w.take<float>((size_t)std::min(SLOPE_GROUPS, std::max<int64_t>(M, 1)) * part_pitch(N));
-    return w.used;
+    SlopeCut c;
+    c.across = 1;
+    while (c.across < 256 && c.across * 8 < cols) c.across *= 2;
+    c.pieces = (cols + 8 * c.across - 1) / (8 * c.across);
+    const int64_t down = 256 / c.across;
+    c.groups = std::max<int64_t>(1, std::min<int64_t>((M + 4 * down - 1) / (4 * down), 1024 / std::min<int64_t>(c.pieces, 4)));
+    return c;
 }
-struct GatedBack {
-    float *dg, *du;
+
+// Workspace of the linear backward call.
+struct LinearBack {
+    __bf16 *dz;
+    float *part;
+    size_t used;
 };
-size_t gated_back_pieces(void *ws, int64_t M, int64_t F, GatedBack *p)
+LinearBack linear_back(Pieces &w, int64_t M, int64_t N, int dt)
 {
-    Pieces w(ws);
-    p->dg = w.take<float>((size_t)M * F);
-    p->du = w.take<float>((size_t)M * F);
-    return w.used;
+    LinearBack p;
+    p.dz = w.take<__bf16>((size_t)M * up64(N) * (dt == RCD_F32 ? 3 : 1));
+    p.part = w.take<float>((size_t)slope_cut(M, up64(N)).groups * part_pitch(N));
+    return p;
 }
 
 // Types and extents of a product's call.
@@ -147,6 +479,60 @@ int check_product(int dt, int out_dt, int64_t M, int64_t N, int64_t K, int act)
     if (act < RCD_ACT_NONE || act > RCD_ACT_GELU) return RCD_ERR_UNSUPPORTED;
     if (M < 0 || N < 1 || K < 1) return RCD_ERR_INVALID_ARG;
     if (M > MAX_EXTENT || N > MAX_EXTENT || K > MAX_EXTENT) return RCD_ERR_UNSUPPORTED;
+    return RCD_OK;
+}
+
+inline bool product_sizes_ok(int64_t M, int64_t N, int64_t K) { return extent_ok(M) && extent_ok(N) && extent_ok(K); }
+
+Epilogue one_output(void *out, int64_t ld, int dt, int act)
+{
+    Epilogue e{};
+    e.out = out;
+    e.ld_o = ld;
+    e.act = act;
+    e.split_row = e.rows_each = 0x7fffffff;
+    e.out_f32 = dt == RCD_F32;
+    e.vec = rows_aligned(out, ld, size_of(dt));
+    return e;
+}
+
+few::Args few_args(int dt, const void *a, const uint8_t *scale, int64_t ld, int64_t ld_scale, int64_t M, int64_t N, int64_t K, const Epilogue &e)
+{
+    few::Args x{};
+    x.a = (const unsigned char *)a;
+    x.a_pitch = ld * size_of(dt);
+    x.sa = scale;
+    x.sa_pitch = ld_scale;
+    x.e = e;
+    x.M = (int)M; x.N = (int)N; x.K = (int)K;
+    x.vec = rows_aligned(a, ld, size_of(dt));
+    return x;
+}
+void few_weight(few::Args &x, int dt, bool second, const void *w, const uint8_t *scale, int64_t ld, int64_t ld_scale)
+{
+    (second ? x.b2 : x.b) = (const unsigned char *)w;
+    (second ? x.b2_pitch : x.b_pitch) = ld * size_of(dt);
+    (second ? x.sb2 : x.sb) = scale;
+    (second ? x.sb2_pitch : x.sb_pitch) = ld_scale;
+    x.vec = x.vec && rows_aligned(w, ld, size_of(dt));
+}
+
+// The gated block's two weights.  The tile kernel wants one pitch for both: if they differ, or one can be read in place
+// and the other not, both are packed.
+int lay_pair(Packer &pack, Pieces &room, Laid (&b)[2], int dt, const void *wg, const uint8_t *sg, int64_t ld_g, int64_t ld_sg,
+             const void *wu, const uint8_t *su, int64_t ld_u, int64_t ld_su, int64_t F, int64_t K)
+{
+    const int jobs = pack.njobs, bytes = pack.nbytes;
+    const size_t used = room.used;
+    b[0] = pack.lay(room, wg, sg, ld_sg, F, K, ld_g);
+    b[1] = pack.lay(room, wu, su, ld_su, F, K, ld_u);
+    if (b[0].pitch == b[1].pitch && b[0].scale_pitch == b[1].scale_pitch && b[0].plane == b[1].plane) return RCD_OK;
+    pack.njobs = jobs;
+    pack.nbytes = bytes;
+    room.used = used;
+    pack.always = true;
+    b[0] = pack.lay(room, wg, sg, ld_sg, F, K, ld_g);
+    b[1] = pack.lay(room, wu, su, ld_su, F, K, ld_u);
     return RCD_OK;
 }
 
@@ -236,14 +622,19 @@ int rcd_rms_norm_backward(const void *dY_dev, int dt, int64_t rows, int64_t d, i
     return dweight_dev ? sum_columns(a.part, a.part_pitch, groups, d, dweight_dev, dt, stream) : RCD_OK;
 }
 
-size_t rcd_linear_workspace_bytes(int64_t, int64_t, int64_t, int) { return 0; }
+size_t rcd_linear_workspace_bytes(int64_t M, int64_t N, int64_t K, int dt)
+{
+    if (!product_sizes_ok(M, N, K) || dt < RCD_F32 || dt > RCD_MXFP8 || M <= few_rows(dt)) return 0;
+    return packed_bytes(M, K, dt) + packed_bytes(N, K, dt) + parts_bytes(cut_of(M, N, K, product_type(dt, K), 1, false), M, N, false);
+}
 
 int rcd_linear(const void *A_dev, const uint8_t *A_scale_dev, int64_t ld_a, int64_t ld_a_scale,
                const void *W_dev, const uint8_t *W_scale_dev, int64_t ld_w, int64_t ld_w_scale, int dt, int out_dt,
                int64_t M, int64_t N, int64_t K, const void *bias_dev, int act, const void *residual_dev, int64_t ld_r,
                float *preact_dev, int64_t ld_p, void *Y_dev, int64_t ld_y,
-               void *workspace_dev, size_t workspace_bytes, void *stream)
+               void *workspace_dev, size_t workspace_bytes, void *stream_)
 {
+    hipStream_t stream = (hipStream_t)stream_;
     ENC_TRY(check_product(dt, out_dt, M, N, K, act));
     if (ld_a < K || ld_w < K || ld_y < N || (residual_dev && ld_r < N) || (preact_dev && ld_p < N)) return RCD_ERR_INVALID_ARG;
     if (M == 0) return RCD_OK;
@@ -251,15 +642,41 @@ int rcd_linear(const void *A_dev, const uint8_t *A_scale_dev, int64_t ld_a, int6
     ENC_TRY(check_mx_operand(dt, A_scale_dev, ld_a_scale, K));
     ENC_TRY(check_mx_operand(dt, W_scale_dev, ld_w_scale, K));
     ENC_TRY(check_pieces(workspace_dev, workspace_bytes, rcd_linear_workspace_bytes(M, N, K, dt)));
-    const Operand a{A_dev, A_scale_dev, ld_a, 1, ld_a_scale, dt}, b{W_dev, W_scale_dev, ld_w, 1, ld_w_scale, dt};
-    const Epilogue e{bias_dev, residual_dev, preact_dev, Y_dev, ld_r, ld_p, ld_y, act, out_dt == RCD_F32};
-    return launch_product(false, a, b, a, b, 1, M, N, K, e, (hipStream_t)stream);
+    const int64_t osz = size_of(out_dt);
+    Epilogue e = one_output(Y_dev, ld_y, out_dt, act);
+    e.bias = bias_dev;
+    e.residual = residual_dev;
+    e.preact = preact_dev;
+    e.ld_r = ld_r;
+    e.ld_p = ld_p;
+    e.vec = rows_aligned(Y_dev, ld_y, osz) && rows_aligned(bias_dev, 0, osz) && rows_aligned(residual_dev, ld_r, osz) &&
+            rows_aligned(preact_dev, ld_p, 4);
+    if (M <= few_rows(dt)) {
+        few::Args x = few_args(dt, A_dev, A_scale_dev, ld_a, ld_a_scale, M, N, K, e);
+        few_weight(x, dt, false, W_dev, W_scale_dev, ld_w, ld_w_scale);
+        return launch_few(dt, false, x, stream);
+    }
+    Pieces room(workspace_dev);
+    Packer pack{dt};
+    Product p{};
+    p.M = M; p.N = N; p.K = K;
+    p.dt = product_type(dt, K);
+    p.pairs = 1;
+    p.a[0] = pack.lay(room, A_dev, A_scale_dev, ld_a_scale, M, K, ld_a);
+    p.b[0] = pack.lay(room, W_dev, W_scale_dev, ld_w_scale, N, K, ld_w);
+    p.e = e;
+    ENC_TRY(pack.launch(stream));
+    return launch_product(p, room, stream);
 }
 
 size_t rcd_linear_backward_workspace_bytes(int64_t M, int64_t N, int64_t K, int dt)
 {
-    LinearBack p;
-    return M >= 1 && extent_ok(N) && extent_ok(K) && is_matrix_type(dt) ? linear_back_pieces(nullptr, M, N, &p) : 0;
+    if (!product_sizes_ok(M, N, K) || !is_matrix_type(dt)) return 0;
+    Pieces w(nullptr);
+    linear_back(w, M, N, dt);
+    // (the two products run one after the other: the larger one's parts)
+    return w.used + packed_bytes(M, K, dt) + packed_bytes(N, K, dt) +
+           std::max(parts_bytes(cut_of(M, K, N, dt, 1, false), M, K, false), parts_bytes(cut_of(N, K, M, dt, 1, false), N, K, false));
 }
 
 int rcd_linear_backward(const void *dY_dev, int64_t ld_dy, const void *A_dev, int64_t ld_a, const void *W_dev, int64_t ld_w,
@@ -278,43 +695,82 @@ int rcd_linear_backward(const void *dY_dev, int64_t ld_dy, const void *A_dev, in
     }
     if (!dY_dev || (dW_dev && !A_dev) || (dA_dev && !W_dev) || (act != RCD_ACT_NONE && !preact_dev)) return RCD_ERR_INVALID_ARG;
     ENC_TRY(check_pieces(workspace_dev, workspace_bytes, rcd_linear_backward_workspace_bytes(M, N, K, dt)));
-    LinearBack p;
-    linear_back_pieces(workspace_dev, M, N, &p);
-    const int64_t groups = std::min(SLOPE_GROUPS, M), pitch = part_pitch(N);
-    const dim3 grid((unsigned)((N + 255) / 256), (unsigned)groups);
-    if (dt == RCD_F32)
-        hipLaunchKernelGGL(k_slope<float>, grid, dim3(256), 0, stream, (const float *)dY_dev, (long long)ld_dy, preact_dev,
-                           (long long)ld_p, act, (int)M, (int)N, p.dz, p.part, (long long)pitch);
-    else
-        hipLaunchKernelGGL(k_slope<__bf16>, grid, dim3(256), 0, stream, (const __bf16 *)dY_dev, (long long)ld_dy, preact_dev,
-                           (long long)ld_p, act, (int)M, (int)N, p.dz, p.part, (long long)pitch);
-    ENC_HIP_TRY(hipGetLastError());
-    if (dbias_dev) ENC_TRY(sum_columns(p.part, pitch, groups, N, dbias_dev, dt, stream));
-    Epilogue e{};
-    e.out_f32 = dt == RCD_F32;
-    if (dA_dev) {
-        e.out = dA_dev;
-        e.ld_o = ld_da;
-        const Operand a{p.dz, nullptr, N, 1, 0, RCD_F32}, b{W_dev, nullptr, 1, ld_w, 0, dt};
-        ENC_TRY(launch_product(false, a, b, a, b, 1, M, K, N, e, stream));
+    const bool f32 = dt == RCD_F32;
+    Pieces room(workspace_dev);
+    const LinearBack w = linear_back(room, M, N, dt);
+    Packer pack{dt};
+    // dz itself, in place, where there is no activation and its rows can go into LDS as they are
+    Laid dz;
+    Laid a, b;
+    if (dW_dev) a = pack.lay(room, A_dev, nullptr, 0, M, K, ld_a);
+    if (dA_dev) b = pack.lay(room, W_dev, nullptr, 0, N, K, ld_w);
+    ENC_TRY(pack.launch(stream));
+    const bool as_it_is = act == RCD_ACT_NONE && dt == RCD_BF16 && rows_aligned(dY_dev, ld_dy, 2) && N % 8 == 0 && ld_dy * 2 <= ((int64_t)1 << 23);
+    const int64_t pitch = up64(N);
+    if (as_it_is) {
+        dz.p = (const unsigned char *)dY_dev;
+        dz.pitch = ld_dy * 2;
+        dz.cols = N;
+    } else {
+        dz.p = (const unsigned char *)w.dz;
+        dz.pitch = pitch * 2;
+        dz.plane = M * pitch * 2;
+        dz.cols = pitch;
     }
+    if (!as_it_is || dbias_dev) {
+        const SlopeCut c = slope_cut(M, pitch);
+        SlopeArgs x{};
+        x.dy = dY_dev;
+        x.z = preact_dev;
+        x.dz = as_it_is ? nullptr : w.dz;
+        x.part = dbias_dev ? w.part : nullptr;
+        x.ld_dy = ld_dy; x.ld_z = ld_p; x.pitch = pitch; x.plane = M * pitch; x.part_pitch = part_pitch(N);
+        x.M = (int)M; x.N = (int)N; x.act = act; x.across = c.across;
+        x.vec = rows_aligned(dY_dev, ld_dy, size_of(dt)) && (act == RCD_ACT_NONE || rows_aligned(preact_dev, ld_p, 4));
+        const dim3 grid((unsigned)c.pieces, (unsigned)c.groups);
+        if (f32) hipLaunchKernelGGL((k_slope<float, 3>), grid, dim3(256), 0, stream, x);
+        else hipLaunchKernelGGL((k_slope<__bf16, 1>), grid, dim3(256), 0, stream, x);
+        ENC_HIP_TRY(hipGetLastError());
+        if (dbias_dev) ENC_TRY(sum_columns(w.part, x.part_pitch, c.groups, N, dbias_dev, dt, stream));
+    }
+    Product p{};
+    p.dt = dt;
+    p.pairs = 1;
+    const size_t mark = room.used;
+    if (dA_dev) {
+        p.M = M; p.N = K; p.K = N;
+        p.ka = tile::K_RUNS;
+        p.kb = tile::ROWS_RUN;
+        p.a[0] = dz;
+        p.b[0] = b;
+        p.e = one_output(dA_dev, ld_da, dt, RCD_ACT_NONE);
+        ENC_TRY(launch_product(p, room, stream));
+    }
+    room.used = mark;
     if (dW_dev) {
-        e.out = dW_dev;
-        e.ld_o = ld_dw;
-        const Operand a{p.dz, nullptr, 1, N, 0, RCD_F32}, b{A_dev, nullptr, 1, ld_a, 0, dt};
-        ENC_TRY(launch_product(false, a, b, a, b, 1, N, K, M, e, stream));
+        p.M = N; p.N = K; p.K = M;
+        p.ka = p.kb = tile::ROWS_RUN;
+        p.a[0] = dz;
+        p.b[0] = a;
+        p.e = one_output(dW_dev, ld_dw, dt, RCD_ACT_NONE);
+        ENC_TRY(launch_product(p, room, stream));
     }
     return RCD_OK;
 }
 
-size_t rcd_gated_linear_workspace_bytes(int64_t, int64_t, int64_t, int) { return 0; }
+size_t rcd_gated_linear_workspace_bytes(int64_t M, int64_t F, int64_t K, int dt)
+{
+    if (!product_sizes_ok(M, F, K) || dt < RCD_F32 || dt > RCD_MXFP8 || M <= few_rows(dt)) return 0;
+    return packed_bytes(M, K, dt) + 2 * packed_bytes(F, K, dt) + parts_bytes(cut_of(M, F, K, product_type(dt, K), 1, true), M, F, true);
+}
 
 int rcd_gated_linear(const void *A_dev, const uint8_t *A_scale_dev, int64_t ld_a, int64_t ld_a_scale,
                      const void *Wg_dev, const uint8_t *Wg_scale_dev, int64_t ld_wg, int64_t ld_wg_scale,
                      const void *Wu_dev, const uint8_t *Wu_scale_dev, int64_t ld_wu, int64_t ld_wu_scale,
                      int dt, int out_dt, int64_t M, int64_t F, int64_t K, int act, float *saved_dev,
-                     void *H_dev, int64_t ld_h, void *workspace_dev, size_t workspace_bytes, void *stream)
+                     void *H_dev, int64_t ld_h, void *workspace_dev, size_t workspace_bytes, void *stream_)
 {
+    hipStream_t stream = (hipStream_t)stream_;
     ENC_TRY(check_product(dt, out_dt, M, F, K, act));
     if (ld_a < K || ld_wg < K || ld_wu < K || ld_h < F) return RCD_ERR_INVALID_ARG;
     if (M == 0) return RCD_OK;
@@ -323,22 +779,38 @@ int rcd_gated_linear(const void *A_dev, const uint8_t *A_scale_dev, int64_t ld_a
     ENC_TRY(check_mx_operand(dt, Wg_scale_dev, ld_wg_scale, K));
     ENC_TRY(check_mx_operand(dt, Wu_scale_dev, ld_wu_scale, K));
     ENC_TRY(check_pieces(workspace_dev, workspace_bytes, rcd_gated_linear_workspace_bytes(M, F, K, dt)));
-    const Operand a{A_dev, A_scale_dev, ld_a, 1, ld_a_scale, dt}, b{Wg_dev, Wg_scale_dev, ld_wg, 1, ld_wg_scale, dt},
-        b2{Wu_dev, Wu_scale_dev, ld_wu, 1, ld_wu_scale, dt};
-    Epilogue e{};
+    Epilogue e = one_output(H_dev, ld_h, out_dt, act);
     e.preact = saved_dev;
     e.ld_p = 2 * F;
-    e.out = H_dev;
-    e.ld_o = ld_h;
-    e.act = act;
-    e.out_f32 = out_dt == RCD_F32;
-    return launch_product(true, a, b, a, b2, 1, M, F, K, e, (hipStream_t)stream);
+    e.vec = rows_aligned(H_dev, ld_h, size_of(out_dt)) && rows_aligned(saved_dev, 2 * F, 4);
+    if (M <= few_rows(dt)) {
+        few::Args x = few_args(dt, A_dev, A_scale_dev, ld_a, ld_a_scale, M, F, K, e);
+        few_weight(x, dt, false, Wg_dev, Wg_scale_dev, ld_wg, ld_wg_scale);
+        few_weight(x, dt, true, Wu_dev, Wu_scale_dev, ld_wu, ld_wu_scale);
+        return launch_few(dt, true, x, stream);
+    }
+    Pieces room(workspace_dev);
+    Packer pack{dt};
+    Product p{};
+    p.M = M; p.N = F; p.K = K;
+    p.dt = product_type(dt, K);
+    p.gated = true;
+    p.pairs = 1;
+    p.a[0] = pack.lay(room, A_dev, A_scale_dev, ld_a_scale, M, K, ld_a);
+    ENC_TRY(lay_pair(pack, room, p.b, dt, Wg_dev, Wg_scale_dev, ld_wg, ld_wg_scale, Wu_dev, Wu_scale_dev, ld_wu, ld_wu_scale, F, K));
+    p.e = e;
+    ENC_TRY(pack.launch(stream));
+    return launch_product(p, room, stream);
 }
 
 size_t rcd_gated_linear_backward_workspace_bytes(int64_t M, int64_t F, int64_t K, int dt)
 {
-    GatedBack p;
-    return M >= 1 && extent_ok(F) && extent_ok(K) && is_matrix_type(dt) ? gated_back_pieces(nullptr, M, F, &p) : 0;
+    if (!product_sizes_ok(M, F, K) || !is_matrix_type(dt)) return 0;
+    Pieces w(nullptr);
+    w.take<__bf16>((size_t)M * 2 * up64(F) * (dt == RCD_F32 ? 3 : 1));
+    return w.used + packed_bytes(M, K, dt) + 2 * packed_bytes(F, K, dt) +
+           std::max(parts_bytes(cut_of(M, K, F, dt, 2, false), M, K, false),
+                    parts_bytes(cut_of(2 * up64(F), K, M, dt, 1, false), 2 * up64(F), K, false));
 }
 
 int rcd_gated_linear_backward(const void *dH_dev, int64_t ld_dh, const void *A_dev, int64_t ld_a,
@@ -359,33 +831,59 @@ int rcd_gated_linear_backward(const void *dH_dev, int64_t ld_dh, const void *A_d
     }
     if (!dH_dev || !saved_dev || (dWg_dev && !A_dev) || (dA_dev && (!Wg_dev || !Wu_dev))) return RCD_ERR_INVALID_ARG;
     ENC_TRY(check_pieces(workspace_dev, workspace_bytes, rcd_gated_linear_backward_workspace_bytes(M, F, K, dt)));
-    GatedBack p;
-    gated_back_pieces(workspace_dev, M, F, &p);
-    const dim3 grid((unsigned)((F + 255) / 256), (unsigned)std::min<int64_t>(SLOPE_GROUPS, M));
-    if (dt == RCD_F32)
-        hipLaunchKernelGGL(k_gated_slope<float>, grid, dim3(256), 0, stream, (const float *)dH_dev, (long long)ld_dh, saved_dev, act,
-                           (int)M, (int)F, p.dg, p.du);
-    else
-        hipLaunchKernelGGL(k_gated_slope<__bf16>, grid, dim3(256), 0, stream, (const __bf16 *)dH_dev, (long long)ld_dh, saved_dev, act,
-                           (int)M, (int)F, p.dg, p.du);
+    const bool f32 = dt == RCD_F32;
+    const int64_t half = up64(F), pitch = 2 * half;
+    Pieces room(workspace_dev);
+    __bf16 *dgu = room.take<__bf16>((size_t)M * pitch * (f32 ? 3 : 1));
+    Packer pack{dt};
+    Product p{};
+    p.dt = dt;
+    Laid a;
+    if (dWg_dev) a = pack.lay(room, A_dev, nullptr, 0, M, K, ld_a);
+    if (dA_dev) ENC_TRY(lay_pair(pack, room, p.b, dt, Wg_dev, nullptr, ld_wg, 0, Wu_dev, nullptr, ld_wu, 0, F, K));
+    ENC_TRY(pack.launch(stream));
+    const SlopeCut c = slope_cut(M, half);
+    SlopeArgs x{};
+    x.dy = dH_dev;
+    x.z = saved_dev;
+    x.dz = dgu;
+    x.ld_dy = ld_dh; x.ld_z = 2 * F; x.pitch = pitch; x.plane = M * pitch;
+    x.M = (int)M; x.N = (int)F; x.act = act; x.across = c.across; x.half = (int)half;
+    x.vec = rows_aligned(dH_dev, ld_dh, size_of(dt)) && rows_aligned(saved_dev, 2 * F, 4);
+    const dim3 grid((unsigned)c.pieces, (unsigned)c.groups);
+    if (f32) hipLaunchKernelGGL((k_gated_slope<float, 3>), grid, dim3(256), 0, stream, x);
+    else hipLaunchKernelGGL((k_gated_slope<__bf16, 1>), grid, dim3(256), 0, stream, x);
     ENC_HIP_TRY(hipGetLastError());
-    Epilogue e{};
-    e.out_f32 = dt == RCD_F32;
+    Laid d;
+    d.p = (const unsigned char *)dgu;
+    d.pitch = pitch * 2;
+    d.plane = M * pitch * 2;
+    d.cols = pitch;
+    p.a[0] = d;
+    const size_t mark = room.used;
     if (dA_dev) {
-        e.out = dA_dev;
-        e.ld_o = ld_da;
-        const Operand a{p.dg, nullptr, F, 1, 0, RCD_F32}, b{Wg_dev, nullptr, 1, ld_wg, 0, dt};
-        const Operand a2{p.du, nullptr, F, 1, 0, RCD_F32}, b2{Wu_dev, nullptr, 1, ld_wu, 0, dt};
-        ENC_TRY(launch_product(false, a, b, a2, b2, 2, M, K, F, e, stream));
+        p.M = M; p.N = K; p.K = F;
+        p.ka = tile::K_RUNS;
+        p.kb = tile::ROWS_RUN;
+        p.pairs = 2;
+        p.a_shift = half * 2;
+        p.e = one_output(dA_dev, ld_da, dt, RCD_ACT_NONE);
+        ENC_TRY(launch_product(p, room, stream));
     }
+    room.used = mark;
     if (dWg_dev) {
-        const Operand b{A_dev, nullptr, 1, ld_a, 0, dt};
-        for (int i = 0; i < 2; ++i) {
-            const Operand a{i ? p.du : p.dg, nullptr, 1, F, 0, RCD_F32};
-            e.out = i ? dWu_dev : dWg_dev;
-            e.ld_o = i ? ld_dwu : ld_dwg;
-            ENC_TRY(launch_product(false, a, b, a, b, 1, F, K, M, e, stream));
-        }
+        // dg's columns and du's are the rows of one product
+        p.M = pitch; p.N = K; p.K = M;
+        p.ka = p.kb = tile::ROWS_RUN;
+        p.pairs = 1;
+        p.b[0] = a;
+        p.e = one_output(dWg_dev, ld_dwg, dt, RCD_ACT_NONE);
+        p.e.out2 = dWu_dev;
+        p.e.ld_o2 = ld_dwu;
+        p.e.split_row = (int)half;
+        p.e.rows_each = (int)F;
+        p.e.vec = p.e.vec && rows_aligned(dWu_dev, ld_dwu, size_of(dt));
+        ENC_TRY(launch_product(p, room, stream));
     }
     return RCD_OK;
 }

@@ -120,4 +120,27 @@ __device__ __forceinline__ unsigned to_e4m3x4(float a, float b, float c, float d
     return (unsigned)w;
 }
 
+// 2^(s - 127) of a scale byte; 255 is NaN.
+__device__ __forceinline__ float mx_scale(int s)
+{
+    return __builtin_bit_cast(float, s == 255 ? 0x7fc00000u : s == 0 ? 0x00400000u : (unsigned)s << 23);
+}
+
+// Eight e4m3 bytes times their scale as bf16: exact, a value has four significant bits (below 2^-126 bf16 has fewer).
+__device__ __forceinline__ bf16x8 widen8(unsigned lo, unsigned hi, float scale)
+{
+    typedef float f32x2 __attribute__((ext_vector_type(2)));
+    bf16x8 r;
+    const unsigned w[2] = {lo, hi};
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+        const f32x2 a = __builtin_amdgcn_cvt_pk_f32_fp8((int)w[i], false), b = __builtin_amdgcn_cvt_pk_f32_fp8((int)w[i], true);
+        r[4 * i] = (__bf16)(a[0] * scale);
+        r[4 * i + 1] = (__bf16)(a[1] * scale);
+        r[4 * i + 2] = (__bf16)(b[0] * scale);
+        r[4 * i + 3] = (__bf16)(b[1] * scale);
+    }
+    return r;
+}
+
 } // namespace enc

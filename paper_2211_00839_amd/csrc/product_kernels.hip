@@ -1,143 +1,947 @@
-// Matrix products of the feature encoder with what goes before and after them.
+// Matrix products of the feature encoder with what goes before and after them:
+//
+//   C(m, n) = sum over k of a(m, k) b(n, k)
+//
+// on the matrix cores, for operands whose k is contiguous (the forward products) or whose rows are (the gradients: no matrix
+// is ever transposed in memory), in bf16, in fp32 as three bf16 pieces, or in 8 bits with block scales.
 #include "encoder_math.h"
 
 namespace enc {
 
-// Element (row, k) of an operand lies at p + row * rs + k * ks (elements of its type).
-struct Operand {
-    const void *p;
-    const uint8_t *scale;           // RCD_MXFP8: one byte for 32 elements of a row
-    long long rs, ks, ld_scale;
-    int dt;                         // rcd_dtype
-};
-
-__device__ __forceinline__ float element(const Operand &o, long long row, long long k)
-{
-    const long long at = row * o.rs + k * o.ks;
-    if (o.dt == 0) return ((const float *)o.p)[at];
-    if (o.dt == 1) return (float)((const __bf16 *)o.p)[at];
-    const int s = o.scale[row * o.ld_scale + k / MX_BLOCK];
-    const float v = __builtin_amdgcn_cvt_f32_fp8(((const uint8_t *)o.p)[at], 0);
-    return s == 255 ? __builtin_nanf("") : v * ldexpf(1.f, s - 127);
-}
-
-// What becomes of a product's sums.  act(z + bias) + residual, or the gated block's act(g) * u.
+// What becomes of a product's sums: act(z + bias) + residual, the gated block's act(g) * u, or the sums themselves.
 struct Epilogue {
     const void *bias, *residual;    // of the output's type, nullable
     float *preact;                  // z in fp32 (gated: g and u side by side), nullable
-    void *out;
-    long long ld_r, ld_p, ld_o;
+    void *out, *out2;               // rows from split_row on go to out2 (two weights' gradients in one product)
+    long long ld_r, ld_p, ld_o, ld_o2;
     int act;
+    int split_row;                  // 0x7fffffff: one output
+    int rows_each;                  // rows of one output (with two of them, padding lies between)
     bool out_f32;
+    bool vec;                       // 16-byte accesses are allowed for full groups of eight columns
 };
 
-__device__ __forceinline__ float read_as(const void *p, long long at, bool f32)
+template <typename T>
+__device__ __forceinline__ void finish_linear8_as(const Epilogue &e, T *out, long long row, long long m, int n, int count, float (&z)[8])
 {
-    return f32 ? ((const float *)p)[at] : (float)((const __bf16 *)p)[at];
-}
-__device__ __forceinline__ void write_as(void *p, long long at, bool f32, float v)
-{
-    if (f32) ((float *)p)[at] = v;
-    else ((__bf16 *)p)[at] = (__bf16)v;
+    float t[8];
+    if (e.bias) {
+        load8((const T *)e.bias + n, count, e.vec, t);
+#pragma unroll
+        for (int i = 0; i < 8; ++i) z[i] += t[i];
+    }
+    if (e.preact) store8(e.preact + m * e.ld_p + n, count, e.vec, z);
+    if (e.act != 0) {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) z[i] = activate(z[i], e.act);
+    }
+    if (e.residual) {
+        load8((const T *)e.residual + m * e.ld_r + n, count, e.vec, t);
+#pragma unroll
+        for (int i = 0; i < 8; ++i) z[i] += t[i];
+    }
+    store8(out + row + n, count, e.vec, z);
 }
 
-__device__ __forceinline__ void finish_linear(const Epilogue &e, long long m, long long n, float z)
+// Columns n .. n + count - 1 (count <= 8) of row m.
+__device__ __forceinline__ void finish_linear8(const Epilogue &e, int m, int n, int count, float (&z)[8])
 {
-    if (e.bias) z += read_as(e.bias, n, e.out_f32);
-    if (e.preact) e.preact[m * e.ld_p + n] = z;
-    float y = activate(z, e.act);
-    if (e.residual) y += read_as(e.residual, m * e.ld_r + n, e.out_f32);
-    write_as(e.out, m * e.ld_o + n, e.out_f32, y);
+    void *out = e.out;
+    long long row = (long long)m * e.ld_o;
+    if (m >= e.split_row) {
+        out = e.out2;
+        m -= e.split_row;
+        row = (long long)m * e.ld_o2;
+    }
+    if (m >= e.rows_each) return;
+    if (e.out_f32) finish_linear8_as(e, (float *)out, row, m, n, count, z);
+    else finish_linear8_as(e, (__bf16 *)out, row, m, n, count, z);
 }
 
-__device__ __forceinline__ void finish_gated(const Epilogue &e, long long m, long long f, float g, float u)
+__device__ __forceinline__ void finish_gated8(const Epilogue &e, int m, int f, int count, const float (&g)[8], const float (&u)[8])
 {
     if (e.preact) {
-        e.preact[m * e.ld_p + 2 * f] = g;
-        e.preact[m * e.ld_p + 2 * f + 1] = u;
+        float *p = e.preact + (long long)m * e.ld_p + 2 * (long long)f;
+        const float lo[8] = {g[0], u[0], g[1], u[1], g[2], u[2], g[3], u[3]}, hi[8] = {g[4], u[4], g[5], u[5], g[6], u[6], g[7], u[7]};
+        store8(p, 2 * count, e.vec, lo);
+        store8(p + 8, 2 * count - 8, e.vec, hi);
     }
-    write_as(e.out, m * e.ld_o + f, e.out_f32, activate(g, e.act) * u);
+    float h[8];
+#pragma unroll
+    for (int i = 0; i < 8; ++i) h[i] = activate(g[i], e.act) * u[i];
+    const long long at = (long long)m * e.ld_o + f;
+    if (e.out_f32) store8((float *)e.out + at, count, e.vec, h);
+    else store8((__bf16 *)e.out + at, count, e.vec, h);
 }
 
-// sum over k of a(m, k) b(n, k), plus the same of a2 and b2 where there are two pairs; GATED: the sums with b and with b2
-// apart.  One 64 x 64 tile per workgroup, 4 x 4 sums per thread.
+// One operand of a product on the matrix cores.
+struct Side {
+    const unsigned char *p, *p2;    // p2: the gated block's second weight
+    const uint8_t *scale, *scale2;  // 8-bit elements: scale bytes, four to a stage
+    long long pitch;                // bytes from row to row (k contiguous) or from k to k (rows contiguous)
+    long long scale_pitch;
+    int extent;                     // rows of this side; rows contiguous: what may be read of them, a multiple of 8
+};
+
+// k runs through `count` segments of `stages` stages each (fp32: pairs of pieces; two summed products: the pairs).
+constexpr int MAX_SEGMENTS = 12;
+struct Segments {
+    int count, stages;
+    int rem;                        // how many k there are in a segment's last stage; 0: all of it
+    long long a[MAX_SEGMENTS], b[MAX_SEGMENTS];     // byte offsets of the segments' first elements
+};
+
+// fp32 factors as their pieces, to go back to where the pieces' products say nothing: an infinity times a piece that is
+// zero is a NaN.
+struct Pieces3 {
+    const __bf16 *a[2], *b[2];      // per pair; null: not an fp32 product
+    long long a_plane, b_plane, a_row, a_k, b_row, b_k;
+    int pairs, K;
+};
+
+__device__ __forceinline__ float whole(const __bf16 *p, long long plane)
+{
+    return ((float)p[2 * plane] + (float)p[plane]) + (float)p[0];
+}
+
+__device__ __forceinline__ float plain_dot(const Pieces3 &x, int which, int m, int n)
+{
+    float s = 0.f;
+    for (int pair = 0; pair < x.pairs; ++pair) {
+        const __bf16 *a = x.a[pair] + m * x.a_row, *b = (which ? x.b[1] : x.b[pair]) + n * x.b_row;
+        for (int k = 0; k < x.K; ++k) s = fmaf(whole(a + k * x.a_k, x.a_plane), whole(b + k * x.b_k, x.b_plane), s);
+    }
+    return s;
+}
+
+__device__ __forceinline__ void mend8(const Pieces3 &x, int which, int m, int n, int count, float (&z)[8])
+{
+#pragma unroll 1
+    for (int i = 0; i < 8; ++i) {
+        float v = 0.f;
+#pragma unroll
+        for (int j = 0; j < 8; ++j) v = i == j ? z[j] : v;
+        if (i < count && !(fabsf(v) <= 3.402823466e38f)) {
+            v = plain_dot(x, which, m, n + i);
+#pragma unroll
+            for (int j = 0; j < 8; ++j) z[j] = i == j ? v : z[j];
+        }
+    }
+}
+__device__ __forceinline__ bool all_finite(const float (&z)[8])
+{
+    float m = 0.f;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) m = fmaf(z[i], 0.f, m);
+    return m == 0.f;
+}
+
+// ---------------------------------------------------------------------------------------------------------------------------
+// The tile kernel.  A workgroup of four waves (2 x 2) computes a tile of 2 WT x 2 WT sums, each wave WT x WT of them as
+// MFMA blocks of 32 x 32; WT = 128 fills a lane's 256 accumulators (one workgroup to a compute unit), WT = 64 takes
+// a quarter of that (two workgroups to a compute unit).
+//
+// Operands go from global memory straight into LDS (lane L's 16 bytes land at base + 16 L), 128 bytes of k per row and
+// stage, two stages.  k contiguous: the 16-byte chunk c of row r sits at chunk c ^ ((r >> 1) & 7) of the row's 128 bytes,
+// which spreads the 16 rows that one pass of a ds_read_b128 touches over all banks.  Rows contiguous: a stage is 64 lines of k, and
+// ds_read_b64_tr_b16 turns 4 x 16 elements round on their way to the registers; the 64-byte block b of line k
+// sits at block b ^ f(k), so that the lines that one such read touches at once lie in different banks.
+//
+// The loads are inline asm whose completion is awaited by vmcnt, since the compiler would wait for all of them at every barrier.  A
+// stage is four k sub-steps (8 bits: two of twice the k); fragments are read one sub-step ahead, the barrier that
+// frees the stage's buffer sits early in sub-step 2, and the loads of stage s+2 are spread over what follows of stage s.
+// ---------------------------------------------------------------------------------------------------------------------------
+namespace tile {
+
+constexpr int THREADS = 256;
+constexpr int LINE = 128;
+
+enum { K_RUNS = 0, ROWS_RUN = 1 };      // which of an operand's extents is contiguous
+enum { TO_LINEAR = 0, TO_GATED = 1, TO_PARTS = 2, TO_GATED_PARTS = 3 };
+
+template <int WT, bool MX> struct Shape {
+    static constexpr int T = 2 * WT, NB = WT / 32;
+    static constexpr int HALF = T * LINE;                       // bytes of one operand and stage
+    static constexpr int SCALES = MX ? 2 * T * 4 : 0;           // four scale bytes per row
+    static constexpr int STAGE = 2 * HALF + SCALES;
+    static constexpr int NLOAD = 2 * HALF / (THREADS * 16);     // per lane and stage
+    static constexpr int NSCALE = SCALES / (THREADS * 4);
+    static constexpr int LDS_BYTES = 2 * STAGE;
+    static constexpr int TURN_PITCH = WT + 4;                   // floats
+    static_assert(4 * 32 * TURN_PITCH * 4 <= LDS_BYTES, "the waves' turn-round regions fit where the stages were");
+};
+
+// (M0 holds the LDS address; the instruction may follow M0's write only after a wait state)
+__device__ __forceinline__ void load16_to_lds(const void *base, unsigned offset, unsigned lds_addr)
+{
+    asm volatile("s_nop 0\n\t"
+                 "global_load_lds_dwordx4 %0, %1"
+                 :
+                 : "v"(offset), "s"(base), "{m0}"(lds_addr)
+                 : "memory");
+}
+__device__ __forceinline__ void load4_to_lds(const void *base, unsigned offset, unsigned lds_addr)
+{
+    asm volatile("s_nop 0\n\t"
+                 "global_load_lds_dword %0, %1"
+                 :
+                 : "v"(offset), "s"(base), "{m0}"(lds_addr)
+                 : "memory");
+}
+template <int N> __device__ __forceinline__ void wait_loads() { asm volatile("s_waitcnt vmcnt(%0)" ::"n"(N) : "memory"); }
+__device__ __forceinline__ void wait_lds() { asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory"); }
+__device__ __forceinline__ void pin() { __builtin_amdgcn_sched_barrier(0); }
+
+typedef short s16x4 __attribute__((ext_vector_type(4)));
+typedef short s16x8 __attribute__((ext_vector_type(8)));
+
+template <int WT, int KA, int KB, bool MX, bool GATED>
+struct Pipe {
+    using S = Shape<WT, MX>;
+    static constexpr int NB = S::NB, NM = NB * NB, T = S::T;
+    static constexpr int MINE = S::NLOAD;      // this wave's loads: half of one operand's stage
+    unsigned char *lds;
+    unsigned lds_base, wave_dst, scale_dst;
+    unsigned off[S::NLOAD];                    // byte offset of this lane's chunk from the stage's base
+    unsigned soff[MX ? S::NSCALE : 1];
+    bool loads_a;                              // waves 0 and 1 load a, 2 and 3 b
+    const unsigned char *base, *base2;         // the next stage to load (base2: the gated block's second weight)
+    const unsigned char *sbase, *sbase2;
+    const unsigned char *p, *p2, *sp, *sp2;    // this wave's operand at this tile, without its segment's offset
+    long long step;                            // bytes from stage to stage
+    int seg, left;                             // segment of the next stage to load, its stages left
+    int frag_a, frag_b, sw16, hi16;            // k contiguous: this lane's row, swizzle and k half
+    int blk_a[NB], blk_b[NB];                  // rows contiguous: its block offsets
+    f32x16 acc[NB][NB];                        // [block of a's rows][block of b's rows]; a lane holds one row of a
+
+    static __device__ __forceinline__ int line_swizzle(int k) { return T == 256 ? ((k & 3) | (((k >> 3) & 1) << 2)) : (k & 3); }
+
+    // Where load u of this lane comes from, inside the stage: row (or line of k) and 16-byte chunk of it.
+    template <int KIND> static __device__ __forceinline__ void slot(int half, int u, int lane, int *row, int *chunk)
+    {
+        const int ci = (half * S::NLOAD + u) * 64 + lane;
+        if constexpr (KIND == K_RUNS) {
+            *row = ci >> 3;
+            *chunk = (ci & 7) ^ ((*row >> 1) & 7);
+        } else {
+            constexpr int PER = T / 8;
+            *row = ci / PER;
+            const int pos = ci % PER;
+            *chunk = ((((pos >> 2) ^ line_swizzle(*row)) << 2) | (pos & 3));
+        }
+    }
+    template <int KIND> __device__ __forceinline__ void place(const Side &s, int tile0, int half, int lane, bool dual)
+    {
+#pragma unroll
+        for (int u = 0; u < S::NLOAD; ++u) {
+            int row, chunk;
+            slot<KIND>(half, u, lane, &row, &chunk);
+            if constexpr (KIND == K_RUNS) {
+                int r = row;
+                if (dual) r = (row / WT) * (WT / 2) + ((row % WT) >> 6) * 32 + (row & 31);     // 32 rows of the gate, 32 of the other, ...
+                r = min(tile0 + r, s.extent - 1) - tile0;
+                off[u] = (unsigned)((long long)r * s.pitch + chunk * 16);
+            } else {
+                const int c = min(tile0 / 8 + chunk, s.extent / 8 - 1) - tile0 / 8;
+                off[u] = (unsigned)((long long)row * s.pitch + c * 16);
+            }
+        }
+        const long long shift = KIND == K_RUNS ? (long long)tile0 * s.pitch : (long long)tile0 * 2;
+        p = s.p + shift;
+        p2 = dual ? s.p2 + shift : p;
+        step = KIND == K_RUNS ? LINE : 64 * s.pitch;
+        if constexpr (MX) {
+#pragma unroll
+            for (int v = 0; v < S::NSCALE; ++v) {
+                const int row = (half * S::NSCALE + v) * 64 + lane;
+                int r = row;
+                if (dual) r = (row / WT) * (WT / 2) + ((row % WT) >> 6) * 32 + (row & 31);
+                r = min(tile0 + r, s.extent - 1) - tile0;
+                soff[v] = (unsigned)((long long)r * s.scale_pitch);
+                if (dual && ((row >> 5) & 1)) soff[v] |= 0x80000000u;      // (marks the second weight's rows)
+            }
+            sp = s.scale + (long long)tile0 * s.scale_pitch;
+            sp2 = dual ? s.scale2 + (long long)tile0 * s.scale_pitch : sp;
+        }
+    }
+    __device__ __forceinline__ void init(unsigned char *lds_, const Side &a, const Side &b, int m0, int n0)
+    {
+        lds = lds_;
+        const int tid = threadIdx.x, lane = tid & 63;
+        const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+        const int wr = wave >> 1, wc = wave & 1;
+        lds_base = (unsigned)(size_t)(__attribute__((address_space(3))) unsigned char *)lds;
+        wave_dst = lds_base + wave * (S::NLOAD * 1024);
+        scale_dst = lds_base + 2 * S::HALF + wave * (S::NSCALE * 256);
+        loads_a = wave < 2;
+        if (loads_a) place<KA>(a, m0, wave & 1, lane, false);
+        else place<KB>(b, n0, wave & 1, lane, GATED);
+        sw16 = ((lane & 31) >> 1 & 7) << 4;        // (fragment rows differ from lane & 31 by multiples of 32)
+        hi16 = (lane >> 5) << 4;
+        frag_a = (wr * WT + (lane & 31)) * LINE;
+        frag_b = S::HALF + (wc * WT + (lane & 31)) * LINE;
+        const int i16 = lane & 15, f = T == 256 ? ((i16 >> 2) | ((lane >> 5) << 2)) : (i16 >> 2);
+        const int inside = ((lane >> 5) * 8 + (i16 >> 2)) * (T * 2) + ((lane >> 4) & 1) * 32 + (i16 & 3) * 8;
+#pragma unroll
+        for (int i = 0; i < NB; ++i) {
+            blk_a[i] = inside + (((wr * NB + i) ^ f) << 6);
+            blk_b[i] = S::HALF + inside + (((wc * NB + i) ^ f) << 6);
+        }
+    }
+    // The base of stage `stage` (of all segments end to end) becomes the next one to load.
+    __device__ __forceinline__ void seek(const Segments &g, int stage)
+    {
+        seg = stage / g.stages;
+        const int in = stage - seg * g.stages;
+        left = g.stages - in;
+        const long long o = (loads_a ? g.a[seg] : g.b[seg]) + (long long)in * step;
+        base = p + o;
+        base2 = p2 + o;
+        if constexpr (MX) {
+            sbase = sp + in * 4;
+            sbase2 = sp2 + in * 4;
+        }
+    }
+    __device__ __forceinline__ void advance(const Segments &g)
+    {
+        if (--left == 0) {
+            seg = min(seg + 1, g.count - 1);
+            left = g.stages;
+            const long long o = loads_a ? g.a[seg] : g.b[seg];
+            base = p + o;
+            base2 = p2 + o;
+        } else {
+            base += step;
+            base2 += step;
+            if constexpr (MX) {
+                sbase += 4;
+                sbase2 += 4;
+            }
+        }
+    }
+    // Load u of the next stage into buffer buf.  TAIL: only the stage's first `rem` k; the rest of it becomes zeros.
+    template <bool TAIL> __device__ __forceinline__ void load1(int buf, int u, int rem)
+    {
+        const unsigned char *from = GATED && ((u >> 2) & 1) ? base2 : base;
+        const unsigned to = wave_dst + buf * S::STAGE + u * 1024;
+        if constexpr (!TAIL) {
+            load16_to_lds(from, off[u], to);
+        } else {
+            const int lane = threadIdx.x & 63, half = (threadIdx.x >> 6) & 1;
+            int row, chunk;
+            bool there;
+            constexpr int ESZ = MX ? 1 : 2;
+            if (loads_a) {
+                slot<KA>(half, u, lane, &row, &chunk);
+                there = KA == K_RUNS ? chunk * 16 < rem * ESZ : row < rem;
+            } else {
+                slot<KB>(half, u, lane, &row, &chunk);
+                there = KB == K_RUNS ? chunk * 16 < rem * ESZ : row < rem;
+            }
+            if (there) load16_to_lds(from, off[u], to);
+            else *reinterpret_cast<uint4 *>(lds + (to - lds_base) + lane * 16) = make_uint4(0, 0, 0, 0);
+        }
+    }
+    __device__ __forceinline__ void load_scales(int buf)
+    {
+        if constexpr (MX) {
+#pragma unroll
+            for (int v = 0; v < S::NSCALE; ++v) {
+                const unsigned to = scale_dst + buf * S::STAGE + v * 256;
+                if (GATED && !loads_a) {
+                    if (soff[v] & 0x80000000u) load4_to_lds(sbase2, soff[v] & 0x7fffffffu, to);
+                    else load4_to_lds(sbase, soff[v], to);
+                } else {
+                    load4_to_lds(sbase, soff[v], to);
+                }
+            }
+        }
+    }
+
+    struct Frags { uint4 v[2 * NB]; };          // v[0 .. NB-1]: a's blocks, v[NB ..]: b's
+    // fragment i of k sub-step h (0 .. 3)
+    __device__ __forceinline__ void read1(Frags &f, int buf, int h, int i)
+    {
+        const unsigned char *stage = lds + buf * S::STAGE;
+        const bool of_a = i < NB;
+        const int kind = of_a ? KA : KB, blk = of_a ? i : i - NB;
+        if (kind == K_RUNS) {
+            // sub-step h is 32 bytes of k, lanes 0-31 take the first half
+            const int pos = h * 32 + hi16;
+            f.v[i] = *reinterpret_cast<const uint4 *>(stage + (of_a ? frag_a : frag_b) + blk * 32 * LINE + (pos ^ sw16));
+        } else {
+            typedef __attribute__((address_space(3))) s16x4 *lds_ptr;
+            unsigned char *at = const_cast<unsigned char *>(stage) + (of_a ? blk_a[blk] : blk_b[blk]) + h * 16 * (T * 2);
+            const s16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_ptr)at);
+            const s16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_ptr)(at + 4 * (T * 2)));
+            const s16x8 both = __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7);
+            f.v[i] = __builtin_bit_cast(uint4, both);
+        }
+    }
+    struct Frags8 { i32x8 v[2 * NB]; };         // 8 bits: both halves of a pair of sub-steps (0 and 1, or 2 and 3)
+    template <int HALF> __device__ __forceinline__ void read8(Frags8 &f, int buf, int pair, int i)
+    {
+        // a lane holds chunk (lane >> 5) of each of a pair of scale blocks
+        const unsigned char *stage = lds + buf * S::STAGE;
+        const int pos = (pair * 64 + HALF * 32 + hi16) ^ sw16;
+        const uint4 v = *reinterpret_cast<const uint4 *>(stage + (i < NB ? frag_a + i * 32 * LINE : frag_b + (i - NB) * 32 * LINE) + pos);
+        f.v[i][HALF * 4] = (int)v.x;
+        f.v[i][HALF * 4 + 1] = (int)v.y;
+        f.v[i][HALF * 4 + 2] = (int)v.z;
+        f.v[i][HALF * 4 + 3] = (int)v.w;
+    }
+    // this lane's scale words of a stage: two bytes each, byte 0 for its block of sub-steps 0/1, byte 2 for that of 2/3
+    struct Words { int v[2 * NB]; };
+    __device__ __forceinline__ void read_scale(Words &w, int buf, int i)
+    {
+        const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+        const int row = i < NB ? (wave >> 1) * WT + i * 32 + (lane & 31) : T + (wave & 1) * WT + (i - NB) * 32 + (lane & 31);
+        const unsigned word = *reinterpret_cast<const unsigned *>(lds + buf * S::STAGE + 2 * S::HALF + row * 4);
+        w.v[i] = (int)(word >> ((lane >> 5) * 8));
+    }
+
+    // The multiplies of one sub-step (8 bits: of two), b's rows down a block's registers, a's across its lanes.  hook(i)
+    // runs right behind the i-th.
+    template <typename Hook> __device__ __forceinline__ void multiply(const Frags &f, Hook hook)
+    {
+#pragma unroll
+        for (int i = 0; i < NB; ++i)
+#pragma unroll
+            for (int j = 0; j < NB; ++j) {
+                acc[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, f.v[NB + j]),
+                                                                    __builtin_bit_cast(bf16x8, f.v[i]), acc[i][j], 0, 0, 0);
+                pin();
+                hook(i * NB + j);
+                pin();
+            }
+    }
+    template <int SEL, typename Hook> __device__ __forceinline__ void multiply8(const Frags8 &f, const Words &w, Hook hook)
+    {
+#pragma unroll
+        for (int i = 0; i < NB; ++i)
+#pragma unroll
+            for (int j = 0; j < NB; ++j) {
+                acc[i][j] = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(f.v[NB + j], f.v[i], acc[i][j], 0, 0, SEL, w.v[NB + j],
+                                                                            SEL, w.v[i]);
+                // (keeps the multiply where it stands: this instruction alone may be moved across a branch)
+                if constexpr (WT == 128) asm volatile("" : "+a"(acc[i][j]));
+                else asm volatile("" : "+v"(acc[i][j]));
+                pin();
+                hook(i * NB + j);
+                pin();
+            }
+    }
+
+    // All of stages s0 .. s1 - 1.  Ends with a barrier: LDS is free in every wave.
+    __device__ __forceinline__ void run(const Segments &g, int s0, int s1)
+    {
+        constexpr int ALL = S::NLOAD + S::NSCALE;
+#pragma unroll
+        for (int i = 0; i < NB; ++i)
+#pragma unroll
+            for (int j = 0; j < NB; ++j)
+#pragma unroll
+                for (int r = 0; r < 16; ++r) acc[i][j][r] = 0.f;
+        const int n = s1 - s0;
+        seek(g, s0);
+        auto fill = [&](int buf) {
+            load_scales(buf);
+            if (g.rem != 0 && left == 1) {
+#pragma unroll
+                for (int u = 0; u < S::NLOAD; ++u) load1<true>(buf, u, g.rem);
+            } else {
+#pragma unroll
+                for (int u = 0; u < S::NLOAD; ++u) load1<false>(buf, u, 0);
+            }
+            advance(g);
+        };
+        fill(0);
+        if (n > 1) {
+            // (a tail's loads may be fewer than ALL: then all of them are awaited)
+            const bool exact = !(g.rem != 0 && left == 1);
+            fill(1);
+            if (exact) wait_loads<ALL>();
+            else wait_loads<0>();
+        } else {
+            wait_loads<0>();
+        }
+        wait_lds();
+        __builtin_amdgcn_s_barrier();
+        Frags f0, f1, f2, f3;
+        Frags8 p0, p1;
+        Words w, wn;
+#pragma unroll
+        for (int i = 0; i < 2 * NB; ++i) {
+            if constexpr (MX) {
+                read8<0>(p0, 0, 0, i);
+                read8<1>(p0, 0, 0, i);
+                read_scale(w, 0, i);
+            } else {
+                read1(f0, 0, 0, i);
+            }
+        }
+        int buf = 0;
+        constexpr int WAIT = NM / 4 - 1;                        // the multiply behind which the buffer is given up
+        constexpr int PER = (2 * NB + NM - 1) / NM;             // reads of a sub-step's fragments per multiply
+        auto nothing = [](int) {};
+        auto stage = [&](auto more_tag, auto refill_tag) {
+            constexpr bool MORE = decltype(more_tag)::value;
+            constexpr bool REFILL = decltype(refill_tag)::value;    // a whole stage s+2 takes this stage's buffer
+            auto reads = [&](Frags &f, int b, int h, int from, int count) {
+#pragma unroll
+                for (int i = 0; i < count; ++i)
+                    if (from + i < 2 * NB) read1(f, b, h, from + i);
+            };
+            auto give_up = [&]() {
+                wait_loads<0>();
+                wait_lds();
+                __builtin_amdgcn_s_barrier();
+            };
+            // the refill's loads: `done` of them are out, `count` more
+            auto refill = [&](int done, int count) {
+#pragma unroll
+                for (int i = 0; i < count; ++i)
+                    if (done + i < S::NLOAD) load1<false>(buf, done + i, 0);
+            };
+            if constexpr (!MX) {
+                constexpr int EARLY = NM == 16 ? 6 : 3;         // loads behind sub-step 2's multiplies
+                multiply(f0, [&](int i) { reads(f1, buf, 1, i * PER, PER); });
+                multiply(f1, [&](int i) {
+                    constexpr int H = NM / 2;
+                    if (i < H) reads(f2, buf, 2, i * 2 * PER, 2 * PER);
+                    else reads(f3, buf, 3, (i - H) * 2 * PER, 2 * PER);
+                });
+                multiply(f2, [&](int i) {
+                    if (MORE && i == WAIT) give_up();
+                    if constexpr (REFILL) {
+                        if (NM == 16) {
+                            if (i > WAIT && (i & 1) == 0) refill((i - WAIT - 1) / 2, 1);
+                        } else if (i > WAIT) {
+                            refill(i - WAIT - 1, 1);
+                        }
+                    }
+                });
+                multiply(f3, [&](int i) {
+                    if constexpr (MORE) reads(f0, buf ^ 1, 0, i * PER, PER);
+                    if constexpr (REFILL) {
+                        if (NM == 16) refill(EARLY + i, i < S::NLOAD - EARLY ? 1 : 0);
+                        else refill(EARLY + i * 2, 2);
+                    }
+                });
+            } else {
+                multiply8<0>(p0, w, [&](int i) {
+                    constexpr int EACH = (4 * NB + NM - 1) / NM;
+#pragma unroll
+                    for (int k = 0; k < EACH; ++k) {
+                        const int r = i * EACH + k;
+                        if (r < 4 * NB) {
+                            if (r & 1) read8<1>(p1, buf, 1, r >> 1);
+                            else read8<0>(p1, buf, 1, r >> 1);
+                        }
+                    }
+                });
+                multiply8<2>(p1, w, [&](int i) {
+                    if (MORE && i == WAIT) give_up();
+                    if (i > WAIT) {
+                        constexpr int ROOM = NM - 1 - WAIT;
+                        const int at = i - WAIT - 1;
+                        if constexpr (MORE) {
+                            constexpr int EACH = (4 * NB + ROOM - 1) / ROOM;
+#pragma unroll
+                            for (int k = 0; k < EACH; ++k) {
+                                const int r = at * EACH + k;
+                                if (r < 4 * NB) {
+                                    if (r & 1) read8<1>(p0, buf ^ 1, 0, r >> 1);
+                                    else read8<0>(p0, buf ^ 1, 0, r >> 1);
+                                }
+                            }
+                            if (at < 2 * NB && ROOM >= 2 * NB) read_scale(wn, buf ^ 1, at);
+                            if (ROOM < 2 * NB && at == 0) {
+#pragma unroll
+                                for (int k = 0; k < 2 * NB; ++k) read_scale(wn, buf ^ 1, k);
+                            }
+                        }
+                        if constexpr (REFILL) {
+                            constexpr int EACH = (S::NLOAD + ROOM - 1) / ROOM;
+                            if (at == 0) load_scales(buf);
+                            refill(at * EACH, EACH);
+                        }
+                    }
+                });
+                w = wn;
+            }
+            if constexpr (REFILL) advance(g);
+            buf ^= 1;
+        };
+        using std::bool_constant;
+        int s = 0;
+#pragma unroll 1
+        for (;;) {
+            // as long as the stage to load is a whole one; a segment's short last stage is loaded behind its predecessor's
+            // multiplies, outside of this loop
+            int whole = n - 2 - s;
+            if (g.rem != 0) whole = min(whole, left - 1);
+#pragma unroll 1
+            for (; whole > 0; --whole, ++s) stage(bool_constant<true>{}, bool_constant<true>{});
+            if (s + 1 >= n) break;
+            const bool another = s + 2 < n;
+            stage(bool_constant<true>{}, bool_constant<false>{});
+            ++s;
+            if (another) fill(buf ^ 1);
+        }
+        stage(bool_constant<false>{}, bool_constant<false>{});
+        wait_lds();
+        __builtin_amdgcn_s_barrier();
+    }
+};
+
+// Tile number t of the list for workgroup w.  Workgroups are dealt round-robin to the 8 XCDs, each with an L2 of its own:
+// an XCD gets a contiguous run of the list, which walks the grid of tiles in bands of 8 tile rows, down the band first, so
+// that the workgroups that an XCD runs side by side share operand rows in its L2.
+__device__ __forceinline__ bool tile_of_workgroup(int w, int nwg, int tiles_m, int tiles_n, int splits, int *ti, int *tj, int *split)
+{
+    const int per = (nwg + 7) >> 3, tiles = tiles_m * tiles_n;
+    int t = (w & 7) * per + (w >> 3);
+    if (t >= tiles * splits) return false;
+    *split = t / tiles;
+    t -= *split * tiles;
+    constexpr int BAND = 8;
+    const int band = t / (BAND * tiles_n);
+    const int rows = min(BAND, tiles_m - band * BAND);
+    const int r = t - band * BAND * tiles_n;
+    *ti = band * BAND + r % rows;
+    *tj = r / rows;
+    return true;
+}
+
+struct Args {
+    Side a, b;
+    Segments seg;
+    Epilogue e;
+    Pieces3 pieces;
+    float *parts;                   // [split][M][parts_pitch], gated: g's columns, then u's from parts_half on
+    long long parts_pitch;
+    int parts_half;
+    int M, N;                       // N: output columns
+    int tiles_m, tiles_n, splits;
+};
+
+template <int WT, int KA, int KB, bool MX, int TO>
+__global__ void __launch_bounds__(THREADS, WT == 128 ? 1 : 2)
+k_tile(const Args x)
+{
+    constexpr bool GATED = TO == TO_GATED || TO == TO_GATED_PARTS;
+    using P = Pipe<WT, KA, KB, MX, GATED>;
+    using S = typename P::S;
+    extern __shared__ __attribute__((aligned(16))) unsigned char lds[];
+    int ti, tj, split;
+    if (!tile_of_workgroup((int)blockIdx.x, (int)gridDim.x, x.tiles_m, x.tiles_n, x.splits, &ti, &tj, &split)) return;
+    constexpr int COLS = GATED ? WT : 2 * WT;      // output columns of a tile
+    const int m0 = ti * S::T, n0 = tj * COLS;
+    const int all = x.seg.count * x.seg.stages;
+    const int s0 = (int)((long long)all * split / x.splits), s1 = (int)((long long)all * (split + 1) / x.splits);
+    P p;
+    p.init(lds, x.a, x.b, m0, n0);
+    p.run(x.seg, s0, s1);
+
+    // The sums, 32 rows of this wave at a time, are turned round in LDS (a region of its own for each wave), so that a
+    // lane gets eight neighbouring columns and everything behind them is whole 16-byte accesses.
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    float *turn = reinterpret_cast<float *>(lds) + wave * (32 * S::TURN_PITCH);
+    const int wm = m0 + (wave >> 1) * WT, wn = n0 + (wave & 1) * (COLS / 2);
+    constexpr int LANES = (GATED ? WT / 2 : WT) / 8, ROWS = 64 / LANES;      // lanes that share a row; rows per pass
+    const int c8 = lane % LANES, r0 = lane / LANES;
+    const int n = wn + c8 * 8, count = x.N - n;
+#pragma unroll
+    for (int i = 0; i < P::NB; ++i) {
+#pragma unroll
+        for (int j = 0; j < P::NB; ++j)
+#pragma unroll
+            for (int q = 0; q < 4; ++q) {
+                const f32x4 v = {p.acc[i][j][4 * q], p.acc[i][j][4 * q + 1], p.acc[i][j][4 * q + 2], p.acc[i][j][4 * q + 3]};
+                *reinterpret_cast<f32x4 *>(turn + (lane & 31) * S::TURN_PITCH + j * 32 + q * 8 + (lane >> 5) * 4) = v;
+            }
+        pin();
+#pragma unroll 2
+        for (int r = r0; r < 32; r += ROWS) {
+            const int m = wm + i * 32 + r;
+            const float *row = turn + r * S::TURN_PITCH;
+            if (m >= x.M || count <= 0) continue;
+            if constexpr (!GATED) {
+                float z[8];
+                load8(row + c8 * 8, 8, true, z);
+                if constexpr (TO == TO_PARTS) {
+                    store8(x.parts + ((size_t)split * x.M + m) * x.parts_pitch + n, 8, true, z);
+                } else {
+                    if (x.pieces.a[0] && !all_finite(z)) mend8(x.pieces, 0, m, n, count, z);
+                    finish_linear8(x.e, m, n, count, z);
+                }
+            } else {
+                float g[8], u[8];
+                load8(row + (c8 >> 2) * 64 + (c8 & 3) * 8, 8, true, g);
+                load8(row + (c8 >> 2) * 64 + 32 + (c8 & 3) * 8, 8, true, u);
+                if constexpr (TO == TO_GATED_PARTS) {
+                    float *to = x.parts + ((size_t)split * x.M + m) * x.parts_pitch + n;
+                    store8(to, 8, true, g);
+                    store8(to + x.parts_half, 8, true, u);
+                } else {
+                    if (x.pieces.a[0]) {
+                        if (!all_finite(g)) mend8(x.pieces, 0, m, n, count, g);
+                        if (!all_finite(u)) mend8(x.pieces, 1, m, n, count, u);
+                    }
+                    finish_gated8(x.e, m, n, count, g, u);
+                }
+            }
+        }
+        pin();
+    }
+}
+
+// The parts of a product whose k was split among workgroups, in order, and what becomes of their sum.
 template <bool GATED>
 __global__ void __launch_bounds__(256)
-k_product(const Operand a, const Operand b, const Operand a2, const Operand b2, int pairs, int M, int N, int K, const Epilogue e)
+k_join(const Args x)
 {
-    __shared__ float sa[16][65], sb[GATED ? 2 : 1][16][65];
-    const int tn = (N + 63) / 64;
-    const long long m0 = (long long)(blockIdx.x / tn) * 64, n0 = (long long)(blockIdx.x % tn) * 64;
-    const int tid = threadIdx.x, tx = tid & 15, ty = tid >> 4;
-    float acc[GATED ? 2 : 1][4][4] = {};
-    for (int pair = 0; pair < (GATED ? 1 : pairs); ++pair) {
-        const Operand &pa = pair ? a2 : a, &pb = pair ? b2 : b;
-        for (int k0 = 0; k0 < K; k0 += 16) {
-            for (int i = tid; i < 64 * 16; i += 256) {
-                const int k = i & 15, r = i >> 4;
-                const bool ink = k0 + k < K;
-                sa[k][r] = ink && m0 + r < M ? element(pa, m0 + r, k0 + k) : 0.f;
-                sb[0][k][r] = ink && n0 + r < N ? element(pb, n0 + r, k0 + k) : 0.f;
-                if constexpr (GATED) sb[1][k][r] = ink && n0 + r < N ? element(b2, n0 + r, k0 + k) : 0.f;
+    const int groups = (x.N + 7) / 8;
+    const long long all = (long long)x.M * groups, stride = (long long)x.M * x.parts_pitch;
+    for (long long t = (long long)blockIdx.x * 256 + threadIdx.x; t < all; t += (long long)gridDim.x * 256) {
+        const int m = (int)(t / groups), n = (int)(t % groups) * 8, count = x.N - n;
+        const float *p = x.parts + m * x.parts_pitch + n;
+        float z[8], u[8], v[8];
+        load8(p, 8, true, z);
+        if constexpr (GATED) load8(p + x.parts_half, 8, true, u);
+        for (int s = 1; s < x.splits; ++s) {
+            load8(p + s * stride, 8, true, v);
+#pragma unroll
+            for (int i = 0; i < 8; ++i) z[i] += v[i];
+            if constexpr (GATED) {
+                load8(p + s * stride + x.parts_half, 8, true, v);
+#pragma unroll
+                for (int i = 0; i < 8; ++i) u[i] += v[i];
             }
-            __syncthreads();
-#pragma unroll
-            for (int k = 0; k < 16; ++k)
-#pragma unroll
-                for (int s = 0; s < (GATED ? 2 : 1); ++s)
-#pragma unroll
-                    for (int i = 0; i < 4; ++i)
-#pragma unroll
-                        for (int j = 0; j < 4; ++j)
-                            acc[s][i][j] = fmaf(sa[k][ty * 4 + i], sb[s][k][tx + 16 * j], acc[s][i][j]);
-            __syncthreads();
         }
+        if (x.pieces.a[0]) {
+            if (!all_finite(z)) mend8(x.pieces, 0, m, n, count, z);
+            if constexpr (GATED)
+                if (!all_finite(u)) mend8(x.pieces, 1, m, n, count, u);
+        }
+        if constexpr (GATED) finish_gated8(x.e, m, n, count, z, u);
+        else finish_linear8(x.e, m, n, count, z);
     }
-    for (int i = 0; i < 4; ++i)
-        for (int j = 0; j < 4; ++j) {
-            const long long m = m0 + ty * 4 + i, n = n0 + tx + 16 * j;
-            if (m >= M || n >= N) continue;
-            if constexpr (GATED) finish_gated(e, m, n, acc[0][i][j], acc[1][i][j]);
-            else finish_linear(e, m, n, acc[0][i][j]);
-        }
 }
 
-// dz = dy act'(z) of a group of rows and the group's column sums of it.  A thread owns a column; grid = (ceil(N / 256), groups).
-template <typename T>
-__global__ void __launch_bounds__(256)
-k_slope(const T *__restrict__ dy, long long ld_dy, const float *__restrict__ z, long long ld_z, int act, int M, int N,
-        float *__restrict__ dz, float *__restrict__ part, long long part_pitch)
+} // namespace tile
+
+// ---- what goes before a product -------------------------------------------------------------------------------------------
+
+// An fp32 number as three bf16 that add up to it: each piece is the leading 8 bits of what is left, cut off (not rounded),
+// so that no piece of a finite number is infinite.  Of what is not finite the first piece says all.
+__device__ __forceinline__ void pieces_of(float v, __bf16 &a, __bf16 &b, __bf16 &c)
 {
-    const int n = blockIdx.x * 256 + threadIdx.x;
-    if (n >= N) return;
-    float sum = 0.f;
-    for (long long m = blockIdx.y; m < M; m += gridDim.y) {
-        float v = to_f32(dy[m * ld_dy + n]);
-        if (act != 0) {
+    const unsigned bits = __builtin_bit_cast(unsigned, v);
+    if (!(fabsf(v) <= 3.402823466e38f)) {
+        a = __builtin_bit_cast(__bf16, (unsigned short)((bits >> 16) | ((bits & 0x7fffffu) ? 0x40 : 0)));
+        b = c = (__bf16)0.f;
+        return;
+    }
+    const float hi = __builtin_bit_cast(float, bits & 0xffff0000u), r = v - hi;
+    const float mid = __builtin_bit_cast(float, __builtin_bit_cast(unsigned, r) & 0xffff0000u);
+    a = __builtin_bit_cast(__bf16, (unsigned short)(bits >> 16));
+    b = __builtin_bit_cast(__bf16, (unsigned short)(__builtin_bit_cast(unsigned, r) >> 16));
+    c = (__bf16)(r - mid);
+}
+
+// Eight values into a packed operand: bf16, or the three pieces in planes `plane` elements apart.
+template <int PLANES> __device__ __forceinline__ void put8(__bf16 *p, long long plane, const float (&v)[8])
+{
+    bf16x8 a, b, c;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+        if constexpr (PLANES == 1) {
+            a[i] = (__bf16)v[i];
+        } else {
+            __bf16 x, y, z;
+            pieces_of(v[i], x, y, z);
+            a[i] = x;
+            b[i] = y;
+            c[i] = z;
+        }
+    }
+    *reinterpret_cast<bf16x8 *>(p) = a;
+    if constexpr (PLANES == 3) {
+        *reinterpret_cast<bf16x8 *>(p + plane) = b;
+        *reinterpret_cast<bf16x8 *>(p + 2 * plane) = c;
+    }
+}
+
+// Rows laid out for the tile kernel: a pitch that is a multiple of 64 elements, zeros behind the columns, fp32 in its
+// pieces.  grid.y: which matrix.
+struct PackJob {
+    const void *src;
+    __bf16 *dst;
+    long long ld, pitch, plane;
+    int rows, cols;
+    bool vec;
+};
+struct PackJobs {
+    PackJob job[3];
+};
+template <typename T, int PLANES>
+__global__ void __launch_bounds__(256)
+k_pack(const PackJobs jobs)
+{
+    const PackJob &j = jobs.job[blockIdx.y];
+    const int groups = (int)(j.pitch / 8);
+    const long long all = (long long)j.rows * groups;
+    for (long long t = (long long)blockIdx.x * 256 + threadIdx.x; t < all; t += (long long)gridDim.x * 256) {
+        const long long row = t / groups;
+        const int col = (int)(t % groups) * 8;
+        float v[8];
+        load8((const T *)j.src + row * j.ld + col, j.cols - col, j.vec, v);
+        put8<PLANES>(j.dst + row * j.pitch + col, j.plane, v);
+    }
+}
+
+// The same for bytes (8-bit elements and their scales): `pitch` bytes to a row, zeros behind the columns.
+struct ByteJob {
+    const uint8_t *src;
+    uint8_t *dst;
+    long long ld, pitch;
+    int rows, cols;
+};
+struct ByteJobs {
+    ByteJob job[6];
+};
+__global__ void __launch_bounds__(256)
+k_pack_bytes(const ByteJobs jobs)
+{
+    const ByteJob &j = jobs.job[blockIdx.y];
+    const int groups = (int)(j.pitch / 4);
+    const long long all = (long long)j.rows * groups;
+    for (long long t = (long long)blockIdx.x * 256 + threadIdx.x; t < all; t += (long long)gridDim.x * 256) {
+        const long long row = t / groups;
+        const int col = (int)(t % groups) * 4;
+        const uint8_t *s = j.src + row * j.ld + col;
+        unsigned w = 0;
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+            if (col + i < j.cols) w |= (unsigned)s[i] << (8 * i);
+        *reinterpret_cast<unsigned *>(j.dst + row * j.pitch + col) = w;
+    }
+}
+
+// 8-bit rows as packed bf16 (exact).
+struct WidenJob {
+    const uint8_t *src, *scale;
+    __bf16 *dst;
+    long long ld, ld_scale, pitch;
+    int rows, cols;
+    bool vec;
+};
+struct WidenJobs {
+    WidenJob job[3];
+};
+__global__ void __launch_bounds__(256)
+k_widen(const WidenJobs jobs)
+{
+    const WidenJob &j = jobs.job[blockIdx.y];
+    const int groups = (int)(j.pitch / 8);
+    const long long all = (long long)j.rows * groups;
+    for (long long t = (long long)blockIdx.x * 256 + threadIdx.x; t < all; t += (long long)gridDim.x * 256) {
+        const long long row = t / groups;
+        const int col = (int)(t % groups) * 8, count = j.cols - col;
+        const uint8_t *s = j.src + row * j.ld + col;
+        uint2 w = make_uint2(0, 0);
+        if (j.vec && count >= 8) {
+            w = *reinterpret_cast<const uint2 *>(s);
+        } else {
+#pragma unroll
+            for (int i = 0; i < 8; ++i)
+                if (i < count) (i < 4 ? w.x : w.y) |= (unsigned)s[i] << (8 * (i & 3));
+        }
+        const float scale = count > 0 ? mx_scale(j.scale[row * j.ld_scale + col / MX_BLOCK]) : 0.f;
+        bf16x8 v = widen8(w.x, w.y, scale);
+        // (a NaN scale is no business of what lies behind the columns)
+#pragma unroll
+        for (int i = 0; i < 8; ++i) v[i] = i < count ? v[i] : (__bf16)0.f;
+        *reinterpret_cast<bf16x8 *>(j.dst + row * j.pitch + col) = v;
+    }
+}
+
+// dz = dy act'(z), packed, and its column sums over a group of rows.  A thread owns eight columns; `across` threads of a
+// workgroup lie side by side, the others take further rows.  grid = (column pieces, groups).
+struct SlopeArgs {
+    const void *dy;
+    const float *z;                 // preact; gated: g and u side by side
+    __bf16 *dz;                     // packed (null: column sums alone); gated: dg, and du `half` columns on
+    float *part;                    // [group][part_pitch], nullable
+    long long ld_dy, ld_z, pitch, plane, part_pitch;
+    int M, N, act, across, half;
+    bool vec;
+};
+template <typename T, int PLANES>
+__global__ void __launch_bounds__(256)
+k_slope(const SlopeArgs x)
+{
+    __shared__ float sums[256][9];
+    const int c = threadIdx.x % x.across, r = threadIdx.x / x.across, down = 256 / x.across;
+    const int n = (blockIdx.x * x.across + c) * 8, count = x.N - n;
+    float sum[8] = {};
+    if (n < x.pitch) {
+        for (long long m = (long long)blockIdx.y * down + r; m < x.M; m += (long long)gridDim.y * down) {
+            float v[8];
+            load8((const T *)x.dy + m * x.ld_dy + n, count, x.vec, v);
+            if (x.act != 0) {
+                float z[8];
+                load8(x.z + m * x.ld_z + n, count, x.vec, z);
+#pragma unroll
+                for (int i = 0; i < 8; ++i) {
+                    float value, slope;
+                    activate_both(z[i], x.act, &value, &slope);
+                    v[i] = i < count ? v[i] * slope : 0.f;
+                }
+            }
+#pragma unroll
+            for (int i = 0; i < 8; ++i) sum[i] += v[i];
+            if (x.dz) put8<PLANES>(x.dz + m * x.pitch + n, x.plane, v);
+        }
+    }
+    if (!x.part) return;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) sums[threadIdx.x][i] = sum[i];
+    __syncthreads();
+    if (r == 0 && count > 0) {
+        for (int k = 1; k < down; ++k)
+#pragma unroll
+            for (int i = 0; i < 8; ++i) sum[i] += sums[k * x.across + c][i];
+        store8(x.part + (size_t)blockIdx.y * x.part_pitch + n, 8, true, sum);
+    }
+}
+
+// dg = dh u act'(g) and du = dh act(g), packed side by side.
+template <typename T, int PLANES>
+__global__ void __launch_bounds__(256)
+k_gated_slope(const SlopeArgs x)
+{
+    const int c = threadIdx.x % x.across, r = threadIdx.x / x.across, down = 256 / x.across;
+    const int n = (blockIdx.x * x.across + c) * 8, count = x.N - n;
+    if (n >= x.half) return;
+    for (long long m = (long long)blockIdx.y * down + r; m < x.M; m += (long long)gridDim.y * down) {
+        float d[8], lo[8], hi[8], dg[8], du[8];
+        load8((const T *)x.dy + m * x.ld_dy + n, count, x.vec, d);
+        const float *s = x.z + m * x.ld_z + 2 * (long long)n;
+        load8(s, 2 * count, x.vec, lo);
+        load8(s + 8, 2 * count - 8, x.vec, hi);
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            const float g = i < 4 ? lo[2 * i] : hi[2 * i - 8], u = i < 4 ? lo[2 * i + 1] : hi[2 * i - 7];
             float value, slope;
-            activate_both(z[m * ld_z + n], act, &value, &slope);
-            v *= slope;
+            activate_both(g, x.act, &value, &slope);
+            dg[i] = i < count ? d[i] * u * slope : 0.f;
+            du[i] = i < count ? d[i] * value : 0.f;
         }
-        sum += v;
-        dz[m * N + n] = v;
-    }
-    if (part) part[(size_t)blockIdx.y * part_pitch + n] = sum;
-}
-
-// dg = dh u act'(g), du = dh act(g).
-template <typename T>
-__global__ void __launch_bounds__(256)
-k_gated_slope(const T *__restrict__ dh, long long ld_dh, const float *__restrict__ saved, int act, int M, int F,
-              float *__restrict__ dg, float *__restrict__ du)
-{
-    const int f = blockIdx.x * 256 + threadIdx.x;
-    if (f >= F) return;
-    for (long long m = blockIdx.y; m < M; m += gridDim.y) {
-        const float g = saved[2 * (m * F + f)], u = saved[2 * (m * F + f) + 1], d = to_f32(dh[m * ld_dh + f]);
-        float value, slope;
-        activate_both(g, act, &value, &slope);
-        dg[m * F + f] = d * u * slope;
-        du[m * F + f] = d * value;
+        put8<PLANES>(x.dz + m * x.pitch + n, x.plane, dg);
+        put8<PLANES>(x.dz + m * x.pitch + x.half + n, x.plane, du);
     }
 }
 
