@@ -457,6 +457,15 @@ SlopeCut slope_cut(int64_t M, int64_t cols)
     return c;
 }
 
+template <typename Go> void with_act_value(int act, Go go)
+{
+    using std::integral_constant;
+    if (act == RCD_ACT_NONE) go(integral_constant<int, 0>{});
+    else if (act == RCD_ACT_RELU) go(integral_constant<int, 1>{});
+    else if (act == RCD_ACT_SILU) go(integral_constant<int, 2>{});
+    else go(integral_constant<int, 3>{});
+}
+
 // Workspace of the linear backward call.
 struct LinearBack {
     __bf16 *dz;
@@ -728,8 +737,11 @@ int rcd_linear_backward(const void *dY_dev, int64_t ld_dy, const void *A_dev, in
         x.M = (int)M; x.N = (int)N; x.act = act; x.across = c.across;
         x.vec = rows_aligned(dY_dev, ld_dy, size_of(dt)) && (act == RCD_ACT_NONE || rows_aligned(preact_dev, ld_p, 4));
         const dim3 grid((unsigned)c.pieces, (unsigned)c.groups);
-        if (f32) hipLaunchKernelGGL((k_slope<float, 3>), grid, dim3(256), 0, stream, x);
-        else hipLaunchKernelGGL((k_slope<__bf16, 1>), grid, dim3(256), 0, stream, x);
+        with_act_value(act, [&](auto a) {
+            constexpr int A = decltype(a)::value;
+            if (f32) hipLaunchKernelGGL((k_slope<float, 3, A>), grid, dim3(256), 0, stream, x);
+            else hipLaunchKernelGGL((k_slope<__bf16, 1, A>), grid, dim3(256), 0, stream, x);
+        });
         ENC_HIP_TRY(hipGetLastError());
         if (dbias_dev) ENC_TRY(sum_columns(w.part, x.part_pitch, c.groups, N, dbias_dev, dt, stream));
     }
@@ -851,8 +863,11 @@ int rcd_gated_linear_backward(const void *dH_dev, int64_t ld_dh, const void *A_d
     x.M = (int)M; x.N = (int)F; x.act = act; x.across = c.across; x.half = (int)half;
     x.vec = rows_aligned(dH_dev, ld_dh, size_of(dt)) && rows_aligned(saved_dev, 2 * F, 4);
     const dim3 grid((unsigned)c.pieces, (unsigned)c.groups);
-    if (f32) hipLaunchKernelGGL((k_gated_slope<float, 3>), grid, dim3(256), 0, stream, x);
-    else hipLaunchKernelGGL((k_gated_slope<__bf16, 1>), grid, dim3(256), 0, stream, x);
+    with_act_value(act, [&](auto a) {
+        constexpr int A = decltype(a)::value;
+        if (f32) hipLaunchKernelGGL((k_gated_slope<float, 3, A>), grid, dim3(256), 0, stream, x);
+        else hipLaunchKernelGGL((k_gated_slope<__bf16, 1, A>), grid, dim3(256), 0, stream, x);
+    });
     ENC_HIP_TRY(hipGetLastError());
     Laid d;
     d.p = (const unsigned char *)dgu;

@@ -2,6 +2,7 @@
 #pragma once
 #include <hip/hip_runtime.h>
 #include <stdint.h>
+#include <type_traits>
 
 namespace enc {
 
@@ -67,36 +68,66 @@ __device__ __forceinline__ float exp_f32(float x)
     return fmaf(__builtin_amdgcn_exp2f(t), lost * 0.693147181f, __builtin_amdgcn_exp2f(t));
 }
 
-__device__ __forceinline__ float logistic(float z) { return 1.f / (1.f + exp_f32(-z)); }
-__device__ __forceinline__ float normal_cdf(float z) { return fmaf(0.5f, erff(z * 0.707106781f), 0.5f); }
+__device__ __forceinline__ float logistic(float z) { return __builtin_amdgcn_rcpf(1.f + exp_f32(-z)); }
+
+// Phi(z) and the density's e^(-z^2/2), which it is made of: erfc(x) = (a1 t + .. + a5 t^5) e^(-x^2) with
+// t = 1 / (1 + p x), x = |z| / sqrt 2, off by at most 1.5e-7 (Abramowitz and Stegun, 7.1.26); Phi to half of that.  No
+// branch, where a library's erf has two; an epilogue of gelu is as long as its instructions.
+__device__ __forceinline__ float normal_cdf(float z, float *bell)
+{
+    const float e = exp_f32(-0.5f * z * z);
+    const float t = __builtin_amdgcn_rcpf(fmaf(fabsf(z), 0.3275911f * 0.707106781f, 1.f));
+    float q = fmaf(t, 1.061405429f, -1.453152027f);
+    q = fmaf(t, q, 1.421413741f);
+    q = fmaf(t, q, -0.284496736f);
+    q = fmaf(t, q, 0.254829592f);
+    const float tail = 0.5f * t * q * e;
+    *bell = e;
+    return z < 0.f ? tail : 1.f - tail;
+}
 
 // act(z): 0 none, 1 relu, 2 silu, 3 gelu (rcd_act)
+template <int ACT> __device__ __forceinline__ float activate_as(float z)
+{
+    if (ACT == 0) return z;
+    if (ACT == 1) return z < 0.f ? 0.f : z;        // (a NaN stays one)
+    if (ACT == 2) return z * logistic(z);
+    float bell;
+    return z * normal_cdf(z, &bell);
+}
 __device__ __forceinline__ float activate(float z, int act)
 {
-    if (act == 0) return z;
-    if (act == 1) return z < 0.f ? 0.f : z;        // (a NaN stays one)
-    if (act == 2) return z * logistic(z);
-    return z * normal_cdf(z);
+    return act == 0 ? activate_as<0>(z) : act == 1 ? activate_as<1>(z) : act == 2 ? activate_as<2>(z) : activate_as<3>(z);
 }
 
 // act(z) and act'(z)
-__device__ __forceinline__ void activate_both(float z, int act, float *value, float *slope)
+template <int ACT> __device__ __forceinline__ void activate_both_as(float z, float *value, float *slope)
 {
-    if (act == 0) {
+    if (ACT == 0) {
         *value = z;
         *slope = 1.f;
-    } else if (act == 1) {
+    } else if (ACT == 1) {
         *value = z < 0.f ? 0.f : z;
         *slope = z > 0.f ? 1.f : 0.f;
-    } else if (act == 2) {
+    } else if (ACT == 2) {
         const float s = logistic(z);
         *value = z * s;
         *slope = s * fmaf(z, 1.f - s, 1.f);
     } else {
-        const float cdf = normal_cdf(z);
+        float bell;
+        const float cdf = normal_cdf(z, &bell);
         *value = z * cdf;
-        *slope = fmaf(z, 0.398942280f * exp_f32(-0.5f * z * z), cdf);
+        *slope = fmaf(z, 0.398942280f * bell, cdf);
     }
+}
+
+// Calls go(act as a constant): the choice once for many elements.
+template <typename Go> __device__ __forceinline__ void with_act(int act, Go go)
+{
+    if (act == 0) go(std::integral_constant<int, 0>{});
+    else if (act == 1) go(std::integral_constant<int, 1>{});
+    else if (act == 2) go(std::integral_constant<int, 2>{});
+    else go(std::integral_constant<int, 3>{});
 }
 
 // The block exponent e: the least power of two with amax <= 448 * 2^e, not below 2^-127.  448 = 1.75 * 2^8.

@@ -626,6 +626,224 @@ struct Args {
     int tiles_m, tiles_n, splits;
 };
 
+// One accumulator at the point of use.  WT = 128: read explicitly, so that the register allocator does not move all 256 of
+// them into ordinary registers at once, which leaves room for nothing else.
+template <int WT> __device__ __forceinline__ float accumulator(float a)
+{
+    if constexpr (WT != 128) return a;
+    float v;
+    asm("v_accvgpr_read_b32 %0, %1" : "=v"(v) : "a"(a));
+    return v;
+}
+
+// 32 rows of a wave's sums in LDS, and their way out.
+template <int WT, bool GATED> struct Band {
+    static constexpr int PITCH = WT + 4;
+    static constexpr int COLS = GATED ? WT / 2 : WT;        // output columns of the wave
+    float *turn;
+
+    // column c of the wave's: a gated wave has 32 of the gate, 32 of the other, ...
+    static __device__ __forceinline__ int at(int c) { return GATED ? (c >> 5) * 64 + (c & 31) : c; }
+
+    // the bare sums, four columns to a lane; rows and columns of `parts` reach to multiples of eight
+    __device__ __forceinline__ void parts(const Args &x, int split, int m, int n)
+    {
+        const int lane = threadIdx.x & 63;
+        constexpr int LANES = COLS / 4, ROWS = 64 / LANES;
+        const int c = (lane % LANES) * 4, r0 = lane / LANES;
+        if (n + c >= x.N) return;
+        float *to = x.parts + ((size_t)split * x.M + m) * x.parts_pitch + n + c;
+#pragma unroll
+        for (int k = 0; k < 32 / ROWS; ++k) {
+            const int r = r0 + k * ROWS;
+            if (m + r >= x.M) break;
+            *reinterpret_cast<f32x4 *>(to + r * x.parts_pitch) = *reinterpret_cast<const f32x4 *>(turn + r * PITCH + at(c));
+            if constexpr (GATED)
+                *reinterpret_cast<f32x4 *>(to + r * x.parts_pitch + x.parts_half) =
+                    *reinterpret_cast<const f32x4 *>(turn + r * PITCH + at(c) + 32);
+        }
+    }
+
+    // every check, eight columns to a lane
+    __device__ __forceinline__ void checked(const Args &x, int m, int n)
+    {
+        const int lane = threadIdx.x & 63;
+        constexpr int LANES = COLS / 8, ROWS = 64 / LANES;
+        const int c = (lane % LANES) * 8, count = x.N - n - c;
+        if (count <= 0) return;
+#pragma unroll 2
+        for (int r = lane / LANES; r < 32; r += ROWS) {
+            if (m + r >= x.M) break;
+            float z[8];
+            load8(turn + r * PITCH + at(c), 8, true, z);
+            if (x.pieces.a[0] && !all_finite(z)) mend8(x.pieces, 0, m + r, n + c, count, z);
+            if constexpr (GATED) {
+                float u[8];
+                load8(turn + r * PITCH + at(c) + 32, 8, true, u);
+                if (x.pieces.a[0] && !all_finite(u)) mend8(x.pieces, 1, m + r, n + c, count, u);
+                finish_gated8(x.e, m + r, n + c, count, z, u);
+            } else {
+                finish_linear8(x.e, m + r, n + c, count, z);
+            }
+        }
+    }
+
+    // whether all of the band's sums are finite (the same answer in every lane)
+    __device__ __forceinline__ bool finite()
+    {
+        const int lane = threadIdx.x & 63;
+        float zero = 0.f;
+#pragma unroll 4
+        for (int k = 0; k < 32 * WT / 256; ++k) {
+            const int at4 = k * 64 + lane;
+            const f32x4 v = *reinterpret_cast<const f32x4 *>(turn + at4 / (WT / 4) * PITCH + at4 % (WT / 4) * 4);
+            zero = fmaf(v[0], 0.f, zero);
+            zero = fmaf(v[1], 0.f, zero);
+            zero = fmaf(v[2], 0.f, zero);
+            zero = fmaf(v[3], 0.f, zero);
+        }
+        return !__any(!(zero == 0.f));
+    }
+
+    __device__ __forceinline__ void inside(const Epilogue &e, int m, int n)
+    {
+        if constexpr (GATED) {
+            if (e.preact) save_pairs(e, m, n);
+            if (e.out_f32) gated<float, 4>(e, m, n);
+            else gated<__bf16, 8>(e, m, n);
+        } else {
+            if (e.preact) save(e, m, n);
+            if (e.out_f32) linear<float, 4>(e, m, n);
+            else linear<__bf16, 8>(e, m, n);
+        }
+    }
+
+    // V consecutive elements, 16 bytes
+    template <typename T, int V> static __device__ __forceinline__ void get(const T *p, float (&v)[V])
+    {
+        typedef T vec __attribute__((ext_vector_type(V)));
+        const vec t = *reinterpret_cast<const vec *>(p);
+#pragma unroll
+        for (int i = 0; i < V; ++i) v[i] = (float)t[i];
+    }
+    template <typename T, int V> static __device__ __forceinline__ void put(T *p, const float (&v)[V])
+    {
+        typedef T vec __attribute__((ext_vector_type(V)));
+        vec t;
+#pragma unroll
+        for (int i = 0; i < V; ++i) t[i] = (T)v[i];
+        *reinterpret_cast<vec *>(p) = t;
+    }
+    // V sums of row r from column c (of the turned band) on
+    template <int V> __device__ __forceinline__ void sums(int r, int c, float (&z)[V])
+    {
+#pragma unroll
+        for (int h = 0; h < V; h += 4) {
+            const f32x4 t = *reinterpret_cast<const f32x4 *>(turn + r * PITCH + c + h);
+            z[h] = t[0]; z[h + 1] = t[1]; z[h + 2] = t[2]; z[h + 3] = t[3];
+        }
+    }
+
+    // z in fp32, for the backward call: read once, much later, so it passes by the caches
+    __device__ __forceinline__ void save(const Epilogue &e, int m, int n)
+    {
+        const int lane = threadIdx.x & 63;
+        constexpr int LANES = COLS / 4, ROWS = 64 / LANES;
+        const int c = (lane % LANES) * 4, r0 = lane / LANES;
+        float b[4] = {0.f, 0.f, 0.f, 0.f};
+        if (e.bias)
+            for (int i = 0; i < 4; ++i) b[i] = e.out_f32 ? ((const float *)e.bias)[n + c + i] : (float)((const __bf16 *)e.bias)[n + c + i];
+        float *to = e.preact + (long long)m * e.ld_p + n + c;
+#pragma unroll
+        for (int k = 0; k < 32 / ROWS; ++k) {
+            float z[4];
+            sums<4>(r0 + k * ROWS, c, z);
+            const f32x4 v = {z[0] + b[0], z[1] + b[1], z[2] + b[2], z[3] + b[3]};
+            __builtin_nontemporal_store(v, reinterpret_cast<f32x4 *>(to + (r0 + k * ROWS) * e.ld_p));
+        }
+    }
+    // g and u side by side, two pairs to a lane
+    __device__ __forceinline__ void save_pairs(const Epilogue &e, int m, int f)
+    {
+        const int lane = threadIdx.x & 63;
+        constexpr int LANES = COLS / 2, ROWS = 64 / LANES;
+        const int c = (lane % LANES) * 2, r0 = lane / LANES;
+        float *to = e.preact + (long long)m * e.ld_p + 2 * (f + c);
+#pragma unroll
+        for (int k = 0; k < 32 / ROWS; ++k) {
+            const float *from = turn + (r0 + k * ROWS) * PITCH + at(c);
+            const float2 g = *reinterpret_cast<const float2 *>(from), u = *reinterpret_cast<const float2 *>(from + 32);
+            const f32x4 v = {g.x, u.x, g.y, u.y};
+            __builtin_nontemporal_store(v, reinterpret_cast<f32x4 *>(to + (r0 + k * ROWS) * e.ld_p));
+        }
+    }
+
+    template <typename T, int V> __device__ __forceinline__ void linear(const Epilogue &e, int m, int n)
+    {
+        const int lane = threadIdx.x & 63;
+        constexpr int LANES = COLS / V, ROWS = 64 / LANES, R = 32 / ROWS;
+        const int c = (lane % LANES) * V, r0 = lane / LANES;
+        const bool second = m >= e.split_row;
+        T *out = (T *)(second ? e.out2 : e.out);
+        const long long ld = second ? e.ld_o2 : e.ld_o;
+        out += (long long)(m - (second ? e.split_row : 0) + r0) * ld + n + c;
+        const T *res = (const T *)e.residual + (long long)(m + r0) * e.ld_r + n + c;
+        typedef T vec __attribute__((ext_vector_type(V)));
+        vec t[R];
+        float z[R][V], b[V];
+        if (e.residual) {
+#pragma unroll
+            for (int k = 0; k < R; ++k) t[k] = *reinterpret_cast<const vec *>(res + k * ROWS * e.ld_r);
+        }
+        if (e.bias) get<T, V>((const T *)e.bias + n + c, b);
+#pragma unroll
+        for (int k = 0; k < R; ++k) sums<V>(r0 + k * ROWS, c, z[k]);
+        if (e.bias) {
+#pragma unroll
+            for (int k = 0; k < R; ++k)
+#pragma unroll
+                for (int i = 0; i < V; ++i) z[k][i] += b[i];
+        }
+        if (e.act != 0)
+            with_act(e.act, [&](auto a) {
+#pragma unroll
+                for (int k = 0; k < R; ++k)
+#pragma unroll
+                    for (int i = 0; i < V; ++i) z[k][i] = activate_as<decltype(a)::value>(z[k][i]);
+            });
+        if (e.residual) {
+#pragma unroll
+            for (int k = 0; k < R; ++k)
+#pragma unroll
+                for (int i = 0; i < V; ++i) z[k][i] += (float)t[k][i];
+        }
+#pragma unroll
+        for (int k = 0; k < R; ++k) put<T, V>(out + k * ROWS * ld, z[k]);
+    }
+
+    template <typename T, int V> __device__ __forceinline__ void gated(const Epilogue &e, int m, int f)
+    {
+        const int lane = threadIdx.x & 63;
+        constexpr int LANES = COLS / V, ROWS = 64 / LANES, R = 32 / ROWS;
+        const int c = (lane % LANES) * V, r0 = lane / LANES;
+        T *out = (T *)e.out + (long long)(m + r0) * e.ld_o + f + c;
+        with_act(e.act, [&](auto a) {
+            float g[R][V], u[R][V];
+#pragma unroll
+            for (int k = 0; k < R; ++k) {
+                sums<V>(r0 + k * ROWS, at(c), g[k]);
+                sums<V>(r0 + k * ROWS, at(c) + 32, u[k]);
+            }
+#pragma unroll
+            for (int k = 0; k < R; ++k) {
+#pragma unroll
+                for (int i = 0; i < V; ++i) g[k][i] = activate_as<decltype(a)::value>(g[k][i]) * u[k][i];
+                put<T, V>(out + k * ROWS * e.ld_o, g[k]);
+            }
+        });
+    }
+};
+
 template <int WT, int KA, int KB, bool MX, int TO>
 __global__ void __launch_bounds__(THREADS, WT == 128 ? 1 : 2)
 k_tile(const Args x)
@@ -645,54 +863,41 @@ k_tile(const Args x)
     p.run(x.seg, s0, s1);
 
     // The sums, 32 rows of this wave at a time, are turned round in LDS (a region of its own for each wave), so that a
-    // lane gets eight neighbouring columns and everything behind them is whole 16-byte accesses.
+    // lane gets neighbouring columns and everything behind them is whole 16-byte accesses, whole lines by the wave.  A
+    // tile that lies inside the result goes without checks, its loads ahead of its stores.
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-    float *turn = reinterpret_cast<float *>(lds) + wave * (32 * S::TURN_PITCH);
+    Band<WT, GATED> band;
+    band.turn = reinterpret_cast<float *>(lds) + wave * (32 * S::TURN_PITCH);
     const int wm = m0 + (wave >> 1) * WT, wn = n0 + (wave & 1) * (COLS / 2);
-    constexpr int LANES = (GATED ? WT / 2 : WT) / 8, ROWS = 64 / LANES;      // lanes that share a row; rows per pass
-    const int c8 = lane % LANES, r0 = lane / LANES;
-    const int n = wn + c8 * 8, count = x.N - n;
+    const bool own_rows = x.e.split_row == 0x7fffffff || m0 + S::T <= x.e.rows_each ||
+                          (m0 >= x.e.split_row && m0 - x.e.split_row + S::T <= x.e.rows_each);
+    const bool inside = m0 + S::T <= x.M && n0 + COLS <= x.N && x.e.vec && own_rows;
+    auto turn_round = [&](auto band_tag) {
+        constexpr int I = decltype(band_tag)::value;
+        if constexpr (I < P::NB) {
 #pragma unroll
-    for (int i = 0; i < P::NB; ++i) {
+            for (int j = 0; j < P::NB; ++j)
 #pragma unroll
-        for (int j = 0; j < P::NB; ++j)
+                for (int q = 0; q < 4; ++q) {
+                    f32x4 v;
 #pragma unroll
-            for (int q = 0; q < 4; ++q) {
-                const f32x4 v = {p.acc[i][j][4 * q], p.acc[i][j][4 * q + 1], p.acc[i][j][4 * q + 2], p.acc[i][j][4 * q + 3]};
-                *reinterpret_cast<f32x4 *>(turn + (lane & 31) * S::TURN_PITCH + j * 32 + q * 8 + (lane >> 5) * 4) = v;
-            }
-        pin();
-#pragma unroll 2
-        for (int r = r0; r < 32; r += ROWS) {
-            const int m = wm + i * 32 + r;
-            const float *row = turn + r * S::TURN_PITCH;
-            if (m >= x.M || count <= 0) continue;
-            if constexpr (!GATED) {
-                float z[8];
-                load8(row + c8 * 8, 8, true, z);
-                if constexpr (TO == TO_PARTS) {
-                    store8(x.parts + ((size_t)split * x.M + m) * x.parts_pitch + n, 8, true, z);
-                } else {
-                    if (x.pieces.a[0] && !all_finite(z)) mend8(x.pieces, 0, m, n, count, z);
-                    finish_linear8(x.e, m, n, count, z);
+                    for (int e = 0; e < 4; ++e) v[e] = accumulator<WT>(p.acc[I][j][4 * q + e]);
+                    *reinterpret_cast<f32x4 *>(band.turn + (lane & 31) * S::TURN_PITCH + j * 32 + q * 8 + (lane >> 5) * 4) = v;
                 }
-            } else {
-                float g[8], u[8];
-                load8(row + (c8 >> 2) * 64 + (c8 & 3) * 8, 8, true, g);
-                load8(row + (c8 >> 2) * 64 + 32 + (c8 & 3) * 8, 8, true, u);
-                if constexpr (TO == TO_GATED_PARTS) {
-                    float *to = x.parts + ((size_t)split * x.M + m) * x.parts_pitch + n;
-                    store8(to, 8, true, g);
-                    store8(to + x.parts_half, 8, true, u);
-                } else {
-                    if (x.pieces.a[0]) {
-                        if (!all_finite(g)) mend8(x.pieces, 0, m, n, count, g);
-                        if (!all_finite(u)) mend8(x.pieces, 1, m, n, count, u);
-                    }
-                    finish_gated8(x.e, m, n, count, g, u);
-                }
-            }
         }
+    };
+    // (a loop: unrolled, the code behind it would be there four times)
+#pragma unroll 1
+    for (int i = 0; i < P::NB; ++i) {
+        if (i == 0) turn_round(std::integral_constant<int, 0>{});
+        else if (i == 1) turn_round(std::integral_constant<int, 1>{});
+        else if (i == 2) turn_round(std::integral_constant<int, 2>{});
+        else turn_round(std::integral_constant<int, 3>{});
+        pin();
+        const int m = wm + i * 32;
+        if constexpr (TO == TO_PARTS || TO == TO_GATED_PARTS) band.parts(x, split, m, wn);
+        else if (inside && (!x.pieces.a[0] || band.finite())) band.inside(x.e, m, wn);
+        else band.checked(x, m, wn);
         pin();
     }
 }
@@ -879,7 +1084,7 @@ struct SlopeArgs {
     int M, N, act, across, half;
     bool vec;
 };
-template <typename T, int PLANES>
+template <typename T, int PLANES, int ACT>
 __global__ void __launch_bounds__(256)
 k_slope(const SlopeArgs x)
 {
@@ -891,13 +1096,13 @@ k_slope(const SlopeArgs x)
         for (long long m = (long long)blockIdx.y * down + r; m < x.M; m += (long long)gridDim.y * down) {
             float v[8];
             load8((const T *)x.dy + m * x.ld_dy + n, count, x.vec, v);
-            if (x.act != 0) {
+            if constexpr (ACT != 0) {
                 float z[8];
                 load8(x.z + m * x.ld_z + n, count, x.vec, z);
 #pragma unroll
                 for (int i = 0; i < 8; ++i) {
                     float value, slope;
-                    activate_both(z[i], x.act, &value, &slope);
+                    activate_both_as<ACT>(z[i], &value, &slope);
                     v[i] = i < count ? v[i] * slope : 0.f;
                 }
             }
@@ -919,7 +1124,7 @@ k_slope(const SlopeArgs x)
 }
 
 // dg = dh u act'(g) and du = dh act(g), packed side by side.
-template <typename T, int PLANES>
+template <typename T, int PLANES, int ACT>
 __global__ void __launch_bounds__(256)
 k_gated_slope(const SlopeArgs x)
 {
@@ -936,7 +1141,7 @@ k_gated_slope(const SlopeArgs x)
         for (int i = 0; i < 8; ++i) {
             const float g = i < 4 ? lo[2 * i] : hi[2 * i - 8], u = i < 4 ? lo[2 * i + 1] : hi[2 * i - 7];
             float value, slope;
-            activate_both(g, x.act, &value, &slope);
+            activate_both_as<ACT>(g, &value, &slope);
             dg[i] = i < count ? d[i] * u * slope : 0.f;
             du[i] = i < count ? d[i] * value : 0.f;
         }

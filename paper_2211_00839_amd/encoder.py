@@ -11,12 +11,13 @@ from typing import NamedTuple, Optional
 
 import torch
 
-from .binding import RcdError, _check, _dev_ptr, _stream, _workspace, load_library
+from .binding import RcdError, _check, _workspace, load_library
 
 _INVALID, _UNSUPPORTED = 1, 4
 _BLOCK = 32
 _ACTS = {"none": 0, "relu": 1, "silu": 2, "gelu": 3}
-_CODES = {torch.float32: 0, torch.bfloat16: 1, torch.float8_e4m3fn: 2}
+_F32, _BF16, _E4M3, _E8M0 = torch.float32, torch.bfloat16, torch.float8_e4m3fn, torch.float8_e8m0fnu
+_CODES = {_F32: 0, _BF16: 1, _E4M3: 2}
 
 
 class RmsNorm(NamedTuple):
@@ -31,102 +32,131 @@ def _refuse(what: str, status: int = _INVALID):
 
 
 def _act(act: str) -> int:
-    if act not in _ACTS:
+    code = _ACTS.get(act)
+    if code is None:
         _refuse("act must be one of %s" % ", ".join(_ACTS), _UNSUPPORTED)
-    return _ACTS[act]
+    return code
 
 
-def _matrix(name, t, rows=None, cols=None, dtype=None, like=None):
-    """t, checked: a device matrix with contiguous rows, of the sizes, type and device asked for."""
+# The checks are written for the good case: a call of a few microseconds is what a single sample takes, and attribute by
+# attribute they would cost as much as its kernel.  _why() looks again, for the message.
+
+def _first(name, t):
+    """(rows, columns, leading dimension, type, device index) of a call's first matrix, which the others have to match."""
+    if isinstance(t, torch.Tensor) and t.dim() == 2 and t.dtype in _CODES and t.is_cuda:
+        rows, cols = t.shape
+        ld, one = t.stride()
+        if (one == 1 or cols <= 1 or rows == 0) and (ld >= cols or rows <= 1):
+            device = t.get_device()
+            if device != torch.cuda.current_device():
+                _refuse("%s is on another device than the current one" % name)
+            return rows, cols, ld if rows > 1 else max(cols, 1), t.dtype, device
+    _why(name, t, None, None, None, None)
+
+
+def _other(name, t, rows, cols, dtype, device):
+    """The leading dimension of a matrix that has to be rows x cols (rows None: any)."""
+    if isinstance(t, torch.Tensor) and t.dtype is dtype and t.get_device() == device and t.dim() == 2:
+        n, d = t.shape
+        if (n == rows or rows is None) and d == cols:
+            ld, one = t.stride()
+            if (one == 1 or cols <= 1 or n == 0) and (ld >= cols or n <= 1):
+                return ld if n > 1 else max(cols, 1)
+    _why(name, t, rows, cols, dtype, device)
+
+
+def _why(name, t, rows, cols, dtype, device):
     if not isinstance(t, torch.Tensor) or t.dim() != 2:
         _refuse("%s must be a matrix" % name)
     if not t.is_cuda:
         _refuse("%s: device tensor expected (there is no CPU path)" % name, -1)
-    if (rows is not None and t.shape[0] != rows) or (cols is not None and t.shape[1] != cols):
-        _refuse("%s must be %s x %s, got %d x %d" % (name, rows, cols, t.shape[0], t.shape[1]))
-    if t.shape[1] > 1 and t.shape[0] > 0 and t.stride(1) != 1:
-        _refuse("the rows of %s must be contiguous" % name)
-    if t.shape[0] > 1 and t.stride(0) < t.shape[1]:
-        _refuse("the rows of %s overlap" % name)
     if t.dtype not in _CODES:
         _refuse("%s: float32, bfloat16 or float8_e4m3fn expected" % name, _UNSUPPORTED)
     if dtype is not None and t.dtype != dtype:
         _refuse("%s must be %s" % (name, dtype), _UNSUPPORTED)
-    if like is not None and t.device != like.device:
+    if device is not None and t.get_device() != device:
         _refuse("%s is on another device" % name)
-    return t
+    if (rows is not None and t.shape[0] != rows) or (cols is not None and t.shape[1] != cols):
+        _refuse("%s must be %s x %s, got %d x %d" % (name, "any" if rows is None else rows, cols, t.shape[0], t.shape[1]))
+    if t.shape[1] > 1 and t.stride(1) != 1:
+        _refuse("the rows of %s must be contiguous" % name)
+    _refuse("the rows of %s overlap" % name)
 
 
-def _vector(name, t, n, dtype, like):
+def _vector(name, t, n, dtype, device):
+    """The address of a contiguous vector, None for None."""
     if t is None:
         return None
-    if not isinstance(t, torch.Tensor) or t.dim() != 1 or t.shape[0] != n or not (t.is_contiguous() or n == 1):
+    if not isinstance(t, torch.Tensor) or t.dim() != 1 or t.shape[0] != n or not (n <= 1 or t.stride(0) == 1):
         _refuse("%s must be a contiguous vector of %d" % (name, n))
-    if t.dtype != dtype:
+    if t.dtype is not dtype:
         _refuse("%s must be %s" % (name, dtype), _UNSUPPORTED)
-    if t.device != like.device:
+    if t.get_device() != device:
         _refuse("%s is on another device" % name)
-    return t
+    return t.data_ptr()
 
 
-def _scale(name, t, of):
-    """The scales that belong to the 8-bit matrix `of` (None for any other type)."""
-    if of.dtype != torch.float8_e4m3fn:
+def _scale(name, t, dtype, rows, cols, device):
+    """(address, leading dimension) of the scales that belong to an 8-bit matrix; (None, 0) for any other type."""
+    if dtype is not _E4M3:
         if t is not None:
             _refuse("%s goes with float8_e4m3fn elements only" % name)
-        return None
-    blocks = -(-of.shape[1] // _BLOCK)
-    if not isinstance(t, torch.Tensor) or t.dtype not in (torch.uint8, torch.float8_e8m0fnu):
+        return None, 0
+    blocks = -(-cols // _BLOCK)
+    if not isinstance(t, torch.Tensor) or t.dtype not in (torch.uint8, _E8M0):
         _refuse("%s (uint8 or float8_e8m0fnu) is missing" % name)
-    if t.dim() != 2 or t.shape != (of.shape[0], blocks) or (blocks > 1 and t.shape[0] > 0 and t.stride(1) != 1):
-        _refuse("%s must be %d x %d with contiguous rows" % (name, of.shape[0], blocks))
-    if t.device != of.device:
+    if t.dim() != 2 or t.shape != (rows, blocks) or (blocks > 1 and rows > 0 and t.stride(1) != 1):
+        _refuse("%s must be %d x %d with contiguous rows" % (name, rows, blocks))
+    if rows > 1 and t.stride(0) < blocks:
+        _refuse("the rows of %s overlap" % name)
+    if t.get_device() != device:
         _refuse("%s is on another device" % name)
-    return t
+    return t.data_ptr(), t.stride(0) if rows > 1 else blocks
 
 
-def _ld(t) -> int:
-    """Row stride in elements (of one row it means nothing: its length)."""
-    if t is None:
-        return 0
-    return t.stride(0) if t.shape[0] > 1 else max(t.shape[1], 1)
+def _stream(device) -> int:
+    return torch._C._cuda_getCurrentRawStream(device)
 
 
-def _new(rows, cols, dtype, like):
-    return torch.empty((rows, cols), dtype=dtype, device=like.device)
-
-
-def _here(t):
-    """Calls run on the current device's stream: the tensors have to be there."""
-    if t.device.index != torch.cuda.current_device():
-        _refuse("tensors are on %s, the current device is another" % t.device)
-
-
-def _room(workspace, nbytes, like):
+def _room(workspace, nbytes, device):
+    """(tensor to hold on to, address, bytes) of a call's workspace."""
     if workspace is None:
-        return _workspace(nbytes, like.device)
-    if not workspace.is_cuda or not workspace.is_contiguous() or workspace.dtype != torch.uint8:
-        _refuse("the workspace must be a contiguous uint8 device tensor", 5)
-    return workspace
+        if nbytes == 0:
+            return None, None, 0
+        workspace = _workspace(nbytes, torch.device("cuda", device))
+    elif not workspace.is_cuda or not workspace.is_contiguous() or workspace.dtype != torch.uint8 or workspace.get_device() != device:
+        _refuse("the workspace must be a contiguous uint8 tensor on the device", 5)
+    return workspace, workspace.data_ptr(), workspace.numel()
+
+
+def _ptr(t):
+    return None if t is None else t.data_ptr()
 
 
 def rms_norm(x, weight=None, eps: float = 1e-6, residual=None, quantize: bool = False, want_sum: bool = False,
              want_rstd: bool = False) -> RmsNorm:
     """h = x + residual, y = h * rstd * weight with rstd = (mean h^2 + eps)^(-1/2) of each row.  quantize: y in 8 bits with
     scales.  want_sum: h too, rounded to x's type; want_rstd: what rms_norm_backward takes."""
-    _matrix("x", x)
-    _here(x)
-    rows, d = x.shape
-    if residual is not None:
-        _matrix("residual", residual, rows, d, x.dtype, x)
-    _vector("weight", weight, d, x.dtype, x)
-    y = _new(rows, d, torch.float8_e4m3fn if quantize else x.dtype, x)
-    scale = _new(rows, -(-d // _BLOCK), torch.float8_e8m0fnu, x) if quantize else None
-    total = _new(rows, d, x.dtype, x) if want_sum else None
-    rstd = torch.empty(rows, dtype=torch.float32, device=x.device) if want_rstd else None
-    _check(load_library().rcd_rms_norm(
-        _dev_ptr(x), _CODES[x.dtype], rows, d, _ld(x), _dev_ptr(residual), _ld(residual), _dev_ptr(weight), float(eps),
-        _dev_ptr(total), _ld(total), _dev_ptr(y), _CODES[y.dtype], _ld(y), _dev_ptr(scale), _ld(scale), _dev_ptr(rstd), _stream()))
+    rows, d, ld, dtype, device = _first("x", x)
+    ld_r = 0 if residual is None else _other("residual", residual, rows, d, dtype, device)
+    w = _vector("weight", weight, d, dtype, device)
+    scale = rstd = total = None
+    blocks = -(-d // _BLOCK)
+    if quantize:
+        y = x.new_empty((rows, d), dtype=_E4M3)
+        scale = x.new_empty((rows, blocks), dtype=_E8M0)
+    else:
+        y = x.new_empty((rows, d))
+    if want_sum:
+        total = x.new_empty((rows, d))
+    if want_rstd:
+        rstd = x.new_empty(rows, dtype=_F32)
+    code = _CODES[dtype]
+    status = load_library().rcd_rms_norm(
+        x.data_ptr(), code, rows, d, ld, _ptr(residual), ld_r, w, eps, _ptr(total), d, y.data_ptr(), 2 if quantize else code, d,
+        _ptr(scale), blocks, _ptr(rstd), _stream(device))
+    if status:
+        _check(status)
     return RmsNorm(y, scale, total, rstd)
 
 
@@ -134,42 +164,42 @@ def rms_norm_backward(dy, h, rstd, weight=None, dsum=None, want_dweight: bool = 
     """(dx, dweight) of rms_norm: h is its sum (x itself without a residual), rstd its rstd, dsum the gradient that reaches
     h along the residual stream.  dx is the residual's gradient too; dweight is None unless wanted."""
     lib = load_library()
-    _matrix("dy", dy)
-    _here(dy)
-    rows, d = dy.shape
-    _matrix("h", h, rows, d, dy.dtype, dy)
+    rows, d, ld, dtype, device = _first("dy", dy)
+    ld_h = _other("h", h, rows, d, dtype, device)
     if rstd is None:
         _refuse("rstd is missing")
-    _vector("rstd", rstd, rows, torch.float32, dy)
-    _vector("weight", weight, d, dy.dtype, dy)
-    if dsum is not None:
-        _matrix("dsum", dsum, rows, d, dy.dtype, dy)
-    dx = _new(rows, d, dy.dtype, dy)
-    dweight = torch.empty(d, dtype=dy.dtype, device=dy.device) if want_dweight else None
-    ws = _room(workspace, lib.rcd_rms_norm_backward_workspace_bytes(rows, d) if want_dweight else 0, dy)
-    _check(lib.rcd_rms_norm_backward(
-        _dev_ptr(dy), _CODES[dy.dtype], rows, d, _ld(dy), _dev_ptr(h), _ld(h), _dev_ptr(rstd), _dev_ptr(weight), _dev_ptr(dsum),
-        _ld(dsum), _dev_ptr(dx), _ld(dx), _dev_ptr(dweight), _dev_ptr(ws), ws.numel(), _stream()))
+    r, w = _vector("rstd", rstd, rows, _F32, device), _vector("weight", weight, d, dtype, device)
+    ld_s = 0 if dsum is None else _other("dsum", dsum, rows, d, dtype, device)
+    dx = dy.new_empty((rows, d))
+    dweight = dy.new_empty(d) if want_dweight else None
+    held, room, nbytes = _room(workspace, lib.rcd_rms_norm_backward_workspace_bytes(rows, d) if want_dweight else 0, device)
+    status = lib.rcd_rms_norm_backward(
+        dy.data_ptr(), _CODES[dtype], rows, d, ld, h.data_ptr(), ld_h, r, w, _ptr(dsum), ld_s, dx.data_ptr(), d, _ptr(dweight), room,
+        nbytes, _stream(device))
+    if status:
+        _check(status)
     return dx, dweight
 
 
 def quantize_mxfp8(x):
     """(float8_e4m3fn elements, float8_e8m0fnu scales) of the rows of x."""
-    _matrix("x", x)
-    _here(x)
-    rows, d = x.shape
-    q, scale = _new(rows, d, torch.float8_e4m3fn, x), _new(rows, -(-d // _BLOCK), torch.float8_e8m0fnu, x)
-    _check(load_library().rcd_quantize_mxfp8(_dev_ptr(x), _CODES[x.dtype], rows, d, _ld(x), _dev_ptr(q), _ld(q),
-                                             _dev_ptr(scale), _ld(scale), _stream()))
+    rows, d, ld, dtype, device = _first("x", x)
+    blocks = -(-d // _BLOCK)
+    q, scale = x.new_empty((rows, d), dtype=_E4M3), x.new_empty((rows, blocks), dtype=_E8M0)
+    _check(load_library().rcd_quantize_mxfp8(x.data_ptr(), _CODES[dtype], rows, d, ld, q.data_ptr(), d, scale.data_ptr(), blocks,
+                                             _stream(device)))
     return q, scale
 
 
-def _out_dtype(a, out_dtype):
+def _result(name, a, dtype, out_dtype, out, rows, cols, device):
+    """(tensor, its type, leading dimension) of a product's result."""
     if out_dtype is None:
-        return torch.bfloat16 if a.dtype == torch.float8_e4m3fn else a.dtype
-    if out_dtype not in (torch.float32, torch.bfloat16):
-        _refuse("out_dtype must be float32 or bfloat16", _UNSUPPORTED)
-    return out_dtype
+        out_dtype = (_BF16 if dtype is _E4M3 else dtype) if out is None else getattr(out, "dtype", None)
+    if out_dtype is not _F32 and out_dtype is not _BF16:
+        _refuse("the result must be float32 or bfloat16", _UNSUPPORTED)
+    if out is None:
+        return a.new_empty((rows, cols), dtype=out_dtype), out_dtype, cols
+    return out, out_dtype, _other("out", out, rows, cols, out_dtype, device)
 
 
 def linear(a, w, bias=None, act: str = "none", residual=None, a_scale=None, w_scale=None, out_dtype=None,
@@ -177,23 +207,22 @@ def linear(a, w, bias=None, act: str = "none", residual=None, a_scale=None, w_sc
     """act(a w^T + bias) + residual, a (M, K), w (N, K).  out may be the residual.  want_preact: (y, z), z = a w^T + bias in
     float32, what linear_backward takes."""
     lib = load_library()
-    _matrix("a", a)
-    _here(a)
-    M, K = a.shape
-    _matrix("w", w, None, K, a.dtype, a)
+    M, K, ld_a, dtype, device = _first("a", a)
+    ld_w = _other("w", w, None, K, dtype, device)
     N = w.shape[0]
-    a_scale, w_scale = _scale("a_scale", a_scale, a), _scale("w_scale", w_scale, w)
-    dt = _out_dtype(a, out_dtype) if out is None else out.dtype
-    _vector("bias", bias, N, dt, a)
-    if residual is not None:
-        _matrix("residual", residual, M, N, dt, a)
-    y = _new(M, N, dt, a) if out is None else _matrix("out", out, M, N, _out_dtype(a, out_dtype or dt), a)
-    z = _new(M, N, torch.float32, a) if want_preact else None
-    ws = _room(workspace, lib.rcd_linear_workspace_bytes(M, N, K, _CODES[a.dtype]), a)
-    _check(lib.rcd_linear(
-        _dev_ptr(a), _dev_ptr(a_scale), _ld(a), _ld(a_scale), _dev_ptr(w), _dev_ptr(w_scale), _ld(w), _ld(w_scale), _CODES[a.dtype],
-        _CODES[dt], M, N, K, _dev_ptr(bias), _act(act), _dev_ptr(residual), _ld(residual), _dev_ptr(z), _ld(z), _dev_ptr(y), _ld(y),
-        _dev_ptr(ws), ws.numel(), _stream()))
+    sa, ld_sa = _scale("a_scale", a_scale, dtype, M, K, device)
+    sw, ld_sw = _scale("w_scale", w_scale, dtype, N, K, device)
+    y, dt, ld_y = _result("out", a, dtype, out_dtype, out, M, N, device)
+    b = _vector("bias", bias, N, dt, device)
+    ld_r = 0 if residual is None else _other("residual", residual, M, N, dt, device)
+    z = a.new_empty((M, N), dtype=_F32) if want_preact else None
+    code = _CODES[dtype]
+    held, room, nbytes = _room(workspace, lib.rcd_linear_workspace_bytes(M, N, K, code), device)
+    status = lib.rcd_linear(
+        a.data_ptr(), sa, ld_a, ld_sa, w.data_ptr(), sw, ld_w, ld_sw, code, _CODES[dt], M, N, K, b, _act(act), _ptr(residual), ld_r,
+        _ptr(z), N, y.data_ptr(), ld_y, room, nbytes, _stream(device))
+    if status:
+        _check(status)
     return (y, z) if want_preact else y
 
 
@@ -202,23 +231,24 @@ def linear_backward(dy, a, w, preact=None, act: str = "none", want_da: bool = Tr
     """(da, dw, dbias) of linear; preact is its z (not needed for act "none"); what is not wanted is None.  The residual's
     gradient is dy itself."""
     lib = load_library()
-    _matrix("dy", dy)
-    _here(dy)
-    M, N = dy.shape
-    _matrix("a", a, M, None, dy.dtype, dy)
+    M, N, ld_dy, dtype, device = _first("dy", dy)
+    if not isinstance(a, torch.Tensor) or a.dim() != 2:
+        _refuse("a must be a matrix")
     K = a.shape[1]
-    _matrix("w", w, N, K, dy.dtype, dy)
+    ld_a, ld_w = _other("a", a, M, K, dtype, device), _other("w", w, N, K, dtype, device)
     if preact is None and act != "none":
         _refuse("preact is missing")
-    if preact is not None:
-        _matrix("preact", preact, M, N, torch.float32, dy)
-    da = _new(M, K, dy.dtype, dy) if want_da else None
-    dw = _new(N, K, dy.dtype, dy) if want_dw else None
-    db = torch.empty(N, dtype=dy.dtype, device=dy.device) if want_dbias else None
-    ws = _room(workspace, lib.rcd_linear_backward_workspace_bytes(M, N, K, _CODES[dy.dtype]), dy)
-    _check(lib.rcd_linear_backward(
-        _dev_ptr(dy), _ld(dy), _dev_ptr(a), _ld(a), _dev_ptr(w), _ld(w), _CODES[dy.dtype], M, N, K, _dev_ptr(preact), _ld(preact),
-        _act(act), _dev_ptr(da), _ld(da), _dev_ptr(dw), _ld(dw), _dev_ptr(db), _dev_ptr(ws), ws.numel(), _stream()))
+    ld_z = 0 if preact is None else _other("preact", preact, M, N, _F32, device)
+    da = dy.new_empty((M, K)) if want_da else None
+    dw = dy.new_empty((N, K)) if want_dw else None
+    db = dy.new_empty(N) if want_dbias else None
+    code = _CODES[dtype]
+    held, room, nbytes = _room(workspace, lib.rcd_linear_backward_workspace_bytes(M, N, K, code), device)
+    status = lib.rcd_linear_backward(
+        dy.data_ptr(), ld_dy, a.data_ptr(), ld_a, w.data_ptr(), ld_w, code, M, N, K, _ptr(preact), ld_z, _act(act), _ptr(da), K,
+        _ptr(dw), K, _ptr(db), room, nbytes, _stream(device))
+    if status:
+        _check(status)
     return da, dw, db
 
 
@@ -227,22 +257,22 @@ def gated_linear(a, w_gate, w_up, act: str = "silu", a_scale=None, gate_scale=No
     """act(a w_gate^T) * (a w_up^T), a (M, K), both weights (F, K).  want_saved: (h, saved), saved (M, F, 2) in float32 what
     gated_linear_backward takes."""
     lib = load_library()
-    _matrix("a", a)
-    _here(a)
-    M, K = a.shape
-    _matrix("w_gate", w_gate, None, K, a.dtype, a)
+    M, K, ld_a, dtype, device = _first("a", a)
+    ld_g = _other("w_gate", w_gate, None, K, dtype, device)
     F = w_gate.shape[0]
-    _matrix("w_up", w_up, F, K, a.dtype, a)
-    a_scale = _scale("a_scale", a_scale, a)
-    gate_scale, up_scale = _scale("gate_scale", gate_scale, w_gate), _scale("up_scale", up_scale, w_up)
-    dt = _out_dtype(a, out_dtype) if out is None else out.dtype
-    h = _new(M, F, dt, a) if out is None else _matrix("out", out, M, F, _out_dtype(a, out_dtype or dt), a)
-    saved = torch.empty((M, F, 2), dtype=torch.float32, device=a.device) if want_saved else None
-    ws = _room(workspace, lib.rcd_gated_linear_workspace_bytes(M, F, K, _CODES[a.dtype]), a)
-    _check(lib.rcd_gated_linear(
-        _dev_ptr(a), _dev_ptr(a_scale), _ld(a), _ld(a_scale), _dev_ptr(w_gate), _dev_ptr(gate_scale), _ld(w_gate), _ld(gate_scale),
-        _dev_ptr(w_up), _dev_ptr(up_scale), _ld(w_up), _ld(up_scale), _CODES[a.dtype], _CODES[dt], M, F, K, _act(act),
-        _dev_ptr(saved), _dev_ptr(h), _ld(h), _dev_ptr(ws), ws.numel(), _stream()))
+    ld_u = _other("w_up", w_up, F, K, dtype, device)
+    sa, ld_sa = _scale("a_scale", a_scale, dtype, M, K, device)
+    sg, ld_sg = _scale("gate_scale", gate_scale, dtype, F, K, device)
+    su, ld_su = _scale("up_scale", up_scale, dtype, F, K, device)
+    h, dt, ld_h = _result("out", a, dtype, out_dtype, out, M, F, device)
+    saved = a.new_empty((M, F, 2), dtype=_F32) if want_saved else None
+    code = _CODES[dtype]
+    held, room, nbytes = _room(workspace, lib.rcd_gated_linear_workspace_bytes(M, F, K, code), device)
+    status = lib.rcd_gated_linear(
+        a.data_ptr(), sa, ld_a, ld_sa, w_gate.data_ptr(), sg, ld_g, ld_sg, w_up.data_ptr(), su, ld_u, ld_su, code, _CODES[dt], M, F,
+        K, _act(act), _ptr(saved), h.data_ptr(), ld_h, room, nbytes, _stream(device))
+    if status:
+        _check(status)
     return (h, saved) if want_saved else h
 
 
@@ -250,22 +280,23 @@ def gated_linear_backward(dh, a, w_gate, w_up, saved, act: str = "silu", want_da
                           workspace=None):
     """(da, dw_gate, dw_up) of gated_linear; saved is its saved; what is not wanted is None."""
     lib = load_library()
-    _matrix("dh", dh)
-    _here(dh)
-    M, F = dh.shape
-    _matrix("a", a, M, None, dh.dtype, dh)
+    M, F, ld_dh, dtype, device = _first("dh", dh)
+    if not isinstance(a, torch.Tensor) or a.dim() != 2:
+        _refuse("a must be a matrix")
     K = a.shape[1]
-    _matrix("w_gate", w_gate, F, K, dh.dtype, dh)
-    _matrix("w_up", w_up, F, K, dh.dtype, dh)
-    if (not isinstance(saved, torch.Tensor) or saved.shape != (M, F, 2) or saved.dtype != torch.float32
-            or not saved.is_contiguous() or saved.device != dh.device):
+    ld_a = _other("a", a, M, K, dtype, device)
+    ld_g, ld_u = _other("w_gate", w_gate, F, K, dtype, device), _other("w_up", w_up, F, K, dtype, device)
+    if (not isinstance(saved, torch.Tensor) or saved.shape != (M, F, 2) or saved.dtype is not _F32
+            or not saved.is_contiguous() or saved.get_device() != device):
         _refuse("saved must be what gated_linear returned")
-    da = _new(M, K, dh.dtype, dh) if want_da else None
-    dwg = _new(F, K, dh.dtype, dh) if want_dw else None
-    dwu = _new(F, K, dh.dtype, dh) if want_dw else None
-    ws = _room(workspace, lib.rcd_gated_linear_backward_workspace_bytes(M, F, K, _CODES[dh.dtype]), dh)
-    _check(lib.rcd_gated_linear_backward(
-        _dev_ptr(dh), _ld(dh), _dev_ptr(a), _ld(a), _dev_ptr(w_gate), _ld(w_gate), _dev_ptr(w_up), _ld(w_up), _CODES[dh.dtype],
-        M, F, K, _dev_ptr(saved), _act(act), _dev_ptr(da), _ld(da), _dev_ptr(dwg), _ld(dwg), _dev_ptr(dwu), _ld(dwu),
-        _dev_ptr(ws), ws.numel(), _stream()))
+    da = dh.new_empty((M, K)) if want_da else None
+    dwg = dh.new_empty((F, K)) if want_dw else None
+    dwu = dh.new_empty((F, K)) if want_dw else None
+    code = _CODES[dtype]
+    held, room, nbytes = _room(workspace, lib.rcd_gated_linear_backward_workspace_bytes(M, F, K, code), device)
+    status = lib.rcd_gated_linear_backward(
+        dh.data_ptr(), ld_dh, a.data_ptr(), ld_a, w_gate.data_ptr(), ld_g, w_up.data_ptr(), ld_u, code, M, F, K, saved.data_ptr(),
+        _act(act), _ptr(da), K, _ptr(dwg), K, _ptr(dwu), K, room, nbytes, _stream(device))
+    if status:
+        _check(status)
     return da, dwg, dwu
