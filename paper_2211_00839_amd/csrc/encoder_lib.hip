@@ -6,6 +6,7 @@
 #include <type_traits>
 
 #include "host_error.h"
+#include "encoder_rules.h"
 #include "norm_kernels.hip"
 #include "product_kernels.hip"
 #include "few_rows_kernels.hip"
@@ -88,7 +89,7 @@ inline int64_t part_pitch(int64_t d) { return (d + 63) / 64 * 64; }
 // What is set up once per device: the tile kernels use more LDS than a kernel may by default.
 constexpr int MAX_DEVICES = 64;
 std::mutex g_setup_mutex;
-int g_units[MAX_DEVICES] = {};          // compute units; 0: not set up yet
+bool g_ready[MAX_DEVICES] = {};
 
 template <int WT, int KA, int KB, bool MX, int TO> hipError_t raise_lds_limit()
 {
@@ -123,13 +124,13 @@ template <typename Go> int with_tile_variant(int wt, int ka, int kb, bool mx, in
     return wt == 128 ? by_order(integral_constant<int, 128>{}) : by_order(integral_constant<int, 64>{});
 }
 
-int set_up(int *units)
+int set_up()
 {
     int dev = 0;
     ENC_HIP_TRY(hipGetDevice(&dev));
     if (dev < 0 || dev >= MAX_DEVICES) return rcd_note_hip_error("device index beyond 63", hipErrorInvalidDevice);
     std::lock_guard<std::mutex> lock(g_setup_mutex);
-    if (g_units[dev] == 0) {
+    if (!g_ready[dev]) {
         for (int wt : {64, 128})
             for (int order = 0; order < 4; ++order)
                 for (int to : {tile::TO_LINEAR, tile::TO_GATED, tile::TO_PARTS, tile::TO_GATED_PARTS}) {
@@ -142,11 +143,8 @@ int set_up(int *units)
                         return (int)RCD_OK;
                     }));
                 }
-        int cus = 0;
-        ENC_HIP_TRY(hipDeviceGetAttribute(&cus, hipDeviceAttributeMultiprocessorCount, dev));
-        g_units[dev] = std::max(cus, 1);
+        g_ready[dev] = true;
     }
-    *units = g_units[dev];
     return RCD_OK;
 }
 
@@ -200,7 +198,7 @@ struct Packer {
             l.pitch = up64(cols) * 2;
             l.cols = up64(cols);
             wide.job[nwide++] = WidenJob{(const uint8_t *)src, scale, q, (long long)ld, (long long)ld_scale, (long long)up64(cols),
-                                         (int)rows, (int)cols, rows_aligned(src, ld, 1, 8)};
+                                         (int)rows, (int)cols};
             most = std::max(most, rows * up64(cols) / 8);
             return l;
         }
@@ -234,7 +232,7 @@ struct Packer {
             l.plane = rows * l.pitch;
             l.cols = up64(cols);
             jobs.job[njobs++] = PackJob{src, q, (long long)ld, (long long)up64(cols), (long long)(rows * up64(cols)), (int)rows,
-                                        (int)cols, rows_aligned(src, ld, size_of(dt))};
+                                        (int)cols};
             most = std::max(most, rows * up64(cols) / 8);
         }
         return l;
@@ -273,12 +271,6 @@ struct Product {
     Epilogue e;
 };
 
-// The cut of a product into workgroups.
-struct Cut {
-    int wt, splits;
-    int64_t tiles_m, tiles_n;
-};
-
 int64_t stages_of(int64_t K, int dt, int pairs)
 {
     const int64_t per = dt == RCD_MXFP8 ? 128 : 64;
@@ -286,21 +278,10 @@ int64_t stages_of(int64_t K, int dt, int pairs)
 }
 inline int64_t parts_pitch(int64_t N, bool gated) { return (N + 7) / 8 * 8 * (gated ? 2 : 1); }
 
+using enc_rules::Cut;
 Cut cut_of(int64_t M, int64_t N, int64_t K, int dt, int pairs, bool gated)
 {
-    const int64_t stages = stages_of(K, dt, pairs);
-    auto tiles = [&](int wt, Cut &c) {
-        c.wt = wt;
-        c.tiles_m = (M + 2 * wt - 1) / (2 * wt);
-        c.tiles_n = gated ? (N + wt - 1) / wt : (N + 2 * wt - 1) / (2 * wt);
-        return c.tiles_m * c.tiles_n;
-    };
-    Cut c;
-    int64_t t = tiles(128, c);
-    if (t < 192) t = tiles(64, c);
-    c.splits = 1;
-    const int64_t room = 256;
-    if (t < room / 2) c.splits = (int)std::max<int64_t>(1, std::min<int64_t>({room / t, stages / 4, 64}));
+    Cut c = enc_rules::cut_of(M, N, stages_of(K, dt, pairs), gated);
     return c;
 }
 size_t parts_bytes(const Cut &c, int64_t M, int64_t N, bool gated)
@@ -310,8 +291,7 @@ size_t parts_bytes(const Cut &c, int64_t M, int64_t N, bool gated)
 
 int launch_product(const Product &p, Pieces &room, hipStream_t stream)
 {
-    int units = 0;
-    ENC_TRY(set_up(&units));
+    ENC_TRY(set_up());
     const Cut c = cut_of(p.M, p.N, p.K, p.dt, p.pairs, p.gated);
     const int64_t workgroups = c.tiles_m * c.tiles_n * c.splits;
     if (workgroups > 0x7ffffff0) return RCD_ERR_UNSUPPORTED;
@@ -501,7 +481,6 @@ Epilogue one_output(void *out, int64_t ld, int dt, int act)
     e.act = act;
     e.split_row = e.rows_each = 0x7fffffff;
     e.out_f32 = dt == RCD_F32;
-    e.vec = rows_aligned(out, ld, size_of(dt));
     return e;
 }
 
@@ -514,7 +493,6 @@ few::Args few_args(int dt, const void *a, const uint8_t *scale, int64_t ld, int6
     x.sa_pitch = ld_scale;
     x.e = e;
     x.M = (int)M; x.N = (int)N; x.K = (int)K;
-    x.vec = rows_aligned(a, ld, size_of(dt));
     return x;
 }
 void few_weight(few::Args &x, int dt, bool second, const void *w, const uint8_t *scale, int64_t ld, int64_t ld_scale)
@@ -523,7 +501,6 @@ void few_weight(few::Args &x, int dt, bool second, const void *w, const uint8_t 
     (second ? x.b2_pitch : x.b_pitch) = ld * size_of(dt);
     (second ? x.sb2 : x.sb) = scale;
     (second ? x.sb2_pitch : x.sb_pitch) = ld_scale;
-    x.vec = x.vec && rows_aligned(w, ld, size_of(dt));
 }
 
 // The gated block's two weights.  The tile kernel wants one pitch for both: if they differ, or one can be read in place
@@ -568,14 +545,11 @@ int rcd_rms_norm(const void *X_dev, int dt, int64_t rows, int64_t d, int64_t ld_
     if (rows == 0) return RCD_OK;
     if (!X_dev || !Y_dev || (mx && !scale_dev)) return RCD_ERR_INVALID_ARG;
     if (sum_dev == Y_dev) return RCD_ERR_INVALID_ARG;
-    const int64_t esz = size_of(dt);
     NormArgs a{};
     a.x = X_dev; a.r = residual_dev; a.w = weight_dev;
     a.sum = sum_dev; a.y = Y_dev; a.scale = scale_dev; a.rstd = rstd_dev;
     a.ld_x = ld_x; a.ld_r = ld_r; a.ld_s = ld_s; a.ld_y = ld_y; a.ld_scale = ld_scale;
     a.rows = rows; a.d = (int)d; a.eps = eps;
-    a.vec = rows_aligned(X_dev, ld_x, esz) && rows_aligned(residual_dev, ld_r, esz) && rows_aligned(weight_dev, 0, esz) &&
-            rows_aligned(sum_dev, ld_s, esz) && (mx ? rows_aligned(Y_dev, ld_y, 1, 8) : rows_aligned(Y_dev, ld_y, esz));
     return mx ? launch_norm<true, true>(a, dt, (hipStream_t)stream) : launch_norm<false, true>(a, dt, (hipStream_t)stream);
 }
 
@@ -591,7 +565,6 @@ int rcd_quantize_mxfp8(const void *X_dev, int dt, int64_t rows, int64_t d, int64
     a.x = X_dev; a.y = Q_dev; a.scale = scale_dev;
     a.ld_x = ld_x; a.ld_y = ld_q; a.ld_scale = ld_scale;
     a.rows = rows; a.d = (int)d;
-    a.vec = rows_aligned(X_dev, ld_x, size_of(dt)) && rows_aligned(Q_dev, ld_q, 1, 8);
     return launch_norm<true, false>(a, dt, (hipStream_t)stream);
 }
 
@@ -612,15 +585,13 @@ int rcd_rms_norm_backward(const void *dY_dev, int dt, int64_t rows, int64_t d, i
     if (rows > MAX_EXTENT || d > MAX_EXTENT) return RCD_ERR_UNSUPPORTED;
     if (rows == 0) return zero_matrix(dweight_dev, dt, d, 1, d, stream);
     if (!dY_dev || !H_dev || !rstd_dev || !dX_dev) return RCD_ERR_INVALID_ARG;
-    const int64_t esz = size_of(dt), groups = norm_groups(rows, d);
+    const int64_t groups = norm_groups(rows, d);
     if (dweight_dev) ENC_TRY(check_pieces(workspace_dev, workspace_bytes, rcd_rms_norm_backward_workspace_bytes(rows, d)));
     NormBackArgs a{};
     a.dy = dY_dev; a.h = H_dev; a.w = weight_dev; a.dsum = dsum_dev; a.rstd = rstd_dev;
     a.dx = dX_dev; a.part = dweight_dev ? (float *)workspace_dev : nullptr;
     a.ld_dy = ld_dy; a.ld_h = ld_h; a.ld_ds = ld_ds; a.ld_dx = ld_dx; a.part_pitch = part_pitch(d);
     a.rows = rows; a.d = (int)d;
-    a.vec = rows_aligned(dY_dev, ld_dy, esz) && rows_aligned(H_dev, ld_h, esz) && rows_aligned(weight_dev, 0, esz) &&
-            rows_aligned(dsum_dev, ld_ds, esz) && rows_aligned(dX_dev, ld_dx, esz);
     with_row_variant(d, [&](auto wpr, auto chunks) {
         constexpr int W = decltype(wpr)::value, C = decltype(chunks)::value;
         const dim3 grid((unsigned)(groups / RowOf<W>::ROWS));
@@ -651,15 +622,12 @@ int rcd_linear(const void *A_dev, const uint8_t *A_scale_dev, int64_t ld_a, int6
     ENC_TRY(check_mx_operand(dt, A_scale_dev, ld_a_scale, K));
     ENC_TRY(check_mx_operand(dt, W_scale_dev, ld_w_scale, K));
     ENC_TRY(check_pieces(workspace_dev, workspace_bytes, rcd_linear_workspace_bytes(M, N, K, dt)));
-    const int64_t osz = size_of(out_dt);
     Epilogue e = one_output(Y_dev, ld_y, out_dt, act);
     e.bias = bias_dev;
     e.residual = residual_dev;
     e.preact = preact_dev;
     e.ld_r = ld_r;
     e.ld_p = ld_p;
-    e.vec = rows_aligned(Y_dev, ld_y, osz) && rows_aligned(bias_dev, 0, osz) && rows_aligned(residual_dev, ld_r, osz) &&
-            rows_aligned(preact_dev, ld_p, 4);
     if (M <= few_rows(dt)) {
         few::Args x = few_args(dt, A_dev, A_scale_dev, ld_a, ld_a_scale, M, N, K, e);
         few_weight(x, dt, false, W_dev, W_scale_dev, ld_w, ld_w_scale);
@@ -734,8 +702,7 @@ int rcd_linear_backward(const void *dY_dev, int64_t ld_dy, const void *A_dev, in
         x.dz = as_it_is ? nullptr : w.dz;
         x.part = dbias_dev ? w.part : nullptr;
         x.ld_dy = ld_dy; x.ld_z = ld_p; x.pitch = pitch; x.plane = M * pitch; x.part_pitch = part_pitch(N);
-        x.M = (int)M; x.N = (int)N; x.act = act; x.across = c.across;
-        x.vec = rows_aligned(dY_dev, ld_dy, size_of(dt)) && (act == RCD_ACT_NONE || rows_aligned(preact_dev, ld_p, 4));
+        x.M = (int)M; x.N = (int)N; x.across = c.across;
         const dim3 grid((unsigned)c.pieces, (unsigned)c.groups);
         with_act_value(act, [&](auto a) {
             constexpr int A = decltype(a)::value;
@@ -794,7 +761,6 @@ int rcd_gated_linear(const void *A_dev, const uint8_t *A_scale_dev, int64_t ld_a
     Epilogue e = one_output(H_dev, ld_h, out_dt, act);
     e.preact = saved_dev;
     e.ld_p = 2 * F;
-    e.vec = rows_aligned(H_dev, ld_h, size_of(out_dt)) && rows_aligned(saved_dev, 2 * F, 4);
     if (M <= few_rows(dt)) {
         few::Args x = few_args(dt, A_dev, A_scale_dev, ld_a, ld_a_scale, M, F, K, e);
         few_weight(x, dt, false, Wg_dev, Wg_scale_dev, ld_wg, ld_wg_scale);
@@ -860,8 +826,7 @@ int rcd_gated_linear_backward(const void *dH_dev, int64_t ld_dh, const void *A_d
     x.z = saved_dev;
     x.dz = dgu;
     x.ld_dy = ld_dh; x.ld_z = 2 * F; x.pitch = pitch; x.plane = M * pitch;
-    x.M = (int)M; x.N = (int)F; x.act = act; x.across = c.across; x.half = (int)half;
-    x.vec = rows_aligned(dH_dev, ld_dh, size_of(dt)) && rows_aligned(saved_dev, 2 * F, 4);
+    x.M = (int)M; x.N = (int)F; x.across = c.across; x.half = (int)half;
     const dim3 grid((unsigned)c.pieces, (unsigned)c.groups);
     with_act_value(act, [&](auto a) {
         constexpr int A = decltype(a)::value;
@@ -897,7 +862,6 @@ int rcd_gated_linear_backward(const void *dH_dev, int64_t ld_dh, const void *A_d
         p.e.ld_o2 = ld_dwu;
         p.e.split_row = (int)half;
         p.e.rows_each = (int)F;
-        p.e.vec = p.e.vec && rows_aligned(dWu_dev, ld_dwu, size_of(dt));
         ENC_TRY(launch_product(p, room, stream));
     }
     return RCD_OK;

@@ -16,18 +16,30 @@ constexpr int MX_BLOCK = 32;     // elements that share a scale
 __device__ __forceinline__ float to_f32(float v) { return v; }
 __device__ __forceinline__ float to_f32(__bf16 v) { return (float)v; }
 
-// 8 consecutive elements of a row as fp32; `count` of them exist, the others come out as 0.  vec: 16-byte loads are
-// allowed for a full group.
+// Vectors of 16 bytes that need no alignment beyond their element's: global loads and stores of this architecture take any
+// address, and rows of odd lengths are as common as padded ones.
+typedef float f32x4_any __attribute__((ext_vector_type(4), aligned(4)));
+typedef __bf16 bf16x8_any __attribute__((ext_vector_type(8), aligned(2)));
+typedef unsigned u32x4_any __attribute__((ext_vector_type(4), aligned(1)));
+typedef unsigned u32x2_any __attribute__((ext_vector_type(2), aligned(1)));
+template <typename T> struct Any;
+template <> struct Any<float> { typedef f32x4_any type; };
+template <> struct Any<__bf16> { typedef bf16x8_any type; };
+
+// 8 consecutive elements of a row as fp32; `count` of them exist, the others come out as 0.
 template <typename T>
-__device__ __forceinline__ void load8(const T *__restrict__ p, int count, bool vec, float (&v)[8])
+__device__ __forceinline__ void load8(const T *__restrict__ p, int count, float (&v)[8])
 {
-    if (vec && count >= 8) {
+    if (count >= 8) {
         if constexpr (sizeof(T) == 4) {
-            const float4 a = reinterpret_cast<const float4 *>(p)[0], b = reinterpret_cast<const float4 *>(p)[1];
-            v[0] = a.x; v[1] = a.y; v[2] = a.z; v[3] = a.w;
-            v[4] = b.x; v[5] = b.y; v[6] = b.z; v[7] = b.w;
+            const f32x4 a = reinterpret_cast<const f32x4_any *>(p)[0], b = reinterpret_cast<const f32x4_any *>(p)[1];
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                v[i] = a[i];
+                v[4 + i] = b[i];
+            }
         } else {
-            const bf16x8 a = *reinterpret_cast<const bf16x8 *>(p);
+            const bf16x8 a = *reinterpret_cast<const bf16x8_any *>(p);
 #pragma unroll
             for (int i = 0; i < 8; ++i) v[i] = (float)a[i];
         }
@@ -38,17 +50,17 @@ __device__ __forceinline__ void load8(const T *__restrict__ p, int count, bool v
 }
 
 template <typename T>
-__device__ __forceinline__ void store8(T *__restrict__ p, int count, bool vec, const float (&v)[8])
+__device__ __forceinline__ void store8(T *__restrict__ p, int count, const float (&v)[8])
 {
-    if (vec && count >= 8) {
+    if (count >= 8) {
         if constexpr (sizeof(T) == 4) {
-            reinterpret_cast<float4 *>(p)[0] = make_float4(v[0], v[1], v[2], v[3]);
-            reinterpret_cast<float4 *>(p)[1] = make_float4(v[4], v[5], v[6], v[7]);
+            reinterpret_cast<f32x4_any *>(p)[0] = f32x4{v[0], v[1], v[2], v[3]};
+            reinterpret_cast<f32x4_any *>(p)[1] = f32x4{v[4], v[5], v[6], v[7]};
         } else {
             bf16x8 a;
 #pragma unroll
             for (int i = 0; i < 8; ++i) a[i] = (__bf16)v[i];
-            *reinterpret_cast<bf16x8 *>(p) = a;
+            *reinterpret_cast<bf16x8_any *>(p) = a;
         }
         return;
     }

@@ -1,0 +1,68 @@
+// Rules of the encoder's products that are a matter of sizes alone: plain host code, so that the measured points behind
+// them can be tested without a device.
+#pragma once
+#include <algorithm>
+#include <cstdint>
+
+namespace enc_rules {
+
+// The cut of a product into workgroups: tiles of 2 wt x 2 wt sums, k in `splits` parts.
+struct Cut {
+    int wt, splits;
+    int64_t tiles_m, tiles_n;
+};
+
+constexpr int64_t UNITS = 256;      // compute units of the device
+
+inline int64_t ceil_div(int64_t a, int64_t b) { return (a + b - 1) / b; }
+
+// What a cut takes, in microseconds, from what was measured on full and on part-full devices (bf16, k contiguous):
+//   a stage of a 256 x 256 tile      1.0 with few workgroups, 1.5 with one on every unit (the clock falls with the load)
+//   a stage of a 128 x 128 tile      0.55 alone on its unit, 0.88 with a second one beside it
+//   start, filling and epilogue      6 and 4 per round of workgroups
+//   parts                            written and read again at 7 TB/s (they stay in the last-level cache), and a launch of 3.5
+// Measured / by this rule: 16384 x 2048 x 2048 large tiles 115 / 108, small 132 / 129; the weights' gradient of it large in 4
+// parts 121 / 125, in 1 278 / 294, small in 2 132 / 131; 1000 x 2048 x 8192 small in 4 43 / 41, in 1 69 / 75; 256 x 2048 x
+// 2048 small in 3 15 / 15, large in 1 40 / 42.
+inline double time_of(const Cut &c, int64_t M, int64_t N, int64_t stages, bool gated)
+{
+    const int64_t workgroups = c.tiles_m * c.tiles_n * c.splits, deep = ceil_div(stages, c.splits);
+    double t;
+    if (c.wt == 128) {
+        const int64_t rounds = ceil_div(workgroups, UNITS);
+        t = (double)rounds * ((double)deep * (1.0 + 0.5 * std::min(1.0, (double)workgroups / UNITS)) + 6.0);
+    } else {
+        const int64_t full = workgroups / (2 * UNITS), rest = workgroups % (2 * UNITS);
+        t = (double)full * ((double)deep * 0.88 + 4.0);
+        if (rest) t += (double)deep * (rest > UNITS ? 0.88 : 0.55) + 4.0;
+    }
+    if (c.splits > 1) t += 3.5 + 0.25 * c.splits + 2e-6 / 7 * (double)c.splits * (double)M * (double)N * 4 * (gated ? 2 : 1);
+    return t;
+}
+
+// M x N: the result (gated: N columns of each of two products); stages: of k, 64 bf16 or 128 8-bit elements each, three
+// pieces of fp32 make six products.
+inline Cut cut_of(int64_t M, int64_t N, int64_t stages, bool gated)
+{
+    Cut best{};
+    double least = 0.0;
+    for (int wt : {128, 64}) {
+        Cut c;
+        c.wt = wt;
+        c.tiles_m = ceil_div(M, 2 * wt);
+        c.tiles_n = ceil_div(N, gated ? wt : 2 * wt);
+        for (int splits : {1, 2, 3, 4, 5, 6, 8, 10, 12, 16}) {
+            // (a part of fewer than four stages is all start and end)
+            if (splits > 1 && (splits * 4 > stages || c.tiles_m * c.tiles_n * splits > 2 * UNITS)) break;
+            c.splits = splits;
+            const double t = time_of(c, M, N, stages, gated);
+            if (best.splits == 0 || t < least) {
+                best = c;
+                least = t;
+            }
+        }
+    }
+    return best;
+}
+
+} // namespace enc_rules

@@ -12,13 +12,15 @@ struct Args {
     long long sa_pitch, sb_pitch, sb2_pitch;
     Epilogue e;
     int M, N, K;
-    bool vec;                                   // 16-byte loads are allowed
 };
 
 // 16 bytes of a row from byte `at` on; what lies past `bytes` is zero.
-__device__ __forceinline__ uint4 chunk(const unsigned char *row, int at, int bytes, bool vec)
+__device__ __forceinline__ uint4 chunk(const unsigned char *row, int at, int bytes)
 {
-    if (vec && at + 16 <= bytes) return *reinterpret_cast<const uint4 *>(row + at);
+    if (at + 16 <= bytes) {
+        const u32x4_any t = *reinterpret_cast<const u32x4_any *>(row + at);
+        return make_uint4(t[0], t[1], t[2], t[3]);
+    }
     unsigned w[4] = {0, 0, 0, 0};
 #pragma unroll
     for (int i = 0; i < 16; ++i)
@@ -74,8 +76,8 @@ k_few(const Args x)
         int ws[G][2], vs[MT][2];      // (16 k lie in one scale block)
 #pragma unroll
         for (int g = 0; g < G; ++g) {
-            w[g][0] = chunk(b[g], at, bytes, x.vec);
-            w[g][1] = chunk(b[g], at + 64, bytes, x.vec);
+            w[g][0] = chunk(b[g], at, bytes);
+            w[g][1] = chunk(b[g], at + 64, bytes);
             if constexpr (MX)
 #pragma unroll
                 for (int h = 0; h < 2; ++h) {
@@ -85,8 +87,8 @@ k_few(const Args x)
         }
 #pragma unroll
         for (int t = 0; t < MT; ++t) {
-            v[t][0] = chunk(a[t], at, bytes, x.vec);
-            v[t][1] = chunk(a[t], at + 64, bytes, x.vec);
+            v[t][0] = chunk(a[t], at, bytes);
+            v[t][1] = chunk(a[t], at + 64, bytes);
             if constexpr (MX)
 #pragma unroll
                 for (int h = 0; h < 2; ++h) {
@@ -171,7 +173,7 @@ k_few_f32(const Args x)
         for (int i = 0; i < MR; ++i) acc[j][i] = 0.f;
     auto four = [&](const float *p, int k) {
         f32x4 v = {0.f, 0.f, 0.f, 0.f};
-        if (x.vec && k + 4 <= x.K) return *reinterpret_cast<const f32x4 *>(p + k);
+        if (k + 4 <= x.K) return (f32x4)*reinterpret_cast<const f32x4_any *>(p + k);
 #pragma unroll
         for (int e = 0; e < 4; ++e)
             if (k + e < x.K) v[e] = p[k + e];

@@ -42,7 +42,6 @@ struct NormArgs {
     long long rows;
     int d;
     float eps;
-    bool vec;                       // every row of every matrix may be accessed 16 bytes at a time (8 for 8-bit output)
 };
 
 // One chunk of a row in 8 bits: the four lanes of a block share their largest finite magnitude.  Every lane of a block of
@@ -63,8 +62,9 @@ __device__ __forceinline__ void store_mx(const NormArgs &a, size_t row, int col,
     const unsigned lo = to_e4m3x4(v[0] * inv, v[1] * inv, v[2] * inv, v[3] * inv);
     const unsigned hi = to_e4m3x4(v[4] * inv, v[5] * inv, v[6] * inv, v[7] * inv);
     uint8_t *q = (uint8_t *)a.y + row * a.ld_y + col;
-    if (a.vec && count >= 8) {
-        *reinterpret_cast<uint2 *>(q) = make_uint2(lo, hi);
+    if (count >= 8) {
+        typedef unsigned u32x2 __attribute__((ext_vector_type(2)));
+        *reinterpret_cast<u32x2_any *>(q) = u32x2{lo, hi};
     } else {
         for (int i = 0; i < min(count, 8); ++i) q[i] = (uint8_t)((i < 4 ? lo : hi) >> (8 * (i & 3)));
     }
@@ -89,10 +89,10 @@ k_norm(const NormArgs a)
     float h[HELD][8];
     auto fetch = [&](int c, float (&v)[8]) {
         const int col = (c * R::LANES + R::lane()) * 8, count = a.d - col;
-        load8(x + col, count, a.vec, v);
+        load8(x + col, count, v);
         if (r) {
             float u[8];
-            load8(r + col, count, a.vec, u);
+            load8(r + col, count, u);
 #pragma unroll
             for (int i = 0; i < 8; ++i) v[i] += u[i];
         }
@@ -101,10 +101,10 @@ k_norm(const NormArgs a)
         const int col = (c * R::LANES + R::lane()) * 8, count = a.d - col;
         float y[8];
         if constexpr (NORM) {
-            if (sum && count > 0) store8(sum + col, count, a.vec, v);
+            if (sum && count > 0) store8(sum + col, count, v);
             if (w) {
                 float u[8];
-                load8(w + col, count, a.vec, u);
+                load8(w + col, count, u);
 #pragma unroll
                 for (int i = 0; i < 8; ++i) y[i] = v[i] * rstd * u[i];
             } else {
@@ -116,7 +116,7 @@ k_norm(const NormArgs a)
             for (int i = 0; i < 8; ++i) y[i] = v[i];
         }
         if constexpr (MX) store_mx(a, row, col, count, y);
-        else if (count > 0) store8((T *)a.y + row * a.ld_y + col, count, a.vec, y);
+        else if (count > 0) store8((T *)a.y + row * a.ld_y + col, count, y);
     };
     float rstd = 1.f;
     if constexpr (NORM || C > 0) {
@@ -159,7 +159,6 @@ struct NormBackArgs {
     long long ld_dy, ld_h, ld_ds, ld_dx, part_pitch;
     long long rows;
     int d;
-    bool vec;
 };
 
 // A group of WPR waves walks the rows group, group + groups, ...: its sums of dy xh stay in registers from row to row
@@ -184,8 +183,8 @@ k_norm_backward(const NormBackArgs a)
     // g, xh of chunk c, and the chunk's share of sum g xh
     auto fetch = [&](size_t row, int c, float rstd, float (&g)[8], float (&xh)[8], float (&dwc)[8], bool add) {
         const int col = (c * R::LANES + R::lane()) * 8, count = a.d - col;
-        load8((const T *)a.dy + row * a.ld_dy + col, count, a.vec, g);
-        load8((const T *)a.h + row * a.ld_h + col, count, a.vec, xh);
+        load8((const T *)a.dy + row * a.ld_dy + col, count, g);
+        load8((const T *)a.h + row * a.ld_h + col, count, xh);
 #pragma unroll
         for (int i = 0; i < 8; ++i) xh[i] *= rstd;
         if (add) {
@@ -194,7 +193,7 @@ k_norm_backward(const NormBackArgs a)
         }
         if (w) {
             float u[8];
-            load8(w + col, count, a.vec, u);
+            load8(w + col, count, u);
 #pragma unroll
             for (int i = 0; i < 8; ++i) g[i] *= u[i];
         }
@@ -211,11 +210,11 @@ k_norm_backward(const NormBackArgs a)
         for (int i = 0; i < 8; ++i) v[i] = rstd * fmaf(-xh[i], mean, g[i]);
         if (a.dsum) {
             float u[8];
-            load8((const T *)a.dsum + row * a.ld_ds + col, count, a.vec, u);
+            load8((const T *)a.dsum + row * a.ld_ds + col, count, u);
 #pragma unroll
             for (int i = 0; i < 8; ++i) v[i] += u[i];
         }
-        store8((T *)a.dx + row * a.ld_dx + col, count, a.vec, v);
+        store8((T *)a.dx + row * a.ld_dx + col, count, v);
     };
     for (long long row = group; row < a.rows; row += groups) {
         const float rstd = a.rstd[row];
@@ -227,13 +226,13 @@ k_norm_backward(const NormBackArgs a)
             for (int c = 0; c < chunks; ++c) {
                 const int col = (c * R::LANES + R::lane()) * 8;
                 if (part && col < a.d) {       // (part_pitch is a multiple of 8: whole chunks)
-                    if (row != group) load8(part + col, 8, true, dw[0]);
+                    if (row != group) load8(part + col, 8, dw[0]);
                     else
 #pragma unroll
                         for (int i = 0; i < 8; ++i) dw[0][i] = 0.f;
                 }
                 s += fetch(row, c, rstd, g[0], xh[0], dw[0], true);
-                if (part && col < a.d) store8(part + col, 8, true, dw[0]);
+                if (part && col < a.d) store8(part + col, 8, dw[0]);
             }
         }
         const float mean = row_sum<WPR>(s, scratch) * inv_d;
@@ -252,7 +251,7 @@ k_norm_backward(const NormBackArgs a)
 #pragma unroll
             for (int c = 0; c < C; ++c) {
                 const int col = (c * R::LANES + R::lane()) * 8;
-                if (col < a.d) store8(part + col, 8, true, dw[c]);
+                if (col < a.d) store8(part + col, 8, dw[c]);
             }
         }
     }

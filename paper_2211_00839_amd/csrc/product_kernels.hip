@@ -18,7 +18,6 @@ struct Epilogue {
     int split_row;                  // 0x7fffffff: one output
     int rows_each;                  // rows of one output (with two of them, padding lies between)
     bool out_f32;
-    bool vec;                       // 16-byte accesses are allowed for full groups of eight columns
 };
 
 template <typename T>
@@ -26,21 +25,21 @@ __device__ __forceinline__ void finish_linear8_as(const Epilogue &e, T *out, lon
 {
     float t[8];
     if (e.bias) {
-        load8((const T *)e.bias + n, count, e.vec, t);
+        load8((const T *)e.bias + n, count, t);
 #pragma unroll
         for (int i = 0; i < 8; ++i) z[i] += t[i];
     }
-    if (e.preact) store8(e.preact + m * e.ld_p + n, count, e.vec, z);
+    if (e.preact) store8(e.preact + m * e.ld_p + n, count, z);
     if (e.act != 0) {
 #pragma unroll
         for (int i = 0; i < 8; ++i) z[i] = activate(z[i], e.act);
     }
     if (e.residual) {
-        load8((const T *)e.residual + m * e.ld_r + n, count, e.vec, t);
+        load8((const T *)e.residual + m * e.ld_r + n, count, t);
 #pragma unroll
         for (int i = 0; i < 8; ++i) z[i] += t[i];
     }
-    store8(out + row + n, count, e.vec, z);
+    store8(out + row + n, count, z);
 }
 
 // Columns n .. n + count - 1 (count <= 8) of row m.
@@ -63,15 +62,15 @@ __device__ __forceinline__ void finish_gated8(const Epilogue &e, int m, int f, i
     if (e.preact) {
         float *p = e.preact + (long long)m * e.ld_p + 2 * (long long)f;
         const float lo[8] = {g[0], u[0], g[1], u[1], g[2], u[2], g[3], u[3]}, hi[8] = {g[4], u[4], g[5], u[5], g[6], u[6], g[7], u[7]};
-        store8(p, 2 * count, e.vec, lo);
-        store8(p + 8, 2 * count - 8, e.vec, hi);
+        store8(p, 2 * count, lo);
+        store8(p + 8, 2 * count - 8, hi);
     }
     float h[8];
 #pragma unroll
     for (int i = 0; i < 8; ++i) h[i] = activate(g[i], e.act) * u[i];
     const long long at = (long long)m * e.ld_o + f;
-    if (e.out_f32) store8((float *)e.out + at, count, e.vec, h);
-    else store8((__bf16 *)e.out + at, count, e.vec, h);
+    if (e.out_f32) store8((float *)e.out + at, count, h);
+    else store8((__bf16 *)e.out + at, count, h);
 }
 
 // One operand of a product on the matrix cores.
@@ -504,7 +503,7 @@ struct Pipe {
                     if (done + i < S::NLOAD) load1<false>(buf, done + i, 0);
             };
             if constexpr (!MX) {
-                constexpr int EARLY = NM == 16 ? 6 : 3;         // loads behind sub-step 2's multiplies
+                constexpr int EARLY = 6;                        // large tiles: loads behind sub-step 2's multiplies
                 multiply(f0, [&](int i) { reads(f1, buf, 1, i * PER, PER); });
                 multiply(f1, [&](int i) {
                     constexpr int H = NM / 2;
@@ -514,10 +513,11 @@ struct Pipe {
                 multiply(f2, [&](int i) {
                     if (MORE && i == WAIT) give_up();
                     if constexpr (REFILL) {
+                        // (a small tile's stage is shorter than a load takes: all of them at once)
                         if (NM == 16) {
                             if (i > WAIT && (i & 1) == 0) refill((i - WAIT - 1) / 2, 1);
-                        } else if (i > WAIT) {
-                            refill(i - WAIT - 1, 1);
+                        } else if (i == WAIT) {
+                            refill(0, S::NLOAD);
                         }
                     }
                 });
@@ -525,7 +525,6 @@ struct Pipe {
                     if constexpr (MORE) reads(f0, buf ^ 1, 0, i * PER, PER);
                     if constexpr (REFILL) {
                         if (NM == 16) refill(EARLY + i, i < S::NLOAD - EARLY ? 1 : 0);
-                        else refill(EARLY + i * 2, 2);
                     }
                 });
             } else {
@@ -541,7 +540,13 @@ struct Pipe {
                     }
                 });
                 multiply8<2>(p1, w, [&](int i) {
-                    if (MORE && i == WAIT) give_up();
+                    if (MORE && i == WAIT) {
+                        give_up();
+                        if constexpr (REFILL && NM != 16) {
+                            load_scales(buf);
+                            refill(0, S::NLOAD);
+                        }
+                    }
                     if (i > WAIT) {
                         constexpr int ROOM = NM - 1 - WAIT;
                         const int at = i - WAIT - 1;
@@ -561,7 +566,7 @@ struct Pipe {
                                 for (int k = 0; k < 2 * NB; ++k) read_scale(wn, buf ^ 1, k);
                             }
                         }
-                        if constexpr (REFILL) {
+                        if constexpr (REFILL && NM == 16) {
                             constexpr int EACH = (S::NLOAD + ROOM - 1) / ROOM;
                             if (at == 0) load_scales(buf);
                             refill(at * EACH, EACH);
@@ -675,11 +680,11 @@ template <int WT, bool GATED> struct Band {
         for (int r = lane / LANES; r < 32; r += ROWS) {
             if (m + r >= x.M) break;
             float z[8];
-            load8(turn + r * PITCH + at(c), 8, true, z);
+            load8(turn + r * PITCH + at(c), 8, z);
             if (x.pieces.a[0] && !all_finite(z)) mend8(x.pieces, 0, m + r, n + c, count, z);
             if constexpr (GATED) {
                 float u[8];
-                load8(turn + r * PITCH + at(c) + 32, 8, true, u);
+                load8(turn + r * PITCH + at(c) + 32, 8, u);
                 if (x.pieces.a[0] && !all_finite(u)) mend8(x.pieces, 1, m + r, n + c, count, u);
                 finish_gated8(x.e, m + r, n + c, count, z, u);
             } else {
@@ -721,18 +726,16 @@ template <int WT, bool GATED> struct Band {
     // V consecutive elements, 16 bytes
     template <typename T, int V> static __device__ __forceinline__ void get(const T *p, float (&v)[V])
     {
-        typedef T vec __attribute__((ext_vector_type(V)));
-        const vec t = *reinterpret_cast<const vec *>(p);
+        const typename Any<T>::type t = *reinterpret_cast<const typename Any<T>::type *>(p);
 #pragma unroll
         for (int i = 0; i < V; ++i) v[i] = (float)t[i];
     }
     template <typename T, int V> static __device__ __forceinline__ void put(T *p, const float (&v)[V])
     {
-        typedef T vec __attribute__((ext_vector_type(V)));
-        vec t;
+        typename Any<T>::type t;
 #pragma unroll
         for (int i = 0; i < V; ++i) t[i] = (T)v[i];
-        *reinterpret_cast<vec *>(p) = t;
+        *reinterpret_cast<typename Any<T>::type *>(p) = t;
     }
     // V sums of row r from column c (of the turned band) on
     template <int V> __device__ __forceinline__ void sums(int r, int c, float (&z)[V])
@@ -759,7 +762,7 @@ template <int WT, bool GATED> struct Band {
             float z[4];
             sums<4>(r0 + k * ROWS, c, z);
             const f32x4 v = {z[0] + b[0], z[1] + b[1], z[2] + b[2], z[3] + b[3]};
-            __builtin_nontemporal_store(v, reinterpret_cast<f32x4 *>(to + (r0 + k * ROWS) * e.ld_p));
+            __builtin_nontemporal_store(v, reinterpret_cast<f32x4_any *>(to + (r0 + k * ROWS) * e.ld_p));
         }
     }
     // g and u side by side, two pairs to a lane
@@ -774,7 +777,7 @@ template <int WT, bool GATED> struct Band {
             const float *from = turn + (r0 + k * ROWS) * PITCH + at(c);
             const float2 g = *reinterpret_cast<const float2 *>(from), u = *reinterpret_cast<const float2 *>(from + 32);
             const f32x4 v = {g.x, u.x, g.y, u.y};
-            __builtin_nontemporal_store(v, reinterpret_cast<f32x4 *>(to + (r0 + k * ROWS) * e.ld_p));
+            __builtin_nontemporal_store(v, reinterpret_cast<f32x4_any *>(to + (r0 + k * ROWS) * e.ld_p));
         }
     }
 
@@ -788,7 +791,7 @@ template <int WT, bool GATED> struct Band {
         const long long ld = second ? e.ld_o2 : e.ld_o;
         out += (long long)(m - (second ? e.split_row : 0) + r0) * ld + n + c;
         const T *res = (const T *)e.residual + (long long)(m + r0) * e.ld_r + n + c;
-        typedef T vec __attribute__((ext_vector_type(V)));
+        typedef typename Any<T>::type vec;
         vec t[R];
         float z[R][V], b[V];
         if (e.residual) {
@@ -871,7 +874,7 @@ k_tile(const Args x)
     const int wm = m0 + (wave >> 1) * WT, wn = n0 + (wave & 1) * (COLS / 2);
     const bool own_rows = x.e.split_row == 0x7fffffff || m0 + S::T <= x.e.rows_each ||
                           (m0 >= x.e.split_row && m0 - x.e.split_row + S::T <= x.e.rows_each);
-    const bool inside = m0 + S::T <= x.M && n0 + COLS <= x.N && x.e.vec && own_rows;
+    const bool inside = m0 + S::T <= x.M && n0 + COLS <= x.N && own_rows;
     auto turn_round = [&](auto band_tag) {
         constexpr int I = decltype(band_tag)::value;
         if constexpr (I < P::NB) {
@@ -913,14 +916,14 @@ k_join(const Args x)
         const int m = (int)(t / groups), n = (int)(t % groups) * 8, count = x.N - n;
         const float *p = x.parts + m * x.parts_pitch + n;
         float z[8], u[8], v[8];
-        load8(p, 8, true, z);
-        if constexpr (GATED) load8(p + x.parts_half, 8, true, u);
+        load8(p, 8, z);
+        if constexpr (GATED) load8(p + x.parts_half, 8, u);
         for (int s = 1; s < x.splits; ++s) {
-            load8(p + s * stride, 8, true, v);
+            load8(p + s * stride, 8, v);
 #pragma unroll
             for (int i = 0; i < 8; ++i) z[i] += v[i];
             if constexpr (GATED) {
-                load8(p + s * stride + x.parts_half, 8, true, v);
+                load8(p + s * stride + x.parts_half, 8, v);
 #pragma unroll
                 for (int i = 0; i < 8; ++i) u[i] += v[i];
             }
@@ -986,7 +989,6 @@ struct PackJob {
     __bf16 *dst;
     long long ld, pitch, plane;
     int rows, cols;
-    bool vec;
 };
 struct PackJobs {
     PackJob job[3];
@@ -1002,7 +1004,7 @@ k_pack(const PackJobs jobs)
         const long long row = t / groups;
         const int col = (int)(t % groups) * 8;
         float v[8];
-        load8((const T *)j.src + row * j.ld + col, j.cols - col, j.vec, v);
+        load8((const T *)j.src + row * j.ld + col, j.cols - col, v);
         put8<PLANES>(j.dst + row * j.pitch + col, j.plane, v);
     }
 }
@@ -1041,7 +1043,6 @@ struct WidenJob {
     __bf16 *dst;
     long long ld, ld_scale, pitch;
     int rows, cols;
-    bool vec;
 };
 struct WidenJobs {
     WidenJob job[3];
@@ -1057,8 +1058,9 @@ k_widen(const WidenJobs jobs)
         const int col = (int)(t % groups) * 8, count = j.cols - col;
         const uint8_t *s = j.src + row * j.ld + col;
         uint2 w = make_uint2(0, 0);
-        if (j.vec && count >= 8) {
-            w = *reinterpret_cast<const uint2 *>(s);
+        if (count >= 8) {
+            const u32x2_any t = *reinterpret_cast<const u32x2_any *>(s);
+            w = make_uint2(t[0], t[1]);
         } else {
 #pragma unroll
             for (int i = 0; i < 8; ++i)
@@ -1081,8 +1083,7 @@ struct SlopeArgs {
     __bf16 *dz;                     // packed (null: column sums alone); gated: dg, and du `half` columns on
     float *part;                    // [group][part_pitch], nullable
     long long ld_dy, ld_z, pitch, plane, part_pitch;
-    int M, N, act, across, half;
-    bool vec;
+    int M, N, across, half;
 };
 template <typename T, int PLANES, int ACT>
 __global__ void __launch_bounds__(256)
@@ -1095,10 +1096,10 @@ k_slope(const SlopeArgs x)
     if (n < x.pitch) {
         for (long long m = (long long)blockIdx.y * down + r; m < x.M; m += (long long)gridDim.y * down) {
             float v[8];
-            load8((const T *)x.dy + m * x.ld_dy + n, count, x.vec, v);
+            load8((const T *)x.dy + m * x.ld_dy + n, count, v);
             if constexpr (ACT != 0) {
                 float z[8];
-                load8(x.z + m * x.ld_z + n, count, x.vec, z);
+                load8(x.z + m * x.ld_z + n, count, z);
 #pragma unroll
                 for (int i = 0; i < 8; ++i) {
                     float value, slope;
@@ -1119,7 +1120,7 @@ k_slope(const SlopeArgs x)
         for (int k = 1; k < down; ++k)
 #pragma unroll
             for (int i = 0; i < 8; ++i) sum[i] += sums[k * x.across + c][i];
-        store8(x.part + (size_t)blockIdx.y * x.part_pitch + n, 8, true, sum);
+        store8(x.part + (size_t)blockIdx.y * x.part_pitch + n, 8, sum);
     }
 }
 
@@ -1133,10 +1134,10 @@ k_gated_slope(const SlopeArgs x)
     if (n >= x.half) return;
     for (long long m = (long long)blockIdx.y * down + r; m < x.M; m += (long long)gridDim.y * down) {
         float d[8], lo[8], hi[8], dg[8], du[8];
-        load8((const T *)x.dy + m * x.ld_dy + n, count, x.vec, d);
+        load8((const T *)x.dy + m * x.ld_dy + n, count, d);
         const float *s = x.z + m * x.ld_z + 2 * (long long)n;
-        load8(s, 2 * count, x.vec, lo);
-        load8(s + 8, 2 * count - 8, x.vec, hi);
+        load8(s, 2 * count, lo);
+        load8(s + 8, 2 * count - 8, hi);
 #pragma unroll
         for (int i = 0; i < 8; ++i) {
             const float g = i < 4 ? lo[2 * i] : hi[2 * i - 8], u = i < 4 ? lo[2 * i + 1] : hi[2 * i - 7];
