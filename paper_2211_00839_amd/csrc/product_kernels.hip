@@ -710,7 +710,28 @@ template <int WT, bool GATED> struct Band {
         return !__any(!(zero == 0.f));
     }
 
-    __device__ __forceinline__ void inside(const Epilogue &e, int m, int n)
+    // The residual of a band on its way, ahead of the band's sums: nothing else runs on the unit to hide that trip.
+    static constexpr int HELD = GATED ? 1 : 32 * WT / 256;      // fp32: four columns to a lane; bf16 needs half of them
+    f32x4 held[HELD];
+    __device__ __forceinline__ void fetch_residual(const Epilogue &e, int m, int n)
+    {
+        if constexpr (!GATED) {
+            if (!e.residual) return;
+            if (e.out_f32) fetch_as<float, 4>(e, m, n);
+            else fetch_as<__bf16, 8>(e, m, n);
+        }
+    }
+    template <typename T, int V> __device__ __forceinline__ void fetch_as(const Epilogue &e, int m, int n)
+    {
+        const int lane = threadIdx.x & 63;
+        constexpr int LANES = COLS / V, ROWS = 64 / LANES, R = 32 / ROWS;
+        const T *res = (const T *)e.residual + (long long)(m + lane / LANES) * e.ld_r + n + (lane % LANES) * V;
+#pragma unroll
+        for (int k = 0; k < R; ++k) held[k] = *reinterpret_cast<const f32x4_any *>(res + k * ROWS * e.ld_r);
+    }
+
+    // next: the row of the band after this one, or -1
+    __device__ __forceinline__ void inside(const Epilogue &e, int m, int n, int next)
     {
         if constexpr (GATED) {
             if (e.preact) save_pairs(e, m, n);
@@ -718,8 +739,8 @@ template <int WT, bool GATED> struct Band {
             else gated<__bf16, 8>(e, m, n);
         } else {
             if (e.preact) save(e, m, n);
-            if (e.out_f32) linear<float, 4>(e, m, n);
-            else linear<__bf16, 8>(e, m, n);
+            if (e.out_f32) linear<float, 4>(e, m, n, next);
+            else linear<__bf16, 8>(e, m, n, next);
         }
     }
 
@@ -781,7 +802,7 @@ template <int WT, bool GATED> struct Band {
         }
     }
 
-    template <typename T, int V> __device__ __forceinline__ void linear(const Epilogue &e, int m, int n)
+    template <typename T, int V> __device__ __forceinline__ void linear(const Epilogue &e, int m, int n, int next)
     {
         const int lane = threadIdx.x & 63;
         constexpr int LANES = COLS / V, ROWS = 64 / LANES, R = 32 / ROWS;
@@ -790,14 +811,7 @@ template <int WT, bool GATED> struct Band {
         T *out = (T *)(second ? e.out2 : e.out);
         const long long ld = second ? e.ld_o2 : e.ld_o;
         out += (long long)(m - (second ? e.split_row : 0) + r0) * ld + n + c;
-        const T *res = (const T *)e.residual + (long long)(m + r0) * e.ld_r + n + c;
-        typedef typename Any<T>::type vec;
-        vec t[R];
         float z[R][V], b[V];
-        if (e.residual) {
-#pragma unroll
-            for (int k = 0; k < R; ++k) t[k] = *reinterpret_cast<const vec *>(res + k * ROWS * e.ld_r);
-        }
         if (e.bias) get<T, V>((const T *)e.bias + n + c, b);
 #pragma unroll
         for (int k = 0; k < R; ++k) sums<V>(r0 + k * ROWS, c, z[k]);
@@ -816,9 +830,13 @@ template <int WT, bool GATED> struct Band {
             });
         if (e.residual) {
 #pragma unroll
-            for (int k = 0; k < R; ++k)
+            for (int k = 0; k < R; ++k) {
+                typedef T vec __attribute__((ext_vector_type(V)));
+                const vec t = __builtin_bit_cast(vec, held[k]);
 #pragma unroll
-                for (int i = 0; i < V; ++i) z[k][i] += (float)t[k][i];
+                for (int i = 0; i < V; ++i) z[k][i] += (float)t[i];
+            }
+            if (next >= 0) fetch_residual(e, next, n);
         }
 #pragma unroll
         for (int k = 0; k < R; ++k) put<T, V>(out + k * ROWS * ld, z[k]);
@@ -889,6 +907,8 @@ k_tile(const Args x)
                 }
         }
     };
+    if constexpr (TO == TO_LINEAR)
+        if (inside) band.fetch_residual(x.e, wm, wn);
     // (a loop: unrolled, the code behind it would be there four times)
 #pragma unroll 1
     for (int i = 0; i < P::NB; ++i) {
@@ -899,7 +919,7 @@ k_tile(const Args x)
         pin();
         const int m = wm + i * 32;
         if constexpr (TO == TO_PARTS || TO == TO_GATED_PARTS) band.parts(x, split, m, wn);
-        else if (inside && (!x.pieces.a[0] || band.finite())) band.inside(x.e, m, wn);
+        else if (inside && (!x.pieces.a[0] || band.finite())) band.inside(x.e, m, wn, i + 1 < P::NB ? m + 32 : -1);
         else band.checked(x, m, wn);
         pin();
     }
