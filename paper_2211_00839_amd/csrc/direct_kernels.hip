@@ -1,0 +1,178 @@
+// fp32 products too small to pay for their operands' pieces: the operands go to the fp32 matrix instruction as they are,
+// in one launch.
+//
+// That instruction multiplies at a sixteenth of bf16's rate, against six products of pieces; but the pieces are a launch and a
+// trip through memory of their own, and what is left of a small product's time is launches.  A workgroup of four waves (2 x 2)
+// computes 64 x 64 sums (gated: 64 rows of 64 columns of both products), each wave 32 x 32 as one MFMA block (two).  k
+// advances 32 at a time; a stage goes from memory into LDS element by element (4 bytes a lane, so any alignment and any length
+// will do), three stages ahead of its multiplies (gated two), which take less time than a load.
+#include "product_kernels.hip"
+
+namespace enc {
+namespace direct {
+
+constexpr int KS = 32;                      // k of a stage
+constexpr int SIDE = 64 * KS;               // floats of one operand and stage
+
+struct Args {
+    tile::Args t;                           // epilogue, sizes, cut, parts (its sides and segments are not used)
+    const float *a[2], *b[2];               // per pair of a summed product; gated: b[1] is the second weight
+    long long a_pitch, b_pitch[2];          // from row to row (k contiguous) or from k to k (rows contiguous)
+    int a_extent, b_extent;                 // rows of either side that may be read
+    int pairs, K;
+};
+
+// One operand's way into LDS.  Each wave brings a quarter of a stage with eight loads of 64 elements.
+// k contiguous: rows of 32 floats, the four of k / 4 = c of row r at place c ^ (r & 7) (spreads what one pass of a
+// ds_read_b128 touches over the banks).  Rows contiguous: lines of 64 rows, turned by 32 where k has bit 2 set (the two
+// halves of a wave read lines four apart).
+template <int KIND> struct Feed {
+    unsigned row_off[8], kpos[8];           // K_RUNS: byte offset of a load's row, place in k
+    unsigned line_off[2];                   // ROWS_RUN: byte offset of this lane's row, in straight and in turned lines
+    const float *p;
+    long long pitch;
+
+    __device__ __forceinline__ void init(const float *p_, long long pitch_, int row0, int extent, int wave, int lane)
+    {
+        pitch = pitch_;
+        if constexpr (KIND == tile::K_RUNS) {
+            p = p_ + row0 * pitch;
+#pragma unroll
+            for (int u = 0; u < 8; ++u) {
+                const int r = wave * 16 + u * 2 + (lane >> 5);
+                row_off[u] = (unsigned)((min(row0 + r, extent - 1) - row0) * pitch * 4);
+                kpos[u] = ((((lane & 31) >> 2) ^ (r & 7)) << 2) | (lane & 3);
+            }
+        } else {
+            p = p_ + row0;
+            line_off[0] = (unsigned)(min(row0 + lane, extent - 1) - row0) * 4;
+            line_off[1] = (unsigned)(min(row0 + (lane ^ 32), extent - 1) - row0) * 4;
+        }
+    }
+    // The stage from k0 on; from `there` k on there is nothing, what lies past them in LDS is some element of them.
+    __device__ __forceinline__ void load(const float *from, int k0, int there, int wave, unsigned lds)
+    {
+#pragma unroll
+        for (int u = 0; u < 8; ++u) {
+            const unsigned to = lds + (wave * 8 + u) * 256;
+            if constexpr (KIND == tile::K_RUNS) {
+                const unsigned k = min(kpos[u], (unsigned)(there - 1));
+                tile::load4_to_lds(from + k0, row_off[u] + k * 4, to);
+            } else {
+                const int k = wave * 8 + u;
+                tile::load4_to_lds(from + (long long)(k0 + min(k, there - 1)) * pitch, line_off[(k >> 2) & 1], to);
+            }
+        }
+    }
+};
+
+// Four k (k8 + 4 half + 0 .. 3) of this lane's row of a wave's block.  side: the operand's stage.
+template <int KIND> __device__ __forceinline__ f32x4 four(const float *side, int row, int half, int k8)
+{
+    if constexpr (KIND == tile::K_RUNS) {
+        return *reinterpret_cast<const f32x4 *>(side + row * KS + (((k8 >> 2) + half) ^ (row & 7)) * 4);
+    } else {
+        f32x4 v;
+#pragma unroll
+        for (int e = 0; e < 4; ++e) v[e] = side[(k8 + half * 4 + e) * 64 + (row ^ (half * 32))];
+        return v;
+    }
+}
+
+template <int KA, int KB, int TO>
+__global__ void __launch_bounds__(256)
+k_direct(const Args x)
+{
+    constexpr bool GATED = TO == tile::TO_GATED || TO == tile::TO_GATED_PARTS;
+    constexpr int G = GATED ? 2 : 1, DEPTH = GATED ? 3 : 4, LOADS = 8 * (1 + G);
+    constexpr int STAGE = (1 + G) * SIDE;
+    using Out = tile::Band<GATED ? 64 : 32, GATED>;
+    __shared__ __attribute__((aligned(16))) float lds[DEPTH * STAGE];
+    static_assert(4 * 32 * Out::PITCH <= DEPTH * STAGE, "the waves' turn-round regions fit where the stages were");
+    int ti, tj, split;
+    if (!tile::tile_of_workgroup((int)blockIdx.x, (int)gridDim.x, x.t.tiles_m, x.t.tiles_n, x.t.splits, &ti, &tj, &split)) return;
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), wr = wave >> 1, wc = wave & 1;
+    const int m0 = ti * 64, n0 = tj * 64;
+    const int per = (x.K + KS - 1) / KS, all = per * x.pairs;
+    const int s0 = (int)((long long)all * split / x.t.splits), s1 = (int)((long long)all * (split + 1) / x.t.splits);
+    f32x16 acc[G];
+#pragma unroll
+    for (int g = 0; g < G; ++g)
+#pragma unroll
+        for (int r = 0; r < 16; ++r) acc[g][r] = 0.f;
+    Feed<KA> fa;
+    Feed<KB> fb[G];
+    fa.init(x.a[0], x.a_pitch, m0, x.a_extent, wave, lane);
+#pragma unroll
+    for (int g = 0; g < G; ++g) fb[g].init(x.b[g], x.b_pitch[g], n0, x.b_extent, wave, lane);
+    const unsigned lds_base = (unsigned)(size_t)(__attribute__((address_space(3))) float *)lds;
+    auto there = [&](int s) { return min(KS, x.K - (s >= per ? s - per : s) * KS); };       // k of stage s
+    auto fetch = [&](int s) {
+        const bool second = s >= per;
+        const int k0 = (second ? s - per : s) * KS;
+        const unsigned to = lds_base + (unsigned)((s - s0) % DEPTH) * (STAGE * 4);
+        fa.load(second ? fa.p + (x.a[1] - x.a[0]) : fa.p, k0, there(s), wave, to);
+#pragma unroll
+        for (int g = 0; g < G; ++g) {
+            if (!GATED && second) {
+                // (the second pair's b may have a pitch of its own)
+                Feed<KB> other;
+                other.init(x.b[1], x.b_pitch[1], n0, x.b_extent, wave, lane);
+                other.load(other.p, k0, there(s), wave, to + (1 + g) * (SIDE * 4));
+            } else {
+                fb[g].load(fb[g].p, k0, there(s), wave, to + (1 + g) * (SIDE * 4));
+            }
+        }
+    };
+#pragma unroll
+    for (int i = 0; i < DEPTH - 1; ++i)
+        if (s0 + i < s1) fetch(s0 + i);
+    const int half = lane >> 5, ra = wr * 32 + (lane & 31), rb = wc * 32 + (lane & 31);
+    for (int s = s0; s < s1; ++s) {
+        // stage s is there, in every wave, and nobody reads stage s - 1 any more
+        if (s + DEPTH - 2 < s1) tile::wait_loads<(DEPTH - 2) * LOADS>();
+        else tile::wait_loads<0>();
+        tile::wait_lds();
+        tile::meet();
+        if (s + DEPTH - 1 < s1) fetch(s + DEPTH - 1);
+        const float *stage = lds + ((s - s0) % DEPTH) * STAGE;
+        const int mine = there(s) - half * 4;
+#pragma unroll
+        for (int k = 0; k < KS; k += 8) {
+            // lanes 0-31 carry k = 0 .. 3 of each eight, lanes 32-63 k = 4 .. 7, for both operands alike
+            f32x4 a = four<KA>(stage, ra, half, k);
+#pragma unroll
+            for (int e = 0; e < 4; ++e) a[e] = k + e < mine ? a[e] : 0.f;
+#pragma unroll
+            for (int g = 0; g < G; ++g) {
+                f32x4 b = four<KB>(stage + (1 + g) * SIDE, rb, half, k);
+#pragma unroll
+                for (int e = 0; e < 4; ++e) b[e] = k + e < mine ? b[e] : 0.f;
+#pragma unroll
+                for (int e = 0; e < 4; ++e) acc[g] = __builtin_amdgcn_mfma_f32_32x32x2f32(b[e], a[e], acc[g], 0, 0, 0);
+            }
+        }
+    }
+    tile::wait_lds();
+    tile::meet();
+    Out band;
+    band.turn = lds + wave * (32 * Out::PITCH);
+#pragma unroll
+    for (int g = 0; g < G; ++g)
+#pragma unroll
+        for (int q = 0; q < 4; ++q)
+            *reinterpret_cast<f32x4 *>(band.turn + (lane & 31) * Out::PITCH + g * 32 + q * 8 + (lane >> 5) * 4) =
+                f32x4{acc[g][4 * q], acc[g][4 * q + 1], acc[g][4 * q + 2], acc[g][4 * q + 3]};
+    const int m = m0 + wr * 32, n = n0 + wc * 32;
+    if constexpr (TO == tile::TO_PARTS || TO == tile::TO_GATED_PARTS) {
+        band.parts(x.t, split, m, n);
+    } else if (m0 + 64 <= x.t.M && n0 + 64 <= x.t.N && x.t.e.split_row == 0x7fffffff) {
+        band.fetch_residual(x.t.e, m, n);
+        band.inside(x.t.e, m, n, -1);
+    } else {
+        band.checked(x.t, m, n);
+    }
+}
+
+} // namespace direct
+} // namespace enc

@@ -9,6 +9,7 @@
 #include "encoder_rules.h"
 #include "norm_kernels.hip"
 #include "product_kernels.hip"
+#include "direct_kernels.hip"
 #include "few_rows_kernels.hip"
 
 namespace {
@@ -289,6 +290,13 @@ size_t parts_bytes(const Cut &c, int64_t M, int64_t N, bool gated)
     return c.splits > 1 ? up256((size_t)c.splits * M * parts_pitch(N, gated) * 4) : 0;
 }
 
+void launch_join(const tile::Args &x, bool gated, hipStream_t stream)
+{
+    const dim3 grid(copy_grid((int64_t)x.M * ((x.N + 7) / 8)));
+    if (gated) hipLaunchKernelGGL(tile::k_join<true>, grid, dim3(256), 0, stream, x);
+    else hipLaunchKernelGGL(tile::k_join<false>, grid, dim3(256), 0, stream, x);
+}
+
 int launch_product(const Product &p, Pieces &room, hipStream_t stream)
 {
     ENC_TRY(set_up());
@@ -355,11 +363,79 @@ int launch_product(const Product &p, Pieces &room, hipStream_t stream)
                            dim3((unsigned)((workgroups + 7) / 8 * 8)), dim3(tile::THREADS), (tile::Shape<W, X>::LDS_BYTES), stream, x);
         return (int)RCD_OK;
     }));
-    if (c.splits > 1) {
-        const dim3 grid(copy_grid(p.M * ((p.N + 7) / 8)));
-        if (p.gated) hipLaunchKernelGGL(tile::k_join<true>, grid, dim3(256), 0, stream, x);
-        else hipLaunchKernelGGL(tile::k_join<false>, grid, dim3(256), 0, stream, x);
+    if (c.splits > 1) launch_join(x, p.gated, stream);
+    ENC_HIP_TRY(hipGetLastError());
+    return RCD_OK;
+}
+
+// fp32 operands in place.
+struct DirectProduct {
+    int64_t M, N, K;
+    int ka, kb, pairs;
+    bool gated;
+    const float *a[2], *b[2];
+    int64_t a_pitch, b_pitch[2];
+    int64_t a_extent, b_extent;
+    Epilogue e;
+};
+Cut direct_cut(int64_t M, int64_t N, int64_t K, int pairs, bool gated)
+{
+    return enc_rules::direct_cut_of(M, N, enc_rules::ceil_div(K, enc_rules::DIRECT_STAGE) * pairs, gated);
+}
+
+size_t direct_parts(int64_t M, int64_t N, int64_t K, int pairs, bool gated, int dt)
+{
+    return dt == RCD_F32 ? parts_bytes(direct_cut(M, N, K, pairs, gated), M, N, gated) : 0;
+}
+
+// Rows of these pitches lie near enough for the direct kernel's 32-bit offsets inside a tile.
+inline bool near_enough(int64_t ld_a, int64_t ld_b = 0, int64_t ld_c = 0) { return std::max({ld_a, ld_b, ld_c}) <= ((int64_t)1 << 23); }
+
+int launch_direct(const DirectProduct &p, Pieces &room, hipStream_t stream)
+{
+    static_assert(enc_rules::DIRECT_STAGE == direct::KS, "the rule counts the kernel's stages");
+    const Cut c = direct_cut(p.M, p.N, p.K, p.pairs, p.gated);
+    const int64_t workgroups = c.tiles_m * c.tiles_n * c.splits;
+    if (workgroups > 0x7ffffff0) return RCD_ERR_UNSUPPORTED;
+    direct::Args x{};
+    for (int i = 0; i < 2; ++i) {
+        x.a[i] = p.a[i];
+        x.b[i] = p.b[i];
+        x.b_pitch[i] = p.b_pitch[i];
     }
+    x.a_pitch = p.a_pitch;
+    x.a_extent = (int)p.a_extent;
+    x.b_extent = (int)p.b_extent;
+    x.pairs = p.pairs;
+    x.K = (int)p.K;
+    x.t.e = p.e;
+    x.t.M = (int)p.M;
+    x.t.N = (int)p.N;
+    x.t.tiles_m = (int)c.tiles_m;
+    x.t.tiles_n = (int)c.tiles_n;
+    x.t.splits = c.splits;
+    if (c.splits > 1) {
+        x.t.parts_pitch = parts_pitch(p.N, p.gated);
+        x.t.parts_half = (int)(x.t.parts_pitch / 2);
+        x.t.parts = room.take<float>((size_t)c.splits * p.M * x.t.parts_pitch);
+    }
+    const dim3 grid((unsigned)((workgroups + 7) / 8 * 8));
+    constexpr int K = tile::K_RUNS, R = tile::ROWS_RUN;
+    auto go = [&](auto kernel) { hipLaunchKernelGGL(kernel, grid, dim3(256), 0, stream, x); };
+    if (p.gated) {
+        if (c.splits > 1) go(direct::k_direct<K, K, tile::TO_GATED_PARTS>);
+        else go(direct::k_direct<K, K, tile::TO_GATED>);
+    } else if (p.ka == R) {
+        if (c.splits > 1) go(direct::k_direct<R, R, tile::TO_PARTS>);
+        else go(direct::k_direct<R, R, tile::TO_LINEAR>);
+    } else if (p.kb == R) {
+        if (c.splits > 1) go(direct::k_direct<K, R, tile::TO_PARTS>);
+        else go(direct::k_direct<K, R, tile::TO_LINEAR>);
+    } else {
+        if (c.splits > 1) go(direct::k_direct<K, K, tile::TO_PARTS>);
+        else go(direct::k_direct<K, K, tile::TO_LINEAR>);
+    }
+    if (c.splits > 1) launch_join(x.t, p.gated, stream);
     ENC_HIP_TRY(hipGetLastError());
     return RCD_OK;
 }
@@ -605,7 +681,8 @@ int rcd_rms_norm_backward(const void *dY_dev, int dt, int64_t rows, int64_t d, i
 size_t rcd_linear_workspace_bytes(int64_t M, int64_t N, int64_t K, int dt)
 {
     if (!product_sizes_ok(M, N, K) || dt < RCD_F32 || dt > RCD_MXFP8 || M <= few_rows(dt)) return 0;
-    return packed_bytes(M, K, dt) + packed_bytes(N, K, dt) + parts_bytes(cut_of(M, N, K, product_type(dt, K), 1, false), M, N, false);
+    return packed_bytes(M, K, dt) + packed_bytes(N, K, dt) +
+           std::max(parts_bytes(cut_of(M, N, K, product_type(dt, K), 1, false), M, N, false), direct_parts(M, N, K, 1, false, dt));
 }
 
 int rcd_linear(const void *A_dev, const uint8_t *A_scale_dev, int64_t ld_a, int64_t ld_a_scale,
@@ -634,6 +711,20 @@ int rcd_linear(const void *A_dev, const uint8_t *A_scale_dev, int64_t ld_a, int6
         return launch_few(dt, false, x, stream);
     }
     Pieces room(workspace_dev);
+    if (dt == RCD_F32 && enc_rules::direct_forward(M, N, K, false) && near_enough(ld_a, ld_w)) {
+        DirectProduct p{};
+        p.M = M; p.N = N; p.K = K;
+        p.ka = p.kb = tile::K_RUNS;
+        p.pairs = 1;
+        p.a[0] = (const float *)A_dev;
+        p.b[0] = (const float *)W_dev;
+        p.a_pitch = ld_a;
+        p.b_pitch[0] = ld_w;
+        p.a_extent = M;
+        p.b_extent = N;
+        p.e = e;
+        return launch_direct(p, room, stream);
+    }
     Packer pack{dt};
     Product p{};
     p.M = M; p.N = N; p.K = K;
@@ -653,7 +744,8 @@ size_t rcd_linear_backward_workspace_bytes(int64_t M, int64_t N, int64_t K, int 
     linear_back(w, M, N, dt);
     // (the two products run one after the other: the larger one's parts)
     return w.used + packed_bytes(M, K, dt) + packed_bytes(N, K, dt) +
-           std::max(parts_bytes(cut_of(M, K, N, dt, 1, false), M, K, false), parts_bytes(cut_of(N, K, M, dt, 1, false), N, K, false));
+           std::max({parts_bytes(cut_of(M, K, N, dt, 1, false), M, K, false), parts_bytes(cut_of(N, K, M, dt, 1, false), N, K, false),
+                     direct_parts(M, K, N, 1, false, dt), direct_parts(N, K, M, 1, false, dt)});
 }
 
 int rcd_linear_backward(const void *dY_dev, int64_t ld_dy, const void *A_dev, int64_t ld_a, const void *W_dev, int64_t ld_w,
@@ -676,13 +768,15 @@ int rcd_linear_backward(const void *dY_dev, int64_t ld_dy, const void *A_dev, in
     Pieces room(workspace_dev);
     const LinearBack w = linear_back(room, M, N, dt);
     Packer pack{dt};
-    // dz itself, in place, where there is no activation and its rows can go into LDS as they are
+    const bool in_place = f32 && enc_rules::direct_backward(M, N, K, false) && near_enough(ld_dy);     // (no pieces)
+    // dz itself, in place, where there is no activation and its rows can be read as they are
     Laid dz;
     Laid a, b;
-    if (dW_dev) a = pack.lay(room, A_dev, nullptr, 0, M, K, ld_a);
-    if (dA_dev) b = pack.lay(room, W_dev, nullptr, 0, N, K, ld_w);
+    if (dW_dev && !in_place) a = pack.lay(room, A_dev, nullptr, 0, M, K, ld_a);
+    if (dA_dev && !in_place) b = pack.lay(room, W_dev, nullptr, 0, N, K, ld_w);
     ENC_TRY(pack.launch(stream));
-    const bool as_it_is = act == RCD_ACT_NONE && dt == RCD_BF16 && rows_aligned(dY_dev, ld_dy, 2) && N % 8 == 0 && ld_dy * 2 <= ((int64_t)1 << 23);
+    const bool as_it_is = act == RCD_ACT_NONE &&
+                          (in_place || (!f32 && rows_aligned(dY_dev, ld_dy, 2) && N % 8 == 0 && ld_dy * 2 <= ((int64_t)1 << 23)));
     const int64_t pitch = up64(N);
     if (as_it_is) {
         dz.p = (const unsigned char *)dY_dev;
@@ -706,16 +800,46 @@ int rcd_linear_backward(const void *dY_dev, int64_t ld_dy, const void *A_dev, in
         const dim3 grid((unsigned)c.pieces, (unsigned)c.groups);
         with_act_value(act, [&](auto a) {
             constexpr int A = decltype(a)::value;
-            if (f32) hipLaunchKernelGGL((k_slope<float, 3, A>), grid, dim3(256), 0, stream, x);
+            if (in_place) hipLaunchKernelGGL((k_slope<float, 0, A>), grid, dim3(256), 0, stream, x);
+            else if (f32) hipLaunchKernelGGL((k_slope<float, 3, A>), grid, dim3(256), 0, stream, x);
             else hipLaunchKernelGGL((k_slope<__bf16, 1, A>), grid, dim3(256), 0, stream, x);
         });
         ENC_HIP_TRY(hipGetLastError());
         if (dbias_dev) ENC_TRY(sum_columns(w.part, x.part_pitch, c.groups, N, dbias_dev, dt, stream));
     }
+    const size_t mark = room.used;
+    if (in_place) {
+        DirectProduct p{};
+        p.pairs = 1;
+        p.a[0] = as_it_is ? (const float *)dY_dev : (const float *)w.dz;
+        p.a_pitch = as_it_is ? ld_dy : pitch;
+        if (dA_dev) {
+            p.M = M; p.N = K; p.K = N;
+            p.ka = tile::K_RUNS;
+            p.kb = tile::ROWS_RUN;
+            p.b[0] = (const float *)W_dev;
+            p.b_pitch[0] = ld_w;
+            p.a_extent = M;
+            p.b_extent = K;
+            p.e = one_output(dA_dev, ld_da, dt, RCD_ACT_NONE);
+            ENC_TRY(launch_direct(p, room, stream));
+        }
+        room.used = mark;
+        if (dW_dev) {
+            p.M = N; p.N = K; p.K = M;
+            p.ka = p.kb = tile::ROWS_RUN;
+            p.b[0] = (const float *)A_dev;
+            p.b_pitch[0] = ld_a;
+            p.a_extent = N;
+            p.b_extent = K;
+            p.e = one_output(dW_dev, ld_dw, dt, RCD_ACT_NONE);
+            ENC_TRY(launch_direct(p, room, stream));
+        }
+        return RCD_OK;
+    }
     Product p{};
     p.dt = dt;
     p.pairs = 1;
-    const size_t mark = room.used;
     if (dA_dev) {
         p.M = M; p.N = K; p.K = N;
         p.ka = tile::K_RUNS;
@@ -740,7 +864,8 @@ int rcd_linear_backward(const void *dY_dev, int64_t ld_dy, const void *A_dev, in
 size_t rcd_gated_linear_workspace_bytes(int64_t M, int64_t F, int64_t K, int dt)
 {
     if (!product_sizes_ok(M, F, K) || dt < RCD_F32 || dt > RCD_MXFP8 || M <= few_rows(dt)) return 0;
-    return packed_bytes(M, K, dt) + 2 * packed_bytes(F, K, dt) + parts_bytes(cut_of(M, F, K, product_type(dt, K), 1, true), M, F, true);
+    return packed_bytes(M, K, dt) + 2 * packed_bytes(F, K, dt) +
+           std::max(parts_bytes(cut_of(M, F, K, product_type(dt, K), 1, true), M, F, true), direct_parts(M, F, K, 1, true, dt));
 }
 
 int rcd_gated_linear(const void *A_dev, const uint8_t *A_scale_dev, int64_t ld_a, int64_t ld_a_scale,
@@ -768,6 +893,23 @@ int rcd_gated_linear(const void *A_dev, const uint8_t *A_scale_dev, int64_t ld_a
         return launch_few(dt, true, x, stream);
     }
     Pieces room(workspace_dev);
+    if (dt == RCD_F32 && enc_rules::direct_forward(M, F, K, true) && near_enough(ld_a, ld_wg, ld_wu)) {
+        DirectProduct p{};
+        p.M = M; p.N = F; p.K = K;
+        p.ka = p.kb = tile::K_RUNS;
+        p.pairs = 1;
+        p.gated = true;
+        p.a[0] = (const float *)A_dev;
+        p.b[0] = (const float *)Wg_dev;
+        p.b[1] = (const float *)Wu_dev;
+        p.a_pitch = ld_a;
+        p.b_pitch[0] = ld_wg;
+        p.b_pitch[1] = ld_wu;
+        p.a_extent = M;
+        p.b_extent = F;
+        p.e = e;
+        return launch_direct(p, room, stream);
+    }
     Packer pack{dt};
     Product p{};
     p.M = M; p.N = F; p.K = K;
@@ -787,8 +929,9 @@ size_t rcd_gated_linear_backward_workspace_bytes(int64_t M, int64_t F, int64_t K
     Pieces w(nullptr);
     w.take<__bf16>((size_t)M * 2 * up64(F) * (dt == RCD_F32 ? 3 : 1));
     return w.used + packed_bytes(M, K, dt) + 2 * packed_bytes(F, K, dt) +
-           std::max(parts_bytes(cut_of(M, K, F, dt, 2, false), M, K, false),
-                    parts_bytes(cut_of(2 * up64(F), K, M, dt, 1, false), 2 * up64(F), K, false));
+           std::max({parts_bytes(cut_of(M, K, F, dt, 2, false), M, K, false),
+                     parts_bytes(cut_of(2 * up64(F), K, M, dt, 1, false), 2 * up64(F), K, false), direct_parts(M, K, F, 2, false, dt),
+                     direct_parts(2 * up64(F), K, M, 1, false, dt)});
 }
 
 int rcd_gated_linear_backward(const void *dH_dev, int64_t ld_dh, const void *A_dev, int64_t ld_a,
@@ -813,12 +956,13 @@ int rcd_gated_linear_backward(const void *dH_dev, int64_t ld_dh, const void *A_d
     const int64_t half = up64(F), pitch = 2 * half;
     Pieces room(workspace_dev);
     __bf16 *dgu = room.take<__bf16>((size_t)M * pitch * (f32 ? 3 : 1));
+    const bool in_place = f32 && enc_rules::direct_backward(M, F, K, true);      // (no pieces)
     Packer pack{dt};
     Product p{};
     p.dt = dt;
     Laid a;
-    if (dWg_dev) a = pack.lay(room, A_dev, nullptr, 0, M, K, ld_a);
-    if (dA_dev) ENC_TRY(lay_pair(pack, room, p.b, dt, Wg_dev, nullptr, ld_wg, 0, Wu_dev, nullptr, ld_wu, 0, F, K));
+    if (dWg_dev && !in_place) a = pack.lay(room, A_dev, nullptr, 0, M, K, ld_a);
+    if (dA_dev && !in_place) ENC_TRY(lay_pair(pack, room, p.b, dt, Wg_dev, nullptr, ld_wg, 0, Wu_dev, nullptr, ld_wu, 0, F, K));
     ENC_TRY(pack.launch(stream));
     const SlopeCut c = slope_cut(M, half);
     SlopeArgs x{};
@@ -830,10 +974,50 @@ int rcd_gated_linear_backward(const void *dH_dev, int64_t ld_dh, const void *A_d
     const dim3 grid((unsigned)c.pieces, (unsigned)c.groups);
     with_act_value(act, [&](auto a) {
         constexpr int A = decltype(a)::value;
-        if (f32) hipLaunchKernelGGL((k_gated_slope<float, 3, A>), grid, dim3(256), 0, stream, x);
+        if (in_place) hipLaunchKernelGGL((k_gated_slope<float, 0, A>), grid, dim3(256), 0, stream, x);
+        else if (f32) hipLaunchKernelGGL((k_gated_slope<float, 3, A>), grid, dim3(256), 0, stream, x);
         else hipLaunchKernelGGL((k_gated_slope<__bf16, 1, A>), grid, dim3(256), 0, stream, x);
     });
     ENC_HIP_TRY(hipGetLastError());
+    Epilogue both = one_output(dWg_dev, ld_dwg, dt, RCD_ACT_NONE);       // dg's columns and du's are the rows of one product
+    both.out2 = dWu_dev;
+    both.ld_o2 = ld_dwu;
+    both.split_row = (int)half;
+    both.rows_each = (int)F;
+    if (in_place) {
+        DirectProduct q{};
+        const size_t mark = room.used;
+        q.a[0] = (const float *)dgu;
+        q.a[1] = q.a[0] + half;
+        q.a_pitch = pitch;
+        if (dA_dev) {
+            q.M = M; q.N = K; q.K = F;
+            q.ka = tile::K_RUNS;
+            q.kb = tile::ROWS_RUN;
+            q.pairs = 2;
+            q.b[0] = (const float *)Wg_dev;
+            q.b[1] = (const float *)Wu_dev;
+            q.b_pitch[0] = ld_wg;
+            q.b_pitch[1] = ld_wu;
+            q.a_extent = M;
+            q.b_extent = K;
+            q.e = one_output(dA_dev, ld_da, dt, RCD_ACT_NONE);
+            ENC_TRY(launch_direct(q, room, stream));
+        }
+        room.used = mark;
+        if (dWg_dev) {
+            q.M = pitch; q.N = K; q.K = M;
+            q.ka = q.kb = tile::ROWS_RUN;
+            q.pairs = 1;
+            q.b[0] = (const float *)A_dev;
+            q.b_pitch[0] = ld_a;
+            q.a_extent = pitch;
+            q.b_extent = K;
+            q.e = both;
+            ENC_TRY(launch_direct(q, room, stream));
+        }
+        return RCD_OK;
+    }
     Laid d;
     d.p = (const unsigned char *)dgu;
     d.pitch = pitch * 2;
@@ -852,16 +1036,11 @@ int rcd_gated_linear_backward(const void *dH_dev, int64_t ld_dh, const void *A_d
     }
     room.used = mark;
     if (dWg_dev) {
-        // dg's columns and du's are the rows of one product
         p.M = pitch; p.N = K; p.K = M;
         p.ka = p.kb = tile::ROWS_RUN;
         p.pairs = 1;
         p.b[0] = a;
-        p.e = one_output(dWg_dev, ld_dwg, dt, RCD_ACT_NONE);
-        p.e.out2 = dWu_dev;
-        p.e.ld_o2 = ld_dwu;
-        p.e.split_row = (int)half;
-        p.e.rows_each = (int)F;
+        p.e = both;
         ENC_TRY(launch_product(p, room, stream));
     }
     return RCD_OK;

@@ -65,4 +65,59 @@ inline Cut cut_of(int64_t M, int64_t N, int64_t stages, bool gated)
     return best;
 }
 
+// fp32 products go to the fp32 matrix instruction directly (wt 32: tiles of 64 x 64, k in stages of 32) where that takes less
+// than pieces do, whose launch and trip through memory come on top (4.5 us and 10 bytes per element at 5 TB/s).
+constexpr int DIRECT_STAGE = 32;
+inline double direct_time_of(const Cut &c, int64_t M, int64_t N, int64_t stages, bool gated)
+{
+    const int64_t workgroups = c.tiles_m * c.tiles_n * c.splits, deep = ceil_div(stages, c.splits);
+    // a stage takes 0.55 us (gated: of two products) however many workgroups share a unit, up to four
+    double t = 4.0 + (double)ceil_div(workgroups, UNITS) * (double)deep * (gated ? 1.0 : 0.55);
+    if (c.splits > 1) t += 3.5 + 0.25 * c.splits + 2e-6 / 7 * (double)c.splits * (double)M * (double)N * 4 * (gated ? 2 : 1);
+    return t;
+}
+inline Cut direct_cut_of(int64_t M, int64_t N, int64_t stages, bool gated)
+{
+    Cut best{};
+    double least = 0.0;
+    Cut c;
+    c.wt = 32;
+    c.tiles_m = ceil_div(M, 64);
+    c.tiles_n = ceil_div(N, 64);
+    for (int splits : {1, 2, 3, 4, 5, 6, 8, 10, 12, 16}) {
+        if (splits > 1 && (splits * 2 > stages || c.tiles_m * c.tiles_n * splits > 2 * UNITS)) break;
+        c.splits = splits;
+        const double t = direct_time_of(c, M, N, stages, gated);
+        if (best.splits == 0 || t < least) {
+            best = c;
+            least = t;
+        }
+    }
+    return best;
+}
+inline double pieces_time(int64_t elements) { return 4.5 + 1e-6 / 5 * 10.0 * (double)elements; }
+
+// One fp32 product of `pairs` summed ones: by the direct kernel / by pieces, without the making of the pieces.
+inline double direct_time(int64_t M, int64_t N, int64_t K, int pairs, bool gated)
+{
+    const int64_t stages = ceil_div(K, DIRECT_STAGE) * pairs;
+    return direct_time_of(direct_cut_of(M, N, stages, gated), M, N, stages, gated);
+}
+inline double pieces_product_time(int64_t M, int64_t N, int64_t K, int pairs, bool gated)
+{
+    const int64_t stages = ceil_div(K, 64) * 6 * pairs;
+    return time_of(cut_of(M, N, stages, gated), M, N, stages, gated);
+}
+// Whole calls.
+inline bool direct_forward(int64_t M, int64_t N, int64_t K, bool gated)
+{
+    return direct_time(M, N, K, 1, gated) < pieces_product_time(M, N, K, 1, gated) + pieces_time((M + N * (gated ? 2 : 1)) * K);
+}
+inline bool direct_backward(int64_t M, int64_t N, int64_t K, bool gated)
+{
+    const int w = gated ? 2 : 1;
+    return direct_time(M, K, N, w, false) + direct_time(w * N, K, M, 1, false) <
+           pieces_product_time(M, K, N, w, false) + pieces_product_time(w * N, K, M, 1, false) + pieces_time((M + N * w) * K);
+}
+
 } // namespace enc_rules

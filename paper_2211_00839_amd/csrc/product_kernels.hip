@@ -4,6 +4,7 @@
 //
 // on the matrix cores, for operands whose k is contiguous (the forward products) or whose rows are (the gradients: no matrix
 // is ever transposed in memory), in bf16, in fp32 as three bf16 pieces, or in 8 bits with block scales.
+#pragma once
 #include "encoder_math.h"
 
 namespace enc {
@@ -189,6 +190,12 @@ __device__ __forceinline__ void load4_to_lds(const void *base, unsigned offset, 
 }
 template <int N> __device__ __forceinline__ void wait_loads() { asm volatile("s_waitcnt vmcnt(%0)" ::"n"(N) : "memory"); }
 __device__ __forceinline__ void wait_lds() { asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory"); }
+// A barrier that no access to LDS is moved across.
+__device__ __forceinline__ void meet()
+{
+    __builtin_amdgcn_s_barrier();
+    asm volatile("" ::: "memory");
+}
 __device__ __forceinline__ void pin() { __builtin_amdgcn_sched_barrier(0); }
 
 typedef short s16x4 __attribute__((ext_vector_type(4)));
@@ -465,7 +472,7 @@ struct Pipe {
             wait_loads<0>();
         }
         wait_lds();
-        __builtin_amdgcn_s_barrier();
+        meet();
         Frags f0, f1, f2, f3;
         Frags8 p0, p1;
         Words w, wn;
@@ -494,7 +501,7 @@ struct Pipe {
             auto give_up = [&]() {
                 wait_loads<0>();
                 wait_lds();
-                __builtin_amdgcn_s_barrier();
+                meet();
             };
             // the refill's loads: `done` of them are out, `count` more
             auto refill = [&](int done, int count) {
@@ -596,7 +603,7 @@ struct Pipe {
         }
         stage(bool_constant<false>{}, bool_constant<false>{});
         wait_lds();
-        __builtin_amdgcn_s_barrier();
+        meet();
     }
 };
 
@@ -979,9 +986,15 @@ __device__ __forceinline__ void pieces_of(float v, __bf16 &a, __bf16 &b, __bf16 
     c = (__bf16)(r - mid);
 }
 
-// Eight values into a packed operand: bf16, or the three pieces in planes `plane` elements apart.
-template <int PLANES> __device__ __forceinline__ void put8(__bf16 *p, long long plane, const float (&v)[8])
+// Eight values into a packed operand, from element `at` on: bf16, or the three pieces in planes `plane` elements apart, or
+// (PLANES = 0) fp32 as it is.
+template <int PLANES> __device__ __forceinline__ void put8(__bf16 *base, long long at, long long plane, const float (&v)[8])
 {
+    if constexpr (PLANES == 0) {
+        store8((float *)base + at, 8, v);
+        return;
+    }
+    __bf16 *p = base + at;
     bf16x8 a, b, c;
 #pragma unroll
     for (int i = 0; i < 8; ++i) {
@@ -1025,7 +1038,7 @@ k_pack(const PackJobs jobs)
         const int col = (int)(t % groups) * 8;
         float v[8];
         load8((const T *)j.src + row * j.ld + col, j.cols - col, v);
-        put8<PLANES>(j.dst + row * j.pitch + col, j.plane, v);
+        put8<PLANES>(j.dst, row * j.pitch + col, j.plane, v);
     }
 }
 
@@ -1129,7 +1142,7 @@ k_slope(const SlopeArgs x)
             }
 #pragma unroll
             for (int i = 0; i < 8; ++i) sum[i] += v[i];
-            if (x.dz) put8<PLANES>(x.dz + m * x.pitch + n, x.plane, v);
+            if (x.dz) put8<PLANES>(x.dz, m * x.pitch + n, x.plane, v);
         }
     }
     if (!x.part) return;
@@ -1166,8 +1179,8 @@ k_gated_slope(const SlopeArgs x)
             dg[i] = i < count ? d[i] * u * slope : 0.f;
             du[i] = i < count ? d[i] * value : 0.f;
         }
-        put8<PLANES>(x.dz + m * x.pitch + n, x.plane, dg);
-        put8<PLANES>(x.dz + m * x.pitch + x.half + n, x.plane, du);
+        put8<PLANES>(x.dz, m * x.pitch + n, x.plane, dg);
+        put8<PLANES>(x.dz, m * x.pitch + x.half + n, x.plane, du);
     }
 }
 
