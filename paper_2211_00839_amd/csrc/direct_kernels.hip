@@ -13,6 +13,7 @@ namespace direct {
 
 constexpr int KS = 32;                      // k of a stage
 constexpr int SIDE = 64 * KS;               // floats of one operand and stage
+constexpr int LDS_FLOATS = 9 * SIDE;        // three stages of three operands, or four of two
 
 struct Args {
     tile::Args t;                           // epilogue, sizes, cut, parts (its sides and segments are not used)
@@ -80,17 +81,15 @@ template <int KIND> __device__ __forceinline__ f32x4 four(const float *side, int
 }
 
 template <int KA, int KB, int TO>
-__global__ void __launch_bounds__(256)
-k_direct(const Args x)
+__device__ __forceinline__ void direct_body(const Args &x, int wg, int nwg, float *lds)
 {
     constexpr bool GATED = TO == tile::TO_GATED || TO == tile::TO_GATED_PARTS;
     constexpr int G = GATED ? 2 : 1, DEPTH = GATED ? 3 : 4, LOADS = 8 * (1 + G);
     constexpr int STAGE = (1 + G) * SIDE;
     using Out = tile::Band<GATED ? 64 : 32, GATED>;
-    __shared__ __attribute__((aligned(16))) float lds[DEPTH * STAGE];
-    static_assert(4 * 32 * Out::PITCH <= DEPTH * STAGE, "the waves' turn-round regions fit where the stages were");
+    static_assert(DEPTH * STAGE <= LDS_FLOATS && 4 * 32 * Out::PITCH <= DEPTH * STAGE, "the waves' turn-round regions fit where the stages were");
     int ti, tj, split;
-    if (!tile::tile_of_workgroup((int)blockIdx.x, (int)gridDim.x, x.t.tiles_m, x.t.tiles_n, x.t.splits, &ti, &tj, &split)) return;
+    if (!tile::tile_of_workgroup(wg, nwg, x.t.tiles_m, x.t.tiles_n, x.t.splits, &ti, &tj, &split)) return;
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), wr = wave >> 1, wc = wave & 1;
     const int m0 = ti * 64, n0 = tj * 64;
     const int per = (x.K + KS - 1) / KS, all = per * x.pairs;
@@ -171,6 +170,29 @@ k_direct(const Args x)
         band.inside(x.t.e, m, n, -1);
     } else {
         band.checked(x.t, m, n);
+    }
+}
+
+template <int KA, int KB, int TO>
+__global__ void __launch_bounds__(256)
+k_direct(const Args x)
+{
+    __shared__ __attribute__((aligned(16))) float lds[LDS_FLOATS];
+    direct_body<KA, KB, TO>(x, (int)blockIdx.x, (int)gridDim.x, lds);
+}
+
+// A backward call's two products side by side: x's workgroups are the first `first` (a multiple of 8) of the launch.
+__global__ void __launch_bounds__(256)
+k_direct_both(const Args x, const Args y, int first)
+{
+    __shared__ __attribute__((aligned(16))) float lds[LDS_FLOATS];
+    const int wg = (int)blockIdx.x;
+    if (wg < first) {
+        if (x.t.splits > 1) direct_body<tile::K_RUNS, tile::ROWS_RUN, tile::TO_PARTS>(x, wg, first, lds);
+        else direct_body<tile::K_RUNS, tile::ROWS_RUN, tile::TO_LINEAR>(x, wg, first, lds);
+    } else {
+        if (y.t.splits > 1) direct_body<tile::ROWS_RUN, tile::ROWS_RUN, tile::TO_PARTS>(y, wg - first, (int)gridDim.x - first, lds);
+        else direct_body<tile::ROWS_RUN, tile::ROWS_RUN, tile::TO_LINEAR>(y, wg - first, (int)gridDim.x - first, lds);
     }
 }
 

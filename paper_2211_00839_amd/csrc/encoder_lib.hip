@@ -144,6 +144,8 @@ int set_up()
                         return (int)RCD_OK;
                     }));
                 }
+        ENC_HIP_TRY(hipFuncSetAttribute(reinterpret_cast<const void *>(&tile::k_tile_both), hipFuncAttributeMaxDynamicSharedMemorySize,
+                                        (tile::Shape<64, false>::LDS_BYTES)));
         g_ready[dev] = true;
     }
     return RCD_OK;
@@ -290,6 +292,40 @@ size_t parts_bytes(const Cut &c, int64_t M, int64_t N, bool gated)
     return c.splits > 1 ? up256((size_t)c.splits * M * parts_pitch(N, gated) * 4) : 0;
 }
 
+inline unsigned grid_of(const Cut &c) { return (unsigned)((enc_rules::workgroups_of(c) + 7) / 8 * 8); }
+inline bool launchable(const Cut &c) { return enc_rules::workgroups_of(c) <= 0x7ffffff0; }
+
+void take_parts(tile::Args &x, bool gated, Pieces &room)
+{
+    if (x.splits == 1) return;
+    x.parts_pitch = parts_pitch(x.N, gated);
+    x.parts_half = (int)(x.parts_pitch / 2);
+    x.parts = room.take<float>((size_t)x.splits * x.M * x.parts_pitch);
+}
+
+int sum_columns(const tile::Columns &c, hipStream_t stream)
+{
+    const dim3 grid((unsigned)((c.d + 15) / 16));
+    if (c.f32)
+        hipLaunchKernelGGL(k_column_sums<float>, grid, dim3(1024), 0, stream, c.part, c.pitch, c.groups, c.d, (float *)c.out);
+    else
+        hipLaunchKernelGGL(k_column_sums<__bf16>, grid, dim3(1024), 0, stream, c.part, c.pitch, c.groups, c.d, (__bf16 *)c.out);
+    ENC_HIP_TRY(hipGetLastError());
+    return RCD_OK;
+}
+
+int launch_join_both(const tile::Args &x, const tile::Args &y, const tile::Columns &c, hipStream_t stream)
+{
+    if (x.splits > 1 || y.splits > 1 || c.part) {
+        int64_t items = (int64_t)(c.d + 15) / 16 * 256;
+        if (x.splits > 1) items = std::max(items, (int64_t)x.M * ((x.N + 7) / 8));
+        if (y.splits > 1) items = std::max(items, (int64_t)y.M * ((y.N + 7) / 8));
+        hipLaunchKernelGGL(tile::k_join_both, dim3(copy_grid(items), 3), dim3(256), 0, stream, x, y, c);
+    }
+    ENC_HIP_TRY(hipGetLastError());
+    return RCD_OK;
+}
+
 void launch_join(const tile::Args &x, bool gated, hipStream_t stream)
 {
     const dim3 grid(copy_grid((int64_t)x.M * ((x.N + 7) / 8)));
@@ -297,12 +333,9 @@ void launch_join(const tile::Args &x, bool gated, hipStream_t stream)
     else hipLaunchKernelGGL(tile::k_join<false>, grid, dim3(256), 0, stream, x);
 }
 
-int launch_product(const Product &p, Pieces &room, hipStream_t stream)
+// The kernel's arguments; parts are taken from `room`.
+tile::Args plan_product(const Product &p, const Cut &c, Pieces &room)
 {
-    ENC_TRY(set_up());
-    const Cut c = cut_of(p.M, p.N, p.K, p.dt, p.pairs, p.gated);
-    const int64_t workgroups = c.tiles_m * c.tiles_n * c.splits;
-    if (workgroups > 0x7ffffff0) return RCD_ERR_UNSUPPORTED;
     const bool mx = p.dt == RCD_MXFP8;
     tile::Args x{};
     auto side = [](const Laid &l, const Laid &second, int64_t rows, int kind) {
@@ -349,23 +382,64 @@ int launch_product(const Product &p, Pieces &room, hipStream_t stream)
     x.tiles_m = (int)c.tiles_m;
     x.tiles_n = (int)c.tiles_n;
     x.splits = c.splits;
-    int to = p.gated ? tile::TO_GATED : tile::TO_LINEAR;
-    if (c.splits > 1) {
-        to = p.gated ? tile::TO_GATED_PARTS : tile::TO_PARTS;
-        x.parts_pitch = parts_pitch(p.N, p.gated);
-        x.parts_half = (int)(x.parts_pitch / 2);
-        x.parts = room.take<float>((size_t)c.splits * p.M * x.parts_pitch);
-    }
+    take_parts(x, p.gated, room);
+    return x;
+}
+
+int launch_planned(const Product &p, const Cut &c, const tile::Args &x, hipStream_t stream)
+{
+    const bool mx = p.dt == RCD_MXFP8;
+    const int to = c.splits > 1 ? (p.gated ? tile::TO_GATED_PARTS : tile::TO_PARTS) : p.gated ? tile::TO_GATED : tile::TO_LINEAR;
     ENC_TRY(with_tile_variant(c.wt, p.ka, p.kb, mx, to, [&](auto w, auto a, auto b, auto m, auto t) {
         constexpr int W = decltype(w)::value;
         constexpr bool X = decltype(m)::value;
-        hipLaunchKernelGGL((tile::k_tile<W, decltype(a)::value, decltype(b)::value, X, decltype(t)::value>),
-                           dim3((unsigned)((workgroups + 7) / 8 * 8)), dim3(tile::THREADS), (tile::Shape<W, X>::LDS_BYTES), stream, x);
+        hipLaunchKernelGGL((tile::k_tile<W, decltype(a)::value, decltype(b)::value, X, decltype(t)::value>), dim3(grid_of(c)),
+                           dim3(tile::THREADS), (tile::Shape<W, X>::LDS_BYTES), stream, x);
         return (int)RCD_OK;
     }));
     if (c.splits > 1) launch_join(x, p.gated, stream);
     ENC_HIP_TRY(hipGetLastError());
     return RCD_OK;
+}
+
+int launch_product(const Product &p, Pieces &room, hipStream_t stream)
+{
+    ENC_TRY(set_up());
+    const Cut c = cut_of(p.M, p.N, p.K, p.dt, p.pairs, p.gated);
+    if (!launchable(c)) return RCD_ERR_UNSUPPORTED;
+    return launch_planned(p, c, plan_product(p, c, room), stream);
+}
+
+enc_rules::Both both_of(int64_t M, int64_t N, int64_t K, int dt, int pairs)
+{
+    // dA: M x K over N (`pairs` of them), dW: pairs N x K over M
+    return enc_rules::both_of(M, K, stages_of(N, dt, pairs), pairs == 2 ? 2 * up64(N) : N, K, stages_of(M, dt, 1));
+}
+
+// A backward call's two products (either may be missing) and the bias's column sums.
+int launch_both(const Product *da, const Product *dw, const enc_rules::Both &cut, Pieces &room, const tile::Columns &cols,
+                hipStream_t stream)
+{
+    ENC_TRY(set_up());
+    if ((da && !launchable(cut.first)) || (dw && !launchable(cut.second))) return RCD_ERR_UNSUPPORTED;
+    if (da && dw && cut.together) {
+        const tile::Args x = plan_product(*da, cut.first, room), y = plan_product(*dw, cut.second, room);
+        const unsigned first = grid_of(cut.first);
+        hipLaunchKernelGGL(tile::k_tile_both, dim3(first + grid_of(cut.second)), dim3(tile::THREADS),
+                           (tile::Shape<64, false>::LDS_BYTES), stream, x, y, (int)first);
+        return launch_join_both(x, y, cols, stream);
+    }
+    if (cols.part) ENC_TRY(sum_columns(cols, stream));
+    const size_t mark = room.used;
+    if (da) ENC_TRY(launch_planned(*da, cut.first, plan_product(*da, cut.first, room), stream));
+    room.used = mark;
+    if (dw) ENC_TRY(launch_planned(*dw, cut.second, plan_product(*dw, cut.second, room), stream));
+    return RCD_OK;
+}
+size_t both_parts(const enc_rules::Both &b, int64_t M, int64_t N, int64_t M2, int64_t N2)
+{
+    const size_t first = parts_bytes(b.first, M, N, false), second = parts_bytes(b.second, M2, N2, false);
+    return b.together ? first + second : std::max(first, second);
 }
 
 // fp32 operands in place.
@@ -391,12 +465,9 @@ size_t direct_parts(int64_t M, int64_t N, int64_t K, int pairs, bool gated, int 
 // Rows of these pitches lie near enough for the direct kernel's 32-bit offsets inside a tile.
 inline bool near_enough(int64_t ld_a, int64_t ld_b = 0, int64_t ld_c = 0) { return std::max({ld_a, ld_b, ld_c}) <= ((int64_t)1 << 23); }
 
-int launch_direct(const DirectProduct &p, Pieces &room, hipStream_t stream)
+direct::Args plan_direct(const DirectProduct &p, const Cut &c, Pieces &room)
 {
     static_assert(enc_rules::DIRECT_STAGE == direct::KS, "the rule counts the kernel's stages");
-    const Cut c = direct_cut(p.M, p.N, p.K, p.pairs, p.gated);
-    const int64_t workgroups = c.tiles_m * c.tiles_n * c.splits;
-    if (workgroups > 0x7ffffff0) return RCD_ERR_UNSUPPORTED;
     direct::Args x{};
     for (int i = 0; i < 2; ++i) {
         x.a[i] = p.a[i];
@@ -414,12 +485,13 @@ int launch_direct(const DirectProduct &p, Pieces &room, hipStream_t stream)
     x.t.tiles_m = (int)c.tiles_m;
     x.t.tiles_n = (int)c.tiles_n;
     x.t.splits = c.splits;
-    if (c.splits > 1) {
-        x.t.parts_pitch = parts_pitch(p.N, p.gated);
-        x.t.parts_half = (int)(x.t.parts_pitch / 2);
-        x.t.parts = room.take<float>((size_t)c.splits * p.M * x.t.parts_pitch);
-    }
-    const dim3 grid((unsigned)((workgroups + 7) / 8 * 8));
+    take_parts(x.t, p.gated, room);
+    return x;
+}
+
+int launch_planned(const DirectProduct &p, const Cut &c, const direct::Args &x, hipStream_t stream)
+{
+    const dim3 grid(grid_of(c));
     constexpr int K = tile::K_RUNS, R = tile::ROWS_RUN;
     auto go = [&](auto kernel) { hipLaunchKernelGGL(kernel, grid, dim3(256), 0, stream, x); };
     if (p.gated) {
@@ -438,6 +510,46 @@ int launch_direct(const DirectProduct &p, Pieces &room, hipStream_t stream)
     if (c.splits > 1) launch_join(x.t, p.gated, stream);
     ENC_HIP_TRY(hipGetLastError());
     return RCD_OK;
+}
+
+int launch_direct(const DirectProduct &p, Pieces &room, hipStream_t stream)
+{
+    const Cut c = direct_cut(p.M, p.N, p.K, p.pairs, p.gated);
+    if (!launchable(c)) return RCD_ERR_UNSUPPORTED;
+    return launch_planned(p, c, plan_direct(p, c, room), stream);
+}
+
+// The direct kernel's two products of a backward call always run side by side, each cut for half of the device.
+enc_rules::Both direct_both(int64_t M, int64_t N, int64_t K, int pairs)
+{
+    using namespace enc_rules;
+    return Both{true, direct_cut_of(M, K, ceil_div(N, DIRECT_STAGE) * pairs, false, UNITS / 2),
+                direct_cut_of(pairs == 2 ? 2 * up64(N) : N, K, ceil_div(M, DIRECT_STAGE), false, UNITS / 2)};
+}
+
+int launch_both(const DirectProduct *da, const DirectProduct *dw, const enc_rules::Both &cut, Pieces &room, const tile::Columns &cols,
+                hipStream_t stream)
+{
+    if ((da && !launchable(cut.first)) || (dw && !launchable(cut.second))) return RCD_ERR_UNSUPPORTED;
+    if (da && dw) {
+        const direct::Args x = plan_direct(*da, cut.first, room), y = plan_direct(*dw, cut.second, room);
+        const unsigned first = grid_of(cut.first);
+        hipLaunchKernelGGL(direct::k_direct_both, dim3(first + grid_of(cut.second)), dim3(256), 0, stream, x, y, (int)first);
+        return launch_join_both(x.t, y.t, cols, stream);
+    }
+    if (cols.part) ENC_TRY(sum_columns(cols, stream));
+    if (da) ENC_TRY(launch_planned(*da, cut.first, plan_direct(*da, cut.first, room), stream));
+    if (dw) ENC_TRY(launch_planned(*dw, cut.second, plan_direct(*dw, cut.second, room), stream));
+    return RCD_OK;
+}
+
+// Parts of a backward call's two products, whichever way they go.
+size_t backward_parts(int64_t M, int64_t N, int64_t K, int dt, int pairs)
+{
+    const int64_t rows = pairs == 2 ? 2 * up64(N) : N;
+    size_t need = both_parts(both_of(M, N, K, dt, pairs), M, K, rows, K);
+    if (dt == RCD_F32) need = std::max(need, both_parts(direct_both(M, N, K, pairs), M, K, rows, K));
+    return need;
 }
 
 // Up to so many rows the weights are read once, straight into registers.
@@ -482,17 +594,6 @@ int zero_matrix(void *p, int dt, int64_t ld, int64_t rows, int64_t cols, hipStre
     const dim3 grid((unsigned)std::min<int64_t>(rows, 4096));
     if (dt == RCD_F32) hipLaunchKernelGGL(k_zero<float>, grid, dim3(256), 0, stream, (float *)p, (long long)ld, (int)rows, (int)cols);
     else hipLaunchKernelGGL(k_zero<__bf16>, grid, dim3(256), 0, stream, (__bf16 *)p, (long long)ld, (int)rows, (int)cols);
-    ENC_HIP_TRY(hipGetLastError());
-    return RCD_OK;
-}
-
-int sum_columns(const float *part, int64_t pitch, int64_t groups, int64_t d, void *out, int dt, hipStream_t stream)
-{
-    const dim3 grid((unsigned)((d + 15) / 16));
-    if (dt == RCD_F32)
-        hipLaunchKernelGGL(k_column_sums<float>, grid, dim3(1024), 0, stream, part, (long long)pitch, (int)groups, (int)d, (float *)out);
-    else
-        hipLaunchKernelGGL(k_column_sums<__bf16>, grid, dim3(1024), 0, stream, part, (long long)pitch, (int)groups, (int)d, (__bf16 *)out);
     ENC_HIP_TRY(hipGetLastError());
     return RCD_OK;
 }
@@ -675,7 +776,8 @@ int rcd_rms_norm_backward(const void *dY_dev, int dt, int64_t rows, int64_t d, i
         else hipLaunchKernelGGL((k_norm_backward<__bf16, W, C>), grid, dim3(NORM_THREADS), 0, stream, a);
     });
     ENC_HIP_TRY(hipGetLastError());
-    return dweight_dev ? sum_columns(a.part, a.part_pitch, groups, d, dweight_dev, dt, stream) : RCD_OK;
+    if (!dweight_dev) return RCD_OK;
+    return sum_columns(tile::Columns{a.part, dweight_dev, a.part_pitch, (int)groups, (int)d, dt == RCD_F32}, stream);
 }
 
 size_t rcd_linear_workspace_bytes(int64_t M, int64_t N, int64_t K, int dt)
@@ -742,10 +844,7 @@ size_t rcd_linear_backward_workspace_bytes(int64_t M, int64_t N, int64_t K, int 
     if (!product_sizes_ok(M, N, K) || !is_matrix_type(dt)) return 0;
     Pieces w(nullptr);
     linear_back(w, M, N, dt);
-    // (the two products run one after the other: the larger one's parts)
-    return w.used + packed_bytes(M, K, dt) + packed_bytes(N, K, dt) +
-           std::max({parts_bytes(cut_of(M, K, N, dt, 1, false), M, K, false), parts_bytes(cut_of(N, K, M, dt, 1, false), N, K, false),
-                     direct_parts(M, K, N, 1, false, dt), direct_parts(N, K, M, 1, false, dt)});
+    return w.used + packed_bytes(M, K, dt) + packed_bytes(N, K, dt) + backward_parts(M, N, K, dt, 1);
 }
 
 int rcd_linear_backward(const void *dY_dev, int64_t ld_dy, const void *A_dev, int64_t ld_a, const void *W_dev, int64_t ld_w,
@@ -768,7 +867,7 @@ int rcd_linear_backward(const void *dY_dev, int64_t ld_dy, const void *A_dev, in
     Pieces room(workspace_dev);
     const LinearBack w = linear_back(room, M, N, dt);
     Packer pack{dt};
-    const bool in_place = f32 && enc_rules::direct_backward(M, N, K, false) && near_enough(ld_dy);     // (no pieces)
+    const bool in_place = f32 && enc_rules::direct_backward(M, N, K, false) && near_enough(ld_dy, up64(N));     // (no pieces)
     // dz itself, in place, where there is no activation and its rows can be read as they are
     Laid dz;
     Laid a, b;
@@ -788,6 +887,7 @@ int rcd_linear_backward(const void *dY_dev, int64_t ld_dy, const void *A_dev, in
         dz.plane = M * pitch * 2;
         dz.cols = pitch;
     }
+    tile::Columns cols{};
     if (!as_it_is || dbias_dev) {
         const SlopeCut c = slope_cut(M, pitch);
         SlopeArgs x{};
@@ -805,60 +905,44 @@ int rcd_linear_backward(const void *dY_dev, int64_t ld_dy, const void *A_dev, in
             else hipLaunchKernelGGL((k_slope<__bf16, 1, A>), grid, dim3(256), 0, stream, x);
         });
         ENC_HIP_TRY(hipGetLastError());
-        if (dbias_dev) ENC_TRY(sum_columns(w.part, x.part_pitch, c.groups, N, dbias_dev, dt, stream));
+        if (dbias_dev) cols = tile::Columns{w.part, dbias_dev, x.part_pitch, (int)c.groups, (int)N, f32};
     }
-    const size_t mark = room.used;
     if (in_place) {
-        DirectProduct p{};
-        p.pairs = 1;
-        p.a[0] = as_it_is ? (const float *)dY_dev : (const float *)w.dz;
-        p.a_pitch = as_it_is ? ld_dy : pitch;
-        if (dA_dev) {
-            p.M = M; p.N = K; p.K = N;
-            p.ka = tile::K_RUNS;
-            p.kb = tile::ROWS_RUN;
-            p.b[0] = (const float *)W_dev;
-            p.b_pitch[0] = ld_w;
-            p.a_extent = M;
-            p.b_extent = K;
-            p.e = one_output(dA_dev, ld_da, dt, RCD_ACT_NONE);
-            ENC_TRY(launch_direct(p, room, stream));
-        }
-        room.used = mark;
-        if (dW_dev) {
-            p.M = N; p.N = K; p.K = M;
-            p.ka = p.kb = tile::ROWS_RUN;
-            p.b[0] = (const float *)A_dev;
-            p.b_pitch[0] = ld_a;
-            p.a_extent = N;
-            p.b_extent = K;
-            p.e = one_output(dW_dev, ld_dw, dt, RCD_ACT_NONE);
-            ENC_TRY(launch_direct(p, room, stream));
-        }
-        return RCD_OK;
-    }
-    Product p{};
-    p.dt = dt;
-    p.pairs = 1;
-    if (dA_dev) {
+        DirectProduct p{}, q{};
+        p.pairs = q.pairs = 1;
+        p.a[0] = q.a[0] = as_it_is ? (const float *)dY_dev : (const float *)w.dz;
+        p.a_pitch = q.a_pitch = as_it_is ? ld_dy : pitch;
         p.M = M; p.N = K; p.K = N;
         p.ka = tile::K_RUNS;
         p.kb = tile::ROWS_RUN;
-        p.a[0] = dz;
-        p.b[0] = b;
+        p.b[0] = (const float *)W_dev;
+        p.b_pitch[0] = ld_w;
+        p.a_extent = M;
+        p.b_extent = K;
         p.e = one_output(dA_dev, ld_da, dt, RCD_ACT_NONE);
-        ENC_TRY(launch_product(p, room, stream));
+        q.M = N; q.N = K; q.K = M;
+        q.ka = q.kb = tile::ROWS_RUN;
+        q.b[0] = (const float *)A_dev;
+        q.b_pitch[0] = ld_a;
+        q.a_extent = N;
+        q.b_extent = K;
+        q.e = one_output(dW_dev, ld_dw, dt, RCD_ACT_NONE);
+        return launch_both(dA_dev ? &p : nullptr, dW_dev ? &q : nullptr, direct_both(M, N, K, 1), room, cols, stream);
     }
-    room.used = mark;
-    if (dW_dev) {
-        p.M = N; p.N = K; p.K = M;
-        p.ka = p.kb = tile::ROWS_RUN;
-        p.a[0] = dz;
-        p.b[0] = a;
-        p.e = one_output(dW_dev, ld_dw, dt, RCD_ACT_NONE);
-        ENC_TRY(launch_product(p, room, stream));
-    }
-    return RCD_OK;
+    Product p{}, q{};
+    p.dt = q.dt = dt;
+    p.pairs = q.pairs = 1;
+    p.a[0] = q.a[0] = dz;
+    p.M = M; p.N = K; p.K = N;
+    p.ka = tile::K_RUNS;
+    p.kb = tile::ROWS_RUN;
+    p.b[0] = b;
+    p.e = one_output(dA_dev, ld_da, dt, RCD_ACT_NONE);
+    q.M = N; q.N = K; q.K = M;
+    q.ka = q.kb = tile::ROWS_RUN;
+    q.b[0] = a;
+    q.e = one_output(dW_dev, ld_dw, dt, RCD_ACT_NONE);
+    return launch_both(dA_dev ? &p : nullptr, dW_dev ? &q : nullptr, both_of(M, N, K, dt, 1), room, cols, stream);
 }
 
 size_t rcd_gated_linear_workspace_bytes(int64_t M, int64_t F, int64_t K, int dt)
@@ -929,9 +1013,7 @@ size_t rcd_gated_linear_backward_workspace_bytes(int64_t M, int64_t F, int64_t K
     Pieces w(nullptr);
     w.take<__bf16>((size_t)M * 2 * up64(F) * (dt == RCD_F32 ? 3 : 1));
     return w.used + packed_bytes(M, K, dt) + 2 * packed_bytes(F, K, dt) +
-           std::max({parts_bytes(cut_of(M, K, F, dt, 2, false), M, K, false),
-                     parts_bytes(cut_of(2 * up64(F), K, M, dt, 1, false), 2 * up64(F), K, false), direct_parts(M, K, F, 2, false, dt),
-                     direct_parts(2 * up64(F), K, M, 1, false, dt)});
+           backward_parts(M, F, K, dt, 2);
 }
 
 int rcd_gated_linear_backward(const void *dH_dev, int64_t ld_dh, const void *A_dev, int64_t ld_a,
@@ -956,7 +1038,7 @@ int rcd_gated_linear_backward(const void *dH_dev, int64_t ld_dh, const void *A_d
     const int64_t half = up64(F), pitch = 2 * half;
     Pieces room(workspace_dev);
     __bf16 *dgu = room.take<__bf16>((size_t)M * pitch * (f32 ? 3 : 1));
-    const bool in_place = f32 && enc_rules::direct_backward(M, F, K, true);      // (no pieces)
+    const bool in_place = f32 && enc_rules::direct_backward(M, F, K, true) && near_enough(2 * up64(F));      // (no pieces)
     Packer pack{dt};
     Product p{};
     p.dt = dt;
@@ -985,38 +1067,30 @@ int rcd_gated_linear_backward(const void *dH_dev, int64_t ld_dh, const void *A_d
     both.split_row = (int)half;
     both.rows_each = (int)F;
     if (in_place) {
-        DirectProduct q{};
-        const size_t mark = room.used;
-        q.a[0] = (const float *)dgu;
-        q.a[1] = q.a[0] + half;
-        q.a_pitch = pitch;
-        if (dA_dev) {
-            q.M = M; q.N = K; q.K = F;
-            q.ka = tile::K_RUNS;
-            q.kb = tile::ROWS_RUN;
-            q.pairs = 2;
-            q.b[0] = (const float *)Wg_dev;
-            q.b[1] = (const float *)Wu_dev;
-            q.b_pitch[0] = ld_wg;
-            q.b_pitch[1] = ld_wu;
-            q.a_extent = M;
-            q.b_extent = K;
-            q.e = one_output(dA_dev, ld_da, dt, RCD_ACT_NONE);
-            ENC_TRY(launch_direct(q, room, stream));
-        }
-        room.used = mark;
-        if (dWg_dev) {
-            q.M = pitch; q.N = K; q.K = M;
-            q.ka = q.kb = tile::ROWS_RUN;
-            q.pairs = 1;
-            q.b[0] = (const float *)A_dev;
-            q.b_pitch[0] = ld_a;
-            q.a_extent = pitch;
-            q.b_extent = K;
-            q.e = both;
-            ENC_TRY(launch_direct(q, room, stream));
-        }
-        return RCD_OK;
+        DirectProduct p{}, q{};
+        p.a[0] = q.a[0] = (const float *)dgu;
+        p.a[1] = p.a[0] + half;
+        p.a_pitch = q.a_pitch = pitch;
+        p.M = M; p.N = K; p.K = F;
+        p.ka = tile::K_RUNS;
+        p.kb = tile::ROWS_RUN;
+        p.pairs = 2;
+        p.b[0] = (const float *)Wg_dev;
+        p.b[1] = (const float *)Wu_dev;
+        p.b_pitch[0] = ld_wg;
+        p.b_pitch[1] = ld_wu;
+        p.a_extent = M;
+        p.b_extent = K;
+        p.e = one_output(dA_dev, ld_da, dt, RCD_ACT_NONE);
+        q.M = pitch; q.N = K; q.K = M;
+        q.ka = q.kb = tile::ROWS_RUN;
+        q.pairs = 1;
+        q.b[0] = (const float *)A_dev;
+        q.b_pitch[0] = ld_a;
+        q.a_extent = pitch;
+        q.b_extent = K;
+        q.e = both;
+        return launch_both(dA_dev ? &p : nullptr, dWg_dev ? &q : nullptr, direct_both(M, F, K, 2), room, tile::Columns{}, stream);
     }
     Laid d;
     d.p = (const unsigned char *)dgu;
@@ -1024,26 +1098,21 @@ int rcd_gated_linear_backward(const void *dH_dev, int64_t ld_dh, const void *A_d
     d.plane = M * pitch * 2;
     d.cols = pitch;
     p.a[0] = d;
-    const size_t mark = room.used;
-    if (dA_dev) {
-        p.M = M; p.N = K; p.K = F;
-        p.ka = tile::K_RUNS;
-        p.kb = tile::ROWS_RUN;
-        p.pairs = 2;
-        p.a_shift = half * 2;
-        p.e = one_output(dA_dev, ld_da, dt, RCD_ACT_NONE);
-        ENC_TRY(launch_product(p, room, stream));
-    }
-    room.used = mark;
-    if (dWg_dev) {
-        p.M = pitch; p.N = K; p.K = M;
-        p.ka = p.kb = tile::ROWS_RUN;
-        p.pairs = 1;
-        p.b[0] = a;
-        p.e = both;
-        ENC_TRY(launch_product(p, room, stream));
-    }
-    return RCD_OK;
+    p.M = M; p.N = K; p.K = F;
+    p.ka = tile::K_RUNS;
+    p.kb = tile::ROWS_RUN;
+    p.pairs = 2;
+    p.a_shift = half * 2;
+    p.e = one_output(dA_dev, ld_da, dt, RCD_ACT_NONE);
+    Product q{};
+    q.dt = dt;
+    q.a[0] = d;
+    q.M = pitch; q.N = K; q.K = M;
+    q.ka = q.kb = tile::ROWS_RUN;
+    q.pairs = 1;
+    q.b[0] = a;
+    q.e = both;
+    return launch_both(dA_dev ? &p : nullptr, dWg_dev ? &q : nullptr, both_of(M, F, K, dt, 2), room, tile::Columns{}, stream);
 }
 
 } // extern "C"

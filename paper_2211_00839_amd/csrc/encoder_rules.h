@@ -24,25 +24,25 @@ inline int64_t ceil_div(int64_t a, int64_t b) { return (a + b - 1) / b; }
 // Measured / by this rule: 16384 x 2048 x 2048 large tiles 115 / 108, small 132 / 129; the weights' gradient of it large in 4
 // parts 121 / 125, in 1 278 / 294, small in 2 132 / 131; 1000 x 2048 x 8192 small in 4 43 / 41, in 1 69 / 75; 256 x 2048 x
 // 2048 small in 3 15 / 15, large in 1 40 / 42.
-inline double time_of(const Cut &c, int64_t M, int64_t N, int64_t stages, bool gated)
+inline double time_of(const Cut &c, int64_t M, int64_t N, int64_t stages, bool gated, int64_t units = UNITS)
 {
     const int64_t workgroups = c.tiles_m * c.tiles_n * c.splits, deep = ceil_div(stages, c.splits);
     double t;
     if (c.wt == 128) {
-        const int64_t rounds = ceil_div(workgroups, UNITS);
-        t = (double)rounds * ((double)deep * (1.0 + 0.5 * std::min(1.0, (double)workgroups / UNITS)) + 6.0);
+        const int64_t rounds = ceil_div(workgroups, units);
+        t = (double)rounds * ((double)deep * (1.0 + 0.5 * std::min(1.0, (double)workgroups / (double)units)) + 6.0);
     } else {
-        const int64_t full = workgroups / (2 * UNITS), rest = workgroups % (2 * UNITS);
+        const int64_t full = workgroups / (2 * units), rest = workgroups % (2 * units);
         t = (double)full * ((double)deep * 0.88 + 4.0);
-        if (rest) t += (double)deep * (rest > UNITS ? 0.88 : 0.55) + 4.0;
+        if (rest) t += (double)deep * (rest > units ? 0.88 : 0.55) + 4.0;
     }
     if (c.splits > 1) t += 3.5 + 0.25 * c.splits + 2e-6 / 7 * (double)c.splits * (double)M * (double)N * 4 * (gated ? 2 : 1);
     return t;
 }
 
 // M x N: the result (gated: N columns of each of two products); stages: of k, 64 bf16 or 128 8-bit elements each, three
-// pieces of fp32 make six products.
-inline Cut cut_of(int64_t M, int64_t N, int64_t stages, bool gated)
+// pieces of fp32 make six products.  units: what of the device it has to itself.
+inline Cut cut_of(int64_t M, int64_t N, int64_t stages, bool gated, int64_t units = UNITS)
 {
     Cut best{};
     double least = 0.0;
@@ -53,9 +53,9 @@ inline Cut cut_of(int64_t M, int64_t N, int64_t stages, bool gated)
         c.tiles_n = ceil_div(N, gated ? wt : 2 * wt);
         for (int splits : {1, 2, 3, 4, 5, 6, 8, 10, 12, 16}) {
             // (a part of fewer than four stages is all start and end)
-            if (splits > 1 && (splits * 4 > stages || c.tiles_m * c.tiles_n * splits > 2 * UNITS)) break;
+            if (splits > 1 && (splits * 4 > stages || c.tiles_m * c.tiles_n * splits > 2 * units)) break;
             c.splits = splits;
-            const double t = time_of(c, M, N, stages, gated);
+            const double t = time_of(c, M, N, stages, gated, units);
             if (best.splits == 0 || t < least) {
                 best = c;
                 least = t;
@@ -65,18 +65,34 @@ inline Cut cut_of(int64_t M, int64_t N, int64_t stages, bool gated)
     return best;
 }
 
+inline int64_t workgroups_of(const Cut &c) { return c.tiles_m * c.tiles_n * c.splits; }
+
+// A backward call's two products, side by side in one launch where each is small enough to leave room for the other: both in
+// small tiles, all workgroups on the device at once.  2500 x 512 x 1365 in fp32, gated, one after the other / side by side: 194 / 163 us
+// the whole training step.
+struct Both {
+    bool together;
+    Cut first, second;
+};
+inline Both both_of(int64_t M1, int64_t N1, int64_t stages1, int64_t M2, int64_t N2, int64_t stages2)
+{
+    Both b{true, cut_of(M1, N1, stages1, false, UNITS / 2), cut_of(M2, N2, stages2, false, UNITS / 2)};
+    if (b.first.wt == 64 && b.second.wt == 64 && workgroups_of(b.first) + workgroups_of(b.second) <= 2 * UNITS) return b;
+    return Both{false, cut_of(M1, N1, stages1, false), cut_of(M2, N2, stages2, false)};
+}
+
 // fp32 products go to the fp32 matrix instruction directly (wt 32: tiles of 64 x 64, k in stages of 32) where that takes less
 // than pieces do, whose launch and trip through memory come on top (4.5 us and 10 bytes per element at 5 TB/s).
 constexpr int DIRECT_STAGE = 32;
-inline double direct_time_of(const Cut &c, int64_t M, int64_t N, int64_t stages, bool gated)
+inline double direct_time_of(const Cut &c, int64_t M, int64_t N, int64_t stages, bool gated, int64_t units = UNITS)
 {
     const int64_t workgroups = c.tiles_m * c.tiles_n * c.splits, deep = ceil_div(stages, c.splits);
     // a stage takes 0.55 us (gated: of two products) however many workgroups share a unit, up to four
-    double t = 4.0 + (double)ceil_div(workgroups, UNITS) * (double)deep * (gated ? 1.0 : 0.55);
+    double t = 4.0 + (double)ceil_div(workgroups, units) * (double)deep * (gated ? 1.0 : 0.55);
     if (c.splits > 1) t += 3.5 + 0.25 * c.splits + 2e-6 / 7 * (double)c.splits * (double)M * (double)N * 4 * (gated ? 2 : 1);
     return t;
 }
-inline Cut direct_cut_of(int64_t M, int64_t N, int64_t stages, bool gated)
+inline Cut direct_cut_of(int64_t M, int64_t N, int64_t stages, bool gated, int64_t units = UNITS)
 {
     Cut best{};
     double least = 0.0;
@@ -85,9 +101,9 @@ inline Cut direct_cut_of(int64_t M, int64_t N, int64_t stages, bool gated)
     c.tiles_m = ceil_div(M, 64);
     c.tiles_n = ceil_div(N, 64);
     for (int splits : {1, 2, 3, 4, 5, 6, 8, 10, 12, 16}) {
-        if (splits > 1 && (splits * 2 > stages || c.tiles_m * c.tiles_n * splits > 2 * UNITS)) break;
+        if (splits > 1 && (splits * 2 > stages || c.tiles_m * c.tiles_n * splits > 2 * units)) break;
         c.splits = splits;
-        const double t = direct_time_of(c, M, N, stages, gated);
+        const double t = direct_time_of(c, M, N, stages, gated, units);
         if (best.splits == 0 || t < least) {
             best = c;
             least = t;

@@ -5,6 +5,7 @@
 //
 // All of it is a handful of operations per element: bandwidth bounds it, so a row is read once and stays in registers
 // between its statistics and its outputs, eight elements (16 bytes of bf16) to a thread and access.
+#pragma once
 #include "encoder_math.h"
 
 namespace enc {
@@ -257,27 +258,35 @@ k_norm_backward(const NormBackArgs a)
     }
 }
 
-// out[c] = sum over the first `groups` rows of part, in a fixed order: 16 columns to a workgroup of 1024 threads, 64 rows
-// side by side.  grid = ceil(d / 16).
+// out[c] = sum over the first `groups` rows of part, in a fixed order: 16 columns to a workgroup of 16 DOWN threads, DOWN
+// rows side by side.
+template <typename T, int DOWN>
+__device__ __forceinline__ void column_sums(const float *__restrict__ part, long long pitch, int groups, int d, T *__restrict__ out,
+                                            int block, float (&sums)[DOWN][17])
+{
+    const int c = threadIdx.x & 15, r = threadIdx.x >> 4;
+    const int col = block * 16 + c;
+    float s = 0.f;
+    if (col < d) {
+#pragma unroll 4
+        for (int g = r; g < groups; g += DOWN) s += part[(size_t)g * pitch + col];
+    }
+    sums[r][c] = s;
+    __syncthreads();
+    for (int half = DOWN / 2; half >= 1; half >>= 1) {
+        if (r < half) sums[r][c] += sums[r + half][c];
+        __syncthreads();
+    }
+    if (r == 0 && col < d) out[col] = (T)sums[0][c];
+}
+
+// grid = ceil(d / 16)
 template <typename T>
 __global__ void __launch_bounds__(1024)
 k_column_sums(const float *__restrict__ part, long long pitch, int groups, int d, T *__restrict__ out)
 {
     __shared__ float sums[64][17];
-    const int c = threadIdx.x & 15, r = threadIdx.x >> 4;
-    const int col = blockIdx.x * 16 + c;
-    float s = 0.f;
-    if (col < d) {
-#pragma unroll 4
-        for (int g = r; g < groups; g += 64) s += part[(size_t)g * pitch + col];
-    }
-    sums[r][c] = s;
-    __syncthreads();
-    for (int half = 32; half >= 1; half >>= 1) {
-        if (r < half) sums[r][c] += sums[r + half][c];
-        __syncthreads();
-    }
-    if (r == 0 && col < d) out[col] = (T)sums[0][c];
+    column_sums<T, 64>(part, pitch, groups, d, out, (int)blockIdx.x, sums);
 }
 
 } // namespace enc

@@ -5,7 +5,7 @@
 // on the matrix cores, for operands whose k is contiguous (the forward products) or whose rows are (the gradients: no matrix
 // is ever transposed in memory), in bf16, in fp32 as three bf16 pieces, or in 8 bits with block scales.
 #pragma once
-#include "encoder_math.h"
+#include "norm_kernels.hip"
 
 namespace enc {
 
@@ -872,16 +872,16 @@ template <int WT, bool GATED> struct Band {
     }
 };
 
+// Workgroup `wg` of the `nwg` that share one product.
 template <int WT, int KA, int KB, bool MX, int TO>
-__global__ void __launch_bounds__(THREADS, WT == 128 ? 1 : 2)
-k_tile(const Args x)
+__device__ __forceinline__ void tile_body(const Args &x, int wg, int nwg)
 {
     constexpr bool GATED = TO == TO_GATED || TO == TO_GATED_PARTS;
     using P = Pipe<WT, KA, KB, MX, GATED>;
     using S = typename P::S;
     extern __shared__ __attribute__((aligned(16))) unsigned char lds[];
     int ti, tj, split;
-    if (!tile_of_workgroup((int)blockIdx.x, (int)gridDim.x, x.tiles_m, x.tiles_n, x.splits, &ti, &tj, &split)) return;
+    if (!tile_of_workgroup(wg, nwg, x.tiles_m, x.tiles_n, x.splits, &ti, &tj, &split)) return;
     constexpr int COLS = GATED ? WT : 2 * WT;      // output columns of a tile
     const int m0 = ti * S::T, n0 = tj * COLS;
     const int all = x.seg.count * x.seg.stages;
@@ -932,10 +932,29 @@ k_tile(const Args x)
     }
 }
 
+template <int WT, int KA, int KB, bool MX, int TO>
+__global__ void __launch_bounds__(THREADS, WT == 128 ? 1 : 2)
+k_tile(const Args x)
+{
+    tile_body<WT, KA, KB, MX, TO>(x, (int)blockIdx.x, (int)gridDim.x);
+}
+
+// A backward call's two products side by side: x's workgroups are the first `first` (a multiple of 8) of the launch.
+__global__ void __launch_bounds__(THREADS, 2)
+k_tile_both(const Args x, const Args y, int first)
+{
+    const int wg = (int)blockIdx.x;
+    if (wg < first) {
+        if (x.splits > 1) tile_body<64, K_RUNS, ROWS_RUN, false, TO_PARTS>(x, wg, first);
+        else tile_body<64, K_RUNS, ROWS_RUN, false, TO_LINEAR>(x, wg, first);
+    } else {
+        if (y.splits > 1) tile_body<64, ROWS_RUN, ROWS_RUN, false, TO_PARTS>(y, wg - first, (int)gridDim.x - first);
+        else tile_body<64, ROWS_RUN, ROWS_RUN, false, TO_LINEAR>(y, wg - first, (int)gridDim.x - first);
+    }
+}
+
 // The parts of a product whose k was split among workgroups, in order, and what becomes of their sum.
-template <bool GATED>
-__global__ void __launch_bounds__(256)
-k_join(const Args x)
+template <bool GATED> __device__ __forceinline__ void join(const Args &x)
 {
     const int groups = (x.N + 7) / 8;
     const long long all = (long long)x.M * groups, stride = (long long)x.M * x.parts_pitch;
@@ -962,6 +981,38 @@ k_join(const Args x)
         }
         if constexpr (GATED) finish_gated8(x.e, m, n, count, z, u);
         else finish_linear8(x.e, m, n, count, z);
+    }
+}
+
+template <bool GATED>
+__global__ void __launch_bounds__(256)
+k_join(const Args x)
+{
+    join<GATED>(x);
+}
+
+// What a backward call's two products leave to be joined, and the bias's column sums.  grid.y = 3.
+struct Columns {
+    const float *part;              // null: none
+    void *out;
+    long long pitch;
+    int groups, d;
+    bool f32;
+};
+__global__ void __launch_bounds__(256)
+k_join_both(const Args x, const Args y, const Columns c)
+{
+    __shared__ float sums[16][17];
+    if (blockIdx.y == 0) {
+        if (x.splits > 1) join<false>(x);
+    } else if (blockIdx.y == 1) {
+        if (y.splits > 1) join<false>(y);
+    } else if (c.part) {
+        for (int b = (int)blockIdx.x; b < (c.d + 15) / 16; b += (int)gridDim.x) {
+            if (c.f32) column_sums<float, 16>(c.part, c.pitch, c.groups, c.d, (float *)c.out, b, sums);
+            else column_sums<__bf16, 16>(c.part, c.pitch, c.groups, c.d, (__bf16 *)c.out, b, sums);
+            __syncthreads();
+        }
     }
 }
 
