@@ -1,4 +1,5 @@
-"""Builds librcd.so (the HIP library behind the C ABI of include/rcd.h) for gfx950.
+"""Builds librcd.so (the HIP library behind the C ABI of include/rcd.h) for gfx950, and _encoder.so (the argument
+marshalling of encoder.py, which calls it).
 
 Run as ``python -m paper_2211_00839_amd.build``; hipcc cross-compiles without a GPU.
 """
@@ -7,10 +8,12 @@ from __future__ import annotations
 import os
 import subprocess
 import sys
+import sysconfig
 
 HERE = os.path.dirname(os.path.abspath(__file__))
 CSRC = os.path.join(HERE, "csrc")
 LIB = os.path.join(HERE, "librcd.so")
+MARSHAL = os.path.join(HERE, "_encoder.so")
 
 HIPCC_FLAGS = [
     "-O3", "-std=c++17", "--offload-arch=gfx950", "-fPIC",
@@ -40,25 +43,42 @@ def build(verbose: bool = False) -> str:
                 print(" ".join(cmd), flush=True)
             jobs.append(subprocess.Popen(cmd, stdout=subprocess.PIPE, stderr=subprocess.STDOUT, text=True))
         said = [job.communicate()[0] for job in jobs]
-        failed = any(job.returncode != 0 for job in jobs)
-        if not failed:
-            cmd = [hipcc, "--offload-arch=gfx950", "-shared", "-fPIC"] + objects + ["-o", tmp]
-            if verbose:
-                print(" ".join(cmd), flush=True)
-            res = subprocess.run(cmd, stdout=subprocess.PIPE, stderr=subprocess.STDOUT, text=True)
-            said.append(res.stdout)
-            failed = res.returncode != 0
-        out = "\n".join(l for l in "".join(said).splitlines() if "packed-fp32-ops" not in l)
-        if failed:
-            raise RuntimeError("hipcc failed:\n" + out)
-        if verbose and out.strip():
-            print(out)
+        _complain(any(job.returncode != 0 for job in jobs), said, verbose)
+        _run([hipcc, "--offload-arch=gfx950", "-shared", "-fPIC"] + objects + ["-o", tmp], verbose)
         os.replace(tmp, LIB)
+        _run(_marshal_command(MARSHAL + suffix), verbose)
+        os.replace(MARSHAL + suffix, MARSHAL)
     finally:
-        for path in objects + [tmp]:
+        for path in objects + [tmp, MARSHAL + suffix]:
             if os.path.exists(path):
                 os.remove(path)
     return LIB
+
+
+def _complain(failed, said, verbose):
+    out = "\n".join(l for l in "".join(said).splitlines() if "packed-fp32-ops" not in l)
+    if failed:
+        raise RuntimeError("the compiler failed:\n" + out)
+    if verbose and out.strip():
+        print(out)
+
+
+def _run(cmd, verbose):
+    if verbose:
+        print(" ".join(cmd), flush=True)
+    res = subprocess.run(cmd, stdout=subprocess.PIPE, stderr=subprocess.STDOUT, text=True)
+    _complain(res.returncode != 0, [res.stdout], verbose)
+
+
+def _marshal_command(out):
+    """Host code alone, against torch's headers and the library just built."""
+    import torch
+
+    root = os.path.dirname(os.path.abspath(torch.__file__))
+    return [os.environ.get("CXX", "g++"), "-O2", "-std=c++17", "-fPIC", "-shared", "-w", "-I", os.path.join(root, "include"),
+            "-I", os.path.join(root, "include", "torch", "csrc", "api", "include"), "-I", sysconfig.get_path("include"),
+            os.path.join(CSRC, "encoder_marshal.cpp"), "-o", out, "-L", os.path.join(root, "lib"), "-ltorch_python", "-ltorch_cpu",
+            "-ltorch", "-lc10", "-L", HERE, "-lrcd", "-Wl,-rpath,$ORIGIN"]
 
 
 if __name__ == "__main__":
