@@ -580,7 +580,8 @@ int launch_few(int dt, bool gated, const few::Args &x, hipStream_t stream)
             }
         };
         using std::integral_constant;
-        if (x.M <= 16) go(integral_constant<int, 1>{}, integral_constant<int, 8>{});
+        if (x.M <= 16 && grid.x < 256) go(integral_constant<int, 1>{}, integral_constant<int, 16>{});
+        else if (x.M <= 16) go(integral_constant<int, 1>{}, integral_constant<int, 8>{});
         else if (x.M <= 32) go(integral_constant<int, 2>{}, integral_constant<int, 4>{});
         else go(integral_constant<int, 4>{}, integral_constant<int, 4>{});
     }

@@ -67,6 +67,11 @@ k_few(const Args x)
     for (int g = 0; g < G; ++g)
 #pragma unroll
         for (int t = 0; t < MT; ++t) acc[g][t] = f32x4{0.f, 0.f, 0.f, 0.f};
+    // what the epilogue needs from memory is asked for ahead of the sums: eight columns of a row to a thread
+    static_assert(2 * 16 * MT <= 64 * WAVES, "a thread for every eight columns");
+    const int em = threadIdx.x >> 1, ecol = n0 + (threadIdx.x & 1) * 8, ecount = em < x.M ? x.N - ecol : 0;
+    float bias[8], residual[8];
+    if constexpr (!GATED) ahead8(x.e, em, ecol, ecount, bias, residual);
     const int blocks = (x.K + MX_BLOCK - 1) / MX_BLOCK;
 #pragma unroll 4
     for (int c = wave; c < chunks; c += WAVES) {
@@ -129,22 +134,20 @@ k_few(const Args x)
 #pragma unroll
             for (int i = 0; i < 4; ++i) sums[wave][g][t * 16 + (lane & 15)][q * 4 + i] = acc[g][t][i];
     __syncthreads();
-    for (int o = threadIdx.x; o < 2 * x.M; o += 64 * WAVES) {
-        const int m = o >> 1, c8 = (o & 1) * 8, col = n0 + c8, count = x.N - col;
-        if (count <= 0) continue;
-        float z[G][8];
+    if (ecount <= 0) return;
+    float z[G][8];
 #pragma unroll
-        for (int g = 0; g < G; ++g)
+    for (int g = 0; g < G; ++g)
 #pragma unroll
-            for (int i = 0; i < 8; ++i) {
-                float s = sums[0][g][m][c8 + i];
+        for (int i = 0; i < 8; ++i) {
+            const int c = (threadIdx.x & 1) * 8 + i;
+            float s = sums[0][g][em][c];
 #pragma unroll
-                for (int w = 1; w < WAVES; ++w) s += sums[w][g][m][c8 + i];
-                z[g][i] = s;
-            }
-        if constexpr (GATED) finish_gated8(x.e, m, col, count, z[0], z[1]);
-        else finish_linear8(x.e, m, col, count, z[0]);
-    }
+            for (int w = 1; w < WAVES; ++w) s += sums[w][g][em][c];
+            z[g][i] = s;
+        }
+    if constexpr (GATED) finish_gated8(x.e, em, ecol, ecount, z[0], z[1]);
+    else finish_ahead8(x.e, em, ecol, ecount, z[0], bias, residual);
 }
 
 // fp32: 8 columns to a workgroup, MR rows, plain multiply-adds (fp32 matrix instructions have no more).  Each of four waves

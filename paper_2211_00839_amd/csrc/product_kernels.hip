@@ -58,6 +58,42 @@ __device__ __forceinline__ void finish_linear8(const Epilogue &e, int m, int n, 
     else finish_linear8_as(e, (__bf16 *)out, row, m, n, count, z);
 }
 
+// The same in two halves: what is read, and what is made of it (one output, no second one).
+__device__ __forceinline__ void ahead8(const Epilogue &e, int m, int n, int count, float (&bias)[8], float (&residual)[8])
+{
+#pragma unroll
+    for (int i = 0; i < 8; ++i) bias[i] = residual[i] = 0.f;
+    if (count <= 0) return;
+    if (e.bias) {
+        if (e.out_f32) load8((const float *)e.bias + n, count, bias);
+        else load8((const __bf16 *)e.bias + n, count, bias);
+    }
+    if (e.residual) {
+        if (e.out_f32) load8((const float *)e.residual + m * e.ld_r + n, count, residual);
+        else load8((const __bf16 *)e.residual + m * e.ld_r + n, count, residual);
+    }
+}
+__device__ __forceinline__ void finish_ahead8(const Epilogue &e, int m, int n, int count, float (&z)[8], const float (&bias)[8],
+                                              const float (&residual)[8])
+{
+    if (e.bias) {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) z[i] += bias[i];
+    }
+    if (e.preact) store8(e.preact + m * e.ld_p + n, count, z);
+    if (e.act != 0) {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) z[i] = activate(z[i], e.act);
+    }
+    if (e.residual) {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) z[i] += residual[i];
+    }
+    const long long at = (long long)m * e.ld_o + n;
+    if (e.out_f32) store8((float *)e.out + at, count, z);
+    else store8((__bf16 *)e.out + at, count, z);
+}
+
 __device__ __forceinline__ void finish_gated8(const Epilogue &e, int m, int f, int count, const float (&g)[8], const float (&u)[8])
 {
     if (e.preact) {
