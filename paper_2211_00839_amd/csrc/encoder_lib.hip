@@ -552,8 +552,8 @@ size_t backward_parts(int64_t M, int64_t N, int64_t K, int dt, int pairs)
     return need;
 }
 
-// Up to so many rows the weights are read once, straight into registers.
-inline int64_t few_rows(int dt) { return dt == RCD_F32 ? 32 : 64; }
+
+inline bool few_rows(int64_t M, int64_t N, int64_t K, int dt) { return enc_rules::few_rows(M, N, K, dt == RCD_F32, dt == RCD_MXFP8); }
 
 int launch_few(int dt, bool gated, const few::Args &x, hipStream_t stream)
 {
@@ -566,7 +566,8 @@ int launch_few(int dt, bool gated, const few::Args &x, hipStream_t stream)
             else hipLaunchKernelGGL((few::k_few_f32<MR, false>), grid, dim3(256), 0, stream, x);
         };
         if (x.M == 1) go(std::integral_constant<int, 1>{});
-        else go(std::integral_constant<int, 4>{});
+        else if (x.M <= 4) go(std::integral_constant<int, 4>{});
+        else go(std::integral_constant<int, 8>{});
     } else {
         const dim3 grid((unsigned)((x.N + 15) / 16));
         auto go = [&](auto mt, auto waves) {
@@ -783,7 +784,7 @@ int rcd_rms_norm_backward(const void *dY_dev, int dt, int64_t rows, int64_t d, i
 
 size_t rcd_linear_workspace_bytes(int64_t M, int64_t N, int64_t K, int dt)
 {
-    if (!product_sizes_ok(M, N, K) || dt < RCD_F32 || dt > RCD_MXFP8 || M <= few_rows(dt)) return 0;
+    if (!product_sizes_ok(M, N, K) || dt < RCD_F32 || dt > RCD_MXFP8 || few_rows(M, N, K, dt)) return 0;
     return packed_bytes(M, K, dt) + packed_bytes(N, K, dt) +
            std::max(parts_bytes(cut_of(M, N, K, product_type(dt, K), 1, false), M, N, false), direct_parts(M, N, K, 1, false, dt));
 }
@@ -808,7 +809,7 @@ int rcd_linear(const void *A_dev, const uint8_t *A_scale_dev, int64_t ld_a, int6
     e.preact = preact_dev;
     e.ld_r = ld_r;
     e.ld_p = ld_p;
-    if (M <= few_rows(dt)) {
+    if (few_rows(M, N, K, dt)) {
         few::Args x = few_args(dt, A_dev, A_scale_dev, ld_a, ld_a_scale, M, N, K, e);
         few_weight(x, dt, false, W_dev, W_scale_dev, ld_w, ld_w_scale);
         return launch_few(dt, false, x, stream);
@@ -948,7 +949,7 @@ int rcd_linear_backward(const void *dY_dev, int64_t ld_dy, const void *A_dev, in
 
 size_t rcd_gated_linear_workspace_bytes(int64_t M, int64_t F, int64_t K, int dt)
 {
-    if (!product_sizes_ok(M, F, K) || dt < RCD_F32 || dt > RCD_MXFP8 || M <= few_rows(dt)) return 0;
+    if (!product_sizes_ok(M, F, K) || dt < RCD_F32 || dt > RCD_MXFP8 || few_rows(M, F, K, dt)) return 0;
     return packed_bytes(M, K, dt) + 2 * packed_bytes(F, K, dt) +
            std::max(parts_bytes(cut_of(M, F, K, product_type(dt, K), 1, true), M, F, true), direct_parts(M, F, K, 1, true, dt));
 }
@@ -971,7 +972,7 @@ int rcd_gated_linear(const void *A_dev, const uint8_t *A_scale_dev, int64_t ld_a
     Epilogue e = one_output(H_dev, ld_h, out_dt, act);
     e.preact = saved_dev;
     e.ld_p = 2 * F;
-    if (M <= few_rows(dt)) {
+    if (few_rows(M, F, K, dt)) {
         few::Args x = few_args(dt, A_dev, A_scale_dev, ld_a, ld_a_scale, M, F, K, e);
         few_weight(x, dt, false, Wg_dev, Wg_scale_dev, ld_wg, ld_wg_scale);
         few_weight(x, dt, true, Wu_dev, Wu_scale_dev, ld_wu, ld_wu_scale);

@@ -81,6 +81,18 @@ inline Both both_of(int64_t M1, int64_t N1, int64_t stages1, int64_t M2, int64_t
     return Both{false, cut_of(M1, N1, stages1, false), cut_of(M2, N2, stages2, false)};
 }
 
+// Whether a product has so few rows that each weight is best read once, straight into registers.  In us, that way / in
+// tiles: bf16, 17 rows, 2048 x 2048 7.5 / 11.6, 8192 x 2048 10.9 / 15.3, 2048 x 8192 28.4 / 17.6; 33 rows, 2048 x 2048 9.7 / 11.6, 8192 x
+// 2048 15.6 / 15.3; 64 rows, 512 x 512 4.7 / 9.7, 8192 x 2048 21.0 / 15.3; 8 bits, 32 rows, 2048 x 2048 9.1 / 9.6, 64 rows 13.7 / 9.6;
+// fp32, 16 rows here / 17 in tiles, 2048 x 2048 7.7 / 15.4, 8192 x 2048 25.9 / 39.7, 2048 x 8192 22.9 / 41.3.
+inline bool few_rows(int64_t M, int64_t N, int64_t K, bool f32, bool mx)
+{
+    if (M <= 16) return true;
+    if (f32) return false;
+    if (M <= 32) return K <= 4096;
+    return M <= 64 && K <= 2048 && N * K <= (mx ? (int64_t)1 << 20 : (int64_t)1 << 22);
+}
+
 // fp32 products go to the fp32 matrix instruction directly (wt 32: tiles of 64 x 64, k in stages of 32) where that takes less
 // than pieces do, whose launch and trip through memory come on top (4.5 us and 10 bytes per element at 5 TB/s).
 constexpr int DIRECT_STAGE = 32;

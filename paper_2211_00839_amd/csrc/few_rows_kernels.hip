@@ -150,6 +150,31 @@ k_few(const Args x)
     else finish_ahead8(x.e, em, ecol, ecount, z[0], bias, residual);
 }
 
+// Sums over the 64 lanes of LEFT values each: at each step a lane keeps half of its values and sends the others to the lane
+// that keeps those, so all of them take about as many shuffles as there are values, not six times as many.  A lane ends
+// with the whole sum number `mine` in v[0]; of the lanes that hold the same one, one is the `first`.
+template <int LEFT, int OFF, int N>
+__device__ __forceinline__ void spread_sums(float (&v)[N], int lane, int &mine, bool &first)
+{
+    if constexpr (OFF >= 1) {
+        const bool up = (lane & OFF) != 0;
+        if constexpr (LEFT > 1) {
+            constexpr int HALF = LEFT / 2;
+#pragma unroll
+            for (int i = 0; i < HALF; ++i) {
+                const float keep = up ? v[i + HALF] : v[i], send = up ? v[i] : v[i + HALF];
+                v[i] = keep + __shfl_xor(send, OFF);
+            }
+            mine += up ? HALF : 0;
+            spread_sums<HALF, OFF / 2>(v, lane, mine, first);
+        } else {
+            v[0] += __shfl_xor(v[0], OFF);
+            first = first && !up;
+            spread_sums<1, OFF / 2>(v, lane, mine, first);
+        }
+    }
+}
+
 // fp32: 8 columns to a workgroup, MR rows, plain multiply-adds (fp32 matrix instructions have no more).  Each of four waves
 // takes 256 of every 1024 k; grid = (ceil(N / 8), ceil(M / MR)).
 template <int MR, bool GATED>
@@ -195,15 +220,15 @@ k_few_f32(const Args x)
                 for (int e = 0; e < 4; ++e) acc[j][i] = fmaf(w[j][e], v[e], acc[j][i]);
         }
     }
+    float v[SUMS];
 #pragma unroll
     for (int j = 0; j < 8; ++j)
 #pragma unroll
-        for (int i = 0; i < MR; ++i) {
-            float s = acc[j][i];
-#pragma unroll
-            for (int off = 32; off >= 1; off >>= 1) s += __shfl_xor(s, off);
-            if (lane == 0) sums[wave][i * 8 + j] = s;
-        }
+        for (int i = 0; i < MR; ++i) v[i * 8 + j] = acc[j][i];
+    int mine = 0;
+    bool first = true;
+    spread_sums<SUMS, 32>(v, lane, mine, first);
+    if (first) sums[wave][mine] = v[0];
     __syncthreads();
     const int i = threadIdx.x, m = m0 + i, count = x.N - n0;
     if (i >= MR || m >= x.M) return;
