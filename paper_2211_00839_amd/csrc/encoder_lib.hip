@@ -77,11 +77,12 @@ template <bool MX, bool NORM> int launch_norm(const NormArgs &a, int dt, hipStre
     return RCD_OK;
 }
 
-// Row groups of the backward kernel, each with its own sums for the weight's gradient.
+// Row groups of the backward kernel, each with its own sums for the weight's gradient.  Rows of a workgroup of their own: as
+// many workgroups as the device holds at once (50 000 x 2048 bf16: 160 us and 8 for the sums; with half of them 187 and 6).
 inline int64_t norm_groups(int64_t rows, int64_t d)
 {
     const int64_t per = rows_per_workgroup(d);
-    return std::min<int64_t>((rows + per - 1) / per, 1024) * per;
+    return std::min<int64_t>((rows + per - 1) / per, per == 1 ? 2048 : 1024) * per;
 }
 inline int64_t part_pitch(int64_t d) { return (d + 63) / 64 * 64; }
 
