@@ -165,10 +165,10 @@ inline int64_t up64(int64_t n) { return (n + 63) / 64 * 64; }
 inline int64_t up128(int64_t n) { return (n + 127) / 128 * 128; }
 
 // 8-bit products of fewer k than this are computed in bf16, from widened copies.  The scaled matrix instruction lines
-// up the 64 products that it adds with the largest of them and cuts off what lies some 2^-11 below (measured: at most 2^-12.3 of the
-// sum of the products' sizes, over all bit patterns).  From about 1024 k on that is within what an fp32 sum of so many
-// terms may be off, (K + 8) 2^-23; a shorter sum would lose precision by it.
-constexpr int64_t MX_INSTRUCTION_FROM = 1024;
+// up the 64 products that it adds with the largest of them and cuts off what lies some 2^-11 below: measured, over all bit patterns, up
+// to 2^-12.3 of the sum of the products' sizes, and always towards the same side, so it does not average out.  An fp32 sum of K terms
+// may be off by (K + 8) 2^-23 of that sum; from 2048 on the instruction stays within it, a shorter sum would lose by it.
+constexpr int64_t MX_INSTRUCTION_FROM = 2048;
 inline int product_type(int dt, int64_t K) { return dt == RCD_MXFP8 && K < MX_INSTRUCTION_FROM ? RCD_BF16 : dt; }
 
 // Room for a matrix's packed copy, whatever its alignment (8 bits: its scales too).

@@ -99,8 +99,10 @@ constexpr int DIRECT_STAGE = 32;
 inline double direct_time_of(const Cut &c, int64_t M, int64_t N, int64_t stages, bool gated, int64_t units = UNITS)
 {
     const int64_t workgroups = c.tiles_m * c.tiles_n * c.splits, deep = ceil_div(stages, c.splits);
-    // a stage takes 0.55 us (gated: of two products) however many workgroups share a unit, up to four
-    double t = 4.0 + (double)ceil_div(workgroups, units) * (double)deep * (gated ? 1.0 : 0.55);
+    // 960 x 512 over k of 320, 640, 1280, 2560 (120 workgroups): 14.0, 18.1, 28.8, 50.1 us; 1920 x 512 over 640 (240 workgroups)
+    // 25.2; 128 x 8192 over 2048 (256) 72: what the workgroups read through L2 at 4 bytes a lane is the limit from half the units on
+    const double stage = workgroups <= units / 2 ? 0.52 : 1.0 * (double)ceil_div(workgroups, units);
+    double t = 8.0 + (double)deep * stage * (gated ? 1.5 : 1.0);
     if (c.splits > 1) t += 3.5 + 0.25 * c.splits + 2e-6 / 7 * (double)c.splits * (double)M * (double)N * 4 * (gated ? 2 : 1);
     return t;
 }
