@@ -321,17 +321,20 @@ void rcd_profile_read(double *out8_host);
  * Common to all of them
  *   - dt is RCD_F32 or RCD_BF16 for every matrix of a call that is not said to be something else.  Sums, statistics and
  *     products are accumulated in fp32 (or more) whatever dt is, and every output is rounded once, when it is stored.
- *     Products of RCD_F32 operands are exact to fp32: a factor goes to the matrix cores as three bf16 pieces that add up
- *     to it.
+ *     Products of RCD_F32 operands are exact to fp32 (a factor goes to the matrix cores as it is, or as three bf16 pieces
+ *     that add up to it).
  *   - RCD_MXFP8 (where an entry point lists it): elements are e4m3 bytes, and each block of 32 consecutive elements of a
  *     row (the last one may be shorter) shares a scale 2^(s - 127), s one byte; s = 255 means NaN.  Element i of a row
  *     stands for e4m3(byte i) * 2^(s[i / 32] - 127).  Scales are a byte matrix of their own, rows x ceil(d / 32), with a
- *     leading dimension in bytes.
+ *     leading dimension in bytes.  Their products are exact to fp32 for K < 2048 and for few rows; longer ones go to the
+ *     scaled matrix instruction, which cuts off what lies some 2^-11 below the largest of the 64 products it adds: no
+ *     more than an fp32 sum of K terms may be off, (K + 8) 2^-23 of the sum of the products' sizes.
  *   - Asynchronous on `stream`; nothing is allocated, no host wait; calls can be captured into a graph.
  *   - Outputs may not overlap inputs, workspace or each other, except where an entry point says so.  Elements of an
  *     output's rows beyond its columns (a leading dimension larger than the columns) are left alone.
- *   - Zero rows (rows = 0, M = 0) are legal: nothing is read, gradients of weights come out as zero.  Every other extent
- *     is at least 1 and at most 2^31 - 256, products of extents may pass 2^31.
+ *   - Zero rows (rows = 0, M = 0) are legal: nothing is read, gradients of weights come out as zero.  There are at most
+ *     2^31 - 256 rows; a row's length d of the norm and the quantizer is 1 .. 2^30, the products' lengths N, K and F are
+ *     1 .. 2^22.  Products of extents and leading dimensions may pass 2^31.
  *   - NaN and infinities travel as the formulas say, also in RCD_F32 products.
  */
 

@@ -4,8 +4,8 @@
 // That instruction multiplies at a sixteenth of bf16's rate, against six products of pieces; but the pieces are a launch and a
 // trip through memory of their own, and what is left of a small product's time is launches.  A workgroup of four waves (2 x 2)
 // computes 64 x 64 sums (gated: 64 rows of 64 columns of both products), each wave 32 x 32 as one MFMA block (two).  k
-// advances 32 at a time; a stage goes from memory into LDS element by element (4 bytes a lane, so any alignment and any length
-// will do), three stages ahead of its multiplies (gated two), which take less time than a load.
+// advances 32 at a time; a stage goes from memory into LDS 16 bytes a lane or, where rows do not lie so, 4 (any alignment and any
+// length will do), three stages ahead of its multiplies (gated two), which take less time than a load.
 #include "product_kernels.hip"
 
 namespace enc {
@@ -23,47 +23,61 @@ struct Args {
     int pairs, K;
 };
 
-// One operand's way into LDS.  Each wave brings a quarter of a stage with eight loads of 64 elements.
+// One operand's way into LDS.  Each wave brings a quarter of a stage, with eight loads of 64 elements or (WIDE: rows that lie
+// 16 bytes apart, lengths that are multiples of four) two of 256.
 // k contiguous: rows of 32 floats, the four of k / 4 = c of row r at place c ^ (r & 7) (spreads what one pass of a
 // ds_read_b128 touches over the banks).  Rows contiguous: lines of 64 rows, turned by 32 where k has bit 2 set (the two
 // halves of a wave read lines four apart).
-template <int KIND> struct Feed {
-    unsigned row_off[8], kpos[8];           // K_RUNS: byte offset of a load's row, place in k
-    unsigned line_off[2];                   // ROWS_RUN: byte offset of this lane's row, in straight and in turned lines
+template <int KIND, bool WIDE> struct Feed {
+    static constexpr int LOADS = WIDE ? 2 : 8, LANE = WIDE ? 4 : 1;     // loads of a wave and stage, elements of a lane
+    static constexpr int ROWS = 2 * LANE;       // K_RUNS: rows of a load.  ROWS_RUN: LANE lines
+    unsigned row_off[KIND == tile::K_RUNS ? LOADS : 2];     // byte offsets: of a load's row, or of this lane's rows in straight and turned lines
+    unsigned kpos[LOADS];                       // K_RUNS: place in k
     const float *p;
     long long pitch;
 
     __device__ __forceinline__ void init(const float *p_, long long pitch_, int row0, int extent, int wave, int lane)
     {
         pitch = pitch_;
+        constexpr int ACROSS = 32 / LANE;       // lanes side by side in a row's 32 k
         if constexpr (KIND == tile::K_RUNS) {
             p = p_ + row0 * pitch;
 #pragma unroll
-            for (int u = 0; u < 8; ++u) {
-                const int r = wave * 16 + u * 2 + (lane >> 5);
+            for (int u = 0; u < LOADS; ++u) {
+                const int r = wave * 16 + u * ROWS + lane / ACROSS, at = lane % ACROSS * LANE;
                 row_off[u] = (unsigned)((min(row0 + r, extent - 1) - row0) * pitch * 4);
-                kpos[u] = ((((lane & 31) >> 2) ^ (r & 7)) << 2) | (lane & 3);
+                kpos[u] = (((at >> 2) ^ (r & 7)) << 2) | (at & 3);
             }
         } else {
             p = p_ + row0;
-            line_off[0] = (unsigned)(min(row0 + lane, extent - 1) - row0) * 4;
-            line_off[1] = (unsigned)(min(row0 + (lane ^ 32), extent - 1) - row0) * 4;
+            const int at = lane % (64 / LANE) * LANE;
+            row_off[0] = (unsigned)(min(row0 + at, extent - LANE) - row0) * 4;
+            row_off[1] = (unsigned)(min(row0 + (at ^ 32), extent - LANE) - row0) * 4;
         }
     }
     // The stage from k0 on; from `there` k on there is nothing, what lies past them in LDS is some element of them.
-    __device__ __forceinline__ void load(const float *from, int k0, int there, int wave, unsigned lds)
+    __device__ __forceinline__ void load(const float *from, int k0, int there, int wave, int lane, unsigned lds)
     {
 #pragma unroll
-        for (int u = 0; u < 8; ++u) {
-            const unsigned to = lds + (wave * 8 + u) * 256;
+        for (int u = 0; u < LOADS; ++u) {
+            const unsigned to = lds + (wave * LOADS + u) * (256 * LANE);
             if constexpr (KIND == tile::K_RUNS) {
-                const unsigned k = min(kpos[u], (unsigned)(there - 1));
-                tile::load4_to_lds(from + k0, row_off[u] + k * 4, to);
+                // (WIDE: the four k of the last one that there is)
+                const unsigned k = min(kpos[u], (unsigned)(there - 1) & ~(unsigned)(LANE - 1));
+                send(from + k0, row_off[u] + k * 4, to);
+            } else if constexpr (WIDE) {
+                const int k = wave * 8 + u * 4 + lane / 16;         // (bit 2 of k is u)
+                send(from + (long long)k0 * pitch, row_off[u] + (unsigned)(min(k, there - 1) * pitch * 4), to);
             } else {
                 const int k = wave * 8 + u;
-                tile::load4_to_lds(from + (long long)(k0 + min(k, there - 1)) * pitch, line_off[(k >> 2) & 1], to);
+                send(from + (long long)(k0 + min(k, there - 1)) * pitch, row_off[(k >> 2) & 1], to);
             }
         }
+    }
+    static __device__ __forceinline__ void send(const float *from, unsigned offset, unsigned to)
+    {
+        if constexpr (WIDE) tile::load16_to_lds(from, offset, to);
+        else tile::load4_to_lds(from, offset, to);
     }
 };
 
@@ -80,11 +94,11 @@ template <int KIND> __device__ __forceinline__ f32x4 four(const float *side, int
     }
 }
 
-template <int KA, int KB, int TO>
+template <int KA, int KB, int TO, bool WIDE>
 __device__ __forceinline__ void direct_body(const Args &x, int wg, int nwg, float *lds)
 {
     constexpr bool GATED = TO == tile::TO_GATED || TO == tile::TO_GATED_PARTS;
-    constexpr int G = GATED ? 2 : 1, DEPTH = GATED ? 3 : 4, LOADS = 8 * (1 + G);
+    constexpr int G = GATED ? 2 : 1, DEPTH = GATED ? 3 : 4, LOADS = (WIDE ? 2 : 8) * (1 + G);
     constexpr int STAGE = (1 + G) * SIDE;
     using Out = tile::Band<GATED ? 64 : 32, GATED>;
     static_assert(DEPTH * STAGE <= LDS_FLOATS && 4 * 32 * Out::PITCH <= DEPTH * STAGE, "the waves' turn-round regions fit where the stages were");
@@ -99,8 +113,8 @@ __device__ __forceinline__ void direct_body(const Args &x, int wg, int nwg, floa
     for (int g = 0; g < G; ++g)
 #pragma unroll
         for (int r = 0; r < 16; ++r) acc[g][r] = 0.f;
-    Feed<KA> fa;
-    Feed<KB> fb[G];
+    Feed<KA, WIDE> fa;
+    Feed<KB, WIDE> fb[G];
     fa.init(x.a[0], x.a_pitch, m0, x.a_extent, wave, lane);
 #pragma unroll
     for (int g = 0; g < G; ++g) fb[g].init(x.b[g], x.b_pitch[g], n0, x.b_extent, wave, lane);
@@ -110,16 +124,16 @@ __device__ __forceinline__ void direct_body(const Args &x, int wg, int nwg, floa
         const bool second = s >= per;
         const int k0 = (second ? s - per : s) * KS;
         const unsigned to = lds_base + (unsigned)((s - s0) % DEPTH) * (STAGE * 4);
-        fa.load(second ? fa.p + (x.a[1] - x.a[0]) : fa.p, k0, there(s), wave, to);
+        fa.load(second ? fa.p + (x.a[1] - x.a[0]) : fa.p, k0, there(s), wave, lane, to);
 #pragma unroll
         for (int g = 0; g < G; ++g) {
             if (!GATED && second) {
                 // (the second pair's b may have a pitch of its own)
-                Feed<KB> other;
+                Feed<KB, WIDE> other;
                 other.init(x.b[1], x.b_pitch[1], n0, x.b_extent, wave, lane);
-                other.load(other.p, k0, there(s), wave, to + (1 + g) * (SIDE * 4));
+                other.load(other.p, k0, there(s), wave, lane, to + (1 + g) * (SIDE * 4));
             } else {
-                fb[g].load(fb[g].p, k0, there(s), wave, to + (1 + g) * (SIDE * 4));
+                fb[g].load(fb[g].p, k0, there(s), wave, lane, to + (1 + g) * (SIDE * 4));
             }
         }
     };
@@ -136,21 +150,26 @@ __device__ __forceinline__ void direct_body(const Args &x, int wg, int nwg, floa
         if (s + DEPTH - 1 < s1) fetch(s + DEPTH - 1);
         const float *stage = lds + ((s - s0) % DEPTH) * STAGE;
         const int mine = there(s) - half * 4;
+        // lanes 0-31 carry k = 0 .. 3 of each eight, lanes 32-63 k = 4 .. 7, for both operands alike.  The whole stage is read
+        // ahead of its multiplies
+        f32x4 a[KS / 8], b[G][KS / 8];
 #pragma unroll
-        for (int k = 0; k < KS; k += 8) {
-            // lanes 0-31 carry k = 0 .. 3 of each eight, lanes 32-63 k = 4 .. 7, for both operands alike
-            f32x4 a = four<KA>(stage, ra, half, k);
+        for (int k = 0; k < KS / 8; ++k) {
+            a[k] = four<KA>(stage, ra, half, k * 8);
 #pragma unroll
-            for (int e = 0; e < 4; ++e) a[e] = k + e < mine ? a[e] : 0.f;
-#pragma unroll
-            for (int g = 0; g < G; ++g) {
-                f32x4 b = four<KB>(stage + (1 + g) * SIDE, rb, half, k);
-#pragma unroll
-                for (int e = 0; e < 4; ++e) b[e] = k + e < mine ? b[e] : 0.f;
-#pragma unroll
-                for (int e = 0; e < 4; ++e) acc[g] = __builtin_amdgcn_mfma_f32_32x32x2f32(b[e], a[e], acc[g], 0, 0, 0);
-            }
+            for (int g = 0; g < G; ++g) b[g][k] = four<KB>(stage + (1 + g) * SIDE, rb, half, k * 8);
         }
+        tile::pin();
+#pragma unroll
+        for (int k = 0; k < KS / 8; ++k)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+                const bool there = k * 8 + e < mine;
+                const float x = there ? a[k][e] : 0.f;
+#pragma unroll
+                for (int g = 0; g < G; ++g)
+                    acc[g] = __builtin_amdgcn_mfma_f32_32x32x2f32(there ? b[g][k][e] : 0.f, x, acc[g], 0, 0, 0);
+            }
     }
     tile::wait_lds();
     tile::meet();
@@ -173,26 +192,28 @@ __device__ __forceinline__ void direct_body(const Args &x, int wg, int nwg, floa
     }
 }
 
-template <int KA, int KB, int TO>
+template <int KA, int KB, int TO, bool WIDE>
 __global__ void __launch_bounds__(256)
 k_direct(const Args x)
 {
     __shared__ __attribute__((aligned(16))) float lds[LDS_FLOATS];
-    direct_body<KA, KB, TO>(x, (int)blockIdx.x, (int)gridDim.x, lds);
+    direct_body<KA, KB, TO, WIDE>(x, (int)blockIdx.x, (int)gridDim.x, lds);
 }
 
 // A backward call's two products side by side: x's workgroups are the first `first` (a multiple of 8) of the launch.
+template <bool WIDE>
 __global__ void __launch_bounds__(256)
 k_direct_both(const Args x, const Args y, int first)
 {
+    using namespace tile;
     __shared__ __attribute__((aligned(16))) float lds[LDS_FLOATS];
     const int wg = (int)blockIdx.x;
     if (wg < first) {
-        if (x.t.splits > 1) direct_body<tile::K_RUNS, tile::ROWS_RUN, tile::TO_PARTS>(x, wg, first, lds);
-        else direct_body<tile::K_RUNS, tile::ROWS_RUN, tile::TO_LINEAR>(x, wg, first, lds);
+        if (x.t.splits > 1) direct_body<K_RUNS, ROWS_RUN, TO_PARTS, WIDE>(x, wg, first, lds);
+        else direct_body<K_RUNS, ROWS_RUN, TO_LINEAR, WIDE>(x, wg, first, lds);
     } else {
-        if (y.t.splits > 1) direct_body<tile::ROWS_RUN, tile::ROWS_RUN, tile::TO_PARTS>(y, wg - first, (int)gridDim.x - first, lds);
-        else direct_body<tile::ROWS_RUN, tile::ROWS_RUN, tile::TO_LINEAR>(y, wg - first, (int)gridDim.x - first, lds);
+        if (y.t.splits > 1) direct_body<ROWS_RUN, ROWS_RUN, TO_PARTS, WIDE>(y, wg - first, (int)gridDim.x - first, lds);
+        else direct_body<ROWS_RUN, ROWS_RUN, TO_LINEAR, WIDE>(y, wg - first, (int)gridDim.x - first, lds);
     }
 }
 

@@ -16,13 +16,16 @@ namespace {
 
 using namespace enc;
 
-constexpr int64_t MAX_EXTENT = 0x7fffff00;
+constexpr int64_t MAX_EXTENT = 0x7fffff00;          // rows
+constexpr int64_t MAX_NORM_LENGTH = (int64_t)1 << 30;
+// Lengths of a product: 255 rows of two packed ones side by side (a gated block's gradients) stay within the tile kernels' 32-bit
+// byte offsets.
+constexpr int64_t MAX_LENGTH = (int64_t)1 << 22;
 
 inline size_t up256(size_t x) { return (x + 255) & ~(size_t)255; }
 inline bool is_matrix_type(int dt) { return dt == RCD_F32 || dt == RCD_BF16; }
 inline int64_t size_of(int dt) { return dt == RCD_F32 ? 4 : dt == RCD_BF16 ? 2 : 1; }
 inline int64_t blocks_of(int64_t d) { return (d + MX_BLOCK - 1) / MX_BLOCK; }
-inline bool extent_ok(int64_t n) { return n >= 1 && n <= MAX_EXTENT; }
 
 // Rows that may be accessed `bytes` at a time.
 inline bool rows_aligned(const void *p, int64_t ld, int64_t esz, int64_t bytes = 16)
@@ -450,9 +453,20 @@ struct DirectProduct {
     bool gated;
     const float *a[2], *b[2];
     int64_t a_pitch, b_pitch[2];
-    int64_t a_extent, b_extent;
+    int64_t a_extent, b_extent;         // rows
+    int64_t a_cols, b_cols;             // what may be read of a contiguous run: of a row (k contiguous) or of a line (rows contiguous)
     Epilogue e;
 };
+// Whether both operands can go into LDS 16 bytes a lane.
+bool is_wide(const DirectProduct &p)
+{
+    auto side = [&](const float *x, int64_t pitch, int kind, int64_t cols) {
+        return !x || (rows_aligned(x, pitch, 4) && (kind == tile::K_RUNS ? (p.K + 3) / 4 * 4 <= cols : cols % 4 == 0 && pitch <= ((int64_t)1 << 23)));
+    };
+    const bool second = p.pairs == 2;
+    return side(p.a[0], p.a_pitch, p.ka, p.a_cols) && side(second ? p.a[1] : nullptr, p.a_pitch, p.ka, p.a_cols) &&
+           side(p.b[0], p.b_pitch[0], p.kb, p.b_cols) && side(second || p.gated ? p.b[1] : nullptr, p.b_pitch[1], p.kb, p.b_cols);
+}
 Cut direct_cut(int64_t M, int64_t N, int64_t K, int pairs, bool gated)
 {
     return enc_rules::direct_cut_of(M, N, enc_rules::ceil_div(K, enc_rules::DIRECT_STAGE) * pairs, gated);
@@ -476,8 +490,8 @@ direct::Args plan_direct(const DirectProduct &p, const Cut &c, Pieces &room)
         x.b_pitch[i] = p.b_pitch[i];
     }
     x.a_pitch = p.a_pitch;
-    x.a_extent = (int)p.a_extent;
-    x.b_extent = (int)p.b_extent;
+    x.a_extent = (int)(p.ka == tile::K_RUNS ? p.a_extent : p.a_cols);
+    x.b_extent = (int)(p.kb == tile::K_RUNS ? p.b_extent : p.b_cols);
     x.pairs = p.pairs;
     x.K = (int)p.K;
     x.t.e = p.e;
@@ -494,20 +508,25 @@ int launch_planned(const DirectProduct &p, const Cut &c, const direct::Args &x, 
 {
     const dim3 grid(grid_of(c));
     constexpr int K = tile::K_RUNS, R = tile::ROWS_RUN;
-    auto go = [&](auto kernel) { hipLaunchKernelGGL(kernel, grid, dim3(256), 0, stream, x); };
-    if (p.gated) {
-        if (c.splits > 1) go(direct::k_direct<K, K, tile::TO_GATED_PARTS>);
-        else go(direct::k_direct<K, K, tile::TO_GATED>);
-    } else if (p.ka == R) {
-        if (c.splits > 1) go(direct::k_direct<R, R, tile::TO_PARTS>);
-        else go(direct::k_direct<R, R, tile::TO_LINEAR>);
-    } else if (p.kb == R) {
-        if (c.splits > 1) go(direct::k_direct<K, R, tile::TO_PARTS>);
-        else go(direct::k_direct<K, R, tile::TO_LINEAR>);
-    } else {
-        if (c.splits > 1) go(direct::k_direct<K, K, tile::TO_PARTS>);
-        else go(direct::k_direct<K, K, tile::TO_LINEAR>);
-    }
+    auto go = [&](auto wide) {
+        constexpr bool W = decltype(wide)::value;
+        auto launch = [&](auto kernel) { hipLaunchKernelGGL(kernel, grid, dim3(256), 0, stream, x); };
+        if (p.gated) {
+            if (c.splits > 1) launch(direct::k_direct<K, K, tile::TO_GATED_PARTS, W>);
+            else launch(direct::k_direct<K, K, tile::TO_GATED, W>);
+        } else if (p.ka == R) {
+            if (c.splits > 1) launch(direct::k_direct<R, R, tile::TO_PARTS, W>);
+            else launch(direct::k_direct<R, R, tile::TO_LINEAR, W>);
+        } else if (p.kb == R) {
+            if (c.splits > 1) launch(direct::k_direct<K, R, tile::TO_PARTS, W>);
+            else launch(direct::k_direct<K, R, tile::TO_LINEAR, W>);
+        } else {
+            if (c.splits > 1) launch(direct::k_direct<K, K, tile::TO_PARTS, W>);
+            else launch(direct::k_direct<K, K, tile::TO_LINEAR, W>);
+        }
+    };
+    if (is_wide(p)) go(std::true_type{});
+    else go(std::false_type{});
     if (c.splits > 1) launch_join(x.t, p.gated, stream);
     ENC_HIP_TRY(hipGetLastError());
     return RCD_OK;
@@ -535,7 +554,9 @@ int launch_both(const DirectProduct *da, const DirectProduct *dw, const enc_rule
     if (da && dw) {
         const direct::Args x = plan_direct(*da, cut.first, room), y = plan_direct(*dw, cut.second, room);
         const unsigned first = grid_of(cut.first);
-        hipLaunchKernelGGL(direct::k_direct_both, dim3(first + grid_of(cut.second)), dim3(256), 0, stream, x, y, (int)first);
+        const dim3 grid(first + grid_of(cut.second));
+        if (is_wide(*da) && is_wide(*dw)) hipLaunchKernelGGL(direct::k_direct_both<true>, grid, dim3(256), 0, stream, x, y, (int)first);
+        else hipLaunchKernelGGL(direct::k_direct_both<false>, grid, dim3(256), 0, stream, x, y, (int)first);
         return launch_join_both(x.t, y.t, cols, stream);
     }
     if (cols.part) ENC_TRY(sum_columns(cols, stream));
@@ -647,11 +668,14 @@ int check_product(int dt, int out_dt, int64_t M, int64_t N, int64_t K, int act)
     if (!is_matrix_type(out_dt) || (dt == RCD_F32 && out_dt != RCD_F32)) return RCD_ERR_UNSUPPORTED;
     if (act < RCD_ACT_NONE || act > RCD_ACT_GELU) return RCD_ERR_UNSUPPORTED;
     if (M < 0 || N < 1 || K < 1) return RCD_ERR_INVALID_ARG;
-    if (M > MAX_EXTENT || N > MAX_EXTENT || K > MAX_EXTENT) return RCD_ERR_UNSUPPORTED;
+    if (M > MAX_EXTENT || N > MAX_LENGTH || K > MAX_LENGTH) return RCD_ERR_UNSUPPORTED;
     return RCD_OK;
 }
 
-inline bool product_sizes_ok(int64_t M, int64_t N, int64_t K) { return extent_ok(M) && extent_ok(N) && extent_ok(K); }
+inline bool product_sizes_ok(int64_t M, int64_t N, int64_t K)
+{
+    return M >= 1 && M <= MAX_EXTENT && N >= 1 && N <= MAX_LENGTH && K >= 1 && K <= MAX_LENGTH;
+}
 
 Epilogue one_output(void *out, int64_t ld, int dt, int act)
 {
@@ -710,6 +734,8 @@ int check_mx_operand(int dt, const uint8_t *scale, int64_t ld_scale, int64_t K)
 
 } // namespace
 
+int rcd_set_up_encoder() { return set_up(); }
+
 extern "C" {
 
 int rcd_rms_norm(const void *X_dev, int dt, int64_t rows, int64_t d, int64_t ld_x, const void *residual_dev, int64_t ld_r,
@@ -721,7 +747,7 @@ int rcd_rms_norm(const void *X_dev, int dt, int64_t rows, int64_t d, int64_t ld_
     if (rows < 0 || d < 1 || ld_x < d || ld_y < d || (residual_dev && ld_r < d) || (sum_dev && ld_s < d) ||
         (mx && ld_scale < blocks_of(d)) || !(eps >= 0.f) || !std::isfinite(eps))
         return RCD_ERR_INVALID_ARG;
-    if (rows > MAX_EXTENT || d > MAX_EXTENT) return RCD_ERR_UNSUPPORTED;
+    if (rows > MAX_EXTENT || d > MAX_NORM_LENGTH) return RCD_ERR_UNSUPPORTED;
     if (rows == 0) return RCD_OK;
     if (!X_dev || !Y_dev || (mx && !scale_dev)) return RCD_ERR_INVALID_ARG;
     if (sum_dev == Y_dev) return RCD_ERR_INVALID_ARG;
@@ -738,7 +764,7 @@ int rcd_quantize_mxfp8(const void *X_dev, int dt, int64_t rows, int64_t d, int64
 {
     if (!is_matrix_type(dt)) return RCD_ERR_UNSUPPORTED;
     if (rows < 0 || d < 1 || ld_x < d || ld_q < d || ld_scale < blocks_of(d)) return RCD_ERR_INVALID_ARG;
-    if (rows > MAX_EXTENT || d > MAX_EXTENT) return RCD_ERR_UNSUPPORTED;
+    if (rows > MAX_EXTENT || d > MAX_NORM_LENGTH) return RCD_ERR_UNSUPPORTED;
     if (rows == 0) return RCD_OK;
     if (!X_dev || !Q_dev || !scale_dev) return RCD_ERR_INVALID_ARG;
     NormArgs a{};
@@ -750,7 +776,7 @@ int rcd_quantize_mxfp8(const void *X_dev, int dt, int64_t rows, int64_t d, int64
 
 size_t rcd_rms_norm_backward_workspace_bytes(int64_t rows, int64_t d)
 {
-    if (rows < 1 || !extent_ok(d)) return 0;
+    if (rows < 1 || rows > MAX_EXTENT || d < 1 || d > MAX_NORM_LENGTH) return 0;
     return up256((size_t)norm_groups(rows, d) * part_pitch(d) * 4);
 }
 
@@ -762,7 +788,7 @@ int rcd_rms_norm_backward(const void *dY_dev, int dt, int64_t rows, int64_t d, i
     hipStream_t stream = (hipStream_t)stream_;
     if (!is_matrix_type(dt)) return RCD_ERR_UNSUPPORTED;
     if (rows < 0 || d < 1 || ld_dy < d || ld_h < d || ld_dx < d || (dsum_dev && ld_ds < d)) return RCD_ERR_INVALID_ARG;
-    if (rows > MAX_EXTENT || d > MAX_EXTENT) return RCD_ERR_UNSUPPORTED;
+    if (rows > MAX_EXTENT || d > MAX_NORM_LENGTH) return RCD_ERR_UNSUPPORTED;
     if (rows == 0) return zero_matrix(dweight_dev, dt, d, 1, d, stream);
     if (!dY_dev || !H_dev || !rstd_dev || !dX_dev) return RCD_ERR_INVALID_ARG;
     const int64_t groups = norm_groups(rows, d);
@@ -827,6 +853,7 @@ int rcd_linear(const void *A_dev, const uint8_t *A_scale_dev, int64_t ld_a, int6
         p.b_pitch[0] = ld_w;
         p.a_extent = M;
         p.b_extent = N;
+        p.a_cols = p.b_cols = K;
         p.e = e;
         return launch_direct(p, room, stream);
     }
@@ -921,14 +948,13 @@ int rcd_linear_backward(const void *dY_dev, int64_t ld_dy, const void *A_dev, in
         p.b[0] = (const float *)W_dev;
         p.b_pitch[0] = ld_w;
         p.a_extent = M;
-        p.b_extent = K;
+        p.a_cols = q.a_cols = as_it_is ? N : pitch;       // (packed rows end in zeros)
+        p.b_cols = q.b_cols = K;
         p.e = one_output(dA_dev, ld_da, dt, RCD_ACT_NONE);
         q.M = N; q.N = K; q.K = M;
         q.ka = q.kb = tile::ROWS_RUN;
         q.b[0] = (const float *)A_dev;
         q.b_pitch[0] = ld_a;
-        q.a_extent = N;
-        q.b_extent = K;
         q.e = one_output(dW_dev, ld_dw, dt, RCD_ACT_NONE);
         return launch_both(dA_dev ? &p : nullptr, dW_dev ? &q : nullptr, direct_both(M, N, K, 1), room, cols, stream);
     }
@@ -994,6 +1020,7 @@ int rcd_gated_linear(const void *A_dev, const uint8_t *A_scale_dev, int64_t ld_a
         p.b_pitch[1] = ld_wu;
         p.a_extent = M;
         p.b_extent = F;
+        p.a_cols = p.b_cols = K;
         p.e = e;
         return launch_direct(p, room, stream);
     }
@@ -1083,15 +1110,15 @@ int rcd_gated_linear_backward(const void *dH_dev, int64_t ld_dh, const void *A_d
         p.b_pitch[0] = ld_wg;
         p.b_pitch[1] = ld_wu;
         p.a_extent = M;
-        p.b_extent = K;
+        p.a_cols = half;                                  // (packed rows end in zeros)
+        p.b_cols = q.b_cols = K;
         p.e = one_output(dA_dev, ld_da, dt, RCD_ACT_NONE);
         q.M = pitch; q.N = K; q.K = M;
         q.ka = q.kb = tile::ROWS_RUN;
         q.pairs = 1;
         q.b[0] = (const float *)A_dev;
         q.b_pitch[0] = ld_a;
-        q.a_extent = pitch;
-        q.b_extent = K;
+        q.a_cols = pitch;
         q.e = both;
         return launch_both(dA_dev ? &p : nullptr, dWg_dev ? &q : nullptr, direct_both(M, F, K, 2), room, tile::Columns{}, stream);
     }

@@ -80,7 +80,8 @@ __device__ __forceinline__ float exp_f32(float x)
     return fmaf(__builtin_amdgcn_exp2f(t), lost * 0.693147181f, __builtin_amdgcn_exp2f(t));
 }
 
-__device__ __forceinline__ float logistic(float z) { return __builtin_amdgcn_rcpf(1.f + exp_f32(-z)); }
+// 1 / (1 + e^-z); 0 from where it is below the normal numbers on (so that silu of -infinity is the formula's NaN).
+__device__ __forceinline__ float logistic(float z) { return z < -87.f ? 0.f : __builtin_amdgcn_rcpf(1.f + exp_f32(-z)); }
 
 // Phi(z) and the density's e^(-z^2/2), which it is made of: erfc(x) = (a1 t + .. + a5 t^5) e^(-x^2) with
 // t = 1 / (1 + p x), x = |z| / sqrt 2, off by at most 1.5e-7 (Abramowitz and Stegun, 7.1.26); Phi to half of that.  No

@@ -68,8 +68,7 @@ inline Cut cut_of(int64_t M, int64_t N, int64_t stages, bool gated, int64_t unit
 inline int64_t workgroups_of(const Cut &c) { return c.tiles_m * c.tiles_n * c.splits; }
 
 // A backward call's two products, side by side in one launch where each is small enough to leave room for the other: both in
-// small tiles, all workgroups on the device at once.  2500 x 512 x 1365 in fp32, gated, one after the other / side by side: 194 / 163 us
-// the whole training step.
+// small tiles, all workgroups on the device at once.
 struct Both {
     bool together;
     Cut first, second;
@@ -99,10 +98,10 @@ constexpr int DIRECT_STAGE = 32;
 inline double direct_time_of(const Cut &c, int64_t M, int64_t N, int64_t stages, bool gated, int64_t units = UNITS)
 {
     const int64_t workgroups = c.tiles_m * c.tiles_n * c.splits, deep = ceil_div(stages, c.splits);
-    // 960 x 512 over k of 320, 640, 1280, 2560 (120 workgroups): 14.0, 18.1, 28.8, 50.1 us; 1920 x 512 over 640 (240 workgroups)
-    // 25.2; 128 x 8192 over 2048 (256) 72: what the workgroups read through L2 at 4 bytes a lane is the limit from half the units on
-    const double stage = workgroups <= units / 2 ? 0.52 : 1.0 * (double)ceil_div(workgroups, units);
-    double t = 8.0 + (double)deep * stage * (gated ? 1.5 : 1.0);
+    // a stage takes a unit 0.85 us, whether one workgroup has it to itself or two share it (measured, in 1 / 2 / 4 parts: 64 x 8192 over
+    // 2048 61.1 / 36.4 / 31.3 us, 960 x 512 over 640 21.5 / 16.4 / 16.5, 999 x 511 over 300 12.7 / 12.1 / 13.2, 300 x 300 over 1200 37.0 / 22.6 /
+    // 15.0, 2048 x 1024 over 640 33.2 / 42.2 / 46.9)
+    double t = 5.0 + (double)ceil_div(workgroups, units) * (double)deep * (gated ? 1.5 : 0.85);
     if (c.splits > 1) t += 3.5 + 0.25 * c.splits + 2e-6 / 7 * (double)c.splits * (double)M * (double)N * 4 * (gated ? 2 : 1);
     return t;
 }

@@ -8,6 +8,9 @@
 // Notes the text of a failed HIP call for rcd_last_hip_error() of the calling thread; returns RCD_ERR_HIP.
 __attribute__((visibility("hidden"))) int rcd_note_hip_error(const char *what, hipError_t e);
 
+// The encoder's part of rcd_init(): what its kernels need once per device.
+__attribute__((visibility("hidden"))) int rcd_set_up_encoder();
+
 #define ENC_HIP_TRY(expr)                                            \
     do {                                                             \
         hipError_t e_ = (expr);                                      \

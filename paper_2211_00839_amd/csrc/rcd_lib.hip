@@ -1711,6 +1711,7 @@ int rcd_init(void)
     RCD_TRY(sweep_setup());
     RCD_TRY(fast_setup());
     RCD_TRY(static_setup(nullptr));
+    RCD_TRY(rcd_set_up_encoder());
     return RCD_OK;
 }
 

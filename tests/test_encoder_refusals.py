@@ -106,6 +106,10 @@ def test_linear(lib):
     assert linear(lib, dt=MX, out=BF16, sa=P) == INVALID
     assert linear(lib, dt=MX, out=BF16, sa=P, sw=P, K=65, lda=65, ldw=65) == INVALID      # three scales to a row, two apart
     assert linear(lib, M=1 << 31) == UNSUPPORTED
+    long = (1 << 22) + 1
+    assert linear(lib, K=long, lda=long, ldw=long) == UNSUPPORTED
+    assert linear(lib, N=long, ldy=long) == UNSUPPORTED
+    assert lib.rcd_linear_workspace_bytes(64, 64, long, F32) == 0
 
 
 def test_linear_backward(lib):

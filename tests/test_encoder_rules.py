@@ -88,10 +88,29 @@ def test_few_rows_go_past_the_tiles_only_where_that_is_faster(ask):
 
 def test_small_fp32_products_go_without_pieces_where_that_is_faster(ask):
     # (M, N, K, us directly, us by pieces)
-    measured = [(999, 511, 300, 14.8, 21.7), (8000, 2048, 2048, 700, 345)]
+    measured = [(999, 511, 300, 12.7, 21.7), (2048, 2048, 640, 60.9, 52.3), (8000, 2048, 2048, 700, 345)]
     got = ask("\n".join("put(direct_forward(%d, %d, %d, false));" % m[:3] for m in measured))
     for m, direct in zip(measured, got):
         assert bool(direct) == (m[3] < m[4]), m
+
+
+# (M, N, K): {parts: us}, fp32 directly
+MEASURED_DIRECT = {
+    (64, 8192, 2048): {1: 61.1, 2: 36.4, 3: 38.3, 4: 31.3, 6: 33.7},
+    (960, 512, 640): {1: 21.5, 2: 16.4, 3: 17.5, 4: 16.5, 6: 19.0},
+    (999, 511, 300): {1: 12.7, 2: 12.1, 3: 13.2, 4: 13.2},
+    (2048, 1024, 640): {1: 33.2, 2: 42.2},
+    (300, 300, 1200): {1: 37.0, 2: 22.6, 3: 17.4, 4: 15.0, 6: 13.0},
+}
+
+
+def test_direct_products_are_cut_within_a_fifth_of_the_fastest_way_measured(ask):
+    keys = sorted(MEASURED_DIRECT)
+    got = ask("\n".join("put(direct_cut_of(%d, %d, ceil_div(%d, DIRECT_STAGE), false).splits);" % key for key in keys))
+    for key, parts in zip(keys, got):
+        points = MEASURED_DIRECT[key]
+        parts = max(p for p in points if p <= parts)
+        assert points[parts] <= 1.2 * min(points.values()), (key, parts)
 
 
 def test_the_gpu_tests_sizes_reach_every_route(ask):
