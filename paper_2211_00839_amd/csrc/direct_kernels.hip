@@ -192,6 +192,8 @@ __device__ __forceinline__ void direct_body(const Args &x, int wg, int nwg, floa
     }
 }
 
+// Bound by the wait from stage to stage where workgroups are few, by the fp32 instruction where they are many: 999 x 511 x 300 12.7 us,
+// 2048 x 1024 x 640 33.2 us (81 TFLOP/s, 54 % of a large library product).  The loads of 4 bytes take 14.2 and 37.3.
 template <int KA, int KB, int TO, bool WIDE>
 __global__ void __launch_bounds__(256)
 k_direct(const Args x)
@@ -200,7 +202,8 @@ k_direct(const Args x)
     direct_body<KA, KB, TO, WIDE>(x, (int)blockIdx.x, (int)gridDim.x, lds);
 }
 
-// A backward call's two products side by side: x's workgroups are the first `first` (a multiple of 8) of the launch.
+// A backward call's two products side by side: x's workgroups are the first `first` (a multiple of 8) of the launch.  960 x 1280 x 512
+// 41.1 us the call, 57.2 one after the other.
 template <bool WIDE>
 __global__ void __launch_bounds__(256)
 k_direct_both(const Args x, const Args y, int first)

@@ -68,7 +68,9 @@ inline Cut cut_of(int64_t M, int64_t N, int64_t stages, bool gated, int64_t unit
 inline int64_t workgroups_of(const Cut &c) { return c.tiles_m * c.tiles_n * c.splits; }
 
 // A backward call's two products, side by side in one launch where each is small enough to leave room for the other: both in
-// small tiles, all workgroups on the device at once.
+// small tiles, all workgroups on the device at once.  The whole backward call in us, side by side / one after the other, bf16:
+// 128 x 512 x 512 13.5 / 18.9, 1000 x 1024 x 1024 21.8 / 31.6 (gated 31.2 / 42.4), 2500 x 1365 x 512 41.5 / 48.3 (gated 53.0 / 56.8);
+// fp32: 960 x 1280 x 512 41.1 / 57.2, 2000 x 1024 x 1024 79.5 / 97.2.
 struct Both {
     bool together;
     Cut first, second;
