@@ -73,7 +73,10 @@ k_few(const Args x)
     static_assert(2 * 16 * MT <= 64 * WAVES, "a thread for every eight columns");
     const int em = threadIdx.x >> 1, ecol = n0 + (threadIdx.x & 1) * 8, ecount = em < x.M ? x.N - ecol : 0;
     float bias[8], residual[8];
-    if constexpr (!GATED) ahead8(x.e, em, ecol, ecount, bias, residual);
+    if constexpr (!GATED) {
+        bias8(x.e, ecol, ecount, bias);
+        residual8(x.e, em, ecol, ecount, residual);
+    }
     const int blocks = (x.K + MX_BLOCK - 1) / MX_BLOCK;
 #pragma unroll 4
     for (int c = wave; c < chunks; c += WAVES) {

@@ -58,20 +58,22 @@ __device__ __forceinline__ void finish_linear8(const Epilogue &e, int m, int n, 
     else finish_linear8_as(e, (__bf16 *)out, row, m, n, count, z);
 }
 
-// The same in two halves: what is read, and what is made of it (one output, no second one).
-__device__ __forceinline__ void ahead8(const Epilogue &e, int m, int n, int count, float (&bias)[8], float (&residual)[8])
+// The same in two halves: what is read (zeros where there is nothing), and what is made of it (one output, no second one).
+__device__ __forceinline__ void bias8(const Epilogue &e, int n, int count, float (&bias)[8])
 {
 #pragma unroll
-    for (int i = 0; i < 8; ++i) bias[i] = residual[i] = 0.f;
-    if (count <= 0) return;
-    if (e.bias) {
-        if (e.out_f32) load8((const float *)e.bias + n, count, bias);
-        else load8((const __bf16 *)e.bias + n, count, bias);
-    }
-    if (e.residual) {
-        if (e.out_f32) load8((const float *)e.residual + m * e.ld_r + n, count, residual);
-        else load8((const __bf16 *)e.residual + m * e.ld_r + n, count, residual);
-    }
+    for (int i = 0; i < 8; ++i) bias[i] = 0.f;
+    if (!e.bias || count <= 0) return;
+    if (e.out_f32) load8((const float *)e.bias + n, count, bias);
+    else load8((const __bf16 *)e.bias + n, count, bias);
+}
+__device__ __forceinline__ void residual8(const Epilogue &e, int m, int n, int count, float (&residual)[8])
+{
+#pragma unroll
+    for (int i = 0; i < 8; ++i) residual[i] = 0.f;
+    if (!e.residual || count <= 0) return;
+    if (e.out_f32) load8((const float *)e.residual + m * e.ld_r + n, count, residual);
+    else load8((const __bf16 *)e.residual + m * e.ld_r + n, count, residual);
 }
 __device__ __forceinline__ void finish_ahead8(const Epilogue &e, int m, int n, int count, float (&z)[8], const float (&bias)[8],
                                               const float (&residual)[8])
@@ -81,10 +83,11 @@ __device__ __forceinline__ void finish_ahead8(const Epilogue &e, int m, int n, i
         for (int i = 0; i < 8; ++i) z[i] += bias[i];
     }
     if (e.preact) store8(e.preact + m * e.ld_p + n, count, z);
-    if (e.act != 0) {
+    if (e.act != 0)
+        with_act(e.act, [&](auto a) {
 #pragma unroll
-        for (int i = 0; i < 8; ++i) z[i] = activate(z[i], e.act);
-    }
+            for (int i = 0; i < 8; ++i) z[i] = activate_as<decltype(a)::value>(z[i]);
+        });
     if (e.residual) {
 #pragma unroll
         for (int i = 0; i < 8; ++i) z[i] += residual[i];
@@ -712,26 +715,54 @@ template <int WT, bool GATED> struct Band {
         }
     }
 
-    // every check, eight columns to a lane
+    // every check, eight columns to a lane.  The residual of four rows is on its way before the first of them is stored: row after row,
+    // each waited for alone, a tile's edge took as long as its products (5000 x 2048 x 2048 with gelu and residual 96 us)
     __device__ __forceinline__ void checked(const Args &x, int m, int n)
+    {
+        const int lane = threadIdx.x & 63;
+        constexpr int LANES = COLS / 8, ROWS = 64 / LANES, AHEAD = ROWS > 8 ? 32 / ROWS : 4;
+        const int c = (lane % LANES) * 8, count = x.N - n - c;
+        if (count <= 0) return;
+        float bias[8], residual[AHEAD][8];
+        if constexpr (!GATED) bias8(x.e, n + c, count, bias);
+#pragma unroll 1
+        for (int r0 = lane / LANES; r0 < 32; r0 += AHEAD * ROWS) {
+            if constexpr (!GATED) {
+#pragma unroll
+                for (int k = 0; k < AHEAD; ++k) residual8(x.e, min(m + r0 + k * ROWS, x.M - 1), n + c, count, residual[k]);
+            }
+#pragma unroll
+            for (int k = 0; k < AHEAD; ++k) {
+                const int r = r0 + k * ROWS;
+                float z[8];
+                load8(turn + r * PITCH + at(c), 8, z);
+                if constexpr (GATED) {
+                    float u[8];
+                    load8(turn + r * PITCH + at(c) + 32, 8, u);
+                    if (m + r < x.M) finish_gated8(x.e, m + r, n + c, count, z, u);
+                } else if (m + r < x.M) {
+                    if (x.e.split_row != 0x7fffffff) finish_linear8(x.e, m + r, n + c, count, z);
+                    else finish_ahead8(x.e, m + r, n + c, count, z, bias, residual[k]);
+                }
+            }
+        }
+    }
+
+    // fp32 by pieces: sums that are not finite, computed again
+    __device__ __forceinline__ void mend(const Args &x, int m, int n)
     {
         const int lane = threadIdx.x & 63;
         constexpr int LANES = COLS / 8, ROWS = 64 / LANES;
         const int c = (lane % LANES) * 8, count = x.N - n - c;
-        if (count <= 0) return;
-#pragma unroll 2
-        for (int r = lane / LANES; r < 32; r += ROWS) {
-            if (m + r >= x.M) break;
-            float z[8];
-            load8(turn + r * PITCH + at(c), 8, z);
-            if (x.pieces.a[0] && !all_finite(z)) mend8(x.pieces, 0, m + r, n + c, count, z);
-            if constexpr (GATED) {
-                float u[8];
-                load8(turn + r * PITCH + at(c) + 32, 8, u);
-                if (x.pieces.a[0] && !all_finite(u)) mend8(x.pieces, 1, m + r, n + c, count, u);
-                finish_gated8(x.e, m + r, n + c, count, z, u);
-            } else {
-                finish_linear8(x.e, m + r, n + c, count, z);
+#pragma unroll 1
+        for (int r = lane / LANES; r < 32 && m + r < x.M && count > 0; r += ROWS) {
+#pragma unroll 1
+            for (int which = 0; which < (GATED ? 2 : 1); ++which) {
+                float *at8 = turn + r * PITCH + at(c) + which * 32, z[8];
+                load8(at8, 8, z);
+                if (all_finite(z)) continue;
+                mend8(x.pieces, which, m + r, n + c, count, z);
+                store8(at8, 8, z);
             }
         }
     }
@@ -928,14 +959,16 @@ __device__ __forceinline__ void tile_body(const Args &x, int wg, int nwg)
 
     // The sums, 32 rows of this wave at a time, are turned round in LDS (a region of its own for each wave), so that a
     // lane gets neighbouring columns and everything behind them is whole 16-byte accesses, whole lines by the wave.  A
-    // tile that lies inside the result goes without checks, its loads ahead of its stores.
+    // band that lies inside the result goes without checks, its loads ahead of its stores.
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
     Band<WT, GATED> band;
     band.turn = reinterpret_cast<float *>(lds) + wave * (32 * S::TURN_PITCH);
     const int wm = m0 + (wave >> 1) * WT, wn = n0 + (wave & 1) * (COLS / 2);
-    const bool own_rows = x.e.split_row == 0x7fffffff || m0 + S::T <= x.e.rows_each ||
-                          (m0 >= x.e.split_row && m0 - x.e.split_row + S::T <= x.e.rows_each);
-    const bool inside = m0 + S::T <= x.M && n0 + COLS <= x.N && own_rows;
+    // whether the 32 rows from m on lie inside, in this wave's columns
+    auto inside = [&](int m) {
+        return m + 32 <= x.M && wn + COLS / 2 <= x.N &&
+               (x.e.split_row == 0x7fffffff || m + 32 <= x.e.rows_each || (m >= x.e.split_row && m - x.e.split_row + 32 <= x.e.rows_each));
+    };
     auto turn_round = [&](auto band_tag) {
         constexpr int I = decltype(band_tag)::value;
         if constexpr (I < P::NB) {
@@ -951,10 +984,10 @@ __device__ __forceinline__ void tile_body(const Args &x, int wg, int nwg)
         }
     };
     if constexpr (TO == TO_LINEAR)
-        if (inside) band.fetch_residual(x.e, wm, wn);
+        if (inside(wm)) band.fetch_residual(x.e, wm, wn);
     // (a loop: unrolled, the code behind it would be there four times)
 #pragma unroll 1
-    for (int i = 0; i < P::NB; ++i) {
+    for (int i = 0; i < P::NB && wm + i * 32 < x.M; ++i) {
         if (i == 0) turn_round(std::integral_constant<int, 0>{});
         else if (i == 1) turn_round(std::integral_constant<int, 1>{});
         else if (i == 2) turn_round(std::integral_constant<int, 2>{});
@@ -962,8 +995,11 @@ __device__ __forceinline__ void tile_body(const Args &x, int wg, int nwg)
         pin();
         const int m = wm + i * 32;
         if constexpr (TO == TO_PARTS || TO == TO_GATED_PARTS) band.parts(x, split, m, wn);
-        else if (inside && (!x.pieces.a[0] || band.finite())) band.inside(x.e, m, wn, i + 1 < P::NB ? m + 32 : -1);
-        else band.checked(x, m, wn);
+        else {
+            if (x.pieces.a[0] && !band.finite()) band.mend(x, m, wn);
+            if (inside(m)) band.inside(x.e, m, wn, i + 1 < P::NB && inside(m + 32) ? m + 32 : -1);
+            else band.checked(x, m, wn);
+        }
         pin();
     }
 }
