@@ -204,3 +204,21 @@ def test_workspaces_full_of_nan_do_not_show():
             for x, y in zip(rcd.gated_linear_backward(dy, a, w, w, saved, workspace=ws[:-256]), rcd.gated_linear_backward(dy, a, w, w, saved)):
                 assert torch.equal(x, y) and torch.all(torch.isfinite(x))
             assert torch.all(ws[-256:] == 0xff)
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("over", [1, 31, 32, 33, 68, 129, 224, 255])
+def test_rows_of_a_tile_that_is_not_full_are_the_full_ones(dtype, over):
+    """A row's results do not depend on how many rows come after it in its tile: the same bits with `over` of a tile's rows as
+    with all of them, whether the bands of 32 rows that hold them are full or not, infinities among them."""
+    M, N, K, full = 4096 + over, 2056, 200, 4352
+    gen = torch.Generator(device="cuda").manual_seed(over)
+    a, w, w2 = normal(gen, full, K, dtype=dtype), normal(gen, N, K, dtype=dtype, scale=K ** -0.5), normal(gen, N, K, dtype=dtype, scale=K ** -0.5)
+    b, r = normal(gen, N, dtype=dtype), normal(gen, full, N, dtype=dtype)
+    a[4100, 7] = a[4350, 3] = float("inf")
+    for x, y in zip(rcd.linear(a[:M], w, b, act="gelu", residual=r[:M], want_preact=True),
+                    rcd.linear(a, w, b, act="gelu", residual=r, want_preact=True)):
+        assert torch.equal(torch.nan_to_num(x, 1e9, 2e9, -2e9), torch.nan_to_num(y[:M], 1e9, 2e9, -2e9))
+        assert torch.equal(torch.isfinite(x).all(1), torch.isfinite(a[:M].float()).all(1))
+    for x, y in zip(rcd.gated_linear(a[:M], w, w2, act="silu", want_saved=True), rcd.gated_linear(a, w, w2, act="silu", want_saved=True)):
+        assert torch.equal(torch.nan_to_num(x, 1e9, 2e9, -2e9), torch.nan_to_num(y[:M], 1e9, 2e9, -2e9))
