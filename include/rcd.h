@@ -334,7 +334,8 @@ void rcd_profile_read(double *out8_host);
  *     output's rows beyond its columns (a leading dimension larger than the columns) are left alone.
  *   - Zero rows (rows = 0, M = 0) are legal: nothing is read, gradients of weights come out as zero.  There are at most
  *     2^31 - 256 rows; a row's length d of the norm and the quantizer is 1 .. 2^30, the products' lengths N, K and F are
- *     1 .. 2^22.  Products of extents and leading dimensions may pass 2^31.
+ *     1 .. 2^22.  Products of extents and leading dimensions may pass 2^31.  A product of 2^24 tiles of 256 x 256 or more is
+ *     refused (RCD_ERR_UNSUPPORTED); no result that fits this device has them.
  *   - NaN and infinities travel as the formulas say, also in RCD_F32 products.
  */
 

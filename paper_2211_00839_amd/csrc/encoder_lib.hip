@@ -68,15 +68,22 @@ template <typename Go> void with_row_variant(int64_t d, Go go)
 }
 inline int rows_per_workgroup(int64_t d) { return d <= 1024 ? 4 : 1; }
 
-template <bool MX, bool NORM> int launch_norm(const NormArgs &a, int dt, hipStream_t stream)
+// (One launch unless there are 2^24 rows or more.)
+template <bool MX, bool NORM> int launch_norm(NormArgs a, int dt, hipStream_t stream)
 {
-    with_row_variant(a.d, [&](auto wpr, auto chunks) {
-        constexpr int W = decltype(wpr)::value, C = decltype(chunks)::value;
-        const dim3 grid((unsigned)((a.rows + RowOf<W>::ROWS - 1) / RowOf<W>::ROWS));
-        if (dt == RCD_F32) hipLaunchKernelGGL((k_norm<float, W, C, MX, NORM>), grid, dim3(NORM_THREADS), 0, stream, a);
-        else hipLaunchKernelGGL((k_norm<__bf16, W, C, MX, NORM>), grid, dim3(NORM_THREADS), 0, stream, a);
-    });
-    ENC_HIP_TRY(hipGetLastError());
+    static_assert(NORM_THREADS == 256, "the rule counts workgroups of 256");
+    const int64_t rows = a.rows;
+    for (int64_t done = 0; done < rows; done = a.rows) {
+        a.first = done;
+        a.rows = done + enc_rules::rows_of_launch(rows - done, rows_per_workgroup(a.d));
+        with_row_variant(a.d, [&](auto wpr, auto chunks) {
+            constexpr int W = decltype(wpr)::value, C = decltype(chunks)::value;
+            const dim3 grid((unsigned)((a.rows - a.first + RowOf<W>::ROWS - 1) / RowOf<W>::ROWS));
+            if (dt == RCD_F32) hipLaunchKernelGGL((k_norm<float, W, C, MX, NORM>), grid, dim3(NORM_THREADS), 0, stream, a);
+            else hipLaunchKernelGGL((k_norm<__bf16, W, C, MX, NORM>), grid, dim3(NORM_THREADS), 0, stream, a);
+        });
+        ENC_HIP_TRY(hipGetLastError());
+    }
     return RCD_OK;
 }
 
@@ -296,8 +303,8 @@ size_t parts_bytes(const Cut &c, int64_t M, int64_t N, bool gated)
     return c.splits > 1 ? up256((size_t)c.splits * M * parts_pitch(N, gated) * 4) : 0;
 }
 
-inline unsigned grid_of(const Cut &c) { return (unsigned)((enc_rules::workgroups_of(c) + 7) / 8 * 8); }
-inline bool launchable(const Cut &c) { return enc_rules::workgroups_of(c) <= 0x7ffffff0; }
+using enc_rules::launchable;
+inline unsigned grid_size(const Cut &c) { return (unsigned)enc_rules::grid_of(c); }
 
 void take_parts(tile::Args &x, bool gated, Pieces &room)
 {
@@ -397,7 +404,7 @@ int launch_planned(const Product &p, const Cut &c, const tile::Args &x, hipStrea
     ENC_TRY(with_tile_variant(c.wt, p.ka, p.kb, mx, to, [&](auto w, auto a, auto b, auto m, auto t) {
         constexpr int W = decltype(w)::value;
         constexpr bool X = decltype(m)::value;
-        hipLaunchKernelGGL((tile::k_tile<W, decltype(a)::value, decltype(b)::value, X, decltype(t)::value>), dim3(grid_of(c)),
+        hipLaunchKernelGGL((tile::k_tile<W, decltype(a)::value, decltype(b)::value, X, decltype(t)::value>), dim3(grid_size(c)),
                            dim3(tile::THREADS), (tile::Shape<W, X>::LDS_BYTES), stream, x);
         return (int)RCD_OK;
     }));
@@ -428,8 +435,8 @@ int launch_both(const Product *da, const Product *dw, const enc_rules::Both &cut
     if ((da && !launchable(cut.first)) || (dw && !launchable(cut.second))) return RCD_ERR_UNSUPPORTED;
     if (da && dw && cut.together) {
         const tile::Args x = plan_product(*da, cut.first, room), y = plan_product(*dw, cut.second, room);
-        const unsigned first = grid_of(cut.first);
-        hipLaunchKernelGGL(tile::k_tile_both, dim3(first + grid_of(cut.second)), dim3(tile::THREADS),
+        const unsigned first = grid_size(cut.first);
+        hipLaunchKernelGGL(tile::k_tile_both, dim3(first + grid_size(cut.second)), dim3(tile::THREADS),
                            (tile::Shape<64, false>::LDS_BYTES), stream, x, y, (int)first);
         return launch_join_both(x, y, cols, stream);
     }
@@ -506,7 +513,7 @@ direct::Args plan_direct(const DirectProduct &p, const Cut &c, Pieces &room)
 
 int launch_planned(const DirectProduct &p, const Cut &c, const direct::Args &x, hipStream_t stream)
 {
-    const dim3 grid(grid_of(c));
+    const dim3 grid(grid_size(c));
     constexpr int K = tile::K_RUNS, R = tile::ROWS_RUN;
     auto go = [&](auto wide) {
         constexpr bool W = decltype(wide)::value;
@@ -539,22 +546,14 @@ int launch_direct(const DirectProduct &p, Pieces &room, hipStream_t stream)
     return launch_planned(p, c, plan_direct(p, c, room), stream);
 }
 
-// The direct kernel's two products of a backward call always run side by side, each cut for half of the device.
-enc_rules::Both direct_both(int64_t M, int64_t N, int64_t K, int pairs)
-{
-    using namespace enc_rules;
-    return Both{true, direct_cut_of(M, K, ceil_div(N, DIRECT_STAGE) * pairs, false, UNITS / 2),
-                direct_cut_of(pairs == 2 ? 2 * up64(N) : N, K, ceil_div(M, DIRECT_STAGE), false, UNITS / 2)};
-}
-
 int launch_both(const DirectProduct *da, const DirectProduct *dw, const enc_rules::Both &cut, Pieces &room, const tile::Columns &cols,
                 hipStream_t stream)
 {
     if ((da && !launchable(cut.first)) || (dw && !launchable(cut.second))) return RCD_ERR_UNSUPPORTED;
     if (da && dw) {
         const direct::Args x = plan_direct(*da, cut.first, room), y = plan_direct(*dw, cut.second, room);
-        const unsigned first = grid_of(cut.first);
-        const dim3 grid(first + grid_of(cut.second));
+        const unsigned first = grid_size(cut.first);
+        const dim3 grid(first + grid_size(cut.second));
         if (is_wide(*da) && is_wide(*dw)) hipLaunchKernelGGL(direct::k_direct_both<true>, grid, dim3(256), 0, stream, x, y, (int)first);
         else hipLaunchKernelGGL(direct::k_direct_both<false>, grid, dim3(256), 0, stream, x, y, (int)first);
         return launch_join_both(x.t, y.t, cols, stream);
@@ -570,7 +569,7 @@ size_t backward_parts(int64_t M, int64_t N, int64_t K, int dt, int pairs)
 {
     const int64_t rows = pairs == 2 ? 2 * up64(N) : N;
     size_t need = both_parts(both_of(M, N, K, dt, pairs), M, K, rows, K);
-    if (dt == RCD_F32) need = std::max(need, both_parts(direct_both(M, N, K, pairs), M, K, rows, K));
+    if (dt == RCD_F32) need = std::max(need, both_parts(enc_rules::direct_both(M, N, K, pairs == 2), M, K, rows, K));
     return need;
 }
 
@@ -956,7 +955,7 @@ int rcd_linear_backward(const void *dY_dev, int64_t ld_dy, const void *A_dev, in
         q.b[0] = (const float *)A_dev;
         q.b_pitch[0] = ld_a;
         q.e = one_output(dW_dev, ld_dw, dt, RCD_ACT_NONE);
-        return launch_both(dA_dev ? &p : nullptr, dW_dev ? &q : nullptr, direct_both(M, N, K, 1), room, cols, stream);
+        return launch_both(dA_dev ? &p : nullptr, dW_dev ? &q : nullptr, enc_rules::direct_both(M, N, K, false), room, cols, stream);
     }
     Product p{}, q{};
     p.dt = q.dt = dt;
@@ -1120,7 +1119,7 @@ int rcd_gated_linear_backward(const void *dH_dev, int64_t ld_dh, const void *A_d
         q.b_pitch[0] = ld_a;
         q.a_cols = pitch;
         q.e = both;
-        return launch_both(dA_dev ? &p : nullptr, dWg_dev ? &q : nullptr, direct_both(M, F, K, 2), room, tile::Columns{}, stream);
+        return launch_both(dA_dev ? &p : nullptr, dWg_dev ? &q : nullptr, enc_rules::direct_both(M, F, K, true), room, tile::Columns{}, stream);
     }
     Laid d;
     d.p = (const unsigned char *)dgu;

@@ -16,6 +16,16 @@ constexpr int64_t UNITS = 256;      // compute units of the device
 
 inline int64_t ceil_div(int64_t a, int64_t b) { return (a + b - 1) / b; }
 
+// What one launch may hold: the runtime takes fewer than 2^32 threads, and all of these kernels' large grids are of
+// workgroups of 256.
+constexpr int64_t MOST_WORKGROUPS = (((int64_t)1 << 32) - 1) / 256;
+// Of `left` rows, `per` to a workgroup, those that go into the next launch.
+inline int64_t rows_of_launch(int64_t left, int per) { return std::min(left, MOST_WORKGROUPS * per); }
+
+inline int64_t workgroups_of(const Cut &c) { return c.tiles_m * c.tiles_n * c.splits; }
+inline int64_t grid_of(const Cut &c) { return ceil_div(workgroups_of(c), 8) * 8; }      // (the same number for each of the 8 XCDs)
+inline bool launchable(const Cut &c) { return grid_of(c) <= MOST_WORKGROUPS; }
+
 // What a cut takes, in microseconds, from what was measured on full and on part-full devices (bf16, k contiguous):
 //   a stage of a 256 x 256 tile      1.0 with few workgroups, 1.5 with one on every unit (the clock falls with the load)
 //   a stage of a 128 x 128 tile      0.55 alone on its unit, 0.88 with a second one beside it
@@ -56,7 +66,7 @@ inline Cut cut_of(int64_t M, int64_t N, int64_t stages, bool gated, int64_t unit
             if (splits > 1 && (splits * 4 > stages || c.tiles_m * c.tiles_n * splits > 2 * units)) break;
             c.splits = splits;
             const double t = time_of(c, M, N, stages, gated, units);
-            if (best.splits == 0 || t < least) {
+            if (best.splits == 0 || (t < least && launchable(c))) {      // (large tiles come first: if they are too many, all are)
                 best = c;
                 least = t;
             }
@@ -64,8 +74,6 @@ inline Cut cut_of(int64_t M, int64_t N, int64_t stages, bool gated, int64_t unit
     }
     return best;
 }
-
-inline int64_t workgroups_of(const Cut &c) { return c.tiles_m * c.tiles_n * c.splits; }
 
 // A backward call's two products, side by side in one launch where each is small enough to leave room for the other: both in
 // small tiles, all workgroups on the device at once.  The whole backward call in us, side by side / one after the other, bf16:
@@ -142,11 +150,21 @@ inline double pieces_product_time(int64_t M, int64_t N, int64_t K, int pairs, bo
 // Whole calls.
 inline bool direct_forward(int64_t M, int64_t N, int64_t K, bool gated)
 {
+    if (!launchable(direct_cut_of(M, N, ceil_div(K, DIRECT_STAGE), gated))) return false;
     return direct_time(M, N, K, 1, gated) < pieces_product_time(M, N, K, 1, gated) + pieces_time((M + N * (gated ? 2 : 1)) * K);
+}
+// The direct kernel's two products of a backward call always run side by side, each cut for half of the device.
+inline Both direct_both(int64_t M, int64_t N, int64_t K, bool gated)
+{
+    const int w = gated ? 2 : 1;
+    return Both{true, direct_cut_of(M, K, ceil_div(N, DIRECT_STAGE) * w, false, UNITS / 2),
+                direct_cut_of(gated ? 2 * ceil_div(N, 64) * 64 : N, K, ceil_div(M, DIRECT_STAGE), false, UNITS / 2)};
 }
 inline bool direct_backward(int64_t M, int64_t N, int64_t K, bool gated)
 {
     const int w = gated ? 2 : 1;
+    const Both cut = direct_both(M, N, K, gated);
+    if (grid_of(cut.first) + grid_of(cut.second) > MOST_WORKGROUPS) return false;
     return direct_time(M, K, N, w, false) + direct_time(w * N, K, M, 1, false) <
            pieces_product_time(M, K, N, w, false) + pieces_product_time(w * N, K, M, 1, false) + pieces_time((M + N * w) * K);
 }

@@ -40,7 +40,7 @@ struct NormArgs {
     uint8_t *scale;
     float *rstd;                    // nullable
     long long ld_x, ld_r, ld_s, ld_y, ld_scale;
-    long long rows;
+    long long first, rows;          // this launch's rows are first .. rows - 1
     int d;
     float eps;
 };
@@ -82,7 +82,7 @@ k_norm(const NormArgs a)
 {
     __shared__ float scratch[4];
     using R = RowOf<WPR>;
-    const size_t row = (size_t)blockIdx.x * R::ROWS + R::sub();
+    const size_t row = (size_t)a.first + (size_t)blockIdx.x * R::ROWS + R::sub();
     if (WPR == 1 && row >= (size_t)a.rows) return;        // (a whole wave)
     const T *x = (const T *)a.x + row * a.ld_x;
     const T *r = a.r ? (const T *)a.r + row * a.ld_r : nullptr;
