@@ -320,15 +320,18 @@ void rcd_profile_read(double *out8_host);
  *
  * Common to all of them
  *   - dt is RCD_F32 or RCD_BF16 for every matrix of a call that is not said to be something else.  Sums, statistics and
- *     products are accumulated in fp32 (or more) whatever dt is, and every output is rounded once, when it is stored.
+ *     products are accumulated in fp32 (or more) whatever dt is, with one exception (under RCD_MXFP8), and every output is
+ *     rounded once, when it is stored.
  *     Products of RCD_F32 operands are exact to fp32 (a factor goes to the matrix cores as it is, or as three bf16 pieces
  *     that add up to it).
  *   - RCD_MXFP8 (where an entry point lists it): elements are e4m3 bytes, and each block of 32 consecutive elements of a
  *     row (the last one may be shorter) shares a scale 2^(s - 127), s one byte; s = 255 means NaN.  Element i of a row
  *     stands for e4m3(byte i) * 2^(s[i / 32] - 127).  Scales are a byte matrix of their own, rows x ceil(d / 32), with a
- *     leading dimension in bytes.  Their products are exact to fp32 for K < 2048 and for few rows; longer ones go to the
- *     scaled matrix instruction, which cuts off what lies some 2^-11 below the largest of the 64 products it adds: no
- *     more than an fp32 sum of K terms may be off, (K + 8) 2^-23 of the sum of the products' sizes.
+ *     leading dimension in bytes.  Products whose sums leave the call in fp32 (out_dt RCD_F32, or z, or g and u asked for) and
+ *     those of few rows or of K < 2048 are accumulated in fp32.  The exception: with nothing but a bf16 result, products of K >= 2048
+ *     go to the scaled matrix instruction, which cuts off, towards zero, what lies some 2^-11 below the largest of
+ *     the 64 products that it adds: at most 2^-12.3 of the sum of the products' sizes, 1.5e-5 of the result on random operands (its
+ *     rounding to bf16: 1.7e-3).  So the same row may come out a last bit apart in calls of few and of many rows.
  *   - Asynchronous on `stream`; nothing is allocated, no host wait; calls can be captured into a graph.
  *   - Outputs may not overlap inputs, workspace or each other, except where an entry point says so.  Elements of an
  *     output's rows beyond its columns (a leading dimension larger than the columns) are left alone.
