@@ -119,9 +119,13 @@ template <typename Go> int with_tile_variant(int wt, int ka, int kb, bool mx, in
         constexpr int B = decltype(b)::value;
         if (to == tile::TO_LINEAR) return go(w, a, b, x, integral_constant<int, tile::TO_LINEAR>{});
         if (to == tile::TO_PARTS) return go(w, a, b, x, integral_constant<int, tile::TO_PARTS>{});
+        if constexpr (!decltype(x)::value)
+            if (to == tile::TO_LINEAR_PIECES) return go(w, a, b, x, integral_constant<int, tile::TO_LINEAR_PIECES>{});
         if constexpr (A == tile::K_RUNS && B == tile::K_RUNS) {
             if (to == tile::TO_GATED) return go(w, a, b, x, integral_constant<int, tile::TO_GATED>{});
             if (to == tile::TO_GATED_PARTS) return go(w, a, b, x, integral_constant<int, tile::TO_GATED_PARTS>{});
+            if constexpr (!decltype(x)::value)
+                if (to == tile::TO_GATED_PIECES) return go(w, a, b, x, integral_constant<int, tile::TO_GATED_PIECES>{});
         }
         return (int)RCD_ERR_UNSUPPORTED;
     };
@@ -145,18 +149,18 @@ int set_up()
     if (!g_ready[dev]) {
         for (int wt : {64, 128})
             for (int order = 0; order < 4; ++order)
-                for (int to : {tile::TO_LINEAR, tile::TO_GATED, tile::TO_PARTS, tile::TO_GATED_PARTS}) {
+                for (int to : {tile::TO_LINEAR, tile::TO_GATED, tile::TO_PARTS, tile::TO_GATED_PARTS, tile::TO_LINEAR_PIECES, tile::TO_GATED_PIECES}) {
                     const bool mx = order == 3;
                     const int ka = order == 2 ? tile::ROWS_RUN : tile::K_RUNS, kb = order == 1 || order == 2 ? tile::ROWS_RUN : tile::K_RUNS;
-                    if (kb == tile::ROWS_RUN && (to == tile::TO_GATED || to == tile::TO_GATED_PARTS)) continue;
+                    if ((kb == tile::ROWS_RUN && tile::is_gated(to)) || (mx && (to == tile::TO_LINEAR_PIECES || to == tile::TO_GATED_PIECES))) continue;
                     ENC_TRY(with_tile_variant(wt, ka, kb, mx, to, [](auto w, auto a, auto b, auto x, auto t) {
                         ENC_HIP_TRY((raise_lds_limit<decltype(w)::value, decltype(a)::value, decltype(b)::value, decltype(x)::value,
                                                      decltype(t)::value>()));
                         return (int)RCD_OK;
                     }));
                 }
-        ENC_HIP_TRY(hipFuncSetAttribute(reinterpret_cast<const void *>(&tile::k_tile_both), hipFuncAttributeMaxDynamicSharedMemorySize,
-                                        (tile::Shape<64, false>::LDS_BYTES)));
+        for (const void *both : {reinterpret_cast<const void *>(&tile::k_tile_both<false>), reinterpret_cast<const void *>(&tile::k_tile_both<true>)})
+            ENC_HIP_TRY(hipFuncSetAttribute(both, hipFuncAttributeMaxDynamicSharedMemorySize, (tile::Shape<64, false>::LDS_BYTES)));
         g_ready[dev] = true;
     }
     return RCD_OK;
@@ -330,13 +334,21 @@ int sum_columns(const tile::Columns &c, hipStream_t stream)
     return RCD_OK;
 }
 
+// Workgroups that join a product's parts.
+int64_t join_groups(const tile::Args &x)
+{
+    if (x.splits == 1) return 1;
+    const int64_t M = x.M, N = x.N;
+    const int64_t groups = x.pieces.a[0] ? (M + 31) / 32 * ((N + 63) / 64) : (M * ((N + 7) / 8) + 255) / 256;
+    return std::min<int64_t>(groups, 8192);
+}
+
 int launch_join_both(const tile::Args &x, const tile::Args &y, const tile::Columns &c, hipStream_t stream)
 {
     if (x.splits > 1 || y.splits > 1 || c.part) {
-        int64_t items = (int64_t)(c.d + 15) / 16 * 256;
-        if (x.splits > 1) items = std::max(items, (int64_t)x.M * ((x.N + 7) / 8));
-        if (y.splits > 1) items = std::max(items, (int64_t)y.M * ((y.N + 7) / 8));
-        hipLaunchKernelGGL(tile::k_join_both, dim3(copy_grid(items), 3), dim3(256), 0, stream, x, y, c);
+        const dim3 grid((unsigned)std::max({join_groups(x), join_groups(y), std::min<int64_t>((c.d + 15) / 16, 8192)}), 3);
+        if (x.pieces.a[0]) hipLaunchKernelGGL(tile::k_join_both<true>, grid, dim3(256), 0, stream, x, y, c);
+        else hipLaunchKernelGGL(tile::k_join_both<false>, grid, dim3(256), 0, stream, x, y, c);
     }
     ENC_HIP_TRY(hipGetLastError());
     return RCD_OK;
@@ -344,9 +356,10 @@ int launch_join_both(const tile::Args &x, const tile::Args &y, const tile::Colum
 
 void launch_join(const tile::Args &x, bool gated, hipStream_t stream)
 {
-    const dim3 grid(copy_grid((int64_t)x.M * ((x.N + 7) / 8)));
-    if (gated) hipLaunchKernelGGL(tile::k_join<true>, grid, dim3(256), 0, stream, x);
-    else hipLaunchKernelGGL(tile::k_join<false>, grid, dim3(256), 0, stream, x);
+    const dim3 grid((unsigned)join_groups(x));
+    auto launch = [&](auto kernel) { hipLaunchKernelGGL(kernel, grid, dim3(256), 0, stream, x); };
+    if (x.pieces.a[0]) gated ? launch(tile::k_join<true, true>) : launch(tile::k_join<false, true>);
+    else gated ? launch(tile::k_join<true, false>) : launch(tile::k_join<false, false>);
 }
 
 // The kernel's arguments; parts are taken from `room`.
@@ -405,7 +418,10 @@ tile::Args plan_product(const Product &p, const Cut &c, Pieces &room)
 int launch_planned(const Product &p, const Cut &c, const tile::Args &x, hipStream_t stream)
 {
     const bool mx = p.dt == RCD_MXFP8;
-    const int to = c.splits > 1 ? (p.gated ? tile::TO_GATED_PARTS : tile::TO_PARTS) : p.gated ? tile::TO_GATED : tile::TO_LINEAR;
+    const bool pieces = p.dt == RCD_F32;
+    const int to = c.splits > 1 ? (p.gated ? tile::TO_GATED_PARTS : tile::TO_PARTS)
+                   : p.gated    ? (pieces ? tile::TO_GATED_PIECES : tile::TO_GATED)
+                                : (pieces ? tile::TO_LINEAR_PIECES : tile::TO_LINEAR);
     ENC_TRY(with_tile_variant(c.wt, p.ka, p.kb, mx, to, [&](auto w, auto a, auto b, auto m, auto t) {
         constexpr int W = decltype(w)::value;
         constexpr bool X = decltype(m)::value;
@@ -441,8 +457,12 @@ int launch_both(const Product *da, const Product *dw, const enc_rules::Both &cut
     if (da && dw && cut.together) {
         const tile::Args x = plan_product(*da, cut.first, room), y = plan_product(*dw, cut.second, room);
         const unsigned first = grid_size(cut.first);
-        hipLaunchKernelGGL(tile::k_tile_both, dim3(first + grid_size(cut.second)), dim3(tile::THREADS),
-                           (tile::Shape<64, false>::LDS_BYTES), stream, x, y, (int)first);
+        auto launch = [&](auto kernel) {
+            hipLaunchKernelGGL(kernel, dim3(first + grid_size(cut.second)), dim3(tile::THREADS), (tile::Shape<64, false>::LDS_BYTES), stream, x, y,
+                               (int)first);
+        };
+        if (da->dt == RCD_F32) launch(tile::k_tile_both<true>);
+        else launch(tile::k_tile_both<false>);
         return launch_join_both(x, y, cols, stream);
     }
     if (cols.part) ENC_TRY(sum_columns(cols, stream));

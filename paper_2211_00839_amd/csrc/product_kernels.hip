@@ -138,41 +138,76 @@ struct Pieces3 {
     int pairs, K;
 };
 
-__device__ __forceinline__ float whole(const __bf16 *p, long long plane)
+// Factors k + 4 half .. + 3 of the row that lies `lane` elements from `row`, `step` apart; from K on zeros (rows that lie in a run are
+// packed: zeros up to a multiple of 64).  row, k: the same in every lane.
+__device__ __forceinline__ void whole4(const __bf16 *row, unsigned lane, long long plane, long long step, int k, int half, int K, float (&v)[4])
 {
-    return ((float)p[2 * plane] + (float)p[plane]) + (float)p[0];
-}
-
-__device__ __forceinline__ float plain_dot(const Pieces3 &x, int which, int m, int n)
-{
-    float s = 0.f;
-    for (int pair = 0; pair < x.pairs; ++pair) {
-        const __bf16 *a = x.a[pair] + m * x.a_row, *b = (which ? x.b[1] : x.b[pair]) + n * x.b_row;
-        for (int k = 0; k < x.K; ++k) s = fmaf(whole(a + k * x.a_k, x.a_plane), whole(b + k * x.b_k, x.b_plane), s);
-    }
-    return s;
-}
-
-__device__ __forceinline__ void mend8(const Pieces3 &x, int which, int m, int n, int count, float (&z)[8])
-{
-#pragma unroll 1
-    for (int i = 0; i < 8; ++i) {
-        float v = 0.f;
+    typedef __bf16 bf16x4 __attribute__((ext_vector_type(4)));
+    if (step == 1) {
+        const __bf16 *p = row + k;
+        const unsigned at = lane + half * 4;
+        const bf16x4 a = *reinterpret_cast<const bf16x4 *>(p + at), b = *reinterpret_cast<const bf16x4 *>(p + plane + at),
+                     c = *reinterpret_cast<const bf16x4 *>(p + 2 * plane + at);
 #pragma unroll
-        for (int j = 0; j < 8; ++j) v = i == j ? z[j] : v;
-        if (i < count && !(fabsf(v) <= 3.402823466e38f)) {
-            v = plain_dot(x, which, m, n + i);
+        for (int e = 0; e < 4; ++e) v[e] = ((float)c[e] + (float)b[e]) + (float)a[e];
+    } else {
 #pragma unroll
-            for (int j = 0; j < 8; ++j) z[j] = i == j ? v : z[j];
+        for (int e = 0; e < 4; ++e) {
+            const int first = min(k + e, K - 1);
+            const __bf16 *p = row + first * step;
+            const unsigned at = lane + (unsigned)(min(k + e + half * 4, K - 1) - first) * (unsigned)step;
+            const float f = ((float)(p + 2 * plane)[at] + (float)(p + plane)[at]) + (float)p[at];
+            v[e] = k + e + half * 4 < K ? f : 0.f;
         }
     }
 }
-__device__ __forceinline__ bool all_finite(const float (&z)[8])
+
+__device__ __forceinline__ bool is_finite(float v) { return fabsf(v) <= 3.402823466e38f; }
+
+// 32 x 32 sums of a wave, in LDS with rows `pitch` floats apart: those that are not finite (of the first `rows` rows and `cols` columns) are
+// computed again, from whole numbers on the fp32 matrix instruction.  m0, n0: the block's place in the product.  Ends as soon as all of them are NaN,
+// which no further term changes.  Every lane has to come along.  Bound by that instruction and by loads that nothing hides: a call whose every sum
+// is infinite takes up to 14 times what a finite one does (4104 x 2056 x 1040 2.2 ms against 0.16, its gradients 2.5 against 0.29, all NaN 0.3).
+__device__ __forceinline__ void mend_block(const Pieces3 &x, int which, int m0, int n0, int rows, int cols, float *block, int pitch)
 {
-    float m = 0.f;
+    const int lane = threadIdx.x & 63, half = lane >> 5, r = lane & 31;
+    float *mine = block + r * pitch + half * 4;         // sum 4 q + e lies at 8 q + e
+    unsigned wanted = 0;
 #pragma unroll
-    for (int i = 0; i < 8; ++i) m = fmaf(z[i], 0.f, m);
-    return m == 0.f;
+    for (int i = 0; i < 16; ++i) {
+        const int c = (i >> 2) * 8 + (i & 3);
+        if (r < rows && half * 4 + c < cols && !is_finite(mine[c])) wanted |= 1u << i;
+    }
+    if (!__any(wanted != 0)) return;
+    m0 = __builtin_amdgcn_readfirstlane(m0);
+    n0 = __builtin_amdgcn_readfirstlane(n0);
+    const unsigned a_lane = (unsigned)min(r, rows - 1) * (unsigned)x.a_row, b_lane = (unsigned)min(r, cols - 1) * (unsigned)x.b_row;
+    f32x16 acc;
+#pragma unroll
+    for (int i = 0; i < 16; ++i) acc[i] = 0.f;
+    bool open = true;
+    for (int pair = 0; pair < x.pairs && open; ++pair) {
+        const __bf16 *a = x.a[pair] + m0 * x.a_row, *b = (which ? x.b[1] : x.b[pair]) + n0 * x.b_row;
+#pragma unroll 1
+        for (int k0 = 0; k0 < x.K && open; k0 += 64) {
+            const int end = min(x.K, k0 + 64);
+#pragma unroll 1
+            for (int k = k0; k < end; k += 8) {
+                float u[4], v[4];
+                whole4(a, a_lane, x.a_plane, x.a_k, k, half, x.K, u);
+                whole4(b, b_lane, x.b_plane, x.b_k, k, half, x.K, v);
+#pragma unroll
+                for (int e = 0; e < 4; ++e) acc = __builtin_amdgcn_mfma_f32_32x32x2f32(v[e], u[e], acc, 0, 0, 0);
+            }
+            bool mine_open = false;
+#pragma unroll
+            for (int i = 0; i < 16; ++i) mine_open |= ((wanted >> i) & 1) != 0 && acc[i] == acc[i];
+            open = __any(mine_open);
+        }
+    }
+#pragma unroll
+    for (int i = 0; i < 16; ++i)
+        if ((wanted >> i) & 1) mine[(i >> 2) * 8 + (i & 3)] = acc[i];
 }
 
 // ---------------------------------------------------------------------------------------------------------------------------
@@ -196,7 +231,10 @@ constexpr int THREADS = 256;
 constexpr int LINE = 128;
 
 enum { K_RUNS = 0, ROWS_RUN = 1 };      // which of an operand's extents is contiguous
-enum { TO_LINEAR = 0, TO_GATED = 1, TO_PARTS = 2, TO_GATED_PARTS = 3 };
+// What a tile's sums become.  _PIECES: of fp32 by pieces, whose sums that are not finite are looked at again.
+enum { TO_LINEAR = 0, TO_GATED = 1, TO_PARTS = 2, TO_GATED_PARTS = 3, TO_LINEAR_PIECES = 4, TO_GATED_PIECES = 5 };
+constexpr bool is_gated(int to) { return to == TO_GATED || to == TO_GATED_PARTS || to == TO_GATED_PIECES; }
+constexpr bool is_parts(int to) { return to == TO_PARTS || to == TO_GATED_PARTS; }
 
 template <int WT, bool MX> struct Shape {
     static constexpr int T = 2 * WT, NB = WT / 32;
@@ -752,19 +790,10 @@ template <int WT, bool GATED> struct Band {
     // fp32 by pieces: sums that are not finite, computed again
     __device__ __forceinline__ void mend(const Args &x, int m, int n)
     {
-        const int lane = threadIdx.x & 63;
-        constexpr int LANES = COLS / 8, ROWS = 64 / LANES;
-        const int c = (lane % LANES) * 8, count = x.N - n - c;
 #pragma unroll 1
-        for (int r = lane / LANES; r < 32 && m + r < x.M && count > 0; r += ROWS) {
-#pragma unroll 1
-            for (int which = 0; which < (GATED ? 2 : 1); ++which) {
-                float *at8 = turn + r * PITCH + at(c) + which * 32, z[8];
-                load8(at8, 8, z);
-                if (all_finite(z)) continue;
-                mend8(x.pieces, which, m + r, n + c, count, z);
-                store8(at8, 8, z);
-            }
+        for (int j = 0; j < WT / 32; ++j) {
+            const int at = n + (GATED ? j >> 1 : j) * 32;
+            if (at < x.N) mend_block(x.pieces, GATED ? j & 1 : 0, m, at, x.M - m, x.N - at, turn + j * 32, PITCH);
         }
     }
 
@@ -944,7 +973,7 @@ template <int WT, bool GATED> struct Band {
 template <int WT, int KA, int KB, bool MX, int TO>
 __device__ __forceinline__ void tile_body(const Args &x, int wg, int nwg)
 {
-    constexpr bool GATED = TO == TO_GATED || TO == TO_GATED_PARTS;
+    constexpr bool GATED = is_gated(TO);
     using P = Pipe<WT, KA, KB, MX, GATED>;
     using S = typename P::S;
     extern __shared__ __attribute__((aligned(16))) unsigned char lds[];
@@ -984,7 +1013,7 @@ __device__ __forceinline__ void tile_body(const Args &x, int wg, int nwg)
                 }
         }
     };
-    if constexpr (TO == TO_LINEAR)
+    if constexpr (!GATED && !is_parts(TO))
         if (inside(wm)) band.fetch_residual(x.e, wm, wn);
     // (a loop: unrolled, the code behind it would be there four times)
 #pragma unroll 1
@@ -995,9 +1024,10 @@ __device__ __forceinline__ void tile_body(const Args &x, int wg, int nwg)
         else turn_round(std::integral_constant<int, 3>{});
         pin();
         const int m = wm + i * 32;
-        if constexpr (TO == TO_PARTS || TO == TO_GATED_PARTS) band.parts(x, split, m, wn);
+        if constexpr (is_parts(TO)) band.parts(x, split, m, wn);
         else {
-            if (x.pieces.a[0] && !band.finite()) band.mend(x, m, wn);
+            if constexpr (TO == TO_LINEAR_PIECES || TO == TO_GATED_PIECES)
+                if (!band.finite()) band.mend(x, m, wn);
             if (inside(m)) band.inside(x.e, m, wn, i + 1 < P::NB && inside(m + 32) ? m + 32 : -1);
             else band.checked(x, m, wn);
         }
@@ -1019,56 +1049,107 @@ k_tile(const Args x)
 
 // A backward call's two products side by side: x's workgroups are the first `first` (a multiple of 8) of the launch.  Neither fills the
 // device, and what is left is starts and ends: 1000 x 1024 x 1024 bf16 21.8 us the call, 31.6 one after the other.
+template <bool PIECES>
 __global__ void __launch_bounds__(THREADS, 2)
 k_tile_both(const Args x, const Args y, int first)
 {
+    constexpr int WHOLE = PIECES ? TO_LINEAR_PIECES : TO_LINEAR;
     const int wg = (int)blockIdx.x;
     if (wg < first) {
         if (x.splits > 1) tile_body<64, K_RUNS, ROWS_RUN, false, TO_PARTS>(x, wg, first);
-        else tile_body<64, K_RUNS, ROWS_RUN, false, TO_LINEAR>(x, wg, first);
+        else tile_body<64, K_RUNS, ROWS_RUN, false, WHOLE>(x, wg, first);
     } else {
         if (y.splits > 1) tile_body<64, ROWS_RUN, ROWS_RUN, false, TO_PARTS>(y, wg - first, (int)gridDim.x - first);
-        else tile_body<64, ROWS_RUN, ROWS_RUN, false, TO_LINEAR>(y, wg - first, (int)gridDim.x - first);
+        else tile_body<64, ROWS_RUN, ROWS_RUN, false, WHOLE>(y, wg - first, (int)gridDim.x - first);
     }
 }
 
 // The parts of a product whose k was split among workgroups, in order (the sum's bits are the same from run to run), and what
 // becomes of their sum.  Bound by memory: four parts of 2048 x 2048 13.4 us (75 MB, 5.6 TB/s).
+template <bool GATED> __device__ __forceinline__ void add_parts(const Args &x, int m, int n, float (&z)[8], float (&u)[8])
+{
+    const long long stride = (long long)x.M * x.parts_pitch;
+    const float *p = x.parts + m * x.parts_pitch + n;
+    float v[8];
+    load8(p, 8, z);
+    if constexpr (GATED) load8(p + x.parts_half, 8, u);
+    for (int s = 1; s < x.splits; ++s) {
+        load8(p + s * stride, 8, v);
+#pragma unroll
+        for (int i = 0; i < 8; ++i) z[i] += v[i];
+        if constexpr (GATED) {
+            load8(p + s * stride + x.parts_half, 8, v);
+#pragma unroll
+            for (int i = 0; i < 8; ++i) u[i] += v[i];
+        }
+    }
+}
+
 template <bool GATED> __device__ __forceinline__ void join(const Args &x)
 {
     const int groups = (x.N + 7) / 8;
-    const long long all = (long long)x.M * groups, stride = (long long)x.M * x.parts_pitch;
+    const long long all = (long long)x.M * groups;
     for (long long t = (long long)blockIdx.x * 256 + threadIdx.x; t < all; t += (long long)gridDim.x * 256) {
         const int m = (int)(t / groups), n = (int)(t % groups) * 8, count = x.N - n;
-        const float *p = x.parts + m * x.parts_pitch + n;
-        float z[8], u[8], v[8];
-        load8(p, 8, z);
-        if constexpr (GATED) load8(p + x.parts_half, 8, u);
-        for (int s = 1; s < x.splits; ++s) {
-            load8(p + s * stride, 8, v);
-#pragma unroll
-            for (int i = 0; i < 8; ++i) z[i] += v[i];
-            if constexpr (GATED) {
-                load8(p + s * stride + x.parts_half, 8, v);
-#pragma unroll
-                for (int i = 0; i < 8; ++i) u[i] += v[i];
-            }
-        }
-        if (x.pieces.a[0]) {
-            if (!all_finite(z)) mend8(x.pieces, 0, m, n, count, z);
-            if constexpr (GATED)
-                if (!all_finite(u)) mend8(x.pieces, 1, m, n, count, u);
-        }
+        float z[8], u[8];
+        add_parts<GATED>(x, m, n, z, u);
         if constexpr (GATED) finish_gated8(x.e, m, n, count, z, u);
         else finish_linear8(x.e, m, n, count, z);
     }
 }
 
-template <bool GATED>
+// fp32 by pieces: a workgroup to 32 rows of 64 columns, of which the sums that are not finite are computed again in LDS.
+constexpr int JOIN_PITCH = 68;
+constexpr int JOIN_LDS = 32 * JOIN_PITCH;       // floats
+template <bool GATED> __device__ __forceinline__ void join_pieces(const Args &x, float *lds)
+{
+    const int across = (x.N + 63) / 64, r = threadIdx.x >> 3, c = (threadIdx.x & 7) * 8;
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const long long all = (long long)((x.M + 31) / 32) * across;
+    for (long long t = blockIdx.x; t < all; t += gridDim.x) {
+        const int m0 = (int)(t / across) * 32, n0 = (int)(t % across) * 64, count = x.N - n0 - c;
+        const bool there = m0 + r < x.M && count > 0;
+        float z[8], u[8];
+        bool fine = true;
+        if (there) {
+            add_parts<GATED>(x, m0 + r, n0 + c, z, u);
+#pragma unroll
+            for (int e = 0; e < 8; ++e) {
+                fine = fine && (e >= count || is_finite(z[e]));
+                if constexpr (GATED) fine = fine && (e >= count || is_finite(u[e]));
+            }
+        }
+        if (__syncthreads_or(!fine)) {
+            auto mend = [&](int which, float (&v)[8]) {
+                store8(lds + r * JOIN_PITCH + c, 8, v);
+                __syncthreads();
+                if (wave < 2 && n0 + wave * 32 < x.N)
+                    mend_block(x.pieces, which, m0, n0 + wave * 32, x.M - m0, x.N - n0 - wave * 32, lds + wave * 32, JOIN_PITCH);
+                __syncthreads();
+                load8(lds + r * JOIN_PITCH + c, 8, v);
+                __syncthreads();
+            };
+            mend(0, z);
+            if constexpr (GATED) mend(1, u);
+        }
+        if (there) {
+            if constexpr (GATED) finish_gated8(x.e, m0 + r, n0 + c, count, z, u);
+            else finish_linear8(x.e, m0 + r, n0 + c, count, z);
+        }
+    }
+}
+
+template <bool GATED, bool PIECES> __device__ __forceinline__ void join_parts(const Args &x, float *lds)
+{
+    if constexpr (PIECES) join_pieces<GATED>(x, lds);
+    else join<GATED>(x);
+}
+template <bool GATED, bool PIECES>
 __global__ void __launch_bounds__(256)
 k_join(const Args x)
 {
-    join<GATED>(x);
+    __shared__ __attribute__((aligned(16))) float lds[PIECES ? JOIN_LDS : 1];
+    join_parts<GATED, PIECES>(x, lds);
 }
 
 // What a backward call's two products leave to be joined, and the bias's column sums.  grid.y = 3.
@@ -1079,14 +1160,16 @@ struct Columns {
     int groups, d;
     bool f32;
 };
+template <bool PIECES>
 __global__ void __launch_bounds__(256)
 k_join_both(const Args x, const Args y, const Columns c)
 {
-    __shared__ float sums[16][17];
+    __shared__ __attribute__((aligned(16))) float lds[PIECES ? JOIN_LDS : 16 * 17];
+    float (&sums)[16][17] = *reinterpret_cast<float (*)[16][17]>(lds);
     if (blockIdx.y == 0) {
-        if (x.splits > 1) join<false>(x);
+        if (x.splits > 1) join_parts<false, PIECES>(x, lds);
     } else if (blockIdx.y == 1) {
-        if (y.splits > 1) join<false>(y);
+        if (y.splits > 1) join_parts<false, PIECES>(y, lds);
     } else if (c.part) {
         for (int b = (int)blockIdx.x; b < (c.d + 15) / 16; b += (int)gridDim.x) {
             if (c.f32) column_sums<float, 16>(c.part, c.pitch, c.groups, c.d, (float *)c.out, b, sums);
