@@ -322,8 +322,8 @@ void rcd_profile_read(double *out8_host);
  *   - dt is RCD_F32 or RCD_BF16 for every matrix of a call that is not said to be something else.  Sums, statistics and
  *     products are accumulated in fp32 (or more) whatever dt is, with one exception (under RCD_MXFP8), and every output is
  *     rounded once, when it is stored.
- *     Products of RCD_F32 operands are exact to fp32 (a factor goes to the matrix cores as it is, or as three bf16 pieces
- *     that add up to it).
+ *     A factor of an RCD_F32 product goes to the matrix cores as it is, or as three bf16 pieces that add up to it: six of their nine
+ *     products are taken, what is left out is at most 2^-24 (1 + 2^-10) of a product's size, of either sign.
  *   - RCD_MXFP8 (where an entry point lists it): elements are e4m3 bytes, and each block of 32 consecutive elements of a
  *     row (the last one may be shorter) shares a scale 2^(s - 127), s one byte; s = 255 means NaN.  Element i of a row
  *     stands for e4m3(byte i) * 2^(s[i / 32] - 127).  Scales are a byte matrix of their own, rows x ceil(d / 32), with a

@@ -279,9 +279,6 @@ struct Packer {
     }
 };
 
-// The pairs of pieces whose products make up an fp32 product: the dropped ones are below 2^-24 of it.  Largest last.
-constexpr int PIECE_PAIRS[6][2] = {{2, 0}, {0, 2}, {1, 1}, {1, 0}, {0, 1}, {0, 0}};
-
 // C (M x N) = sum over pairs of a_i b_i, over k of K.
 struct Product {
     int64_t M, N, K;

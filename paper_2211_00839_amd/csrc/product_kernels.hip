@@ -5,6 +5,7 @@
 // on the matrix cores, for operands whose k is contiguous (the forward products) or whose rows are (the gradients: no matrix
 // is ever transposed in memory), in bf16, in fp32 as three bf16 pieces, or in 8 bits with block scales.
 #pragma once
+#include "encoder_pieces.h"
 #include "norm_kernels.hip"
 
 namespace enc {
@@ -131,7 +132,7 @@ struct Segments {
 };
 
 // fp32 factors as their pieces, to go back to where the pieces' products say nothing: an infinity times a piece that is
-// zero is a NaN.
+// zero, or times two of opposite signs, is a NaN.
 struct Pieces3 {
     const __bf16 *a[2], *b[2];      // per pair; null: not an fp32 product
     long long a_plane, b_plane, a_row, a_k, b_row, b_k;
@@ -1183,23 +1184,6 @@ k_join_both(const Args x, const Args y, const Columns c)
 
 // ---- what goes before a product -------------------------------------------------------------------------------------------
 
-// An fp32 number as three bf16 that add up to it: each piece is the leading 8 bits of what is left, cut off (not rounded),
-// so that no piece of a finite number is infinite.  Of what is not finite the first piece says all.
-__device__ __forceinline__ void pieces_of(float v, __bf16 &a, __bf16 &b, __bf16 &c)
-{
-    const unsigned bits = __builtin_bit_cast(unsigned, v);
-    if (!(fabsf(v) <= 3.402823466e38f)) {
-        a = __builtin_bit_cast(__bf16, (unsigned short)((bits >> 16) | ((bits & 0x7fffffu) ? 0x40 : 0)));
-        b = c = (__bf16)0.f;
-        return;
-    }
-    const float hi = __builtin_bit_cast(float, bits & 0xffff0000u), r = v - hi;
-    const float mid = __builtin_bit_cast(float, __builtin_bit_cast(unsigned, r) & 0xffff0000u);
-    a = __builtin_bit_cast(__bf16, (unsigned short)(bits >> 16));
-    b = __builtin_bit_cast(__bf16, (unsigned short)(__builtin_bit_cast(unsigned, r) >> 16));
-    c = (__bf16)(r - mid);
-}
-
 // Eight values into a packed operand, from element `at` on: bf16, or the three pieces in planes `plane` elements apart, or
 // (PLANES = 0) fp32 as it is.
 template <int PLANES> __device__ __forceinline__ void put8(__bf16 *base, long long at, long long plane, const float (&v)[8])
@@ -1210,17 +1194,24 @@ template <int PLANES> __device__ __forceinline__ void put8(__bf16 *base, long lo
     }
     __bf16 *p = base + at;
     bf16x8 a, b, c;
+    auto cut = [&](auto pieces) {
 #pragma unroll
-    for (int i = 0; i < 8; ++i) {
-        if constexpr (PLANES == 1) {
-            a[i] = (__bf16)v[i];
-        } else {
-            __bf16 x, y, z;
-            pieces_of(v[i], x, y, z);
-            a[i] = x;
-            b[i] = y;
-            c[i] = z;
+        for (int i = 0; i < 8; ++i) {
+            const Piece3 q = pieces(v[i]);
+            a[i] = __builtin_bit_cast(__bf16, q.a);
+            b[i] = __builtin_bit_cast(__bf16, q.b);
+            c[i] = __builtin_bit_cast(__bf16, q.c);
         }
+    };
+    if constexpr (PLANES == 1) {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) a[i] = (__bf16)v[i];
+    } else {
+        bool ordinary = true;
+#pragma unroll
+        for (int i = 0; i < 8; ++i) ordinary &= is_ordinary(v[i]);
+        if (ordinary) cut([](float f) { return pieces_of_ordinary(f); });
+        else cut([](float f) { return pieces_of(f); });
     }
     *reinterpret_cast<bf16x8 *>(p) = a;
     if constexpr (PLANES == 3) {
