@@ -7,6 +7,7 @@
 #include <torch/csrc/autograd/python_variable.h>
 
 #include <ATen/ATen.h>
+#include <c10/core/GradMode.h>
 #include <c10/core/impl/VirtualGuardImpl.h>
 
 #include <algorithm>
@@ -73,6 +74,16 @@ const at::Tensor *tensor(PyObject *o)
     return &THPVariable_Unpack(o);
 }
 
+// A tensor whose gradients autograd would be expected to record, which these calls do not do: a result without a history must not
+// be taken for one with.
+void no_history(const std::string &name, const at::Tensor &t)
+{
+    if (t.requires_grad() && c10::GradMode::is_enabled())
+        refuse(name + " requires grad, and this call records no history: call it under torch.no_grad() or inside an autograd.Function, "
+                      "with the backward call beside it",
+               RCD_ERR_UNSUPPORTED);
+}
+
 struct Matrix {
     const at::Tensor *t = nullptr;
     int64_t rows = 0, cols = 0, ld = 0;
@@ -88,6 +99,7 @@ Matrix matrix(const char *name, PyObject *o, int64_t rows, int64_t cols, const a
     Matrix m;
     m.t = &THPVariable_Unpack(o);
     const at::Tensor &t = *m.t;
+    no_history(n, t);
     if (t.dim() != 2) refuse(n + " must be a matrix");
     if (!t.is_cuda()) refuse(n + ": device tensor expected (there is no CPU path)", NOT_ON_DEVICE);
     m.type = t.scalar_type();
@@ -119,6 +131,7 @@ const void *vector(const char *name, PyObject *o, int64_t n, at::ScalarType type
     const std::string s = name;
     if (!THPVariable_Check(o)) refuse(s + " must be a contiguous vector of " + std::to_string(n));
     const at::Tensor &t = THPVariable_Unpack(o);
+    no_history(s, t);
     if (t.dim() != 1 || t.size(0) != n || (n > 1 && t.stride(0) != 1)) refuse(s + " must be a contiguous vector of " + std::to_string(n));
     if (t.scalar_type() != type) refuse(s + " must be " + c10::toString(type), RCD_ERR_UNSUPPORTED);
     if (t.device() != like.t->device()) refuse(s + " is on another device");
@@ -235,6 +248,7 @@ Result result(PyObject *out, PyObject *out_type, const Matrix &a, int64_t rows, 
     r.m = matrix("out", out, rows, cols, code >= 0 ? &type : nullptr, &a);
     if (r.m.type == at::kFloat8_e4m3fn) refuse("out must be float32 or bfloat16", RCD_ERR_UNSUPPORTED);
     r.t = *r.m.t;
+    if (!r.t.is_inference()) r.t.unsafeGetTensorImpl()->bump_version();      // (autograd's check of what it has kept of it)
     return r;
 }
 
@@ -397,6 +411,7 @@ PyObject *gated_linear_backward(PyObject *, PyObject *const *a, Py_ssize_t n)
     const int64_t M = dh.rows, F = dh.cols, K = m.cols;
     const Matrix g = matrix("w_gate", a[2], F, K, &dh.type, &dh), u = matrix("w_up", a[3], F, K, &dh.type, &dh);
     const at::Tensor *saved = tensor(a[4]);
+    if (saved) no_history("saved", *saved);
     if (!saved || saved->dim() != 3 || saved->size(0) != M || saved->size(1) != F || saved->size(2) != 2 || saved->scalar_type() != at::kFloat ||
         !saved->is_contiguous() || saved->device() != dh.t->device())
         refuse("saved must be what gated_linear returned");

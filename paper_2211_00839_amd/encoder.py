@@ -6,6 +6,9 @@ Matrices are float32 or bfloat16 device tensors of two dimensions whose last one
 operator takes 8-bit operands they are float8_e4m3fn tensors with their scales beside them: uint8 or float8_e8m0fnu, one for
 each 32 elements of a row.  Every call runs on the current stream; a workspace is allocated unless one is given.  What cannot
 be served raises RcdError.
+
+Autograd records none of these calls: a tensor that requires grad is refused while gradients are recorded.  Call them under
+torch.no_grad(), or in the forward and backward of a torch.autograd.Function, where recording is off.
 """
 from __future__ import annotations
 
