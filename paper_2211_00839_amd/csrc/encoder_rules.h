@@ -103,7 +103,7 @@ inline bool few_rows(int64_t M, int64_t N, int64_t K, bool f32, bool mx)
 }
 
 // fp32 products go to the fp32 matrix instruction directly (wt 32: tiles of 64 x 64, k in stages of 32) where that takes less
-// than pieces do, whose launch and trip through memory come on top (4.5 us and 10 bytes per element at 5 TB/s).
+// than pieces do, whose launch and trip through memory come on top.
 constexpr int DIRECT_STAGE = 32;
 inline double direct_time_of(const Cut &c, int64_t M, int64_t N, int64_t stages, bool gated, int64_t units = UNITS)
 {
@@ -134,24 +134,28 @@ inline Cut direct_cut_of(int64_t M, int64_t N, int64_t stages, bool gated, int64
     }
     return best;
 }
-inline double pieces_time(int64_t elements) { return 4.5 + 1e-6 / 5 * 10.0 * (double)elements; }
 
-// One fp32 product of `pairs` summed ones: by the direct kernel / by pieces, without the making of the pieces.
-inline double direct_time(int64_t M, int64_t N, int64_t K, int pairs, bool gated)
+// Whole fp32 calls, both ways, in us: fitted to 560 calls measured both ways, of 64 .. 16384 rows, 64 .. 8192 columns and k of 64 .. 4096, up to
+// 30 GFLOP a product, epilogues included (bias, activation, residual and z; g and u).  The estimates are off by a tenth (rms); the way they
+// choose takes 0.4 % more than the faster one in the mean, at worst a fifth, where the two lie close together.
+struct Ways {
+    double direct, pieces;
+};
+inline Ways forward_ways(int64_t M, int64_t N, int64_t K, bool gated)
 {
-    const int64_t stages = ceil_div(K, DIRECT_STAGE) * pairs;
-    return direct_time_of(direct_cut_of(M, N, stages, gated), M, N, stages, gated);
+    const double w = gated ? 2 : 1, results = 1e-6 * w * (double)M * (double)N, operands = 1e-6 * (double)(M + (gated ? 2 : 1) * N) * (double)K;
+    const int64_t stages = ceil_div(K, DIRECT_STAGE), deep = ceil_div(K, 64) * 6;
+    const Cut cut = cut_of(M, N, deep, gated);
+    const double direct = direct_time_of(direct_cut_of(M, N, stages, gated), M, N, stages, gated), pieces = time_of(cut, M, N, deep, gated);
+    // large tiles at the result's edge take their epilogue with every check: 4097 x 2056 x 200 62.7 / 91.8, 4096 x 2048 x 200 55.6 / 56.0
+    const bool edge = cut.wt == 128 && cut.splits == 1 && N % (gated ? 128 : 256) != 0;
+    return gated ? Ways{0.88 * direct + 1.0 + 0.7 * results, 7.6 + 0.9 * pieces + 1.6 * operands + 0.9 * results + (edge ? 14.0 : 0.0)}
+                 : Ways{0.88 * direct + 0.6 + 1.5 * results, 10.0 + 0.72 * pieces + 2.1 * operands + 2.7 * results + (edge ? 22.0 : 0.0)};
 }
-inline double pieces_product_time(int64_t M, int64_t N, int64_t K, int pairs, bool gated)
-{
-    const int64_t stages = ceil_div(K, 64) * 6 * pairs;
-    return time_of(cut_of(M, N, stages, gated), M, N, stages, gated);
-}
-// Whole calls.
 inline bool direct_forward(int64_t M, int64_t N, int64_t K, bool gated)
 {
-    if (!launchable(direct_cut_of(M, N, ceil_div(K, DIRECT_STAGE), gated))) return false;
-    return direct_time(M, N, K, 1, gated) < pieces_product_time(M, N, K, 1, gated) + pieces_time((M + N * (gated ? 2 : 1)) * K);
+    const Ways t = forward_ways(M, N, K, gated);
+    return launchable(direct_cut_of(M, N, ceil_div(K, DIRECT_STAGE), gated)) && t.direct < t.pieces;
 }
 // The direct kernel's two products of a backward call always run side by side, each cut for half of the device.
 inline Both direct_both(int64_t M, int64_t N, int64_t K, bool gated)
@@ -160,13 +164,28 @@ inline Both direct_both(int64_t M, int64_t N, int64_t K, bool gated)
     return Both{true, direct_cut_of(M, K, ceil_div(N, DIRECT_STAGE) * w, false, UNITS / 2),
                 direct_cut_of(gated ? 2 * ceil_div(N, 64) * 64 : N, K, ceil_div(M, DIRECT_STAGE), false, UNITS / 2)};
 }
-inline bool direct_backward(int64_t M, int64_t N, int64_t K, bool gated)
+// Both gradients.  Directly: what all workgroups have to do, shared among the units, and the longest one's own way; by pieces: the products
+// as they are cut, side by side or one after the other.  dz is made on the way in both, in four or in six bytes.
+inline Ways backward_ways(int64_t M, int64_t N, int64_t K, bool gated)
 {
     const int w = gated ? 2 : 1;
+    const int64_t rows = gated ? 2 * ceil_div(N, 64) * 64 : N;
+    const double slopes = 1e-6 * w * (double)M * (double)N, operands = 1e-6 * (double)(M + w * N) * (double)K, result = 1e-6 * (double)M * (double)K;
+    const Both d = direct_both(M, N, K, gated);
+    const double deep1 = 0.85 * (double)ceil_div(ceil_div(N, DIRECT_STAGE) * w, d.first.splits), deep2 = 0.85 * (double)ceil_div(ceil_div(M, DIRECT_STAGE), d.second.splits);
+    const double load = ((double)workgroups_of(d.first) * deep1 + (double)workgroups_of(d.second) * deep2) / (double)UNITS;
+    const int64_t stages1 = ceil_div(N, 64) * 6 * w, stages2 = ceil_div(M, 64) * 6;
+    const Both p = both_of(M, K, stages1, rows, K, stages2);
+    const int64_t units = p.together ? UNITS / 2 : UNITS;
+    const double t1 = time_of(p.first, M, K, stages1, false, units), t2 = time_of(p.second, rows, K, stages2, false, units);
+    return Ways{13.0 + 0.73 * load + 0.6 * std::max(deep1, deep2) + 2.0 * slopes + 3.2 * result,
+                15.0 + 0.85 * (p.together ? std::max(t1, t2) : t1 + t2) + 3.5 * operands + 2.7 * slopes + 0.2 * result};
+}
+inline bool direct_backward(int64_t M, int64_t N, int64_t K, bool gated)
+{
     const Both cut = direct_both(M, N, K, gated);
-    if (grid_of(cut.first) + grid_of(cut.second) > MOST_WORKGROUPS) return false;
-    return direct_time(M, K, N, w, false) + direct_time(w * N, K, M, 1, false) <
-           pieces_product_time(M, K, N, w, false) + pieces_product_time(w * N, K, M, 1, false) + pieces_time((M + N * w) * K);
+    const Ways t = backward_ways(M, N, K, gated);
+    return grid_of(cut.first) + grid_of(cut.second) <= MOST_WORKGROUPS && t.direct < t.pieces;
 }
 
 } // namespace enc_rules
