@@ -1,11 +1,13 @@
 """Builds librcd.so (the HIP library behind the C ABI of include/rcd.h) for gfx950, and _encoder.so (the argument
 marshalling of encoder.py, which calls it).
 
-Run as ``python -m paper_2211_00839_amd.build``; hipcc cross-compiles without a GPU.
+Run as ``python -m paper_2211_00839_amd.build``; hipcc cross-compiles without a GPU.  librcd.so needs nothing else; where a
+host compiler, torch or a header of Python's is missing, _encoder.so is left out with a word, and encoder.py's calls raise.
 """
 from __future__ import annotations
 
 import os
+import shutil
 import subprocess
 import sys
 import sysconfig
@@ -46,8 +48,14 @@ def build(verbose: bool = False) -> str:
         _complain(any(job.returncode != 0 for job in jobs), said, verbose)
         _run([hipcc, "--offload-arch=gfx950", "-shared", "-fPIC"] + objects + ["-o", tmp], verbose)
         os.replace(tmp, LIB)
-        _run(_marshal_command(MARSHAL + suffix), verbose)
-        os.replace(MARSHAL + suffix, MARSHAL)
+        missing = _missing_for_marshalling()
+        if missing:
+            if os.path.exists(MARSHAL):       # (of another build)
+                os.remove(MARSHAL)
+            print("_encoder.so is not built: %s" % missing, file=sys.stderr, flush=True)
+        else:
+            _run(_marshal_command(MARSHAL + suffix), verbose)
+            os.replace(MARSHAL + suffix, MARSHAL)
     finally:
         for path in objects + [tmp, MARSHAL + suffix]:
             if os.path.exists(path):
@@ -70,12 +78,31 @@ def _run(cmd, verbose):
     _complain(res.returncode != 0, [res.stdout], verbose)
 
 
+def _host_compiler():
+    return os.environ.get("CXX", "g++")
+
+
+def _missing_for_marshalling():
+    """What _encoder.so cannot be built without and is not there, or None."""
+    if not shutil.which(_host_compiler()):
+        return "no host compiler %s" % _host_compiler()
+    if not os.path.exists(os.path.join(sysconfig.get_path("include"), "Python.h")):
+        return "no Python.h"
+    try:
+        import torch
+    except ImportError as e:
+        return "no torch (%s)" % e
+    if not os.path.exists(os.path.join(os.path.dirname(os.path.abspath(torch.__file__)), "include", "ATen", "ATen.h")):
+        return "no headers of torch"
+    return None
+
+
 def _marshal_command(out):
     """Host code alone, against torch's headers and the library just built."""
     import torch
 
     root = os.path.dirname(os.path.abspath(torch.__file__))
-    return [os.environ.get("CXX", "g++"), "-O2", "-std=c++17", "-fPIC", "-shared", "-w", "-I", os.path.join(root, "include"),
+    return [_host_compiler(), "-O2", "-std=c++17", "-fPIC", "-shared", "-w", "-I", os.path.join(root, "include"),
             "-I", os.path.join(root, "include", "torch", "csrc", "api", "include"), "-I", sysconfig.get_path("include"),
             os.path.join(CSRC, "encoder_marshal.cpp"), "-o", out, "-L", os.path.join(root, "lib"), "-ltorch_python", "-ltorch_cpu",
             "-ltorch", "-lc10", "-L", HERE, "-lrcd", "-Wl,-rpath,$ORIGIN"]
