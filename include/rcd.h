@@ -323,7 +323,8 @@ void rcd_profile_read(double *out8_host);
  *     products are accumulated in fp32 (or more) whatever dt is, with one exception (under RCD_MXFP8), and every output is
  *     rounded once, when it is stored.
  *     A factor of an RCD_F32 product goes to the matrix cores as it is, or as three bf16 pieces that add up to it: six of their nine
- *     products are taken, what is left out is at most 2^-24 (1 + 2^-10) of a product's size, of either sign.
+ *     products are taken, what is left out is at most 2^-24 (1 + 2^-10) of a product's size, of either sign
+ *     (of a factor below 2^-110, what lies below 2^-133 is lost too).
  *   - RCD_MXFP8 (where an entry point lists it): elements are e4m3 bytes, and each block of 32 consecutive elements of a
  *     row (the last one may be shorter) shares a scale 2^(s - 127), s one byte; s = 255 means NaN.  Element i of a row
  *     stands for e4m3(byte i) * 2^(s[i / 32] - 127).  Scales are a byte matrix of their own, rows x ceil(d / 32), with a
@@ -343,7 +344,8 @@ void rcd_profile_read(double *out8_host);
  */
 
 typedef enum { RCD_ACT_NONE = 0, RCD_ACT_RELU = 1, RCD_ACT_SILU = 2, RCD_ACT_GELU = 3 } rcd_act;
-/* relu max(z, 0) with slope 0 at 0; silu z / (1 + e^-z); gelu z * Phi(z), Phi the normal distribution (not its tanh form) */
+/* relu max(z, 0) with slope 0 at 0; silu z / (1 + e^-z); gelu z * Phi(z), Phi the normal distribution (not its tanh form),
+ * computed to some 1e-7 absolute: where z is far below 0, gelu(z) is exact to 1e-7 |z|, not relative to its own small size */
 
 /*
  * Root-mean-square norm with the residual's addition:

@@ -88,7 +88,7 @@ template <bool MX, bool NORM> int launch_norm(NormArgs a, int dt, hipStream_t st
 }
 
 // Row groups of the backward kernel, each with its own sums for the weight's gradient.  Rows of a workgroup of their own: as
-// many workgroups as the device holds at once (50 000 x 2048 bf16: 160 us and 8 for the sums; with half of them 187 and 6).
+// many workgroups as the device holds at once (50 000 x 2048 bf16: 161 us and 8 for the sums; with half of them 187 and 6).
 inline int64_t norm_groups(int64_t rows, int64_t d)
 {
     const int64_t per = rows_per_workgroup(d);

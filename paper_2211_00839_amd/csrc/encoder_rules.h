@@ -136,8 +136,9 @@ inline Cut direct_cut_of(int64_t M, int64_t N, int64_t stages, bool gated, int64
 }
 
 // Whole fp32 calls, both ways, in us: fitted to 560 calls measured both ways, of 64 .. 16384 rows, 64 .. 8192 columns and k of 64 .. 4096, up to
-// 30 GFLOP a product, epilogues included (bias, activation, residual and z; g and u).  The estimates are off by a tenth (rms); the way they
-// choose takes 0.4 % more than the faster one in the mean, at worst a fifth, where the two lie close together.
+// 30 GFLOP a product, epilogues included (bias, activation, residual and z; g and u).  The estimates are off by a tenth (rms); over 860 calls, 300 of
+// them long and narrow and not fitted to, the way they choose takes 0.6 % more than the faster one in the mean, at worst three tenths, where the two
+// lie close together.
 struct Ways {
     double direct, pieces;
 };

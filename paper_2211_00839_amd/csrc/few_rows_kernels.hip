@@ -39,7 +39,7 @@ __device__ __forceinline__ void widen(const uint4 (&c)[2], float s0, float s1, b
 // Sums of 16 columns and up to 16 MT rows on 16 x 16 MFMA blocks, bf16 or 8 bits (widened to bf16 in registers, which is
 // exact and costs nothing beside the weights' way from memory).  The waves of a workgroup take the
 // chunks of 128 bytes of k in turn and add up their sums through LDS, wave by wave.  Bound by the weights' reading: 8 rows, twice 8192 x 2048
-// bf16 14.8 us (67 MB, 4.5 TB/s); one row, 2048 x 2048 6.5 us (8.4 MB: 128 workgroups of sixteen waves, whose start, one wait for memory, sum and
+// bf16 15.8 us (67 MB, 4.2 TB/s); one row, 2048 x 2048 6.3 us (8.4 MB: 128 workgroups of sixteen waves, whose start, one wait for memory, sum and
 // epilogue are most of it).
 template <int MT, int WAVES, bool MX, bool GATED>
 __global__ void __launch_bounds__(64 * WAVES)

@@ -73,8 +73,8 @@ __device__ __forceinline__ void store_mx(const NormArgs &a, size_t row, int col,
 }
 
 // One wave to a row of up to 1024 elements, four to a longer one (past 8192 it is read twice).  Bound by memory: 50 000 x 2048
-// bf16 with residual and sum 131 us (819 MB, 6.2 TB/s: part of it stays in the last-level cache), 5000 x 2048 into 8 bits 13
-// to 15 us (72 MB); one row of 2048 2.4 us: a launch, two waits for memory and a barrier.
+// bf16 with residual and sum 135 us (819 MB, 6.1 TB/s: part of it stays in the last-level cache), 5000 x 2048 into 8 bits 14
+// to 16 us (72 MB); one row of 2048 2.6 us: a launch, two waits for memory and a barrier.
 // NORM = false: the rows themselves in 8 bits (no statistics).
 template <typename T, int WPR, int C, bool MX, bool NORM>
 __global__ void __launch_bounds__(NORM_THREADS)
@@ -166,7 +166,7 @@ struct NormBackArgs {
 };
 
 // A group of WPR waves walks the rows group, group + groups, ...: its sums of dy xh stay in registers from row to row
-// (C = 0: in its row of `part`).  Bound by memory: 50 000 x 2048 bf16 160 us (819 MB, 5.1 TB/s).  Adding to dw with atomics would
+// (C = 0: in its row of `part`).  Bound by memory: 50 000 x 2048 bf16 161 us (819 MB, 5.1 TB/s).  Adding to dw with atomics would
 // need no second launch, but its bits would change from run to run.
 template <typename T, int WPR, int C>
 __global__ void __launch_bounds__(NORM_THREADS)
@@ -284,7 +284,7 @@ __device__ __forceinline__ void column_sums(const float *__restrict__ part, long
     if (r == 0 && col < d) out[col] = (T)sums[0][c];
 }
 
-// grid = ceil(d / 16).  Latency: 2048 columns of 512 groups 8 us
+// grid = ceil(d / 16).  Latency: 2048 columns of 2048 groups 8 us
 template <typename T>
 __global__ void __launch_bounds__(1024)
 k_column_sums(const float *__restrict__ part, long long pitch, int groups, int d, T *__restrict__ out)

@@ -1036,10 +1036,10 @@ __device__ __forceinline__ void tile_body(const Args &x, int wg, int nwg)
     }
 }
 
-// Bound by the matrix cores where there are many tiles: the gradients of 16384 tokens' gated block of 8192 x 2048, in 256 x 256 tiles, 836 us
-// (the tokens') and 814 (the weights'), 1.1 TFLOP each: 1.32 and 1.35 PFLOP/s, 94 and 96 % of a large library product, the clock being held down by
-// power.  What the epilogue moves comes on top where workgroups end together: 16384 x 2048 x 2048 with gelu, residual and z 205 us, of which 268 MB
-// of epilogue; the gated block forward, g and u kept, 1177 us of which 786 are multiplies.  8 bits: 5000 x 2048 x 8192 130 us in 160 tiles on 256 units,
+// Bound by the matrix cores where there are many tiles: the gradients of 16384 tokens' gated block of 8192 x 2048, in 256 x 256 tiles, 861 us
+// (the tokens') and 842 (the weights'), 1.1 TFLOP each: 1.28 and 1.31 PFLOP/s, 93 and 95 % of a large library product, the clock being held down by
+// power.  What the epilogue moves comes on top where workgroups end together: 16384 x 2048 x 2048 with gelu, residual and z 212 us, of which 268 MB
+// of epilogue; the gated block forward, g and u kept, 1198 us of which 786 are multiplies.  8 bits: 5000 x 2048 x 8192 125 us in 160 tiles on 256 units,
 // 1.3 PFLOP/s (2.1 on the units in use).
 template <int WT, int KA, int KB, bool MX, int TO>
 __global__ void __launch_bounds__(THREADS, WT == 128 ? 1 : 2)
@@ -1066,7 +1066,7 @@ k_tile_both(const Args x, const Args y, int first)
 }
 
 // The parts of a product whose k was split among workgroups, in order (the sum's bits are the same from run to run), and what
-// becomes of their sum.  Bound by memory: four parts of 2048 x 2048 13.4 us (75 MB, 5.6 TB/s).
+// becomes of their sum.  Bound by memory: four parts of 2048 x 2048 13.2 us (75 MB, 5.7 TB/s).
 template <bool GATED> __device__ __forceinline__ void add_parts(const Args &x, int m, int n, float (&z)[8], float (&u)[8])
 {
     const long long stride = (long long)x.M * x.parts_pitch;
@@ -1221,7 +1221,7 @@ template <int PLANES> __device__ __forceinline__ void put8(__bf16 *base, long lo
 }
 
 // Rows laid out for the tile kernel: a pitch that is a multiple of 64 elements, zeros behind the columns, fp32 in its
-// pieces.  grid.y: which matrix.  Bound by memory, and by its launch where small: 2500 x 512 and 2730 x 512 fp32 6.2 us (10.7 MB in, 16 out).
+// pieces.  grid.y: which matrix.  Bound by memory, and by its launch where small: 2500 x 512 and 2730 x 512 fp32 6.8 us (10.7 MB in, 16 out).
 struct PackJob {
     const void *src;
     __bf16 *dst;
@@ -1315,8 +1315,8 @@ k_widen(const WidenJobs jobs)
 }
 
 // dz = dy act'(z), packed, and its column sums over a group of rows.  A thread owns eight columns; `across` threads of a
-// workgroup lie side by side, the others take further rows.  grid = (column pieces, groups).  Bound by memory: 16384 x 2048, z in fp32, 58 us
-// (268 MB, 4.6 TB/s).
+// workgroup lie side by side, the others take further rows.  grid = (column pieces, groups).  Bound by memory: 16384 x 2048, z in fp32, 60 us
+// (268 MB, 4.5 TB/s).
 struct SlopeArgs {
     const void *dy;
     const float *z;                 // preact; gated: g and u side by side
@@ -1364,7 +1364,7 @@ k_slope(const SlopeArgs x)
     }
 }
 
-// dg = dh u act'(g) and du = dh act(g), packed side by side.  Bound by memory: 16384 x 8192 346 us (1.88 GB, 5.4 TB/s).
+// dg = dh u act'(g) and du = dh act(g), packed side by side.  Bound by memory: 16384 x 8192 354 us (1.88 GB, 5.3 TB/s).
 template <typename T, int PLANES, int ACT>
 __global__ void __launch_bounds__(256)
 k_gated_slope(const SlopeArgs x)
