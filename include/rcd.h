@@ -436,6 +436,73 @@ int rcd_gated_linear_backward(const void *dH_dev, int64_t ld_dh, const void *A_d
                               void *workspace_dev, size_t workspace_bytes, void *stream);
 size_t rcd_gated_linear_backward_workspace_bytes(int64_t M, int64_t F, int64_t K, int dt);
 
+/*
+ * Attention, what mixes the tokens of a sample (a sequence), with the learned bias of relative positions.  For each head
+ *     out_i = sum_j p_ij v_j,   p_ij = exp(s_ij) / sum_j' exp(s_ij'),   s_ij = scale q_i k_j + bias[bucket(j - pos_i)]
+ * Query i of a sequence of n queries and m keys stands at the position pos_i = i + m - n (its queries are the last n of its keys), whether
+ * causal (keys j > pos_i are masked) or not.  A query that sees no key, by its mask, an empty sequence or a bias of -infinity throughout,
+ * gets zeros, and no gradient goes through it.  What is masked has no part in anything: a NaN in a key or value that a query does not see
+ * does not reach it, and rows behind a sequence are not read.
+ *
+ *   dt                  RCD_F32 or RCD_BF16, of every matrix.  Scores, statistics and sums are fp32; for RCD_BF16 p and its gradient are
+ *                       rounded to bf16 on their way into the second product (2^-9 of each, what v, k and q have lost already)
+ *   heads, kv_heads     heads is a multiple of kv_heads: head h of q goes with head h / (heads / kv_heads) of k and v.  d: 1 .. 128
+ *   q_rows, k_rows      rows of each of `batch` sequences, whose places are their strides rcd_heads.batch; or with q_offsets_dev, k_offsets_dev
+ *                       (int32[batch + 1], not decreasing) rows of all of them one after the other, sequence b from offset b up to offset
+ *                       b + 1 (no batch stride).  Each of the two by itself.  At most 2^29.  Offsets outside 0 .. rows are held inside.
+ *   k_lengths_dev       int32[batch], nullable, without k_offsets_dev: how many of the k_rows keys of each sequence there are
+ *   longest_q, longest_k   with offsets: the longest sequence, or 0.  They set the launch only: a longer one is served too, slower
+ *   scale               positive
+ *   bias_dev            nullable: buckets x heads of bias_dt (RCD_F32 or RCD_BF16), contiguous.  borders_host (host memory) are the distances
+ *                       1 <= border[0] <= border[1] .. <= 1024 at which the next bucket begins: the bucket of a distance is the number of borders
+ *                       that are not above it.  causal: buckets - 1 of them; else buckets / 2 - 1, for keys at or before the query, and
+ *                       keys behind it have the second half of the table by the same borders.  2 .. 128 buckets in a direction.
+ *   rcd_heads           a matrix's address (of its element 0) and its strides in elements from sequence to sequence, row to row and head to
+ *                       head; an element of a row follows the other.  Rows are less than 2^24 bytes apart.
+ */
+typedef struct {
+    void *p;
+    int64_t batch, row, head;
+} rcd_heads;
+
+typedef struct {
+    int dt;
+    int64_t batch, heads, kv_heads, d, q_rows, k_rows;
+    const int32_t *q_offsets_dev, *k_offsets_dev, *k_lengths_dev;
+    int64_t longest_q, longest_k;
+    int causal;
+    float scale;
+    const void *bias_dev;
+    int bias_dt;
+    int64_t buckets;
+    const int32_t *borders_host;
+} rcd_attention_shape;
+
+/*
+ *   saved_dev (nullable)  float[2 x rows of q x heads], what the backward call takes: for each row and head the scores' maximum (or a number
+ *                         below it by at most 8), in powers of two, and log2 of the sum of the exponentials over it
+ *   clear                 with q_offsets_dev: rows of out that belong to no sequence become zeros; else they are left as they were
+ * workspace: rcd_attention_workspace_bytes(shape) bytes.
+ */
+int rcd_attention(const rcd_attention_shape *shape, const rcd_heads *q, const rcd_heads *k, const rcd_heads *v, const rcd_heads *out,
+                  float *saved_dev, int clear, void *workspace_dev, size_t workspace_bytes, void *stream);
+size_t rcd_attention_workspace_bytes(const rcd_attention_shape *shape);
+
+/*
+ * Its gradients, with the probabilities computed again.  With delta_i = dout_i out_i and ds_ij = p_ij (dout_i v_j - delta_i):
+ *     dq_i = scale sum_j ds_ij k_j,   dk_j = scale sum_i ds_ij q_i,   dv_j = sum_i p_ij dout_i,   dbias[c] = sum of ds_ij over bucket c's pairs
+ * dk and dv are sums over the query heads that share their head, dbias over everything; all in a fixed order.
+ *   out, saved_dev        of the forward call
+ *   dbias_dev (nullable)  buckets x heads of bias_dt, contiguous
+ *   clear                 rows of dq, dk and dv that belong to no sequence, and rows behind k_lengths_dev, become zeros; else they are
+ *                         left as they were
+ * workspace: rcd_attention_backward_workspace_bytes(shape) bytes.
+ */
+int rcd_attention_backward(const rcd_attention_shape *shape, const rcd_heads *dout, const rcd_heads *q, const rcd_heads *k,
+                           const rcd_heads *v, const rcd_heads *out, const float *saved_dev, const rcd_heads *dq, const rcd_heads *dk,
+                           const rcd_heads *dv, void *dbias_dev, int clear, void *workspace_dev, size_t workspace_bytes, void *stream);
+size_t rcd_attention_backward_workspace_bytes(const rcd_attention_shape *shape);
+
 #ifdef __cplusplus
 }
 #endif

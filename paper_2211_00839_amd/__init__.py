@@ -7,6 +7,12 @@ Every function only marshals torch device tensors into the C ABI declared in
 kernels.  There is no CPU fallback: without the built library, or without a
 GPU, calls raise.
 """
+from .attention import (  # noqa: F401
+    AttentionGrads,
+    attention,
+    attention_backward,
+    position_borders,
+)
 from .binding import (  # noqa: F401
     RcdError,
     bandwidth,

@@ -24,6 +24,7 @@ EXPORTS = [
     "rcd_linear", "rcd_linear_workspace_bytes", "rcd_linear_backward", "rcd_linear_backward_workspace_bytes",
     "rcd_gated_linear", "rcd_gated_linear_workspace_bytes", "rcd_gated_linear_backward",
     "rcd_gated_linear_backward_workspace_bytes",
+    "rcd_attention", "rcd_attention_workspace_bytes", "rcd_attention_backward", "rcd_attention_backward_workspace_bytes",
 ]
 
 
@@ -124,6 +125,14 @@ def load_library():
         query = getattr(lib, name + "_workspace_bytes")
         query.restype = sz
         query.argtypes = [i64, i64, i64, i32]
+    # (pointers to rcd_attention_shape and rcd_heads)
+    lib.rcd_attention.restype = i32
+    lib.rcd_attention.argtypes = [vp, vp, vp, vp, vp, vp, i32, vp, sz, vp]
+    lib.rcd_attention_backward.restype = i32
+    lib.rcd_attention_backward.argtypes = [vp, vp, vp, vp, vp, vp, vp, vp, vp, vp, vp, i32, vp, sz, vp]
+    for name in ("rcd_attention_workspace_bytes", "rcd_attention_backward_workspace_bytes"):
+        getattr(lib, name).restype = sz
+        getattr(lib, name).argtypes = [vp]
     _lib = lib
     return lib
 

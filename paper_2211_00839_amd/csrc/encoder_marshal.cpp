@@ -1,4 +1,4 @@
-// Argument marshalling of encoder.py in C++: the checks, the results' allocation and the call into the C ABI.
+// Argument marshalling of encoder.py and attention.py in C++: the checks, the results' allocation and the call into the C ABI.
 //
 // One sample through one operator is a kernel of 3 to 7 us.  Looking at five tensors attribute by attribute from Python and
 // passing twenty numbers through ctypes took 10 to 18 us; here it takes about one, beside the allocations and the launch.  Nothing but
@@ -11,7 +11,9 @@
 #include <c10/core/impl/VirtualGuardImpl.h>
 
 #include <algorithm>
+#include <cmath>
 #include <string>
+#include <utility>
 
 #include "../../include/rcd.h"
 
@@ -432,6 +434,220 @@ PyObject *gated_linear_backward(PyObject *, PyObject *const *a, Py_ssize_t n)
     MARSHAL_END
 }
 
+// ---- attention ------------------------------------------------------------------------------------------------------------
+
+// Rows of heads: (batch, rows, heads, d), or (rows, heads, d) where offsets say which sequence a row belongs to.
+struct Rows {
+    const at::Tensor *t = nullptr;
+    int64_t batch = 0, rows = 0, heads = 0, d = 0;
+    rcd_heads h{};
+};
+
+// The strides of a tensor of heads; written: its elements may not share memory.
+rcd_heads strides(const std::string &n, const at::Tensor &t, bool written)
+{
+    const int64_t dims = t.dim();
+    if (t.size(dims - 1) > 1 && t.stride(dims - 1) != 1 && t.numel() > 0) refuse("the last dimension of " + n + " must be contiguous");
+    int64_t s[4] = {0, 0, 0, 0};                // (of a dimension of one the stride means nothing)
+    for (int64_t i = 0; i < dims; ++i) s[4 - dims + i] = t.size(i) > 1 ? t.stride(i) : 0;
+    if (written && t.numel() > 0) {
+        std::pair<int64_t, int64_t> by[4];
+        int count = 0;
+        for (int64_t i = 0; i < dims; ++i)
+            if (t.size(i) > 1) by[count++] = {t.stride(i), t.size(i)};
+        std::sort(by, by + count);
+        int64_t extent = 1;
+        for (int i = 0; i < count; ++i) {
+            if (by[i].first < extent) refuse("elements of " + n + " overlap");
+            extent += by[i].first * (by[i].second - 1);
+        }
+    }
+    return {t.data_ptr(), s[0], s[1], s[2]};
+}
+
+Rows rows(const char *name, PyObject *o, bool ragged, const at::ScalarType *type, const at::Tensor *like, bool written = false)
+{
+    const std::string n = name, shape = ragged ? "(rows, heads, d)" : "(batch, rows, heads, d)";
+    if (!THPVariable_Check(o)) refuse(n + " must be a tensor " + shape);
+    Rows r;
+    r.t = &THPVariable_Unpack(o);
+    const at::Tensor &t = *r.t;
+    no_history(n, t);
+    if (t.dim() != (ragged ? 3 : 4)) refuse(n + " must be a tensor " + shape + (ragged ? " where it has offsets" : ""));
+    if (!t.is_cuda()) refuse(n + ": device tensor expected (there is no CPU path)", NOT_ON_DEVICE);
+    if (t.scalar_type() != at::kFloat && t.scalar_type() != at::kBFloat16) refuse(n + ": float32 or bfloat16 expected", RCD_ERR_UNSUPPORTED);
+    if (type && t.scalar_type() != *type) refuse(n + " must be " + c10::toString(*type), RCD_ERR_UNSUPPORTED);
+    if (like) {
+        if (t.device() != like->device()) refuse(n + " is on another device");
+    } else if (c10::impl::VirtualGuardImpl(at::kCUDA).getDevice() != t.device()) {
+        refuse(n + " is on another device than the current one");
+    }
+    const int64_t d = t.dim();
+    r.batch = ragged ? 1 : t.size(0);
+    r.rows = t.size(d - 3);
+    r.heads = t.size(d - 2);
+    r.d = t.size(d - 1);
+    r.h = strides(n, t, written);
+    return r;
+}
+void same_shape(const char *name, const Rows &r, const Rows &as, const char *of)
+{
+    if (r.t->sizes() != as.t->sizes()) refuse(std::string(name) + " must have the shape of " + of);
+}
+const int32_t *indices(const char *name, PyObject *o, int64_t least, int64_t n, const at::Tensor &like, int64_t *count)
+{
+    if (o == Py_None) return nullptr;
+    const std::string s = name;
+    if (!THPVariable_Check(o)) refuse(s + " must be a contiguous int32 vector");
+    const at::Tensor &t = THPVariable_Unpack(o);
+    if (t.dim() != 1 || t.scalar_type() != at::kInt || !t.is_contiguous()) refuse(s + " must be a contiguous int32 vector");
+    if (t.device() != like.device()) refuse(s + " is on another device");
+    if (t.size(0) < least || (n >= 0 && t.size(0) != n)) refuse(s + " must have " + std::to_string(n >= 0 ? n : least) + " elements" + (n >= 0 ? "" : " at least"));
+    if (count) *count = t.size(0);
+    return static_cast<const int32_t *>(t.data_ptr());
+}
+
+// What both calls are told of the sequences: a[0] q_offsets, k_offsets, k_lengths, longest_q, longest_k, scale, causal, bias, a[8] borders.
+struct Call {
+    rcd_attention_shape s{};
+    Rows q, k, v;
+    at::ScalarType type;
+    const at::Tensor *bias = nullptr;
+};
+Call attention_call(PyObject *q, PyObject *k, PyObject *v, PyObject *const *a)
+{
+    Call c;
+    const bool q_ragged = a[0] != Py_None, k_ragged = a[1] != Py_None;
+    c.q = rows("q", q, q_ragged, nullptr, nullptr);
+    const at::Tensor &like = *c.q.t;
+    c.type = like.scalar_type();
+    c.k = rows("k", k, k_ragged, &c.type, &like);
+    c.v = rows("v", v, k_ragged, &c.type, &like);
+    same_shape("v", c.v, c.k, "k");
+    if (c.k.d != c.q.d) refuse("k must have heads of q's size");
+    int64_t ends = -1;
+    c.s.q_offsets_dev = indices("q_offsets", a[0], 1, -1, like, &ends);
+    c.s.k_offsets_dev = indices("k_offsets", a[1], 1, ends, like, &ends);
+    c.s.batch = ends >= 0 ? ends - 1 : c.q.batch;
+    if ((!q_ragged && c.q.batch != c.s.batch) || (!k_ragged && c.k.batch != c.s.batch)) refuse("q and k must have the same number of sequences");
+    if (k_ragged && a[2] != Py_None) refuse("k_lengths go without k_offsets");
+    c.s.k_lengths_dev = indices("k_lengths", a[2], 0, c.s.batch, like, nullptr);
+    c.s.longest_q = number(a[3]);
+    c.s.longest_k = number(a[4]);
+    if (c.s.longest_q < 0 || c.s.longest_k < 0) refuse("longest_q and longest_k must not be negative");
+    if (c.k.heads < 1 || c.q.heads < 1 || c.q.heads % c.k.heads != 0) refuse("q's heads must be a multiple of k's");
+    if (c.q.d < 1) refuse("heads must have elements");
+    if (c.q.d > 128) refuse("heads of 128 elements at most", RCD_ERR_UNSUPPORTED);
+    const double scale = a[5] == Py_None ? 1.0 / std::sqrt((double)c.q.d) : PyFloat_AsDouble(a[5]);
+    if (scale == -1.0 && PyErr_Occurred()) throw python_error();
+    c.s.scale = (float)scale;
+    c.s.causal = truth(a[6]);
+    c.s.dt = code_of(c.type);
+    c.s.heads = c.q.heads;
+    c.s.kv_heads = c.k.heads;
+    c.s.d = c.q.d;
+    c.s.q_rows = c.q.rows;
+    c.s.k_rows = c.k.rows;
+    if (a[7] != Py_None) {
+        if (!THPVariable_Check(a[7])) refuse("bias must be a contiguous tensor (buckets, heads)");
+        c.bias = &THPVariable_Unpack(a[7]);
+        no_history("bias", *c.bias);
+        if (c.bias->dim() != 2 || c.bias->size(1) != c.q.heads || !c.bias->is_contiguous()) refuse("bias must be a contiguous tensor (buckets, heads)");
+        if (c.bias->scalar_type() != at::kFloat && c.bias->scalar_type() != c.type) refuse("bias must be float32 or of q's type", RCD_ERR_UNSUPPORTED);
+        if (c.bias->device() != like.device()) refuse("bias is on another device");
+        char *borders = nullptr;
+        Py_ssize_t bytes = 0;
+        if (PyBytes_AsStringAndSize(a[8], &borders, &bytes) < 0) throw python_error();
+        c.s.bias_dev = c.bias->data_ptr();
+        c.s.bias_dt = code_of(c.bias->scalar_type());
+        c.s.buckets = c.bias->size(0);
+        const int64_t each = c.s.causal ? c.s.buckets : c.s.buckets / 2;
+        if (bytes < (each - 1) * 4) refuse("too few borders");
+        c.s.borders_host = reinterpret_cast<const int32_t *>(borders);
+    }
+    return c;
+}
+
+// A result in the shape of `as`: `given`, or a new contiguous one (its rows that belong to no sequence are cleared by the call).
+struct Made {
+    at::Tensor t;
+    rcd_heads h{};
+};
+Made made(const char *name, PyObject *given, const Rows &as, const Call &c)
+{
+    Made m;
+    if (given == Py_None) {
+        m.t = at::empty(as.t->sizes(), as.t->options().requires_grad(false));
+        m.h = strides(name, m.t, true);
+        return m;
+    }
+    const Rows r = rows(name, given, as.t->dim() == 3, &c.type, c.q.t, true);
+    same_shape(name, r, as, "what it is of");
+    m.t = *r.t;
+    m.h = r.h;
+    if (!m.t.is_inference()) m.t.unsafeGetTensorImpl()->bump_version();
+    return m;
+}
+Room room(PyObject *o, size_t need, const at::Tensor &like)
+{
+    Matrix m;
+    m.t = &like;
+    return room(o, need, m);
+}
+
+// q, k, v, [nine of attention_call], out, want_saved, workspace, stream -> (out, saved)
+PyObject *attention(PyObject *, PyObject *const *a, Py_ssize_t n)
+{
+    MARSHAL_BEGIN
+    expect(n, 16);
+    const Call c = attention_call(a[0], a[1], a[2], a + 3);
+    const Made out = made("out", a[12], c.q, c);
+    at::Tensor saved;
+    if (truth(a[13])) {
+        auto sizes = c.q.t->sizes().vec();
+        sizes.back() = 2;
+        saved = at::empty(sizes, c.q.t->options().dtype(at::kFloat).requires_grad(false));
+    }
+    const Room ws = room(a[14], rcd_attention_workspace_bytes(&c.s), *c.q.t);
+    void *const on = stream(a[15]);
+    const int clear = a[12] == Py_None;
+    run([&] { return rcd_attention(&c.s, &c.q.h, &c.k.h, &c.v.h, &out.h, (float *)p(saved), clear, ws.p, ws.bytes, on); });
+    return tuple(out.t, saved);
+    MARSHAL_END
+}
+
+// dout, q, k, v, out, saved, [nine of attention_call], dq, dk, dv, want_dbias, workspace, stream -> (dq, dk, dv, dbias)
+PyObject *attention_backward(PyObject *, PyObject *const *a, Py_ssize_t n)
+{
+    MARSHAL_BEGIN
+    expect(n, 21);
+    const Call c = attention_call(a[1], a[2], a[3], a + 6);
+    const bool q_ragged = c.q.t->dim() == 3;
+    const Rows dout = rows("dout", a[0], q_ragged, &c.type, c.q.t), out = rows("out", a[4], q_ragged, &c.type, c.q.t);
+    same_shape("dout", dout, c.q, "q");
+    same_shape("out", out, c.q, "q");
+    const at::Tensor *saved = tensor(a[5]);
+    auto sizes = c.q.t->sizes().vec();
+    sizes.back() = 2;
+    if (saved) no_history("saved", *saved);
+    if (!saved || saved->sizes() != at::IntArrayRef(sizes) || saved->scalar_type() != at::kFloat || !saved->is_contiguous() ||
+        saved->device() != c.q.t->device())
+        refuse("saved must be what attention returned");
+    const int given = (a[15] != Py_None) + (a[16] != Py_None) + (a[17] != Py_None);
+    if (given != 0 && given != 3) refuse("grads must be (dq, dk, dv)");
+    const Made dq = made("dq", a[15], c.q, c), dk = made("dk", a[16], c.k, c), dv = made("dv", a[17], c.v, c);
+    at::Tensor dbias;
+    if (c.bias && truth(a[18])) dbias = at::empty(c.bias->sizes(), c.bias->options().requires_grad(false));
+    const Room ws = room(a[19], rcd_attention_backward_workspace_bytes(&c.s), *c.q.t);
+    void *const on = stream(a[20]);
+    run([&] {
+        return rcd_attention_backward(&c.s, &dout.h, &c.q.h, &c.k.h, &c.v.h, &out.h, (const float *)saved->data_ptr(), &dq.h, &dk.h, &dv.h, p(dbias),
+                                      given == 0, ws.p, ws.bytes, on);
+    });
+    return tuple(dq.t, dk.t, dv.t, dbias);
+    MARSHAL_END
+}
+
 PyObject *set_error(PyObject *, PyObject *cls)
 {
     Py_XDECREF(g_error);
@@ -442,7 +658,8 @@ PyObject *set_error(PyObject *, PyObject *cls)
 
 #define FAST(name) {#name, (PyCFunction)(void (*)(void))name, METH_FASTCALL, nullptr}
 PyMethodDef methods[] = {FAST(rms_norm),        FAST(rms_norm_backward), FAST(quantize_mxfp8),        FAST(linear),
-                         FAST(linear_backward), FAST(gated_linear),      FAST(gated_linear_backward), {"set_error", set_error, METH_O, nullptr},
+                         FAST(linear_backward), FAST(gated_linear),      FAST(gated_linear_backward), FAST(attention),       FAST(attention_backward),
+                         {"set_error", set_error, METH_O, nullptr},
                          {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module_def = {PyModuleDef_HEAD_INIT, "_encoder", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};
 

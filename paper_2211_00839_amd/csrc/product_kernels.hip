@@ -5,6 +5,7 @@
 // on the matrix cores, for operands whose k is contiguous (the forward products) or whose rows are (the gradients: no matrix
 // is ever transposed in memory), in bf16, in fp32 as three bf16 pieces, or in 8 bits with block scales.
 #pragma once
+#include "encoder_lds.h"
 #include "encoder_pieces.h"
 #include "norm_kernels.hip"
 
@@ -249,34 +250,8 @@ template <int WT, bool MX> struct Shape {
     static_assert(4 * 32 * TURN_PITCH * 4 <= LDS_BYTES, "the waves' turn-round regions fit where the stages were");
 };
 
-// (M0 holds the LDS address; the instruction may follow M0's write only after a wait state)
-__device__ __forceinline__ void load16_to_lds(const void *base, unsigned offset, unsigned lds_addr)
-{
-    asm volatile("s_nop 0\n\t"
-                 "global_load_lds_dwordx4 %0, %1"
-                 :
-                 : "v"(offset), "s"(base), "{m0}"(lds_addr)
-                 : "memory");
-}
-__device__ __forceinline__ void load4_to_lds(const void *base, unsigned offset, unsigned lds_addr)
-{
-    asm volatile("s_nop 0\n\t"
-                 "global_load_lds_dword %0, %1"
-                 :
-                 : "v"(offset), "s"(base), "{m0}"(lds_addr)
-                 : "memory");
-}
-template <int N> __device__ __forceinline__ void wait_loads() { asm volatile("s_waitcnt vmcnt(%0)" ::"n"(N) : "memory"); }
-__device__ __forceinline__ void wait_lds() { asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory"); }
-// A barrier that no access to LDS is moved across.
-__device__ __forceinline__ void meet()
-{
-    __builtin_amdgcn_s_barrier();
-    asm volatile("" ::: "memory");
-}
 __device__ __forceinline__ void pin() { __builtin_amdgcn_sched_barrier(0); }
 
-typedef short s16x4 __attribute__((ext_vector_type(4)));
 typedef short s16x8 __attribute__((ext_vector_type(8)));
 
 template <int WT, int KA, int KB, bool MX, bool GATED>

@@ -1712,6 +1712,7 @@ int rcd_init(void)
     RCD_TRY(fast_setup());
     RCD_TRY(static_setup(nullptr));
     RCD_TRY(rcd_set_up_encoder());
+    RCD_TRY(rcd_set_up_attention());
     return RCD_OK;
 }
 
