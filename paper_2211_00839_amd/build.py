@@ -29,7 +29,7 @@ HIPCC_FLAGS = [
 
 
 # one object each, compiled side by side
-SOURCES = ["rcd_lib.hip", "encoder_lib.hip", "attention_lib.hip"]
+SOURCES = ["rcd_lib.hip", "encoder_lib.hip", "attention_lib.hip", "attention_backward_lib.hip"]
 
 
 def build(verbose: bool = False) -> str:

@@ -22,7 +22,7 @@ template <typename T, int DP, bool BIAS> struct Backward {
     static constexpr int TURN_PITCH = 40, TURN_BYTES = 32 * TURN_PITCH * 4;
 };
 
-template <typename T, int DP, bool BIAS>
+template <typename T, int DP, bool BIAS, bool DIRECT>
 __global__ __launch_bounds__(THREADS, sizeof(T) == 2 ? 2 : 1) void k_attention_dq(Args a)
 {
     using W = Backward<T, DP, BIAS>;
@@ -57,6 +57,9 @@ __global__ __launch_bounds__(THREADS, sizeof(T) == 2 ? 2 : 1) void k_attention_d
     const unsigned lds_addr = (unsigned)(size_t)(__attribute__((address_space(3))) unsigned char *)lds;
     Reader<T, DP> reader;
     reader.init();
+    Loader<T, DP, W::TILE, THREADS, DIRECT> load_k, load_v;
+    load_k.init(a.k.row, a.D, tid);
+    load_v.init(a.v.row, a.D, tid);
     for (int tile0 = first_tile * ROWS; tile0 < seq.q_len; tile0 += a.tiles * ROWS) {
         const int mine0 = tile0 + wave * 32, row = mine0 + (lane & 31), h_row = min(row, seq.q_len - 1), pos = shift + h_row;
         const bool there = row < seq.q_len;
@@ -70,9 +73,9 @@ __global__ __launch_bounds__(THREADS, sizeof(T) == 2 ? 2 : 1) void k_attention_d
             for (int s = 0; s < R::STEPS; ++s) {
                 q[s] = g[s] = make_uint4(0, 0, 0, 0);
                 if (!there) continue;
-                q[s] = chunk_of<T>(pq, 2 * s + half, a.D);
-                g[s] = chunk_of<T>(pg, 2 * s + half, a.D);
-                const uint4 o = chunk_of<T>(po, 2 * s + half, a.D);
+                q[s] = chunk_of<T, DIRECT>(pq, 2 * s + half, a.D);
+                g[s] = chunk_of<T, DIRECT>(pg, 2 * s + half, a.D);
+                const uint4 o = chunk_of<T, DIRECT>(po, 2 * s + half, a.D);
                 const unsigned x[4] = {g[s].x, g[s].y, g[s].z, g[s].w}, y[4] = {o.x, o.y, o.z, o.w};
 #pragma unroll
                 for (int e = 0; e < 4; ++e) {
@@ -105,10 +108,10 @@ __global__ __launch_bounds__(THREADS, sizeof(T) == 2 ? 2 : 1) void k_attention_d
         const int tiles = (end + W::TILE - 1) / W::TILE;
         auto load = [&](int t, int buf) {
             const int k0 = t * W::TILE;
-            load_rows<T, DP, W::TILE, THREADS>(lds + buf * W::STAGE, lds_addr + buf * W::STAGE, keys + (long long)k0 * a.k.row, (int)a.k.row, end - k0, a.D,
-                                               a.direct, wave);
-            load_rows<T, DP, W::TILE, THREADS>(lds + buf * W::STAGE + W::HALF, lds_addr + buf * W::STAGE + W::HALF, values + (long long)k0 * a.v.row,
-                                               (int)a.v.row, end - k0, a.D, a.direct, wave);
+            unsigned char *const to = lds + buf * W::STAGE;
+            const unsigned to_addr = lds_addr + buf * W::STAGE;
+            load_k.issue(to, to_addr, keys + (long long)k0 * a.k.row, end - k0, a.D, wave);
+            load_v.issue(to + W::HALF, to_addr + W::HALF, values + (long long)k0 * a.v.row, end - k0, a.D, wave);
         };
         f32x16 acc[1][R::BLOCKS];
 #pragma unroll
@@ -116,9 +119,11 @@ __global__ __launch_bounds__(THREADS, sizeof(T) == 2 ? 2 : 1) void k_attention_d
 #pragma unroll
             for (int i = 0; i < 16; ++i) acc[0][d][i] = 0.f;
         if (tiles > 0) load(0, 0);
+        bool left_out = false;
         int buf = 0;
         for (int t = 0; t < tiles; ++t, buf ^= 1) {
             tile::wait_loads<0>();
+            if (end - t * W::TILE < W::TILE) load_k.clear(lds + buf * W::STAGE, end - t * W::TILE, wave);
             tile::wait_lds();
             tile::meet();
             if (t + 1 < tiles) load(t + 1, buf ^ 1);
@@ -142,16 +147,10 @@ __global__ __launch_bounds__(THREADS, sizeof(T) == 2 ? 2 : 1) void k_attention_d
                     const float p = __builtin_amdgcn_exp2f(BIAS ? (s[i] - top) - log_sum : fmaf(s[i], a.scale2, -both));
                     ds[0][i] = p * (dp[i] - delta);
                 }
-                unsigned seen[1] = {0xffffu};
                 if (edge) {
-                    seen[0] = 0;
                     const int most = min(a.causal ? pos : end - 1, end - 1) - j0;
 #pragma unroll
-                    for (int i = 0; i < 16; ++i) {
-                        const bool in = row_of(i, half) <= most;
-                        ds[0][i] = in ? ds[0][i] : 0.f;
-                        seen[0] |= in ? 1u << i : 0u;
-                    }
+                    for (int i = 0; i < 16; ++i) ds[0][i] = row_of(i, half) <= most ? ds[0][i] : 0.f;
                 }
                 if constexpr (BIAS) {
                     const int lo = j0 - (lowest + 31), hi = j0 + 31 - lowest;       // offsets of the whole block
@@ -181,17 +180,33 @@ __global__ __launch_bounds__(THREADS, sizeof(T) == 2 ? 2 : 1) void k_attention_d
                         }
                     }
                 }
-                if (border) weigh_seen<T, DP, 1>(reader, ktile, kb, ds, seen, acc);
+                if (border && any_not_finite<T, DP>(ktile, kb)) left_out = true;
                 else weigh<T, DP, 1>(reader, ktile, kb, ds, acc);
+            }
+        }
+        if (left_out) {
+#pragma unroll 1
+            for (int j0 = 0; j0 < end; j0 += 32) {
+                if (j0 + 31 <= lowest || j0 > highest || !any_not_finite<T>(keys + (long long)j0 * a.k.row, a.k.row, end - j0, a.D)) continue;
+                const char *const mine = rows_of(a.q, b, q_ragged, seq.q0 + h_row, head), *const my_grad = rows_of(a.dout, b, q_ragged, seq.q0 + h_row, head);
+#pragma unroll 1
+                for (int j = j0; j < min(end, j0 + 32); ++j) {
+                    if (j > pos || !there) continue;
+                    const char *const key = keys + (long long)j * a.k.row;
+                    const float x = dot<T>(mine, key, a.D), dp = dot<T>(my_grad, values + (long long)j * a.v.row, a.D);
+                    const float p = __builtin_amdgcn_exp2f(BIAS ? (fmaf(x, a.scale2, table[bias_entry(a, j - pos)]) - top) - log_sum : fmaf(x, a.scale2, -both));
+                    add_row<T, DP>(key, a.D, p * (dp - delta), acc[0]);
+                }
             }
         }
         if (there) {
             T *const to = reinterpret_cast<T *>(rows_of(a.dq, b, q_ragged, seq.q0 + row, head));
+            const int D = opaque(a.D), first = opaque(4 * half);
 #pragma unroll
             for (int d = 0; d < 4 * R::BLOCKS; ++d) {
-                const int e = 8 * d + 4 * half;
-                if (e < a.D)
-                    store4(to + e, a.D - e, acc[0][d >> 2][4 * (d & 3)] * a.scale, acc[0][d >> 2][4 * (d & 3) + 1] * a.scale,
+                const int e = first + 8 * d;
+                if (e < D)
+                    store4<T, DIRECT>(to + e, D - e, acc[0][d >> 2][4 * (d & 3)] * a.scale, acc[0][d >> 2][4 * (d & 3) + 1] * a.scale,
                            acc[0][d >> 2][4 * (d & 3) + 2] * a.scale, acc[0][d >> 2][4 * (d & 3) + 3] * a.scale);
             }
         }
@@ -243,7 +258,7 @@ template <typename T> __global__ __launch_bounds__(THREADS) void k_bias_gradient
     if (threadIdx.x == 0) to[c * heads + head] = (T)((sums[0] + sums[1]) + (sums[2] + sums[3]));
 }
 
-template <typename T, int DP, bool BIAS> __global__ __launch_bounds__(THREADS, 1) void k_attention_dkv(Args a)
+template <typename T, int DP, bool BIAS, bool DIRECT> __global__ __launch_bounds__(THREADS, 1) void k_attention_dkv(Args a)
 {
     using W = Backward<T, DP, BIAS>;
     using R = Row<T, DP>;
@@ -269,6 +284,9 @@ template <typename T, int DP, bool BIAS> __global__ __launch_bounds__(THREADS, 1
     const unsigned lds_addr = (unsigned)(size_t)(__attribute__((address_space(3))) unsigned char *)lds;
     Reader<T, DP> reader;
     reader.init();
+    Loader<T, DP, W::TILE, THREADS, DIRECT> load_q, load_g;
+    load_q.init(a.q.row, a.D, tid);
+    load_g.init(a.dout.row, a.D, tid);
     const int rows = a.clear && !k_ragged ? a.k_rows : seq.k_len;       // rows behind the sequence get zeros
     for (int tile0 = first_tile * ROWS; tile0 < rows; tile0 += a.tiles * ROWS) {
         const int mine0 = tile0 + wave * 32, key = mine0 + (lane & 31);
@@ -278,8 +296,8 @@ template <typename T, int DP, bool BIAS> __global__ __launch_bounds__(THREADS, 1
             const char *pk = rows_of(a.k, b, k_ragged, seq.k0 + key, kv_head), *pv = rows_of(a.v, b, k_ragged, seq.k0 + key, kv_head);
 #pragma unroll
             for (int s = 0; s < R::STEPS; ++s) {
-                k[s] = there ? chunk_of<T>(pk, 2 * s + half, a.D) : make_uint4(0, 0, 0, 0);
-                v[s] = there ? chunk_of<T>(pv, 2 * s + half, a.D) : make_uint4(0, 0, 0, 0);
+                k[s] = there ? chunk_of<T, DIRECT>(pk, 2 * s + half, a.D) : make_uint4(0, 0, 0, 0);
+                v[s] = there ? chunk_of<T, DIRECT>(pv, 2 * s + half, a.D) : make_uint4(0, 0, 0, 0);
             }
         }
         const int q_tiles = (seq.q_len + W::TILE - 1) / W::TILE, q_from = a.causal ? min(max(0, tile0 - shift) / W::TILE, q_tiles) : 0;
@@ -287,15 +305,16 @@ template <typename T, int DP, bool BIAS> __global__ __launch_bounds__(THREADS, 1
         auto load = [&](int g, int t, int buf) {
             const int head = kv_head * a.group + g, i0 = t * W::TILE;
             const char *pq = rows_of(a.q, b, q_ragged, seq.q0 + i0, head), *pg = rows_of(a.dout, b, q_ragged, seq.q0 + i0, head);
-            load_rows<T, DP, W::TILE, THREADS>(lds + buf * W::STAGE, lds_addr + buf * W::STAGE, pq, (int)a.q.row, seq.q_len - i0, a.D, a.direct, wave);
-            load_rows<T, DP, W::TILE, THREADS>(lds + buf * W::STAGE + W::HALF, lds_addr + buf * W::STAGE + W::HALF, pg, (int)a.dout.row, seq.q_len - i0,
-                                               a.D, a.direct, wave);
+            unsigned char *const to_tile = lds + buf * W::STAGE;
+            const unsigned to_addr = lds_addr + buf * W::STAGE;
+            load_q.issue(to_tile, to_addr, pq, seq.q_len - i0, a.D, wave);
+            load_g.issue(to_tile + W::HALF, to_addr + W::HALF, pg, seq.q_len - i0, a.D, wave);
             // a plane of facts by each wave: delta behind what the exponents are taken from
             if (wave < W::FACTS && lane < W::TILE) {
                 const int plane = BIAS ? (wave == 0 ? 2 : wave == 1 ? 1 : 3) : wave;
                 const float *from = a.stats + plane * a.plane + (long long)head * a.q_all + seq.q_first + i0;
                 const int to = (buf * W::FACTS + wave) * W::TILE;
-                if (i0 + lane < seq.q_len) tile::load4_to_lds(from, lane * 4, lds_addr + W::TILES_BYTES + to * 4);
+                if (i0 + lane < seq.q_len) bring4(uniform(from), lane * 4, lds_addr + W::TILES_BYTES + to * 4);
                 else facts[to + lane] = wave == 0 ? __builtin_inff() : 0.f;
             }
         };
@@ -304,13 +323,18 @@ template <typename T, int DP, bool BIAS> __global__ __launch_bounds__(THREADS, 1
         for (int d = 0; d < R::BLOCKS; ++d)
 #pragma unroll
             for (int i = 0; i < 16; ++i) dk[0][d][i] = dv[0][d][i] = 0.f;
+        bool left_out = false;
         int g = 0, t = q_from, buf = 0;
         if (count > 0) load(0, q_from, 0);
         for (int c = 0; c < count; ++c, buf ^= 1) {
+            const int g_now = g, i_tile = t * W::TILE;
             tile::wait_loads<0>();
+            if (seq.q_len - i_tile < W::TILE) {
+                load_q.clear(lds + buf * W::STAGE, seq.q_len - i_tile, wave);
+                load_g.clear(lds + buf * W::STAGE + W::HALF, seq.q_len - i_tile, wave);
+            }
             tile::wait_lds();
             tile::meet();
-            const int g_now = g, i_tile = t * W::TILE;
             if (++t == q_tiles) {
                 t = q_from;
                 ++g;
@@ -352,21 +376,47 @@ template <typename T, int DP, bool BIAS> __global__ __launch_bounds__(THREADS, 1
                         ds[0][i] = p[0][i] * (dp[i] - delta[e]);
                     }
                 }
-                unsigned seen[1] = {0xffffu};
                 if (border) {
-                    seen[0] = 0;
 #pragma unroll
                     for (int i = 0; i < 16; ++i) {
                         const bool in = key <= p0 + row_of(i, half);
                         p[0][i] = in ? p[0][i] : 0.f;
                         ds[0][i] = in ? ds[0][i] : 0.f;
-                        seen[0] |= in ? 1u << i : 0u;
                     }
-                    weigh_seen<T, DP, 1>(reader, gtile, rb, p, seen, dv);
-                    weigh_seen<T, DP, 1>(reader, qtile, rb, ds, seen, dk);
+                }
+                if (border && (any_not_finite<T, DP>(gtile, rb) || any_not_finite<T, DP>(qtile, rb))) {
+                    left_out = true;
                 } else {
                     weigh<T, DP, 1>(reader, gtile, rb, p, dv);
                     weigh<T, DP, 1>(reader, qtile, rb, ds, dk);
+                }
+            }
+        }
+        if (left_out) {
+            const char *const mine = rows_of(a.k, b, k_ragged, seq.k0 + min(key, seq.k_len - 1), kv_head),
+                             *const my_value = rows_of(a.v, b, k_ragged, seq.k0 + min(key, seq.k_len - 1), kv_head);
+#pragma unroll 1
+            for (int h = kv_head * a.group; h < (kv_head + 1) * a.group; ++h) {
+#pragma unroll 1
+                for (int i0 = q_from * W::TILE; i0 < seq.q_len && shift + i0 < mine0 + 31; i0 += 32) {
+                    const char *const pq = rows_of(a.q, b, q_ragged, seq.q0 + i0, h), *const pg = rows_of(a.dout, b, q_ragged, seq.q0 + i0, h);
+                    if (shift + i0 + 31 < mine0 || (!any_not_finite<T>(pg, a.dout.row, seq.q_len - i0, a.D) && !any_not_finite<T>(pq, a.q.row, seq.q_len - i0, a.D)))
+                        continue;
+#pragma unroll 1
+                    for (int i = i0; i < min(seq.q_len, i0 + 32); ++i) {
+                        if (key > shift + i || !there) continue;
+                        const char *const row_q = pq + (long long)(i - i0) * a.q.row, *const row_g = pg + (long long)(i - i0) * a.dout.row;
+                        const float *const fact = a.stats + (long long)h * a.q_all + seq.q_first + i;
+                        float x = dot<T>(row_q, mine, a.D) * a.scale2;
+                        if constexpr (BIAS) {
+                            const int at = bucket_of(a.bias, key - shift - i) * a.heads + h;
+                            x += (a.bias.f32 ? ((const float *)a.bias.table)[at] : (float)((const __bf16 *)a.bias.table)[at]) * 1.44269504f;
+                        }
+                        const float p = __builtin_amdgcn_exp2f((x - fact[2 * a.plane]) - fact[3 * a.plane]);
+                        const float ds = p * (dot<T>(row_g, my_value, a.D) - fact[a.plane]);
+                        add_row<T, DP>(row_g, a.D, p, dv[0]);
+                        add_row<T, DP>(row_q, a.D, ds, dk[0]);
+                    }
                 }
             }
         }
@@ -375,12 +425,13 @@ template <typename T, int DP, bool BIAS> __global__ __launch_bounds__(THREADS, 1
                     *const to_v = reinterpret_cast<T *>(rows_of(a.dv, b, k_ragged, seq.k0 + key, kv_head));
             // (a row behind the sequence: zeros, whatever the weights of its zeros came to)
             auto of = [&](float x) { return there ? x : 0.f; };
+            const int D = opaque(a.D), first = opaque(4 * half);
 #pragma unroll
             for (int d = 0; d < 4 * R::BLOCKS; ++d) {
-                const int e = 8 * d + 4 * half, x = d >> 2, y = 4 * (d & 3);
-                if (e >= a.D) continue;
-                store4(to_k + e, a.D - e, of(dk[0][x][y] * a.scale), of(dk[0][x][y + 1] * a.scale), of(dk[0][x][y + 2] * a.scale), of(dk[0][x][y + 3] * a.scale));
-                store4(to_v + e, a.D - e, of(dv[0][x][y]), of(dv[0][x][y + 1]), of(dv[0][x][y + 2]), of(dv[0][x][y + 3]));
+                const int e = first + 8 * d, x = d >> 2, y = 4 * (d & 3);
+                if (e >= D) continue;
+                store4<T, DIRECT>(to_k + e, D - e, of(dk[0][x][y] * a.scale), of(dk[0][x][y + 1] * a.scale), of(dk[0][x][y + 2] * a.scale), of(dk[0][x][y + 3] * a.scale));
+                store4<T, DIRECT>(to_v + e, D - e, of(dv[0][x][y]), of(dv[0][x][y + 1]), of(dv[0][x][y + 2]), of(dv[0][x][y + 3]));
             }
         }
         tile::wait_loads<0>();

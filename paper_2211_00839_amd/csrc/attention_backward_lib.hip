@@ -1,0 +1,119 @@
+// Attention's backward call.
+#include "attention_host.h"
+#include "attention_backward_kernels.hip"
+
+namespace {
+
+SetUp g_set_up;
+
+int set_up()
+{
+    return g_set_up([](auto t, auto dp, auto bias, auto direct) {
+        using T = decltype(t);
+        constexpr int DP = decltype(dp)::value;
+        constexpr bool BIAS = decltype(bias)::value, DIRECT = decltype(direct)::value;
+        const hipError_t e = raise_lds(&k_attention_dq<T, DP, BIAS, DIRECT>);
+        return e != hipSuccess ? e : raise_lds(&k_attention_dkv<T, DP, BIAS, DIRECT>);
+    });
+}
+
+// Workgroups of 128 rows for each sequence and head of the gradients' kernels.
+int64_t tiles_of(int64_t longest, int64_t across)
+{
+    const int64_t tiles = std::max<int64_t>(1, attn_rules::ceil_div(longest, 128));
+    return std::max<int64_t>(1, std::min(tiles, attn_rules::MOST_WORKGROUPS / std::max<int64_t>(across, 1)));
+}
+int64_t dq_tiles(const rcd_attention_shape &s)
+{
+    return tiles_of(attn_rules::longest_of(s.longest_q, s.q_rows, s.batch, s.q_offsets_dev != nullptr), (s.batch + 1) * s.heads);
+}
+
+size_t backward_bytes(const rcd_attention_shape &s, void *base, Args *a)
+{
+    Pieces room(base);
+    const size_t plane = up256((size_t)all_rows(s.q_offsets_dev, s.q_rows, s.batch) * s.heads * 4) / 4;
+    float *const stats = room.take(4 * plane);
+    float *const parts = s.bias_dev ? room.take((size_t)s.heads * s.batch * dq_tiles(s) * s.buckets) : nullptr;
+    if (a) {
+        a->stats = stats;
+        a->plane = (long long)plane;
+        a->part_bias = parts;
+    }
+    return room.used;
+}
+
+} // namespace
+
+int rcd_set_up_attention_backward() { return set_up(); }
+
+extern "C" {
+
+size_t rcd_attention_backward_workspace_bytes(const rcd_attention_shape *s)
+{
+    if (check_shape(s) != RCD_OK) return 0;
+    return backward_bytes(*s, nullptr, nullptr);
+}
+
+int rcd_attention_backward(const rcd_attention_shape *s, const rcd_heads *dout, const rcd_heads *q, const rcd_heads *k, const rcd_heads *v,
+                           const rcd_heads *out, const float *saved_dev, const rcd_heads *dq, const rcd_heads *dk, const rcd_heads *dv, void *dbias_dev,
+                           int clear, void *workspace_dev, size_t workspace_bytes, void *stream_)
+{
+    hipStream_t stream = (hipStream_t)stream_;
+    ENC_TRY(check_shape(s));
+    for (const rcd_heads *h : {dout, q, out, dq}) ENC_TRY(check_heads(h, s->q_rows, s->batch, s->dt));
+    for (const rcd_heads *h : {k, v, dk, dv}) ENC_TRY(check_heads(h, s->k_rows, s->batch, s->dt));
+    if (!saved_dev && s->q_rows > 0 && s->batch > 0) return RCD_ERR_INVALID_ARG;
+    if (dbias_dev && !s->bias_dev) return RCD_ERR_INVALID_ARG;
+    Args a = args_of(*s);
+    ENC_TRY(check_workspace(workspace_dev, workspace_bytes, backward_bytes(*s, workspace_dev, &a)));
+    ENC_TRY(set_up());
+    a.q = heads_of(q, s->dt);
+    a.k = heads_of(k, s->dt);
+    a.v = heads_of(v, s->dt);
+    a.o = heads_of(out, s->dt);
+    a.dout = heads_of(dout, s->dt);
+    a.dq = heads_of(dq, s->dt);
+    a.dk = heads_of(dk, s->dt);
+    a.dv = heads_of(dv, s->dt);
+    a.saved = const_cast<float *>(saved_dev);
+    a.clear = clear != 0;
+    const int entries = (int)entries_of(*s);
+    if (s->q_rows > 0 && s->batch > 0) {
+        Args x = a;
+        x.tiles = (int)dq_tiles(*s);
+        if (!dbias_dev) x.part_bias = nullptr;
+        const int64_t groups = x.tiles * s->heads * (s->batch + (a.clear && a.q_offsets ? 1 : 0));
+        const bool direct = aligned(a.k, s->d, s->dt) && aligned(a.v, s->d, s->dt);
+        ENC_TRY(with_variant(s->dt, s->d, s->bias_dev != nullptr, direct, [&](auto t, auto dp, auto bias, auto way) {
+            using T = decltype(t);
+            constexpr int DP = decltype(dp)::value;
+            constexpr bool BIAS = decltype(bias)::value, DIRECT = decltype(way)::value;
+            using W = Backward<T, DP, BIAS>;
+            return launch(&k_attention_dq<T, DP, BIAS, DIRECT>, groups, W::TILES_BYTES + (BIAS ? 5 * entries * 4 + 4 * W::TURN_BYTES : 0), x, stream);
+        }));
+    }
+    if (dbias_dev) {
+        const long long count = s->q_rows > 0 ? s->batch * dq_tiles(*s) : 0;
+        const dim3 grid((unsigned)(s->buckets * s->heads));
+        if (s->bias_dt == RCD_F32)
+            hipLaunchKernelGGL((k_bias_gradient<float>), grid, dim3(THREADS), 0, stream, a.part_bias, count, (int)s->buckets, (int)s->heads, (float *)dbias_dev);
+        else
+            hipLaunchKernelGGL((k_bias_gradient<__bf16>), grid, dim3(THREADS), 0, stream, a.part_bias, count, (int)s->buckets, (int)s->heads, (__bf16 *)dbias_dev);
+        ENC_HIP_TRY(hipGetLastError());
+    }
+    if (s->k_rows > 0 && s->batch > 0) {
+        a.tiles = (int)tiles_of(attn_rules::longest_of(s->longest_k, s->k_rows, s->batch, s->k_offsets_dev != nullptr), (s->batch + 1) * s->kv_heads);
+        const int64_t groups = a.tiles * s->kv_heads * (s->batch + (a.clear && a.k_offsets ? 1 : 0));
+        const bool direct = aligned(a.q, s->d, s->dt) && aligned(a.dout, s->d, s->dt);
+        ENC_TRY(with_variant(s->dt, s->d, s->bias_dev != nullptr, direct, [&](auto t, auto dp, auto bias, auto way) {
+            using T = decltype(t);
+            constexpr int DP = decltype(dp)::value;
+            constexpr bool BIAS = decltype(bias)::value, DIRECT = decltype(way)::value;
+            using W = Backward<T, DP, BIAS>;
+            return launch(&k_attention_dkv<T, DP, BIAS, DIRECT>, groups, W::TILES_BYTES + W::FACTS_BYTES + (BIAS ? entries * 4 : 0), a, stream);
+        }));
+    }
+    return RCD_OK;
+}
+
+} // extern "C"

@@ -38,10 +38,10 @@ struct Args {
     int batch, heads, kv_heads, group;  // group: query heads that share a head of k and v
     int q_rows, k_rows;                 // of a sequence; with offsets: of all of them
     int D, pack;                        // pack: query heads whose rows lie side by side in a tile
-    bool causal, clear, direct;         // clear: rows that belong to no sequence become zeros; direct: rows are read 16 bytes at a time
+    bool causal, clear;                 // clear: rows that belong to no sequence become zeros
     float scale, scale2;                // scale2: times log2 e
     Bias bias;
-    int tiles, splits;
+    int tiles, splits, least;           // least: tiles of a split
     float *part_o, *part_ml;            // with splits: their sums, and per row maximum and sum
     float *part_bias;                   // the table's gradient, a part of each workgroup
 };
@@ -53,6 +53,7 @@ struct Sequence {
     int q_len, k_len;
     long long q_first;                  // counted over all sequences
 };
+__device__ __forceinline__ int uniform(int x) { return __builtin_amdgcn_readfirstlane(x); }
 __device__ __forceinline__ Sequence sequence(const Args &a, int b)
 {
     Sequence s;
@@ -61,16 +62,16 @@ __device__ __forceinline__ Sequence sequence(const Args &a, int b)
     s.k_len = a.k_rows;
     s.q_first = (long long)b * a.q_rows;
     if (a.q_offsets) {
-        const int from = min(max(a.q_offsets[b], 0), a.q_rows), to = min(max(a.q_offsets[b + 1], from), a.q_rows);
+        const int from = uniform(min(max(a.q_offsets[b], 0), a.q_rows)), to = uniform(min(max(a.q_offsets[b + 1], from), a.q_rows));
         s.q0 = s.q_first = from;
         s.q_len = to - from;
     }
     if (a.k_offsets) {
-        const int from = min(max(a.k_offsets[b], 0), a.k_rows), to = min(max(a.k_offsets[b + 1], from), a.k_rows);
+        const int from = uniform(min(max(a.k_offsets[b], 0), a.k_rows)), to = uniform(min(max(a.k_offsets[b + 1], from), a.k_rows));
         s.k0 = from;
         s.k_len = to - from;
     } else if (a.k_lengths) {
-        s.k_len = min(max(a.k_lengths[b], 0), a.k_rows);
+        s.k_len = uniform(min(max(a.k_lengths[b], 0), a.k_rows));
     }
     return s;
 }
@@ -100,11 +101,16 @@ template <typename T, int DP> struct Row {
     }
 };
 
-// Chunk `chunk` of a row of D elements at any alignment; what lies behind the row is zeros.
-template <typename T> __device__ __forceinline__ uint4 chunk_of(const char *row, int chunk, int D)
+// Chunk `chunk` of a row of D elements at any alignment; what lies behind the row is zeros.  WHOLE: D is a multiple of a chunk's elements.
+template <typename T, bool WHOLE> __device__ __forceinline__ uint4 chunk_of(const char *row, int chunk, int D)
 {
     constexpr int EACH = 16 / (int)sizeof(T);
     const int count = D - chunk * EACH;
+    if constexpr (WHOLE) {
+        if (count <= 0) return make_uint4(0, 0, 0, 0);
+        const u32x4_any v = *reinterpret_cast<const u32x4_any *>(row + chunk * 16);
+        return make_uint4(v[0], v[1], v[2], v[3]);
+    }
     if (count >= EACH) {
         const u32x4_any v = *reinterpret_cast<const u32x4_any *>(row + chunk * 16);
         return make_uint4(v[0], v[1], v[2], v[3]);
@@ -120,10 +126,17 @@ template <typename T> __device__ __forceinline__ uint4 chunk_of(const char *row,
     return make_uint4(w[0], w[1], w[2], w[3]);
 }
 
-// `count` consecutive elements (at most four) of a row of results.
-template <typename T> __device__ __forceinline__ void store4(T *p, int count, float a, float b, float c, float d)
+// A value of which the compiler knows nothing: what is made of it is made where it is used, not kept in registers through the loops before.
+__device__ __forceinline__ int opaque(int x)
 {
-    if (count >= 4) {
+    asm volatile("" : "+v"(x));
+    return x;
+}
+
+// `count` consecutive elements (at most four; WHOLE: four) of a row of results.
+template <typename T, bool WHOLE> __device__ __forceinline__ void store4(T *p, int count, float a, float b, float c, float d)
+{
+    if (WHOLE || count >= 4) {
         if constexpr (sizeof(T) == 4) {
             *reinterpret_cast<f32x4_any *>(p) = f32x4{a, b, c, d};
         } else {
@@ -139,30 +152,98 @@ template <typename T> __device__ __forceinline__ void store4(T *p, int count, fl
         if (i < count) p[i] = (T)v[i];
 }
 
-// Loads ROWS rows to `lds` (lds_addr: the same, as an address), LOADERS threads together; wave: which of theirs this one is.  `rows` of them
-// exist; the others, and what lies behind D, become zeros, which no weight of zero turns into anything else.
-template <typename T, int DP, int ROWS, int LOADERS>
-__device__ __forceinline__ void load_rows(unsigned char *lds, unsigned lds_addr, const char *base, int pitch, int rows, int D, bool direct, int wave)
+// 16 or 4 bytes of each lane to LDS.  The base may have been put into its scalar registers by a vector instruction right before (a register that
+// was held in a lane of another one comes back so), which a memory instruction may follow only after five wait states; the compiler does
+// not see into the asm and puts none there.
+__device__ __forceinline__ const void *uniform(const void *p)
 {
+    const unsigned long long x = (unsigned long long)p;
+    const unsigned lo = __builtin_amdgcn_readfirstlane((unsigned)x), hi = __builtin_amdgcn_readfirstlane((unsigned)(x >> 32));
+    return (const void *)(((unsigned long long)hi << 32) | lo);
+}
+__device__ __forceinline__ void bring16(const void *base, unsigned offset, unsigned lds_addr)
+{
+    asm volatile("s_nop 4\n\t"
+                 "global_load_lds_dwordx4 %0, %1"
+                 :
+                 : "v"(offset), "s"(base), "{m0}"(lds_addr)
+                 : "memory");
+}
+__device__ __forceinline__ void bring4(const void *base, unsigned offset, unsigned lds_addr)
+{
+    asm volatile("s_nop 4\n\t"
+                 "global_load_lds_dword %0, %1"
+                 :
+                 : "v"(offset), "s"(base), "{m0}"(lds_addr)
+                 : "memory");
+}
+
+// Brings ROWS rows of a matrix to LDS, LOADERS threads together, each always the same places of a tile.  DIRECT: straight from memory (all rows
+// 16-byte aligned, D a multiple of 16 bytes; what lies behind D then holds other elements of the row, which meet zeros on the other side or lead
+// to results that are not stored), else through the registers with zeros behind D.  Of a last tile's rows that do not exist the last one stands in
+// until clear() puts zeros there, which no weight of zero turns into anything else.
+template <typename T, int DP, int ROWS, int LOADERS, bool DIRECT> struct Loader {
     using R = Row<T, DP>;
-    constexpr int N = ROWS * R::CHUNKS / LOADERS;
-    static_assert(N * LOADERS == ROWS * R::CHUNKS, "whole rounds");
-    const int lane = threadIdx.x & 63;
-    const bool whole = direct && rows >= ROWS && D == DP;
+    static constexpr int N = ROWS * R::CHUNKS / LOADERS, STEP = LOADERS / R::CHUNKS;       // rounds; rows from round to round
+    static constexpr int KINDS = STEP >= 16 ? 1 : 16 / STEP < N ? 16 / STEP : N;          // (rows 16 apart are turned alike)
+    static_assert(N * LOADERS == ROWS * R::CHUNKS && STEP >= 1, "whole rounds");
+    int row, pitch;
+    unsigned off[KINDS];
+    int chunk[DIRECT ? 1 : KINDS];
+    __device__ __forceinline__ void init(long long pitch_, int D, int t)
+    {
+        row = t / R::CHUNKS;
+        pitch = (int)pitch_;
 #pragma unroll
-    for (int u = 0; u < N; ++u) {
-        const int at = u * LOADERS + wave * 64;
-        const int ci = at + lane, row = ci / R::CHUNKS, chunk = (ci % R::CHUNKS) ^ R::turn(row);
-        if (whole) {
-            tile::load16_to_lds(base, (unsigned)(row * pitch + chunk * 16), lds_addr + at * 16);
-        } else {
-            const bool there = row < rows && chunk * R::EACH < D;
-            if (there && direct) tile::load16_to_lds(base, (unsigned)(row * pitch + chunk * 16), lds_addr + at * 16);
-            else *reinterpret_cast<uint4 *>(lds + ci * 16) = there ? chunk_of<T>(base + (unsigned)(row * pitch), chunk, D) : make_uint4(0, 0, 0, 0);
+        for (int i = 0; i < KINDS; ++i) {
+            const int c = (t % R::CHUNKS) ^ R::turn(row + i * STEP);
+            if constexpr (DIRECT) {
+                off[i] = (unsigned)(row * pitch + min(c, D / R::EACH - 1) * 16);
+            } else {
+                chunk[i] = c;
+            }
         }
     }
-}
-template <typename T, int DP, int ROWS, int LOADERS> constexpr int loads_of() { return ROWS * Row<T, DP>::CHUNKS / LOADERS; }
+    // wave: which of the loaders' waves this is
+    __device__ __forceinline__ void issue(unsigned char *lds, unsigned lds_addr, const char *base, int rows, int D, int wave) const
+    {
+        if constexpr (DIRECT) {
+            base = (const char *)uniform(base);
+            if (rows >= ROWS) {
+#pragma unroll
+                for (int u = 0; u < N; ++u) bring16(base, off[u % KINDS] + (unsigned)(u * STEP * pitch), lds_addr + (u * LOADERS + wave * 64) * 16);
+            } else {
+#pragma unroll 1
+                for (int u = 0; u < N; ++u) {
+                    const int r = min(row + u * STEP, rows - 1);
+                    unsigned o = off[0];
+#pragma unroll
+                    for (int i = 1; i < KINDS; ++i) o = u % KINDS == i ? off[i] : o;
+                    bring16(base, o + (unsigned)((r - row) * pitch), lds_addr + (u * LOADERS + wave * 64) * 16);
+                }
+            }
+        } else {
+            const int lane = threadIdx.x & 63;
+#pragma unroll
+            for (int u = 0; u < N; ++u) {
+                const int r = row + u * STEP;
+                const bool there = r < rows && chunk[u % KINDS] * R::EACH < D;
+                *reinterpret_cast<uint4 *>(lds + (u * LOADERS + wave * 64 + lane) * 16) =
+                    there ? chunk_of<T, false>(base + (unsigned)(r * pitch), chunk[u % KINDS], D) : make_uint4(0, 0, 0, 0);
+            }
+        }
+    }
+    // Once the loads are in.
+    __device__ __forceinline__ void clear(unsigned char *lds, int rows, int wave) const
+    {
+        if constexpr (DIRECT) {
+            const int lane = threadIdx.x & 63;
+#pragma unroll 1
+            for (int u = 0; u < N; ++u)
+                if (row + u * STEP >= rows) *reinterpret_cast<uint4 *>(lds + (u * LOADERS + wave * 64 + lane) * 16) = make_uint4(0, 0, 0, 0);
+        }
+    }
+};
 
 // Where this lane reads: its row's chunks, and the transposed ones.
 template <typename T, int DP> struct Reader {
@@ -248,63 +329,70 @@ __device__ __forceinline__ void weigh(const Reader<T, DP> &at, const unsigned ch
     }
 }
 
-// Is there an infinity or a NaN in 32 rows of a tile?
+// ---- infinities and NaN at the border of what may be seen -----------------------------------------------------------------
+//
+// A row that is not seen has no part in a sum at all, where a weight of zero would make a NaN of an infinity.  Only blocks on the causal
+// border are weighed for lanes that do not see all of their rows; one that holds something that is not finite is left out there, and added row by row
+// once everything else is done.  Rare: what it takes is code behind the loops, not time or registers in them.
+
+// The largest size among a chunk's elements, as bits; and whether it is a number's.
+template <typename T> __device__ __forceinline__ unsigned largest(const uint4 &v, unsigned m)
+{
+    const unsigned w[4] = {v.x, v.y, v.z, v.w};
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        if constexpr (sizeof(T) == 4) {
+            m = max(m, w[i] & 0x7fffffffu);
+        } else {
+            typedef unsigned short u16x2 __attribute__((ext_vector_type(2)));
+            m = __builtin_bit_cast(unsigned, __builtin_elementwise_max(__builtin_bit_cast(u16x2, m), __builtin_bit_cast(u16x2, w[i] & 0x7fff7fffu)));
+        }
+    }
+    return m;
+}
+template <typename T> __device__ __forceinline__ bool any_not_finite(unsigned m)
+{
+    return __any(sizeof(T) == 4 ? m >= 0x7f800000u : m >= 0x7f800000u || (m & 0xffffu) >= 0x7f80u);
+}
+// Of 32 rows of a tile.
 template <typename T, int DP> __device__ __forceinline__ bool any_not_finite(const unsigned char *tile, int block)
 {
     using R = Row<T, DP>;
     const int lane = threadIdx.x & 63;
-    bool bad = false;
+    unsigned m = 0;
 #pragma unroll
-    for (int u = 0; u < 32 * R::CHUNKS / 64; ++u) {
-        const uint4 v = *reinterpret_cast<const uint4 *>(tile + block * 32 * R::BYTES + (u * 64 + lane) * 16);
-        const unsigned w[4] = {v.x, v.y, v.z, v.w};
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            bad |= (w[i] & 0x7f800000u) == 0x7f800000u;
-            if constexpr (sizeof(T) == 2) bad |= (w[i] & 0x7f80u) == 0x7f80u;
-        }
-    }
-    return __any(bad);
+    for (int u = 0; u < 32 * R::CHUNKS / 64; ++u)
+        m = largest<T>(*reinterpret_cast<const uint4 *>(tile + block * 32 * R::BYTES + (u * 64 + lane) * 16), m);
+    return any_not_finite<T>(m);
 }
-
-// weigh() for a block on the border of what may be seen: `seen` has a bit for each register.  A row that is not seen has no part in a sum at
-// all, also where it is not finite and its weight of zero would make a NaN of it; such rows are rare, and then each row is added by itself.
-template <typename T, int DP, int N>
-__device__ __forceinline__ void weigh_seen(const Reader<T, DP> &at, const unsigned char *tile, int block, const f32x16 (&p)[N], const unsigned (&seen)[N],
-                                           f32x16 (&acc)[N][DP / 32])
+// The same of up to 32 rows in memory.
+template <typename T> __device__ __forceinline__ bool any_not_finite(const char *rows, long long pitch, int count, int D)
 {
-    using R = Row<T, DP>;
-    if (!any_not_finite<T, DP>(tile, block)) {
-        weigh<T, DP, N>(at, tile, block, p, acc);
-        return;
-    }
-    const int half = (threadIdx.x & 63) >> 5;
+    const int lane = threadIdx.x & 63, r = lane & 31;
+    unsigned m = 0;
+    if (r < count)
 #pragma unroll 1
-    for (int r = 0; r < 32; ++r) {
-        const int reg = ((r >> 3) << 2) | (r & 3), owner = (r >> 2) & 1;
+        for (int c = lane >> 5; c * (16 / (int)sizeof(T)) < D; c += 2) m = largest<T>(chunk_of<T, false>(rows + r * pitch, c, D), m);
+    return any_not_finite<T>(m);
+}
+template <typename T> __device__ __forceinline__ float dot(const char *a, const char *b, int D)
+{
+    float sum = 0.f;
+#pragma unroll 1
+    for (int d = 0; d < D; ++d) sum = fmaf(to_f32(reinterpret_cast<const T *>(a)[d]), to_f32(reinterpret_cast<const T *>(b)[d]), sum);
+    return sum;
+}
+// acc += weight row
+template <typename T, int DP> __device__ __forceinline__ void add_row(const char *row, int D, float weight, f32x16 (&acc)[DP / 32])
+{
+    const int first = opaque(4 * ((threadIdx.x & 63) >> 5));
 #pragma unroll
-        for (int n = 0; n < N; ++n) {
-            float w = 0.f;
+    for (int b = 0; b < DP / 32; ++b)
 #pragma unroll
-            for (int i = 0; i < 16; ++i) w = i == reg ? p[n][i] : w;
-            int there = (seen[n] >> reg) & 1;
-            const float other = __shfl_xor(w, 32);
-            const int there_too = __shfl_xor(there, 32);
-            if (owner != half) {
-                w = other;
-                there = there_too;
-            }
-#pragma unroll
-            for (int b = 0; b < R::BLOCKS; ++b)
-#pragma unroll
-                for (int i = 0; i < 16; ++i) {
-                    const int d = 32 * b + row_of(i, half);
-                    const T v = *reinterpret_cast<const T *>(tile + (block * 32 + r) * R::BYTES + (((d / R::EACH) ^ R::turn(r)) << 4) +
-                                                             (d % R::EACH) * (int)sizeof(T));
-                    if (there) acc[n][b][i] = fmaf(w, to_f32(v), acc[n][b][i]);
-                }
+        for (int i = 0; i < 16; ++i) {
+            const int d = min(first + 32 * b + row_of(i, 0), D - 1);        // (what lies behind D is not stored)
+            acc[b][i] = fmaf(weight, to_f32(reinterpret_cast<const T *>(row)[d]), acc[b][i]);
         }
-    }
 }
 
 // Both halves' values.

@@ -8,6 +8,8 @@ namespace attn_rules {
 constexpr int64_t MOST_WORKGROUPS = ((int64_t)1 << 24) - 8;     // a launch stays below 2^32 threads
 inline int64_t ceil_div(int64_t a, int64_t b) { return (a + b - 1) / b; }
 
+constexpr int64_t MOST_SPLITS = 512;
+
 // How long a sequence is taken to be where the caller does not say: four times the mean, all there is at most.  (Longer ones are
 // gone through all the same, by fewer workgroups.)
 inline int64_t longest_of(int64_t said, int64_t rows, int64_t batch, bool ragged)
@@ -22,6 +24,7 @@ struct Cut {
     int blocks;         // blocks of 32 rows in each wave
     int64_t tiles;      // workgroups for each sequence and (packed) head
     int64_t splits;     // parts of the keys
+    int64_t least;      // tiles of 32 keys (keys false: 64) in a part, unless there are fewer
 };
 
 // bias_entries: floats of the bias for each head, 0 without one.  resident: a workgroup's tiles take an unpacked compute unit each.
@@ -38,9 +41,13 @@ inline Cut cut_of(int64_t batch, int64_t heads, int64_t group, int64_t longest_q
     c.tiles = std::max<int64_t>(1, std::min(c.tiles, MOST_WORKGROUPS / std::max<int64_t>(across, 1)));
     const int64_t groups = c.tiles * across;
     c.splits = 1;
-    if (groups < 256 && groups > 0) {
-        const int64_t least = c.keys ? 512 : 1024;      // keys of a part
-        c.splits = std::max<int64_t>(1, std::min(512 / groups, longest_k / least));
+    c.least = 1;
+    if (groups < 1024 && groups > 0) {
+        const int64_t least = c.keys ? (f32 ? 128 : 512) : 1024;            // keys of a part
+        // as many parts as fill the compute units once; more where sequences may differ in length, since the longest is what is waited for
+        const int64_t wanted = std::max<int64_t>(256 / groups, longest_k / 1024);
+        c.splits = std::max<int64_t>(1, std::min({wanted, longest_k / least, 1024 / groups, MOST_SPLITS}));
+        c.least = least / (c.keys ? 32 : 64);
     }
     return c;
 }

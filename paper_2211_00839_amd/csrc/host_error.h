@@ -11,6 +11,7 @@ __attribute__((visibility("hidden"))) int rcd_note_hip_error(const char *what, h
 // The encoder's part of rcd_init(): what its kernels need once per device.
 __attribute__((visibility("hidden"))) int rcd_set_up_encoder();
 __attribute__((visibility("hidden"))) int rcd_set_up_attention();
+__attribute__((visibility("hidden"))) int rcd_set_up_attention_backward();
 
 #define ENC_HIP_TRY(expr)                                            \
     do {                                                             \

@@ -1713,6 +1713,7 @@ int rcd_init(void)
     RCD_TRY(static_setup(nullptr));
     RCD_TRY(rcd_set_up_encoder());
     RCD_TRY(rcd_set_up_attention());
+    RCD_TRY(rcd_set_up_attention_backward());
     return RCD_OK;
 }
 

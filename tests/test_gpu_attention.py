@@ -112,3 +112,39 @@ def test_ragged_queries_over_a_cache(dtype):
     for causal in (False, True):
         forward_and_backward(q, k, v, dout, sequences, None, 128, causal=causal, q_offsets=torch.tensor(offsets, dtype=torch.int32, device=DEV),
                              k_lengths=torch.tensor(lengths, dtype=torch.int32, device=DEV))
+
+
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+@pytest.mark.parametrize("d", [64, 33, 128])
+@pytest.mark.parametrize("n", [30, 200])
+def test_nothing_comes_from_what_is_not_seen(n, d, dtype):
+    """Causal: a key and value of NaN and infinities reaches no query in front of it, a query and gradient of them no key behind it."""
+    gen = generator(n, d, 5)
+    heads, kv, bad = 4, 2, n - 20
+    q, dout = normal(gen, 1, n, heads, d, dtype=dtype), normal(gen, 1, n, heads, d, dtype=dtype)
+    k, v = normal(gen, 1, n, kv, d, dtype=dtype), normal(gen, 1, n, kv, d, dtype=dtype)
+    value, bound = ref.attention(q, k, v, None, True, ref.padded(1, [n]), None, 128, dout)
+    for bias in (None, torch.zeros(8, heads, device=DEV)):
+        for fill in (float("nan"), float("inf")):
+            k2, v2 = k.clone(), v.clone()
+            k2[:, bad], v2[:, bad, :, ::2] = fill, fill
+            out, saved = rcd.attention(q, k2, v2, causal=True, bias=bias, want_saved=True)
+            grads = rcd.attention_backward(dout, q, k2, v2, out, saved, causal=True, bias=bias)
+            ref.check("out", out[:, :bad], value["out"][:, :bad], bound["out"][:, :bad])
+            ref.check("dq", grads.dq[:, :bad], value["dq"][:, :bad], bound["dq"][:, :bad])
+            # an infinite value alone: where it stands, and in every query that sees it
+            v3 = v.clone()
+            v3[:, bad, :, 0] = fill
+            out = rcd.attention(q, k, v3, causal=True, bias=bias)
+            assert not out[:, bad:, :, 0].isfinite().any()
+            ref.check("out", out[:, :bad], value["out"][:, :bad], bound["out"][:, :bad])
+            ref.check("out", out[:, :, :, 1:], value["out"][:, :, :, 1:], bound["out"][:, :, :, 1:])
+            q2, dout2 = q.clone(), dout.clone()
+            q2[:, bad, :, 1::2], dout2[:, bad] = fill, fill
+            out, saved = rcd.attention(q2, k, v, causal=True, bias=bias, want_saved=True)
+            grads = rcd.attention_backward(dout2, q2, k, v, out, saved, causal=True, bias=bias)
+            rest = [i for i in range(n) if i != bad]
+            ref.check("out", out[:, rest], value["out"][:, rest], bound["out"][:, rest])
+            ref.check("dq", grads.dq[:, rest], value["dq"][:, rest], bound["dq"][:, rest])
+            for name in ("dk", "dv"):
+                ref.check(name, getattr(grads, name)[:, bad + 1:], value[name][:, bad + 1:], bound[name][:, bad + 1:])
