@@ -12,22 +12,65 @@
 
 namespace attn {
 
-template <typename T, int DP, bool BIAS> struct Backward {
+// SHARED false: a workgroup's four waves have 32 rows each and share the tiles they go along; true, where that would make few workgroups: they
+// have the same 32 rows, go along every fourth tile of 32 each by itself, and add up at the end.
+template <typename T, int DP, bool SHARED, bool BIAS> struct Backward {
     using R = Row<T, DP>;
-    static constexpr int TILE = R::BYTES == 512 || (BIAS && R::BYTES == 256) ? 32 : 64;         // rows in LDS at once
-    static constexpr int HALF = TILE * R::BYTES, STAGE = 2 * HALF, TILES_BYTES = 2 * STAGE;
+    static constexpr int ROWS = SHARED ? 32 : 128, LOADERS = SHARED ? 64 : THREADS;
+    static constexpr int TILE = SHARED || R::BYTES == 512 || (BIAS && R::BYTES == 256) ? 32 : 64;       // rows in LDS at once
+    static constexpr int STAGES = SHARED && (R::BYTES == 512 || (BIAS && R::BYTES == 256)) ? 1 : 2;
+    static constexpr int HALF = TILE * R::BYTES, STAGE = 2 * HALF, TILES_BYTES = STAGES * STAGE * (SHARED ? 4 : 1);
+    static constexpr int LOADS = 2 * TILE * R::CHUNKS / LOADERS;
     // gradients of k and v: what is known of each query of a tile
-    static constexpr int FACTS = BIAS ? 3 : 2, FACTS_BYTES = 2 * FACTS * TILE * 4;
+    static constexpr int FACTS = BIAS ? 3 : 2, FACTS_STAGE = FACTS * TILE, FACTS_BYTES = STAGES * FACTS_STAGE * 4 * (SHARED ? 4 : 1);
     // the bias's gradient: a wave's block of ds on its way to the sums along its diagonals
     static constexpr int TURN_PITCH = 40, TURN_BYTES = 32 * TURN_PITCH * 4;
+    static_assert(!SHARED || 4 * DP * 32 * 4 <= TILES_BYTES, "the waves' sums fit where the tiles were");
 };
 
-template <typename T, int DP, bool BIAS, bool DIRECT>
-__global__ __launch_bounds__(THREADS, sizeof(T) == 2 ? 2 : 1) void k_attention_dq(Args a)
+// The four waves' sums, a quarter of the elements in each wave: groups of four elements from 8 wave BLOCKS on.  Every wave has to come along.
+template <int BLOCKS> __device__ __forceinline__ void add_waves(unsigned char *lds, f32x16 (&acc)[BLOCKS])
 {
-    using W = Backward<T, DP, BIAS>;
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    float *const sums = reinterpret_cast<float *>(lds);
+    tile::wait_lds();
+    tile::meet();
+#pragma unroll
+    for (int d = 0; d < BLOCKS; ++d)
+#pragma unroll
+        for (int i = 0; i < 16; ++i) sums[((wave * BLOCKS + d) * 16 + i) * 64 + lane] = acc[d][i];
+    tile::wait_lds();
+    tile::meet();
+#pragma unroll
+    for (int g = 0; g < BLOCKS; ++g)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+            float v = 0.f;
+#pragma unroll
+            for (int w = 0; w < 4; ++w) v += sums[((w * BLOCKS * 4 + wave * BLOCKS + g) * 4 + e) * 64 + lane];
+            acc[g >> 2][4 * (g & 3) + e] = v;
+        }
+}
+// Rows of results: groups of four elements from element `first` on, as many as there are in `acc` (shared: of this wave's quarter).
+template <typename T, int BLOCKS, int GROUPS, bool WHOLE>
+__device__ __forceinline__ void store_row(T *to, int first, int D_, float scale, bool there, const f32x16 (&acc)[BLOCKS])
+{
+    const int D = opaque(D_), e0 = opaque(first);
+    // (a row behind its sequence: zeros, whatever the weights of its zeros came to)
+    auto of = [&](float x) { return there ? x * scale : 0.f; };
+#pragma unroll
+    for (int g = 0; g < GROUPS; ++g) {
+        const int e = e0 + 8 * g, x = g >> 2, y = 4 * (g & 3);
+        if (e < D) store4<T, WHOLE>(to + e, D - e, of(acc[x][y]), of(acc[x][y + 1]), of(acc[x][y + 2]), of(acc[x][y + 3]));
+    }
+}
+
+template <typename T, int DP, bool SHARED, bool BIAS, bool DIRECT>
+__global__ __launch_bounds__(THREADS, sizeof(T) == 2 && !SHARED ? 2 : 1) void k_attention_dq(Args a)
+{
+    using W = Backward<T, DP, SHARED, BIAS>;
     using R = Row<T, DP>;
-    constexpr int ROWS = 128, BLOCKS = W::TILE / 32;
+    constexpr int BLOCKS = W::TILE / 32;
     extern __shared__ __align__(1024) unsigned char lds[];
     const int tid = threadIdx.x, lane = tid & 63, half = lane >> 5, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int total = a.tiles * a.heads * (a.batch + (a.clear && a.q_offsets ? 1 : 0));
@@ -41,42 +84,67 @@ __global__ __launch_bounds__(THREADS, sizeof(T) == 2 ? 2 : 1) void k_attention_d
         return;
     }
     const Sequence seq = sequence(a, b);
+    const int buckets = a.bias.buckets, all = a.bias.both ? 2 * buckets : buckets;
+    float *const part = BIAS && a.part_bias ? a.part_bias + (((long long)head * a.batch + b) * a.tiles + first_tile) * all : nullptr;
+    if (first_tile * W::ROWS >= seq.q_len) {
+        if (part)
+            for (int c = tid; c < all; c += THREADS) part[c] = 0.f;
+        return;
+    }
     const int kv_head = head / a.group, shift = seq.k_len - seq.q_len;
     const bool q_ragged = a.q_offsets != nullptr, k_ragged = a.k_offsets != nullptr;
     const char *const keys = rows_of(a.k, b, k_ragged, seq.k0, kv_head), *const values = rows_of(a.v, b, k_ragged, seq.k0, kv_head);
-    const int entries = BIAS ? bias_entries(a) : 0, reach = a.bias.reach;
+    const int reach = a.bias.reach, width = BIAS ? bias_width(reach, a.causal) : 0, entries = BIAS ? bias_entries(reach, a.causal) : 0;
     float *const table = reinterpret_cast<float *>(lds + W::TILES_BYTES);
-    float *const turn = reinterpret_cast<float *>(lds + W::TILES_BYTES + wave * W::TURN_BYTES) + entries;
-    float *const near = reinterpret_cast<float *>(lds + W::TILES_BYTES + 4 * W::TURN_BYTES) + entries;       // [wave][entries]
-    float *const mine_near = near + wave * entries;
+    float *const turn = reinterpret_cast<float *>(lds + W::TILES_BYTES + wave * W::TURN_BYTES) + width;
+    float *const nears = reinterpret_cast<float *>(lds + W::TILES_BYTES + 4 * W::TURN_BYTES) + width;         // [wave][entries]
+    float *const mine_near = nears + wave * entries;
     float far_before = 0.f, far_behind = 0.f;
     if constexpr (BIAS) {
-        fill_bias(a, head, table);
+        fill_bias(a, head, 1, table);
         for (int e = lane; e < entries; e += 64) mine_near[e] = 0.f;
+        tile::wait_lds();
+        tile::meet();
     }
-    const unsigned lds_addr = (unsigned)(size_t)(__attribute__((address_space(3))) unsigned char *)lds;
+    unsigned char *const stages = lds + (SHARED ? wave * W::STAGES * W::STAGE : 0);
+    const unsigned stages_addr = (unsigned)(size_t)(__attribute__((address_space(3))) unsigned char *)lds + (SHARED ? wave * W::STAGES * W::STAGE : 0);
+    const int loader = SHARED ? 0 : wave;
     Reader<T, DP> reader;
     reader.init();
-    Loader<T, DP, W::TILE, THREADS, DIRECT> load_k, load_v;
-    load_k.init(a.k.row, a.D, tid);
-    load_v.init(a.v.row, a.D, tid);
-    for (int tile0 = first_tile * ROWS; tile0 < seq.q_len; tile0 += a.tiles * ROWS) {
-        const int mine0 = tile0 + wave * 32, row = mine0 + (lane & 31), h_row = min(row, seq.q_len - 1), pos = shift + h_row;
+    Loader<T, DP, W::TILE, W::LOADERS, DIRECT> load_k, load_v;
+    load_k.init(a.k.row, a.D, SHARED ? lane : tid);
+    load_v.init(a.v.row, a.D, SHARED ? lane : tid);
+    for (int tile0 = first_tile * W::ROWS; tile0 < seq.q_len; tile0 += a.tiles * W::ROWS) {
+        const int mine0 = tile0 + (SHARED ? 0 : wave * 32), row = mine0 + (lane & 31), h_row = min(row, seq.q_len - 1), pos = shift + h_row;
         const bool there = row < seq.q_len;
         const long long place = seq.q_first + h_row;
+        const int last = shift + min(tile0 + W::ROWS, seq.q_len) - 1, end = a.causal ? max(0, min(seq.k_len, last + 1)) : seq.k_len;
+        const int lowest = shift + mine0, highest = shift + min(mine0 + 32, seq.q_len) - 1;
+        const int tiles = (end + W::TILE - 1) / W::TILE, t0 = SHARED ? wave : 0, step = SHARED ? 4 : 1;
+        auto load = [&](int t, int buf) {
+            const int k0 = t * W::TILE;
+            unsigned char *const to = stages + buf * W::STAGE;
+            const unsigned to_addr = stages_addr + buf * W::STAGE;
+            load_k.issue(to, to_addr, keys + (long long)k0 * a.k.row, end - k0, a.D, loader);
+            load_v.issue(to + W::HALF, to_addr + W::HALF, values + (long long)k0 * a.v.row, end - k0, a.D, loader);
+        };
+        if (W::STAGES == 2 && t0 < tiles) load(t0, 0);
         uint4 q[R::STEPS], g[R::STEPS];
         float delta = 0.f;
         {
             const char *pq = rows_of(a.q, b, q_ragged, seq.q0 + h_row, head), *pg = rows_of(a.dout, b, q_ragged, seq.q0 + h_row, head),
                        *po = rows_of(a.o, b, q_ragged, seq.q0 + h_row, head);
+            uint4 o[R::STEPS];
 #pragma unroll
             for (int s = 0; s < R::STEPS; ++s) {
-                q[s] = g[s] = make_uint4(0, 0, 0, 0);
-                if (!there) continue;
                 q[s] = chunk_of<T, DIRECT>(pq, 2 * s + half, a.D);
                 g[s] = chunk_of<T, DIRECT>(pg, 2 * s + half, a.D);
-                const uint4 o = chunk_of<T, DIRECT>(po, 2 * s + half, a.D);
-                const unsigned x[4] = {g[s].x, g[s].y, g[s].z, g[s].w}, y[4] = {o.x, o.y, o.z, o.w};
+                o[s] = chunk_of<T, DIRECT>(po, 2 * s + half, a.D);
+            }
+#pragma unroll
+            for (int s = 0; s < R::STEPS; ++s) {
+                if (!there) q[s] = g[s] = o[s] = make_uint4(0, 0, 0, 0);
+                const unsigned x[4] = {g[s].x, g[s].y, g[s].z, g[s].w}, y[4] = {o[s].x, o[s].y, o[s].z, o[s].w};
 #pragma unroll
                 for (int e = 0; e < 4; ++e) {
                     if constexpr (sizeof(T) == 4) {
@@ -96,43 +164,28 @@ __global__ __launch_bounds__(THREADS, sizeof(T) == 2 ? 2 : 1) void k_attention_d
             log_sum = v.y;
         }
         const float both = top + log_sum;
-        if (there && half == 0) {
+        if (there && half == 0 && (!SHARED || wave == 0)) {
             float *const to = a.stats + (long long)head * a.q_all + place;
             to[0] = both;
             to[a.plane] = delta;
             to[2 * a.plane] = top;
             to[3 * a.plane] = log_sum;
         }
-        const int last = shift + min(tile0 + ROWS, seq.q_len) - 1, end = a.causal ? max(0, min(seq.k_len, last + 1)) : seq.k_len;
-        const int lowest = shift + mine0, highest = shift + min(mine0 + 32, seq.q_len) - 1;
-        const int tiles = (end + W::TILE - 1) / W::TILE;
-        auto load = [&](int t, int buf) {
-            const int k0 = t * W::TILE;
-            unsigned char *const to = lds + buf * W::STAGE;
-            const unsigned to_addr = lds_addr + buf * W::STAGE;
-            load_k.issue(to, to_addr, keys + (long long)k0 * a.k.row, end - k0, a.D, wave);
-            load_v.issue(to + W::HALF, to_addr + W::HALF, values + (long long)k0 * a.v.row, end - k0, a.D, wave);
-        };
         f32x16 acc[1][R::BLOCKS];
 #pragma unroll
         for (int d = 0; d < R::BLOCKS; ++d)
 #pragma unroll
             for (int i = 0; i < 16; ++i) acc[0][d][i] = 0.f;
-        if (tiles > 0) load(0, 0);
         bool left_out = false;
-        int buf = 0;
-        for (int t = 0; t < tiles; ++t, buf ^= 1) {
-            tile::wait_loads<0>();
-            if (end - t * W::TILE < W::TILE) load_k.clear(lds + buf * W::STAGE, end - t * W::TILE, wave);
-            tile::wait_lds();
-            tile::meet();
-            if (t + 1 < tiles) load(t + 1, buf ^ 1);
-            const unsigned char *const ktile = lds + buf * W::STAGE, *const vtile = ktile + W::HALF;
+        // One tile.  edge: some of it is masked; near: its offsets are not all in the bias's last bucket.
+        auto compute = [&](bool edge, bool near, int k0, const unsigned char *ktile) {
+            const unsigned char *const vtile = ktile + W::HALF;
+            const bool skip = edge && a.causal && any_not_finite<T, DP, W::TILE>(ktile);
+            left_out |= skip;
 #pragma unroll
             for (int kb = 0; kb < BLOCKS; ++kb) {
-                const int j0 = t * W::TILE + 32 * kb;
-                if (j0 >= end || (a.causal && j0 > highest) || mine0 >= seq.q_len) continue;
-                const bool border = a.causal && j0 + 31 > lowest, edge = border || j0 + 32 > end;
+                __builtin_amdgcn_sched_barrier(0);          // (a block's fragments at a time: there are no registers for more)
+                const int j0 = k0 + 32 * kb;
                 f32x16 s, dp;
 #pragma unroll
                 for (int i = 0; i < 16; ++i) s[i] = dp[i] = 0.f;
@@ -140,106 +193,143 @@ __global__ __launch_bounds__(THREADS, sizeof(T) == 2 ? 2 : 1) void k_attention_d
                 for (int f = 0; f < R::STEPS; ++f) s = scores<T>(reader.along(ktile, kb, f), q[f], s);
 #pragma unroll
                 for (int f = 0; f < R::STEPS; ++f) dp = scores<T>(reader.along(vtile, kb, f), g[f], dp);
-                if constexpr (BIAS) add_bias(a, table, j0 - pos, j0 - highest, j0 + 31 - lowest, a.scale2, s);
                 f32x16 ds[1];
+                if constexpr (BIAS) {
+                    if (near) {
+                        const float *const bias = table + (j0 - pos) + 4 * half + reach + MARGIN;
 #pragma unroll
-                for (int i = 0; i < 16; ++i) {
-                    const float p = __builtin_amdgcn_exp2f(BIAS ? (s[i] - top) - log_sum : fmaf(s[i], a.scale2, -both));
-                    ds[0][i] = p * (dp[i] - delta);
+                        for (int i = 0; i < 16; ++i) s[i] = fmaf(s[i], a.scale2, bias[row_of(i, 0)]);
+                    } else {
+                        const float bias = far_bias(a, table, k0 + W::TILE - 1 - lowest);
+#pragma unroll
+                        for (int i = 0; i < 16; ++i) s[i] = fmaf(s[i], a.scale2, bias);
+                    }
                 }
+#pragma unroll
+                for (int i = 0; i < 16; ++i)
+                    ds[0][i] = __builtin_amdgcn_exp2f(BIAS ? (s[i] - top) - log_sum : fmaf(s[i], a.scale2, -both)) * (dp[i] - delta);
                 if (edge) {
                     const int most = min(a.causal ? pos : end - 1, end - 1) - j0;
 #pragma unroll
                     for (int i = 0; i < 16; ++i) ds[0][i] = row_of(i, half) <= most ? ds[0][i] : 0.f;
                 }
-                if constexpr (BIAS) {
-                    const int lo = j0 - (lowest + 31), hi = j0 + 31 - lowest;       // offsets of the whole block
-                    if (hi <= -reach || (!a.causal && lo >= reach)) {
-                        float sum = 0.f;
+                if (BIAS && !near) {
+                    float sum = 0.f;
 #pragma unroll
-                        for (int i = 0; i < 16; ++i) sum += ds[0][i];
-                        if (hi <= -reach) far_before += sum;
-                        else far_behind += sum;
-                    } else {
-                        // lane l sums the diagonal of offset lo + l, each in its order
+                    for (int i = 0; i < 16; ++i) sum += ds[0][i];
+                    if (k0 + W::TILE - 1 - lowest <= -reach) far_before += sum;
+                    else far_behind += sum;
+                }
+                if (BIAS && near) {
+                    // lane l sums the diagonal of offset j0 - (lowest + 31) + l, each in its order
 #pragma unroll
-                        for (int i = 0; i < 16; ++i) turn[row_of(i, half) * W::TURN_PITCH + (lane & 31)] = ds[0][i];
-                        asm volatile("" ::: "memory");
-                        float sum = 0.f;
+                    for (int i = 0; i < 16; ++i) turn[row_of(i, half) * W::TURN_PITCH + (lane & 31)] = ds[0][i];
+                    asm volatile("" ::: "memory");
+                    float sum = 0.f;
 #pragma unroll
-                        for (int r = 0; r < 32; ++r) {
-                            const int c = r + 31 - lane;
-                            if (c >= 0 && c < 32) sum += turn[r * W::TURN_PITCH + c];
-                        }
-                        asm volatile("" ::: "memory");
-                        const int offset = lo + lane;
-                        if (lane < 63) {
-                            if (offset <= -reach) far_before += sum;
-                            else if (a.causal ? offset > 0 : offset >= reach) far_behind += sum;       // (causal: zeros)
-                            else mine_near[offset + reach] += sum;
-                        }
+                    for (int r = 0; r < 32; ++r) {
+                        const int c = r + 31 - lane;
+                        const float x = turn[r * W::TURN_PITCH + (c & 31)];
+                        sum += c >= 0 && c < 32 ? x : 0.f;
+                    }
+                    asm volatile("" ::: "memory");
+                    const int offset = j0 - (lowest + 31) + lane;
+                    if (lane < 63) {
+                        if (offset <= -reach) far_before += sum;
+                        else if (a.causal ? offset > 0 : offset >= reach) far_behind += sum;       // (causal: zeros)
+                        else mine_near[offset + reach] += sum;
                     }
                 }
-                if (border && any_not_finite<T, DP>(ktile, kb)) left_out = true;
-                else weigh<T, DP, 1>(reader, ktile, kb, ds, acc);
+                if (!skip) weigh<T, DP, 1>(reader, ktile, kb, ds, acc);
             }
-        }
-        if (left_out) {
-#pragma unroll 1
-            for (int j0 = 0; j0 < end; j0 += 32) {
-                if (j0 + 31 <= lowest || j0 > highest || !any_not_finite<T>(keys + (long long)j0 * a.k.row, a.k.row, end - j0, a.D)) continue;
-                const char *const mine = rows_of(a.q, b, q_ragged, seq.q0 + h_row, head), *const my_grad = rows_of(a.dout, b, q_ragged, seq.q0 + h_row, head);
-#pragma unroll 1
-                for (int j = j0; j < min(end, j0 + 32); ++j) {
-                    if (j > pos || !there) continue;
-                    const char *const key = keys + (long long)j * a.k.row;
-                    const float x = dot<T>(mine, key, a.D), dp = dot<T>(my_grad, values + (long long)j * a.v.row, a.D);
-                    const float p = __builtin_amdgcn_exp2f(BIAS ? (fmaf(x, a.scale2, table[bias_entry(a, j - pos)]) - top) - log_sum : fmaf(x, a.scale2, -both));
-                    add_row<T, DP>(key, a.D, p * (dp - delta), acc[0]);
+        };
+        int buf = 0;
+        for (int t = t0; t < tiles; t += step, buf ^= W::STAGES - 1) {
+            if constexpr (SHARED) {
+                tile::wait_lds();
+                if (W::STAGES == 1) {
+                    load(t, 0);
+                    tile::wait_loads<0>();
+                } else if (t + step < tiles) {
+                    load(t + step, buf ^ 1);
+                    if (DIRECT) tile::wait_loads<W::LOADS>();
+                } else {
+                    tile::wait_loads<0>();
                 }
+            } else {
+                tile::wait_loads<0>();
             }
+            if (end - t * W::TILE < W::TILE) load_k.clear(stages + buf * W::STAGE, end - t * W::TILE, loader);
+            tile::wait_lds();
+            if constexpr (!SHARED) {
+                tile::meet();
+                if (t + 1 < tiles) load(t + 1, buf ^ 1);
+            }
+            const int k0 = t * W::TILE;
+            if (!SHARED && ((a.causal && k0 > highest) || mine0 >= seq.q_len)) continue;
+            const unsigned char *const ktile = stages + buf * W::STAGE;
+            const bool edge = k0 + W::TILE > end || (a.causal && k0 + W::TILE - 1 > lowest);
+            compute(edge, BIAS && !is_far(a, k0 - (lowest + 31), k0 + W::TILE - 1 - lowest), k0, ktile);
         }
-        if (there) {
-            T *const to = reinterpret_cast<T *>(rows_of(a.dq, b, q_ragged, seq.q0 + row, head));
-            const int D = opaque(a.D), first = opaque(4 * half);
-#pragma unroll
-            for (int d = 0; d < 4 * R::BLOCKS; ++d) {
-                const int e = first + 8 * d;
-                if (e < D)
-                    store4<T, DIRECT>(to + e, D - e, acc[0][d >> 2][4 * (d & 3)] * a.scale, acc[0][d >> 2][4 * (d & 3) + 1] * a.scale,
-                           acc[0][d >> 2][4 * (d & 3) + 2] * a.scale, acc[0][d >> 2][4 * (d & 3) + 3] * a.scale);
-            }
+        if (!SHARED && a.causal) tile::meet();
+        if (left_out) {
+            // the tiles on the border that hold something that is not finite
+            const char *const mine = rows_of(a.q, b, q_ragged, seq.q0 + h_row, head), *const my_grad = rows_of(a.dout, b, q_ragged, seq.q0 + h_row, head);
+            add_rows<T, DP>(SHARED ? stages : lds + wave * 4096, a.D, acc[0], [&](auto add) {
+#pragma unroll 1
+                for (int t = t0; t < tiles; t += step) {
+                    const int j0 = t * W::TILE, count = min(W::TILE, end - j0);
+                    if ((j0 + W::TILE <= end && j0 + W::TILE - 1 <= lowest) || j0 > highest) continue;
+                    if (!any_not_finite<T>(keys + (long long)j0 * a.k.row, a.k.row, count, a.D)) continue;
+#pragma unroll 1
+                    for (int j = j0; j < j0 + count; ++j) {
+                        if (j > pos || !there) continue;
+                        const char *const key = keys + (long long)j * a.k.row;
+                        float x = dot<T>(mine, key, a.D) * a.scale2;
+                        if constexpr (BIAS) x += bias_at(a, head, j - pos);
+                        const float p = __builtin_amdgcn_exp2f((x - top) - log_sum);
+                        add(p * (dot<T>(my_grad, values + (long long)j * a.v.row, a.D) - delta), key);
+                    }
+                }
+            });
+        }
+        T *const to = reinterpret_cast<T *>(rows_of(a.dq, b, q_ragged, seq.q0 + h_row, head));
+        if constexpr (SHARED) {
+            add_waves<R::BLOCKS>(lds, acc[0]);
+            if (there) store_row<T, R::BLOCKS, R::BLOCKS, DIRECT>(to, 8 * wave * R::BLOCKS + 4 * half, a.D, a.scale, true, acc[0]);
+        } else {
+            if (there) store_row<T, R::BLOCKS, 4 * R::BLOCKS, DIRECT>(to, 4 * half, a.D, a.scale, true, acc[0]);
         }
         tile::wait_loads<0>();
         tile::wait_lds();
-        __syncthreads();
+        tile::meet();
     }
     if constexpr (BIAS) {
-        if (!a.part_bias) return;
+        if (!part) return;
 #pragma unroll
         for (int o = 1; o < 64; o <<= 1) {
             far_before += __shfl_xor(far_before, o);
             far_behind += __shfl_xor(far_behind, o);
         }
         float *const far = table;           // (the bias itself is not needed any more)
-        __syncthreads();
         if (lane == 0) {
             far[2 * wave] = far_before;
             far[2 * wave + 1] = far_behind;
         }
-        __syncthreads();
-        const int buckets = a.bias.buckets, all = a.bias.both ? 2 * buckets : buckets;
+        tile::wait_lds();
+        tile::meet();
         for (int c = tid; c < all; c += THREADS) {
             const int in = c < buckets ? c : c - buckets, sign = c < buckets ? -1 : 1;
             float sum = 0.f;
             if (in == buckets - 1) {
                 for (int w = 0; w < 4; ++w) sum += far[2 * w + (sign > 0 ? 1 : 0)];
             } else {
-                const int from = in == 0 ? (sign > 0 ? 1 : 0) : a.bias.border[in - 1], to = a.bias.border[in];
+                int from, to;
+                distances(a.bias, in, &from, &to);
                 for (int w = 0; w < 4; ++w)
-                    for (int r = from; r < to; ++r) sum += near[w * entries + sign * r + reach];
+                    for (int r = max(from, sign > 0 ? 1 : 0); r < to; ++r) sum += nears[w * entries + sign * r + reach];
             }
-            a.part_bias[(((long long)head * a.batch + b) * a.tiles + first_tile) * all + c] = sum;
+            part[c] = sum;
         }
     }
 }
@@ -258,11 +348,11 @@ template <typename T> __global__ __launch_bounds__(THREADS) void k_bias_gradient
     if (threadIdx.x == 0) to[c * heads + head] = (T)((sums[0] + sums[1]) + (sums[2] + sums[3]));
 }
 
-template <typename T, int DP, bool BIAS, bool DIRECT> __global__ __launch_bounds__(THREADS, 1) void k_attention_dkv(Args a)
+template <typename T, int DP, bool SHARED, bool BIAS, bool DIRECT> __global__ __launch_bounds__(THREADS, 1) void k_attention_dkv(Args a)
 {
-    using W = Backward<T, DP, BIAS>;
+    using W = Backward<T, DP, SHARED, BIAS>;
     using R = Row<T, DP>;
-    constexpr int ROWS = 128, BLOCKS = W::TILE / 32;
+    constexpr int BLOCKS = W::TILE / 32;
     extern __shared__ __align__(1024) unsigned char lds[];
     const int tid = threadIdx.x, lane = tid & 63, half = lane >> 5, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int total = a.tiles * a.kv_heads * (a.batch + (a.clear && a.k_offsets ? 1 : 0));
@@ -279,81 +369,83 @@ template <typename T, int DP, bool BIAS, bool DIRECT> __global__ __launch_bounds
     const Sequence seq = sequence(a, b);
     const int shift = seq.k_len - seq.q_len;
     const bool q_ragged = a.q_offsets != nullptr, k_ragged = a.k_offsets != nullptr;
-    float *const facts = reinterpret_cast<float *>(lds + W::TILES_BYTES), *const table = facts + W::FACTS_BYTES / 4;
-    int table_of = -1;                                          // the query head whose bias is there
+    float *const all_facts = reinterpret_cast<float *>(lds + W::TILES_BYTES), *const table = all_facts + W::FACTS_BYTES / 4;
+    float *const facts = all_facts + (SHARED ? wave * W::STAGES * W::FACTS_STAGE : 0);
+    unsigned char *const stages = lds + (SHARED ? wave * W::STAGES * W::STAGE : 0);
     const unsigned lds_addr = (unsigned)(size_t)(__attribute__((address_space(3))) unsigned char *)lds;
+    const unsigned stages_addr = lds_addr + (SHARED ? wave * W::STAGES * W::STAGE : 0);
+    const unsigned facts_addr = lds_addr + W::TILES_BYTES + (SHARED ? wave * W::STAGES * W::FACTS_STAGE * 4 : 0);
+    const int loader = SHARED ? 0 : wave;
+    int table_of = -1;                                          // the query head whose bias is there
     Reader<T, DP> reader;
     reader.init();
-    Loader<T, DP, W::TILE, THREADS, DIRECT> load_q, load_g;
-    load_q.init(a.q.row, a.D, tid);
-    load_g.init(a.dout.row, a.D, tid);
+    Loader<T, DP, W::TILE, W::LOADERS, DIRECT> load_q, load_g;
+    load_q.init(a.q.row, a.D, SHARED ? lane : tid);
+    load_g.init(a.dout.row, a.D, SHARED ? lane : tid);
     const int rows = a.clear && !k_ragged ? a.k_rows : seq.k_len;       // rows behind the sequence get zeros
-    for (int tile0 = first_tile * ROWS; tile0 < rows; tile0 += a.tiles * ROWS) {
-        const int mine0 = tile0 + wave * 32, key = mine0 + (lane & 31);
+    for (int tile0 = first_tile * W::ROWS; tile0 < rows; tile0 += a.tiles * W::ROWS) {
+        const int mine0 = tile0 + (SHARED ? 0 : wave * 32), key = mine0 + (lane & 31), h_key = min(key, seq.k_len - 1);
         const bool there = key < seq.k_len;
-        uint4 k[R::STEPS], v[R::STEPS];
-        {
-            const char *pk = rows_of(a.k, b, k_ragged, seq.k0 + key, kv_head), *pv = rows_of(a.v, b, k_ragged, seq.k0 + key, kv_head);
-#pragma unroll
-            for (int s = 0; s < R::STEPS; ++s) {
-                k[s] = there ? chunk_of<T, DIRECT>(pk, 2 * s + half, a.D) : make_uint4(0, 0, 0, 0);
-                v[s] = there ? chunk_of<T, DIRECT>(pv, 2 * s + half, a.D) : make_uint4(0, 0, 0, 0);
-            }
-        }
         const int q_tiles = (seq.q_len + W::TILE - 1) / W::TILE, q_from = a.causal ? min(max(0, tile0 - shift) / W::TILE, q_tiles) : 0;
-        const int per = tile0 < seq.k_len ? q_tiles - q_from : 0, count = per * a.group;
-        auto load = [&](int g, int t, int buf) {
-            const int head = kv_head * a.group + g, i0 = t * W::TILE;
+        const int per = tile0 < seq.k_len ? q_tiles - q_from : 0;
+        const int count = per * a.group, step = SHARED ? 4 : 1;
+        const int rounds = SHARED && BIAS ? a.group : 1, each = SHARED && BIAS ? per : count;       // (a bias is a head's)
+        auto load = [&](int c, int buf) {
+            const int g = c / per, i0 = (q_from + c - g * per) * W::TILE, head = kv_head * a.group + g;
             const char *pq = rows_of(a.q, b, q_ragged, seq.q0 + i0, head), *pg = rows_of(a.dout, b, q_ragged, seq.q0 + i0, head);
-            unsigned char *const to_tile = lds + buf * W::STAGE;
-            const unsigned to_addr = lds_addr + buf * W::STAGE;
-            load_q.issue(to_tile, to_addr, pq, seq.q_len - i0, a.D, wave);
-            load_g.issue(to_tile + W::HALF, to_addr + W::HALF, pg, seq.q_len - i0, a.D, wave);
-            // a plane of facts by each wave: delta behind what the exponents are taken from
-            if (wave < W::FACTS && lane < W::TILE) {
-                const int plane = BIAS ? (wave == 0 ? 2 : wave == 1 ? 1 : 3) : wave;
+            unsigned char *const to = stages + buf * W::STAGE;
+            const unsigned to_addr = stages_addr + buf * W::STAGE;
+            load_q.issue(to, to_addr, pq, seq.q_len - i0, a.D, loader);
+            load_g.issue(to + W::HALF, to_addr + W::HALF, pg, seq.q_len - i0, a.D, loader);
+            // what the exponents are taken from, delta, and with a bias the sum's logarithm by itself: a plane of each
+#pragma unroll
+            for (int f = 0; f < W::FACTS; ++f) {
+                if (!SHARED && wave != f) continue;
+                const int plane = !BIAS ? f : f == 0 ? 2 : f == 1 ? 1 : 3;
                 const float *from = a.stats + plane * a.plane + (long long)head * a.q_all + seq.q_first + i0;
-                const int to = (buf * W::FACTS + wave) * W::TILE;
-                if (i0 + lane < seq.q_len) bring4(uniform(from), lane * 4, lds_addr + W::TILES_BYTES + to * 4);
-                else facts[to + lane] = wave == 0 ? __builtin_inff() : 0.f;
+                if (lane < W::TILE) bring4(uniform(from), min(lane, seq.q_len - 1 - i0) * 4, facts_addr + (buf * W::FACTS_STAGE + f * W::TILE) * 4);
             }
         };
+        // A tile that has come; rows that are not there become zeros with weights of zero.
+        auto clear = [&](int i0, int buf) {
+            const int rows = seq.q_len - i0;
+            if (rows >= W::TILE) return;
+            load_q.clear(stages + buf * W::STAGE, rows, loader);
+            load_g.clear(stages + buf * W::STAGE + W::HALF, rows, loader);
+#pragma unroll
+            for (int f = 0; f < W::FACTS; ++f) {
+                if (!SHARED && wave != f) continue;
+                if (lane < W::TILE && lane >= rows) facts[buf * W::FACTS_STAGE + f * W::TILE + lane] = f == 0 ? __builtin_inff() : 0.f;
+            }
+        };
+        if (W::STAGES == 2 && (SHARED ? wave : 0) < each) load(SHARED ? wave : 0, 0);
+        uint4 k[R::STEPS], v[R::STEPS];
+        {
+            const char *pk = rows_of(a.k, b, k_ragged, seq.k0 + max(h_key, 0), kv_head), *pv = rows_of(a.v, b, k_ragged, seq.k0 + max(h_key, 0), kv_head);
+#pragma unroll
+            for (int s = 0; s < R::STEPS; ++s) {
+                k[s] = v[s] = make_uint4(0, 0, 0, 0);
+                if (count > 0) {
+                    k[s] = chunk_of<T, DIRECT>(pk, 2 * s + half, a.D);
+                    v[s] = chunk_of<T, DIRECT>(pv, 2 * s + half, a.D);
+                }
+            }
+        }
         f32x16 dk[1][R::BLOCKS], dv[1][R::BLOCKS];
 #pragma unroll
         for (int d = 0; d < R::BLOCKS; ++d)
 #pragma unroll
             for (int i = 0; i < 16; ++i) dk[0][d][i] = dv[0][d][i] = 0.f;
         bool left_out = false;
-        int g = 0, t = q_from, buf = 0;
-        if (count > 0) load(0, q_from, 0);
-        for (int c = 0; c < count; ++c, buf ^= 1) {
-            const int g_now = g, i_tile = t * W::TILE;
-            tile::wait_loads<0>();
-            if (seq.q_len - i_tile < W::TILE) {
-                load_q.clear(lds + buf * W::STAGE, seq.q_len - i_tile, wave);
-                load_g.clear(lds + buf * W::STAGE + W::HALF, seq.q_len - i_tile, wave);
-            }
-            tile::wait_lds();
-            tile::meet();
-            if (++t == q_tiles) {
-                t = q_from;
-                ++g;
-            }
-            if constexpr (BIAS)
-                if (g_now != table_of) {
-                    fill_bias(a, kv_head * a.group + g_now, table);
-                    table_of = g_now;
-                    tile::wait_lds();
-                    tile::meet();
-                }
-            if (c + 1 < count) load(g, t, buf ^ 1);
-            const unsigned char *const qtile = lds + buf * W::STAGE, *const gtile = qtile + W::HALF;
-            const float *const fact = facts + buf * W::FACTS * W::TILE;
+        auto compute = [&](bool edge, bool near, int i_tile, int buf) {
+            const unsigned char *const qtile = stages + buf * W::STAGE, *const gtile = qtile + W::HALF;
+            const float *const fact = facts + buf * W::FACTS_STAGE;
+            const bool skip = edge && (any_not_finite<T, DP, W::TILE>(gtile) || any_not_finite<T, DP, W::TILE>(qtile));
+            left_out |= skip;
 #pragma unroll
             for (int rb = 0; rb < BLOCKS; ++rb) {
-                const int i0 = i_tile + 32 * rb, p0 = shift + i0;
-                if (i0 >= seq.q_len || mine0 >= seq.k_len || (a.causal && p0 + 31 < mine0)) continue;
-                const bool border = a.causal && p0 < mine0 + 31;
+                __builtin_amdgcn_sched_barrier(0);          // (a block's fragments at a time: there are no registers for more)
+                const int p0 = shift + i_tile + 32 * rb;
                 f32x16 s, dp;
 #pragma unroll
                 for (int i = 0; i < 16; ++i) s[i] = dp[i] = 0.f;
@@ -361,7 +453,17 @@ template <typename T, int DP, bool BIAS, bool DIRECT> __global__ __launch_bounds
                 for (int f = 0; f < R::STEPS; ++f) s = scores<T>(reader.along(qtile, rb, f), k[f], s);
 #pragma unroll
                 for (int f = 0; f < R::STEPS; ++f) dp = scores<T>(reader.along(gtile, rb, f), v[f], dp);
-                if constexpr (BIAS) add_bias_down(a, table, key - p0, mine0 - (p0 + 31), mine0 + 31 - p0, a.scale2, s);
+                if constexpr (BIAS) {
+                    if (near) {
+                        const float *const bias = table + (key - p0) - 4 * half + a.bias.reach + MARGIN;
+#pragma unroll
+                        for (int i = 0; i < 16; ++i) s[i] = fmaf(s[i], a.scale2, bias[-row_of(i, 0)]);
+                    } else {
+                        const float bias = far_bias(a, table, mine0 + 31 - (shift + i_tile));
+#pragma unroll
+                        for (int i = 0; i < 16; ++i) s[i] = fmaf(s[i], a.scale2, bias);
+                    }
+                }
                 f32x16 p[1], ds[1];
 #pragma unroll
                 for (int f = 0; f < 4; ++f) {
@@ -376,7 +478,7 @@ template <typename T, int DP, bool BIAS, bool DIRECT> __global__ __launch_bounds
                         ds[0][i] = p[0][i] * (dp[i] - delta[e]);
                     }
                 }
-                if (border) {
+                if (edge) {
 #pragma unroll
                     for (int i = 0; i < 16; ++i) {
                         const bool in = key <= p0 + row_of(i, half);
@@ -384,59 +486,112 @@ template <typename T, int DP, bool BIAS, bool DIRECT> __global__ __launch_bounds
                         ds[0][i] = in ? ds[0][i] : 0.f;
                     }
                 }
-                if (border && (any_not_finite<T, DP>(gtile, rb) || any_not_finite<T, DP>(qtile, rb))) {
-                    left_out = true;
-                } else {
+                if (!skip) {
                     weigh<T, DP, 1>(reader, gtile, rb, p, dv);
                     weigh<T, DP, 1>(reader, qtile, rb, ds, dk);
                 }
             }
-        }
-        if (left_out) {
-            const char *const mine = rows_of(a.k, b, k_ragged, seq.k0 + min(key, seq.k_len - 1), kv_head),
-                             *const my_value = rows_of(a.v, b, k_ragged, seq.k0 + min(key, seq.k_len - 1), kv_head);
-#pragma unroll 1
-            for (int h = kv_head * a.group; h < (kv_head + 1) * a.group; ++h) {
-#pragma unroll 1
-                for (int i0 = q_from * W::TILE; i0 < seq.q_len && shift + i0 < mine0 + 31; i0 += 32) {
-                    const char *const pq = rows_of(a.q, b, q_ragged, seq.q0 + i0, h), *const pg = rows_of(a.dout, b, q_ragged, seq.q0 + i0, h);
-                    if (shift + i0 + 31 < mine0 || (!any_not_finite<T>(pg, a.dout.row, seq.q_len - i0, a.D) && !any_not_finite<T>(pq, a.q.row, seq.q_len - i0, a.D)))
-                        continue;
-#pragma unroll 1
-                    for (int i = i0; i < min(seq.q_len, i0 + 32); ++i) {
-                        if (key > shift + i || !there) continue;
-                        const char *const row_q = pq + (long long)(i - i0) * a.q.row, *const row_g = pg + (long long)(i - i0) * a.dout.row;
-                        const float *const fact = a.stats + (long long)h * a.q_all + seq.q_first + i;
-                        float x = dot<T>(row_q, mine, a.D) * a.scale2;
-                        if constexpr (BIAS) {
-                            const int at = bucket_of(a.bias, key - shift - i) * a.heads + h;
-                            x += (a.bias.f32 ? ((const float *)a.bias.table)[at] : (float)((const __bf16 *)a.bias.table)[at]) * 1.44269504f;
+        };
+        auto choose = [&](int i_tile, int buf) {
+            const int p0 = shift + i_tile, p1 = p0 + W::TILE - 1;       // the tile's positions
+            if (mine0 >= seq.k_len || (a.causal && p1 < mine0)) return;
+            compute(a.causal && p0 < mine0 + 31, BIAS && !is_far(a, mine0 - p1, mine0 + 31 - p0), i_tile, buf);
+        };
+        if constexpr (SHARED) {
+            for (int g = 0; g < rounds; ++g) {
+                if constexpr (BIAS) {
+                    tile::wait_lds();
+                    tile::meet();
+                    fill_bias(a, kv_head * a.group + g, 1, table);
+                    tile::wait_lds();
+                    tile::meet();
+                }
+                int buf = 0;
+                for (int c = wave; c < each; c += 4, buf ^= W::STAGES - 1) {
+                    const int now = g * each + c, i_tile = (q_from + now % per) * W::TILE;
+                    tile::wait_lds();
+                    if (W::STAGES == 1) {
+                        load(now, 0);
+                        tile::wait_loads<0>();
+                    } else {
+                        if (g > 0 && c == wave) load(now, 0);
+                        if (c + 4 < each) {
+                            load(now + 4, buf ^ 1);
+                            if (DIRECT) tile::wait_loads<W::LOADS + W::FACTS>();
+                            else tile::wait_loads<0>();
+                        } else {
+                            tile::wait_loads<0>();
                         }
-                        const float p = __builtin_amdgcn_exp2f((x - fact[2 * a.plane]) - fact[3 * a.plane]);
-                        const float ds = p * (dot<T>(row_g, my_value, a.D) - fact[a.plane]);
-                        add_row<T, DP>(row_g, a.D, p, dv[0]);
-                        add_row<T, DP>(row_q, a.D, ds, dk[0]);
                     }
+                    clear(i_tile, buf);
+                    tile::wait_lds();
+                    choose(i_tile, buf);
                 }
             }
-        }
-        if (key < rows) {
-            T *const to_k = reinterpret_cast<T *>(rows_of(a.dk, b, k_ragged, seq.k0 + key, kv_head)),
-                    *const to_v = reinterpret_cast<T *>(rows_of(a.dv, b, k_ragged, seq.k0 + key, kv_head));
-            // (a row behind the sequence: zeros, whatever the weights of its zeros came to)
-            auto of = [&](float x) { return there ? x : 0.f; };
-            const int D = opaque(a.D), first = opaque(4 * half);
-#pragma unroll
-            for (int d = 0; d < 4 * R::BLOCKS; ++d) {
-                const int e = first + 8 * d, x = d >> 2, y = 4 * (d & 3);
-                if (e >= D) continue;
-                store4<T, DIRECT>(to_k + e, D - e, of(dk[0][x][y] * a.scale), of(dk[0][x][y + 1] * a.scale), of(dk[0][x][y + 2] * a.scale), of(dk[0][x][y + 3] * a.scale));
-                store4<T, DIRECT>(to_v + e, D - e, of(dv[0][x][y]), of(dv[0][x][y + 1]), of(dv[0][x][y + 2]), of(dv[0][x][y + 3]));
+        } else {
+            int buf = 0;
+            for (int c = 0; c < count; ++c, buf ^= 1) {
+                const int g_now = c / per, i_tile = (q_from + c - g_now * per) * W::TILE;
+                tile::wait_loads<0>();
+                clear(i_tile, buf);
+                tile::wait_lds();
+                tile::meet();
+                if constexpr (BIAS)
+                    if (g_now != table_of) {
+                        fill_bias(a, kv_head * a.group + g_now, 1, table);
+                        table_of = g_now;
+                        tile::wait_lds();
+                        tile::meet();
+                    }
+                if (c + 1 < count) load(c + 1, buf ^ 1);
+                choose(i_tile, buf);
             }
+        }
+        if (!SHARED && a.causal) tile::meet();
+        if (left_out) {
+            // the tiles on the border that hold something that is not finite
+            const char *const mine = rows_of(a.k, b, k_ragged, seq.k0 + h_key, kv_head), *const my_value = rows_of(a.v, b, k_ragged, seq.k0 + h_key, kv_head);
+            auto visit = [&](bool of_v, auto add) {
+#pragma unroll 1
+                for (int round = 0; round < rounds; ++round)
+#pragma unroll 1
+                    for (int c = SHARED ? wave : 0; c < each; c += step) {
+                        const int now = round * each + c, h = kv_head * a.group + now / per, i0 = (q_from + now % per) * W::TILE, n = min(W::TILE, seq.q_len - i0);
+                        const char *const pq = rows_of(a.q, b, q_ragged, seq.q0 + i0, h), *const pg = rows_of(a.dout, b, q_ragged, seq.q0 + i0, h);
+                        if (shift + i0 >= mine0 + 31 || shift + i0 + W::TILE - 1 < mine0) continue;
+                        if (!any_not_finite<T>(pg, a.dout.row, n, a.D) && !any_not_finite<T>(pq, a.q.row, n, a.D)) continue;
+#pragma unroll 1
+                        for (int i = 0; i < n; ++i) {
+                            if (key > shift + i0 + i || !there) continue;
+                            const char *const row_q = pq + (long long)i * a.q.row, *const row_g = pg + (long long)i * a.dout.row;
+                            const float *const fact = a.stats + (long long)h * a.q_all + seq.q_first + i0 + i;
+                            float x = dot<T>(row_q, mine, a.D) * a.scale2;
+                            if constexpr (BIAS) x += bias_at(a, h, key - shift - i0 - i);
+                            const float p = __builtin_amdgcn_exp2f((x - fact[2 * a.plane]) - fact[3 * a.plane]);
+                            if (of_v) add(p, row_g);
+                            else add(p * (dot<T>(row_g, my_value, a.D) - fact[a.plane]), row_q);
+                        }
+                    }
+            };
+            add_rows<T, DP>(SHARED ? stages : lds + wave * 4096, a.D, dv[0], [&](auto add) { visit(true, add); });
+            add_rows<T, DP>(SHARED ? stages : lds + wave * 4096, a.D, dk[0], [&](auto add) { visit(false, add); });
+        }
+        const bool stored = key < rows;
+        T *const to_k = reinterpret_cast<T *>(rows_of(a.dk, b, k_ragged, seq.k0 + key, kv_head)),
+                *const to_v = reinterpret_cast<T *>(rows_of(a.dv, b, k_ragged, seq.k0 + key, kv_head));
+        if constexpr (SHARED) {
+            const int first = 8 * wave * R::BLOCKS + 4 * half;
+            add_waves<R::BLOCKS>(lds, dk[0]);
+            if (stored) store_row<T, R::BLOCKS, R::BLOCKS, DIRECT>(to_k, first, a.D, a.scale, there, dk[0]);
+            add_waves<R::BLOCKS>(lds, dv[0]);
+            if (stored) store_row<T, R::BLOCKS, R::BLOCKS, DIRECT>(to_v, first, a.D, 1.f, there, dv[0]);
+        } else if (stored) {
+            store_row<T, R::BLOCKS, 4 * R::BLOCKS, DIRECT>(to_k, 4 * half, a.D, a.scale, there, dk[0]);
+            store_row<T, R::BLOCKS, 4 * R::BLOCKS, DIRECT>(to_v, 4 * half, a.D, 1.f, there, dv[0]);
         }
         tile::wait_loads<0>();
         tile::wait_lds();
-        __syncthreads();
+        tile::meet();
     }
 }
 

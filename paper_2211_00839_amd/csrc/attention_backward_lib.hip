@@ -12,20 +12,36 @@ int set_up()
         using T = decltype(t);
         constexpr int DP = decltype(dp)::value;
         constexpr bool BIAS = decltype(bias)::value, DIRECT = decltype(direct)::value;
-        const hipError_t e = raise_lds(&k_attention_dq<T, DP, BIAS, DIRECT>);
-        return e != hipSuccess ? e : raise_lds(&k_attention_dkv<T, DP, BIAS, DIRECT>);
+        hipError_t e = raise_lds(&k_attention_dq<T, DP, false, BIAS, DIRECT>);
+        if (e == hipSuccess) e = raise_lds(&k_attention_dq<T, DP, true, BIAS, DIRECT>);
+        if (e == hipSuccess) e = raise_lds(&k_attention_dkv<T, DP, false, BIAS, DIRECT>);
+        return e != hipSuccess ? e : raise_lds(&k_attention_dkv<T, DP, true, BIAS, DIRECT>);
     });
 }
 
-// Workgroups of 128 rows for each sequence and head of the gradients' kernels.
-int64_t tiles_of(int64_t longest, int64_t across)
+template <typename W> int dq_lds(bool bias, int reach, bool causal)
 {
-    const int64_t tiles = std::max<int64_t>(1, attn_rules::ceil_div(longest, 128));
-    return std::max<int64_t>(1, std::min(tiles, attn_rules::MOST_WORKGROUPS / std::max<int64_t>(across, 1)));
+    return W::TILES_BYTES + (bias ? (bias_width(reach, causal) + 4 * bias_entries(reach, causal)) * 4 + 4 * W::TURN_BYTES : 0);
 }
-int64_t dq_tiles(const rcd_attention_shape &s)
+template <typename W> int dkv_lds(bool bias, int reach, bool causal) { return W::TILES_BYTES + W::FACTS_BYTES + (bias ? bias_width(reach, causal) * 4 : 0); }
+
+// The gradient of q: whether the waves share their rows (where there is room for it), and the workgroups for each sequence and head.
+struct Way {
+    bool shared;
+    int64_t tiles;
+};
+Way dq_way(const rcd_attention_shape &s)
 {
-    return tiles_of(attn_rules::longest_of(s.longest_q, s.q_rows, s.batch, s.q_offsets_dev != nullptr), (s.batch + 1) * s.heads);
+    const int64_t longest = attn_rules::longest_of(s.longest_q, s.q_rows, s.batch, s.q_offsets_dev != nullptr);
+    Way w;
+    w.shared = attn_rules::shared_rows(s.batch * s.heads, longest);
+    if (w.shared)
+        w.shared = with_variant(s.dt, s.d, s.bias_dev != nullptr, true, [&](auto t, auto dp, auto bias, auto) {
+                       using W = Backward<decltype(t), decltype(dp)::value, true, decltype(bias)::value>;
+                       return dq_lds<W>(s.bias_dev != nullptr, reach_of(s), s.causal != 0);
+                   }) <= MOST_LDS;
+    w.tiles = attn_rules::tiles_of((s.batch + 1) * s.heads, longest, w.shared);
+    return w;
 }
 
 size_t backward_bytes(const rcd_attention_shape &s, void *base, Args *a)
@@ -33,7 +49,7 @@ size_t backward_bytes(const rcd_attention_shape &s, void *base, Args *a)
     Pieces room(base);
     const size_t plane = up256((size_t)all_rows(s.q_offsets_dev, s.q_rows, s.batch) * s.heads * 4) / 4;
     float *const stats = room.take(4 * plane);
-    float *const parts = s.bias_dev ? room.take((size_t)s.heads * s.batch * dq_tiles(s) * s.buckets) : nullptr;
+    float *const parts = s.bias_dev ? room.take((size_t)s.heads * s.batch * dq_way(s).tiles * s.buckets) : nullptr;
     if (a) {
         a->stats = stats;
         a->plane = (long long)plane;
@@ -77,23 +93,25 @@ int rcd_attention_backward(const rcd_attention_shape *s, const rcd_heads *dout, 
     a.dv = heads_of(dv, s->dt);
     a.saved = const_cast<float *>(saved_dev);
     a.clear = clear != 0;
-    const int entries = (int)entries_of(*s);
+    const int reach = reach_of(*s);
+    const bool causal = s->causal != 0;
+    const Way way = dq_way(*s);
     if (s->q_rows > 0 && s->batch > 0) {
         Args x = a;
-        x.tiles = (int)dq_tiles(*s);
+        x.tiles = (int)way.tiles;
         if (!dbias_dev) x.part_bias = nullptr;
         const int64_t groups = x.tiles * s->heads * (s->batch + (a.clear && a.q_offsets ? 1 : 0));
         const bool direct = aligned(a.k, s->d, s->dt) && aligned(a.v, s->d, s->dt);
-        ENC_TRY(with_variant(s->dt, s->d, s->bias_dev != nullptr, direct, [&](auto t, auto dp, auto bias, auto way) {
+        ENC_TRY(with_variant(s->dt, s->d, s->bias_dev != nullptr, direct, [&](auto t, auto dp, auto bias, auto how) {
             using T = decltype(t);
             constexpr int DP = decltype(dp)::value;
-            constexpr bool BIAS = decltype(bias)::value, DIRECT = decltype(way)::value;
-            using W = Backward<T, DP, BIAS>;
-            return launch(&k_attention_dq<T, DP, BIAS, DIRECT>, groups, W::TILES_BYTES + (BIAS ? 5 * entries * 4 + 4 * W::TURN_BYTES : 0), x, stream);
+            constexpr bool BIAS = decltype(bias)::value, DIRECT = decltype(how)::value;
+            if (way.shared) return launch(&k_attention_dq<T, DP, true, BIAS, DIRECT>, groups, dq_lds<Backward<T, DP, true, BIAS>>(BIAS, reach, causal), x, stream);
+            return launch(&k_attention_dq<T, DP, false, BIAS, DIRECT>, groups, dq_lds<Backward<T, DP, false, BIAS>>(BIAS, reach, causal), x, stream);
         }));
     }
     if (dbias_dev) {
-        const long long count = s->q_rows > 0 ? s->batch * dq_tiles(*s) : 0;
+        const long long count = s->q_rows > 0 ? s->batch * way.tiles : 0;
         const dim3 grid((unsigned)(s->buckets * s->heads));
         if (s->bias_dt == RCD_F32)
             hipLaunchKernelGGL((k_bias_gradient<float>), grid, dim3(THREADS), 0, stream, a.part_bias, count, (int)s->buckets, (int)s->heads, (float *)dbias_dev);
@@ -102,15 +120,17 @@ int rcd_attention_backward(const rcd_attention_shape *s, const rcd_heads *dout, 
         ENC_HIP_TRY(hipGetLastError());
     }
     if (s->k_rows > 0 && s->batch > 0) {
-        a.tiles = (int)tiles_of(attn_rules::longest_of(s->longest_k, s->k_rows, s->batch, s->k_offsets_dev != nullptr), (s->batch + 1) * s->kv_heads);
+        const int64_t longest = attn_rules::longest_of(s->longest_k, s->k_rows, s->batch, s->k_offsets_dev != nullptr);
+        const bool shared = attn_rules::shared_rows(s->batch * s->kv_heads, longest);
+        a.tiles = (int)attn_rules::tiles_of((s->batch + 1) * s->kv_heads, longest, shared);
         const int64_t groups = a.tiles * s->kv_heads * (s->batch + (a.clear && a.k_offsets ? 1 : 0));
         const bool direct = aligned(a.q, s->d, s->dt) && aligned(a.dout, s->d, s->dt);
-        ENC_TRY(with_variant(s->dt, s->d, s->bias_dev != nullptr, direct, [&](auto t, auto dp, auto bias, auto way) {
+        ENC_TRY(with_variant(s->dt, s->d, s->bias_dev != nullptr, direct, [&](auto t, auto dp, auto bias, auto how) {
             using T = decltype(t);
             constexpr int DP = decltype(dp)::value;
-            constexpr bool BIAS = decltype(bias)::value, DIRECT = decltype(way)::value;
-            using W = Backward<T, DP, BIAS>;
-            return launch(&k_attention_dkv<T, DP, BIAS, DIRECT>, groups, W::TILES_BYTES + W::FACTS_BYTES + (BIAS ? entries * 4 : 0), a, stream);
+            constexpr bool BIAS = decltype(bias)::value, DIRECT = decltype(how)::value;
+            if (shared) return launch(&k_attention_dkv<T, DP, true, BIAS, DIRECT>, groups, dkv_lds<Backward<T, DP, true, BIAS>>(BIAS, reach, causal), a, stream);
+            return launch(&k_attention_dkv<T, DP, false, BIAS, DIRECT>, groups, dkv_lds<Backward<T, DP, false, BIAS>>(BIAS, reach, causal), a, stream);
         }));
     }
     return RCD_OK;

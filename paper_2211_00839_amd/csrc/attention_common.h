@@ -7,6 +7,8 @@
 #include "encoder_lds.h"
 #include "encoder_math.h"
 
+#include <type_traits>
+
 namespace attn {
 
 using namespace enc;
@@ -332,7 +334,7 @@ __device__ __forceinline__ void weigh(const Reader<T, DP> &at, const unsigned ch
 // ---- infinities and NaN at the border of what may be seen -----------------------------------------------------------------
 //
 // A row that is not seen has no part in a sum at all, where a weight of zero would make a NaN of an infinity.  Only blocks on the causal
-// border are weighed for lanes that do not see all of their rows; one that holds something that is not finite is left out there, and added row by row
+// border are weighed for lanes that do not see all of their rows; a tile there that holds something that is not finite is left out, and added row by row
 // once everything else is done.  Rare: what it takes is code behind the loops, not time or registers in them.
 
 // The largest size among a chunk's elements, as bits; and whether it is a number's.
@@ -354,23 +356,22 @@ template <typename T> __device__ __forceinline__ bool any_not_finite(unsigned m)
 {
     return __any(sizeof(T) == 4 ? m >= 0x7f800000u : m >= 0x7f800000u || (m & 0xffffu) >= 0x7f80u);
 }
-// Of 32 rows of a tile.
-template <typename T, int DP> __device__ __forceinline__ bool any_not_finite(const unsigned char *tile, int block)
+// Of a tile's rows.
+template <typename T, int DP, int ROWS> __device__ __forceinline__ bool any_not_finite(const unsigned char *tile)
 {
-    using R = Row<T, DP>;
     const int lane = threadIdx.x & 63;
     unsigned m = 0;
-#pragma unroll
-    for (int u = 0; u < 32 * R::CHUNKS / 64; ++u)
-        m = largest<T>(*reinterpret_cast<const uint4 *>(tile + block * 32 * R::BYTES + (u * 64 + lane) * 16), m);
+#pragma unroll 4
+    for (int u = 0; u < ROWS * Row<T, DP>::CHUNKS / 64; ++u) m = largest<T>(*reinterpret_cast<const uint4 *>(tile + (u * 64 + lane) * 16), m);
     return any_not_finite<T>(m);
 }
-// The same of up to 32 rows in memory.
+// The same of `count` rows in memory.
 template <typename T> __device__ __forceinline__ bool any_not_finite(const char *rows, long long pitch, int count, int D)
 {
-    const int lane = threadIdx.x & 63, r = lane & 31;
+    const int lane = threadIdx.x & 63;
     unsigned m = 0;
-    if (r < count)
+#pragma unroll 1
+    for (int r = lane & 31; r < count; r += 32)
 #pragma unroll 1
         for (int c = lane >> 5; c * (16 / (int)sizeof(T)) < D; c += 2) m = largest<T>(chunk_of<T, false>(rows + r * pitch, c, D), m);
     return any_not_finite<T>(m);
@@ -382,17 +383,27 @@ template <typename T> __device__ __forceinline__ float dot(const char *a, const 
     for (int d = 0; d < D; ++d) sum = fmaf(to_f32(reinterpret_cast<const T *>(a)[d]), to_f32(reinterpret_cast<const T *>(b)[d]), sum);
     return sum;
 }
-// acc += weight row
-template <typename T, int DP> __device__ __forceinline__ void add_row(const char *row, int D, float weight, f32x16 (&acc)[DP / 32])
+// Adds rows by themselves: visit(add) calls add(weight, row) for each.  The sums lie in LDS meanwhile (4 KB of the wave's own), block by block.
+template <typename T, int DP, typename Visit> __device__ __forceinline__ void add_rows(unsigned char *lds, int D, f32x16 (&acc)[DP / 32], Visit visit)
 {
-    const int first = opaque(4 * ((threadIdx.x & 63) >> 5));
+    const int lane = threadIdx.x & 63;
+    float *const sums = reinterpret_cast<float *>(lds) + lane;
 #pragma unroll
-    for (int b = 0; b < DP / 32; ++b)
+    for (int b = 0; b < DP / 32; ++b) {
+        __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
-        for (int i = 0; i < 16; ++i) {
-            const int d = min(first + 32 * b + row_of(i, 0), D - 1);        // (what lies behind D is not stored)
-            acc[b][i] = fmaf(weight, to_f32(reinterpret_cast<const T *>(row)[d]), acc[b][i]);
-        }
+        for (int i = 0; i < 16; ++i) sums[i * 64] = acc[b][i];
+        visit([&](float weight, const char *row) {
+#pragma unroll 1
+            for (int i = 0; i < 16; ++i) {
+                const int d = min(32 * b + row_of(i, lane >> 5), D - 1);        // (what lies behind D is not stored)
+                sums[i * 64] = fmaf(weight, to_f32(reinterpret_cast<const T *>(row)[d]), sums[i * 64]);
+            }
+        });
+#pragma unroll
+        for (int i = 0; i < 16; ++i) acc[b][i] = sums[i * 64];
+        __builtin_amdgcn_sched_barrier(0);
+    }
 }
 
 // Both halves' values.
@@ -421,66 +432,55 @@ __device__ __forceinline__ float max_halves(float x)
 
 // ---- bias -----------------------------------------------------------------------------------------------------------------
 
-// The bias by offset, key's position - query's, in powers of two: entry `reach + offset` of a head's, offsets -reach .. reach (causal: .. 0).
-__device__ __forceinline__ int bias_entries(const Args &a) { return a.causal ? a.bias.reach + 1 : 2 * a.bias.reach + 1; }
+// The bias by offset, key's position - query's, in powers of two: entry MARGIN + reach + offset of a head's, offsets -reach .. reach (causal: .. 0)
+// and the last bucket's value as far beyond them as a tile on their border goes, so that no offset of such a tile needs a limit.
+constexpr int MARGIN = 96;
+inline __host__ __device__ int bias_width(int reach, bool causal) { return (causal ? reach + 1 : 2 * reach + 1) + 2 * MARGIN; }
+// Of the gradient's sums by offset, without the margin.
+inline __host__ __device__ int bias_entries(int reach, bool causal) { return causal ? reach + 1 : 2 * reach + 1; }
 
-__device__ __forceinline__ int bucket_of(const Bias &b, int offset)
+// The distances of bucket c of one direction: from .. to - 1.
+__device__ __forceinline__ void distances(const Bias &b, int c, int *from, int *to)
 {
-    const int size = abs(offset);
-    int c = 0;
-    for (int i = 0; i < b.buckets - 1; ++i) c += size >= (int)b.border[i] ? 1 : 0;
-    return c + (b.both && offset > 0 ? b.buckets : 0);
+    *from = c == 0 ? 0 : (int)b.border[c - 1];
+    *to = c == b.buckets - 1 ? b.reach + MARGIN + 1 : (int)b.border[c];
 }
-__device__ __forceinline__ void fill_bias(const Args &a, int head, float *to)
+// A thread for each bucket, or several where there are few.  (What is behind the query is masked where causal.)
+__device__ __forceinline__ void fill_bias(const Args &a, int head, int count, float *to)
 {
-    const int n = bias_entries(a);
-    for (int e = threadIdx.x; e < n; e += THREADS) {
-        const int at = bucket_of(a.bias, e - a.bias.reach) * a.heads + head;
-        const float v = a.bias.f32 ? ((const float *)a.bias.table)[at] : (float)((const __bf16 *)a.bias.table)[at];
+    const int all = a.bias.both ? 2 * a.bias.buckets : a.bias.buckets, parts = all <= 32 ? 8 : all <= 64 ? 4 : all <= 128 ? 2 : 1;
+    const int c = threadIdx.x / parts, width = bias_width(a.bias.reach, !a.bias.both);
+    if (c >= all) return;
+    const bool behind = c >= a.bias.buckets;
+    int from, until;
+    distances(a.bias, behind ? c - a.bias.buckets : c, &from, &until);
+    for (int g = 0; g < count; ++g) {
+        const int at = c * a.heads + head + g;
+        float v = a.bias.f32 ? ((const float *)a.bias.table)[at] : (float)((const __bf16 *)a.bias.table)[at];
         // (the type's lowest value, as a mask, stays a number: a row of nothing else is a row of equal scores)
-        to[e] = fabsf(v) <= 3.402823466e38f ? __builtin_amdgcn_fmed3f(v * 1.44269504f, -3.4e38f, 3.4e38f) : v;
+        if (fabsf(v) <= 3.402823466e38f) v = __builtin_amdgcn_fmed3f(v * 1.44269504f, -3.4e38f, 3.4e38f);
+        float *const zero = to + g * width + MARGIN + a.bias.reach;
+        for (int r = from + (int)threadIdx.x % parts; r < until; r += parts)
+            if (!behind) zero[-r] = v;
+            else if (r > 0) zero[r] = v;
     }
 }
-// Entry of an offset.
-__device__ __forceinline__ int bias_entry(const Args &a, int offset)
+// The table's value at an offset, in powers of two.
+__device__ __forceinline__ float bias_at(const Args &a, int head, int offset)
 {
-    return min(max(offset, -a.bias.reach), a.causal ? 0 : a.bias.reach) + a.bias.reach;
-}
-
-// Adds the bias to a block of scaled scores: register i's offset is first + row_of(i, half).  lo .. hi: the block's offsets over the wave.
-__device__ __forceinline__ void add_bias(const Args &a, const float *table, int first, int lo, int hi, float scale2, f32x16 &s)
-{
-    const int half = (threadIdx.x & 63) >> 5;
-    if (hi <= -a.bias.reach || (lo >= a.bias.reach && !a.causal)) {
-        const float b = table[hi <= -a.bias.reach ? 0 : 2 * a.bias.reach];
-#pragma unroll
-        for (int i = 0; i < 16; ++i) s[i] = fmaf(s[i], scale2, b);
-    } else if (lo >= -a.bias.reach && hi <= (a.causal ? 0 : a.bias.reach)) {
-        const float *at = table + first + 4 * half + a.bias.reach;
-#pragma unroll
-        for (int i = 0; i < 16; ++i) s[i] = fmaf(s[i], scale2, at[8 * (i >> 2) + (i & 3)]);
-    } else {
-#pragma unroll
-        for (int i = 0; i < 16; ++i) s[i] = fmaf(s[i], scale2, table[bias_entry(a, first + row_of(i, half))]);
-    }
+    int c = 0;
+    for (int i = 0; i < a.bias.buckets - 1; ++i) c += abs(offset) >= (int)a.bias.border[i] ? 1 : 0;
+    const int at = (c + (a.bias.both && offset > 0 ? a.bias.buckets : 0)) * a.heads + head;
+    const float v = a.bias.f32 ? ((const float *)a.bias.table)[at] : (float)((const __bf16 *)a.bias.table)[at];
+    return fabsf(v) <= 3.402823466e38f ? __builtin_amdgcn_fmed3f(v * 1.44269504f, -3.4e38f, 3.4e38f) : v;
 }
 
-// The same where the registers hold queries and the lanes keys: register i's offset is first - row_of(i, half).
-__device__ __forceinline__ void add_bias_down(const Args &a, const float *table, int first, int lo, int hi, float scale2, f32x16 &s)
+// Is every offset lo .. hi in the last bucket of one direction?
+__device__ __forceinline__ bool is_far(const Args &a, int lo, int hi) { return hi <= -a.bias.reach || (lo >= a.bias.reach && !a.causal); }
+// That bucket's value.
+__device__ __forceinline__ float far_bias(const Args &a, const float *table, int hi)
 {
-    const int half = (threadIdx.x & 63) >> 5;
-    if (hi <= -a.bias.reach || (lo >= a.bias.reach && !a.causal)) {
-        const float b = table[hi <= -a.bias.reach ? 0 : 2 * a.bias.reach];
-#pragma unroll
-        for (int i = 0; i < 16; ++i) s[i] = fmaf(s[i], scale2, b);
-    } else if (lo >= -a.bias.reach && hi <= (a.causal ? 0 : a.bias.reach)) {
-        const float *at = table + first - 4 * half + a.bias.reach;
-#pragma unroll
-        for (int i = 0; i < 16; ++i) s[i] = fmaf(s[i], scale2, at[-(8 * (i >> 2) + (i & 3))]);
-    } else {
-#pragma unroll
-        for (int i = 0; i < 16; ++i) s[i] = fmaf(s[i], scale2, table[bias_entry(a, first - row_of(i, half))]);
-    }
+    return table[MARGIN + (hi <= -a.bias.reach ? 0 : 2 * a.bias.reach)];
 }
 
 // Rows in front of the first sequence and behind the last one become zeros; part: which of `parts` workgroups this is.

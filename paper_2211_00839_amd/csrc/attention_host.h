@@ -69,12 +69,8 @@ int check_shape(const rcd_attention_shape *s)
     return RCD_OK;
 }
 
-int64_t entries_of(const rcd_attention_shape &s)
-{
-    if (!s.bias_dev) return 0;
-    const int64_t reach = s.borders_host[(s.causal ? s.buckets : s.buckets / 2) - 2];
-    return s.causal ? reach + 1 : 2 * reach + 1;
-}
+int reach_of(const rcd_attention_shape &s) { return s.bias_dev ? s.borders_host[(s.causal ? s.buckets : s.buckets / 2) - 2] : 0; }
+int width_of(const rcd_attention_shape &s) { return s.bias_dev ? bias_width(reach_of(s), s.causal != 0) : 0; }
 
 int check_heads(const rcd_heads *h, int64_t rows, int64_t batch, int dt)
 {

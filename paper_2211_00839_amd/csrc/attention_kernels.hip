@@ -4,109 +4,188 @@
 
 namespace attn {
 
-// KEYS false: a workgroup's four waves hold 32 N rows of q each and share tiles of TILE keys, the next one on its way while one is used.
-// KEYS true: few rows of q (one block of 32), and each wave goes through blocks of 32 keys of its own, every fourth one, without meeting
+// SHARED false: a workgroup's four waves hold 32 rows of q each and share tiles of TILE keys, the next one on its way while one is used.
+// SHARED true: few rows of q.  The waves hold the same 32, and each goes through tiles of 32 keys of its own, every fourth one, without meeting
 // the others; their sums are joined at the end.  Either may leave its keys to several workgroups (splits), joined by k_attention_join.
-template <typename T, int DP, bool KEYS> struct Forward {
+template <typename T, int DP, bool SHARED> struct Forward {
     using R = Row<T, DP>;
-    static constexpr int TILE = KEYS || R::BYTES == 512 ? 32 : 64;
-    static constexpr int LOADERS = KEYS ? 64 : THREADS;
-    static constexpr int STAGES = KEYS && R::BYTES == 512 ? 1 : 2;
+    static constexpr int TILE = SHARED || R::BYTES == 512 ? 32 : 64;
+    static constexpr int LOADERS = SHARED ? 64 : THREADS;
+    static constexpr int STAGES = SHARED && R::BYTES == 512 ? 1 : 2;
     static constexpr int HALF = TILE * R::BYTES, STAGE = 2 * HALF;              // of keys, of keys and values
-    static constexpr int TILES_BYTES = STAGES * STAGE * (KEYS ? 4 : 1);
+    static constexpr int TILES_BYTES = STAGES * STAGE * (SHARED ? 4 : 1);
     static constexpr int LOADS = 2 * TILE * R::CHUNKS / LOADERS;                // of a lane, to a stage
 };
 
-template <typename T, int DP, int N, bool KEYS, bool BIAS, bool DIRECT>
-__global__ __launch_bounds__(THREADS, N == 1 && sizeof(T) == 2 && !KEYS ? 2 : 1) void k_attention(Args a)
+template <typename T, int DP, bool SHARED, bool BIAS, bool DIRECT>
+__global__ __launch_bounds__(THREADS, sizeof(T) == 2 && !SHARED ? 2 : 1) void k_attention(Args a)
 {
-    using F = Forward<T, DP, KEYS>;
+    using F = Forward<T, DP, SHARED>;
     using R = Row<T, DP>;
-    constexpr int MINE = 32 * N, ROWS = KEYS ? 32 : 4 * MINE, BLOCKS = F::TILE / 32;
+    constexpr int ROWS = SHARED ? 32 : 128, BLOCKS = F::TILE / 32;
     extern __shared__ __align__(1024) unsigned char lds[];
     const int tid = threadIdx.x, lane = tid & 63, half = lane >> 5, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
-    const int groups = a.heads / a.pack;
-    const int total = a.tiles * groups * (a.batch + (a.clear ? 1 : 0)) * a.splits;
+    const int groups = a.heads / a.pack, sequences = a.batch + (a.clear ? 1 : 0);
+    const int total = a.tiles * groups * sequences * a.splits;
     int at = place_of(blockIdx.x, total);
     if (at >= total) return;
-    const int split = at % a.splits;
-    at /= a.splits;
     const int first_tile = a.tiles - 1 - at % a.tiles;          // (causal: the longest first)
     at /= a.tiles;
-    const int group = at % groups, b = at / groups;
+    const int group = at % groups;
+    at /= groups;
+    const int b = at % sequences, split = at / sequences;       // (the last splits, of which short sequences have none, last)
     if (b == a.batch) {
         if (split == 0)
             for (int g = 0; g < a.pack; ++g) clear_rows<T>(a.o, a.q_offsets, a.batch, a.q_rows, group * a.pack + g, a.D, first_tile, a.tiles);
         return;
     }
     const Sequence seq = sequence(a, b);
+    const int columns = seq.q_len * a.pack;
+    if (first_tile * ROWS >= columns) return;
     const int head0 = group * a.pack, kv_head = head0 / a.group, shift = seq.k_len - seq.q_len;
     const char *const keys = rows_of(a.k, b, a.k_offsets != nullptr, seq.k0, kv_head), *const values = rows_of(a.v, b, a.k_offsets != nullptr, seq.k0, kv_head);
     float *const table = reinterpret_cast<float *>(lds + F::TILES_BYTES);
-    const int entries = BIAS ? bias_entries(a) : 0;
-    if constexpr (BIAS)
-        for (int g = 0; g < a.pack; ++g) fill_bias(a, head0 + g, table + g * entries);
-    unsigned char *const stages = lds + (KEYS ? wave * F::STAGES * F::STAGE : 0);
-    const unsigned stages_addr = (unsigned)(size_t)(__attribute__((address_space(3))) unsigned char *)lds + (KEYS ? wave * F::STAGES * F::STAGE : 0);
+    const int width = BIAS ? bias_width(a.bias.reach, a.causal) : 0;
+    bool filled = false;
+    unsigned char *const stages = lds + (SHARED ? wave * F::STAGES * F::STAGE : 0);
+    const unsigned stages_addr = (unsigned)(size_t)(__attribute__((address_space(3))) unsigned char *)lds + (SHARED ? wave * F::STAGES * F::STAGE : 0);
     Reader<T, DP> reader;
     reader.init();
     Loader<T, DP, F::TILE, F::LOADERS, DIRECT> load_k, load_v;
-    load_k.init(a.k.row, a.D, KEYS ? lane : tid);
-    load_v.init(a.v.row, a.D, KEYS ? lane : tid);
-    const int columns = seq.q_len * a.pack;
+    load_k.init(a.k.row, a.D, SHARED ? lane : tid);
+    load_v.init(a.v.row, a.D, SHARED ? lane : tid);
     for (int tile0 = first_tile * ROWS; tile0 < columns; tile0 += a.tiles * ROWS) {
-        // ---- this wave's rows of q
-        const int mine0 = tile0 + (KEYS ? 0 : wave * MINE);
-        uint4 q[N][R::STEPS];
-        int pos[N], head[N], row[N];
-        bool there[N];
-#pragma unroll
-        for (int n = 0; n < N; ++n) {
-            const int c = mine0 + 32 * n + (lane & 31), in = min(c, columns - 1);
-            there[n] = c < columns;
-            row[n] = in / a.pack;
-            head[n] = in - row[n] * a.pack;
-            pos[n] = shift + row[n];
-            const char *p = rows_of(a.q, b, a.q_offsets != nullptr, seq.q0 + row[n], head0 + head[n]);
-#pragma unroll
-            for (int s = 0; s < R::STEPS; ++s) q[n][s] = chunk_of<T, DIRECT>(p, 2 * s + half, a.D);
-        }
-        // ---- the keys that any of them sees, and this workgroup's and this wave's tiles of them
+        // ---- the keys that any of this workgroup's rows sees, and its and this wave's tiles of them
+        const int mine0 = tile0 + (SHARED ? 0 : wave * 32);
         const int last = shift + (min(tile0 + ROWS, columns) - 1) / a.pack;                     // the last row's position
         const int end = a.causal ? max(0, min(seq.k_len, last + 1)) : seq.k_len;
-        const int lowest = shift + min(mine0, columns - 1) / a.pack, highest = shift + (min(mine0 + MINE, columns) - 1) / a.pack;
+        const int lowest = shift + min(mine0, columns - 1) / a.pack, highest = shift + (min(mine0 + 32, columns) - 1) / a.pack;
         const int tiles = (end + F::TILE - 1) / F::TILE, per = max((tiles + a.splits - 1) / a.splits, min(tiles, a.least));
-        const int t0 = split * per + (KEYS ? wave : 0), t1 = min(tiles, (split + 1) * per), step = KEYS ? 4 : 1;
+        const int from = split * per, t0 = from + (SHARED ? wave : 0), t1 = min(tiles, from + per), step = SHARED ? 4 : 1;
+        // ---- this wave's rows of q
+        const int column = mine0 + (lane & 31), in = min(column, columns - 1);
+        const bool there = column < columns;
+        const int row = in / a.pack, head = head0 + in - row * a.pack, pos = shift + row;
+        const long long slot = (seq.q_first + row) * a.heads + head;
+        if (a.splits > 1 && from >= t1 && split > 0) {
+            if (there && half == 0 && (!SHARED || wave == 0))
+                *reinterpret_cast<float2 *>(a.part_ml + 2 * ((long long)split * (a.q_all * a.heads) + slot)) = make_float2(-__builtin_inff(), 0.f);
+            continue;
+        }
         auto load = [&](int t, int buf) {
             const int k0 = t * F::TILE;
             unsigned char *const to = stages + buf * F::STAGE;
             const unsigned to_addr = stages_addr + buf * F::STAGE;
-            load_k.issue(to, to_addr, keys + (long long)k0 * a.k.row, end - k0, a.D, KEYS ? 0 : wave);
-            load_v.issue(to + F::HALF, to_addr + F::HALF, values + (long long)k0 * a.v.row, end - k0, a.D, KEYS ? 0 : wave);
+            load_k.issue(to, to_addr, keys + (long long)k0 * a.k.row, end - k0, a.D, SHARED ? 0 : wave);
+            load_v.issue(to + F::HALF, to_addr + F::HALF, values + (long long)k0 * a.v.row, end - k0, a.D, SHARED ? 0 : wave);
         };
         // A tile that has come; of the keys behind the last one the scores are masked, of the values there have to be zeros.
         auto clear = [&](int t, int buf) {
             const int rows = end - t * F::TILE;
-            if (rows < F::TILE) load_v.clear(stages + buf * F::STAGE + F::HALF, rows, KEYS ? 0 : wave);
+            if (rows < F::TILE) load_v.clear(stages + buf * F::STAGE + F::HALF, rows, SHARED ? 0 : wave);
         };
-        // top: the maximum that the exponents are taken from (it follows the scores' maximum when that is 2^8 above it); sum: of this lane's keys
-        float top[N], sum[N];
-        f32x16 acc[N][R::BLOCKS];
-#pragma unroll
-        for (int n = 0; n < N; ++n) {
-            top[n] = -__builtin_inff();
-            sum[n] = 0.f;
-#pragma unroll
-            for (int d = 0; d < R::BLOCKS; ++d)
-#pragma unroll
-                for (int i = 0; i < 16; ++i) acc[n][d][i] = 0.f;
-        }
-        bool left_out = false;
         if (F::STAGES == 2 && t0 < t1) load(t0, 0);
-        if constexpr (KEYS && BIAS) __syncthreads();
+        uint4 q[R::STEPS];
+        {
+            const char *p = rows_of(a.q, b, a.q_offsets != nullptr, seq.q0 + row, head);
+#pragma unroll
+            for (int s = 0; s < R::STEPS; ++s) q[s] = chunk_of<T, DIRECT>(p, 2 * s + half, a.D);
+        }
+        const float *const my_table = table + (head - head0) * width;
+        if constexpr (BIAS)
+            if (!filled) {
+                fill_bias(a, head0, a.pack, table);
+                filled = true;
+                if constexpr (SHARED) {
+                    tile::wait_lds();
+                    tile::meet();
+                }
+            }
+        // top: the maximum that the exponents are taken from (it follows the scores' maximum when that is 2^8 above it); sum: of this lane's keys
+        float top = -__builtin_inff(), sum = 0.f;
+        f32x16 acc[1][R::BLOCKS];
+#pragma unroll
+        for (int d = 0; d < R::BLOCKS; ++d)
+#pragma unroll
+            for (int i = 0; i < 16; ++i) acc[0][d][i] = 0.f;
+        bool left_out = false;
+        // One tile.  edge: some of it is masked; near: its offsets are not all in the bias's last bucket.  (One body for all of them: several would each
+        // want the sums in registers of their own.)
+        auto compute = [&](bool edge, bool near, int k0, const unsigned char *ktile) {
+            const unsigned char *const vtile = ktile + F::HALF;
+            f32x16 p[BLOCKS][1];
+#pragma unroll
+            for (int kb = 0; kb < BLOCKS; ++kb) {
+#pragma unroll
+                for (int i = 0; i < 16; ++i) p[kb][0][i] = 0.f;
+#pragma unroll
+                for (int s = 0; s < R::STEPS; ++s) p[kb][0] = scores<T>(reader.along(ktile, kb, s), q[s], p[kb][0]);
+            }
+            float by = a.scale2, plus = 0.f;        // what is still to be done to the scores
+            if (BIAS && near) {
+                const float *const bias = my_table + (k0 - pos) + 4 * half + a.bias.reach + MARGIN;
+#pragma unroll
+                for (int kb = 0; kb < BLOCKS; ++kb)
+#pragma unroll
+                    for (int i = 0; i < 16; ++i) p[kb][0][i] = fmaf(p[kb][0][i], a.scale2, bias[32 * kb + row_of(i, 0)]);
+                by = 1.f;
+            } else if (BIAS) {
+                plus = far_bias(a, my_table, k0 + F::TILE - 1 - lowest);
+                if (__any(!(fabsf(plus) < 4096.f))) {
+                    // (where the bias swallows the scores, as the type's lowest value does, it has to do so in every tile)
+#pragma unroll
+                    for (int kb = 0; kb < BLOCKS; ++kb)
+#pragma unroll
+                        for (int i = 0; i < 16; ++i) p[kb][0][i] = fmaf(p[kb][0][i], a.scale2, plus);
+                    by = 1.f;
+                    plus = 0.f;
+                }
+            }
+            if (edge) {
+                const int most = min(a.causal ? pos : end - 1, end - 1) - k0;
+#pragma unroll
+                for (int kb = 0; kb < BLOCKS; ++kb)
+#pragma unroll
+                    for (int i = 0; i < 16; ++i) p[kb][0][i] = 32 * kb + row_of(i, half) <= most ? p[kb][0][i] : -__builtin_inff();
+            }
+            float m = p[0][0][0];
+#pragma unroll
+            for (int kb = 0; kb < BLOCKS; ++kb)
+#pragma unroll
+                for (int i = 0; i < 16; ++i) m = fmaxf(m, p[kb][0][i]);
+            m = max_halves(m);
+            m = fmaf(m, by, plus);
+            if (__any(m > top + 8.f)) {
+                const float next = fmaxf(m, top);
+                const float back = top == next ? 1.f : __builtin_amdgcn_exp2f(top - next);
+                top = next;
+                sum *= back;
+#pragma unroll
+                for (int d = 0; d < R::BLOCKS; ++d)
+#pragma unroll
+                    for (int i = 0; i < 16; ++i) acc[0][d][i] *= back;
+            }
+            const float from = (top == -__builtin_inff() ? 0.f : top) - plus;
+            float part[4] = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+            for (int kb = 0; kb < BLOCKS; ++kb)
+#pragma unroll
+                for (int i = 0; i < 16; ++i) {
+                    const float e = __builtin_amdgcn_exp2f(fmaf(p[kb][0][i], by, -from));
+                    p[kb][0][i] = e;
+                    part[i & 3] += e;
+                }
+            sum += (part[0] + part[1]) + (part[2] + part[3]);
+            if (edge && a.causal && any_not_finite<T, DP, F::TILE>(vtile)) {
+                left_out = true;
+                return;
+            }
+#pragma unroll
+            for (int kb = 0; kb < BLOCKS; ++kb) weigh<T, DP, 1>(reader, vtile, kb, p[kb], acc);
+        };
         int buf = 0;
         for (int t = t0; t < t1; t += step, buf ^= F::STAGES - 1) {
-            if constexpr (KEYS) {
+            if constexpr (SHARED) {
                 tile::wait_lds();
                 if (F::STAGES == 1) {
                     load(t, 0);
@@ -127,108 +206,38 @@ __global__ __launch_bounds__(THREADS, N == 1 && sizeof(T) == 2 && !KEYS ? 2 : 1)
                 if (t + 1 < t1) load(t + 1, buf ^ 1);
             }
             const int k0 = t * F::TILE;
-            if (!KEYS && a.causal && k0 > highest) continue;
-            const unsigned char *const ktile = stages + buf * F::STAGE, *const vtile = ktile + F::HALF;
-            const bool border = a.causal && k0 + F::TILE - 1 > lowest, edge = border || k0 + F::TILE > end;
-            f32x16 p[BLOCKS][N];
-#pragma unroll
-            for (int kb = 0; kb < BLOCKS; ++kb) {
-#pragma unroll
-                for (int n = 0; n < N; ++n)
-#pragma unroll
-                    for (int i = 0; i < 16; ++i) p[kb][n][i] = 0.f;
-#pragma unroll
-                for (int s = 0; s < R::STEPS; ++s) {
-                    const uint4 k = reader.along(ktile, kb, s);
-#pragma unroll
-                    for (int n = 0; n < N; ++n) p[kb][n] = scores<T>(k, q[n][s], p[kb][n]);
-                }
-            }
-            if constexpr (BIAS) {
-#pragma unroll
-                for (int kb = 0; kb < BLOCKS; ++kb)
-#pragma unroll
-                    for (int n = 0; n < N; ++n) {
-                        const int j0 = k0 + 32 * kb;
-                        add_bias(a, table + head[n] * entries, j0 - pos[n], j0 - highest, j0 + 31 - lowest, a.scale2, p[kb][n]);
-                    }
-            }
-            if (edge) {
-#pragma unroll
-                for (int kb = 0; kb < BLOCKS; ++kb)
-#pragma unroll
-                    for (int n = 0; n < N; ++n) {
-                        const int most = min(a.causal ? pos[n] : end - 1, end - 1) - k0 - 32 * kb;
-#pragma unroll
-                        for (int i = 0; i < 16; ++i) p[kb][n][i] = row_of(i, half) <= most ? p[kb][n][i] : -__builtin_inff();
-                    }
-            }
-            const float by = BIAS ? 1.f : a.scale2;
-#pragma unroll
-            for (int n = 0; n < N; ++n) {
-                float m = p[0][n][0];
-#pragma unroll
-                for (int kb = 0; kb < BLOCKS; ++kb)
-#pragma unroll
-                    for (int i = 0; i < 16; ++i) m = fmaxf(m, p[kb][n][i]);
-                m = max_halves(m) * by;
-                if (__any(m > top[n] + 8.f)) {
-                    const float next = fmaxf(m, top[n]);
-                    const float back = top[n] == next ? 1.f : __builtin_amdgcn_exp2f(top[n] - next);
-                    top[n] = next;
-                    sum[n] *= back;
-#pragma unroll
-                    for (int d = 0; d < R::BLOCKS; ++d)
-#pragma unroll
-                        for (int i = 0; i < 16; ++i) acc[n][d][i] *= back;
-                }
-                const float from = top[n] == -__builtin_inff() ? 0.f : top[n];
-                float part[4] = {0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-                for (int kb = 0; kb < BLOCKS; ++kb)
-#pragma unroll
-                    for (int i = 0; i < 16; ++i) {
-                        const float e = __builtin_amdgcn_exp2f(BIAS ? p[kb][n][i] - from : fmaf(p[kb][n][i], a.scale2, -from));
-                        p[kb][n][i] = e;
-                        part[i & 3] += e;
-                    }
-                sum[n] += (part[0] + part[1]) + (part[2] + part[3]);
-            }
-#pragma unroll
-            for (int kb = 0; kb < BLOCKS; ++kb) {
-                if (border && any_not_finite<T, DP>(vtile, kb)) left_out = true;
-                else weigh<T, DP, N>(reader, vtile, kb, p[kb], acc);
-            }
+            if (!SHARED && ((a.causal && k0 > highest) || mine0 >= columns)) continue;
+            const unsigned char *const ktile = stages + buf * F::STAGE;
+            const bool edge = k0 + F::TILE > end || (a.causal && k0 + F::TILE - 1 > lowest);
+            compute(edge, BIAS && !is_far(a, k0 - highest, k0 + F::TILE - 1 - lowest), k0, ktile);
         }
+        if (!SHARED && a.causal) tile::meet();
         if (left_out) {
-            // the blocks on the border that hold something that is not finite
+            // the tiles on the border that hold something that is not finite
+            const char *const mine = rows_of(a.q, b, a.q_offsets != nullptr, seq.q0 + row, head);
+            add_rows<T, DP>(SHARED ? stages : lds + wave * 4096, a.D, acc[0], [&](auto add) {
 #pragma unroll 1
-            for (int t = t0; t < t1; t += step)
+                for (int t = t0; t < t1; t += step) {
+                    const int j0 = t * F::TILE, count = min(F::TILE, end - j0);
+                    if ((j0 + F::TILE <= end && j0 + F::TILE - 1 <= lowest) || j0 > highest) continue;
+                    if (!any_not_finite<T>(values + (long long)j0 * a.v.row, a.v.row, count, a.D)) continue;
 #pragma unroll 1
-                for (int j0 = t * F::TILE; j0 < min(end, (t + 1) * F::TILE); j0 += 32) {
-                    const char *const rows = values + (long long)j0 * a.v.row;
-                    if (t * F::TILE + F::TILE - 1 <= lowest || t * F::TILE > highest || !any_not_finite<T>(rows, a.v.row, end - j0, a.D)) continue;
-#pragma unroll
-                    for (int n = 0; n < N; ++n) {
-                        const char *const mine = rows_of(a.q, b, a.q_offsets != nullptr, seq.q0 + row[n], head0 + head[n]);
-#pragma unroll 1
-                        for (int j = j0; j < min(end, j0 + 32); ++j) {
-                            if (j > pos[n]) continue;
-                            const float s = dot<T>(mine, keys + (long long)j * a.k.row, a.D);
-                            const float x = BIAS ? fmaf(s, a.scale2, table[head[n] * entries + bias_entry(a, j - pos[n])]) : s * a.scale2;
-                            add_row<T, DP>(values + (long long)j * a.v.row, a.D, __builtin_amdgcn_exp2f(x - (top[n] == -__builtin_inff() ? 0.f : top[n])), acc[n]);
-                        }
+                    for (int j = j0; j < j0 + count; ++j) {
+                        if (j > pos) continue;
+                        float x = dot<T>(mine, keys + (long long)j * a.k.row, a.D) * a.scale2;
+                        if constexpr (BIAS) x += bias_at(a, head, j - pos);
+                        add(__builtin_amdgcn_exp2f(x - (top == -__builtin_inff() ? 0.f : top)), values + (long long)j * a.v.row);
                     }
                 }
+            });
         }
         // ---- what leaves
-#pragma unroll
-        for (int n = 0; n < N; ++n) sum[n] = add_halves(sum[n]);
-        int d0 = 0, d1 = 4 * R::BLOCKS;                         // groups of four elements that this wave stores
-        if constexpr (KEYS) {
+        sum = add_halves(sum);
+        int d0 = 0;                             // groups of four elements that this wave stores
+        if constexpr (SHARED) {
             // the waves' sums over one maximum, a quarter of the elements in each wave
             tile::wait_lds();
-            __syncthreads();
+            tile::meet();
             float *const sums = reinterpret_cast<float *>(lds), *const ml = sums + 4 * DP * 32;
             static_assert(4 * DP * 32 * 4 + 4 * 64 * 4 <= F::TILES_BYTES, "they fit where the tiles were");
 #pragma unroll
@@ -236,10 +245,11 @@ __global__ __launch_bounds__(THREADS, N == 1 && sizeof(T) == 2 && !KEYS ? 2 : 1)
 #pragma unroll
                 for (int i = 0; i < 16; ++i) sums[((wave * R::BLOCKS + d) * 16 + i) * 64 + lane] = acc[0][d][i];
             if (half == 0) {
-                ml[wave * 64 + lane] = top[0];
-                ml[wave * 64 + 32 + lane] = sum[0];
+                ml[wave * 64 + lane] = top;
+                ml[wave * 64 + 32 + lane] = sum;
             }
-            __syncthreads();
+            tile::wait_lds();
+            tile::meet();
             float m = -__builtin_inff(), weight[4], total_sum = 0.f;
 #pragma unroll
             for (int w = 0; w < 4; ++w) m = fmaxf(m, ml[w * 64 + (lane & 31)]);
@@ -251,10 +261,9 @@ __global__ __launch_bounds__(THREADS, N == 1 && sizeof(T) == 2 && !KEYS ? 2 : 1)
                 if (l == 0.f) weight[w] = 0.f;
                 total_sum = l == 0.f ? total_sum : fmaf(weight[w], l, total_sum);
             }
-            top[0] = m;
-            sum[0] = total_sum;
+            top = m;
+            sum = total_sum;
             d0 = wave * R::BLOCKS;
-            d1 = d0 + R::BLOCKS;
 #pragma unroll
             for (int g = 0; g < R::BLOCKS; ++g)
 #pragma unroll
@@ -268,44 +277,36 @@ __global__ __launch_bounds__(THREADS, N == 1 && sizeof(T) == 2 && !KEYS ? 2 : 1)
                     acc[0][g >> 2][4 * (g & 3) + e] = v;
                 }
         }
-#pragma unroll
-        for (int n = 0; n < N; ++n) {
-            if (!there[n]) continue;
-            const int h = head0 + head[n];
-            const long long slot = (seq.q_first + row[n]) * a.heads + h;
+        if (there) {
+            const bool none = sum == 0.f, one = half == 0 && (!SHARED || wave == 0);
             const int D = opaque(a.D), first = opaque(8 * d0 + 4 * half);
             if (a.splits > 1) {
-                const long long in = (long long)split * (a.q_all * a.heads) + slot;
-                if (half == 0 && (!KEYS || wave == 0)) *reinterpret_cast<float2 *>(a.part_ml + 2 * in) = make_float2(top[n], sum[n]);
+                const long long part = (long long)split * (a.q_all * a.heads) + slot;
+                if (one) *reinterpret_cast<float2 *>(a.part_ml + 2 * part) = make_float2(top, sum);
 #pragma unroll
-                for (int g = 0; g < (KEYS ? R::BLOCKS : 4 * R::BLOCKS); ++g) {
-                    const int d = first + 8 * g;
-                    if (d < D)
-                        store4<float, DIRECT>(a.part_o + in * a.D + d, D - d, acc[n][g >> 2][4 * (g & 3)], acc[n][g >> 2][4 * (g & 3) + 1], acc[n][g >> 2][4 * (g & 3) + 2],
-                               acc[n][g >> 2][4 * (g & 3) + 3]);
+                for (int g = 0; g < (SHARED ? R::BLOCKS : 4 * R::BLOCKS); ++g) {
+                    const int d = first + 8 * g, x = g >> 2, y = 4 * (g & 3);
+                    if (d < D) store4<float, DIRECT>(a.part_o + part * a.D + d, D - d, acc[0][x][y], acc[0][x][y + 1], acc[0][x][y + 2], acc[0][x][y + 3]);
                 }
-                continue;
-            }
-            const float scale = sum[n] == 0.f ? 0.f : 1.f / sum[n];
-            T *const out = reinterpret_cast<T *>(rows_of(a.o, b, a.q_offsets != nullptr, seq.q0 + row[n], h));
+            } else {
+                const float scale = none ? 0.f : 1.f / sum;
+                T *const out = reinterpret_cast<T *>(rows_of(a.o, b, a.q_offsets != nullptr, seq.q0 + row, head));
 #pragma unroll
-            for (int g = 0; g < (KEYS ? R::BLOCKS : 4 * R::BLOCKS); ++g) {
-                const int d = first + 8 * g;
-                if (d < D)
-                    store4<T, DIRECT>(out + d, D - d, acc[n][g >> 2][4 * (g & 3)] * scale, acc[n][g >> 2][4 * (g & 3) + 1] * scale,
-                           acc[n][g >> 2][4 * (g & 3) + 2] * scale, acc[n][g >> 2][4 * (g & 3) + 3] * scale);
-            }
-            if (a.saved && half == 0 && (!KEYS || wave == 0)) {
-                // a row that sees no key: a maximum that leaves every weight at zero
-                const bool none = sum[n] == 0.f;
-                const float m = top[n] == -__builtin_inff() ? 0.f : top[n];
-                *reinterpret_cast<float2 *>(a.saved + 2 * slot) = make_float2(none ? __builtin_inff() : m, none ? 0.f : __builtin_amdgcn_logf(sum[n]));
+                for (int g = 0; g < (SHARED ? R::BLOCKS : 4 * R::BLOCKS); ++g) {
+                    const int d = first + 8 * g, x = g >> 2, y = 4 * (g & 3);
+                    if (d < D)
+                        store4<T, DIRECT>(out + d, D - d, acc[0][x][y] * scale, acc[0][x][y + 1] * scale, acc[0][x][y + 2] * scale, acc[0][x][y + 3] * scale);
+                }
+                // (a row that sees no key: a maximum that leaves every weight at zero)
+                if (a.saved && one)
+                    *reinterpret_cast<float2 *>(a.saved + 2 * slot) =
+                        make_float2(none ? __builtin_inff() : top == -__builtin_inff() ? 0.f : top, none ? 0.f : __builtin_amdgcn_logf(sum));
             }
         }
         // (another round of rows uses the tiles again)
         tile::wait_loads<0>();
         tile::wait_lds();
-        __syncthreads();
+        tile::meet();
     }
 }
 

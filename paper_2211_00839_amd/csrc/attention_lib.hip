@@ -7,7 +7,7 @@ namespace {
 attn_rules::Cut forward_cut(const rcd_attention_shape &s)
 {
     return attn_rules::cut_of(s.batch, s.heads, s.heads / s.kv_heads, attn_rules::longest_of(s.longest_q, s.q_rows, s.batch, s.q_offsets_dev != nullptr),
-                              attn_rules::longest_of(s.longest_k, s.k_rows, s.batch, s.k_offsets_dev != nullptr), s.q_rows, s.dt == RCD_F32, entries_of(s));
+                              attn_rules::longest_of(s.longest_k, s.k_rows, s.batch, s.k_offsets_dev != nullptr), s.q_rows, s.dt == RCD_F32, width_of(s));
 }
 
 SetUp g_set_up;
@@ -18,8 +18,8 @@ int set_up()
         using T = decltype(t);
         constexpr int DP = decltype(dp)::value;
         constexpr bool BIAS = decltype(bias)::value, DIRECT = decltype(direct)::value;
-        const hipError_t e = raise_lds(&k_attention<T, DP, 1, false, BIAS, DIRECT>);
-        return e != hipSuccess ? e : raise_lds(&k_attention<T, DP, 1, true, BIAS, DIRECT>);
+        const hipError_t e = raise_lds(&k_attention<T, DP, false, BIAS, DIRECT>);
+        return e != hipSuccess ? e : raise_lds(&k_attention<T, DP, true, BIAS, DIRECT>);
     });
 }
 
@@ -73,14 +73,14 @@ int rcd_attention(const rcd_attention_shape *s, const rcd_heads *q, const rcd_he
     a.splits = (int)c.splits;
     a.least = (int)c.least;
     const int64_t groups = c.tiles * (s->heads / c.pack) * (s->batch + (a.clear ? 1 : 0)) * c.splits;
-    const int bias_bytes = (int)entries_of(*s) * c.pack * 4;
+    const int bias_bytes = width_of(*s) * c.pack * 4;
     const bool direct = aligned(a.k, s->d, s->dt) && aligned(a.v, s->d, s->dt);
     ENC_TRY(with_variant(s->dt, s->d, s->bias_dev != nullptr, direct, [&](auto t, auto dp, auto bias, auto way) {
         using T = decltype(t);
         constexpr int DP = decltype(dp)::value;
         constexpr bool BIAS = decltype(bias)::value, DIRECT = decltype(way)::value;
-        if (c.keys) return launch(&k_attention<T, DP, 1, true, BIAS, DIRECT>, groups, Forward<T, DP, true>::TILES_BYTES + bias_bytes, a, stream);
-        return launch(&k_attention<T, DP, 1, false, BIAS, DIRECT>, groups, Forward<T, DP, false>::TILES_BYTES + bias_bytes, a, stream);
+        if (c.shared) return launch(&k_attention<T, DP, true, BIAS, DIRECT>, groups, Forward<T, DP, true>::TILES_BYTES + bias_bytes, a, stream);
+        return launch(&k_attention<T, DP, false, BIAS, DIRECT>, groups, Forward<T, DP, false>::TILES_BYTES + bias_bytes, a, stream);
     }));
     if (c.splits > 1) {
         const int64_t slots = a.q_all * s->heads;
