@@ -21,11 +21,17 @@ template <typename T, int DP, bool SHARED, bool BIAS> struct Backward {
     static constexpr int STAGES = SHARED && (R::BYTES == 512 || (BIAS && R::BYTES == 256)) ? 1 : 2;
     static constexpr int HALF = TILE * R::BYTES, STAGE = 2 * HALF, TILES_BYTES = STAGES * STAGE * (SHARED ? 4 : 1);
     static constexpr int LOADS = 2 * TILE * R::CHUNKS / LOADERS;
-    // gradients of k and v: what is known of each query of a tile
-    static constexpr int FACTS = BIAS ? 3 : 2, FACTS_STAGE = FACTS * TILE, FACTS_BYTES = STAGES * FACTS_STAGE * 4 * (SHARED ? 4 : 1);
     // the bias's gradient: a wave's block of ds on its way to the sums along its diagonals
     static constexpr int TURN_PITCH = 40, TURN_BYTES = 32 * TURN_PITCH * 4;
     static_assert(!SHARED || 4 * DP * 32 * 4 <= TILES_BYTES, "the waves' sums fit where the tiles were");
+    // gradients of k and v.  Of wide bf16 rows two waves to a SIMD have no registers for their rows of v, which lie in LDS, and tiles of 32
+    // leave room for them (T 8192, 32 heads of 128: 2.40 ms; one wave to a SIMD with all of it in registers 3.0, with the two products of
+    // a block side by side and spilled registers 2.9).
+    static constexpr bool TIGHT = !SHARED && sizeof(T) == 2 && DP == 128;
+    static constexpr int KV_TILE = TIGHT ? 32 : TILE, KV_HALF = KV_TILE * R::BYTES, KV_STAGE = 2 * KV_HALF, KV_TILES_BYTES = STAGES * KV_STAGE * (SHARED ? 4 : 1),
+                         KV_LOADS = 2 * KV_TILE * R::CHUNKS / LOADERS, V_BYTES = TIGHT ? 128 * R::BYTES : 0;
+    // what is known of each query of a tile
+    static constexpr int FACTS = BIAS ? 3 : 2, FACTS_STAGE = FACTS * KV_TILE, FACTS_BYTES = STAGES * FACTS_STAGE * 4 * (SHARED ? 4 : 1);
 };
 
 // The four waves' sums, a quarter of the elements in each wave: groups of four elements from 8 wave BLOCKS on.  Every wave has to come along.
@@ -66,7 +72,7 @@ __device__ __forceinline__ void store_row(T *to, int first, int D_, float scale,
 }
 
 template <typename T, int DP, bool SHARED, bool BIAS, bool DIRECT>
-__global__ __launch_bounds__(THREADS, sizeof(T) == 2 && !SHARED ? 2 : 1) void k_attention_dq(Args a)
+__global__ __launch_bounds__(THREADS, sizeof(T) == 2 && !SHARED ? (DP == 64 ? 3 : 2) : 1) void k_attention_dq(Args a)
 {
     using W = Backward<T, DP, SHARED, BIAS>;
     using R = Row<T, DP>;
@@ -186,13 +192,8 @@ __global__ __launch_bounds__(THREADS, sizeof(T) == 2 && !SHARED ? 2 : 1) void k_
             for (int kb = 0; kb < BLOCKS; ++kb) {
                 __builtin_amdgcn_sched_barrier(0);          // (a block's fragments at a time: there are no registers for more)
                 const int j0 = k0 + 32 * kb;
-                f32x16 s, dp;
-#pragma unroll
-                for (int i = 0; i < 16; ++i) s[i] = dp[i] = 0.f;
-#pragma unroll
-                for (int f = 0; f < R::STEPS; ++f) s = scores<T>(reader.along(ktile, kb, f), q[f], s);
-#pragma unroll
-                for (int f = 0; f < R::STEPS; ++f) dp = scores<T>(reader.along(vtile, kb, f), g[f], dp);
+                f32x16 s = scores<T, DP>(reader, ktile, kb, q);
+                const f32x16 dp = scores<T, DP>(reader, vtile, kb, g);
                 f32x16 ds[1];
                 if constexpr (BIAS) {
                     if (near) {
@@ -348,20 +349,23 @@ template <typename T> __global__ __launch_bounds__(THREADS) void k_bias_gradient
     if (threadIdx.x == 0) to[c * heads + head] = (T)((sums[0] + sums[1]) + (sums[2] + sums[3]));
 }
 
-template <typename T, int DP, bool SHARED, bool BIAS, bool DIRECT> __global__ __launch_bounds__(THREADS, 1) void k_attention_dkv(Args a)
+template <typename T, int DP, bool SHARED, bool BIAS, bool DIRECT> __global__ __launch_bounds__(THREADS, sizeof(T) == 2 && !SHARED ? 2 : 1) void k_attention_dkv(Args a)
 {
     using W = Backward<T, DP, SHARED, BIAS>;
     using R = Row<T, DP>;
-    constexpr int BLOCKS = W::TILE / 32;
+    constexpr int BLOCKS = W::KV_TILE / 32;
     extern __shared__ __align__(1024) unsigned char lds[];
     const int tid = threadIdx.x, lane = tid & 63, half = lane >> 5, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
-    const int total = a.tiles * a.kv_heads * (a.batch + (a.clear && a.k_offsets ? 1 : 0));
+    const int total = a.tiles * a.kv_heads * (a.batch + (a.clear && a.k_offsets ? 1 : 0)) * a.splits;
     int at = place_of(blockIdx.x, total);
     if (at >= total) return;
+    const int split = at % a.splits;
+    at /= a.splits;
     const int first_tile = at % a.tiles;                        // (causal: the first keys have the most queries)
     at /= a.tiles;
     const int kv_head = at % a.kv_heads, b = at / a.kv_heads;
     if (b == a.batch) {
+        if (split > 0) return;
         clear_rows<T>(a.dk, a.k_offsets, a.batch, a.k_rows, kv_head, a.D, first_tile, a.tiles);
         clear_rows<T>(a.dv, a.k_offsets, a.batch, a.k_rows, kv_head, a.D, first_tile, a.tiles);
         return;
@@ -369,66 +373,71 @@ template <typename T, int DP, bool SHARED, bool BIAS, bool DIRECT> __global__ __
     const Sequence seq = sequence(a, b);
     const int shift = seq.k_len - seq.q_len;
     const bool q_ragged = a.q_offsets != nullptr, k_ragged = a.k_offsets != nullptr;
-    float *const all_facts = reinterpret_cast<float *>(lds + W::TILES_BYTES), *const table = all_facts + W::FACTS_BYTES / 4;
+    unsigned char *const my_values = lds + W::KV_TILES_BYTES + wave * 32 * R::BYTES;       // (TIGHT)
+    float *const all_facts = reinterpret_cast<float *>(lds + W::KV_TILES_BYTES + W::V_BYTES), *const table = all_facts + W::FACTS_BYTES / 4;
     float *const facts = all_facts + (SHARED ? wave * W::STAGES * W::FACTS_STAGE : 0);
-    unsigned char *const stages = lds + (SHARED ? wave * W::STAGES * W::STAGE : 0);
+    unsigned char *const stages = lds + (SHARED ? wave * W::STAGES * W::KV_STAGE : 0);
     const unsigned lds_addr = (unsigned)(size_t)(__attribute__((address_space(3))) unsigned char *)lds;
-    const unsigned stages_addr = lds_addr + (SHARED ? wave * W::STAGES * W::STAGE : 0);
-    const unsigned facts_addr = lds_addr + W::TILES_BYTES + (SHARED ? wave * W::STAGES * W::FACTS_STAGE * 4 : 0);
+    const unsigned stages_addr = lds_addr + (SHARED ? wave * W::STAGES * W::KV_STAGE : 0);
+    const unsigned facts_addr = lds_addr + W::KV_TILES_BYTES + W::V_BYTES + (SHARED ? wave * W::STAGES * W::FACTS_STAGE * 4 : 0);
     const int loader = SHARED ? 0 : wave;
     int table_of = -1;                                          // the query head whose bias is there
     Reader<T, DP> reader;
     reader.init();
-    Loader<T, DP, W::TILE, W::LOADERS, DIRECT> load_q, load_g;
+    Loader<T, DP, W::KV_TILE, W::LOADERS, DIRECT> load_q, load_g;
     load_q.init(a.q.row, a.D, SHARED ? lane : tid);
     load_g.init(a.dout.row, a.D, SHARED ? lane : tid);
     const int rows = a.clear && !k_ragged ? a.k_rows : seq.k_len;       // rows behind the sequence get zeros
     for (int tile0 = first_tile * W::ROWS; tile0 < rows; tile0 += a.tiles * W::ROWS) {
         const int mine0 = tile0 + (SHARED ? 0 : wave * 32), key = mine0 + (lane & 31), h_key = min(key, seq.k_len - 1);
         const bool there = key < seq.k_len;
-        const int q_tiles = (seq.q_len + W::TILE - 1) / W::TILE, q_from = a.causal ? min(max(0, tile0 - shift) / W::TILE, q_tiles) : 0;
+        const int q_tiles = (seq.q_len + W::KV_TILE - 1) / W::KV_TILE, q_from = a.causal ? min(max(0, tile0 - shift) / W::KV_TILE, q_tiles) : 0;
         const int per = tile0 < seq.k_len ? q_tiles - q_from : 0;
-        const int count = per * a.group, step = SHARED ? 4 : 1;
-        const int rounds = SHARED && BIAS ? a.group : 1, each = SHARED && BIAS ? per : count;       // (a bias is a head's)
+        // this workgroup's tiles, of all the heads' end to end: c0 .. c1 - 1
+        const int count = per * a.group, c0 = (int)((long long)count * split / a.splits), c1 = (int)((long long)count * (split + 1) / a.splits);
+        const int c_mine = c0 + (SHARED ? wave : 0), c_first = SHARED && BIAS && c1 > c0 ? min(c1, (c0 / per + 1) * per) : c1;      // (its first head's end)
         auto load = [&](int c, int buf) {
-            const int g = c / per, i0 = (q_from + c - g * per) * W::TILE, head = kv_head * a.group + g;
+            const int g = c / per, i0 = (q_from + c - g * per) * W::KV_TILE, head = kv_head * a.group + g;
             const char *pq = rows_of(a.q, b, q_ragged, seq.q0 + i0, head), *pg = rows_of(a.dout, b, q_ragged, seq.q0 + i0, head);
-            unsigned char *const to = stages + buf * W::STAGE;
-            const unsigned to_addr = stages_addr + buf * W::STAGE;
+            unsigned char *const to = stages + buf * W::KV_STAGE;
+            const unsigned to_addr = stages_addr + buf * W::KV_STAGE;
             load_q.issue(to, to_addr, pq, seq.q_len - i0, a.D, loader);
-            load_g.issue(to + W::HALF, to_addr + W::HALF, pg, seq.q_len - i0, a.D, loader);
+            load_g.issue(to + W::KV_HALF, to_addr + W::KV_HALF, pg, seq.q_len - i0, a.D, loader);
             // what the exponents are taken from, delta, and with a bias the sum's logarithm by itself: a plane of each
 #pragma unroll
             for (int f = 0; f < W::FACTS; ++f) {
                 if (!SHARED && wave != f) continue;
                 const int plane = !BIAS ? f : f == 0 ? 2 : f == 1 ? 1 : 3;
                 const float *from = a.stats + plane * a.plane + (long long)head * a.q_all + seq.q_first + i0;
-                if (lane < W::TILE) bring4(uniform(from), min(lane, seq.q_len - 1 - i0) * 4, facts_addr + (buf * W::FACTS_STAGE + f * W::TILE) * 4);
+                if (lane < W::KV_TILE) bring4(uniform(from), min(lane, seq.q_len - 1 - i0) * 4, facts_addr + (buf * W::FACTS_STAGE + f * W::KV_TILE) * 4);
             }
         };
         // A tile that has come; rows that are not there become zeros with weights of zero.
         auto clear = [&](int i0, int buf) {
             const int rows = seq.q_len - i0;
-            if (rows >= W::TILE) return;
-            load_q.clear(stages + buf * W::STAGE, rows, loader);
-            load_g.clear(stages + buf * W::STAGE + W::HALF, rows, loader);
+            if (rows >= W::KV_TILE) return;
+            load_q.clear(stages + buf * W::KV_STAGE, rows, loader);
+            load_g.clear(stages + buf * W::KV_STAGE + W::KV_HALF, rows, loader);
 #pragma unroll
             for (int f = 0; f < W::FACTS; ++f) {
                 if (!SHARED && wave != f) continue;
-                if (lane < W::TILE && lane >= rows) facts[buf * W::FACTS_STAGE + f * W::TILE + lane] = f == 0 ? __builtin_inff() : 0.f;
+                if (lane < W::KV_TILE && lane >= rows) facts[buf * W::FACTS_STAGE + f * W::KV_TILE + lane] = f == 0 ? __builtin_inff() : 0.f;
             }
         };
-        if (W::STAGES == 2 && (SHARED ? wave : 0) < each) load(SHARED ? wave : 0, 0);
-        uint4 k[R::STEPS], v[R::STEPS];
+        if (W::STAGES == 2 && c_mine < c_first) load(c_mine, 0);
+        uint4 k[R::STEPS], v[W::TIGHT ? 1 : R::STEPS];
         {
             const char *pk = rows_of(a.k, b, k_ragged, seq.k0 + max(h_key, 0), kv_head), *pv = rows_of(a.v, b, k_ragged, seq.k0 + max(h_key, 0), kv_head);
 #pragma unroll
             for (int s = 0; s < R::STEPS; ++s) {
-                k[s] = v[s] = make_uint4(0, 0, 0, 0);
-                if (count > 0) {
-                    k[s] = chunk_of<T, DIRECT>(pk, 2 * s + half, a.D);
-                    v[s] = chunk_of<T, DIRECT>(pv, 2 * s + half, a.D);
+                uint4 x = make_uint4(0, 0, 0, 0), y = x;
+                if (c1 > c0) {
+                    x = chunk_of<T, DIRECT>(pk, 2 * s + half, a.D);
+                    y = chunk_of<T, DIRECT>(pv, 2 * s + half, a.D);
                 }
+                k[s] = x;
+                if constexpr (W::TIGHT) *reinterpret_cast<uint4 *>(my_values + (reader.here ^ (s << 5))) = y;
+                else v[s] = y;
             }
         }
         f32x16 dk[1][R::BLOCKS], dv[1][R::BLOCKS];
@@ -438,86 +447,105 @@ template <typename T, int DP, bool SHARED, bool BIAS, bool DIRECT> __global__ __
             for (int i = 0; i < 16; ++i) dk[0][d][i] = dv[0][d][i] = 0.f;
         bool left_out = false;
         auto compute = [&](bool edge, bool near, int i_tile, int buf) {
-            const unsigned char *const qtile = stages + buf * W::STAGE, *const gtile = qtile + W::HALF;
+            const unsigned char *const qtile = stages + buf * W::KV_STAGE, *const gtile = qtile + W::KV_HALF;
             const float *const fact = facts + buf * W::FACTS_STAGE;
-            const bool skip = edge && (any_not_finite<T, DP, W::TILE>(gtile) || any_not_finite<T, DP, W::TILE>(qtile));
+            const bool skip = edge && (any_not_finite<T, DP, W::KV_TILE>(gtile) || any_not_finite<T, DP, W::KV_TILE>(qtile));
             left_out |= skip;
 #pragma unroll
             for (int rb = 0; rb < BLOCKS; ++rb) {
-                __builtin_amdgcn_sched_barrier(0);          // (a block's fragments at a time: there are no registers for more)
                 const int p0 = shift + i_tile + 32 * rb;
-                f32x16 s, dp;
-#pragma unroll
-                for (int i = 0; i < 16; ++i) s[i] = dp[i] = 0.f;
-#pragma unroll
-                for (int f = 0; f < R::STEPS; ++f) s = scores<T>(reader.along(qtile, rb, f), k[f], s);
-#pragma unroll
-                for (int f = 0; f < R::STEPS; ++f) dp = scores<T>(reader.along(gtile, rb, f), v[f], dp);
+                f32x16 p[1] = {scores<T, DP>(reader, qtile, rb, k)}, ds[1];
                 if constexpr (BIAS) {
                     if (near) {
                         const float *const bias = table + (key - p0) - 4 * half + a.bias.reach + MARGIN;
 #pragma unroll
-                        for (int i = 0; i < 16; ++i) s[i] = fmaf(s[i], a.scale2, bias[-row_of(i, 0)]);
+                        for (int i = 0; i < 16; ++i) p[0][i] = fmaf(p[0][i], a.scale2, bias[-row_of(i, 0)]);
                     } else {
                         const float bias = far_bias(a, table, mine0 + 31 - (shift + i_tile));
 #pragma unroll
-                        for (int i = 0; i < 16; ++i) s[i] = fmaf(s[i], a.scale2, bias);
+                        for (int i = 0; i < 16; ++i) p[0][i] = fmaf(p[0][i], a.scale2, bias);
                     }
                 }
-                f32x16 p[1], ds[1];
+                const float *const known = fact + 32 * rb + 4 * half;
 #pragma unroll
                 for (int f = 0; f < 4; ++f) {
-                    const int r = 32 * rb + 8 * f + 4 * half;
-                    const f32x4 from = *reinterpret_cast<const f32x4 *>(fact + r), delta = *reinterpret_cast<const f32x4 *>(fact + W::TILE + r);
+                    const f32x4 from = *reinterpret_cast<const f32x4 *>(known + 8 * f);
                     f32x4 log_sum = {0.f, 0.f, 0.f, 0.f};
-                    if constexpr (BIAS) log_sum = *reinterpret_cast<const f32x4 *>(fact + 2 * W::TILE + r);
+                    if constexpr (BIAS) log_sum = *reinterpret_cast<const f32x4 *>(known + 2 * W::KV_TILE + 8 * f);
 #pragma unroll
                     for (int e = 0; e < 4; ++e) {
-                        const int i = 4 * f + e;
-                        p[0][i] = __builtin_amdgcn_exp2f(BIAS ? (s[i] - from[e]) - log_sum[e] : fmaf(s[i], a.scale2, -from[e]));
-                        ds[0][i] = p[0][i] * (dp[i] - delta[e]);
+                        const float x = p[0][4 * f + e];
+                        p[0][4 * f + e] = __builtin_amdgcn_exp2f(BIAS ? (x - from[e]) - log_sum[e] : fmaf(x, a.scale2, -from[e]));
                     }
+                }
+                auto hide = [&](f32x16 &x) {
+#pragma unroll
+                    for (int i = 0; i < 16; ++i) x[i] = key <= p0 + row_of(i, half) ? x[i] : 0.f;
+                };
+                if constexpr (W::TIGHT) {
+                    if (edge) hide(p[0]);
+                    if (!skip) weigh<T, DP, 1>(reader, gtile, rb, p, dv);
+                    __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+                    for (int i = 0; i < 16; ++i) ds[0][i] = 0.f;
+                    const int here = opaque(reader.here);
+#pragma unroll
+                    for (int f = 0; f < R::STEPS; ++f) ds[0] = scores<T>(reader.along(gtile, here, rb, f), reader.along(my_values, here, 0, f), ds[0]);
+                } else {
+                    ds[0] = scores<T, DP>(reader, gtile, rb, v);
+                }
+#pragma unroll
+                for (int f = 0; f < 4; ++f) {
+                    const f32x4 delta = *reinterpret_cast<const f32x4 *>(known + W::KV_TILE + 8 * f);
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) ds[0][4 * f + e] = p[0][4 * f + e] * (ds[0][4 * f + e] - delta[e]);
                 }
                 if (edge) {
-#pragma unroll
-                    for (int i = 0; i < 16; ++i) {
-                        const bool in = key <= p0 + row_of(i, half);
-                        p[0][i] = in ? p[0][i] : 0.f;
-                        ds[0][i] = in ? ds[0][i] : 0.f;
-                    }
+                    if (!W::TIGHT) hide(p[0]);
+                    hide(ds[0]);
                 }
                 if (!skip) {
-                    weigh<T, DP, 1>(reader, gtile, rb, p, dv);
+                    if (!W::TIGHT) weigh<T, DP, 1>(reader, gtile, rb, p, dv);
                     weigh<T, DP, 1>(reader, qtile, rb, ds, dk);
                 }
+                __builtin_amdgcn_sched_barrier(0);          // (a block's fragments at a time: there are no registers for more)
             }
         };
         auto choose = [&](int i_tile, int buf) {
-            const int p0 = shift + i_tile, p1 = p0 + W::TILE - 1;       // the tile's positions
+            const int p0 = shift + i_tile, p1 = p0 + W::KV_TILE - 1;       // the tile's positions
             if (mine0 >= seq.k_len || (a.causal && p1 < mine0)) return;
             compute(a.causal && p0 < mine0 + 31, BIAS && !is_far(a, mine0 - p1, mine0 + 31 - p0), i_tile, buf);
         };
+        // Brings the bias of a query head; every wave has to come along.
+        auto bias_of = [&](int g) {
+            fill_bias(a, kv_head * a.group + g, 1, table);
+            table_of = g;
+            tile::wait_lds();
+            tile::meet();
+        };
+        int buf = 0;
         if constexpr (SHARED) {
-            for (int g = 0; g < rounds; ++g) {
-                if constexpr (BIAS) {
-                    tile::wait_lds();
-                    tile::meet();
-                    fill_bias(a, kv_head * a.group + g, 1, table);
-                    tile::wait_lds();
-                    tile::meet();
-                }
-                int buf = 0;
-                for (int c = wave; c < each; c += 4, buf ^= W::STAGES - 1) {
-                    const int now = g * each + c, i_tile = (q_from + now % per) * W::TILE;
+            // with a bias head by head, since it is a head's: end is where this head's tiles end
+            int from = c0;
+            do {
+                const int end = BIAS && per > 0 ? min(c1, (from / per + 1) * per) : c1;
+                if constexpr (BIAS)
+                    if (from < c1 && from / per != table_of) {
+                        tile::wait_lds();
+                        tile::meet();
+                        bias_of(from / per);
+                    }
+                for (int c = from + wave; c < end; c += 4, buf ^= W::STAGES - 1) {
+                    const int i_tile = (q_from + c % per) * W::KV_TILE;
                     tile::wait_lds();
                     if (W::STAGES == 1) {
-                        load(now, 0);
+                        load(c, 0);
                         tile::wait_loads<0>();
                     } else {
-                        if (g > 0 && c == wave) load(now, 0);
-                        if (c + 4 < each) {
-                            load(now + 4, buf ^ 1);
-                            if (DIRECT) tile::wait_loads<W::LOADS + W::FACTS>();
+                        if (c == from + wave && from > c0) load(c, buf);
+                        if (c + 4 < end) {
+                            load(c + 4, buf ^ 1);
+                            if (DIRECT) tile::wait_loads<W::KV_LOADS + W::FACTS>();
                             else tile::wait_loads<0>();
                         } else {
                             tile::wait_loads<0>();
@@ -527,23 +555,18 @@ template <typename T, int DP, bool SHARED, bool BIAS, bool DIRECT> __global__ __
                     tile::wait_lds();
                     choose(i_tile, buf);
                 }
-            }
+                from = end;
+            } while (from < c1);
         } else {
-            int buf = 0;
-            for (int c = 0; c < count; ++c, buf ^= 1) {
-                const int g_now = c / per, i_tile = (q_from + c - g_now * per) * W::TILE;
+            for (int c = c0; c < c1; ++c, buf ^= 1) {
+                const int g_now = c / per, i_tile = (q_from + c - g_now * per) * W::KV_TILE;
                 tile::wait_loads<0>();
                 clear(i_tile, buf);
                 tile::wait_lds();
                 tile::meet();
                 if constexpr (BIAS)
-                    if (g_now != table_of) {
-                        fill_bias(a, kv_head * a.group + g_now, 1, table);
-                        table_of = g_now;
-                        tile::wait_lds();
-                        tile::meet();
-                    }
-                if (c + 1 < count) load(c + 1, buf ^ 1);
+                    if (g_now != table_of) bias_of(g_now);
+                if (c + 1 < c1) load(c + 1, buf ^ 1);
                 choose(i_tile, buf);
             }
         }
@@ -553,12 +576,11 @@ template <typename T, int DP, bool SHARED, bool BIAS, bool DIRECT> __global__ __
             const char *const mine = rows_of(a.k, b, k_ragged, seq.k0 + h_key, kv_head), *const my_value = rows_of(a.v, b, k_ragged, seq.k0 + h_key, kv_head);
             auto visit = [&](bool of_v, auto add) {
 #pragma unroll 1
-                for (int round = 0; round < rounds; ++round)
-#pragma unroll 1
-                    for (int c = SHARED ? wave : 0; c < each; c += step) {
-                        const int now = round * each + c, h = kv_head * a.group + now / per, i0 = (q_from + now % per) * W::TILE, n = min(W::TILE, seq.q_len - i0);
+                    for (int c = c0; c < c1; ++c) {
+                        if (SHARED && (c - (BIAS ? max(c0, c / per * per) : c0)) % 4 != wave) continue;
+                        const int h = kv_head * a.group + c / per, i0 = (q_from + c % per) * W::KV_TILE, n = min(W::KV_TILE, seq.q_len - i0);
                         const char *const pq = rows_of(a.q, b, q_ragged, seq.q0 + i0, h), *const pg = rows_of(a.dout, b, q_ragged, seq.q0 + i0, h);
-                        if (shift + i0 >= mine0 + 31 || shift + i0 + W::TILE - 1 < mine0) continue;
+                        if (shift + i0 >= mine0 + 31 || shift + i0 + W::KV_TILE - 1 < mine0) continue;
                         if (!any_not_finite<T>(pg, a.dout.row, n, a.D) && !any_not_finite<T>(pq, a.q.row, n, a.D)) continue;
 #pragma unroll 1
                         for (int i = 0; i < n; ++i) {
@@ -576,22 +598,70 @@ template <typename T, int DP, bool SHARED, bool BIAS, bool DIRECT> __global__ __
             add_rows<T, DP>(SHARED ? stages : lds + wave * 4096, a.D, dv[0], [&](auto add) { visit(true, add); });
             add_rows<T, DP>(SHARED ? stages : lds + wave * 4096, a.D, dk[0], [&](auto add) { visit(false, add); });
         }
-        const bool stored = key < rows;
-        T *const to_k = reinterpret_cast<T *>(rows_of(a.dk, b, k_ragged, seq.k0 + key, kv_head)),
-                *const to_v = reinterpret_cast<T *>(rows_of(a.dv, b, k_ragged, seq.k0 + key, kv_head));
-        if constexpr (SHARED) {
-            const int first = 8 * wave * R::BLOCKS + 4 * half;
-            add_waves<R::BLOCKS>(lds, dk[0]);
-            if (stored) store_row<T, R::BLOCKS, R::BLOCKS, DIRECT>(to_k, first, a.D, a.scale, there, dk[0]);
-            add_waves<R::BLOCKS>(lds, dv[0]);
-            if (stored) store_row<T, R::BLOCKS, R::BLOCKS, DIRECT>(to_v, first, a.D, 1.f, there, dv[0]);
-        } else if (stored) {
-            store_row<T, R::BLOCKS, 4 * R::BLOCKS, DIRECT>(to_k, 4 * half, a.D, a.scale, there, dk[0]);
-            store_row<T, R::BLOCKS, 4 * R::BLOCKS, DIRECT>(to_v, 4 * half, a.D, 1.f, there, dv[0]);
-        }
+        // What leaves: rows of dk and dv, or with splits their parts in fp32.
+        const bool stored = a.splits > 1 ? there : key < rows;
+        const long long place = ((split * a.k_all + seq.k_first + key) * a.kv_heads + kv_head) * a.D;
+        constexpr int GROUPS = SHARED ? R::BLOCKS : 4 * R::BLOCKS;
+        const int first = (SHARED ? 8 * wave * R::BLOCKS : 0) + 4 * half;
+        auto store = [&](const Heads &to, float *parts, float scale, f32x16 (&acc)[R::BLOCKS]) {
+            if constexpr (SHARED) add_waves<R::BLOCKS>(lds, acc);
+            if (!stored) return;
+            if (a.splits > 1) store_row<float, R::BLOCKS, GROUPS, DIRECT>(parts + place, first, a.D, 1.f, true, acc);
+            else store_row<T, R::BLOCKS, GROUPS, DIRECT>(reinterpret_cast<T *>(rows_of(to, b, k_ragged, seq.k0 + key, kv_head)), first, a.D, scale, there, acc);
+        };
+        store(a.dk, a.part_k, a.scale, dk[0]);
+        store(a.dv, a.part_v, 1.f, dv[0]);
         tile::wait_loads<0>();
         tile::wait_lds();
         tile::meet();
+    }
+}
+
+// Adds up the splits' parts of dk and dv, four elements to a thread.
+template <typename T> __global__ __launch_bounds__(THREADS) void k_attention_dkv_join(Args a)
+{
+    const int fours = (a.D + 3) / 4;
+    const long long all = a.k_all * a.kv_heads * fours, each = a.k_all * a.kv_heads * a.D;
+    for (long long at = (long long)blockIdx.x * THREADS + threadIdx.x; at < all; at += (long long)gridDim.x * THREADS) {
+        const int d = (int)(at % fours) * 4, head = (int)(at / fours % a.kv_heads);
+        const long long row = at / fours / a.kv_heads;
+        int b = 0;
+        long long in = row;
+        bool there;
+        if (a.k_offsets) {
+            const int from = min(max(a.k_offsets[0], 0), a.k_rows), to = min(max(a.k_offsets[a.batch], from), a.k_rows);
+            there = row >= from && row < to;
+            if (!there) continue;               // (cleared, where they are to be, by the call's first kernel)
+        } else {
+            b = (int)(row / a.k_rows);
+            in = row - (long long)b * a.k_rows;
+            there = !a.k_lengths || in < min(max(a.k_lengths[b], 0), a.k_rows);
+            if (!there && !a.clear) continue;
+        }
+        float k[4] = {0.f, 0.f, 0.f, 0.f}, v[4] = {0.f, 0.f, 0.f, 0.f};
+        const long long first = (row * a.kv_heads + head) * a.D + d;
+        const int count = min(4, a.D - d);
+        if (there)
+            for (int s = 0; s < a.splits; ++s) {
+                const float *const pk = a.part_k + s * each + first, *const pv = a.part_v + s * each + first;
+                if (count == 4) {
+                    const f32x4 x = *reinterpret_cast<const f32x4_any *>(pk), y = *reinterpret_cast<const f32x4_any *>(pv);
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) {
+                        k[e] += x[e];
+                        v[e] += y[e];
+                    }
+                } else {
+#pragma unroll
+                    for (int e = 0; e < 3; ++e)
+                        if (e < count) {
+                            k[e] += pk[e];
+                            v[e] += pv[e];
+                        }
+                }
+            }
+        store4<T, false>(reinterpret_cast<T *>(rows_of(a.dk, b, a.k_offsets != nullptr, in, head)) + d, count, k[0] * a.scale, k[1] * a.scale, k[2] * a.scale, k[3] * a.scale);
+        store4<T, false>(reinterpret_cast<T *>(rows_of(a.dv, b, a.k_offsets != nullptr, in, head)) + d, count, v[0], v[1], v[2], v[3]);
     }
 }
 

@@ -23,7 +23,7 @@ template <typename W> int dq_lds(bool bias, int reach, bool causal)
 {
     return W::TILES_BYTES + (bias ? (bias_width(reach, causal) + 4 * bias_entries(reach, causal)) * 4 + 4 * W::TURN_BYTES : 0);
 }
-template <typename W> int dkv_lds(bool bias, int reach, bool causal) { return W::TILES_BYTES + W::FACTS_BYTES + (bias ? bias_width(reach, causal) * 4 : 0); }
+template <typename W> int dkv_lds(bool bias, int reach, bool causal) { return W::KV_TILES_BYTES + W::V_BYTES + W::FACTS_BYTES + (bias ? bias_width(reach, causal) * 4 : 0); }
 
 // The gradient of q: whether the waves share their rows (where there is room for it), and the workgroups for each sequence and head.
 struct Way {
@@ -44,13 +44,35 @@ Way dq_way(const rcd_attention_shape &s)
     return w;
 }
 
+// The gradients of k and v: and into how many parts the queries are cut.
+struct KvWay {
+    bool shared;
+    int64_t tiles, parts;
+};
+KvWay dkv_way(const rcd_attention_shape &s)
+{
+    const int64_t longest = attn_rules::longest_of(s.longest_k, s.k_rows, s.batch, s.k_offsets_dev != nullptr);
+    const int64_t longest_q = attn_rules::longest_of(s.longest_q, s.q_rows, s.batch, s.q_offsets_dev != nullptr);
+    KvWay w;
+    w.shared = attn_rules::shared_rows(s.batch * s.kv_heads, longest);
+    w.tiles = attn_rules::tiles_of((s.batch + 1) * s.kv_heads, longest, w.shared);
+    const bool uneven = s.causal || s.q_offsets_dev || s.k_offsets_dev || s.k_lengths_dev;
+    w.parts = attn_rules::parts_of(w.tiles * s.kv_heads * s.batch, uneven, longest_q, s.heads / s.kv_heads);
+    return w;
+}
+
 size_t backward_bytes(const rcd_attention_shape &s, void *base, Args *a)
 {
     Pieces room(base);
     const size_t plane = up256((size_t)all_rows(s.q_offsets_dev, s.q_rows, s.batch) * s.heads * 4) / 4;
     float *const stats = room.take(4 * plane);
     float *const parts = s.bias_dev ? room.take((size_t)s.heads * s.batch * dq_way(s).tiles * s.buckets) : nullptr;
+    const int64_t splits = dkv_way(s).parts;
+    const size_t sums = splits > 1 ? (size_t)splits * all_rows(s.k_offsets_dev, s.k_rows, s.batch) * s.kv_heads * s.d : 0;
+    float *const part_k = splits > 1 ? room.take(sums) : nullptr, *const part_v = splits > 1 ? room.take(sums) : nullptr;
     if (a) {
+        a->part_k = part_k;
+        a->part_v = part_v;
         a->stats = stats;
         a->plane = (long long)plane;
         a->part_bias = parts;
@@ -120,18 +142,25 @@ int rcd_attention_backward(const rcd_attention_shape *s, const rcd_heads *dout, 
         ENC_HIP_TRY(hipGetLastError());
     }
     if (s->k_rows > 0 && s->batch > 0) {
-        const int64_t longest = attn_rules::longest_of(s->longest_k, s->k_rows, s->batch, s->k_offsets_dev != nullptr);
-        const bool shared = attn_rules::shared_rows(s->batch * s->kv_heads, longest);
-        a.tiles = (int)attn_rules::tiles_of((s->batch + 1) * s->kv_heads, longest, shared);
-        const int64_t groups = a.tiles * s->kv_heads * (s->batch + (a.clear && a.k_offsets ? 1 : 0));
+        const KvWay kv = dkv_way(*s);
+        a.tiles = (int)kv.tiles;
+        a.splits = (int)kv.parts;
+        const int64_t groups = a.tiles * s->kv_heads * (s->batch + (a.clear && a.k_offsets ? 1 : 0)) * kv.parts;
         const bool direct = aligned(a.q, s->d, s->dt) && aligned(a.dout, s->d, s->dt);
         ENC_TRY(with_variant(s->dt, s->d, s->bias_dev != nullptr, direct, [&](auto t, auto dp, auto bias, auto how) {
             using T = decltype(t);
             constexpr int DP = decltype(dp)::value;
             constexpr bool BIAS = decltype(bias)::value, DIRECT = decltype(how)::value;
-            if (shared) return launch(&k_attention_dkv<T, DP, true, BIAS, DIRECT>, groups, dkv_lds<Backward<T, DP, true, BIAS>>(BIAS, reach, causal), a, stream);
+            if (kv.shared) return launch(&k_attention_dkv<T, DP, true, BIAS, DIRECT>, groups, dkv_lds<Backward<T, DP, true, BIAS>>(BIAS, reach, causal), a, stream);
             return launch(&k_attention_dkv<T, DP, false, BIAS, DIRECT>, groups, dkv_lds<Backward<T, DP, false, BIAS>>(BIAS, reach, causal), a, stream);
         }));
+        if (kv.parts > 1) {
+            const int64_t fours = a.k_all * s->kv_heads * attn_rules::ceil_div(s->d, 4);
+            const dim3 grid((unsigned)std::min<int64_t>(attn_rules::ceil_div(fours, THREADS), 8192));
+            if (s->dt == RCD_F32) hipLaunchKernelGGL((k_attention_dkv_join<float>), grid, dim3(THREADS), 0, stream, a);
+            else hipLaunchKernelGGL((k_attention_dkv_join<__bf16>), grid, dim3(THREADS), 0, stream, a);
+            ENC_HIP_TRY(hipGetLastError());
+        }
     }
     return RCD_OK;
 }

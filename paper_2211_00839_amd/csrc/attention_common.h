@@ -35,7 +35,7 @@ struct Args {
     float *saved;                       // per row of q and head: the scores' maximum in powers of two, log2 of the sum over it
     float *stats;                       // gradients, four planes [head][row of q]: both added, delta, each of the two
     long long plane;                    // floats of such a plane
-    long long q_all;                    // rows of q in all sequences
+    long long q_all, k_all;             // rows of q and of k in all sequences
     const int *q_offsets, *k_offsets, *k_lengths;
     int batch, heads, kv_heads, group;  // group: query heads that share a head of k and v
     int q_rows, k_rows;                 // of a sequence; with offsets: of all of them
@@ -45,6 +45,7 @@ struct Args {
     Bias bias;
     int tiles, splits, least;           // least: tiles of a split
     float *part_o, *part_ml;            // with splits: their sums, and per row maximum and sum
+    float *part_k, *part_v;             // gradients of k and v with splits: their sums
     float *part_bias;                   // the table's gradient, a part of each workgroup
 };
 
@@ -53,7 +54,7 @@ struct Args {
 struct Sequence {
     long long q0, k0;
     int q_len, k_len;
-    long long q_first;                  // counted over all sequences
+    long long q_first, k_first;         // counted over all sequences
 };
 __device__ __forceinline__ int uniform(int x) { return __builtin_amdgcn_readfirstlane(x); }
 __device__ __forceinline__ Sequence sequence(const Args &a, int b)
@@ -63,6 +64,7 @@ __device__ __forceinline__ Sequence sequence(const Args &a, int b)
     s.q_len = a.q_rows;
     s.k_len = a.k_rows;
     s.q_first = (long long)b * a.q_rows;
+    s.k_first = (long long)b * a.k_rows;
     if (a.q_offsets) {
         const int from = uniform(min(max(a.q_offsets[b], 0), a.q_rows)), to = uniform(min(max(a.q_offsets[b + 1], from), a.q_rows));
         s.q0 = s.q_first = from;
@@ -70,7 +72,7 @@ __device__ __forceinline__ Sequence sequence(const Args &a, int b)
     }
     if (a.k_offsets) {
         const int from = uniform(min(max(a.k_offsets[b], 0), a.k_rows)), to = uniform(min(max(a.k_offsets[b + 1], from), a.k_rows));
-        s.k0 = from;
+        s.k0 = s.k_first = from;
         s.k_len = to - from;
     } else if (a.k_lengths) {
         s.k_len = uniform(min(max(a.k_lengths[b], 0), a.k_rows));
@@ -87,6 +89,13 @@ __device__ __forceinline__ int place_of(int id, int total)
 {
     const int each = (total + 7) / 8;
     return (id & 7) * each + (id >> 3);
+}
+
+// A value of which the compiler knows nothing: what is made of it is made where it is used, not kept in registers through the loops before.
+__device__ __forceinline__ int opaque(int x)
+{
+    asm volatile("" : "+v"(x));
+    return x;
 }
 
 // ---- rows of up to DP elements ----------------------------------------------------------------------------------------------
@@ -126,13 +135,6 @@ template <typename T, bool WHOLE> __device__ __forceinline__ uint4 chunk_of(cons
             else w[e / 2] |= (unsigned)__builtin_bit_cast(unsigned short, p[e]) << (16 * (e & 1));
         }
     return make_uint4(w[0], w[1], w[2], w[3]);
-}
-
-// A value of which the compiler knows nothing: what is made of it is made where it is used, not kept in registers through the loops before.
-__device__ __forceinline__ int opaque(int x)
-{
-    asm volatile("" : "+v"(x));
-    return x;
 }
 
 // `count` consecutive elements (at most four; WHOLE: four) of a row of results.
@@ -247,30 +249,23 @@ template <typename T, int DP, int ROWS, int LOADERS, bool DIRECT> struct Loader 
     }
 };
 
-// Where this lane reads: its row's chunks, and the transposed ones.
+// Where this lane reads: its row's chunks, and the transposed ones.  One address of each, from which the others differ in single bits; they are
+// made anew for each block, for there are better uses for sixteen registers.
 template <typename T, int DP> struct Reader {
     using R = Row<T, DP>;
-    int row, swap;                      // byte of row lane & 31; its turn with this lane's half, times 16
-    int up[R::BLOCKS], down[R::BLOCKS]; // bf16: 4 x 16 blocks of rows 4 half .. and 8 + 4 half ..
+    int here;                           // chunk `half` of row lane & 31
+    int across;                         // bf16: the 4 x 16 block of rows 4 half .. and elements 0 ..
     __device__ __forceinline__ void init()
     {
         const int lane = threadIdx.x & 63, half = lane >> 5, r = lane & 31, i16 = lane & 15;
-        row = r * R::BYTES;
-        swap = (half ^ R::turn(r)) << 4;
-        if constexpr (sizeof(T) == 2) {
-            const int line = 4 * half + (i16 >> 2);
-#pragma unroll
-            for (int b = 0; b < R::BLOCKS; ++b) {
-                const int chunk = 4 * b + 2 * ((lane >> 4) & 1) + ((i16 & 3) >> 1);
-                up[b] = line * R::BYTES + ((chunk ^ R::turn(line)) << 4) + (i16 & 1) * 8;
-                down[b] = (line + 8) * R::BYTES + ((chunk ^ R::turn(line + 8)) << 4) + (i16 & 1) * 8;
-            }
-        }
+        here = r * R::BYTES + ((half ^ R::turn(r)) << 4);
+        const int line = 4 * half + (i16 >> 2), chunk = 2 * ((lane >> 4) & 1) + ((i16 & 3) >> 1);
+        across = line * R::BYTES + ((chunk ^ R::turn(line)) << 4) + (i16 & 1) * 8;
     }
-    // Fragment s of row 32 block + (lane & 31).
-    __device__ __forceinline__ uint4 along(const unsigned char *tile, int block, int s) const
+    // Fragment s of row 32 block + (lane & 31), from `here`.
+    static __device__ __forceinline__ uint4 along(const unsigned char *tile, int here, int block, int s)
     {
-        return *reinterpret_cast<const uint4 *>(tile + block * 32 * R::BYTES + row + ((s << 5) ^ swap));
+        return *reinterpret_cast<const uint4 *>(tile + block * 32 * R::BYTES + (here ^ (s << 5)));
     }
 };
 
@@ -290,6 +285,19 @@ template <typename T> __device__ __forceinline__ f32x16 scores(const uint4 &rows
     }
 }
 
+// 32 rows of a tile against 32 rows in registers, their whole length.
+template <typename T, int DP>
+__device__ __forceinline__ f32x16 scores(const Reader<T, DP> &at, const unsigned char *tile, int block, const uint4 (&mine)[Row<T, DP>::STEPS])
+{
+    f32x16 acc;
+#pragma unroll
+    for (int i = 0; i < 16; ++i) acc[i] = 0.f;
+    const int here = opaque(at.here);
+#pragma unroll
+    for (int s = 0; s < Row<T, DP>::STEPS; ++s) acc = scores<T>(at.along(tile, here, block, s), mine[s], acc);
+    return acc;
+}
+
 // acc[.][block] += (32 rows of a tile)^T p: block's 32 elements of the rows, weighted.  p as scores() leaves it; bf16: rounded to bf16 on
 // its way into the product, to half a step of 2^-8 each, as the rows themselves were.
 template <typename T, int DP, int N>
@@ -299,6 +307,7 @@ __device__ __forceinline__ void weigh(const Reader<T, DP> &at, const unsigned ch
     if constexpr (sizeof(T) == 2) {
         typedef __attribute__((address_space(3))) tile::s16x4 *lds_ptr;
         unsigned char *from = const_cast<unsigned char *>(tile) + block * 32 * R::BYTES;
+        const int across = opaque(at.across);
 #pragma unroll
         for (int s = 0; s < 2; ++s) {
             bf16x8 w[N];
@@ -308,8 +317,8 @@ __device__ __forceinline__ void weigh(const Reader<T, DP> &at, const unsigned ch
                 for (int e = 0; e < 8; ++e) w[n][e] = (__bf16)p[n][8 * s + e];
 #pragma unroll
             for (int b = 0; b < R::BLOCKS; ++b) {
-                const tile::s16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_ptr)(from + at.up[b] + s * 16 * R::BYTES));
-                const tile::s16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_ptr)(from + at.down[b] + s * 16 * R::BYTES));
+                const tile::s16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_ptr)(from + (across ^ (b << 6)) + s * 16 * R::BYTES));
+                const tile::s16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_ptr)(from + (across ^ (b << 6) ^ 32) + (s * 16 + 8) * R::BYTES));
                 const bf16x8 v = __builtin_bit_cast(bf16x8, __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7));
 #pragma unroll
                 for (int n = 0; n < N; ++n) acc[n][b] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(v, w[n], acc[n][b], 0, 0, 0);

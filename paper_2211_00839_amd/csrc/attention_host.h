@@ -105,6 +105,7 @@ Args args_of(const rcd_attention_shape &s)
     a.q_rows = (int)s.q_rows;
     a.k_rows = (int)s.k_rows;
     a.q_all = all_rows(s.q_offsets_dev, s.q_rows, s.batch);
+    a.k_all = all_rows(s.k_offsets_dev, s.k_rows, s.batch);
     a.D = (int)s.d;
     a.pack = a.splits = 1;
     a.causal = s.causal != 0;

@@ -18,7 +18,7 @@ template <typename T, int DP, bool SHARED> struct Forward {
 };
 
 template <typename T, int DP, bool SHARED, bool BIAS, bool DIRECT>
-__global__ __launch_bounds__(THREADS, sizeof(T) == 2 && !SHARED ? 2 : 1) void k_attention(Args a)
+__global__ __launch_bounds__(THREADS, sizeof(T) == 2 && !SHARED ? (DP == 64 ? 3 : 2) : 1) void k_attention(Args a)
 {
     using F = Forward<T, DP, SHARED>;
     using R = Row<T, DP>;
@@ -115,12 +115,8 @@ __global__ __launch_bounds__(THREADS, sizeof(T) == 2 && !SHARED ? 2 : 1) void k_
             const unsigned char *const vtile = ktile + F::HALF;
             f32x16 p[BLOCKS][1];
 #pragma unroll
-            for (int kb = 0; kb < BLOCKS; ++kb) {
-#pragma unroll
-                for (int i = 0; i < 16; ++i) p[kb][0][i] = 0.f;
-#pragma unroll
-                for (int s = 0; s < R::STEPS; ++s) p[kb][0] = scores<T>(reader.along(ktile, kb, s), q[s], p[kb][0]);
-            }
+            for (int kb = 0; kb < BLOCKS; ++kb)
+                p[kb][0] = scores<T, DP>(reader, ktile, kb, q);
             float by = a.scale2, plus = 0.f;        // what is still to be done to the scores
             if (BIAS && near) {
                 const float *const bias = my_table + (k0 - pos) + 4 * half + a.bias.reach + MARGIN;

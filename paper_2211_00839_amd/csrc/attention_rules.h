@@ -28,6 +28,15 @@ inline int64_t tiles_of(int64_t across, int64_t longest, bool shared)
     return std::max<int64_t>(1, std::min(tiles, MOST_WORKGROUPS / std::max<int64_t>(across, 1)));
 }
 
+// Parts of the queries that a workgroup of the gradients of k and v goes along, added up behind: two workgroups fit a compute unit, and where some are
+// longer than others twice that many are wanted, so that the short ones fill the gaps.  At most 8, of 256 rows at least.
+inline int64_t parts_of(int64_t groups, bool uneven, int64_t longest_q, int64_t group)
+{
+    const int64_t wanted = uneven ? 1024 : 512;
+    if (groups <= 0 || groups >= wanted) return 1;
+    return std::max<int64_t>(1, std::min<int64_t>({ceil_div(wanted, groups), longest_q * group / 256, 8}));
+}
+
 struct Cut {
     bool shared;
     int pack;           // heads that share their keys, side by side in a tile of rows
