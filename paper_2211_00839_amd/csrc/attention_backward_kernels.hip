@@ -72,19 +72,17 @@ __device__ __forceinline__ void store_row(T *to, int first, int D_, float scale,
 }
 
 template <typename T, int DP, bool SHARED, bool BIAS, bool DIRECT>
-__global__ __launch_bounds__(THREADS, sizeof(T) == 2 && !SHARED ? (DP == 64 ? 3 : 2) : 1) void k_attention_dq(Args a)
+__global__ __launch_bounds__(THREADS, sizeof(T) == 2 && !SHARED ? (DP == 64 && !BIAS ? 3 : 2) : 1) void k_attention_dq(Args a)
 {
     using W = Backward<T, DP, SHARED, BIAS>;
     using R = Row<T, DP>;
     constexpr int BLOCKS = W::TILE / 32;
     extern __shared__ __align__(1024) unsigned char lds[];
     const int tid = threadIdx.x, lane = tid & 63, half = lane >> 5, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
-    const int total = a.tiles * a.heads * (a.batch + (a.clear && a.q_offsets ? 1 : 0));
-    int at = place_of(blockIdx.x, total);
-    if (at >= total) return;
-    const int first_tile = a.tiles - 1 - at % a.tiles;
-    at /= a.tiles;
-    const int head = at % a.heads, b = at / a.heads;
+    Unit unit;
+    if (!unit_of(blockIdx.x, a.batch + (a.clear && a.q_offsets ? 1 : 0), a.kv_heads, a.tiles * a.group, &unit)) return;
+    const int b = unit.sequence, kv_head = unit.kv_head, head = kv_head * a.group + unit.in / a.tiles;
+    const int first_tile = a.tiles - 1 - unit.in % a.tiles;     // (causal: the longest first)
     if (b == a.batch) {
         clear_rows<T>(a.dq, a.q_offsets, a.batch, a.q_rows, head, a.D, first_tile, a.tiles);
         return;
@@ -97,7 +95,7 @@ __global__ __launch_bounds__(THREADS, sizeof(T) == 2 && !SHARED ? (DP == 64 ? 3 
             for (int c = tid; c < all; c += THREADS) part[c] = 0.f;
         return;
     }
-    const int kv_head = head / a.group, shift = seq.k_len - seq.q_len;
+    const int shift = seq.k_len - seq.q_len;
     const bool q_ragged = a.q_offsets != nullptr, k_ragged = a.k_offsets != nullptr;
     const char *const keys = rows_of(a.k, b, k_ragged, seq.k0, kv_head), *const values = rows_of(a.v, b, k_ragged, seq.k0, kv_head);
     const int reach = a.bias.reach, width = BIAS ? bias_width(reach, a.causal) : 0, entries = BIAS ? bias_entries(reach, a.causal) : 0;
@@ -356,14 +354,10 @@ template <typename T, int DP, bool SHARED, bool BIAS, bool DIRECT> __global__ __
     constexpr int BLOCKS = W::KV_TILE / 32;
     extern __shared__ __align__(1024) unsigned char lds[];
     const int tid = threadIdx.x, lane = tid & 63, half = lane >> 5, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
-    const int total = a.tiles * a.kv_heads * (a.batch + (a.clear && a.k_offsets ? 1 : 0)) * a.splits;
-    int at = place_of(blockIdx.x, total);
-    if (at >= total) return;
-    const int split = at % a.splits;
-    at /= a.splits;
-    const int first_tile = at % a.tiles;                        // (causal: the first keys have the most queries)
-    at /= a.tiles;
-    const int kv_head = at % a.kv_heads, b = at / a.kv_heads;
+    Unit unit;
+    if (!unit_of(blockIdx.x, a.batch + (a.clear && a.k_offsets ? 1 : 0), a.kv_heads, a.tiles * a.splits, &unit)) return;
+    const int b = unit.sequence, kv_head = unit.kv_head, split = unit.in % a.splits;
+    const int first_tile = unit.in / a.splits;                  // (causal: the first keys have the most queries)
     if (b == a.batch) {
         if (split > 0) return;
         clear_rows<T>(a.dk, a.k_offsets, a.batch, a.k_rows, kv_head, a.D, first_tile, a.tiles);

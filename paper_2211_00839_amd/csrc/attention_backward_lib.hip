@@ -40,7 +40,7 @@ Way dq_way(const rcd_attention_shape &s)
                        using W = Backward<decltype(t), decltype(dp)::value, true, decltype(bias)::value>;
                        return dq_lds<W>(s.bias_dev != nullptr, reach_of(s), s.causal != 0);
                    }) <= MOST_LDS;
-    w.tiles = attn_rules::tiles_of((s.batch + 1) * s.heads, longest, w.shared);
+    w.tiles = attn_rules::tiles_of(attn_rules::units_of(s.batch, s.kv_heads) * (s.heads / s.kv_heads), longest, w.shared);
     return w;
 }
 
@@ -55,7 +55,7 @@ KvWay dkv_way(const rcd_attention_shape &s)
     const int64_t longest_q = attn_rules::longest_of(s.longest_q, s.q_rows, s.batch, s.q_offsets_dev != nullptr);
     KvWay w;
     w.shared = attn_rules::shared_rows(s.batch * s.kv_heads, longest);
-    w.tiles = attn_rules::tiles_of((s.batch + 1) * s.kv_heads, longest, w.shared);
+    w.tiles = attn_rules::tiles_of(attn_rules::units_of(s.batch, s.kv_heads), longest, w.shared);
     const bool uneven = s.causal || s.q_offsets_dev || s.k_offsets_dev || s.k_lengths_dev;
     w.parts = attn_rules::parts_of(w.tiles * s.kv_heads * s.batch, uneven, longest_q, s.heads / s.kv_heads);
     return w;
@@ -122,14 +122,14 @@ int rcd_attention_backward(const rcd_attention_shape *s, const rcd_heads *dout, 
         Args x = a;
         x.tiles = (int)way.tiles;
         if (!dbias_dev) x.part_bias = nullptr;
-        const int64_t groups = x.tiles * s->heads * (s->batch + (a.clear && a.q_offsets ? 1 : 0));
+        const int64_t sequences = s->batch + (a.clear && a.q_offsets ? 1 : 0), each = way.tiles * a.group;
         const bool direct = aligned(a.k, s->d, s->dt) && aligned(a.v, s->d, s->dt);
         ENC_TRY(with_variant(s->dt, s->d, s->bias_dev != nullptr, direct, [&](auto t, auto dp, auto bias, auto how) {
             using T = decltype(t);
             constexpr int DP = decltype(dp)::value;
             constexpr bool BIAS = decltype(bias)::value, DIRECT = decltype(how)::value;
-            if (way.shared) return launch(&k_attention_dq<T, DP, true, BIAS, DIRECT>, groups, dq_lds<Backward<T, DP, true, BIAS>>(BIAS, reach, causal), x, stream);
-            return launch(&k_attention_dq<T, DP, false, BIAS, DIRECT>, groups, dq_lds<Backward<T, DP, false, BIAS>>(BIAS, reach, causal), x, stream);
+            if (way.shared) return launch(&k_attention_dq<T, DP, true, BIAS, DIRECT>, sequences, each, dq_lds<Backward<T, DP, true, BIAS>>(BIAS, reach, causal), x, stream);
+            return launch(&k_attention_dq<T, DP, false, BIAS, DIRECT>, sequences, each, dq_lds<Backward<T, DP, false, BIAS>>(BIAS, reach, causal), x, stream);
         }));
     }
     if (dbias_dev) {
@@ -145,14 +145,14 @@ int rcd_attention_backward(const rcd_attention_shape *s, const rcd_heads *dout, 
         const KvWay kv = dkv_way(*s);
         a.tiles = (int)kv.tiles;
         a.splits = (int)kv.parts;
-        const int64_t groups = a.tiles * s->kv_heads * (s->batch + (a.clear && a.k_offsets ? 1 : 0)) * kv.parts;
+        const int64_t sequences = s->batch + (a.clear && a.k_offsets ? 1 : 0), each = kv.tiles * kv.parts;
         const bool direct = aligned(a.q, s->d, s->dt) && aligned(a.dout, s->d, s->dt);
         ENC_TRY(with_variant(s->dt, s->d, s->bias_dev != nullptr, direct, [&](auto t, auto dp, auto bias, auto how) {
             using T = decltype(t);
             constexpr int DP = decltype(dp)::value;
             constexpr bool BIAS = decltype(bias)::value, DIRECT = decltype(how)::value;
-            if (kv.shared) return launch(&k_attention_dkv<T, DP, true, BIAS, DIRECT>, groups, dkv_lds<Backward<T, DP, true, BIAS>>(BIAS, reach, causal), a, stream);
-            return launch(&k_attention_dkv<T, DP, false, BIAS, DIRECT>, groups, dkv_lds<Backward<T, DP, false, BIAS>>(BIAS, reach, causal), a, stream);
+            if (kv.shared) return launch(&k_attention_dkv<T, DP, true, BIAS, DIRECT>, sequences, each, dkv_lds<Backward<T, DP, true, BIAS>>(BIAS, reach, causal), a, stream);
+            return launch(&k_attention_dkv<T, DP, false, BIAS, DIRECT>, sequences, each, dkv_lds<Backward<T, DP, false, BIAS>>(BIAS, reach, causal), a, stream);
         }));
         if (kv.parts > 1) {
             const int64_t fours = a.k_all * s->kv_heads * attn_rules::ceil_div(s->d, 4);

@@ -84,11 +84,35 @@ __device__ __forceinline__ char *rows_of(const Heads &h, int b, bool offsets, lo
     return h.p + (offsets ? 0 : (long long)b * h.batch) + row0 * h.row + (long long)head * h.head;
 }
 
-// Workgroups go round the eight dies; each die takes a run of consecutive ones, whose keys its L2 then holds.
-__device__ __forceinline__ int place_of(int id, int total)
+// What a workgroup is for.  Workgroups go round the eight dies; all those of a sequence and a head of k and v (a unit) go to one of them, whose L2
+// then holds that head's rows, and the next head's to the next, so that a long sequence is everyone's.  Few units that do not go round evenly are
+// cut instead: each die gets an eighth of all there is, in order.  each: workgroups of a unit.
+struct Unit {
+    int sequence, kv_head, in;          // in: which of the unit's
+};
+inline __host__ __device__ bool goes_round(long long units) { return (units + 7) / 8 * 8 * 5 <= units * 6; }
+__device__ __forceinline__ bool unit_of(int id, int sequences, int kv_heads, int each, Unit *u)
 {
-    const int each = (total + 7) / 8;
-    return (id & 7) * each + (id >> 3);
+    const int units = sequences * kv_heads, turn = id >> 3, die = id & 7;
+    int unit;
+    if (goes_round(units)) {
+        unit = turn / each * 8 + die;
+        if (unit >= units) return false;
+        u->in = turn % each;
+    } else {
+        const int all = units * each, place = die * ((all + 7) / 8) + turn;
+        if (place >= all || turn >= (all + 7) / 8) return false;
+        unit = place / each;
+        u->in = place % each;
+    }
+    u->kv_head = unit % kv_heads;
+    u->sequence = unit / kv_heads;
+    return true;
+}
+inline long long workgroups_of(long long sequences, long long kv_heads, long long each)
+{
+    const long long units = sequences * kv_heads;
+    return goes_round(units) ? (units + 7) / 8 * 8 * each : (units * each + 7) / 8 * 8;
 }
 
 // A value of which the compiler knows nothing: what is made of it is made where it is used, not kept in registers through the loops before.

@@ -54,7 +54,7 @@ int check_shape(const rcd_attention_shape *s)
     const float scale2 = s->scale * 1.44269504f;
     if (!(s->scale > 0.f) || !std::isnormal(s->scale) || !std::isnormal(scale2)) return RCD_ERR_INVALID_ARG;
     if (s->d > MOST_D || s->heads > MOST_HEADS || s->q_rows > MOST_ROWS || s->k_rows > MOST_ROWS || s->batch > MOST_ROWS ||
-        s->batch * s->heads > attn_rules::MOST_WORKGROUPS - s->heads)
+        attn_rules::units_of(s->batch, s->kv_heads) * (s->heads / s->kv_heads) > attn_rules::MOST_WORKGROUPS)
         return RCD_ERR_UNSUPPORTED;
     if (s->bias_dev) {
         if (s->bias_dt != RCD_F32 && s->bias_dt != RCD_BF16) return RCD_ERR_UNSUPPORTED;
@@ -161,10 +161,11 @@ struct SetUp {
     }
 };
 
-template <typename K> int launch(K kernel, int64_t groups, int lds, const Args &a, hipStream_t stream)
+// each: workgroups of a sequence and head of k and v
+template <typename K> int launch(K kernel, int64_t sequences, int64_t each, int lds, const Args &a, hipStream_t stream)
 {
     if (lds > MOST_LDS) return RCD_ERR_UNSUPPORTED;
-    hipLaunchKernelGGL(kernel, dim3((unsigned)(attn_rules::ceil_div(groups, 8) * 8)), dim3(THREADS), lds, stream, a);
+    hipLaunchKernelGGL(kernel, dim3((unsigned)workgroups_of(sequences, a.kv_heads, each)), dim3(THREADS), lds, stream, a);
     ENC_HIP_TRY(hipGetLastError());
     return RCD_OK;
 }

@@ -25,24 +25,21 @@ __global__ __launch_bounds__(THREADS, sizeof(T) == 2 && !SHARED ? (DP == 64 ? 3 
     constexpr int ROWS = SHARED ? 32 : 128, BLOCKS = F::TILE / 32;
     extern __shared__ __align__(1024) unsigned char lds[];
     const int tid = threadIdx.x, lane = tid & 63, half = lane >> 5, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
-    const int groups = a.heads / a.pack, sequences = a.batch + (a.clear ? 1 : 0);
-    const int total = a.tiles * groups * sequences * a.splits;
-    int at = place_of(blockIdx.x, total);
-    if (at >= total) return;
-    const int first_tile = a.tiles - 1 - at % a.tiles;          // (causal: the longest first)
-    at /= a.tiles;
-    const int group = at % groups;
-    at /= groups;
-    const int b = at % sequences, split = at / sequences;       // (the last splits, of which short sequences have none, last)
+    const int packs = a.group / a.pack;                         // of packed heads that share a head of k and v
+    Unit unit;
+    if (!unit_of(blockIdx.x, a.batch + (a.clear ? 1 : 0), a.kv_heads, a.tiles * packs * a.splits, &unit)) return;
+    const int b = unit.sequence, kv_head = unit.kv_head;
+    const int first_tile = a.tiles - 1 - unit.in % a.tiles;     // (causal: the longest first)
+    const int head0 = (kv_head * packs + unit.in / a.tiles % packs) * a.pack, split = unit.in / a.tiles / packs;
     if (b == a.batch) {
         if (split == 0)
-            for (int g = 0; g < a.pack; ++g) clear_rows<T>(a.o, a.q_offsets, a.batch, a.q_rows, group * a.pack + g, a.D, first_tile, a.tiles);
+            for (int g = 0; g < a.pack; ++g) clear_rows<T>(a.o, a.q_offsets, a.batch, a.q_rows, head0 + g, a.D, first_tile, a.tiles);
         return;
     }
     const Sequence seq = sequence(a, b);
     const int columns = seq.q_len * a.pack;
     if (first_tile * ROWS >= columns) return;
-    const int head0 = group * a.pack, kv_head = head0 / a.group, shift = seq.k_len - seq.q_len;
+    const int shift = seq.k_len - seq.q_len;
     const char *const keys = rows_of(a.k, b, a.k_offsets != nullptr, seq.k0, kv_head), *const values = rows_of(a.v, b, a.k_offsets != nullptr, seq.k0, kv_head);
     float *const table = reinterpret_cast<float *>(lds + F::TILES_BYTES);
     const int width = BIAS ? bias_width(a.bias.reach, a.causal) : 0;

@@ -72,15 +72,15 @@ int rcd_attention(const rcd_attention_shape *s, const rcd_heads *q, const rcd_he
     a.tiles = (int)c.tiles;
     a.splits = (int)c.splits;
     a.least = (int)c.least;
-    const int64_t groups = c.tiles * (s->heads / c.pack) * (s->batch + (a.clear ? 1 : 0)) * c.splits;
+    const int64_t sequences = s->batch + (a.clear ? 1 : 0), each = c.tiles * (a.group / c.pack) * c.splits;
     const int bias_bytes = width_of(*s) * c.pack * 4;
     const bool direct = aligned(a.k, s->d, s->dt) && aligned(a.v, s->d, s->dt);
     ENC_TRY(with_variant(s->dt, s->d, s->bias_dev != nullptr, direct, [&](auto t, auto dp, auto bias, auto way) {
         using T = decltype(t);
         constexpr int DP = decltype(dp)::value;
         constexpr bool BIAS = decltype(bias)::value, DIRECT = decltype(way)::value;
-        if (c.shared) return launch(&k_attention<T, DP, true, BIAS, DIRECT>, groups, Forward<T, DP, true>::TILES_BYTES + bias_bytes, a, stream);
-        return launch(&k_attention<T, DP, false, BIAS, DIRECT>, groups, Forward<T, DP, false>::TILES_BYTES + bias_bytes, a, stream);
+        if (c.shared) return launch(&k_attention<T, DP, true, BIAS, DIRECT>, sequences, each, Forward<T, DP, true>::TILES_BYTES + bias_bytes, a, stream);
+        return launch(&k_attention<T, DP, false, BIAS, DIRECT>, sequences, each, Forward<T, DP, false>::TILES_BYTES + bias_bytes, a, stream);
     }));
     if (c.splits > 1) {
         const int64_t slots = a.q_all * s->heads;

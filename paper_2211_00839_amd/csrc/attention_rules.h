@@ -37,6 +37,9 @@ inline int64_t parts_of(int64_t groups, bool uneven, int64_t longest_q, int64_t 
     return std::max<int64_t>(1, std::min<int64_t>({ceil_div(wanted, groups), longest_q * group / 256, 8}));
 }
 
+// Sequences (and one for the rows outside them) times heads of k and v, in whole rounds over the eight dies.
+inline int64_t units_of(int64_t batch, int64_t kv_heads) { return ceil_div((batch + 1) * kv_heads, 8) * 8; }
+
 struct Cut {
     bool shared;
     int pack;           // heads that share their keys, side by side in a tile of rows
@@ -50,7 +53,7 @@ inline Cut cut_of(int64_t batch, int64_t heads, int64_t group, int64_t longest_q
 {
     Cut c{};
     c.pack = group > 1 && longest_q * group <= 64 && q_rows * group <= ((int64_t)1 << 29) && width * group <= 8192 ? (int)group : 1;
-    const int64_t across = batch * (heads / c.pack), most = (batch + 1) * (heads / c.pack);
+    const int64_t across = batch * (heads / c.pack), most = units_of(batch, heads / group) * (group / c.pack);
     c.shared = shared_rows(across, longest_q * c.pack);
     c.tiles = tiles_of(most, longest_q * c.pack, c.shared);
     c.splits = c.least = 1;
