@@ -72,7 +72,7 @@ __device__ __forceinline__ void store_row(T *to, int first, int D_, float scale,
 }
 
 template <typename T, int DP, bool SHARED, bool BIAS, bool DIRECT>
-__global__ __launch_bounds__(THREADS, sizeof(T) == 2 && !SHARED ? (DP == 64 && !BIAS ? 3 : 2) : 1) void k_attention_dq(Args a)
+__global__ __launch_bounds__(THREADS, sizeof(T) == 2 && !SHARED ? 2 : 1) void k_attention_dq(Args a)
 {
     using W = Backward<T, DP, SHARED, BIAS>;
     using R = Row<T, DP>;
@@ -167,6 +167,8 @@ __global__ __launch_bounds__(THREADS, sizeof(T) == 2 && !SHARED ? (DP == 64 && !
             top = v.x;
             log_sum = v.y;
         }
+        arrive(q);
+        arrive(g);
         const float both = top + log_sum;
         if (there && half == 0 && (!SHARED || wave == 0)) {
             float *const to = a.stats + (long long)head * a.q_all + place;
@@ -190,9 +192,10 @@ __global__ __launch_bounds__(THREADS, sizeof(T) == 2 && !SHARED ? (DP == 64 && !
             for (int kb = 0; kb < BLOCKS; ++kb) {
                 __builtin_amdgcn_sched_barrier(0);          // (a block's fragments at a time: there are no registers for more)
                 const int j0 = k0 + 32 * kb;
-                f32x16 s = scores<T, DP>(reader, ktile, kb, q);
-                const f32x16 dp = scores<T, DP>(reader, vtile, kb, g);
-                f32x16 ds[1];
+                f32x16 of[2], ds[1];
+                scores<T, DP>(reader, ktile, vtile, kb, q, g, of);
+                f32x16 &s = of[0];
+                const f32x16 &dp = of[1];
                 if constexpr (BIAS) {
                     if (near) {
                         const float *const bias = table + (j0 - pos) + 4 * half + reach + MARGIN;
@@ -239,7 +242,7 @@ __global__ __launch_bounds__(THREADS, sizeof(T) == 2 && !SHARED ? (DP == 64 && !
                         else mine_near[offset + reach] += sum;
                     }
                 }
-                if (!skip) weigh<T, DP, 1>(reader, ktile, kb, ds, acc);
+                if (!skip) weigh<T, DP, 1>(reader, ktile, kb, ds, acc[0]);
             }
         };
         int buf = 0;
@@ -434,6 +437,8 @@ template <typename T, int DP, bool SHARED, bool BIAS, bool DIRECT> __global__ __
                 else v[s] = y;
             }
         }
+        arrive(k);
+        if constexpr (!W::TIGHT) arrive(v);
         f32x16 dk[1][R::BLOCKS], dv[1][R::BLOCKS];
 #pragma unroll
         for (int d = 0; d < R::BLOCKS; ++d)
@@ -448,7 +453,15 @@ template <typename T, int DP, bool SHARED, bool BIAS, bool DIRECT> __global__ __
 #pragma unroll
             for (int rb = 0; rb < BLOCKS; ++rb) {
                 const int p0 = shift + i_tile + 32 * rb;
-                f32x16 p[1] = {scores<T, DP>(reader, qtile, rb, k)}, ds[1];
+                f32x16 p[1], ds[1];
+                if constexpr (W::TIGHT) {
+                    scores<T, DP, 1>(reader, qtile + 32 * rb * R::BYTES, k, p);
+                } else {
+                    f32x16 of[2];
+                    scores<T, DP>(reader, qtile, gtile, rb, k, v, of);
+                    p[0] = of[0];
+                    ds[0] = of[1];
+                }
                 if constexpr (BIAS) {
                     if (near) {
                         const float *const bias = table + (key - p0) - 4 * half + a.bias.reach + MARGIN;
@@ -478,15 +491,15 @@ template <typename T, int DP, bool SHARED, bool BIAS, bool DIRECT> __global__ __
                 };
                 if constexpr (W::TIGHT) {
                     if (edge) hide(p[0]);
-                    if (!skip) weigh<T, DP, 1>(reader, gtile, rb, p, dv);
+                    if (!skip) weigh<T, DP, 1>(reader, gtile, rb, p, dv[0]);
                     __builtin_amdgcn_sched_barrier(0);
-#pragma unroll
-                    for (int i = 0; i < 16; ++i) ds[0][i] = 0.f;
+                    struct Pair {
+                        uint4 theirs, mine;
+                    };
                     const int here = opaque(reader.here);
-#pragma unroll
-                    for (int f = 0; f < R::STEPS; ++f) ds[0] = scores<T>(reader.along(gtile, here, rb, f), reader.along(my_values, here, 0, f), ds[0]);
-                } else {
-                    ds[0] = scores<T, DP>(reader, gtile, rb, v);
+                    set_zero(ds);
+                    in_turn<R::STEPS, 2>([&](int i) { return Pair{reader.along(gtile, here, rb, i), reader.along(my_values, here, 0, i)}; },
+                                         [&](int i, const Pair &x) { ds[0] = scores<T>(x.theirs, x.mine, ds[0]); });
                 }
 #pragma unroll
                 for (int f = 0; f < 4; ++f) {
@@ -499,8 +512,8 @@ template <typename T, int DP, bool SHARED, bool BIAS, bool DIRECT> __global__ __
                     hide(ds[0]);
                 }
                 if (!skip) {
-                    if (!W::TIGHT) weigh<T, DP, 1>(reader, gtile, rb, p, dv);
-                    weigh<T, DP, 1>(reader, qtile, rb, ds, dk);
+                    if (!W::TIGHT) weigh<T, DP, 1>(reader, gtile, rb, p, dv[0]);
+                    weigh<T, DP, 1>(reader, qtile, rb, ds, dk[0]);
                 }
                 __builtin_amdgcn_sched_barrier(0);          // (a block's fragments at a time: there are no registers for more)
             }

@@ -128,8 +128,8 @@ int rcd_attention_backward(const rcd_attention_shape *s, const rcd_heads *dout, 
             using T = decltype(t);
             constexpr int DP = decltype(dp)::value;
             constexpr bool BIAS = decltype(bias)::value, DIRECT = decltype(how)::value;
-            if (way.shared) return launch(&k_attention_dq<T, DP, true, BIAS, DIRECT>, sequences, each, dq_lds<Backward<T, DP, true, BIAS>>(BIAS, reach, causal), x, stream);
-            return launch(&k_attention_dq<T, DP, false, BIAS, DIRECT>, sequences, each, dq_lds<Backward<T, DP, false, BIAS>>(BIAS, reach, causal), x, stream);
+            if (way.shared) return launch(&k_attention_dq<T, DP, true, BIAS, DIRECT>, sequences, each, THREADS, 0, dq_lds<Backward<T, DP, true, BIAS>>(BIAS, reach, causal), x, stream);
+            return launch(&k_attention_dq<T, DP, false, BIAS, DIRECT>, sequences, each, THREADS, 0, dq_lds<Backward<T, DP, false, BIAS>>(BIAS, reach, causal), x, stream);
         }));
     }
     if (dbias_dev) {
@@ -151,8 +151,8 @@ int rcd_attention_backward(const rcd_attention_shape *s, const rcd_heads *dout, 
             using T = decltype(t);
             constexpr int DP = decltype(dp)::value;
             constexpr bool BIAS = decltype(bias)::value, DIRECT = decltype(how)::value;
-            if (kv.shared) return launch(&k_attention_dkv<T, DP, true, BIAS, DIRECT>, sequences, each, dkv_lds<Backward<T, DP, true, BIAS>>(BIAS, reach, causal), a, stream);
-            return launch(&k_attention_dkv<T, DP, false, BIAS, DIRECT>, sequences, each, dkv_lds<Backward<T, DP, false, BIAS>>(BIAS, reach, causal), a, stream);
+            if (kv.shared) return launch(&k_attention_dkv<T, DP, true, BIAS, DIRECT>, sequences, each, THREADS, 0, dkv_lds<Backward<T, DP, true, BIAS>>(BIAS, reach, causal), a, stream);
+            return launch(&k_attention_dkv<T, DP, false, BIAS, DIRECT>, sequences, each, THREADS, 0, dkv_lds<Backward<T, DP, false, BIAS>>(BIAS, reach, causal), a, stream);
         }));
         if (kv.parts > 1) {
             const int64_t fours = a.k_all * s->kv_heads * attn_rules::ceil_div(s->d, 4);

@@ -44,6 +44,7 @@ struct Args {
     float scale, scale2;                // scale2: times log2 e
     Bias bias;
     int tiles, splits, least;           // least: tiles of a split
+    int workgroups;                     // all there are
     float *part_o, *part_ml;            // with splits: their sums, and per row maximum and sum
     float *part_k, *part_v;             // gradients of k and v with splits: their sums
     float *part_bias;                   // the table's gradient, a part of each workgroup
@@ -91,14 +92,15 @@ struct Unit {
     int sequence, kv_head, in;          // in: which of the unit's
 };
 inline __host__ __device__ bool goes_round(long long units) { return (units + 7) / 8 * 8 * 5 <= units * 6; }
-__device__ __forceinline__ bool unit_of(int id, int sequences, int kv_heads, int each, Unit *u)
+// round: how often this workgroup has had one before; it shifts a unit's workgroups by that, so that nobody has only the first parts of theirs.
+__device__ __forceinline__ bool unit_of(int id, int sequences, int kv_heads, int each, Unit *u, int round = 0)
 {
     const int units = sequences * kv_heads, turn = id >> 3, die = id & 7;
     int unit;
     if (goes_round(units)) {
         unit = turn / each * 8 + die;
         if (unit >= units) return false;
-        u->in = turn % each;
+        u->in = (turn + round) % each;
     } else {
         const int all = units * each, place = die * ((all + 7) / 8) + turn;
         if (place >= all || turn >= (all + 7) / 8) return false;
@@ -159,6 +161,13 @@ template <typename T, bool WHOLE> __device__ __forceinline__ uint4 chunk_of(cons
             else w[e / 2] |= (unsigned)__builtin_bit_cast(unsigned short, p[e]) << (16 * (e & 1));
         }
     return make_uint4(w[0], w[1], w[2], w[3]);
+}
+
+// Waits for loaded values here, not at their first use, which may lie in a loop and would wait for that loop's own loads too, each time round.
+template <int N> __device__ __forceinline__ void arrive(uint4 (&v)[N])
+{
+#pragma unroll
+    for (int i = 0; i < N; ++i) asm volatile("" : "+v"(v[i].x), "+v"(v[i].y), "+v"(v[i].z), "+v"(v[i].w));
 }
 
 // `count` consecutive elements (at most four; WHOLE: four) of a row of results.
@@ -309,58 +318,89 @@ template <typename T> __device__ __forceinline__ f32x16 scores(const uint4 &rows
     }
 }
 
-// 32 rows of a tile against 32 rows in registers, their whole length.
-template <typename T, int DP>
-__device__ __forceinline__ f32x16 scores(const Reader<T, DP> &at, const unsigned char *tile, int block, const uint4 (&mine)[Row<T, DP>::STEPS])
+// Fragments are asked for this many products before they are used (left to itself the compiler asks for one and waits for it, every time: the
+// latency of LDS four times the length of a product).  Rows of 64 leave registers for three waves to a SIMD, which need less of it.
+template <int DP> constexpr int AHEAD = DP == 64 ? 2 : 4;
+
+// `count` products, product(i, fragment) of the fragment that read(i) asks for.
+template <int COUNT, int CLOSE, typename Read, typename Product> __device__ __forceinline__ void in_turn(Read read, Product product)
 {
-    f32x16 acc;
+    decltype(read(0)) f[COUNT];
 #pragma unroll
-    for (int i = 0; i < 16; ++i) acc[i] = 0.f;
-    const int here = opaque(at.here);
+    for (int i = 0; i < (CLOSE < COUNT ? CLOSE : COUNT); ++i) f[i] = read(i);
 #pragma unroll
-    for (int s = 0; s < Row<T, DP>::STEPS; ++s) acc = scores<T>(at.along(tile, here, block, s), mine[s], acc);
-    return acc;
+    for (int i = 0; i < COUNT; ++i) {
+        if (i + CLOSE < COUNT) f[i + CLOSE] = read(i + CLOSE);
+        tile::pin();
+        product(i, f[i]);
+        tile::pin();
+    }
 }
 
-// acc[.][block] += (32 rows of a tile)^T p: block's 32 elements of the rows, weighted.  p as scores() leaves it; bf16: rounded to bf16 on
-// its way into the product, to half a step of 2^-8 each, as the rows themselves were.
+template <int N> __device__ __forceinline__ void set_zero(f32x16 (&x)[N])
+{
+#pragma unroll
+    for (int n = 0; n < N; ++n)
+#pragma unroll
+        for (int i = 0; i < 16; ++i) x[n][i] = 0.f;
+}
+
+// All blocks of 32 rows of a tile against 32 rows in registers, their whole length; the blocks take turns, each a chain of its own.
 template <typename T, int DP, int N>
-__device__ __forceinline__ void weigh(const Reader<T, DP> &at, const unsigned char *tile, int block, const f32x16 (&p)[N], f32x16 (&acc)[N][DP / 32])
+__device__ __forceinline__ void scores(const Reader<T, DP> &at, const unsigned char *tile, const uint4 (&mine)[Row<T, DP>::STEPS], f32x16 (&to)[N])
+{
+    const int here = opaque(at.here);
+    set_zero(to);
+    in_turn<N * Row<T, DP>::STEPS, AHEAD<DP>>([&](int i) { return at.along(tile, here, i % N, i / N); },
+                                   [&](int i, const uint4 &rows) { to[i % N] = scores<T>(rows, mine[i / N], to[i % N]); });
+}
+// A block of each of two tiles against rows of their own.
+template <typename T, int DP>
+__device__ __forceinline__ void scores(const Reader<T, DP> &at, const unsigned char *tile0, const unsigned char *tile1, int block,
+                                       const uint4 (&mine0)[Row<T, DP>::STEPS], const uint4 (&mine1)[Row<T, DP>::STEPS], f32x16 (&to)[2])
+{
+    const int here = opaque(at.here);
+    set_zero(to);
+    in_turn<2 * Row<T, DP>::STEPS, AHEAD<DP>>([&](int i) { return at.along(i & 1 ? tile1 : tile0, here, block, i >> 1); },
+                                   [&](int i, const uint4 &rows) { to[i & 1] = scores<T>(rows, i & 1 ? mine1[i >> 1] : mine0[i >> 1], to[i & 1]); });
+}
+
+// acc[b] += (rows of N blocks of a tile, from `block` on)^T p: block b's 32 elements of the rows, weighted.  p as scores() leaves it; bf16: rounded
+// to bf16 on its way into the product, to half a step of 2^-8 each, as the rows themselves were.
+template <typename T, int DP, int N>
+__device__ __forceinline__ void weigh(const Reader<T, DP> &at, const unsigned char *tile, int block, const f32x16 (&p)[N], f32x16 (&acc)[DP / 32])
 {
     using R = Row<T, DP>;
     if constexpr (sizeof(T) == 2) {
         typedef __attribute__((address_space(3))) tile::s16x4 *lds_ptr;
         unsigned char *from = const_cast<unsigned char *>(tile) + block * 32 * R::BYTES;
         const int across = opaque(at.across);
+        bf16x8 w;
+        in_turn<N * 2 * R::BLOCKS, AHEAD<DP>>(
+            [&](int i) {
+                const int b = i % R::BLOCKS, first = i / R::BLOCKS * 16;
+                const tile::s16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_ptr)(from + (across ^ (b << 6)) + first * R::BYTES));
+                const tile::s16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_ptr)(from + (across ^ (b << 6) ^ 32) + (first + 8) * R::BYTES));
+                return __builtin_bit_cast(bf16x8, __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7));
+            },
+            [&](int i, const bf16x8 &v) {
+                const int b = i % R::BLOCKS, s = i / R::BLOCKS;
+                if (b == 0)
 #pragma unroll
-        for (int s = 0; s < 2; ++s) {
-            bf16x8 w[N];
-#pragma unroll
-            for (int n = 0; n < N; ++n)
-#pragma unroll
-                for (int e = 0; e < 8; ++e) w[n][e] = (__bf16)p[n][8 * s + e];
-#pragma unroll
-            for (int b = 0; b < R::BLOCKS; ++b) {
-                const tile::s16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_ptr)(from + (across ^ (b << 6)) + s * 16 * R::BYTES));
-                const tile::s16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_ptr)(from + (across ^ (b << 6) ^ 32) + (s * 16 + 8) * R::BYTES));
-                const bf16x8 v = __builtin_bit_cast(bf16x8, __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7));
-#pragma unroll
-                for (int n = 0; n < N; ++n) acc[n][b] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(v, w[n], acc[n][b], 0, 0, 0);
-            }
-        }
+                    for (int e = 0; e < 8; ++e) w[e] = (__bf16)p[s >> 1][8 * (s & 1) + e];
+                acc[b] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(v, w, acc[b], 0, 0, 0);
+            });
     } else {
         const int lane = threadIdx.x & 63, half = lane >> 5, l = lane & 31;
-#pragma unroll
-        for (int i = 0; i < 16; ++i) {
-            const int r = row_of(i, half);
-#pragma unroll
-            for (int b = 0; b < R::BLOCKS; ++b) {
-                const int chunk = 8 * b + (l >> 2);
-                const float v = *reinterpret_cast<const float *>(tile + (block * 32 + r) * R::BYTES + ((chunk ^ R::turn(r)) << 4) + (l & 3) * 4);
-#pragma unroll
-                for (int n = 0; n < N; ++n) acc[n][b] = __builtin_amdgcn_mfma_f32_32x32x2f32(v, p[n][i], acc[n][b], 0, 0, 0);
-            }
-        }
+        in_turn<N * 16 * R::BLOCKS, 4>(
+            [&](int i) {
+                const int b = i % R::BLOCKS, r = row_of(i / R::BLOCKS % 16, half), chunk = 8 * b + (l >> 2);
+                return *reinterpret_cast<const float *>(tile + ((block + i / R::BLOCKS / 16) * 32 + r) * R::BYTES + ((chunk ^ R::turn(r)) << 4) + (l & 3) * 4);
+            },
+            [&](int i, float v) {
+                const int b = i % R::BLOCKS, j = i / R::BLOCKS;
+                acc[b] = __builtin_amdgcn_mfma_f32_32x32x2f32(v, p[j / 16][j % 16], acc[b], 0, 0, 0);
+            });
     }
 }
 
@@ -487,15 +527,23 @@ __device__ __forceinline__ void fill_bias(const Args &a, int head, int count, fl
     const bool behind = c >= a.bias.buckets;
     int from, until;
     distances(a.bias, behind ? c - a.bias.buckets : c, &from, &until);
-    for (int g = 0; g < count; ++g) {
-        const int at = c * a.heads + head + g;
-        float v = a.bias.f32 ? ((const float *)a.bias.table)[at] : (float)((const __bf16 *)a.bias.table)[at];
-        // (the type's lowest value, as a mask, stays a number: a row of nothing else is a row of equal scores)
-        if (fabsf(v) <= 3.402823466e38f) v = __builtin_amdgcn_fmed3f(v * 1.44269504f, -3.4e38f, 3.4e38f);
-        float *const zero = to + g * width + MARGIN + a.bias.reach;
-        for (int r = from + (int)threadIdx.x % parts; r < until; r += parts)
-            if (!behind) zero[-r] = v;
-            else if (r > 0) zero[r] = v;
+    for (int g0 = 0; g0 < count; g0 += 4) {
+        float v[4];                     // (four heads' values on their way at once)
+#pragma unroll
+        for (int g = 0; g < 4; ++g) {
+            const int at = c * a.heads + head + min(g0 + g, count - 1);
+            v[g] = a.bias.f32 ? ((const float *)a.bias.table)[at] : (float)((const __bf16 *)a.bias.table)[at];
+        }
+#pragma unroll
+        for (int g = 0; g < 4; ++g) {
+            if (g0 + g >= count) break;
+            // (the type's lowest value, as a mask, stays a number: a row of nothing else is a row of equal scores)
+            const float x = fabsf(v[g]) <= 3.402823466e38f ? __builtin_amdgcn_fmed3f(v[g] * 1.44269504f, -3.4e38f, 3.4e38f) : v[g];
+            float *const zero = to + (g0 + g) * width + MARGIN + a.bias.reach;
+            for (int r = from + (int)threadIdx.x % parts; r < until; r += parts)
+                if (!behind) zero[-r] = x;
+                else if (r > 0) zero[r] = x;
+        }
     }
 }
 // The table's value at an offset, in powers of two.

@@ -161,11 +161,14 @@ struct SetUp {
     }
 };
 
-// each: workgroups of a sequence and head of k and v
-template <typename K> int launch(K kernel, int64_t sequences, int64_t each, int lds, const Args &a, hipStream_t stream)
+// each: workgroups of a sequence and head of k and v.  most: workgroups that are launched, where each of them goes on to others.
+template <typename K> int launch(K kernel, int64_t sequences, int64_t each, int threads, int64_t most, int lds, Args &a, hipStream_t stream)
 {
     if (lds > MOST_LDS) return RCD_ERR_UNSUPPORTED;
-    hipLaunchKernelGGL(kernel, dim3((unsigned)workgroups_of(sequences, a.kv_heads, each)), dim3(THREADS), lds, stream, a);
+    const int64_t all = workgroups_of(sequences, a.kv_heads, each);
+    if (all > attn_rules::MOST_WORKGROUPS + 8) return RCD_ERR_UNSUPPORTED;
+    a.workgroups = (int)all;
+    hipLaunchKernelGGL(kernel, dim3((unsigned)(most > 0 ? std::min(all, most) : all)), dim3(threads), lds, stream, a);
     ENC_HIP_TRY(hipGetLastError());
     return RCD_OK;
 }

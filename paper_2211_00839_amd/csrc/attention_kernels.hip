@@ -5,302 +5,333 @@
 namespace attn {
 
 // SHARED false: a workgroup's four waves hold 32 rows of q each and share tiles of TILE keys, the next one on its way while one is used.
-// SHARED true: few rows of q.  The waves hold the same 32, and each goes through tiles of 32 keys of its own, every fourth one, without meeting
-// the others; their sums are joined at the end.  Either may leave its keys to several workgroups (splits), joined by k_attention_join.
+// SHARED true: few rows of q.  Eight waves (four where tiles are large) hold the same 32, and each goes through tiles of 32 keys of its own, every
+// eighth one, without meeting the others; their sums are joined at the end.  A workgroup takes on one row tile and part of the keys after the other.
+// Either may leave its keys to several workgroups (splits), joined by k_attention_join.
 template <typename T, int DP, bool SHARED> struct Forward {
     using R = Row<T, DP>;
     static constexpr int TILE = SHARED || R::BYTES == 512 ? 32 : 64;
-    static constexpr int LOADERS = SHARED ? 64 : THREADS;
-    static constexpr int STAGES = SHARED && R::BYTES == 512 ? 1 : 2;
+    static constexpr int WAVES = SHARED && R::BYTES < 512 ? 8 : 4, GROUP = 64 * WAVES;
+    static constexpr int LOADERS = SHARED ? 64 : GROUP;
+    static constexpr int STAGES = SHARED && R::BYTES >= 256 ? 1 : 2;
     static constexpr int HALF = TILE * R::BYTES, STAGE = 2 * HALF;              // of keys, of keys and values
-    static constexpr int TILES_BYTES = STAGES * STAGE * (SHARED ? 4 : 1);
+    static constexpr int TILES_BYTES = STAGES * STAGE * (SHARED ? WAVES : 1);
+    static constexpr int STATS_BYTES = SHARED ? WAVES * 64 * 4 : 0;             // a maximum and a sum for each of the 32 rows
     static constexpr int LOADS = 2 * TILE * R::CHUNKS / LOADERS;                // of a lane, to a stage
 };
 
 template <typename T, int DP, bool SHARED, bool BIAS, bool DIRECT>
-__global__ __launch_bounds__(THREADS, sizeof(T) == 2 && !SHARED ? (DP == 64 ? 3 : 2) : 1) void k_attention(Args a)
+__global__ __launch_bounds__(SHARED && sizeof(T) * DP < 512 ? 512 : 256, SHARED ? (sizeof(T) * DP < 512 ? 2 : 1) : sizeof(T) == 4 ? 1 : DP == 64 ? 3 : 2)
+    void k_attention(Args a)
 {
     using F = Forward<T, DP, SHARED>;
     using R = Row<T, DP>;
-    constexpr int ROWS = SHARED ? 32 : 128, BLOCKS = F::TILE / 32;
+    constexpr int ROWS = SHARED ? 32 : 128, BLOCKS = F::TILE / 32, WAVES = F::WAVES;
+    constexpr int GROUPS = SHARED ? 4 * R::BLOCKS / WAVES : 4 * R::BLOCKS;      // of four elements, that a wave stores of its rows
     extern __shared__ __align__(1024) unsigned char lds[];
     const int tid = threadIdx.x, lane = tid & 63, half = lane >> 5, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int packs = a.group / a.pack;                         // of packed heads that share a head of k and v
-    Unit unit;
-    if (!unit_of(blockIdx.x, a.batch + (a.clear ? 1 : 0), a.kv_heads, a.tiles * packs * a.splits, &unit)) return;
-    const int b = unit.sequence, kv_head = unit.kv_head;
-    const int first_tile = a.tiles - 1 - unit.in % a.tiles;     // (causal: the longest first)
-    const int head0 = (kv_head * packs + unit.in / a.tiles % packs) * a.pack, split = unit.in / a.tiles / packs;
-    if (b == a.batch) {
-        if (split == 0)
-            for (int g = 0; g < a.pack; ++g) clear_rows<T>(a.o, a.q_offsets, a.batch, a.q_rows, head0 + g, a.D, first_tile, a.tiles);
-        return;
-    }
-    const Sequence seq = sequence(a, b);
-    const int columns = seq.q_len * a.pack;
-    if (first_tile * ROWS >= columns) return;
-    const int shift = seq.k_len - seq.q_len;
-    const char *const keys = rows_of(a.k, b, a.k_offsets != nullptr, seq.k0, kv_head), *const values = rows_of(a.v, b, a.k_offsets != nullptr, seq.k0, kv_head);
-    float *const table = reinterpret_cast<float *>(lds + F::TILES_BYTES);
-    const int width = BIAS ? bias_width(a.bias.reach, a.causal) : 0;
-    bool filled = false;
-    unsigned char *const stages = lds + (SHARED ? wave * F::STAGES * F::STAGE : 0);
-    const unsigned stages_addr = (unsigned)(size_t)(__attribute__((address_space(3))) unsigned char *)lds + (SHARED ? wave * F::STAGES * F::STAGE : 0);
-    Reader<T, DP> reader;
-    reader.init();
-    Loader<T, DP, F::TILE, F::LOADERS, DIRECT> load_k, load_v;
-    load_k.init(a.k.row, a.D, SHARED ? lane : tid);
-    load_v.init(a.v.row, a.D, SHARED ? lane : tid);
-    for (int tile0 = first_tile * ROWS; tile0 < columns; tile0 += a.tiles * ROWS) {
-        // ---- the keys that any of this workgroup's rows sees, and its and this wave's tiles of them
-        const int mine0 = tile0 + (SHARED ? 0 : wave * 32);
-        const int last = shift + (min(tile0 + ROWS, columns) - 1) / a.pack;                     // the last row's position
-        const int end = a.causal ? max(0, min(seq.k_len, last + 1)) : seq.k_len;
-        const int lowest = shift + min(mine0, columns - 1) / a.pack, highest = shift + (min(mine0 + 32, columns) - 1) / a.pack;
-        const int tiles = (end + F::TILE - 1) / F::TILE, per = max((tiles + a.splits - 1) / a.splits, min(tiles, a.least));
-        const int from = split * per, t0 = from + (SHARED ? wave : 0), t1 = min(tiles, from + per), step = SHARED ? 4 : 1;
-        // ---- this wave's rows of q
-        const int column = mine0 + (lane & 31), in = min(column, columns - 1);
-        const bool there = column < columns;
-        const int row = in / a.pack, head = head0 + in - row * a.pack, pos = shift + row;
-        const long long slot = (seq.q_first + row) * a.heads + head;
-        if (a.splits > 1 && from >= t1 && split > 0) {
-            if (there && half == 0 && (!SHARED || wave == 0))
-                *reinterpret_cast<float2 *>(a.part_ml + 2 * ((long long)split * (a.q_all * a.heads) + slot)) = make_float2(-__builtin_inff(), 0.f);
+    const int sequences = a.batch + (a.clear ? 1 : 0), each = a.tiles * packs * a.splits;
+    int id = blockIdx.x, round = 0;
+    do {
+        Unit unit;
+        if (!unit_of(id, sequences, a.kv_heads, each, &unit, round)) continue;
+        const int b = unit.sequence, kv_head = unit.kv_head;
+        const int first_tile = a.tiles - 1 - unit.in % a.tiles;     // (causal: the longest first)
+        const int head0 = (kv_head * packs + unit.in / a.tiles % packs) * a.pack, split = unit.in / a.tiles / packs;
+        if (b == a.batch) {
+            if (split == 0)
+                for (int g = 0; g < a.pack; ++g) clear_rows<T>(a.o, a.q_offsets, a.batch, a.q_rows, head0 + g, a.D, first_tile, a.tiles);
             continue;
         }
-        auto load = [&](int t, int buf) {
-            const int k0 = t * F::TILE;
-            unsigned char *const to = stages + buf * F::STAGE;
-            const unsigned to_addr = stages_addr + buf * F::STAGE;
-            load_k.issue(to, to_addr, keys + (long long)k0 * a.k.row, end - k0, a.D, SHARED ? 0 : wave);
-            load_v.issue(to + F::HALF, to_addr + F::HALF, values + (long long)k0 * a.v.row, end - k0, a.D, SHARED ? 0 : wave);
-        };
-        // A tile that has come; of the keys behind the last one the scores are masked, of the values there have to be zeros.
-        auto clear = [&](int t, int buf) {
-            const int rows = end - t * F::TILE;
-            if (rows < F::TILE) load_v.clear(stages + buf * F::STAGE + F::HALF, rows, SHARED ? 0 : wave);
-        };
-        if (F::STAGES == 2 && t0 < t1) load(t0, 0);
-        uint4 q[R::STEPS];
-        {
-            const char *p = rows_of(a.q, b, a.q_offsets != nullptr, seq.q0 + row, head);
-#pragma unroll
-            for (int s = 0; s < R::STEPS; ++s) q[s] = chunk_of<T, DIRECT>(p, 2 * s + half, a.D);
-        }
-        const float *const my_table = table + (head - head0) * width;
-        if constexpr (BIAS)
-            if (!filled) {
-                fill_bias(a, head0, a.pack, table);
-                filled = true;
-                if constexpr (SHARED) {
-                    tile::wait_lds();
-                    tile::meet();
-                }
+        const Sequence seq = sequence(a, b);
+        const int columns = seq.q_len * a.pack, shift = seq.k_len - seq.q_len;
+        if (first_tile * ROWS >= columns) continue;
+        const char *const keys = rows_of(a.k, b, a.k_offsets != nullptr, seq.k0, kv_head), *const values = rows_of(a.v, b, a.k_offsets != nullptr, seq.k0, kv_head);
+        float *const table = reinterpret_cast<float *>(lds + F::TILES_BYTES + F::STATS_BYTES);
+        const int width = BIAS ? bias_width(a.bias.reach, a.causal) : 0;
+        bool filled = false;
+        unsigned char *const stages = lds + (SHARED ? wave * F::STAGES * F::STAGE : 0);
+        const unsigned stages_addr = (unsigned)(size_t)(__attribute__((address_space(3))) unsigned char *)lds + (SHARED ? wave * F::STAGES * F::STAGE : 0);
+        Reader<T, DP> reader;
+        reader.init();
+        Loader<T, DP, F::TILE, F::LOADERS, DIRECT> load_k, load_v;
+        load_k.init(a.k.row, a.D, SHARED ? lane : tid);
+        load_v.init(a.v.row, a.D, SHARED ? lane : tid);
+        for (int tile0 = first_tile * ROWS; tile0 < columns; tile0 += a.tiles * ROWS) {
+            // ---- the keys that any of this workgroup's rows sees, and its and this wave's tiles of them
+            const int mine0 = tile0 + (SHARED ? 0 : wave * 32);
+            const int last = shift + (min(tile0 + ROWS, columns) - 1) / a.pack;                     // the last row's position
+            const int end = a.causal ? max(0, min(seq.k_len, last + 1)) : seq.k_len;
+            const int lowest = shift + min(mine0, columns - 1) / a.pack, highest = shift + (min(mine0 + 32, columns) - 1) / a.pack;
+            const int tiles = (end + F::TILE - 1) / F::TILE, per = max((tiles + a.splits - 1) / a.splits, min(tiles, a.least));
+            const int from = split * per, t0 = from + (SHARED ? wave : 0), t1 = min(tiles, from + per), step = SHARED ? WAVES : 1;
+            // ---- this wave's rows of q
+            const int column = mine0 + (lane & 31), in = min(column, columns - 1);
+            const bool there = column < columns;
+            const int row = in / a.pack, head = head0 + in - row * a.pack, pos = shift + row;
+            const long long slot = (seq.q_first + row) * a.heads + head;
+            if (a.splits > 1 && from >= t1 && split > 0) {
+                if (there && half == 0 && (!SHARED || wave == 0))
+                    *reinterpret_cast<float2 *>(a.part_ml + 2 * ((long long)split * (a.q_all * a.heads) + slot)) = make_float2(-__builtin_inff(), 0.f);
+                continue;
             }
-        // top: the maximum that the exponents are taken from (it follows the scores' maximum when that is 2^8 above it); sum: of this lane's keys
-        float top = -__builtin_inff(), sum = 0.f;
-        f32x16 acc[1][R::BLOCKS];
+            auto load_keys = [&](int t, int buf) {
+                const int k0 = t * F::TILE;
+                load_k.issue(stages + buf * F::STAGE, stages_addr + buf * F::STAGE, keys + (long long)k0 * a.k.row, end - k0, a.D, SHARED ? 0 : wave);
+            };
+            auto load_values = [&](int t, int buf) {
+                const int k0 = t * F::TILE;
+                load_v.issue(stages + buf * F::STAGE + F::HALF, stages_addr + buf * F::STAGE + F::HALF, values + (long long)k0 * a.v.row, end - k0, a.D,
+                             SHARED ? 0 : wave);
+            };
+            auto load = [&](int t, int buf) {
+                load_keys(t, buf);
+                load_values(t, buf);
+            };
+            // A tile that has come; of the keys behind the last one the scores are masked, of the values there have to be zeros.
+            auto clear = [&](int t, int buf) {
+                const int rows = end - t * F::TILE;
+                if (rows < F::TILE) load_v.clear(stages + buf * F::STAGE + F::HALF, rows, SHARED ? 0 : wave);
+            };
+            if (t0 < t1) load(t0, 0);
+            uint4 q[R::STEPS];
+            {
+                const char *p = rows_of(a.q, b, a.q_offsets != nullptr, seq.q0 + row, head);
 #pragma unroll
-        for (int d = 0; d < R::BLOCKS; ++d)
-#pragma unroll
-            for (int i = 0; i < 16; ++i) acc[0][d][i] = 0.f;
-        bool left_out = false;
-        // One tile.  edge: some of it is masked; near: its offsets are not all in the bias's last bucket.  (One body for all of them: several would each
-        // want the sums in registers of their own.)
-        auto compute = [&](bool edge, bool near, int k0, const unsigned char *ktile) {
-            const unsigned char *const vtile = ktile + F::HALF;
-            f32x16 p[BLOCKS][1];
-#pragma unroll
-            for (int kb = 0; kb < BLOCKS; ++kb)
-                p[kb][0] = scores<T, DP>(reader, ktile, kb, q);
-            float by = a.scale2, plus = 0.f;        // what is still to be done to the scores
-            if (BIAS && near) {
-                const float *const bias = my_table + (k0 - pos) + 4 * half + a.bias.reach + MARGIN;
-#pragma unroll
-                for (int kb = 0; kb < BLOCKS; ++kb)
-#pragma unroll
-                    for (int i = 0; i < 16; ++i) p[kb][0][i] = fmaf(p[kb][0][i], a.scale2, bias[32 * kb + row_of(i, 0)]);
-                by = 1.f;
-            } else if (BIAS) {
-                plus = far_bias(a, my_table, k0 + F::TILE - 1 - lowest);
-                if (__any(!(fabsf(plus) < 4096.f))) {
-                    // (where the bias swallows the scores, as the type's lowest value does, it has to do so in every tile)
-#pragma unroll
-                    for (int kb = 0; kb < BLOCKS; ++kb)
-#pragma unroll
-                        for (int i = 0; i < 16; ++i) p[kb][0][i] = fmaf(p[kb][0][i], a.scale2, plus);
-                    by = 1.f;
-                    plus = 0.f;
-                }
+                for (int s = 0; s < R::STEPS; ++s) q[s] = chunk_of<T, DIRECT>(p, 2 * s + half, a.D);
+                arrive(q);
             }
-            if (edge) {
-                const int most = min(a.causal ? pos : end - 1, end - 1) - k0;
-#pragma unroll
-                for (int kb = 0; kb < BLOCKS; ++kb)
-#pragma unroll
-                    for (int i = 0; i < 16; ++i) p[kb][0][i] = 32 * kb + row_of(i, half) <= most ? p[kb][0][i] : -__builtin_inff();
-            }
-            float m = p[0][0][0];
-#pragma unroll
-            for (int kb = 0; kb < BLOCKS; ++kb)
-#pragma unroll
-                for (int i = 0; i < 16; ++i) m = fmaxf(m, p[kb][0][i]);
-            m = max_halves(m);
-            m = fmaf(m, by, plus);
-            if (__any(m > top + 8.f)) {
-                const float next = fmaxf(m, top);
-                const float back = top == next ? 1.f : __builtin_amdgcn_exp2f(top - next);
-                top = next;
-                sum *= back;
-#pragma unroll
-                for (int d = 0; d < R::BLOCKS; ++d)
-#pragma unroll
-                    for (int i = 0; i < 16; ++i) acc[0][d][i] *= back;
-            }
-            const float from = (top == -__builtin_inff() ? 0.f : top) - plus;
-            float part[4] = {0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-            for (int kb = 0; kb < BLOCKS; ++kb)
-#pragma unroll
-                for (int i = 0; i < 16; ++i) {
-                    const float e = __builtin_amdgcn_exp2f(fmaf(p[kb][0][i], by, -from));
-                    p[kb][0][i] = e;
-                    part[i & 3] += e;
-                }
-            sum += (part[0] + part[1]) + (part[2] + part[3]);
-            if (edge && a.causal && any_not_finite<T, DP, F::TILE>(vtile)) {
-                left_out = true;
-                return;
-            }
-#pragma unroll
-            for (int kb = 0; kb < BLOCKS; ++kb) weigh<T, DP, 1>(reader, vtile, kb, p[kb], acc);
-        };
-        int buf = 0;
-        for (int t = t0; t < t1; t += step, buf ^= F::STAGES - 1) {
-            if constexpr (SHARED) {
-                tile::wait_lds();
-                if (F::STAGES == 1) {
-                    load(t, 0);
-                    tile::wait_loads<0>();
-                } else if (t + step < t1) {
-                    load(t + step, buf ^ 1);
-                    if (DIRECT) tile::wait_loads<F::LOADS>();
-                } else {
-                    tile::wait_loads<0>();
-                }
-                clear(t, buf);
-                tile::wait_lds();
-            } else {
-                tile::wait_loads<0>();
-                clear(t, buf);
-                tile::wait_lds();
-                tile::meet();
-                if (t + 1 < t1) load(t + 1, buf ^ 1);
-            }
-            const int k0 = t * F::TILE;
-            if (!SHARED && ((a.causal && k0 > highest) || mine0 >= columns)) continue;
-            const unsigned char *const ktile = stages + buf * F::STAGE;
-            const bool edge = k0 + F::TILE > end || (a.causal && k0 + F::TILE - 1 > lowest);
-            compute(edge, BIAS && !is_far(a, k0 - highest, k0 + F::TILE - 1 - lowest), k0, ktile);
-        }
-        if (!SHARED && a.causal) tile::meet();
-        if (left_out) {
-            // the tiles on the border that hold something that is not finite
-            const char *const mine = rows_of(a.q, b, a.q_offsets != nullptr, seq.q0 + row, head);
-            add_rows<T, DP>(SHARED ? stages : lds + wave * 4096, a.D, acc[0], [&](auto add) {
-#pragma unroll 1
-                for (int t = t0; t < t1; t += step) {
-                    const int j0 = t * F::TILE, count = min(F::TILE, end - j0);
-                    if ((j0 + F::TILE <= end && j0 + F::TILE - 1 <= lowest) || j0 > highest) continue;
-                    if (!any_not_finite<T>(values + (long long)j0 * a.v.row, a.v.row, count, a.D)) continue;
-#pragma unroll 1
-                    for (int j = j0; j < j0 + count; ++j) {
-                        if (j > pos) continue;
-                        float x = dot<T>(mine, keys + (long long)j * a.k.row, a.D) * a.scale2;
-                        if constexpr (BIAS) x += bias_at(a, head, j - pos);
-                        add(__builtin_amdgcn_exp2f(x - (top == -__builtin_inff() ? 0.f : top)), values + (long long)j * a.v.row);
+            const float *const my_table = table + (head - head0) * width;
+            if constexpr (BIAS)
+                if (!filled) {
+                    fill_bias(a, head0, a.pack, table);
+                    filled = true;
+                    if constexpr (SHARED) {
+                        tile::wait_lds();
+                        tile::meet();
                     }
                 }
-            });
-        }
-        // ---- what leaves
-        sum = add_halves(sum);
-        int d0 = 0;                             // groups of four elements that this wave stores
-        if constexpr (SHARED) {
-            // the waves' sums over one maximum, a quarter of the elements in each wave
-            tile::wait_lds();
-            tile::meet();
-            float *const sums = reinterpret_cast<float *>(lds), *const ml = sums + 4 * DP * 32;
-            static_assert(4 * DP * 32 * 4 + 4 * 64 * 4 <= F::TILES_BYTES, "they fit where the tiles were");
+            // top: the maximum that the exponents are taken from (it follows the scores' maximum when that is 2^8 above it); sum: of this lane's keys
+            float top = -__builtin_inff(), sum = 0.f;
+            f32x16 acc[R::BLOCKS];
 #pragma unroll
             for (int d = 0; d < R::BLOCKS; ++d)
 #pragma unroll
-                for (int i = 0; i < 16; ++i) sums[((wave * R::BLOCKS + d) * 16 + i) * 64 + lane] = acc[0][d][i];
-            if (half == 0) {
-                ml[wave * 64 + lane] = top;
-                ml[wave * 64 + 32 + lane] = sum;
+                for (int i = 0; i < 16; ++i) acc[d][i] = 0.f;
+            bool left_out = false;
+            // One tile.  edge: some of it is masked; near: its offsets are not all in the bias's last bucket.  (One body for all of them: several would each
+            // want the sums in registers of their own.)
+            auto compute = [&](bool edge, bool near, int k0, const unsigned char *ktile, auto keys_read, auto values_wanted) {
+                const unsigned char *const vtile = ktile + F::HALF;
+                f32x16 p[BLOCKS];
+                scores<T, DP, BLOCKS>(reader, ktile, q, p);
+                keys_read();
+                float by = a.scale2, plus = 0.f;        // what is still to be done to the scores
+                if (BIAS && near) {
+                    const float *const bias = my_table + (k0 - pos) + 4 * half + a.bias.reach + MARGIN;
+#pragma unroll
+                    for (int kb = 0; kb < BLOCKS; ++kb)
+#pragma unroll
+                        for (int i = 0; i < 16; ++i) p[kb][i] = fmaf(p[kb][i], a.scale2, bias[32 * kb + row_of(i, 0)]);
+                    by = 1.f;
+                } else if (BIAS) {
+                    plus = far_bias(a, my_table, k0 + F::TILE - 1 - lowest);
+                    if (__any(!(fabsf(plus) < 4096.f))) {
+                        // (where the bias swallows the scores, as the type's lowest value does, it has to do so in every tile)
+#pragma unroll
+                        for (int kb = 0; kb < BLOCKS; ++kb)
+#pragma unroll
+                            for (int i = 0; i < 16; ++i) p[kb][i] = fmaf(p[kb][i], a.scale2, plus);
+                        by = 1.f;
+                        plus = 0.f;
+                    }
+                }
+                if (edge) {
+                    const int most = min(a.causal ? pos : end - 1, end - 1) - k0;
+#pragma unroll
+                    for (int kb = 0; kb < BLOCKS; ++kb)
+#pragma unroll
+                        for (int i = 0; i < 16; ++i) p[kb][i] = 32 * kb + row_of(i, half) <= most ? p[kb][i] : -__builtin_inff();
+                }
+                float m = p[0][0];
+#pragma unroll
+                for (int kb = 0; kb < BLOCKS; ++kb)
+#pragma unroll
+                    for (int i = 0; i < 16; ++i) m = fmaxf(m, p[kb][i]);
+                m = max_halves(m);
+                m = fmaf(m, by, plus);
+                if (__any(m > top + 8.f)) {
+                    const float next = fmaxf(m, top);
+                    const float back = top == next ? 1.f : __builtin_amdgcn_exp2f(top - next);
+                    top = next;
+                    sum *= back;
+#pragma unroll
+                    for (int d = 0; d < R::BLOCKS; ++d)
+#pragma unroll
+                        for (int i = 0; i < 16; ++i) acc[d][i] *= back;
+                }
+                const float from = (top == -__builtin_inff() ? 0.f : top) - plus;
+                float part[4] = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+                for (int kb = 0; kb < BLOCKS; ++kb)
+#pragma unroll
+                    for (int i = 0; i < 16; ++i) {
+                        const float e = __builtin_amdgcn_exp2f(fmaf(p[kb][i], by, -from));
+                        p[kb][i] = e;
+                        part[i & 3] += e;
+                    }
+                sum += (part[0] + part[1]) + (part[2] + part[3]);
+                values_wanted();
+                if (edge && a.causal && any_not_finite<T, DP, F::TILE>(vtile)) {
+                    left_out = true;
+                    return;
+                }
+                weigh<T, DP, BLOCKS>(reader, vtile, 0, p, acc);
+            };
+            int buf = 0;
+            for (int t = t0; t < t1; t += step, buf ^= F::STAGES - 1) {
+                const int k0 = t * F::TILE;
+                const unsigned char *const ktile = stages + buf * F::STAGE;
+                const bool edge = k0 + F::TILE > end || (a.causal && k0 + F::TILE - 1 > lowest);
+                const bool near = BIAS && !is_far(a, k0 - highest, k0 + F::TILE - 1 - lowest);
+                if constexpr (SHARED && F::STAGES == 1) {
+                    // one stage: the next keys are asked for once these are read, the next values once these are
+                    if (DIRECT) tile::wait_loads<F::LOADS / 2>();
+                    tile::wait_lds();
+                    compute(edge, near, k0, ktile,
+                            [&] {
+                                tile::wait_lds();
+                                if (t + step < t1) load_keys(t + step, 0);
+                            },
+                            [&] {
+                                if (DIRECT && t + step < t1) tile::wait_loads<F::LOADS / 2>();
+                                else tile::wait_loads<0>();
+                                clear(t, 0);
+                                tile::wait_lds();
+                            });
+                    tile::wait_lds();
+                    if (t + step < t1) load_values(t + step, 0);
+                    continue;
+                }
+                if constexpr (SHARED) {
+                    tile::wait_lds();
+                    if (t + step < t1) {
+                        load(t + step, buf ^ 1);
+                        if (DIRECT) tile::wait_loads<F::LOADS>();
+                    } else {
+                        tile::wait_loads<0>();
+                    }
+                    clear(t, buf);
+                    tile::wait_lds();
+                } else {
+                    tile::wait_loads<0>();
+                    clear(t, buf);
+                    tile::wait_lds();
+                    tile::meet();
+                    if (t + 1 < t1) load(t + 1, buf ^ 1);
+                    if ((a.causal && k0 > highest) || mine0 >= columns) continue;
+                }
+                compute(edge, near, k0, ktile, [] {}, [] {});
             }
+            if (!SHARED && a.causal) tile::meet();
+            if (left_out) {
+                // the tiles on the border that hold something that is not finite
+                const char *const mine = rows_of(a.q, b, a.q_offsets != nullptr, seq.q0 + row, head);
+                add_rows<T, DP>(SHARED ? stages : lds + wave * 4096, a.D, acc, [&](auto add) {
+#pragma unroll 1
+                    for (int t = t0; t < t1; t += step) {
+                        const int j0 = t * F::TILE, count = min(F::TILE, end - j0);
+                        if ((j0 + F::TILE <= end && j0 + F::TILE - 1 <= lowest) || j0 > highest) continue;
+                        if (!any_not_finite<T>(values + (long long)j0 * a.v.row, a.v.row, count, a.D)) continue;
+#pragma unroll 1
+                        for (int j = j0; j < j0 + count; ++j) {
+                            if (j > pos) continue;
+                            float x = dot<T>(mine, keys + (long long)j * a.k.row, a.D) * a.scale2;
+                            if constexpr (BIAS) x += bias_at(a, head, j - pos);
+                            add(__builtin_amdgcn_exp2f(x - (top == -__builtin_inff() ? 0.f : top)), values + (long long)j * a.v.row);
+                        }
+                    }
+                });
+            }
+            // ---- what leaves
+            sum = add_halves(sum);
+            int d0 = 0;                             // groups of four elements that this wave stores
+            if constexpr (SHARED) {
+                // the waves' sums over one maximum, as many of the elements in each wave
+                tile::wait_lds();
+                tile::meet();
+                float *const sums = reinterpret_cast<float *>(lds), *const ml = reinterpret_cast<float *>(lds + F::TILES_BYTES);
+                static_assert(WAVES * DP * 32 * 4 <= F::TILES_BYTES, "they fit where the tiles were");
+#pragma unroll
+                for (int d = 0; d < R::BLOCKS; ++d)
+#pragma unroll
+                    for (int i = 0; i < 16; ++i) sums[((wave * R::BLOCKS + d) * 16 + i) * 64 + lane] = acc[d][i];
+                if (half == 0) {
+                    ml[wave * 64 + lane] = top;
+                    ml[wave * 64 + 32 + lane] = sum;
+                }
+                tile::wait_lds();
+                tile::meet();
+                float m = -__builtin_inff(), weight[WAVES], total_sum = 0.f;
+#pragma unroll
+                for (int w = 0; w < WAVES; ++w) m = fmaxf(m, ml[w * 64 + (lane & 31)]);
+#pragma unroll
+                for (int w = 0; w < WAVES; ++w) {
+                    const float its = ml[w * 64 + (lane & 31)], l = ml[w * 64 + 32 + (lane & 31)];
+                    weight[w] = its == m ? 1.f : __builtin_amdgcn_exp2f(its - m);
+                    // (a wave without keys has no part in it; one whose scores are all NaN has)
+                    if (l == 0.f) weight[w] = 0.f;
+                    total_sum = l == 0.f ? total_sum : fmaf(weight[w], l, total_sum);
+                }
+                top = m;
+                sum = total_sum;
+                d0 = wave * GROUPS;
+#pragma unroll
+                for (int g = 0; g < GROUPS; ++g)
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) {
+                        float v = 0.f;
+#pragma unroll
+                        for (int w = 0; w < WAVES; ++w) {
+                            const float part = sums[((w * R::BLOCKS * 4 + d0 + g) * 4 + e) * 64 + lane];
+                            v = weight[w] == 0.f ? v : fmaf(weight[w], part, v);
+                        }
+                        acc[0][4 * g + e] = v;
+                    }
+            }
+            if (there) {
+                const bool none = sum == 0.f, one = half == 0 && (!SHARED || wave == 0);
+                const int D = opaque(a.D), first = opaque(8 * d0 + 4 * half);
+                if (a.splits > 1) {
+                    const long long part = (long long)split * (a.q_all * a.heads) + slot;
+                    if (one) *reinterpret_cast<float2 *>(a.part_ml + 2 * part) = make_float2(top, sum);
+#pragma unroll
+                    for (int g = 0; g < GROUPS; ++g) {
+                        const int d = first + 8 * g, x = g >> 2, y = 4 * (g & 3);
+                        if (d < D) store4<float, DIRECT>(a.part_o + part * a.D + d, D - d, acc[x][y], acc[x][y + 1], acc[x][y + 2], acc[x][y + 3]);
+                    }
+                } else {
+                    const float scale = none ? 0.f : 1.f / sum;
+                    T *const out = reinterpret_cast<T *>(rows_of(a.o, b, a.q_offsets != nullptr, seq.q0 + row, head));
+#pragma unroll
+                    for (int g = 0; g < GROUPS; ++g) {
+                        const int d = first + 8 * g, x = g >> 2, y = 4 * (g & 3);
+                        if (d < D)
+                            store4<T, DIRECT>(out + d, D - d, acc[x][y] * scale, acc[x][y + 1] * scale, acc[x][y + 2] * scale, acc[x][y + 3] * scale);
+                    }
+                    // (a row that sees no key: a maximum that leaves every weight at zero)
+                    if (a.saved && one)
+                        *reinterpret_cast<float2 *>(a.saved + 2 * slot) =
+                            make_float2(none ? __builtin_inff() : top == -__builtin_inff() ? 0.f : top, none ? 0.f : __builtin_amdgcn_logf(sum));
+                }
+            }
+            // (another round of rows uses the tiles again)
+            tile::wait_loads<0>();
             tile::wait_lds();
             tile::meet();
-            float m = -__builtin_inff(), weight[4], total_sum = 0.f;
-#pragma unroll
-            for (int w = 0; w < 4; ++w) m = fmaxf(m, ml[w * 64 + (lane & 31)]);
-#pragma unroll
-            for (int w = 0; w < 4; ++w) {
-                const float its = ml[w * 64 + (lane & 31)], l = ml[w * 64 + 32 + (lane & 31)];
-                weight[w] = its == m ? 1.f : __builtin_amdgcn_exp2f(its - m);
-                // (a wave without keys has no part in it; one whose scores are all NaN has)
-                if (l == 0.f) weight[w] = 0.f;
-                total_sum = l == 0.f ? total_sum : fmaf(weight[w], l, total_sum);
-            }
-            top = m;
-            sum = total_sum;
-            d0 = wave * R::BLOCKS;
-#pragma unroll
-            for (int g = 0; g < R::BLOCKS; ++g)
-#pragma unroll
-                for (int e = 0; e < 4; ++e) {
-                    float v = 0.f;
-#pragma unroll
-                    for (int w = 0; w < 4; ++w) {
-                        const float part = sums[((w * R::BLOCKS * 4 + d0 + g) * 4 + e) * 64 + lane];
-                        v = weight[w] == 0.f ? v : fmaf(weight[w], part, v);
-                    }
-                    acc[0][g >> 2][4 * (g & 3) + e] = v;
-                }
         }
-        if (there) {
-            const bool none = sum == 0.f, one = half == 0 && (!SHARED || wave == 0);
-            const int D = opaque(a.D), first = opaque(8 * d0 + 4 * half);
-            if (a.splits > 1) {
-                const long long part = (long long)split * (a.q_all * a.heads) + slot;
-                if (one) *reinterpret_cast<float2 *>(a.part_ml + 2 * part) = make_float2(top, sum);
-#pragma unroll
-                for (int g = 0; g < (SHARED ? R::BLOCKS : 4 * R::BLOCKS); ++g) {
-                    const int d = first + 8 * g, x = g >> 2, y = 4 * (g & 3);
-                    if (d < D) store4<float, DIRECT>(a.part_o + part * a.D + d, D - d, acc[0][x][y], acc[0][x][y + 1], acc[0][x][y + 2], acc[0][x][y + 3]);
-                }
-            } else {
-                const float scale = none ? 0.f : 1.f / sum;
-                T *const out = reinterpret_cast<T *>(rows_of(a.o, b, a.q_offsets != nullptr, seq.q0 + row, head));
-#pragma unroll
-                for (int g = 0; g < (SHARED ? R::BLOCKS : 4 * R::BLOCKS); ++g) {
-                    const int d = first + 8 * g, x = g >> 2, y = 4 * (g & 3);
-                    if (d < D)
-                        store4<T, DIRECT>(out + d, D - d, acc[0][x][y] * scale, acc[0][x][y + 1] * scale, acc[0][x][y + 2] * scale, acc[0][x][y + 3] * scale);
-                }
-                // (a row that sees no key: a maximum that leaves every weight at zero)
-                if (a.saved && one)
-                    *reinterpret_cast<float2 *>(a.saved + 2 * slot) =
-                        make_float2(none ? __builtin_inff() : top == -__builtin_inff() ? 0.f : top, none ? 0.f : __builtin_amdgcn_logf(sum));
-            }
-        }
-        // (another round of rows uses the tiles again)
-        tile::wait_loads<0>();
-        tile::wait_lds();
-        tile::meet();
-    }
+    } while (SHARED && (++round, id += (int)gridDim.x) < a.workgroups);
 }
 
 // Joins the splits' sums: a workgroup of eight waves for each row and head, each with every eighth split.

@@ -79,8 +79,11 @@ int rcd_attention(const rcd_attention_shape *s, const rcd_heads *q, const rcd_he
         using T = decltype(t);
         constexpr int DP = decltype(dp)::value;
         constexpr bool BIAS = decltype(bias)::value, DIRECT = decltype(way)::value;
-        if (c.shared) return launch(&k_attention<T, DP, true, BIAS, DIRECT>, sequences, each, Forward<T, DP, true>::TILES_BYTES + bias_bytes, a, stream);
-        return launch(&k_attention<T, DP, false, BIAS, DIRECT>, sequences, each, Forward<T, DP, false>::TILES_BYTES + bias_bytes, a, stream);
+        using S = Forward<T, DP, true>;
+        using F = Forward<T, DP, false>;
+        // (a compute unit has room for one workgroup that shares its rows)
+        if (c.shared) return launch(&k_attention<T, DP, true, BIAS, DIRECT>, sequences, each, S::GROUP, 256, S::TILES_BYTES + S::STATS_BYTES + bias_bytes, a, stream);
+        return launch(&k_attention<T, DP, false, BIAS, DIRECT>, sequences, each, F::GROUP, 0, F::TILES_BYTES + bias_bytes, a, stream);
     }));
     if (c.splits > 1) {
         const int64_t slots = a.q_all * s->heads;

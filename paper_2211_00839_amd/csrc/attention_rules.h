@@ -48,18 +48,18 @@ struct Cut {
     int64_t least;      // tiles in a part, unless there are fewer
 };
 
-// The forward call.  width: floats of the bias for each head, 0 without one; a workgroup has room for 8192.
+// The forward call.  width: floats of the bias for each head, 0 without one; a workgroup has room for 7168.
 inline Cut cut_of(int64_t batch, int64_t heads, int64_t group, int64_t longest_q, int64_t longest_k, int64_t q_rows, bool f32, int64_t width)
 {
     Cut c{};
-    c.pack = group > 1 && longest_q * group <= 64 && q_rows * group <= ((int64_t)1 << 29) && width * group <= 8192 ? (int)group : 1;
+    c.pack = group > 1 && longest_q * group <= 64 && q_rows * group <= ((int64_t)1 << 29) && width * group <= 7168 ? (int)group : 1;
     const int64_t across = batch * (heads / c.pack), most = units_of(batch, heads / group) * (group / c.pack);
     c.shared = shared_rows(across, longest_q * c.pack);
     c.tiles = tiles_of(most, longest_q * c.pack, c.shared);
     c.splits = c.least = 1;
     const int64_t groups = c.tiles * across;
     if (groups < 1024 && groups > 0) {
-        const int64_t least = c.shared ? (f32 ? 128 : 512) : 1024;          // keys of a part
+        const int64_t least = c.shared ? (f32 ? 256 : 512) : 1024;          // keys of a part
         // as many parts as fill the compute units once; more where sequences may differ in length, since the longest is what is waited for
         const int64_t wanted = std::max<int64_t>(256 / groups, longest_k / 1024);
         c.splits = std::max<int64_t>(1, std::min({wanted, longest_k / least, 1024 / groups, MOST_SPLITS}));

@@ -33,5 +33,7 @@ __device__ __forceinline__ void meet()
     asm volatile("" ::: "memory");
 }
 
+__device__ __forceinline__ void pin() { __builtin_amdgcn_sched_barrier(0); }
+
 } // namespace tile
 } // namespace enc

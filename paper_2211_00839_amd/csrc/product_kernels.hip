@@ -250,7 +250,6 @@ template <int WT, bool MX> struct Shape {
     static_assert(4 * 32 * TURN_PITCH * 4 <= LDS_BYTES, "the waves' turn-round regions fit where the stages were");
 };
 
-__device__ __forceinline__ void pin() { __builtin_amdgcn_sched_barrier(0); }
 
 typedef short s16x8 __attribute__((ext_vector_type(8)));
 
