@@ -80,9 +80,10 @@ __global__ __launch_bounds__(THREADS, sizeof(T) == 2 && !SHARED ? 2 : 1) void k_
     extern __shared__ __align__(1024) unsigned char lds[];
     const int tid = threadIdx.x, lane = tid & 63, half = lane >> 5, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     Unit unit;
-    if (!unit_of(blockIdx.x, a.batch + (a.clear && a.q_offsets ? 1 : 0), a.kv_heads, a.tiles * a.group, &unit)) return;
-    const int b = unit.sequence, kv_head = unit.kv_head, head = kv_head * a.group + unit.in / a.tiles;
-    const int first_tile = a.tiles - 1 - unit.in % a.tiles;     // (causal: the longest first)
+    if (!unit_of(a, blockIdx.x, a.batch + (a.clear && a.q_offsets ? 1 : 0), &unit)) return;
+    int in_turn;
+    const int b = unit.sequence, kv_head = unit.kv_head, head = kv_head * a.group + divide(unit.in, a.by_tiles, &in_turn);
+    const int first_tile = a.tiles - 1 - in_turn;               // (causal: the longest first)
     if (b == a.batch) {
         clear_rows<T>(a.dq, a.q_offsets, a.batch, a.q_rows, head, a.D, first_tile, a.tiles);
         return;
@@ -358,9 +359,10 @@ template <typename T, int DP, bool SHARED, bool BIAS, bool DIRECT> __global__ __
     extern __shared__ __align__(1024) unsigned char lds[];
     const int tid = threadIdx.x, lane = tid & 63, half = lane >> 5, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     Unit unit;
-    if (!unit_of(blockIdx.x, a.batch + (a.clear && a.k_offsets ? 1 : 0), a.kv_heads, a.tiles * a.splits, &unit)) return;
-    const int b = unit.sequence, kv_head = unit.kv_head, split = unit.in % a.splits;
-    const int first_tile = unit.in / a.splits;                  // (causal: the first keys have the most queries)
+    if (!unit_of(a, blockIdx.x, a.batch + (a.clear && a.k_offsets ? 1 : 0), &unit)) return;
+    int split;
+    const int b = unit.sequence, kv_head = unit.kv_head;
+    const int first_tile = divide(unit.in, a.by_splits, &split);        // (causal: the first keys have the most queries)
     if (b == a.batch) {
         if (split > 0) return;
         clear_rows<T>(a.dk, a.k_offsets, a.batch, a.k_rows, kv_head, a.D, first_tile, a.tiles);
@@ -393,8 +395,8 @@ template <typename T, int DP, bool SHARED, bool BIAS, bool DIRECT> __global__ __
         // this workgroup's tiles, of all the heads' end to end: c0 .. c1 - 1
         const int count = per * a.group, c0 = (int)((long long)count * split / a.splits), c1 = (int)((long long)count * (split + 1) / a.splits);
         const int c_mine = c0 + (SHARED ? wave : 0), c_first = SHARED && BIAS && c1 > c0 ? min(c1, (c0 / per + 1) * per) : c1;      // (its first head's end)
-        auto load = [&](int c, int buf) {
-            const int g = c / per, i0 = (q_from + c - g * per) * W::KV_TILE, head = kv_head * a.group + g;
+        auto load = [&](int g, int t, int buf) {
+            const int i0 = (q_from + t) * W::KV_TILE, head = kv_head * a.group + g;
             const char *pq = rows_of(a.q, b, q_ragged, seq.q0 + i0, head), *pg = rows_of(a.dout, b, q_ragged, seq.q0 + i0, head);
             unsigned char *const to = stages + buf * W::KV_STAGE;
             const unsigned to_addr = stages_addr + buf * W::KV_STAGE;
@@ -421,7 +423,9 @@ template <typename T, int DP, bool SHARED, bool BIAS, bool DIRECT> __global__ __
                 if (lane < W::KV_TILE && lane >= rows) facts[buf * W::FACTS_STAGE + f * W::KV_TILE + lane] = f == 0 ? __builtin_inff() : 0.f;
             }
         };
-        if (W::STAGES == 2 && c_mine < c_first) load(c_mine, 0);
+        // a tile is the t-th of head g; steps go through them without dividing each time
+        int g = per > 0 ? c_mine / per : 0, t = c_mine - g * per;
+        if (W::STAGES == 2 && c_mine < c_first) load(g, t, 0);
         uint4 k[R::STEPS], v[W::TIGHT ? 1 : R::STEPS];
         {
             const char *pk = rows_of(a.k, b, k_ragged, seq.k0 + max(h_key, 0), kv_head), *pv = rows_of(a.v, b, k_ragged, seq.k0 + max(h_key, 0), kv_head);
@@ -531,27 +535,40 @@ template <typename T, int DP, bool SHARED, bool BIAS, bool DIRECT> __global__ __
             tile::meet();
         };
         int buf = 0;
+        auto next = [&](int step) {
+            t += step;
+            while (t >= per) {
+                t -= per;
+                ++g;
+            }
+        };
         if constexpr (SHARED) {
             // with a bias head by head, since it is a head's: end is where this head's tiles end
             int from = c0;
             do {
-                const int end = BIAS && per > 0 ? min(c1, (from / per + 1) * per) : c1;
+                const int head = per > 0 ? from / per : 0, end = BIAS ? min(c1, (head + 1) * per) : c1;
                 if constexpr (BIAS)
-                    if (from < c1 && from / per != table_of) {
+                    if (from < c1 && head != table_of) {
                         tile::wait_lds();
                         tile::meet();
-                        bias_of(from / per);
+                        bias_of(head);
                     }
+                if (from + wave < end) {
+                    g = (from + wave) / per;
+                    t = from + wave - g * per;
+                }
                 for (int c = from + wave; c < end; c += 4, buf ^= W::STAGES - 1) {
-                    const int i_tile = (q_from + c % per) * W::KV_TILE;
+                    const int i_tile = (q_from + t) * W::KV_TILE;
                     tile::wait_lds();
                     if (W::STAGES == 1) {
-                        load(c, 0);
+                        load(g, t, 0);
+                        next(4);
                         tile::wait_loads<0>();
                     } else {
-                        if (c == from + wave && from > c0) load(c, buf);
+                        if (c == from + wave && from > c0) load(g, t, buf);
+                        next(4);
                         if (c + 4 < end) {
-                            load(c + 4, buf ^ 1);
+                            load(g, t, buf ^ 1);
                             if (DIRECT) tile::wait_loads<W::KV_LOADS + W::FACTS>();
                             else tile::wait_loads<0>();
                         } else {
@@ -566,14 +583,15 @@ template <typename T, int DP, bool SHARED, bool BIAS, bool DIRECT> __global__ __
             } while (from < c1);
         } else {
             for (int c = c0; c < c1; ++c, buf ^= 1) {
-                const int g_now = c / per, i_tile = (q_from + c - g_now * per) * W::KV_TILE;
+                const int g_now = g, i_tile = (q_from + t) * W::KV_TILE;
                 tile::wait_loads<0>();
                 clear(i_tile, buf);
                 tile::wait_lds();
                 tile::meet();
                 if constexpr (BIAS)
                     if (g_now != table_of) bias_of(g_now);
-                if (c + 1 < c1) load(c + 1, buf ^ 1);
+                next(1);
+                if (c + 1 < c1) load(g, t, buf ^ 1);
                 choose(i_tile, buf);
             }
         }

@@ -22,6 +22,23 @@ struct Heads {
     long long batch, row, head;         // bytes from sequence to sequence, row to row, head to head
 };
 
+// A divisor and what makes its quotients cheap: x times floor(2^32 / d) over 2^32 is x / d or one less.
+struct Divisor {
+    unsigned d, m;
+    Divisor() = default;
+    explicit Divisor(long long v) : d((unsigned)v), m(v == 1 ? 0xffffffffu : (unsigned)((1ull << 32) / (unsigned long long)v)) {}
+};
+__device__ __forceinline__ int divide(int x, const Divisor &by, int *rest = nullptr)
+{
+    unsigned q = (unsigned)(((unsigned long long)(unsigned)x * by.m) >> 32), r = (unsigned)x - q * by.d;
+    if (r >= by.d) {
+        ++q;
+        r -= by.d;
+    }
+    if (rest) *rest = (int)r;
+    return (int)q;
+}
+
 struct Bias {
     const void *table;                  // null: none
     bool f32, both;                     // both: what follows the query has the table's second half
@@ -45,6 +62,7 @@ struct Args {
     Bias bias;
     int tiles, splits, least;           // least: tiles of a split
     int workgroups;                     // all there are
+    Divisor by_each, by_tiles, by_packs, by_pack, by_kv_heads, by_splits;      // each: workgroups of a unit; packs: of packed heads to a head of k and v
     float *part_o, *part_ml;            // with splits: their sums, and per row maximum and sum
     float *part_k, *part_v;             // gradients of k and v with splits: their sums
     float *part_bias;                   // the table's gradient, a part of each workgroup
@@ -93,22 +111,20 @@ struct Unit {
 };
 inline __host__ __device__ bool goes_round(long long units) { return (units + 7) / 8 * 8 * 5 <= units * 6; }
 // round: how often this workgroup has had one before; it shifts a unit's workgroups by that, so that nobody has only the first parts of theirs.
-__device__ __forceinline__ bool unit_of(int id, int sequences, int kv_heads, int each, Unit *u, int round = 0)
+__device__ __forceinline__ bool unit_of(const Args &a, int id, int sequences, Unit *u, int round = 0)
 {
-    const int units = sequences * kv_heads, turn = id >> 3, die = id & 7;
+    const int units = sequences * a.kv_heads, each = (int)a.by_each.d, turn = id >> 3, die = id & 7;
     int unit;
     if (goes_round(units)) {
-        unit = turn / each * 8 + die;
+        unit = divide(turn, a.by_each, &u->in) * 8 + die;
         if (unit >= units) return false;
-        u->in = (turn + round) % each;
+        if (round) divide(u->in + round, a.by_each, &u->in);
     } else {
-        const int all = units * each, place = die * ((all + 7) / 8) + turn;
-        if (place >= all || turn >= (all + 7) / 8) return false;
-        unit = place / each;
-        u->in = place % each;
+        const int all = units * each, some = (all + 7) >> 3, place = die * some + turn;
+        if (place >= all || turn >= some) return false;
+        unit = divide(place, a.by_each, &u->in);
     }
-    u->kv_head = unit % kv_heads;
-    u->sequence = unit / kv_heads;
+    u->sequence = divide(unit, a.by_kv_heads, &u->kv_head);
     return true;
 }
 inline long long workgroups_of(long long sequences, long long kv_heads, long long each)

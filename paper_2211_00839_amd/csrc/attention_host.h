@@ -168,6 +168,12 @@ template <typename K> int launch(K kernel, int64_t sequences, int64_t each, int 
     const int64_t all = workgroups_of(sequences, a.kv_heads, each);
     if (all > attn_rules::MOST_WORKGROUPS + 8) return RCD_ERR_UNSUPPORTED;
     a.workgroups = (int)all;
+    a.by_each = Divisor(each);
+    a.by_tiles = Divisor(a.tiles);
+    a.by_packs = Divisor(a.group / a.pack);
+    a.by_pack = Divisor(a.pack);
+    a.by_kv_heads = Divisor(a.kv_heads);
+    a.by_splits = Divisor(a.splits);
     hipLaunchKernelGGL(kernel, dim3((unsigned)(most > 0 ? std::min(all, most) : all)), dim3(threads), lds, stream, a);
     ENC_HIP_TRY(hipGetLastError());
     return RCD_OK;

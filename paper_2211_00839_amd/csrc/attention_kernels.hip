@@ -30,15 +30,16 @@ __global__ __launch_bounds__(SHARED && sizeof(T) * DP < 512 ? 512 : 256, SHARED 
     constexpr int GROUPS = SHARED ? 4 * R::BLOCKS / WAVES : 4 * R::BLOCKS;      // of four elements, that a wave stores of its rows
     extern __shared__ __align__(1024) unsigned char lds[];
     const int tid = threadIdx.x, lane = tid & 63, half = lane >> 5, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
-    const int packs = a.group / a.pack;                         // of packed heads that share a head of k and v
-    const int sequences = a.batch + (a.clear ? 1 : 0), each = a.tiles * packs * a.splits;
+    const int sequences = a.batch + (a.clear ? 1 : 0);
     int id = blockIdx.x, round = 0;
     do {
         Unit unit;
-        if (!unit_of(id, sequences, a.kv_heads, each, &unit, round)) continue;
+        if (!unit_of(a, id, sequences, &unit, round)) continue;
         const int b = unit.sequence, kv_head = unit.kv_head;
-        const int first_tile = a.tiles - 1 - unit.in % a.tiles;     // (causal: the longest first)
-        const int head0 = (kv_head * packs + unit.in / a.tiles % packs) * a.pack, split = unit.in / a.tiles / packs;
+        int in_turn, pack;
+        const int split = divide(divide(unit.in, a.by_tiles, &in_turn), a.by_packs, &pack);
+        const int first_tile = a.tiles - 1 - in_turn;           // (causal: the longest first)
+        const int head0 = (kv_head * (int)a.by_packs.d + pack) * a.pack;
         if (b == a.batch) {
             if (split == 0)
                 for (int g = 0; g < a.pack; ++g) clear_rows<T>(a.o, a.q_offsets, a.batch, a.q_rows, head0 + g, a.D, first_tile, a.tiles);
@@ -61,15 +62,16 @@ __global__ __launch_bounds__(SHARED && sizeof(T) * DP < 512 ? 512 : 256, SHARED 
         for (int tile0 = first_tile * ROWS; tile0 < columns; tile0 += a.tiles * ROWS) {
             // ---- the keys that any of this workgroup's rows sees, and its and this wave's tiles of them
             const int mine0 = tile0 + (SHARED ? 0 : wave * 32);
-            const int last = shift + (min(tile0 + ROWS, columns) - 1) / a.pack;                     // the last row's position
+            const int last = shift + divide(min(tile0 + ROWS, columns) - 1, a.by_pack);                     // the last row's position
             const int end = a.causal ? max(0, min(seq.k_len, last + 1)) : seq.k_len;
-            const int lowest = shift + min(mine0, columns - 1) / a.pack, highest = shift + (min(mine0 + 32, columns) - 1) / a.pack;
-            const int tiles = (end + F::TILE - 1) / F::TILE, per = max((tiles + a.splits - 1) / a.splits, min(tiles, a.least));
+            const int lowest = shift + divide(min(mine0, columns - 1), a.by_pack), highest = shift + divide(min(mine0 + 32, columns) - 1, a.by_pack);
+            const int tiles = (end + F::TILE - 1) / F::TILE, per = max(divide(tiles + a.splits - 1, a.by_splits), min(tiles, a.least));
             const int from = split * per, t0 = from + (SHARED ? wave : 0), t1 = min(tiles, from + per), step = SHARED ? WAVES : 1;
             // ---- this wave's rows of q
             const int column = mine0 + (lane & 31), in = min(column, columns - 1);
             const bool there = column < columns;
-            const int row = in / a.pack, head = head0 + in - row * a.pack, pos = shift + row;
+            int in_pack;
+            const int row = divide(in, a.by_pack, &in_pack), head = head0 + in_pack, pos = shift + row;
             const long long slot = (seq.q_first + row) * a.heads + head;
             if (a.splits > 1 && from >= t1 && split > 0) {
                 if (there && half == 0 && (!SHARED || wave == 0))
@@ -263,6 +265,8 @@ __global__ __launch_bounds__(SHARED && sizeof(T) * DP < 512 ? 512 : 256, SHARED 
                 tile::meet();
                 float *const sums = reinterpret_cast<float *>(lds), *const ml = reinterpret_cast<float *>(lds + F::TILES_BYTES);
                 static_assert(WAVES * DP * 32 * 4 <= F::TILES_BYTES, "they fit where the tiles were");
+                const int had = max(1, min(WAVES, t1 - from));       // waves that had keys
+                if (wave < had)
 #pragma unroll
                 for (int d = 0; d < R::BLOCKS; ++d)
 #pragma unroll
@@ -294,6 +298,7 @@ __global__ __launch_bounds__(SHARED && sizeof(T) * DP < 512 ? 512 : 256, SHARED 
                         float v = 0.f;
 #pragma unroll
                         for (int w = 0; w < WAVES; ++w) {
+                            if (w >= had) break;
                             const float part = sums[((w * R::BLOCKS * 4 + d0 + g) * 4 + e) * 64 + lane];
                             v = weight[w] == 0.f ? v : fmaf(weight[w], part, v);
                         }
