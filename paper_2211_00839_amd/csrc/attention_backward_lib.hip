@@ -118,6 +118,7 @@ int rcd_attention_backward(const rcd_attention_shape *s, const rcd_heads *dout, 
     const int reach = reach_of(*s);
     const bool causal = s->causal != 0;
     const Way way = dq_way(*s);
+    const bool uneven = s->q_offsets_dev || s->k_offsets_dev || s->k_lengths_dev;
     if (s->q_rows > 0 && s->batch > 0) {
         Args x = a;
         x.tiles = (int)way.tiles;
@@ -128,8 +129,8 @@ int rcd_attention_backward(const rcd_attention_shape *s, const rcd_heads *dout, 
             using T = decltype(t);
             constexpr int DP = decltype(dp)::value;
             constexpr bool BIAS = decltype(bias)::value, DIRECT = decltype(how)::value;
-            if (way.shared) return launch(&k_attention_dq<T, DP, true, BIAS, DIRECT>, sequences, each, THREADS, 0, dq_lds<Backward<T, DP, true, BIAS>>(BIAS, reach, causal), x, stream);
-            return launch(&k_attention_dq<T, DP, false, BIAS, DIRECT>, sequences, each, THREADS, 0, dq_lds<Backward<T, DP, false, BIAS>>(BIAS, reach, causal), x, stream);
+            if (way.shared) return launch(&k_attention_dq<T, DP, true, BIAS, DIRECT>, sequences, each, THREADS, uneven ? 512 : 0, dq_lds<Backward<T, DP, true, BIAS>>(BIAS, reach, causal), x, stream);
+            return launch(&k_attention_dq<T, DP, false, BIAS, DIRECT>, sequences, each, THREADS, uneven ? 512 : 0, dq_lds<Backward<T, DP, false, BIAS>>(BIAS, reach, causal), x, stream);
         }));
     }
     if (dbias_dev) {
@@ -151,8 +152,8 @@ int rcd_attention_backward(const rcd_attention_shape *s, const rcd_heads *dout, 
             using T = decltype(t);
             constexpr int DP = decltype(dp)::value;
             constexpr bool BIAS = decltype(bias)::value, DIRECT = decltype(how)::value;
-            if (kv.shared) return launch(&k_attention_dkv<T, DP, true, BIAS, DIRECT>, sequences, each, THREADS, 0, dkv_lds<Backward<T, DP, true, BIAS>>(BIAS, reach, causal), a, stream);
-            return launch(&k_attention_dkv<T, DP, false, BIAS, DIRECT>, sequences, each, THREADS, 0, dkv_lds<Backward<T, DP, false, BIAS>>(BIAS, reach, causal), a, stream);
+            if (kv.shared) return launch(&k_attention_dkv<T, DP, true, BIAS, DIRECT>, sequences, each, THREADS, uneven ? 512 : 0, dkv_lds<Backward<T, DP, true, BIAS>>(BIAS, reach, causal), a, stream);
+            return launch(&k_attention_dkv<T, DP, false, BIAS, DIRECT>, sequences, each, THREADS, uneven ? 512 : 0, dkv_lds<Backward<T, DP, false, BIAS>>(BIAS, reach, causal), a, stream);
         }));
         if (kv.parts > 1) {
             const int64_t fours = a.k_all * s->kv_heads * attn_rules::ceil_div(s->d, 4);

@@ -62,7 +62,7 @@ struct Args {
     Bias bias;
     int tiles, splits, least;           // least: tiles of a split
     int workgroups;                     // all there are
-    Divisor by_each, by_tiles, by_packs, by_pack, by_kv_heads, by_splits;      // each: workgroups of a unit; packs: of packed heads to a head of k and v
+    Divisor by_round, by_each, by_tiles, by_packs, by_pack, by_kv_heads, by_splits;      // round: a die's units between a workgroup's and its next; each: workgroups of a unit; packs: of packed heads to a head of k and v
     float *part_o, *part_ml;            // with splits: their sums, and per row maximum and sum
     float *part_k, *part_v;             // gradients of k and v with splits: their sums
     float *part_bias;                   // the table's gradient, a part of each workgroup
@@ -110,15 +110,17 @@ struct Unit {
     int sequence, kv_head, in;          // in: which of the unit's
 };
 inline __host__ __device__ bool goes_round(long long units) { return (units + 7) / 8 * 8 * 5 <= units * 6; }
-// round: how often this workgroup has had one before; it shifts a unit's workgroups by that, so that nobody has only the first parts of theirs.
-__device__ __forceinline__ bool unit_of(const Args &a, int id, int sequences, Unit *u, int round = 0)
+// Workgroups that go on from one to the next have every so many units' the same `in`: a unit's order is shifted by how many such rounds lie before
+// it, so that nobody has only the first parts of theirs.
+__device__ __forceinline__ bool unit_of(const Args &a, int id, int sequences, Unit *u)
 {
     const int units = sequences * a.kv_heads, each = (int)a.by_each.d, turn = id >> 3, die = id & 7;
     int unit;
     if (goes_round(units)) {
-        unit = divide(turn, a.by_each, &u->in) * 8 + die;
+        const int mine = divide(turn, a.by_each, &u->in);
+        unit = mine * 8 + die;
         if (unit >= units) return false;
-        if (round) divide(u->in + round, a.by_each, &u->in);
+        divide(u->in + divide(mine, a.by_round), a.by_each, &u->in);
     } else {
         const int all = units * each, some = (all + 7) >> 3, place = die * some + turn;
         if (place >= all || turn >= some) return false;
@@ -266,13 +268,10 @@ template <typename T, int DP, int ROWS, int LOADERS, bool DIRECT> struct Loader 
 #pragma unroll
                 for (int u = 0; u < N; ++u) bring16(base, off[u % KINDS] + (unsigned)(u * STEP * pitch), lds_addr + (u * LOADERS + wave * 64) * 16);
             } else {
-#pragma unroll 1
-                for (int u = 0; u < N; ++u) {
-                    const int r = min(row + u * STEP, rows - 1);
-                    unsigned o = off[0];
 #pragma unroll
-                    for (int i = 1; i < KINDS; ++i) o = u % KINDS == i ? off[i] : o;
-                    bring16(base, o + (unsigned)((r - row) * pitch), lds_addr + (u * LOADERS + wave * 64) * 16);
+                for (int u = 0; u < N; ++u) {
+                    const int back = min(rows - 1 - row - u * STEP, 0);         // (to the last row there is)
+                    bring16(base, off[u % KINDS] + (unsigned)((u * STEP + back) * pitch), lds_addr + (u * LOADERS + wave * 64) * 16);
                 }
             }
         } else {
@@ -291,7 +290,7 @@ template <typename T, int DP, int ROWS, int LOADERS, bool DIRECT> struct Loader 
     {
         if constexpr (DIRECT) {
             const int lane = threadIdx.x & 63;
-#pragma unroll 1
+#pragma unroll
             for (int u = 0; u < N; ++u)
                 if (row + u * STEP >= rows) *reinterpret_cast<uint4 *>(lds + (u * LOADERS + wave * 64 + lane) * 16) = make_uint4(0, 0, 0, 0);
         }

@@ -6,7 +6,7 @@ namespace attn {
 
 // SHARED false: a workgroup's four waves hold 32 rows of q each and share tiles of TILE keys, the next one on its way while one is used.
 // SHARED true: few rows of q.  Eight waves (four where tiles are large) hold the same 32, and each goes through tiles of 32 keys of its own, every
-// eighth one, without meeting the others; their sums are joined at the end.  A workgroup takes on one row tile and part of the keys after the other.
+// eighth one, without meeting the others; their sums are joined at the end.
 // Either may leave its keys to several workgroups (splits), joined by k_attention_join.
 template <typename T, int DP, bool SHARED> struct Forward {
     using R = Row<T, DP>;
@@ -31,10 +31,10 @@ __global__ __launch_bounds__(SHARED && sizeof(T) * DP < 512 ? 512 : 256, SHARED 
     extern __shared__ __align__(1024) unsigned char lds[];
     const int tid = threadIdx.x, lane = tid & 63, half = lane >> 5, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int sequences = a.batch + (a.clear ? 1 : 0);
-    int id = blockIdx.x, round = 0;
+    int id = blockIdx.x;
     do {
         Unit unit;
-        if (!unit_of(a, id, sequences, &unit, round)) continue;
+        if (!unit_of(a, id, sequences, &unit)) continue;
         const int b = unit.sequence, kv_head = unit.kv_head;
         int in_turn, pack;
         const int split = divide(divide(unit.in, a.by_tiles, &in_turn), a.by_packs, &pack);
@@ -185,7 +185,7 @@ __global__ __launch_bounds__(SHARED && sizeof(T) * DP < 512 ? 512 : 256, SHARED 
                     }
                 sum += (part[0] + part[1]) + (part[2] + part[3]);
                 values_wanted();
-                if (edge && a.causal && any_not_finite<T, DP, F::TILE>(vtile)) {
+                if (a.causal && min(k0 + F::TILE, end) - 1 > lowest && any_not_finite<T, DP, F::TILE>(vtile)) {
                     left_out = true;
                     return;
                 }
@@ -244,7 +244,7 @@ __global__ __launch_bounds__(SHARED && sizeof(T) * DP < 512 ? 512 : 256, SHARED 
 #pragma unroll 1
                     for (int t = t0; t < t1; t += step) {
                         const int j0 = t * F::TILE, count = min(F::TILE, end - j0);
-                        if ((j0 + F::TILE <= end && j0 + F::TILE - 1 <= lowest) || j0 > highest) continue;
+                        if (j0 + count - 1 <= lowest || j0 > highest) continue;
                         if (!any_not_finite<T>(values + (long long)j0 * a.v.row, a.v.row, count, a.D)) continue;
 #pragma unroll 1
                         for (int j = j0; j < j0 + count; ++j) {
@@ -336,7 +336,7 @@ __global__ __launch_bounds__(SHARED && sizeof(T) * DP < 512 ? 512 : 256, SHARED 
             tile::wait_lds();
             tile::meet();
         }
-    } while (SHARED && (++round, id += (int)gridDim.x) < a.workgroups);
+    } while ((id += (int)gridDim.x) < a.workgroups);
 }
 
 // Joins the splits' sums: a workgroup of eight waves for each row and head, each with every eighth split.

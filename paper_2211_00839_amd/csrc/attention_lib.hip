@@ -74,6 +74,7 @@ int rcd_attention(const rcd_attention_shape *s, const rcd_heads *q, const rcd_he
     a.least = (int)c.least;
     const int64_t sequences = s->batch + (a.clear ? 1 : 0), each = c.tiles * (a.group / c.pack) * c.splits;
     const int bias_bytes = width_of(*s) * c.pack * 4;
+    const bool uneven = s->q_offsets_dev || s->k_offsets_dev || s->k_lengths_dev;
     const bool direct = aligned(a.k, s->d, s->dt) && aligned(a.v, s->d, s->dt);
     ENC_TRY(with_variant(s->dt, s->d, s->bias_dev != nullptr, direct, [&](auto t, auto dp, auto bias, auto way) {
         using T = decltype(t);
@@ -83,7 +84,7 @@ int rcd_attention(const rcd_attention_shape *s, const rcd_heads *q, const rcd_he
         using F = Forward<T, DP, false>;
         // (a compute unit has room for one workgroup that shares its rows)
         if (c.shared) return launch(&k_attention<T, DP, true, BIAS, DIRECT>, sequences, each, S::GROUP, 256, S::TILES_BYTES + S::STATS_BYTES + bias_bytes, a, stream);
-        return launch(&k_attention<T, DP, false, BIAS, DIRECT>, sequences, each, F::GROUP, 0, F::TILES_BYTES + bias_bytes, a, stream);
+        return launch(&k_attention<T, DP, false, BIAS, DIRECT>, sequences, each, F::GROUP, uneven ? 256 * (F::TILES_BYTES < 48 * 1024 ? 3 : 2) : 0, F::TILES_BYTES + bias_bytes, a, stream);
     }));
     if (c.splits > 1) {
         const int64_t slots = a.q_all * s->heads;

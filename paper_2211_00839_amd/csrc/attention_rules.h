@@ -58,8 +58,9 @@ inline Cut cut_of(int64_t batch, int64_t heads, int64_t group, int64_t longest_q
     c.tiles = tiles_of(most, longest_q * c.pack, c.shared);
     c.splits = c.least = 1;
     const int64_t groups = c.tiles * across;
-    if (groups < 1024 && groups > 0) {
-        const int64_t least = c.shared ? (f32 ? 256 : 512) : 1024;          // keys of a part
+    // Parts of the keys cost a second launch, some 7 us: not for bf16 where a wave has fewer than eight tiles of them anyway (fp32 takes 3 us a tile).
+    if (groups < 1024 && groups > 0 && longest_k >= (f32 ? 256 : 2048)) {
+        const int64_t least = c.shared ? (f32 ? 128 : 512) : 1024;          // keys of a part
         // as many parts as fill the compute units once; more where sequences may differ in length, since the longest is what is waited for
         const int64_t wanted = std::max<int64_t>(256 / groups, longest_k / 1024);
         c.splits = std::max<int64_t>(1, std::min({wanted, longest_k / least, 1024 / groups, MOST_SPLITS}));
