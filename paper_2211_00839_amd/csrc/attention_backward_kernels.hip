@@ -81,18 +81,44 @@ __global__ __launch_bounds__(THREADS, sizeof(T) == 2 && !SHARED ? 2 : 1) void k_
     const int tid = threadIdx.x, lane = tid & 63, half = lane >> 5, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     int id = blockIdx.x;
     do {
-        Unit unit;
-        if (!unit_of(a, id, a.batch + (a.clear && a.q_offsets ? 1 : 0), &unit)) continue;
-        int in_turn;
-        const int b = unit.sequence, kv_head = unit.kv_head, head = kv_head * a.group + divide(unit.in, a.by_tiles, &in_turn);
-        const int first_tile = a.tiles - 1 - in_turn;               // (causal: the longest first)
-        if (b == a.batch) {
-            clear_rows<T>(a.dq, a.q_offsets, a.batch, a.q_rows, head, a.D, first_tile, a.tiles);
+        int b, head, first_tile, tiles_here = a.tiles;
+        long long part_at;                                      // this workgroup's part of the bias's gradient, of its head's
+        bool nothing = false;
+        if (a.packed) {
+            const int slot = divide(id, a.by_heads, &head);
+            part_at = (long long)head * a.slots + slot;
+            int of;
+            if (tile_of<THREADS, W::ROWS>(a.q_offsets, a.q_rows, a.batch, 1, slot, lds, &b, &first_tile, &of)) {
+                first_tile = of - 1 - first_tile;               // (causal: the longest first)
+                tiles_here = of;
+            } else {
+                // those left over clear the rows that belong to no sequence
+                if (a.clear) clear_rows<T>(a.dq, a.q_offsets, a.batch, a.q_rows, head, a.D, slot - first_tile, a.slots + 1 - first_tile);
+                nothing = true;
+            }
+            if (slot >= a.slots) continue;                      // (the one behind them has no part)
+        } else {
+            Unit unit;
+            if (!unit_of(a, id, a.batch + (a.clear && a.q_offsets ? 1 : 0), &unit)) continue;
+            int in_turn;
+            b = unit.sequence;
+            head = unit.kv_head * a.group + divide(unit.in, a.by_tiles, &in_turn);
+            first_tile = a.tiles - 1 - in_turn;
+            part_at = ((long long)head * a.batch + b) * a.tiles + first_tile;
+            if (b == a.batch) {
+                clear_rows<T>(a.dq, a.q_offsets, a.batch, a.q_rows, head, a.D, first_tile, a.tiles);
+                continue;
+            }
+        }
+        const int kv_head = divide(head, a.by_group);
+        const int buckets = a.bias.buckets, all = a.bias.both ? 2 * buckets : buckets;
+        float *const part = BIAS && a.part_bias ? a.part_bias + part_at * all : nullptr;
+        if (nothing) {
+            if (part)
+                for (int c = tid; c < all; c += THREADS) part[c] = 0.f;
             continue;
         }
         const Sequence seq = sequence(a, b);
-        const int buckets = a.bias.buckets, all = a.bias.both ? 2 * buckets : buckets;
-        float *const part = BIAS && a.part_bias ? a.part_bias + (((long long)head * a.batch + b) * a.tiles + first_tile) * all : nullptr;
         if (first_tile * W::ROWS >= seq.q_len) {
             if (part)
                 for (int c = tid; c < all; c += THREADS) part[c] = 0.f;
@@ -121,7 +147,7 @@ __global__ __launch_bounds__(THREADS, sizeof(T) == 2 && !SHARED ? 2 : 1) void k_
         Loader<T, DP, W::TILE, W::LOADERS, DIRECT> load_k, load_v;
         load_k.init(a.k.row, a.D, SHARED ? lane : tid);
         load_v.init(a.v.row, a.D, SHARED ? lane : tid);
-        for (int tile0 = first_tile * W::ROWS; tile0 < seq.q_len; tile0 += a.tiles * W::ROWS) {
+        for (int tile0 = first_tile * W::ROWS; tile0 < seq.q_len; tile0 += tiles_here * W::ROWS) {
             const int mine0 = tile0 + (SHARED ? 0 : wave * 32), row = mine0 + (lane & 31), h_row = min(row, seq.q_len - 1), pos = shift + h_row;
             const bool there = row < seq.q_len;
             const long long place = seq.q_first + h_row;
@@ -339,7 +365,7 @@ __global__ __launch_bounds__(THREADS, sizeof(T) == 2 && !SHARED ? 2 : 1) void k_
             tile::wait_lds();
             tile::meet();
         }
-    } while ((id += (int)gridDim.x) < a.workgroups);
+    } while (SHARED && (id += (int)gridDim.x) < a.workgroups);
 }
 
 // Adds up the table's gradient over the workgroups that computed parts of it: a workgroup for each bucket and head.
@@ -365,16 +391,32 @@ template <typename T, int DP, bool SHARED, bool BIAS, bool DIRECT> __global__ __
     const int tid = threadIdx.x, lane = tid & 63, half = lane >> 5, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     int id = blockIdx.x;
     do {
-        Unit unit;
-        if (!unit_of(a, id, a.batch + (a.clear && a.k_offsets ? 1 : 0), &unit)) continue;
-        int split;
-        const int b = unit.sequence, kv_head = unit.kv_head;
-        const int first_tile = divide(unit.in, a.by_splits, &split);        // (causal: the first keys have the most queries)
-        if (b == a.batch) {
-            if (split > 0) continue;
-            clear_rows<T>(a.dk, a.k_offsets, a.batch, a.k_rows, kv_head, a.D, first_tile, a.tiles);
-            clear_rows<T>(a.dv, a.k_offsets, a.batch, a.k_rows, kv_head, a.D, first_tile, a.tiles);
-            continue;
+        int b, kv_head, split, first_tile, tiles_here = a.tiles;
+        if (a.packed) {
+            int in;
+            const int slot = divide(id, a.by_heads, &in);
+            kv_head = divide(in, a.by_splits, &split);
+            int of;
+            if (!tile_of<THREADS, W::ROWS>(a.k_offsets, a.k_rows, a.batch, 1, slot, lds, &b, &first_tile, &of)) {
+                if (a.clear && split == 0) {
+                    clear_rows<T>(a.dk, a.k_offsets, a.batch, a.k_rows, kv_head, a.D, slot - first_tile, a.slots + 1 - first_tile);
+                    clear_rows<T>(a.dv, a.k_offsets, a.batch, a.k_rows, kv_head, a.D, slot - first_tile, a.slots + 1 - first_tile);
+                }
+                continue;
+            }
+            tiles_here = of;
+        } else {
+            Unit unit;
+            if (!unit_of(a, id, a.batch + (a.clear && a.k_offsets ? 1 : 0), &unit)) continue;
+            b = unit.sequence;
+            kv_head = unit.kv_head;
+            first_tile = divide(unit.in, a.by_splits, &split);          // (causal: the first keys have the most queries)
+            if (b == a.batch) {
+                if (split > 0) continue;
+                clear_rows<T>(a.dk, a.k_offsets, a.batch, a.k_rows, kv_head, a.D, first_tile, a.tiles);
+                clear_rows<T>(a.dv, a.k_offsets, a.batch, a.k_rows, kv_head, a.D, first_tile, a.tiles);
+                continue;
+            }
         }
         const Sequence seq = sequence(a, b);
         const int shift = seq.k_len - seq.q_len;
@@ -394,7 +436,7 @@ template <typename T, int DP, bool SHARED, bool BIAS, bool DIRECT> __global__ __
         load_q.init(a.q.row, a.D, SHARED ? lane : tid);
         load_g.init(a.dout.row, a.D, SHARED ? lane : tid);
         const int rows = a.clear && !k_ragged ? a.k_rows : seq.k_len;       // rows behind the sequence get zeros
-        for (int tile0 = first_tile * W::ROWS; tile0 < rows; tile0 += a.tiles * W::ROWS) {
+        for (int tile0 = first_tile * W::ROWS; tile0 < rows; tile0 += tiles_here * W::ROWS) {
             const int mine0 = tile0 + (SHARED ? 0 : wave * 32), key = mine0 + (lane & 31), h_key = min(key, seq.k_len - 1);
             const bool there = key < seq.k_len;
             const int q_tiles = (seq.q_len + W::KV_TILE - 1) / W::KV_TILE, q_from = a.causal ? min(max(0, tile0 - shift) / W::KV_TILE, q_tiles) : 0;
@@ -647,7 +689,7 @@ template <typename T, int DP, bool SHARED, bool BIAS, bool DIRECT> __global__ __
             tile::wait_lds();
             tile::meet();
         }
-    } while ((id += (int)gridDim.x) < a.workgroups);
+    } while (SHARED && (id += (int)gridDim.x) < a.workgroups);
 }
 
 // Adds up the splits' parts of dk and dv, four elements to a thread.

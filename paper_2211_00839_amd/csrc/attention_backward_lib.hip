@@ -25,10 +25,12 @@ template <typename W> int dq_lds(bool bias, int reach, bool causal)
 }
 template <typename W> int dkv_lds(bool bias, int reach, bool causal) { return W::KV_TILES_BYTES + W::V_BYTES + W::FACTS_BYTES + (bias ? bias_width(reach, causal) * 4 : 0); }
 
-// The gradient of q: whether the waves share their rows (where there is room for it), and the workgroups for each sequence and head.
+// The gradient of q: whether the waves share their rows (where there is room for it), the workgroups for each sequence and head, and where sequences
+// lie end to end the most tiles that all of them have.
 struct Way {
     bool shared;
-    int64_t tiles;
+    int64_t tiles, packed_tiles;
+    int64_t parts(int64_t batch) const { return std::max(packed_tiles, batch * tiles); }      // (of the bias's gradient, for each head)
 };
 Way dq_way(const rcd_attention_shape &s)
 {
@@ -41,6 +43,7 @@ Way dq_way(const rcd_attention_shape &s)
                        return dq_lds<W>(s.bias_dev != nullptr, reach_of(s), s.causal != 0);
                    }) <= MOST_LDS;
     w.tiles = attn_rules::tiles_of(attn_rules::units_of(s.batch, s.kv_heads) * (s.heads / s.kv_heads), longest, w.shared);
+    w.packed_tiles = s.q_offsets_dev ? s.q_rows / (w.shared ? 32 : 128) + s.batch : 0;
     return w;
 }
 
@@ -66,7 +69,7 @@ size_t backward_bytes(const rcd_attention_shape &s, void *base, Args *a)
     Pieces room(base);
     const size_t plane = up256((size_t)all_rows(s.q_offsets_dev, s.q_rows, s.batch) * s.heads * 4) / 4;
     float *const stats = room.take(4 * plane);
-    float *const parts = s.bias_dev ? room.take((size_t)s.heads * s.batch * dq_way(s).tiles * s.buckets) : nullptr;
+    float *const parts = s.bias_dev ? room.take((size_t)s.heads * dq_way(s).parts(s.batch) * s.buckets) : nullptr;
     const int64_t splits = dkv_way(s).parts;
     const size_t sums = splits > 1 ? (size_t)splits * all_rows(s.k_offsets_dev, s.k_rows, s.batch) * s.kv_heads * s.d : 0;
     float *const part_k = splits > 1 ? room.take(sums) : nullptr, *const part_v = splits > 1 ? room.take(sums) : nullptr;
@@ -118,23 +121,25 @@ int rcd_attention_backward(const rcd_attention_shape *s, const rcd_heads *dout, 
     const int reach = reach_of(*s);
     const bool causal = s->causal != 0;
     const Way way = dq_way(*s);
-    const bool uneven = s->q_offsets_dev || s->k_offsets_dev || s->k_lengths_dev;
+    bool packed = false;            // the gradient of q's workgroups were counted over all sequences' tiles
     if (s->q_rows > 0 && s->batch > 0) {
         Args x = a;
         x.tiles = (int)way.tiles;
         if (!dbias_dev) x.part_bias = nullptr;
-        const int64_t sequences = s->batch + (a.clear && a.q_offsets ? 1 : 0), each = way.tiles * a.group;
+        Grid grid{s->batch + (a.clear && a.q_offsets ? 1 : 0), way.tiles * a.group, way.packed_tiles, s->heads, 0};
         const bool direct = aligned(a.k, s->d, s->dt) && aligned(a.v, s->d, s->dt);
         ENC_TRY(with_variant(s->dt, s->d, s->bias_dev != nullptr, direct, [&](auto t, auto dp, auto bias, auto how) {
             using T = decltype(t);
             constexpr int DP = decltype(dp)::value;
             constexpr bool BIAS = decltype(bias)::value, DIRECT = decltype(how)::value;
-            if (way.shared) return launch(&k_attention_dq<T, DP, true, BIAS, DIRECT>, sequences, each, THREADS, uneven ? 512 : 0, dq_lds<Backward<T, DP, true, BIAS>>(BIAS, reach, causal), x, stream);
-            return launch(&k_attention_dq<T, DP, false, BIAS, DIRECT>, sequences, each, THREADS, uneven ? 512 : 0, dq_lds<Backward<T, DP, false, BIAS>>(BIAS, reach, causal), x, stream);
+            if (!way.shared) return launch(&k_attention_dq<T, DP, false, BIAS, DIRECT>, grid, THREADS, dq_lds<Backward<T, DP, false, BIAS>>(BIAS, reach, causal), x, stream);
+            grid.most = 512;
+            return launch(&k_attention_dq<T, DP, true, BIAS, DIRECT>, grid, THREADS, dq_lds<Backward<T, DP, true, BIAS>>(BIAS, reach, causal), x, stream);
         }));
+        packed = x.packed;
     }
     if (dbias_dev) {
-        const long long count = s->q_rows > 0 ? s->batch * way.tiles : 0;
+        const long long count = s->q_rows > 0 ? packed ? way.packed_tiles : s->batch * way.tiles : 0;
         const dim3 grid((unsigned)(s->buckets * s->heads));
         if (s->bias_dt == RCD_F32)
             hipLaunchKernelGGL((k_bias_gradient<float>), grid, dim3(THREADS), 0, stream, a.part_bias, count, (int)s->buckets, (int)s->heads, (float *)dbias_dev);
@@ -146,14 +151,16 @@ int rcd_attention_backward(const rcd_attention_shape *s, const rcd_heads *dout, 
         const KvWay kv = dkv_way(*s);
         a.tiles = (int)kv.tiles;
         a.splits = (int)kv.parts;
-        const int64_t sequences = s->batch + (a.clear && a.k_offsets ? 1 : 0), each = kv.tiles * kv.parts;
+        Grid grid{s->batch + (a.clear && a.k_offsets ? 1 : 0), kv.tiles * kv.parts, 0, s->kv_heads * kv.parts, 0};
+        if (s->k_offsets_dev) grid.packed_tiles = s->k_rows / (kv.shared ? 32 : 128) + s->batch;
         const bool direct = aligned(a.q, s->d, s->dt) && aligned(a.dout, s->d, s->dt);
         ENC_TRY(with_variant(s->dt, s->d, s->bias_dev != nullptr, direct, [&](auto t, auto dp, auto bias, auto how) {
             using T = decltype(t);
             constexpr int DP = decltype(dp)::value;
             constexpr bool BIAS = decltype(bias)::value, DIRECT = decltype(how)::value;
-            if (kv.shared) return launch(&k_attention_dkv<T, DP, true, BIAS, DIRECT>, sequences, each, THREADS, uneven ? 512 : 0, dkv_lds<Backward<T, DP, true, BIAS>>(BIAS, reach, causal), a, stream);
-            return launch(&k_attention_dkv<T, DP, false, BIAS, DIRECT>, sequences, each, THREADS, uneven ? 512 : 0, dkv_lds<Backward<T, DP, false, BIAS>>(BIAS, reach, causal), a, stream);
+            if (!kv.shared) return launch(&k_attention_dkv<T, DP, false, BIAS, DIRECT>, grid, THREADS, dkv_lds<Backward<T, DP, false, BIAS>>(BIAS, reach, causal), a, stream);
+            grid.most = 512;
+            return launch(&k_attention_dkv<T, DP, true, BIAS, DIRECT>, grid, THREADS, dkv_lds<Backward<T, DP, true, BIAS>>(BIAS, reach, causal), a, stream);
         }));
         if (kv.parts > 1) {
             const int64_t fours = a.k_all * s->kv_heads * attn_rules::ceil_div(s->d, 4);

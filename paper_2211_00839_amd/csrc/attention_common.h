@@ -62,7 +62,9 @@ struct Args {
     Bias bias;
     int tiles, splits, least;           // least: tiles of a split
     int workgroups;                     // all there are
-    Divisor by_round, by_each, by_tiles, by_packs, by_pack, by_kv_heads, by_splits;      // round: a die's units between a workgroup's and its next; each: workgroups of a unit; packs: of packed heads to a head of k and v
+    bool packed;                        // workgroups go to the tiles that there are, whatever sequence they lie in (see tile_of)
+    int slots;                          // packed: most tiles of all sequences together, for each head
+    Divisor by_heads, by_round, by_each, by_tiles, by_packs, by_pack, by_kv_heads, by_splits, by_group;      // round: a die's units between a workgroup's and its next; each: workgroups of a unit; packs: of packed heads to a head of k and v
     float *part_o, *part_ml;            // with splits: their sums, and per row maximum and sum
     float *part_k, *part_v;             // gradients of k and v with splits: their sums
     float *part_bias;                   // the table's gradient, a part of each workgroup
@@ -128,6 +130,60 @@ __device__ __forceinline__ bool unit_of(const Args &a, int id, int sequences, Un
     }
     u->sequence = divide(unit, a.by_kv_heads, &u->kv_head);
     return true;
+}
+// The same where sequences lie end to end by offsets: the slot-th tile of `ROWS` rows (of `pack` heads side by side) of all of them, counted over the
+// sequences, so that no workgroup is started for a tile that a shorter sequence does not have (one that starts for nothing costs as much as a small
+// one's work: 256 samples of 1 to 512 tokens with a bias, 8 heads: forward 130 us).  Every thread of the workgroup has to come along; lds: 64 bytes.
+// False: there are fewer tiles, `tile` is how many.
+template <int THREADS_, int ROWS> __device__ __forceinline__ bool tile_of(const int *offsets, int rows, int batch, int pack, int slot, void *lds, int *sequence, int *tile, int *tiles)
+{
+    constexpr int WAVES = THREADS_ / 64;
+    int *const sums = (int *)lds, *const found = sums + 8;
+    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+    int before = 0;
+    if (tid == 0) found[0] = -1;
+    for (int b0 = 0; b0 < batch; b0 += THREADS_) {
+        const int b = b0 + tid;
+        int mine = 0;
+        if (b < batch) {
+            const int from = min(max(offsets[b], 0), rows), to = min(max(offsets[b + 1], from), rows);
+            mine = ((to - from) * pack + ROWS - 1) / ROWS;
+        }
+        int sum = mine;
+#pragma unroll
+        for (int o = 1; o < 64; o <<= 1) {
+            const int x = __shfl_up(sum, o);
+            sum += lane >= o ? x : 0;
+        }
+        if (lane == 63) sums[wave] = sum;
+        tile::wait_lds();
+        tile::meet();
+        int all = 0;
+#pragma unroll
+        for (int w = 0; w < WAVES; ++w) {
+            const int x = sums[w];
+            sum += w < wave ? x : 0;
+            all += x;
+        }
+        const int first = before + sum - mine;
+        if (slot >= first && slot < first + mine) {
+            found[0] = b;
+            found[1] = slot - first;
+            found[2] = mine;
+        }
+        before += all;
+        tile::wait_lds();
+        tile::meet();
+        if (slot < before) break;
+    }
+    if (batch == 0) tile::meet();
+    const int b = uniform(found[0]);
+    *tile = b < 0 ? uniform(before) : uniform(found[1]);
+    *tiles = uniform(found[2]);
+    *sequence = b;
+    tile::wait_lds();
+    tile::meet();
+    return b >= 0;
 }
 inline long long workgroups_of(long long sequences, long long kv_heads, long long each)
 {

@@ -161,23 +161,32 @@ struct SetUp {
     }
 };
 
-// each: workgroups of a sequence and head of k and v.  most: how many are launched, where each goes on to others; 0: all of them.  (Sequences of
-// different lengths leave many workgroups nothing to do, and one that starts for that costs as much as a small one's work: 256 samples of 1 to 512
-// tokens with a bias, 8 heads, forward 130 us with all of them.)
-template <typename K> int launch(K kernel, int64_t sequences, int64_t each, int threads, int64_t most, int lds, Args &a, hipStream_t stream)
+// How a kernel's workgroups are counted.  each: those of a sequence and head of k and v.  packed_tiles: where sequences lie end to end by offsets, the
+// most tiles that all of them together have (0: not so), and heads: workgroups of one such tile.  most: how many are launched, where each goes on
+// to others; 0: all of them.
+struct Grid {
+    int64_t sequences, each, packed_tiles, heads, most;
+};
+template <typename K> int launch(K kernel, const Grid &g, int threads, int lds, Args &a, hipStream_t stream)
 {
     if (lds > MOST_LDS) return RCD_ERR_UNSUPPORTED;
-    const int64_t all = workgroups_of(sequences, a.kv_heads, each);
+    // (one slot more than there are tiles: its workgroups clear rows that belong to no sequence)
+    const int64_t packed = g.packed_tiles > 0 ? (g.packed_tiles + 1) * g.heads : 0;
+    a.packed = packed > 0 && packed <= attn_rules::MOST_WORKGROUPS;
+    a.slots = a.packed ? (int)g.packed_tiles : 0;
+    const int64_t all = a.packed ? packed : workgroups_of(g.sequences, a.kv_heads, g.each);
     if (all > attn_rules::MOST_WORKGROUPS + 8) return RCD_ERR_UNSUPPORTED;
+    const int64_t launched = g.most > 0 ? std::min(all, g.most) : all;
     a.workgroups = (int)all;
-    const int64_t launched = most > 0 ? std::min(all, most) : all;
-    a.by_round = Divisor(launched < all ? std::max<int64_t>(1, launched / 8 / each) : (int64_t)1 << 30);
-    a.by_each = Divisor(each);
+    a.by_heads = Divisor(std::max<int64_t>(g.heads, 1));
+    a.by_round = Divisor(launched < all ? std::max<int64_t>(1, launched / 8 / g.each) : (int64_t)1 << 30);
+    a.by_each = Divisor(g.each);
     a.by_tiles = Divisor(a.tiles);
     a.by_packs = Divisor(a.group / a.pack);
     a.by_pack = Divisor(a.pack);
     a.by_kv_heads = Divisor(a.kv_heads);
     a.by_splits = Divisor(a.splits);
+    a.by_group = Divisor(a.group);
     hipLaunchKernelGGL(kernel, dim3((unsigned)launched), dim3(threads), lds, stream, a);
     ENC_HIP_TRY(hipGetLastError());
     return RCD_OK;

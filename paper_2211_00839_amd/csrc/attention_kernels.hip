@@ -33,12 +33,31 @@ __global__ __launch_bounds__(SHARED && sizeof(T) * DP < 512 ? 512 : 256, SHARED 
     const int sequences = a.batch + (a.clear ? 1 : 0);
     int id = blockIdx.x;
     do {
-        Unit unit;
-        if (!unit_of(a, id, sequences, &unit)) continue;
-        const int b = unit.sequence, kv_head = unit.kv_head;
-        int in_turn, pack;
-        const int split = divide(divide(unit.in, a.by_tiles, &in_turn), a.by_packs, &pack);
-        const int first_tile = a.tiles - 1 - in_turn;           // (causal: the longest first)
+        int b, kv_head, pack, first_tile, split = 0, tiles_here = a.tiles;
+        if (a.packed) {
+            int head;
+            const int slot = divide(id, a.by_heads, &head);
+            kv_head = divide(head, a.by_packs, &pack);
+            int of;
+            if (!tile_of<F::GROUP, ROWS>(a.q_offsets, a.q_rows, a.batch, a.pack, slot, lds, &b, &first_tile, &of)) {
+                // those left over clear the rows that belong to no sequence
+                if (a.clear)
+                    for (int g = 0; g < a.pack; ++g)
+                        clear_rows<T>(a.o, a.q_offsets, a.batch, a.q_rows, (kv_head * (int)a.by_packs.d + pack) * a.pack + g, a.D, slot - first_tile,
+                                      a.slots + 1 - first_tile);
+                continue;
+            }
+            first_tile = of - 1 - first_tile;                   // (causal: the longest first)
+            tiles_here = of;
+        } else {
+            Unit unit;
+            if (!unit_of(a, id, sequences, &unit)) continue;
+            int in_turn;
+            b = unit.sequence;
+            kv_head = unit.kv_head;
+            split = divide(divide(unit.in, a.by_tiles, &in_turn), a.by_packs, &pack);
+            first_tile = a.tiles - 1 - in_turn;
+        }
         const int head0 = (kv_head * (int)a.by_packs.d + pack) * a.pack;
         if (b == a.batch) {
             if (split == 0)
@@ -59,7 +78,7 @@ __global__ __launch_bounds__(SHARED && sizeof(T) * DP < 512 ? 512 : 256, SHARED 
         Loader<T, DP, F::TILE, F::LOADERS, DIRECT> load_k, load_v;
         load_k.init(a.k.row, a.D, SHARED ? lane : tid);
         load_v.init(a.v.row, a.D, SHARED ? lane : tid);
-        for (int tile0 = first_tile * ROWS; tile0 < columns; tile0 += a.tiles * ROWS) {
+        for (int tile0 = first_tile * ROWS; tile0 < columns; tile0 += tiles_here * ROWS) {
             // ---- the keys that any of this workgroup's rows sees, and its and this wave's tiles of them
             const int mine0 = tile0 + (SHARED ? 0 : wave * 32);
             const int last = shift + divide(min(tile0 + ROWS, columns) - 1, a.by_pack);                     // the last row's position
@@ -336,7 +355,7 @@ __global__ __launch_bounds__(SHARED && sizeof(T) * DP < 512 ? 512 : 256, SHARED 
             tile::wait_lds();
             tile::meet();
         }
-    } while ((id += (int)gridDim.x) < a.workgroups);
+    } while (SHARED && (id += (int)gridDim.x) < a.workgroups);
 }
 
 // Joins the splits' sums: a workgroup of eight waves for each row and head, each with every eighth split.

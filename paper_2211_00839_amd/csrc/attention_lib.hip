@@ -72,9 +72,10 @@ int rcd_attention(const rcd_attention_shape *s, const rcd_heads *q, const rcd_he
     a.tiles = (int)c.tiles;
     a.splits = (int)c.splits;
     a.least = (int)c.least;
-    const int64_t sequences = s->batch + (a.clear ? 1 : 0), each = c.tiles * (a.group / c.pack) * c.splits;
     const int bias_bytes = width_of(*s) * c.pack * 4;
-    const bool uneven = s->q_offsets_dev || s->k_offsets_dev || s->k_lengths_dev;
+    const int64_t rows = c.shared ? 32 : 128;
+    Grid grid{s->batch + (a.clear ? 1 : 0), c.tiles * (a.group / c.pack) * c.splits, 0, s->heads / c.pack, 0};
+    if (s->q_offsets_dev && c.splits == 1) grid.packed_tiles = s->q_rows * c.pack / rows + s->batch;
     const bool direct = aligned(a.k, s->d, s->dt) && aligned(a.v, s->d, s->dt);
     ENC_TRY(with_variant(s->dt, s->d, s->bias_dev != nullptr, direct, [&](auto t, auto dp, auto bias, auto way) {
         using T = decltype(t);
@@ -82,9 +83,9 @@ int rcd_attention(const rcd_attention_shape *s, const rcd_heads *q, const rcd_he
         constexpr bool BIAS = decltype(bias)::value, DIRECT = decltype(way)::value;
         using S = Forward<T, DP, true>;
         using F = Forward<T, DP, false>;
-        // (a compute unit has room for one workgroup that shares its rows)
-        if (c.shared) return launch(&k_attention<T, DP, true, BIAS, DIRECT>, sequences, each, S::GROUP, 256, S::TILES_BYTES + S::STATS_BYTES + bias_bytes, a, stream);
-        return launch(&k_attention<T, DP, false, BIAS, DIRECT>, sequences, each, F::GROUP, uneven ? 256 * (F::TILES_BYTES < 48 * 1024 ? 3 : 2) : 0, F::TILES_BYTES + bias_bytes, a, stream);
+        if (!c.shared) return launch(&k_attention<T, DP, false, BIAS, DIRECT>, grid, F::GROUP, F::TILES_BYTES + bias_bytes, a, stream);
+        grid.most = 256;            // (a compute unit has room for one)
+        return launch(&k_attention<T, DP, true, BIAS, DIRECT>, grid, S::GROUP, S::TILES_BYTES + S::STATS_BYTES + bias_bytes, a, stream);
     }));
     if (c.splits > 1) {
         const int64_t slots = a.q_all * s->heads;
