@@ -88,7 +88,8 @@ __global__ __launch_bounds__(THREADS, sizeof(T) == 2 && !SHARED ? 2 : 1) void k_
             const int slot = divide(id, a.by_heads, &head);
             part_at = (long long)head * a.slots + slot;
             int of;
-            if (tile_of<THREADS, W::ROWS>(a.q_offsets, a.q_rows, a.batch, 1, slot, lds, &b, &first_tile, &of)) {
+            if (tile_of<THREADS>(
+                    a.batch, slot, lds, [&](int b) { return tiles_between(a.q_offsets, a.q_rows, b, 1, W::ROWS); }, &b, &first_tile, &of)) {
                 first_tile = of - 1 - first_tile;               // (causal: the longest first)
                 tiles_here = of;
             } else {
@@ -397,7 +398,8 @@ template <typename T, int DP, bool SHARED, bool BIAS, bool DIRECT> __global__ __
             const int slot = divide(id, a.by_heads, &in);
             kv_head = divide(in, a.by_splits, &split);
             int of;
-            if (!tile_of<THREADS, W::ROWS>(a.k_offsets, a.k_rows, a.batch, 1, slot, lds, &b, &first_tile, &of)) {
+            if (!tile_of<THREADS>(
+                    a.batch, slot, lds, [&](int b) { return tiles_between(a.k_offsets, a.k_rows, b, 1, W::ROWS); }, &b, &first_tile, &of)) {
                 if (a.clear && split == 0) {
                     clear_rows<T>(a.dk, a.k_offsets, a.batch, a.k_rows, kv_head, a.D, slot - first_tile, a.slots + 1 - first_tile);
                     clear_rows<T>(a.dv, a.k_offsets, a.batch, a.k_rows, kv_head, a.D, slot - first_tile, a.slots + 1 - first_tile);

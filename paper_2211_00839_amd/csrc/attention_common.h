@@ -62,7 +62,7 @@ struct Args {
     Bias bias;
     int tiles, splits, least;           // least: tiles of a split
     int workgroups;                     // all there are
-    bool packed;                        // workgroups go to the tiles that there are, whatever sequence they lie in (see tile_of)
+    int packed;                         // workgroups go to the tiles that there are, whatever sequence they lie in (see tile_of): 1 of rows, 2 parts of keys
     int slots;                          // packed: most tiles of all sequences together, for each head
     Divisor by_heads, by_round, by_each, by_tiles, by_packs, by_pack, by_kv_heads, by_splits, by_group;      // round: a die's units between a workgroup's and its next; each: workgroups of a unit; packs: of packed heads to a head of k and v
     float *part_o, *part_ml;            // with splits: their sums, and per row maximum and sum
@@ -135,7 +135,8 @@ __device__ __forceinline__ bool unit_of(const Args &a, int id, int sequences, Un
 // sequences, so that no workgroup is started for a tile that a shorter sequence does not have (one that starts for nothing costs as much as a small
 // one's work: 256 samples of 1 to 512 tokens with a bias, 8 heads: forward 130 us).  Every thread of the workgroup has to come along; lds: 64 bytes.
 // False: there are fewer tiles, `tile` is how many.
-template <int THREADS_, int ROWS> __device__ __forceinline__ bool tile_of(const int *offsets, int rows, int batch, int pack, int slot, void *lds, int *sequence, int *tile, int *tiles)
+// count(b): tiles of sequence b.
+template <int THREADS_, typename Count> __device__ __forceinline__ bool tile_of(int batch, int slot, void *lds, Count count, int *sequence, int *tile, int *tiles)
 {
     constexpr int WAVES = THREADS_ / 64;
     int *const sums = (int *)lds, *const found = sums + 8;
@@ -144,11 +145,7 @@ template <int THREADS_, int ROWS> __device__ __forceinline__ bool tile_of(const 
     if (tid == 0) found[0] = -1;
     for (int b0 = 0; b0 < batch; b0 += THREADS_) {
         const int b = b0 + tid;
-        int mine = 0;
-        if (b < batch) {
-            const int from = min(max(offsets[b], 0), rows), to = min(max(offsets[b + 1], from), rows);
-            mine = ((to - from) * pack + ROWS - 1) / ROWS;
-        }
+        const int mine = b < batch ? count(b) : 0;
         int sum = mine;
 #pragma unroll
         for (int o = 1; o < 64; o <<= 1) {
@@ -185,6 +182,20 @@ template <int THREADS_, int ROWS> __device__ __forceinline__ bool tile_of(const 
     tile::meet();
     return b >= 0;
 }
+// Tiles of `size` rows of sequence b, `pack` heads of a row side by side.
+__device__ __forceinline__ int tiles_between(const int *offsets, int rows, int b, int pack, int size)
+{
+    const int from = min(max(offsets[b], 0), rows), to = min(max(offsets[b + 1], from), rows);
+    return ((to - from) * pack + size - 1) / size;
+}
+// Tiles of keys in one part of them, of a sequence of `tiles`; and how many parts that makes.
+__device__ __forceinline__ int tiles_of_part(const Args &a, int tiles) { return max(divide(tiles + a.splits - 1, a.by_splits), min(tiles, a.least)); }
+__device__ __forceinline__ int parts_of(const Args &a, int tiles)
+{
+    const int per = tiles_of_part(a, tiles);
+    return tiles == 0 ? 1 : (tiles + per - 1) / per;
+}
+__device__ __forceinline__ int keys_of(const Args &a, int b) { return a.k_lengths ? min(max(a.k_lengths[b], 0), a.k_rows) : a.k_rows; }
 inline long long workgroups_of(long long sequences, long long kv_heads, long long each)
 {
     const long long units = sequences * kv_heads;

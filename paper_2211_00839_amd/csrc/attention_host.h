@@ -166,13 +166,14 @@ struct SetUp {
 // to others; 0: all of them.
 struct Grid {
     int64_t sequences, each, packed_tiles, heads, most;
+    bool of_keys = false;       // those are parts of keys
 };
 template <typename K> int launch(K kernel, const Grid &g, int threads, int lds, Args &a, hipStream_t stream)
 {
     if (lds > MOST_LDS) return RCD_ERR_UNSUPPORTED;
     // (one slot more than there are tiles: its workgroups clear rows that belong to no sequence)
     const int64_t packed = g.packed_tiles > 0 ? (g.packed_tiles + 1) * g.heads : 0;
-    a.packed = packed > 0 && packed <= attn_rules::MOST_WORKGROUPS;
+    a.packed = packed > 0 && packed <= attn_rules::MOST_WORKGROUPS ? g.of_keys ? 2 : 1 : 0;
     a.slots = a.packed ? (int)g.packed_tiles : 0;
     const int64_t all = a.packed ? packed : workgroups_of(g.sequences, a.kv_heads, g.each);
     if (all > attn_rules::MOST_WORKGROUPS + 8) return RCD_ERR_UNSUPPORTED;

@@ -34,12 +34,20 @@ __global__ __launch_bounds__(SHARED && sizeof(T) * DP < 512 ? 512 : 256, SHARED 
     int id = blockIdx.x;
     do {
         int b, kv_head, pack, first_tile, split = 0, tiles_here = a.tiles;
-        if (a.packed) {
+        if (SHARED && a.packed == 2) {
+            int in, of;
+            const int slot = divide(id, a.by_heads, &in);
+            if (!tile_of<F::GROUP>(
+                    a.batch, slot, lds, [&](int b) { return parts_of(a, (keys_of(a, b) + F::TILE - 1) / F::TILE); }, &b, &split, &of))
+                break;                                          // (nor are there any behind it)
+            kv_head = divide(divide(in, a.by_tiles, &first_tile), a.by_packs, &pack);
+        } else if (a.packed) {
             int head;
             const int slot = divide(id, a.by_heads, &head);
             kv_head = divide(head, a.by_packs, &pack);
             int of;
-            if (!tile_of<F::GROUP, ROWS>(a.q_offsets, a.q_rows, a.batch, a.pack, slot, lds, &b, &first_tile, &of)) {
+            if (!tile_of<F::GROUP>(
+                    a.batch, slot, lds, [&](int b) { return tiles_between(a.q_offsets, a.q_rows, b, a.pack, ROWS); }, &b, &first_tile, &of)) {
                 // those left over clear the rows that belong to no sequence
                 if (a.clear)
                     for (int g = 0; g < a.pack; ++g)
@@ -84,7 +92,7 @@ __global__ __launch_bounds__(SHARED && sizeof(T) * DP < 512 ? 512 : 256, SHARED 
             const int last = shift + divide(min(tile0 + ROWS, columns) - 1, a.by_pack);                     // the last row's position
             const int end = a.causal ? max(0, min(seq.k_len, last + 1)) : seq.k_len;
             const int lowest = shift + divide(min(mine0, columns - 1), a.by_pack), highest = shift + divide(min(mine0 + 32, columns) - 1, a.by_pack);
-            const int tiles = (end + F::TILE - 1) / F::TILE, per = max(divide(tiles + a.splits - 1, a.by_splits), min(tiles, a.least));
+            const int tiles = (end + F::TILE - 1) / F::TILE, per = tiles_of_part(a, tiles);
             const int from = split * per, t0 = from + (SHARED ? wave : 0), t1 = min(tiles, from + per), step = SHARED ? WAVES : 1;
             // ---- this wave's rows of q
             const int column = mine0 + (lane & 31), in = min(column, columns - 1);
@@ -368,8 +376,11 @@ template <typename T> __global__ __launch_bounds__(JOIN_THREADS) void k_attentio
     const long long row = slot / a.heads;
     const int h = (int)(slot % a.heads);
     if (a.q_offsets && (row < min(max(a.q_offsets[0], 0), a.q_rows) || row >= min(max(a.q_offsets[a.batch], 0), a.q_rows))) return;
+    // (parts behind a sequence's keys were not computed)
+    const int b = a.q_offsets ? 0 : (int)(row / a.q_rows);
+    const int splits = a.packed == 2 ? min(a.splits, parts_of(a, (keys_of(a, b) + 31) / 32)) : a.splits;
     float2 ml = make_float2(-__builtin_inff(), 0.f);
-    if (tid < a.splits) ml = *reinterpret_cast<const float2 *>(a.part_ml + 2 * (tid * slots + slot));
+    if (tid < splits) ml = *reinterpret_cast<const float2 *>(a.part_ml + 2 * (tid * slots + slot));
     float m = ml.x;
 #pragma unroll
     for (int o = 1; o < 64; o <<= 1) m = fmaxf(m, __shfl_xor(m, o));
@@ -388,7 +399,7 @@ template <typename T> __global__ __launch_bounds__(JOIN_THREADS) void k_attentio
     float v0 = 0.f, v1 = 0.f;
     const float *p = a.part_o + slot * a.D + lane;
 #pragma unroll 4
-    for (int s = wave; s < a.splits; s += 8) {
+    for (int s = wave; s < splits; s += 8) {
         const float x = weight[s];
         const float *const from = p + s * slots * a.D;
         const float y0 = lane < a.D ? from[0] : 0.f, y1 = lane + 64 < a.D ? from[64] : 0.f;

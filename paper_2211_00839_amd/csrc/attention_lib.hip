@@ -7,7 +7,7 @@ namespace {
 attn_rules::Cut forward_cut(const rcd_attention_shape &s)
 {
     return attn_rules::cut_of(s.batch, s.heads, s.heads / s.kv_heads, attn_rules::longest_of(s.longest_q, s.q_rows, s.batch, s.q_offsets_dev != nullptr),
-                              attn_rules::longest_of(s.longest_k, s.k_rows, s.batch, s.k_offsets_dev != nullptr), s.q_rows, s.dt == RCD_F32, width_of(s));
+                              attn_rules::longest_of(s.longest_k, s.k_rows, s.batch, s.k_offsets_dev != nullptr), s.q_rows, s.dt == RCD_F32, width_of(s), s.k_lengths_dev != nullptr);
 }
 
 SetUp g_set_up;
@@ -75,7 +75,13 @@ int rcd_attention(const rcd_attention_shape *s, const rcd_heads *q, const rcd_he
     const int bias_bytes = width_of(*s) * c.pack * 4;
     const int64_t rows = c.shared ? 32 : 128;
     Grid grid{s->batch + (a.clear ? 1 : 0), c.tiles * (a.group / c.pack) * c.splits, 0, s->heads / c.pack, 0};
-    if (s->q_offsets_dev && c.splits == 1) grid.packed_tiles = s->q_rows * c.pack / rows + s->batch;
+    if (s->q_offsets_dev && c.splits == 1) {
+        grid.packed_tiles = s->q_rows * c.pack / rows + s->batch;
+    } else if (c.shared && c.splits > 1 && !s->q_offsets_dev && s->k_lengths_dev) {
+        grid.packed_tiles = s->batch * c.splits;
+        grid.heads *= c.tiles;
+        grid.of_keys = true;
+    }
     const bool direct = aligned(a.k, s->d, s->dt) && aligned(a.v, s->d, s->dt);
     ENC_TRY(with_variant(s->dt, s->d, s->bias_dev != nullptr, direct, [&](auto t, auto dp, auto bias, auto way) {
         using T = decltype(t);

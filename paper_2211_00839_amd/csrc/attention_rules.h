@@ -48,8 +48,8 @@ struct Cut {
     int64_t least;      // tiles in a part, unless there are fewer
 };
 
-// The forward call.  width: floats of the bias for each head, 0 without one; a workgroup has room for 7168.
-inline Cut cut_of(int64_t batch, int64_t heads, int64_t group, int64_t longest_q, int64_t longest_k, int64_t q_rows, bool f32, int64_t width)
+// The forward call.  uneven: sequences have lengths of their own.  width: floats of the bias for each head, 0 without one; a workgroup has room for 7168.
+inline Cut cut_of(int64_t batch, int64_t heads, int64_t group, int64_t longest_q, int64_t longest_k, int64_t q_rows, bool f32, int64_t width, bool uneven)
 {
     Cut c{};
     c.pack = group > 1 && longest_q * group <= 64 && q_rows * group <= ((int64_t)1 << 29) && width * group <= 7168 ? (int)group : 1;
@@ -61,9 +61,10 @@ inline Cut cut_of(int64_t batch, int64_t heads, int64_t group, int64_t longest_q
     // Parts of the keys cost a second launch, some 7 us: not for bf16 where a wave has fewer than eight tiles of them anyway (fp32 takes 3 us a tile).
     if (groups < 1024 && groups > 0 && longest_k >= (f32 ? 256 : 2048)) {
         const int64_t least = c.shared ? (f32 ? 128 : 512) : 1024;          // keys of a part
-        // as many parts as fill the compute units once; more where sequences may differ in length, since the longest is what is waited for
+        // as many parts as fill the compute units once; more where sequences differ in length, since the longest is what is waited for (and the short
+        // ones' missing parts cost nothing)
         const int64_t wanted = std::max<int64_t>(256 / groups, longest_k / 1024);
-        c.splits = std::max<int64_t>(1, std::min({wanted, longest_k / least, 1024 / groups, MOST_SPLITS}));
+        c.splits = std::max<int64_t>(1, std::min({wanted, longest_k / least, (uneven ? 4096 : 1024) / groups, MOST_SPLITS}));
         c.least = least / (c.shared ? 32 : 64);
     }
     return c;
