@@ -92,7 +92,8 @@ __global__ __launch_bounds__(SHARED && sizeof(T) * DP < 512 ? 512 : 256, SHARED 
             const int last = shift + divide(min(tile0 + ROWS, columns) - 1, a.by_pack);                     // the last row's position
             const int end = a.causal ? max(0, min(seq.k_len, last + 1)) : seq.k_len;
             const int lowest = shift + divide(min(mine0, columns - 1), a.by_pack), highest = shift + divide(min(mine0 + 32, columns) - 1, a.by_pack);
-            const int tiles = (end + F::TILE - 1) / F::TILE, per = tiles_of_part(a, tiles);
+            // (counted parts are those of all the keys: fewer tiles may make more parts)
+            const int tiles = (end + F::TILE - 1) / F::TILE, per = tiles_of_part(a, a.packed == 2 ? (seq.k_len + F::TILE - 1) / F::TILE : tiles);
             const int from = split * per, t0 = from + (SHARED ? wave : 0), t1 = min(tiles, from + per), step = SHARED ? WAVES : 1;
             // ---- this wave's rows of q
             const int column = mine0 + (lane & 31), in = min(column, columns - 1);

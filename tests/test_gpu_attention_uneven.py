@@ -66,3 +66,17 @@ def test_gradients_in_parts(dtype):
         for b in (None, bias):
             _, _, grads = forward_and_backward(q, k, v, dout, ref.padded(3, lengths), b, 40, causal=causal, k_lengths=at)
             assert not grads.dk[1, 90:].any() and not grads.dv[1, 90:].any() and not grads.dk[2].any()
+
+
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+@pytest.mark.parametrize("length", [9248, 9247, 9300])
+def test_rows_that_see_fewer_tiles_than_their_sequence(length, dtype):
+    """Fewer tiles of keys can make more parts of them than the whole sequence has (288 in parts of 16, 289 in parts of 17): the first queries'
+    last keys count all the same."""
+    gen = generator(length, 14)
+    q, k, v = normal(gen, 1, 64, 1, 64, dtype=dtype), normal(gen, 1, length, 1, 64, dtype=dtype), normal(gen, 1, length, 1, 64, dtype=dtype)
+    k[:, -100:] = q.mean(1, keepdim=True) * 8           # (what is seen last weighs most)
+    at = torch.tensor([length], dtype=torch.int32, device=DEV)
+    out = rcd.attention(q, k, v, causal=True, k_lengths=at)
+    value, bound = ref.attention(q, k, v, None, True, ref.padded(1, [length]))
+    ref.check("out", out, value["out"], bound["out"])
