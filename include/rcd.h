@@ -442,7 +442,7 @@ size_t rcd_gated_linear_backward_workspace_bytes(int64_t M, int64_t F, int64_t K
  * Query i of a sequence of n queries and m keys stands at the position pos_i = i + m - n (its queries are the last n of its keys), whether
  * causal (keys j > pos_i are masked) or not.  A query that sees no key, by its mask, an empty sequence or a bias of -infinity throughout,
  * gets zeros, and no gradient goes through it.  What is masked has no part in anything: a NaN in a key or value that a query does not see
- * does not reach it, and rows behind a sequence are not read.
+ * does not reach it, and rows behind a sequence are not read.  Where a key that is seen holds an infinity, its scores may come out NaN.
  *
  *   dt                  RCD_F32 or RCD_BF16, of every matrix.  Scores, statistics and sums are fp32; for RCD_BF16 p and its gradient are
  *                       rounded to bf16 on their way into the second product (2^-9 of each, what v, k and q have lost already)
@@ -480,7 +480,8 @@ typedef struct {
 
 /*
  *   saved_dev (nullable)  float[2 x rows of q x heads], what the backward call takes: for each row and head the scores' maximum (or a number
- *                         below it by at most 8), in powers of two, and log2 of the sum of the exponentials over it
+ *                         below it by at most 8), in powers of two, and log2 of the sum of the exponentials over it; rows
+ *                         that belong to no sequence are left
  *   clear                 with q_offsets_dev: rows of out that belong to no sequence become zeros; else they are left as they were
  * workspace: rcd_attention_workspace_bytes(shape) bytes.
  */

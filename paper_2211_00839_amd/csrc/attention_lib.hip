@@ -7,7 +7,8 @@ namespace {
 attn_rules::Cut forward_cut(const rcd_attention_shape &s)
 {
     return attn_rules::cut_of(s.batch, s.heads, s.heads / s.kv_heads, attn_rules::longest_of(s.longest_q, s.q_rows, s.batch, s.q_offsets_dev != nullptr),
-                              attn_rules::longest_of(s.longest_k, s.k_rows, s.batch, s.k_offsets_dev != nullptr), s.q_rows, s.dt == RCD_F32, width_of(s), s.k_lengths_dev != nullptr);
+                              attn_rules::longest_of(s.longest_k, s.k_rows, s.batch, s.k_offsets_dev != nullptr), s.q_rows, s.dt == RCD_F32, width_of(s), s.k_lengths_dev != nullptr,
+                              s.q_offsets_dev != nullptr);
 }
 
 SetUp g_set_up;

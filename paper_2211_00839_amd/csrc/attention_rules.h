@@ -49,7 +49,9 @@ struct Cut {
 };
 
 // The forward call.  uneven: sequences have lengths of their own.  width: floats of the bias for each head, 0 without one; a workgroup has room for 7168.
-inline Cut cut_of(int64_t batch, int64_t heads, int64_t group, int64_t longest_q, int64_t longest_k, int64_t q_rows, bool f32, int64_t width, bool uneven)
+// (q_rows: of a sequence, or where they lie end to end, ragged, of all of them.)
+inline Cut cut_of(int64_t batch, int64_t heads, int64_t group, int64_t longest_q, int64_t longest_k, int64_t q_rows, bool f32, int64_t width, bool uneven,
+                  bool ragged = false)
 {
     Cut c{};
     c.pack = group > 1 && longest_q * group <= 64 && q_rows * group <= ((int64_t)1 << 29) && width * group <= 7168 ? (int)group : 1;
@@ -59,7 +61,9 @@ inline Cut cut_of(int64_t batch, int64_t heads, int64_t group, int64_t longest_q
     c.splits = c.least = 1;
     const int64_t groups = c.tiles * across;
     // Parts of the keys cost a second launch, some 7 us: not for bf16 where a wave has fewer than eight tiles of them anyway (fp32 takes 3 us a tile).
-    if (groups < 1024 && groups > 0 && longest_k >= (f32 ? 256 : 2048)) {
+    // Nor where there are far more rows than the lengths say: their parts are memory too.
+    const int64_t slots = (ragged ? q_rows : q_rows * batch) * heads;
+    if (groups < 1024 && groups > 0 && longest_k >= (f32 ? 256 : 2048) && slots <= 1024 * 128) {
         const int64_t least = c.shared ? (f32 ? 128 : 512) : 1024;          // keys of a part
         // as many parts as fill the compute units once; more where sequences differ in length, since the longest is what is waited for (and the short
         // ones' missing parts cost nothing)

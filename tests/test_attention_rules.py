@@ -59,3 +59,10 @@ def test_parts_of_the_gradients(ask):
         assert 1 <= parts <= 8 and (parts == 1 or parts * 256 <= q * g)
         assert parts == 1 or groups < (1024 if uneven else 512)
         assert parts * groups < 2048 or parts == 1
+
+
+def test_rows_of_no_sequence(ask):
+    """A token of one sequence in a tensor with room for many: parts of the keys where their sums stay small, none where they would be
+    as large as all that room."""
+    got = ask("\n".join("put(cut_of(1, 32, 4, 1, 100000, %d, false, 0, false, true).splits);" % rows for rows in (1, 4096, 4097, 2 ** 29)))
+    assert got[0] > 1 and got[1] == got[0] and got[2:] == [1, 1]
