@@ -457,6 +457,7 @@ size_t rcd_gated_linear_backward_workspace_bytes(int64_t M, int64_t F, int64_t K
  *                       1 <= border[0] <= border[1] .. <= 1024 at which the next bucket begins: the bucket of a distance is the number of borders
  *                       that are not above it.  causal: buckets - 1 of them; else buckets / 2 - 1, for keys at or before the query, and
  *                       keys behind it have the second half of the table by the same borders.  2 .. 128 buckets in a direction.
+ *                       No result shares elements with an operand, another result or the workspace.
  *   rcd_heads           a matrix's address (of its element 0) and its strides in elements from sequence to sequence, row to row and head to
  *                       head; an element of a row follows the other.  Rows are less than 2^24 bytes apart.
  */

@@ -75,7 +75,7 @@ def attention(q, k, v, scale=None, causal: bool = False, q_offsets=None, k_offse
     """softmax(scale q k^T + bias) v, scale d^(-1/2) unless given.  k_lengths (int32): how many keys of each sequence there are.
     longest_q, longest_k: the longest sequence, where the caller knows it (for speed alone).  bias (buckets, heads), float32 or
     of q's type: what position_borders() makes of max_distance says which bucket a pair has.  A query that sees no key gets zeros;
-    rows outside every sequence become zeros, in `out` they are left.  want_saved: (out, saved), what attention_backward takes."""
+    rows outside every sequence become zeros, in `out` they are left; `out` shares no elements with the rest.  want_saved: (out, saved), what attention_backward takes."""
     result, saved = _lib().attention(q, k, v, q_offsets, k_offsets, k_lengths, longest_q, longest_k, scale, causal, bias,
                                      _packed(bias, max_distance, causal), out, want_saved, workspace, _stream(q))
     return (result, saved) if want_saved else result

@@ -588,6 +588,12 @@ Made made(const char *name, PyObject *given, const Rows &as, const Call &c)
     if (!m.t.is_inference()) m.t.unsafeGetTensorImpl()->bump_version();
     return m;
 }
+// A result that begins where an operand or another result does would be read while it is written.  (That they share no element further on is the
+// caller's part: results may well lie between operands' rows.)
+template <typename... T> void apart(const char *name, const Made &m, const T &...others)
+{
+    if (m.t.numel() > 0 && ((others.h.p == m.h.p) || ...)) refuse(std::string(name) + " is an operand or another result too");
+}
 Room room(PyObject *o, size_t need, const at::Tensor &like)
 {
     Matrix m;
@@ -602,6 +608,7 @@ PyObject *attention(PyObject *, PyObject *const *a, Py_ssize_t n)
     expect(n, 16);
     const Call c = attention_call(a[0], a[1], a[2], a + 3);
     const Made out = made("out", a[12], c.q, c);
+    apart("out", out, c.q, c.k, c.v);
     at::Tensor saved;
     if (truth(a[13])) {
         auto sizes = c.q.t->sizes().vec();
@@ -636,6 +643,9 @@ PyObject *attention_backward(PyObject *, PyObject *const *a, Py_ssize_t n)
     const int given = (a[15] != Py_None) + (a[16] != Py_None) + (a[17] != Py_None);
     if (given != 0 && given != 3) refuse("grads must be (dq, dk, dv)");
     const Made dq = made("dq", a[15], c.q, c), dk = made("dk", a[16], c.k, c), dv = made("dv", a[17], c.v, c);
+    apart("dq", dq, dk, dv, dout, c.q, c.k, c.v, out);
+    apart("dk", dk, dv, dout, c.q, c.k, c.v, out);
+    apart("dv", dv, dout, c.q, c.k, c.v, out);
     at::Tensor dbias;
     if (c.bias && truth(a[18])) dbias = at::empty(c.bias->sizes(), c.bias->options().requires_grad(false));
     const Room ws = room(a[19], rcd_attention_backward_workspace_bytes(&c.s), *c.q.t);

@@ -187,6 +187,10 @@ def test_refusals():
     refused(rcd.attention_backward, q[:, :4], q, k, k, out, saved)
     refused(rcd.attention_backward, q, q, k, k, out, saved, grads=(torch.empty_like(q), None, torch.empty_like(k)))
     refused(rcd.attention_backward, q, q, k, k, out, saved, workspace=torch.empty(16, dtype=torch.uint8, device=DEV))
+    refused(rcd.attention, q, q, q, out=q)
+    refused(rcd.attention_backward, q, q, k, k, out, saved, grads=(out, torch.empty_like(k), torch.empty_like(k)))
+    both = torch.empty_like(k)
+    refused(rcd.attention_backward, q, q, k, k, out, saved, grads=(torch.empty_like(q), both, both))
     refused(rcd.attention, q.clone().requires_grad_(), k, k)
     with torch.no_grad():
         rcd.attention(q.clone().requires_grad_(), k, k)
