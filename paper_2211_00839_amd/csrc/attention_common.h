@@ -133,7 +133,7 @@ __device__ __forceinline__ bool unit_of(const Args &a, int id, int sequences, Un
 }
 // The same where sequences lie end to end by offsets: the slot-th tile of `ROWS` rows (of `pack` heads side by side) of all of them, counted over the
 // sequences, so that no workgroup is started for a tile that a shorter sequence does not have (one that starts for nothing costs as much as a small
-// one's work: 256 samples of 1 to 512 tokens with a bias, 8 heads: forward 130 us).  Every thread of the workgroup has to come along; lds: 64 bytes.
+// one's work: 256 samples of 1 to 512 tokens with a bias, 8 heads: forward 129 us, now 72).  Every thread of the workgroup has to come along; lds: 64 bytes.
 // False: there are fewer tiles, `tile` is how many.
 // count(b): tiles of sequence b.
 template <int THREADS_, typename Count> __device__ __forceinline__ bool tile_of(int batch, int slot, void *lds, Count count, int *sequence, int *tile, int *tiles)

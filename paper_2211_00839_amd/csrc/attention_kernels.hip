@@ -1,4 +1,9 @@
 // Attention forward: out = softmax(scale Q K^T + bias) V, one pass over the keys with the running maximum and sum of the softmax.
+//
+// Bounds: long sequences by the matrix cores (4 d multiplies and adds a pair) beside one exponential a pair, few rows by reading k and v once, a single
+// short one by latency.  Measured, bf16: 2 x 8192 tokens, 16 heads of 128: 1.07 ms, 1030 TFLOP/s (64 rows to a wave spilled: 381; three waves to a SIMD
+// with tiles of 32 keys were slower); heads of 64, 4 x 2048 x 16 with a bias: 118 us, 580 TFLOP/s; one token over 100 003 keys, 16 heads on 2 of
+// 128: 25 us, 4.1 TB/s, and 6 for the join; one token over 300 keys: 9.6 us.
 #pragma once
 #include "attention_common.h"
 
