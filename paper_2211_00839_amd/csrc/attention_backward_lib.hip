@@ -36,7 +36,7 @@ Way dq_way(const rcd_attention_shape &s)
 {
     const int64_t longest = attn_rules::longest_of(s.longest_q, s.q_rows, s.batch, s.q_offsets_dev != nullptr);
     Way w;
-    w.shared = attn_rules::shared_rows(s.batch * s.heads, longest);
+    w.shared = attn_rules::shared_rows(s.batch * s.heads, longest, attn_rules::FEW_WORKGROUPS);
     if (w.shared)
         w.shared = with_variant(s.dt, s.d, s.bias_dev != nullptr, true, [&](auto t, auto dp, auto bias, auto) {
                        using W = Backward<decltype(t), decltype(dp)::value, true, decltype(bias)::value>;
@@ -57,7 +57,7 @@ KvWay dkv_way(const rcd_attention_shape &s)
     const int64_t longest = attn_rules::longest_of(s.longest_k, s.k_rows, s.batch, s.k_offsets_dev != nullptr);
     const int64_t longest_q = attn_rules::longest_of(s.longest_q, s.q_rows, s.batch, s.q_offsets_dev != nullptr);
     KvWay w;
-    w.shared = attn_rules::shared_rows(s.batch * s.kv_heads, longest);
+    w.shared = attn_rules::shared_rows(s.batch * s.kv_heads, longest, attn_rules::FEW_WORKGROUPS);
     w.tiles = attn_rules::tiles_of(attn_rules::units_of(s.batch, s.kv_heads), longest, w.shared);
     const bool uneven = s.causal || s.q_offsets_dev || s.k_offsets_dev || s.k_lengths_dev;
     w.parts = attn_rules::parts_of(w.tiles * s.kv_heads * s.batch, uneven, longest_q, s.heads / s.kv_heads);

@@ -372,6 +372,33 @@ __global__ __launch_bounds__(SHARED && sizeof(T) * DP < 512 ? 512 : 256, SHARED 
     } while (SHARED && (id += (int)gridDim.x) < a.workgroups);
 }
 
+// What the joins share: a row and head's place, and how many parts it has; false: it belongs to no sequence.
+struct Joined {
+    long long row;
+    int head, splits;
+};
+__device__ __forceinline__ bool joined(const Args &a, long long slot, Joined *j)
+{
+    j->row = slot / a.heads;
+    j->head = (int)(slot % a.heads);
+    if (a.q_offsets && (j->row < min(max(a.q_offsets[0], 0), a.q_rows) || j->row >= min(max(a.q_offsets[a.batch], 0), a.q_rows))) return false;
+    // (parts behind a sequence's keys were not computed)
+    const int b = a.q_offsets ? 0 : (int)(j->row / a.q_rows);
+    j->splits = a.packed == 2 ? min(a.splits, parts_of(a, (keys_of(a, b) + 31) / 32)) : a.splits;
+    return true;
+}
+template <typename T> __device__ __forceinline__ T *joined_row(const Args &a, const Joined &j)
+{
+    const long long in = a.q_offsets ? j.row : j.row % a.q_rows;
+    return reinterpret_cast<T *>(a.o.p + (a.q_offsets ? 0 : j.row / a.q_rows * a.o.batch) + in * a.o.row + (long long)j.head * a.o.head);
+}
+__device__ __forceinline__ void save_joined(const Args &a, long long slot, float most, float total)
+{
+    const bool none = total == 0.f;
+    const float t = most == -__builtin_inff() ? 0.f : most;
+    *reinterpret_cast<float2 *>(a.saved + 2 * slot) = make_float2(none ? __builtin_inff() : t, none ? 0.f : __builtin_amdgcn_logf(total));
+}
+
 // Joins the splits' sums: a workgroup of eight waves for each row and head, each with every eighth split.
 constexpr int JOIN_THREADS = 512, MOST_SPLITS = 512;
 template <typename T> __global__ __launch_bounds__(JOIN_THREADS) void k_attention_join(Args a)
@@ -379,12 +406,9 @@ template <typename T> __global__ __launch_bounds__(JOIN_THREADS) void k_attentio
     __shared__ float weight[MOST_SPLITS], most[8], sums[8][128], totals[8];
     const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
     const long long slots = a.q_all * a.heads, slot = blockIdx.x;
-    const long long row = slot / a.heads;
-    const int h = (int)(slot % a.heads);
-    if (a.q_offsets && (row < min(max(a.q_offsets[0], 0), a.q_rows) || row >= min(max(a.q_offsets[a.batch], 0), a.q_rows))) return;
-    // (parts behind a sequence's keys were not computed)
-    const int b = a.q_offsets ? 0 : (int)(row / a.q_rows);
-    const int splits = a.packed == 2 ? min(a.splits, parts_of(a, (keys_of(a, b) + 31) / 32)) : a.splits;
+    Joined j;
+    if (!joined(a, slot, &j)) return;
+    const int splits = j.splits;
     float2 ml = make_float2(-__builtin_inff(), 0.f);
     if (tid < splits) ml = *reinterpret_cast<const float2 *>(a.part_ml + 2 * (tid * slots + slot));
     float m = ml.x;
@@ -418,19 +442,47 @@ template <typename T> __global__ __launch_bounds__(JOIN_THREADS) void k_attentio
     total = 0.f;
 #pragma unroll
     for (int i = 0; i < 8; ++i) total += totals[i];
-    const long long in = a.q_offsets ? row : row % a.q_rows;
-    T *const out = reinterpret_cast<T *>(a.o.p + (a.q_offsets ? 0 : row / a.q_rows * a.o.batch) + in * a.o.row + (long long)h * a.o.head);
+    T *const out = joined_row<T>(a, j);
     if (tid < a.D) {
         float v = 0.f;
 #pragma unroll
         for (int i = 0; i < 8; ++i) v += sums[i][tid];
         out[tid] = (T)(total == 0.f ? 0.f : v / total);
     }
-    if (a.saved && tid == 0) {
-        const bool none = total == 0.f;
-        const float t = m == -__builtin_inff() ? 0.f : m;
-        *reinterpret_cast<float2 *>(a.saved + 2 * slot) = make_float2(none ? __builtin_inff() : t, none ? 0.f : __builtin_amdgcn_logf(total));
+    if (a.saved && tid == 0) save_joined(a, slot, m, total);
+}
+
+// The same with many rows and up to 64 splits: a wave for each row and head.  Bound by reading the parts.
+template <typename T> __global__ __launch_bounds__(JOIN_THREADS) void k_attention_join_many(Args a)
+{
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const long long slots = a.q_all * a.heads, slot = (long long)blockIdx.x * (JOIN_THREADS / 64) + wave;
+    Joined j;
+    if (slot >= slots || !joined(a, slot, &j)) return;
+    float2 ml = make_float2(-__builtin_inff(), 0.f);
+    if (lane < j.splits) ml = *reinterpret_cast<const float2 *>(a.part_ml + 2 * (lane * slots + slot));
+    float m = ml.x;
+#pragma unroll
+    for (int o = 1; o < 64; o <<= 1) m = fmaxf(m, __shfl_xor(m, o));
+    // (a split without keys has no part in it; one whose scores are all NaN has)
+    const float w = ml.y == 0.f ? 0.f : ml.x == m ? 1.f : __builtin_amdgcn_exp2f(ml.x - m);
+    float total = ml.y == 0.f ? 0.f : w * ml.y;
+#pragma unroll
+    for (int o = 1; o < 64; o <<= 1) total += __shfl_xor(total, o);
+    float v0 = 0.f, v1 = 0.f;
+    const float *p = a.part_o + slot * a.D + lane;
+#pragma unroll 4
+    for (int s = 0; s < j.splits; ++s) {
+        const float x = __shfl(w, s);
+        const float *const from = p + s * slots * a.D;
+        const float y0 = lane < a.D ? from[0] : 0.f, y1 = lane + 64 < a.D ? from[64] : 0.f;
+        v0 = x == 0.f ? v0 : fmaf(x, y0, v0);
+        v1 = x == 0.f ? v1 : fmaf(x, y1, v1);
     }
+    T *const out = joined_row<T>(a, j);
+    if (lane < a.D) out[lane] = (T)(total == 0.f ? 0.f : v0 / total);
+    if (lane + 64 < a.D) out[lane + 64] = (T)(total == 0.f ? 0.f : v1 / total);
+    if (a.saved && lane == 0) save_joined(a, slot, m, total);
 }
 
 } // namespace attn

@@ -96,8 +96,15 @@ int rcd_attention(const rcd_attention_shape *s, const rcd_heads *q, const rcd_he
     }));
     if (c.splits > 1) {
         const int64_t slots = a.q_all * s->heads;
-        if (s->dt == RCD_F32) hipLaunchKernelGGL((k_attention_join<float>), dim3((unsigned)slots), dim3(JOIN_THREADS), 0, stream, a);
-        else hipLaunchKernelGGL((k_attention_join<__bf16>), dim3((unsigned)slots), dim3(JOIN_THREADS), 0, stream, a);
+        const bool many = attn_rules::many_joins(slots, c.splits);
+        const dim3 joins((unsigned)(many ? attn_rules::ceil_div(slots, JOIN_THREADS / 64) : slots));
+        if (s->dt == RCD_F32) {
+            if (many) hipLaunchKernelGGL((k_attention_join_many<float>), joins, dim3(JOIN_THREADS), 0, stream, a);
+            else hipLaunchKernelGGL((k_attention_join<float>), joins, dim3(JOIN_THREADS), 0, stream, a);
+        } else {
+            if (many) hipLaunchKernelGGL((k_attention_join_many<__bf16>), joins, dim3(JOIN_THREADS), 0, stream, a);
+            else hipLaunchKernelGGL((k_attention_join<__bf16>), joins, dim3(JOIN_THREADS), 0, stream, a);
+        }
         ENC_HIP_TRY(hipGetLastError());
     }
     return RCD_OK;

@@ -18,8 +18,11 @@ inline int64_t longest_of(int64_t said, int64_t rows, int64_t batch, bool ragged
     return std::min(rows, said > 0 ? said : 4 * ceil_div(rows, std::max<int64_t>(batch, 1)));
 }
 
-// Few rows, or few workgroups of 128 rows for each sequence and head: then the waves share 32 rows and divide what those go along.
-inline bool shared_rows(int64_t across, int64_t longest) { return longest <= 64 || across * ceil_div(longest, 128) < 256; }
+// Few rows, or few workgroups of 128 rows for each sequence and head: then the waves share 32 rows and divide what those go along.  Where the two meet was
+// measured with 1024 rows of 64, us shared / 128 rows, by workgroups of 128 rows: bf16 forward 64: 14.0 / 20.9, 128: 23.5 / 20.9, 240: 41.8 / 22.1; gradients
+// 128: 54 / 58, 192: 76 / 74, 240: 96 / 78; fp32 forward 128: 52 / 80, 192: 78 / 80, 240: 103 / 83; gradients 192: 256 / 281, 240: 340 / 300.
+constexpr int64_t FEW_WORKGROUPS = 200, FEW_WORKGROUPS_BF16_FORWARD = 112;
+inline bool shared_rows(int64_t across, int64_t longest, int64_t few) { return longest <= 64 || across * ceil_div(longest, 128) < few; }
 
 // Workgroups for each sequence and head; a kernel goes on to the rows that these leave.
 inline int64_t tiles_of(int64_t across, int64_t longest, bool shared)
@@ -56,7 +59,7 @@ inline Cut cut_of(int64_t batch, int64_t heads, int64_t group, int64_t longest_q
     Cut c{};
     c.pack = group > 1 && longest_q * group <= 64 && q_rows * group <= ((int64_t)1 << 29) && width * group <= 7168 ? (int)group : 1;
     const int64_t across = batch * (heads / c.pack), most = units_of(batch, heads / group) * (group / c.pack);
-    c.shared = shared_rows(across, longest_q * c.pack);
+    c.shared = shared_rows(across, longest_q * c.pack, f32 ? FEW_WORKGROUPS : FEW_WORKGROUPS_BF16_FORWARD);
     c.tiles = tiles_of(most, longest_q * c.pack, c.shared);
     c.splits = c.least = 1;
     const int64_t groups = c.tiles * across;
@@ -67,11 +70,14 @@ inline Cut cut_of(int64_t batch, int64_t heads, int64_t group, int64_t longest_q
         const int64_t least = c.shared ? (f32 ? 128 : 512) : 1024;          // keys of a part
         // as many parts as fill the compute units once; more where sequences differ in length, since the longest is what is waited for (and the short
         // ones' missing parts cost nothing)
-        const int64_t wanted = std::max<int64_t>(256 / groups, longest_k / 1024);
+        const int64_t wanted = std::max<int64_t>(256 / groups, uneven ? longest_k / 1024 : 0);
         c.splits = std::max<int64_t>(1, std::min({wanted, longest_k / least, (uneven ? 4096 : 1024) / groups, MOST_SPLITS}));
         c.least = least / (c.shared ? 32 : 64);
     }
     return c;
 }
+
+// Sums of parts are joined by a wave for each row and head where there are many, by a workgroup's eight where there are few and parts may be.
+inline bool many_joins(int64_t slots, int64_t splits) { return slots >= 4096 && splits <= 64; }
 
 } // namespace attn_rules

@@ -66,3 +66,11 @@ def test_rows_of_no_sequence(ask):
     as large as all that room."""
     got = ask("\n".join("put(cut_of(1, 32, 4, 1, 100000, %d, false, 0, false, true).splits);" % rows for rows in (1, 4096, 4097, 2 ** 29)))
     assert got[0] > 1 and got[1] == got[0] and got[2:] == [1, 1]
+
+
+def test_even_calls_have_no_more_parts_than_fill_the_device(ask):
+    cases = [(b, h, q, k, f) for b in (1, 4) for h in (1, 8, 24, 64) for q in (128, 2048, 8192) for k in (2048, 30000) for f in (0, 1)]
+    got = iter(ask("\n".join("{ const Cut c = cut_of(%d, %d, 1, %d, %d, %d, %d, 0, false); put(c.tiles); put(c.splits); }" % (b, h, q, k, q, f) for b, h, q, k, f in cases)))
+    for b, h, q, k, f in cases:
+        tiles, splits = int(next(got)), int(next(got))
+        assert splits == 1 or tiles * b * h * splits <= 256, (b, h, q, k, f)

@@ -80,3 +80,15 @@ def test_rows_that_see_fewer_tiles_than_their_sequence(length, dtype):
     out = rcd.attention(q, k, v, causal=True, k_lengths=at)
     value, bound = ref.attention(q, k, v, None, True, ref.padded(1, [length]))
     ref.check("out", out, value["out"], bound["out"])
+
+
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+@pytest.mark.parametrize("causal", [False, True])
+def test_many_rows_over_parts_of_the_keys(causal, dtype):
+    gen = generator(causal, 15)
+    for batch, n, heads, kv, d, lengths in ((1, 4096, 1, 1, 64, [4200]), (2, 1100, 2, 1, 72, [5000, 1500]), (3, 700, 2, 2, 33, [2300, 0, 700])):
+        m = max(lengths)
+        q, dout = normal(gen, batch, n, heads, d, dtype=dtype), normal(gen, batch, n, heads, d, dtype=dtype)
+        k, v = normal(gen, batch, m, kv, d, dtype=dtype), normal(gen, batch, m, kv, d, dtype=dtype)
+        how = {} if batch == 1 else dict(k_lengths=torch.tensor(lengths, dtype=torch.int32, device=DEV))
+        forward_and_backward(q, k, v, dout, ref.padded(batch, lengths), causal=causal, **how)
