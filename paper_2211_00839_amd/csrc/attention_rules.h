@@ -59,7 +59,9 @@ inline Cut cut_of(int64_t batch, int64_t heads, int64_t group, int64_t longest_q
     Cut c{};
     c.pack = group > 1 && longest_q * group <= 64 && q_rows * group <= ((int64_t)1 << 29) && width * group <= 7168 ? (int)group : 1;
     const int64_t across = batch * (heads / c.pack), most = units_of(batch, heads / group) * (group / c.pack);
-    c.shared = shared_rows(across, longest_q * c.pack, f32 ? FEW_WORKGROUPS : FEW_WORKGROUPS_BF16_FORWARD);
+    // (fp32: a compute unit has room for one workgroup of 128 rows, so that 257 of them take as long as 512: 320 of the above 160 us, shared 127; 512: 162, 200)
+    const int64_t rounds = ceil_div(across * ceil_div(longest_q * c.pack, 128), 256);
+    c.shared = shared_rows(across, longest_q * c.pack, f32 ? FEW_WORKGROUPS * std::max<int64_t>(rounds, 1) : FEW_WORKGROUPS_BF16_FORWARD);
     c.tiles = tiles_of(most, longest_q * c.pack, c.shared);
     c.splits = c.least = 1;
     const int64_t groups = c.tiles * across;
