@@ -79,7 +79,8 @@ inline Cut cut_of(int64_t batch, int64_t heads, int64_t group, int64_t longest_q
     return c;
 }
 
-// Sums of parts are joined by a wave for each row and head where there are many, by a workgroup's eight where there are few and parts may be.
-inline bool many_joins(int64_t slots, int64_t splits) { return slots >= 4096 && splits <= 64; }
+// Sums of parts are joined by a wave for each row and head where there are many, by a workgroup's eight where there are few and parts may be many.
+// Whole calls over caches of 4096 keys of 128, us by workgroups / by waves: 1024 rows and heads 65.0 / 64.3, 4096: 50.3 / 40.1, 16384: 156 / 115.
+inline bool many_joins(int64_t slots, int64_t splits) { return slots >= 2048 && splits <= 64; }
 
 } // namespace attn_rules
