@@ -494,6 +494,7 @@ size_t rcd_attention_workspace_bytes(const rcd_attention_shape *shape);
  * Its gradients, with the probabilities computed again.  With delta_i = dout_i out_i and ds_ij = p_ij (dout_i v_j - delta_i):
  *     dq_i = scale sum_j ds_ij k_j,   dk_j = scale sum_i ds_ij q_i,   dv_j = sum_i p_ij dout_i,   dbias[c] = sum of ds_ij over bucket c's pairs
  * dk and dv are sums over the query heads that share their head, dbias over everything; all in a fixed order.
+ * A query that sees one key alone, by its mask or since its sequence has one, has a weight of 1 whatever its score is: its ds is exactly zero.
  *   out, saved_dev        of the forward call
  *   dbias_dev (nullable)  buckets x heads of bias_dt, contiguous
  *   clear                 rows of dq, dk and dv that belong to no sequence, and rows behind k_lengths_dev, become zeros; else they are

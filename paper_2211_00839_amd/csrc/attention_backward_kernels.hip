@@ -244,7 +244,9 @@ __global__ __launch_bounds__(THREADS, sizeof(T) == 2 && !SHARED ? 2 : 1) void k_
                     for (int i = 0; i < 16; ++i)
                         ds[0][i] = __builtin_amdgcn_exp2f(BIAS ? (s[i] - top) - log_sum : fmaf(s[i], a.scale2, -both)) * (dp[i] - delta);
                     if (edge) {
-                        const int most = min(a.causal ? pos : end - 1, end - 1) - j0;
+                        // (a row that sees one key alone has p = 1 and dp = delta: nothing, where the two roundings of one number would leave a residue;
+                        // such a row's key is the first, which lies in a tile of this kind)
+                        const int seen = min(a.causal ? pos : end - 1, end - 1), most = (seen == 0 ? -1 : seen) - j0;
 #pragma unroll
                         for (int i = 0; i < 16; ++i) ds[0][i] = row_of(i, half) <= most ? ds[0][i] : 0.f;
                     }
@@ -318,7 +320,7 @@ __global__ __launch_bounds__(THREADS, sizeof(T) == 2 && !SHARED ? 2 : 1) void k_
                         if (!any_not_finite<T>(keys + (long long)j0 * a.k.row, a.k.row, count, a.D)) continue;
 #pragma unroll 1
                         for (int j = j0; j < j0 + count; ++j) {
-                            if (j > pos || !there) continue;
+                            if (j > pos || pos == 0 || !there) continue;       // (pos 0: one key alone)
                             const char *const key = keys + (long long)j * a.k.row;
                             float x = dot<T>(mine, key, a.D) * a.scale2;
                             if constexpr (BIAS) x += bias_at(a, head, j - pos);
@@ -355,7 +357,8 @@ __global__ __launch_bounds__(THREADS, sizeof(T) == 2 && !SHARED ? 2 : 1) void k_
             tile::meet();
             // Several threads to a bucket where there are few: a wide one has a hundred numbers to add, which short sequences wait for (100 samples of 1
             // to 512 tokens, 8 heads of 64, a training step: 184 us; with one thread to a bucket 197).
-            const int parts = all <= 32 ? 8 : all <= 64 ? 4 : all <= 128 ? 2 : 1, c = tid / parts, k = tid % parts;
+            // (The thread's number is looked at anew: kept from fill_bias() on, it would be a register that the compiler has to put somewhere all the while.)
+            const int parts = all <= 32 ? 8 : all <= 64 ? 4 : all <= 128 ? 2 : 1, me = opaque(tid), c = me / parts, k = me % parts;
             float sum = 0.f;
             if (c < all) {
                 const int in = c < buckets ? c : c - buckets, sign = c < buckets ? -1 : 1;
@@ -549,12 +552,13 @@ template <typename T, int DP, bool SHARED, bool BIAS, bool DIRECT> __global__ __
                             p[0][4 * f + e] = __builtin_amdgcn_exp2f(BIAS ? (x - from[e]) - log_sum[e] : fmaf(x, a.scale2, -from[e]));
                         }
                     }
-                    auto hide = [&](f32x16 &x) {
+                    // least: the first position whose query sees this lane's key
+                    auto hide = [&](f32x16 &x, int least) {
 #pragma unroll
-                        for (int i = 0; i < 16; ++i) x[i] = key <= p0 + row_of(i, half) ? x[i] : 0.f;
+                        for (int i = 0; i < 16; ++i) x[i] = least <= p0 + row_of(i, half) ? x[i] : 0.f;
                     };
                     if constexpr (W::TIGHT) {
-                        if (edge) hide(p[0]);
+                        if (edge) hide(p[0], key);
                         if (!skip) weigh<T, DP, 1>(reader, gtile, rb, p, dv[0]);
                         __builtin_amdgcn_sched_barrier(0);
                         struct Pair {
@@ -572,8 +576,8 @@ template <typename T, int DP, bool SHARED, bool BIAS, bool DIRECT> __global__ __
                         for (int e = 0; e < 4; ++e) ds[0][4 * f + e] = p[0][4 * f + e] * (ds[0][4 * f + e] - delta[e]);
                     }
                     if (edge) {
-                        if (!W::TIGHT) hide(p[0]);
-                        hide(ds[0]);
+                        if (!W::TIGHT) hide(p[0], key);
+                        hide(ds[0], max(key, 1));           // (position 0 sees one key alone: its ds is nothing, as in k_attention_dq)
                     }
                     if (!skip) {
                         if (!W::TIGHT) weigh<T, DP, 1>(reader, gtile, rb, p, dv[0]);
@@ -670,6 +674,7 @@ template <typename T, int DP, bool SHARED, bool BIAS, bool DIRECT> __global__ __
 #pragma unroll 1
                             for (int i = 0; i < n; ++i) {
                                 if (key > shift + i0 + i || !there) continue;
+                                if (!of_v && shift + i0 + i == 0) continue;         // (one key alone)
                                 const char *const row_q = pq + (long long)i * a.q.row, *const row_g = pg + (long long)i * a.dout.row;
                                 const float *const fact = a.stats + (long long)h * a.q_all + seq.q_first + i0 + i;
                                 float x = dot<T>(row_q, mine, a.D) * a.scale2;
@@ -688,14 +693,14 @@ template <typename T, int DP, bool SHARED, bool BIAS, bool DIRECT> __global__ __
             const long long place = ((split * a.k_all + seq.k_first + key) * a.kv_heads + kv_head) * a.D;
             constexpr int GROUPS = SHARED ? R::BLOCKS : 4 * R::BLOCKS;
             const int first = (SHARED ? 8 * wave * R::BLOCKS : 0) + 4 * half;
-            auto store = [&](const Heads &to, float *parts, float scale, f32x16 (&acc)[R::BLOCKS]) {
+            auto store = [&](const Heads &to, float *parts, float scale, bool zeros, f32x16 (&acc)[R::BLOCKS]) {
                 if constexpr (SHARED) add_waves<R::BLOCKS>(lds, acc);
                 if (!stored) return;
-                if (a.splits > 1) store_row<float, R::BLOCKS, GROUPS, DIRECT>(parts + place, first, a.D, 1.f, true, acc);
-                else store_row<T, R::BLOCKS, GROUPS, DIRECT>(reinterpret_cast<T *>(rows_of(to, b, k_ragged, seq.k0 + key, kv_head)), first, a.D, scale, there, acc);
+                if (a.splits > 1) store_row<float, R::BLOCKS, GROUPS, DIRECT>(parts + place, first, a.D, 1.f, !zeros, acc);
+                else store_row<T, R::BLOCKS, GROUPS, DIRECT>(reinterpret_cast<T *>(rows_of(to, b, k_ragged, seq.k0 + key, kv_head)), first, a.D, scale, there && !zeros, acc);
             };
-            store(a.dk, a.part_k, a.scale, dk[0]);
-            store(a.dv, a.part_v, 1.f, dv[0]);
+            store(a.dk, a.part_k, a.scale, seq.k_len == 1, dk[0]);          // (a key that is alone: every weight of it is 1)
+            store(a.dv, a.part_v, 1.f, false, dv[0]);
             tile::wait_loads<0>();
             tile::wait_lds();
             tile::meet();
