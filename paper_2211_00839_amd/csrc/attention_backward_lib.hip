@@ -101,8 +101,10 @@ int rcd_attention_backward(const rcd_attention_shape *s, const rcd_heads *dout, 
 {
     hipStream_t stream = (hipStream_t)stream_;
     ENC_TRY(check_shape(s));
-    for (const rcd_heads *h : {dout, q, out, dq}) ENC_TRY(check_heads(h, s->q_rows, s->batch, s->dt));
-    for (const rcd_heads *h : {k, v, dk, dv}) ENC_TRY(check_heads(h, s->k_rows, s->batch, s->dt));
+    for (const rcd_heads *h : {dout, q, out}) ENC_TRY(check_heads(h, s->q_rows, s->batch, s->dt));
+    for (const rcd_heads *h : {k, v}) ENC_TRY(check_heads(h, s->k_rows, s->batch, s->dt));
+    ENC_TRY(check_result(dq, s->q_rows, s->batch, s->dt, clear != 0, s->q_offsets_dev));
+    for (const rcd_heads *h : {dk, dv}) ENC_TRY(check_result(h, s->k_rows, s->batch, s->dt, clear != 0, s->k_offsets_dev));
     if (!saved_dev && s->q_rows > 0 && s->batch > 0) return RCD_ERR_INVALID_ARG;
     if (dbias_dev && !s->bias_dev) return RCD_ERR_INVALID_ARG;
     Args a = args_of(*s);
@@ -122,7 +124,7 @@ int rcd_attention_backward(const rcd_attention_shape *s, const rcd_heads *dout, 
     const bool causal = s->causal != 0;
     const Way way = dq_way(*s);
     bool packed = false;            // the gradient of q's workgroups were counted over all sequences' tiles
-    if (s->q_rows > 0 && s->batch > 0) {
+    if (works_on(s->q_rows, s->batch, a.clear, s->q_offsets_dev)) {
         Args x = a;
         x.tiles = (int)way.tiles;
         if (!dbias_dev) x.part_bias = nullptr;
@@ -147,7 +149,7 @@ int rcd_attention_backward(const rcd_attention_shape *s, const rcd_heads *dout, 
             hipLaunchKernelGGL((k_bias_gradient<__bf16>), grid, dim3(THREADS), 0, stream, a.part_bias, count, (int)s->buckets, (int)s->heads, (__bf16 *)dbias_dev);
         ENC_HIP_TRY(hipGetLastError());
     }
-    if (s->k_rows > 0 && s->batch > 0) {
+    if (works_on(s->k_rows, s->batch, a.clear, s->k_offsets_dev)) {
         const KvWay kv = dkv_way(*s);
         a.tiles = (int)kv.tiles;
         a.splits = (int)kv.parts;

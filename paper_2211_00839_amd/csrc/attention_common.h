@@ -173,7 +173,10 @@ template <int THREADS_, typename Count> __device__ __forceinline__ bool tile_of(
         tile::meet();
         if (slot < before) break;
     }
-    if (batch == 0) tile::meet();
+    if (batch == 0) {
+        tile::wait_lds();
+        tile::meet();
+    }
     const int b = uniform(found[0]);
     *tile = b < 0 ? uniform(before) : uniform(found[1]);
     *tiles = uniform(found[2]);

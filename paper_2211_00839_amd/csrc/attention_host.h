@@ -81,6 +81,14 @@ int check_heads(const rcd_heads *h, int64_t rows, int64_t batch, int dt)
     return RCD_OK;
 }
 
+// Results of a call without sequences: there is a kernel all the same where rows that belong to none are to become zeros.
+bool works_on(int64_t rows, int64_t batch, bool clear, const int32_t *offsets) { return rows > 0 && (batch > 0 || (clear && offsets)); }
+int check_result(const rcd_heads *h, int64_t rows, int64_t batch, int dt, bool clear, const int32_t *offsets)
+{
+    ENC_TRY(check_heads(h, rows, batch, dt));
+    return works_on(rows, batch, clear, offsets) && !h->p ? RCD_ERR_INVALID_ARG : RCD_OK;
+}
+
 Heads heads_of(const rcd_heads *h, int dt)
 {
     const long long e = size_of(dt);

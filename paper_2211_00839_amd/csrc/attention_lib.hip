@@ -57,8 +57,8 @@ int rcd_attention(const rcd_attention_shape *s, const rcd_heads *q, const rcd_he
     ENC_TRY(check_heads(q, s->q_rows, s->batch, s->dt));
     ENC_TRY(check_heads(k, s->k_rows, s->batch, s->dt));
     ENC_TRY(check_heads(v, s->k_rows, s->batch, s->dt));
-    ENC_TRY(check_heads(out, s->q_rows, s->batch, s->dt));
-    if (s->q_rows == 0 || s->batch == 0) return RCD_OK;
+    ENC_TRY(check_result(out, s->q_rows, s->batch, s->dt, clear != 0, s->q_offsets_dev));
+    if (!works_on(s->q_rows, s->batch, clear != 0, s->q_offsets_dev)) return RCD_OK;
     const attn_rules::Cut c = forward_cut(*s);
     Args a = args_of(*s);
     ENC_TRY(check_workspace(workspace_dev, workspace_bytes, forward_bytes(*s, c, workspace_dev, &a)));
