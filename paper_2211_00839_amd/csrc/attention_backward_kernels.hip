@@ -471,7 +471,7 @@ template <typename T, int DP, bool SHARED, bool BIAS, bool DIRECT> __global__ __
                     if (!SHARED && wave != f) continue;
                     const int plane = !BIAS ? f : f == 0 ? 2 : f == 1 ? 1 : 3;
                     const float *from = a.stats + plane * a.plane + (long long)head * a.q_all + seq.q_first + i0;
-                    if (lane < W::KV_TILE) bring4(uniform(from), min(lane, seq.q_len - 1 - i0) * 4, facts_addr + (buf * W::FACTS_STAGE + f * W::KV_TILE) * 4);
+                    if (lane < W::KV_TILE) tile::load4_to_lds(uniform(from), min(lane, seq.q_len - 1 - i0) * 4, facts_addr + (buf * W::FACTS_STAGE + f * W::KV_TILE) * 4);
                 }
             };
             // A tile that has come; rows that are not there become zeros with weights of zero.

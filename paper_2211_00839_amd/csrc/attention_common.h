@@ -277,30 +277,12 @@ template <typename T, bool WHOLE> __device__ __forceinline__ void store4(T *p, i
         if (i < count) p[i] = (T)v[i];
 }
 
-// 16 or 4 bytes of each lane to LDS.  The base may have been put into its scalar registers by a vector instruction right before (a register that
-// was held in a lane of another one comes back so), which a memory instruction may follow only after five wait states; the compiler does
-// not see into the asm and puts none there.
+// An address that is the same in all lanes, for loads that take it from scalar registers.
 __device__ __forceinline__ const void *uniform(const void *p)
 {
     const unsigned long long x = (unsigned long long)p;
     const unsigned lo = __builtin_amdgcn_readfirstlane((unsigned)x), hi = __builtin_amdgcn_readfirstlane((unsigned)(x >> 32));
     return (const void *)(((unsigned long long)hi << 32) | lo);
-}
-__device__ __forceinline__ void bring16(const void *base, unsigned offset, unsigned lds_addr)
-{
-    asm volatile("s_nop 4\n\t"
-                 "global_load_lds_dwordx4 %0, %1"
-                 :
-                 : "v"(offset), "s"(base), "{m0}"(lds_addr)
-                 : "memory");
-}
-__device__ __forceinline__ void bring4(const void *base, unsigned offset, unsigned lds_addr)
-{
-    asm volatile("s_nop 4\n\t"
-                 "global_load_lds_dword %0, %1"
-                 :
-                 : "v"(offset), "s"(base), "{m0}"(lds_addr)
-                 : "memory");
 }
 
 // Brings ROWS rows of a matrix to LDS, LOADERS threads together, each always the same places of a tile.  DIRECT: straight from memory (all rows
@@ -336,12 +318,12 @@ template <typename T, int DP, int ROWS, int LOADERS, bool DIRECT> struct Loader 
             base = (const char *)uniform(base);
             if (rows >= ROWS) {
 #pragma unroll
-                for (int u = 0; u < N; ++u) bring16(base, off[u % KINDS] + (unsigned)(u * STEP * pitch), lds_addr + (u * LOADERS + wave * 64) * 16);
+                for (int u = 0; u < N; ++u) tile::load16_to_lds(base, off[u % KINDS] + (unsigned)(u * STEP * pitch), lds_addr + (u * LOADERS + wave * 64) * 16);
             } else {
 #pragma unroll
                 for (int u = 0; u < N; ++u) {
                     const int back = min(rows - 1 - row - u * STEP, 0);         // (to the last row there is)
-                    bring16(base, off[u % KINDS] + (unsigned)((u * STEP + back) * pitch), lds_addr + (u * LOADERS + wave * 64) * 16);
+                    tile::load16_to_lds(base, off[u % KINDS] + (unsigned)((u * STEP + back) * pitch), lds_addr + (u * LOADERS + wave * 64) * 16);
                 }
             }
         } else {

@@ -7,10 +7,12 @@ namespace tile {
 
 typedef short s16x4 __attribute__((ext_vector_type(4)));
 
-// (M0 holds the LDS address; the instruction may follow M0's write only after a wait state)
+// 16 or 4 bytes of each lane, from a base that all lanes share.  M0 holds the LDS address; the instruction may follow M0's write only after a wait
+// state, and the base's by five where a vector instruction wrote it: a register that was held in a lane of another one comes back so, and the
+// compiler, which does not see into the asm, puts nothing between.  s_nop 4 is five.
 __device__ __forceinline__ void load16_to_lds(const void *base, unsigned offset, unsigned lds_addr)
 {
-    asm volatile("s_nop 0\n\t"
+    asm volatile("s_nop 4\n\t"
                  "global_load_lds_dwordx4 %0, %1"
                  :
                  : "v"(offset), "s"(base), "{m0}"(lds_addr)
@@ -18,7 +20,7 @@ __device__ __forceinline__ void load16_to_lds(const void *base, unsigned offset,
 }
 __device__ __forceinline__ void load4_to_lds(const void *base, unsigned offset, unsigned lds_addr)
 {
-    asm volatile("s_nop 0\n\t"
+    asm volatile("s_nop 4\n\t"
                  "global_load_lds_dword %0, %1"
                  :
                  : "v"(offset), "s"(base), "{m0}"(lds_addr)
