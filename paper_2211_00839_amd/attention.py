@@ -85,7 +85,7 @@ def attention_backward(dout, q, k, v, out, saved, scale=None, causal: bool = Fal
                        longest_q: int = 0, longest_k: int = 0, bias=None, max_distance: int = 128, want_dbias: bool = True,
                        grads=None, workspace=None) -> AttentionGrads:
     """The gradients of attention's q, k, v and bias; out and saved are what it returned, the other arguments what it was given.
-    grads: (dq, dk, dv) to write to; their rows that belong to no sequence are left (zeros in new ones)."""
+    grads: (dq, dk, dv) to write to, which share no elements with the rest; their rows that belong to no sequence are left (zeros in new ones)."""
     dq, dk, dv = (None, None, None) if grads is None else grads
     return AttentionGrads._make(_lib().attention_backward(
         dout, q, k, v, out, saved, q_offsets, k_offsets, k_lengths, longest_q, longest_k, scale, causal, bias,

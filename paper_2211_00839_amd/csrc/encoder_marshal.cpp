@@ -12,10 +12,12 @@
 
 #include <algorithm>
 #include <cmath>
+#include <initializer_list>
 #include <string>
 #include <utility>
 
 #include "../../include/rcd.h"
+#include "overlap.h"
 
 namespace {
 
@@ -512,7 +514,7 @@ struct Call {
     rcd_attention_shape s{};
     Rows q, k, v;
     at::ScalarType type;
-    const at::Tensor *bias = nullptr;
+    const at::Tensor *bias = nullptr, *q_offsets = nullptr, *k_offsets = nullptr, *k_lengths = nullptr;
 };
 Call attention_call(PyObject *q, PyObject *k, PyObject *v, PyObject *const *a)
 {
@@ -532,6 +534,9 @@ Call attention_call(PyObject *q, PyObject *k, PyObject *v, PyObject *const *a)
     if ((!q_ragged && c.q.batch != c.s.batch) || (!k_ragged && c.k.batch != c.s.batch)) refuse("q and k must have the same number of sequences");
     if (k_ragged && a[2] != Py_None) refuse("k_lengths go without k_offsets");
     c.s.k_lengths_dev = indices("k_lengths", a[2], 0, c.s.batch, like, nullptr);
+    c.q_offsets = tensor(a[0]);
+    c.k_offsets = tensor(a[1]);
+    c.k_lengths = tensor(a[2]);
     c.s.longest_q = number(a[3]);
     c.s.longest_k = number(a[4]);
     if (c.s.longest_q < 0 || c.s.longest_k < 0) refuse("longest_q and longest_k must not be negative");
@@ -588,11 +593,30 @@ Made made(const char *name, PyObject *given, const Rows &as, const Call &c)
     if (!m.t.is_inference()) m.t.unsafeGetTensorImpl()->bump_version();
     return m;
 }
-// A result that begins where an operand or another result does would be read while it is written.  (That they share no element further on is the
-// caller's part: results may well lie between operands' rows.)
-template <typename... T> void apart(const char *name, const Made &m, const T &...others)
+overlap::Array places(const at::Tensor &t)
 {
-    if (m.t.numel() > 0 && ((others.h.p == m.h.p) || ...)) refuse(std::string(name) + " is an operand or another result too");
+    overlap::Array a;
+    const int64_t dims = t.dim(), e = t.element_size();
+    a.p = reinterpret_cast<uintptr_t>(t.data_ptr());
+    if (t.is_contiguous()) {
+        a.run = t.numel() * e;
+        return a;
+    }
+    a.run = t.size(dims - 1) * e;               // (the last dimension of everything here is contiguous)
+    for (int64_t i = 0; i + 1 < dims; ++i) a.dim(t.stride(i) * e, t.size(i));
+    return a;
+}
+// A result that shares elements with an operand or another result would be read, or written again, while it is written.  (Where thousands of steps do
+// not settle it, which the views of one buffer never take, it is the caller's part.)
+void apart(const char *name, const Made &m, std::initializer_list<const at::Tensor *> others, const Room &ws, size_t need)
+{
+    const overlap::Array mine = places(m.t);
+    overlap::Array used;
+    used.p = reinterpret_cast<uintptr_t>(ws.p);
+    used.run = (int64_t)std::min(need, ws.bytes);
+    bool shared = overlap::of(mine, used) == overlap::SHARED;
+    for (const at::Tensor *o : others) shared = shared || (o && overlap::of(mine, places(*o)) == overlap::SHARED);
+    if (shared) refuse(std::string(name) + " shares elements with an operand, another result or the workspace");
 }
 Room room(PyObject *o, size_t need, const at::Tensor &like)
 {
@@ -608,14 +632,15 @@ PyObject *attention(PyObject *, PyObject *const *a, Py_ssize_t n)
     expect(n, 16);
     const Call c = attention_call(a[0], a[1], a[2], a + 3);
     const Made out = made("out", a[12], c.q, c);
-    apart("out", out, c.q, c.k, c.v);
     at::Tensor saved;
     if (truth(a[13])) {
         auto sizes = c.q.t->sizes().vec();
         sizes.back() = 2;
         saved = at::empty(sizes, c.q.t->options().dtype(at::kFloat).requires_grad(false));
     }
-    const Room ws = room(a[14], rcd_attention_workspace_bytes(&c.s), *c.q.t);
+    const size_t need = rcd_attention_workspace_bytes(&c.s);
+    const Room ws = room(a[14], need, *c.q.t);
+    if (a[12] != Py_None) apart("out", out, {c.q.t, c.k.t, c.v.t, c.bias, c.q_offsets, c.k_offsets, c.k_lengths}, ws, need);
     void *const on = stream(a[15]);
     const int clear = a[12] == Py_None;
     run([&] { return rcd_attention(&c.s, &c.q.h, &c.k.h, &c.v.h, &out.h, (float *)p(saved), clear, ws.p, ws.bytes, on); });
@@ -643,12 +668,16 @@ PyObject *attention_backward(PyObject *, PyObject *const *a, Py_ssize_t n)
     const int given = (a[15] != Py_None) + (a[16] != Py_None) + (a[17] != Py_None);
     if (given != 0 && given != 3) refuse("grads must be (dq, dk, dv)");
     const Made dq = made("dq", a[15], c.q, c), dk = made("dk", a[16], c.k, c), dv = made("dv", a[17], c.v, c);
-    apart("dq", dq, dk, dv, dout, c.q, c.k, c.v, out);
-    apart("dk", dk, dv, dout, c.q, c.k, c.v, out);
-    apart("dv", dv, dout, c.q, c.k, c.v, out);
     at::Tensor dbias;
     if (c.bias && truth(a[18])) dbias = at::empty(c.bias->sizes(), c.bias->options().requires_grad(false));
-    const Room ws = room(a[19], rcd_attention_backward_workspace_bytes(&c.s), *c.q.t);
+    const size_t need = rcd_attention_backward_workspace_bytes(&c.s);
+    const Room ws = room(a[19], need, *c.q.t);
+    if (given) {
+        for (const auto &[name, made] : {std::pair("dq", &dq), std::pair("dk", &dk), std::pair("dv", &dv)})
+            apart(name, *made, {dout.t, c.q.t, c.k.t, c.v.t, out.t, saved, c.bias, c.q_offsets, c.k_offsets, c.k_lengths}, ws, need);
+        apart("dq", dq, {&dk.t, &dv.t}, ws, need);
+        apart("dk", dk, {&dv.t}, ws, need);
+    }
     void *const on = stream(a[20]);
     run([&] {
         return rcd_attention_backward(&c.s, &dout.h, &c.q.h, &c.k.h, &c.v.h, &out.h, (const float *)saved->data_ptr(), &dq.h, &dk.h, &dv.h, p(dbias),
