@@ -442,10 +442,12 @@ size_t rcd_gated_linear_backward_workspace_bytes(int64_t M, int64_t F, int64_t K
  * Query i of a sequence of n queries and m keys stands at the position pos_i = i + m - n (its queries are the last n of its keys), whether
  * causal (keys j > pos_i are masked) or not.  A query that sees no key, by its mask, an empty sequence or a bias of -infinity throughout,
  * gets zeros, and no gradient goes through it.  What is masked has no part in anything: a NaN in a key or value that a query does not see
- * does not reach it, and rows behind a sequence are not read.  Where a key that is seen holds an infinity, its scores may come out NaN.
+ * does not reach it, and rows behind a sequence are not read.  Where a key that is seen holds an infinity, its scores may come out NaN.  A bias of
+ * -infinity is added like any other: it takes the weight of a score that is a number, and zero times a value that is not one stays NaN.
  *
  *   dt                  RCD_F32 or RCD_BF16, of every matrix.  Scores, statistics and sums are fp32; for RCD_BF16 p and its gradient are
- *                       rounded to bf16 on their way into the second product (2^-9 of each, what v, k and q have lost already)
+ *                       rounded to bf16 on their way into the second product (half a step, 2^-8 of each at most, as v, k and q were),
+ *                       and the gradients' delta is made of out as it was stored
  *   heads, kv_heads     heads is a multiple of kv_heads: head h of q goes with head h / (heads / kv_heads) of k and v.  d: 1 .. 128
  *   q_rows, k_rows      rows of each of `batch` sequences, whose places are their strides rcd_heads.batch; or with q_offsets_dev, k_offsets_dev
  *                       (int32[batch + 1], not decreasing) rows of all of them one after the other, sequence b from offset b up to offset

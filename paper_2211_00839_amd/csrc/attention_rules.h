@@ -59,7 +59,9 @@ inline Cut cut_of(int64_t batch, int64_t heads, int64_t group, int64_t longest_q
     Cut c{};
     c.pack = group > 1 && longest_q * group <= 64 && q_rows * group <= ((int64_t)1 << 29) && width * group <= 7168 ? (int)group : 1;
     const int64_t across = batch * (heads / c.pack), most = units_of(batch, heads / group) * (group / c.pack);
-    // (fp32: a compute unit has room for one workgroup of 128 rows, so that 257 of them take as long as 512: 320 of the above 160 us, shared 127; 512: 162, 200)
+    // (fp32: a compute unit has room for one workgroup of 128 rows, so that 257 of them take as long as 512.  1024 rows of 64, us shared / 128 rows, by
+    // workgroups of 128 rows: 320: 127 / 160, 384: 151 / 159, 400: 174 / 159, 512: 200 / 162, 520: 220 / 234, 576: 226 / 238, 592: 246 / 238, 640: 249 / 238, 752: 297 / 239,
+    // 776: 318 / 312, 792: 319 / 313, 832: 322 / 317: the rule is 3 percent off at most, just under 600 and 800.)
     const int64_t rounds = ceil_div(across * ceil_div(longest_q * c.pack, 128), 256);
     c.shared = shared_rows(across, longest_q * c.pack, f32 ? FEW_WORKGROUPS * std::max<int64_t>(rounds, 1) : FEW_WORKGROUPS_BF16_FORWARD);
     c.tiles = tiles_of(most, longest_q * c.pack, c.shared);
